@@ -15,6 +15,10 @@
  *   local_adamw_step   AdamW inner optimiser             (Section 4.2, Appendix C.2)
  *   local_shb_step     momentum-SGD inner optimiser      (Section 6.1)
  *   replica_average    x^m <- (1/M) sum_m x^m            (Eq. local_sgd_alt, line 2)
+ *   local_muon_step    orthogonalised-momentum (Muon) inner optimiser for matrices
+ *   abs_layer_norm, abs_layer_norm_backward
+ *                      layer norm; its backward pass also gives per-sample gradient
+ *                      rows of weight and bias for the test
  *
  * Conventions
  *   - Every function returns an int: ABS_OK (0) or a negative ABS_ERR_* code.
@@ -325,6 +329,61 @@ int local_shb_step(abs_ctx* ctx, float* X, float* Buf, const float* Gb, int M, l
                    long long replica_stride, float lr, float momentum, float weight_decay,
                    int average_after, void* stream);
 
+/* ---- orthogonalisation and the Muon step ---------------------------------------------------
+ * Newton-Schulz iteration towards the orthogonal polar factor of a matrix: from
+ *   X_0 = G / ( ||G||_F + eps )
+ * each step applies, with A = X X' (X' X for a matrix taller than wide),
+ *   X <- a X + (b A + c A^2) X,
+ * i.e. p(s) = a s + b s^3 + c s^5 to every singular value.  (3.4445, -4.7750, 2.0315)
+ * with 5 steps is the choice users of Muon make; (1.5, -0.5, 0) is the classical cubic.  */
+typedef enum {
+  ABS_NS_F16 = 0,       /* operands of the products rounded to 11 bits (fp16), X carried with 22 bits:
+                           result within about 2e-3 (normwise) of the exact iteration                  */
+  ABS_NS_F32 = 1        /* operands of 22 bits, three products each: fp32-grade                         */
+} abs_ns_precision;
+
+typedef struct {
+  float a, b, c;        /* finite; ABS_ERR_UNSUPPORTED if they let singular values pass 1024            */
+  float eps;            /* >= 0; a zero matrix gives a zero result for eps > 0, NaN for eps = 0          */
+  int steps;            /* 1..32                                                                         */
+  int precision;        /* abs_ns_precision                                                              */
+} abs_ns_cfg;           /* 24 bytes */
+
+/* Bytes of device scratch that abs_orthogonalise (count matrices) or local_muon_step
+ * (count = M * matrices) needs; matrices are worked on in groups, so this stays near
+ * 100 MB however many there are.  cfg is a HOST pointer; needs no context.           */
+int abs_ns_scratch_bytes(int count, long long rows, long long cols, const abs_ns_cfg* cfg, size_t* out);
+
+/* O[q] = the iterate after cfg->steps steps from G[q], q < count.  Element (q, r, c) of G at
+ * G[q*g_matrix_stride + r*g_row_stride + c], row strides >= cols, matrices disjoint (strides of
+ * count == 1 are ignored).  fp32 or bf16 in and out.  O may be G (same type and strides).
+ * rows, cols <= 65536.  A non-finite entry makes its matrix NaN, no other.  If a wait inside a
+ * product runs out (the "stats_timeout_cycles" key), the results are NaN.                         */
+int abs_orthogonalise(abs_ctx* ctx, const void* G, abs_dtype g_dtype, int count, long long rows, long long cols,
+                      long long g_row_stride, long long g_matrix_stride, void* O, abs_dtype o_dtype,
+                      long long o_row_stride, long long o_matrix_stride, const abs_ns_cfg* cfg, void* scratch,
+                      size_t scratch_bytes, void* stream);
+
+typedef struct {
+  float lr, momentum, weight_decay;
+  float scale;          /* factor on the orthogonalised update: sqrt(max(1, rows/cols)), or
+                           0.2 sqrt(max(rows, cols)) to match the update size of AdamW                  */
+  int nesterov;
+  int reserved;         /* zero */
+  abs_ns_cfg ns;
+} abs_muon_cfg;         /* 48 bytes */
+
+/* Local Muon step for all replicas of `matrices` equal-shaped parameter matrices:
+ *   u <- momentum u + g ;  v = nesterov ? g + momentum u : u
+ *   x <- x (1 - lr wd) - lr scale O(v),  O as in abs_orthogonalise, matrix by matrix
+ * Matrix l of replica m is [rows][cols], contiguous, at + m*replica_stride + l*matrix_stride in X,
+ * Buf (the momentum u) and Gb, all fp32 (so the matrices may lie inside flat parameter vectors).
+ * average_after != 0: X[m] <- mean over replicas of the updated X; the momentum stays local.
+ * cfg is a HOST pointer.  The result of a step whose products ran out of time is NaN.            */
+int local_muon_step(abs_ctx* ctx, float* X, float* Buf, const float* Gb, int M, int matrices, long long rows,
+                    long long cols, long long matrix_stride, long long replica_stride, const abs_muon_cfg* cfg,
+                    int average_after, void* scratch, size_t scratch_bytes, void* stream);
+
 /* Model averaging (Eq. local_sgd_alt, second line; Algorithm 1 "update the
  * global model"): every replica receives (1/M) sum_m X[m], in place.            */
 int replica_average(abs_ctx* ctx, float* X, int M, long long d, long long replica_stride,
@@ -462,6 +521,39 @@ int abs_logreg_rounds_fused_opts(abs_ctx* ctx, const float* A, const float* y, l
                                  int H, float lr, const abs_test_cfg* cfg, const abs_round_opts* opts,
                                  abs_stats* stats, long long* T_out, long long* b_hist,
                                  long long* b_dev, void* stream);
+
+/* ---- layer norm ---------------------------------------------------------------------------
+ * Rows of d features, fp32 or bf16, for M replicas with parameters of their own (fp32):
+ *   mean = (1/d) sum_j x_j,  rstd = 1 / sqrt( (1/d) sum_j (x_j - mean)^2 + eps ),
+ *   y_j = (x_j - mean) rstd weight_j + bias_j
+ *   X, Y        row r of replica m at + m*worker_stride + r*row_stride (>= d; replicas disjoint;
+ *               the worker strides are ignored for M == 1).  Y may be X (same strides).
+ *   weight, bias  replica m at + m*param_stride (0: all replicas share them), or NULL (ones / zeros)
+ *   mean, rstd  [M][rows] fp32 for the backward pass, or NULL
+ *   rows may be 0.  Statistics are fp32 from values held in registers or read twice: the
+ *   variance is that of centred values, and y is rounded once.                              */
+int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int M, long long rows, long long d,
+                   long long x_row_stride, long long x_worker_stride, const float* weight, const float* bias,
+                   long long param_stride, float eps, void* Y, long long y_row_stride, long long y_worker_stride,
+                   float* mean, float* rstd, void* stream);
+
+/* Its backward pass.  A replica's rows are `samples` samples of `tokens` consecutive rows.  With
+ * xh = (x - mean) rstd and a = weight dy:
+ *   dx = rstd ( a - (1/d) sum_j a_j - xh (1/d) sum_j a_j xh_j )
+ *   per-sample gradients (Algorithm 1, per-sample gradient step), sums over the sample's rows:
+ *     Gw[i] = sum_t dy xh,  Gb[i] = sum_t dy     at + m*g_worker_stride + i*g_row_stride
+ *   and their sums over the samples, dW, dB, at + m*grad_stride.
+ * dX, dW, dB, Gw, Gb may each be NULL.  Gw and Gb may be two parts of one row, as abs_test_stats
+ * takes them.  dX may be dY or X (same strides).  samples and tokens may be 0 (sums of nothing
+ * are zero).  mean, rstd: [M][samples*tokens] as the forward pass wrote them.  All sums are fp32
+ * in a fixed order: repeated calls give the same bits.
+ * ABS_ERR_WORKSPACE if the context's workspace cannot hold one partial sum per replica.       */
+int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long dy_row_stride, long long dy_worker_stride,
+                            const void* X, long long x_row_stride, long long x_worker_stride, abs_dtype dtype, int M,
+                            long long samples, long long tokens, long long d, const float* mean, const float* rstd,
+                            const float* weight, long long param_stride, void* dX, long long dx_row_stride,
+                            long long dx_worker_stride, float* dW, float* dB, long long grad_stride, float* Gw,
+                            float* Gb, long long g_row_stride, long long g_worker_stride, void* stream);
 
 /* Three-layer ReLU MLP with softmax cross-entropy (the second synthetic problem).
  * dims = {n0, n1, n2, n3} layer widths.  One replica's parameters are a flat fp32

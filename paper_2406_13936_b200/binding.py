@@ -50,6 +50,16 @@ class RoundOpts(ctypes.Structure):
                 ("ctl", ctypes.c_void_p)]
 
 
+class NsCfg(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float),
+                ("steps", ctypes.c_int), ("precision", ctypes.c_int)]
+
+
+class MuonCfg(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("scale", ctypes.c_float), ("nesterov", ctypes.c_int), ("reserved", ctypes.c_int), ("ns", NsCfg)]
+
+
 class StatsPlan(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in
                 ("route", "lanes_per_row", "warps_per_box", "boxes_per_stage", "stages", "box_rows", "row_boxes",
@@ -131,6 +141,25 @@ EXPORTS = {
                        ctypes.c_int, ctypes.c_void_p],
     "replica_average": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong,
                         ctypes.c_void_p],
+    "abs_ns_scratch_bytes": [ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.POINTER(NsCfg),
+                             ctypes.POINTER(ctypes.c_size_t)],
+    "abs_orthogonalise": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_longlong,
+                          ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_int,
+                          ctypes.c_longlong, ctypes.c_longlong, ctypes.POINTER(NsCfg), ctypes.c_void_p,
+                          ctypes.c_size_t, ctypes.c_void_p],
+    "local_muon_step": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
+                        ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
+                        ctypes.POINTER(MuonCfg), ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+    "abs_layer_norm": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_longlong,
+                       ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p,
+                       ctypes.c_longlong, ctypes.c_float, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
+                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
+    "abs_layer_norm_backward": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p,
+                                ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_longlong,
+                                ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
+                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p,
+                                ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p],
 }
 
 _lib = None
@@ -298,6 +327,144 @@ class Context:
         self._check(self._lib.local_shb_step(self._h, _ptr(X2), _ptr(Buf), _ptr(Gb), M, d, stride, float(lr),
                                              float(momentum), float(weight_decay), int(bool(average_after)),
                                              _stream(stream)), "local_shb_step")
+
+    # ---- orthogonalisation and the Muon step -------------------------------------------------
+    def ns_scratch(self, count, rows, cols, cfg):
+        """Device scratch tensor (uint8) for abs_orthogonalise / local_muon_step on `count` matrices."""
+        out = ctypes.c_size_t()
+        rc = self._lib.abs_ns_scratch_bytes(int(count), int(rows), int(cols), ctypes.byref(cfg), ctypes.byref(out))
+        if rc != 0:
+            raise AbsError("abs_ns_scratch_bytes failed (%d): %s" % (rc, self._lib.abs_last_error(None).decode()))
+        return torch.empty(out.value, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def abs_orthogonalise(self, G, O, cfg, scratch, stream=None):
+        """G, O: [count, rows, cols] or [rows, cols] device tensors (fp32 or bf16, last dim contiguous; O may be
+        G); cfg from make_ns_cfg; scratch from ns_scratch(count, rows, cols, cfg)."""
+        if G.dim() == 2:
+            G = G.unsqueeze(0)
+        if O.dim() == 2:
+            O = O.unsqueeze(0)
+        if G.shape != O.shape or G.dim() != 3:
+            raise AbsError("G and O must be matrices of the same shape, got %s and %s" % (tuple(G.shape), tuple(O.shape)))
+        count, rows, cols = G.shape
+        g_row, g_mat = self._matrix_strides(G)
+        o_row, o_mat = self._matrix_strides(O)
+        self._check(self._lib.abs_orthogonalise(self._h, _ptr(G), _dtype_code(G), count, rows, cols, g_row, g_mat, _ptr(O),
+                                                _dtype_code(O), o_row, o_mat, ctypes.byref(cfg), _ptr(scratch),
+                                                scratch.numel(), _stream(stream)), "abs_orthogonalise")
+        return O
+
+    @staticmethod
+    def _matrix_strides(G):
+        """(row stride, matrix stride) of [count, rows, cols]; the strides of dimensions of one element are free."""
+        count, rows, cols = G.shape
+        if G.stride(2) != 1 and cols > 1:
+            raise AbsError("the last dimension of a matrix must be contiguous")
+        row = G.stride(1) if rows > 1 else cols
+        return row, G.stride(0) if count > 1 else row * rows
+
+    def local_muon_step(self, X, Buf, Gb, cfg, scratch, average_after=False, stream=None):
+        """X, Buf, Gb: fp32 views [M, L, rows, cols] (or [M, rows, cols]) with the same strides, every matrix
+        contiguous; cfg from make_muon_cfg; scratch from ns_scratch(M * L, rows, cols, cfg.ns)."""
+        if X.dim() == 3:
+            X, Buf, Gb = X.unsqueeze(1), Buf.unsqueeze(1), Gb.unsqueeze(1)
+        M, L, rows, cols = X.shape
+        strides = X.stride()
+        if (cols > 1 and strides[3] != 1) or (rows > 1 and strides[2] != cols):
+            raise AbsError("each matrix must be contiguous")
+        for t in (Buf, Gb):
+            if t.shape != X.shape or any(a != b for a, b, n in zip(t.stride(), strides, X.shape) if n > 1):
+                raise AbsError("X, Buf and Gb must share shape and strides")
+        for t in (X, Buf, Gb):
+            if t.dtype != torch.float32:
+                raise AbsError("X, Buf and Gb must be float32, got %s" % t.dtype)
+        self._check(self._lib.local_muon_step(self._h, _ptr(X), _ptr(Buf), _ptr(Gb), M, L, rows, cols, strides[1],
+                                              strides[0], ctypes.byref(cfg), int(bool(average_after)), _ptr(scratch),
+                                              scratch.numel(), _stream(stream)), "local_muon_step")
+
+    # ---- layer norm ------------------------------------------------------------------------------
+    @staticmethod
+    def _rows(t, what):
+        """(row stride, worker stride) of [M, rows, d]; the strides of dimensions of one element are free."""
+        M, rows, d = t.shape
+        if t.stride(2) != 1 and d > 1:
+            raise AbsError("the last dimension of %s must be contiguous" % what)
+        row = t.stride(1) if rows > 1 else d
+        return row, t.stride(0) if M > 1 else row * rows
+
+    @staticmethod
+    def _params(t, M, d, what):
+        """Checks [M, d] fp32 parameters (a replica each) and returns their stride."""
+        if t.dtype != torch.float32 or t.shape != (M, d) or (d > 1 and t.stride(1) != 1):
+            raise AbsError("%s must be float32 [%d, %d] with contiguous rows" % (what, M, d))
+        return t.stride(0) if M > 1 else d
+
+    @classmethod
+    def _same_stride(cls, tensors, M, d, what):
+        strides = {cls._params(t, M, d, what) for t in tensors if t is not None}
+        if len(strides) > 1:
+            raise AbsError("%s must share the replica stride" % what)
+        return strides.pop() if strides else d
+
+    def abs_layer_norm(self, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
+        """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight, bias: [M, d] (or [d]) fp32 or None; mean, rstd:
+        contiguous fp32 [M, rows] or None.  Y may be X."""
+        if X.dim() == 2:
+            X, Y = X.unsqueeze(0), Y.unsqueeze(0)
+            weight, bias = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, bias))
+        if X.dim() != 3 or X.shape != Y.shape or X.dtype != Y.dtype:
+            raise AbsError("X and Y must be [M, rows, d] of one type")
+        M, rows, d = X.shape
+        p_stride = self._same_stride((weight, bias), M, d, "weight and bias")
+        self._statistics((mean, rstd), M * rows)
+        x_rs, x_ws = self._rows(X, "X")
+        y_rs, y_ws = self._rows(Y, "Y")
+        self._check(self._lib.abs_layer_norm(self._h, _ptr(X), _dtype_code(X), M, rows, d, x_rs, x_ws, _ptr(weight),
+                                             _ptr(bias), p_stride, float(eps), _ptr(Y), y_rs, y_ws, _ptr(mean), _ptr(rstd),
+                                             _stream(stream)), "abs_layer_norm")
+        return Y
+
+    @staticmethod
+    def _statistics(tensors, n):
+        for t in tensors:
+            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+                raise AbsError("mean and rstd must be contiguous float32 tensors of %d values" % n)
+
+    def abs_layer_norm_backward(self, dY, X, mean, rstd, weight, dX=None, dW=None, dB=None, samples=1, Gw=None, Gb=None,
+                                stream=None):
+        """dY, X, dX: [M, samples * tokens, d] (or [rows, d]); mean, rstd as abs_layer_norm wrote them; weight [M, d] or
+        None.  dW, dB: fp32 [M, d]; Gw, Gb: fp32 [M, samples, d] per-sample gradients with a shared row stride (two
+        parts of the rows that abs_test_stats takes).  Every output may be None."""
+        if X.dim() == 2:
+            dY, X, dX = (t if t is None else t.unsqueeze(0) for t in (dY, X, dX))
+            weight, dW, dB = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, dW, dB))
+            Gw, Gb = (t if t is None or t.dim() == 3 else t.unsqueeze(0) for t in (Gw, Gb))
+        for t in (dY, X, dX):
+            if t is not None and (t.dim() != 3 or t.shape != X.shape or t.dtype != X.dtype):
+                raise AbsError("dY, X and dX must be [M, rows, d] of one type")
+        M, rows, d = X.shape
+        samples = int(samples)
+        if samples < 0 or (samples == 0 and rows) or (samples and rows % samples):
+            raise AbsError("%d rows are not %d samples of equal length" % (rows, samples))
+        p_stride = self._same_stride((weight,), M, d, "weight")
+        grad_stride = self._same_stride((dW, dB), M, d, "dW and dB")
+        self._statistics((mean, rstd), M * rows)
+        g_strides = set()
+        for t in (Gw, Gb):
+            if t is not None:
+                if t.dtype != torch.float32 or t.shape != (M, samples, d):
+                    raise AbsError("Gw and Gb must be float32 [%d, %d, %d]" % (M, samples, d))
+                g_strides.add(self._rows(t, "Gw and Gb"))
+        if len(g_strides) > 1:
+            raise AbsError("Gw and Gb must share their strides")
+        g_rs, g_ws = g_strides.pop() if g_strides else (d, d * samples)
+        y_rs, y_ws = self._rows(dY, "dY")
+        x_rs, x_ws = self._rows(X, "X")
+        dx_rs, dx_ws = self._rows(dX, "dX") if dX is not None else (d, d)
+        self._check(self._lib.abs_layer_norm_backward(
+            self._h, _ptr(dY), y_rs, y_ws, _ptr(X), x_rs, x_ws, _dtype_code(X), M, samples,
+            rows // samples if samples else 0, d, _ptr(mean), _ptr(rstd), _ptr(weight), p_stride, _ptr(dX), dx_rs, dx_ws,
+            _ptr(dW), _ptr(dB), grad_stride, _ptr(Gw), _ptr(Gb), g_rs, g_ws, _stream(stream)), "abs_layer_norm_backward")
 
     # ---- producers and rounds ----------------------------------------------------------------
     def abs_logreg_grads(self, A, y, idx, X, b, G, stream=None):
@@ -499,3 +666,17 @@ def make_round_opts(test_every_step=False, per_worker=False, eta_m=None, ctl=Non
 
 def make_adamw_cfg(lr, beta1, beta2, eps, weight_decay, step):
     return AdamWCfg(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), 0, int(step))
+
+
+NS_PRECISION = {"f16": 0, "f32": 1}
+
+
+def make_ns_cfg(steps=5, a=3.4445, b=-4.7750, c=2.0315, eps=1e-7, precision="f16"):
+    """abs_ns_cfg: the Newton-Schulz iteration of abs_orthogonalise and local_muon_step."""
+    return NsCfg(float(a), float(b), float(c), float(eps), int(steps), NS_PRECISION[precision])
+
+
+def make_muon_cfg(lr, momentum=0.95, weight_decay=0.0, scale=1.0, nesterov=True, ns=None):
+    """abs_muon_cfg; ns from make_ns_cfg (default: its defaults)."""
+    return MuonCfg(float(lr), float(momentum), float(weight_decay), float(scale), int(bool(nesterov)), 0,
+                   ns if ns is not None else make_ns_cfg())

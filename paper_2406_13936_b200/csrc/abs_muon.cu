@@ -1,0 +1,402 @@
+// Orthogonalisation of a matrix by Newton-Schulz products, and the local Muon step built on it.
+//
+// From X_0 = G / (||G||_F + eps) (all singular values in [0, 1]) each step applies the odd polynomial
+// p(s) = a s + b s^3 + c s^5 to the singular values:
+//   A = X X',   X <- a X + (b A + c A^2) X          (on the short side, m <= n).
+//
+// Rounding.  The products run on fp16 operands (11 significant bits, fp32 accumulation); X itself is
+// carried as hi + lo (22 bits) and the linear term uses both.  Small singular values grow by a factor a
+// in every step (3.4445^5 = 485), and only through the linear term: rounding X to 11 bits there would
+// lift the rounding noise of large directions into empty ones (fp16 simulation, 512 x 1024 of rank 8:
+// 4e-2 of the result's norm; bfloat16 0.35), while rounding inside B X stays in proportion to B X
+// (7e-4 to 1.6e-3 on Gaussian, 1/k, exponentially decaying, rank-8 and spiked spectra).  With
+// ABS_NS_F32 every operand is hi + lo and a product is three tensor-core products (fp32-grade).
+#include <math.h>
+
+#include <cuda_bf16.h>
+
+#include "abs_ns.cuh"
+
+namespace absk {
+namespace {
+
+constexpr int kTile = 32;
+constexpr int kPassThreads = 256;
+
+// Where the matrices of a call live: matrix q is worker q / L, layer q % L.
+struct NsSource {
+  const void* G;          // orthogonalise: the input; Muon: the gradients
+  int src_bf16;
+  float* Buf;             // Muon: momentum buffers
+  float momentum;
+  int nesterov;
+  int muon;
+  int L;
+  long long replica_stride, matrix_stride, row_stride;
+  int rows, cols;
+};
+struct NsTarget {
+  void* O;                // orthogonalise: the result
+  int dst_bf16;
+  float* X;               // Muon: the parameters
+  float decay, step;      // x <- decay x - step o
+  long long replica_stride, matrix_stride, row_stride;
+};
+
+__device__ __forceinline__ long long matrix_base(int q, int L, long long replica_stride, long long matrix_stride) {
+  const int m = q / L;
+  return m * replica_stride + static_cast<long long>(q - m * L) * matrix_stride;
+}
+__device__ __forceinline__ float load_src(const NsSource& s, long long i) {
+  return s.src_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short*>(s.G)[i]) << 16)
+                    : static_cast<const float*>(s.G)[i];
+}
+// The matrix to orthogonalise, after ns_norm_kernel has updated the momentum buffer.
+__device__ __forceinline__ float load_update(const NsSource& s, long long i) {
+  if (!s.muon) return load_src(s, i);
+  const float b = s.Buf[i];
+  return s.nesterov ? fmaf(s.momentum, b, load_src(s, i)) : b;
+}
+
+// Momentum update (Muon) and partial sums of squares in fp64 (no overflow, no lost small entries).
+__global__ void __launch_bounds__(kPassThreads)
+ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* flag) {
+  __shared__ double red[kPassThreads / 32];
+  const int z = blockIdx.y;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (blockIdx.x == 0 && z == 0 && threadIdx.x == 0 && q0 == 0) *flag = 0u;
+  const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
+  const long long count = static_cast<long long>(s.rows) * s.cols;
+  double sum = 0.0;
+  for (long long e = static_cast<long long>(blockIdx.x) * kPassThreads + threadIdx.x; e < count;
+       e += static_cast<long long>(gridDim.x) * kPassThreads) {
+    const long long r = e / s.cols, i = base + r * s.row_stride + (e - r * s.cols);
+    float u;
+    if (s.muon) {
+      const float g = load_src(s, i), b = fmaf(s.momentum, s.Buf[i], g);
+      s.Buf[i] = b;
+      u = s.nesterov ? fmaf(s.momentum, b, g) : b;
+    } else {
+      u = load_src(s, i);
+    }
+    sum += static_cast<double>(u) * u;
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kPassThreads / 32; ++w) sum += red[w];
+    part[static_cast<long long>(z) * kNormParts + blockIdx.x] = sum;
+  }
+}
+
+// X_0 = U / (||U||_F + eps), scaled by sx, as hi + lo, transposed where U is taller than wide.
+__global__ void __launch_bounds__(kPassThreads)
+ns_split_kernel(const NsSource s, int q0, const NsBuffers w, float eps, float sx, int tiles_c) {
+  __shared__ float tile[kTile][kTile + 1];
+  __shared__ double scale_s;
+  const int z = blockIdx.y, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (threadIdx.x == 0) {
+    double sum = 0.0;
+    for (int k = 0; k < kNormParts; ++k) sum += w.part[static_cast<long long>(z) * kNormParts + k];
+    scale_s = static_cast<double>(sx) / (sqrt(sum) + static_cast<double>(eps));
+  }
+  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+  const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
+  const int c = tc * kTile + tx;
+#pragma unroll
+  for (int k = 0; k < kTile; k += 8) {
+    const int r = tr * kTile + ty + k;
+    if (r < s.rows && c < s.cols) tile[ty + k][tx] = load_update(s, base + static_cast<long long>(r) * s.row_stride + c);
+  }
+  __syncthreads();
+  const double scale = scale_s;              // fp64: a tiny norm's inverse may pass the range of fp32
+  const bool tall = s.rows > s.cols;
+  const long long zoff = z * w.ldx * w.m;
+#pragma unroll
+  for (int k = 0; k < kTile; k += 8) {
+    const int i = (tall ? tc : tr) * kTile + ty + k, j = (tall ? tr : tc) * kTile + tx;      // row and column of X
+    if (i >= w.m || j >= w.n) continue;
+    const float v = static_cast<float>((tall ? tile[tx][ty + k] : tile[ty + k][tx]) * scale);
+    const __half h = __float2half_rn(v);
+    const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
+    w.xh[0][o] = h;
+    w.xl[0][o] = __float2half_rn(v - __half2float(h));
+  }
+}
+
+// O = X / sx back in the caller's orientation: the result, or the parameter update.
+__global__ void __launch_bounds__(kPassThreads)
+ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, int cur, float inv_sx, int tiles_c,
+                 const unsigned* flag) {
+  __shared__ float tile[kTile][kTile + 1];
+  const int z = blockIdx.y, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+  const bool tall = s.rows > s.cols;
+  const long long zoff = z * w.ldx * w.m;
+  const float bad = *flag ? __int_as_float(0x7fc00000) : 0.f;          // a product whose wait ran out: nothing is valid
+#pragma unroll
+  for (int k = 0; k < kTile; k += 8) {
+    const int i = (tall ? tc : tr) * kTile + ty + k, j = (tall ? tr : tc) * kTile + tx;
+    if (i >= w.m || j >= w.n) continue;
+    const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
+    const float v = (__half2float(w.xh[cur][o]) + __half2float(w.xl[cur][o])) * inv_sx + bad;
+    if (tall) tile[tx][ty + k] = v;
+    else tile[ty + k][tx] = v;
+  }
+  __syncthreads();
+  const long long base = matrix_base(q0 + z, s.L, t.replica_stride, t.matrix_stride);
+  const int c = tc * kTile + tx;
+#pragma unroll
+  for (int k = 0; k < kTile; k += 8) {
+    const int r = tr * kTile + ty + k;
+    if (r >= s.rows || c >= s.cols) continue;
+    const long long i = base + static_cast<long long>(r) * t.row_stride + c;
+    const float v = tile[ty + k][tx];
+    if (s.muon) t.X[i] = fmaf(-t.step, v, t.decay * t.X[i]);
+    else if (t.dst_bf16) static_cast<__nv_bfloat16*>(t.O)[i] = __float2bfloat16_rn(v);
+    else static_cast<float*>(t.O)[i] = v;
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+// Largest |p| on [0, hi] for p(s) = a s + b s^3 + c s^5, and for q(s) = b s^2 + c s^4.
+double bound_poly(double a, double b, double c, double hi) {
+  auto p = [&](double s) { return fabs(s * (a + s * s * (b + s * s * c))); };
+  double best = p(hi);
+  // p'(s) = a + 3 b t + 5 c t^2 with t = s^2
+  const double A = 5.0 * c, B = 3.0 * b;
+  double roots[2];
+  int n = 0;
+  if (A != 0.0) {
+    const double disc = B * B - 4.0 * A * a;
+    if (disc >= 0.0) {
+      roots[n++] = (-B + sqrt(disc)) / (2.0 * A);
+      roots[n++] = (-B - sqrt(disc)) / (2.0 * A);
+    }
+  } else if (B != 0.0) {
+    roots[n++] = -a / B;
+  }
+  for (int k = 0; k < n; ++k)
+    if (roots[k] > 0.0 && roots[k] < hi * hi) best = fmax(best, p(sqrt(roots[k])));
+  return best;
+}
+double bound_even(double b, double c, double hi) {
+  auto q = [&](double t) { return fabs(t * (b + t * c)); };
+  double best = q(hi * hi);
+  if (c != 0.0) {
+    const double t = -b / (2.0 * c);
+    if (t > 0.0 && t < hi * hi) best = fmax(best, q(t));
+  }
+  return best;
+}
+// The largest power of two that keeps entries up to `bound` at or below 2^14.
+float pow2_scale(double bound) { return static_cast<float>(exp2(floor(log2(16384.0 / fmax(bound, 1e-6))))); }
+
+constexpr double kMaxSingular = 1024.0;
+
+int validate_ns(abs_ctx* ctx, int count, long long rows, long long cols, const abs_ns_cfg* cfg) {
+  if (cfg == nullptr) return set_error(ctx, ABS_ERR_INVALID_ARG, "cfg is null");
+  if (count < 1 || rows < 1 || cols < 1)
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "need at least one matrix of at least 1 x 1 (count=%d rows=%lld cols=%lld)",
+                     count, rows, cols);
+  if (cfg->steps < 1 || cfg->steps > kNsMaxSteps)
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "steps must be 1..%d, got %d", kNsMaxSteps, cfg->steps);
+  if (cfg->precision != ABS_NS_F16 && cfg->precision != ABS_NS_F32)
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "unknown precision %d", cfg->precision);
+  if (!(cfg->eps >= 0.f) || !isfinite(cfg->eps) || !isfinite(cfg->a) || !isfinite(cfg->b) || !isfinite(cfg->c))
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "coefficients must be finite and eps finite and >= 0");
+  if (rows > 65536 || cols > 65536 || count > (1 << 24))
+    return set_error(ctx, ABS_ERR_UNSUPPORTED, "matrices are at most 65536 x 65536 and 2^24 in number");
+  return ABS_OK;
+}
+
+long long align_up(long long v, long long a) { return (v + a - 1) / a * a; }
+
+struct NsPlan {
+  int m, n;
+  long long ldx, ldm, x_halves, m_halves;    // per matrix
+  bool split;
+  size_t per_matrix() const {
+    return static_cast<size_t>(4 * x_halves + (split ? 4 : 2) * m_halves) * 2 + kNormParts * sizeof(double);
+  }
+};
+constexpr size_t kNsFixedBytes = 16 * 1024;       // alignment of the buffers
+// Matrices that are worked on together: as many as keep what a step reads and writes inside L2.
+constexpr size_t kGroupBytes = 96ull << 20;
+
+NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
+  NsPlan p;
+  p.m = static_cast<int>(rows < cols ? rows : cols);
+  p.n = static_cast<int>(rows < cols ? cols : rows);
+  p.ldx = align_up(p.n, 8);
+  p.ldm = align_up(p.m, 8);
+  p.x_halves = p.ldx * p.m;
+  p.m_halves = p.ldm * p.m;
+  // Up to 64 rows the operands are split at either precision: with few rows the roundings of 11 bits do
+  // not average out (simulated, worst of 200 Gaussian matrices: 2 x 2 1.8e-2, 4 x 4 6.5e-3, 10 x 1024
+  // 2e-3), and a product of one row tile is bound by latency, not by its three tensor-core products.
+  p.split = cfg->precision == ABS_NS_F32 || p.m <= 64;
+  return p;
+}
+int group_size(const NsPlan& p, int count) {
+  long long z = static_cast<long long>(kGroupBytes / p.per_matrix());
+  if (z < 1) z = 1;
+  if (z > count) z = count;
+  if (z > 65535) z = 65535;
+  return static_cast<int>(z);
+}
+
+int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, const abs_ns_cfg* cfg, void* scratch,
+           size_t scratch_bytes, cudaStream_t st) {
+  const NsPlan p = plan_ns(src.rows, src.cols, cfg);
+  const int zmax = group_size(p, count);
+  const size_t need = kNsFixedBytes + zmax * p.per_matrix();
+  if (scratch == nullptr || scratch_bytes < need)
+    return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes is too small: %zu needed", scratch_bytes, need);
+  // scales of the stored matrices, from bounds on the singular values step by step
+  NsScales sc;
+  double hi = 1.0;
+  for (int k = 0; k < cfg->steps; ++k) {
+    sc.sx[k] = pow2_scale(hi);
+    sc.ta[k] = pow2_scale(hi * hi);
+    sc.tb[k] = pow2_scale(bound_even(cfg->b, cfg->c, hi));
+    hi = bound_poly(cfg->a, cfg->b, cfg->c, hi);
+    if (!(hi <= kMaxSingular))
+      return set_error(ctx, ABS_ERR_UNSUPPORTED, "the coefficients let singular values grow beyond %g in step %d",
+                       kMaxSingular, k + 1);
+  }
+  sc.sx[cfg->steps] = pow2_scale(hi);
+
+  const int tiles_c = (src.cols + kTile - 1) / kTile, tiles_r = (src.rows + kTile - 1) / kTile;
+  for (int q0 = 0; q0 < count; q0 += zmax) {
+    NsBuffers w = {};
+    w.Z = count - q0 < zmax ? count - q0 : zmax;
+    w.m = p.m; w.n = p.n; w.ldx = p.ldx; w.ldm = p.ldm;
+    uintptr_t at = reinterpret_cast<uintptr_t>(scratch);
+    auto take = [&](size_t bytes) {
+      at = (at + 1023) / 1024 * 1024;
+      void* r = reinterpret_cast<void*>(at);
+      at += bytes;
+      return r;
+    };
+    const size_t xb = static_cast<size_t>(p.x_halves) * zmax * 2, mb = static_cast<size_t>(p.m_halves) * zmax * 2;
+    for (int k = 0; k < 2; ++k) {
+      w.xh[k] = static_cast<__half*>(take(xb));
+      w.xl[k] = static_cast<__half*>(take(xb));
+    }
+    w.ah = static_cast<__half*>(take(mb));
+    w.bh = static_cast<__half*>(take(mb));
+    if (p.split) {
+      w.al = static_cast<__half*>(take(mb));
+      w.bl = static_cast<__half*>(take(mb));
+    }
+    w.part = static_cast<double*>(take(static_cast<size_t>(zmax) * kNormParts * sizeof(double)));
+
+    unsigned* flag = ctx->flags + kNsFlagWord;
+    ABS_CUDA_TRY(ctx, launch_dependent(ns_norm_kernel, dim3(kNormParts, w.Z), dim3(kPassThreads), 0, st, src, q0, w.part, flag));
+    const dim3 tiles(static_cast<unsigned>(tiles_c) * tiles_r, w.Z);
+    ABS_CUDA_TRY(ctx, launch_dependent(ns_split_kernel, tiles, dim3(kPassThreads), 0, st, src, q0, w, cfg->eps, sc.sx[0], tiles_c));
+    int cur = 0;
+    for (int k = 0; k < cfg->steps; ++k, cur ^= 1) {
+      const int rc = launch_ns_step(ctx, w, cur, cfg->a, cfg->b, cfg->c, sc.sx[k], sc.ta[k], sc.tb[k], sc.sx[k + 1], p.split, st);
+      if (rc != ABS_OK) return rc;
+    }
+    ABS_CUDA_TRY(ctx, launch_dependent(ns_finish_kernel, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur,
+                                       1.0f / sc.sx[cfg->steps], tiles_c, static_cast<const unsigned*>(flag)));
+  }
+  return ABS_OK;
+}
+
+struct DeviceGuardNs {
+  int prev = -1;
+  bool ok = true;
+  explicit DeviceGuardNs(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
+    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+    if (prev == dev) prev = -1;
+  }
+  ~DeviceGuardNs() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+}  // namespace
+}  // namespace absk
+
+using namespace absk;
+
+extern "C" int abs_ns_scratch_bytes(int count, long long rows, long long cols, const abs_ns_cfg* cfg, size_t* out) {
+  if (out == nullptr) return ABS_ERR_INVALID_ARG;
+  *out = 0;
+  const int rc = validate_ns(nullptr, count, rows, cols, cfg);
+  if (rc != ABS_OK) return rc;
+  const NsPlan p = plan_ns(rows, cols, cfg);
+  *out = kNsFixedBytes + group_size(p, count) * p.per_matrix();
+  return ABS_OK;
+}
+
+extern "C" int abs_orthogonalise(abs_ctx* ctx, const void* G, abs_dtype g_dtype, int count, long long rows, long long cols,
+                                 long long g_row_stride, long long g_matrix_stride, void* O, abs_dtype o_dtype,
+                                 long long o_row_stride, long long o_matrix_stride, const abs_ns_cfg* cfg, void* scratch,
+                                 size_t scratch_bytes, void* stream) {
+  if (ctx == nullptr) return ABS_ERR_INVALID_ARG;
+  const int rc = validate_ns(ctx, count, rows, cols, cfg);
+  if (rc != ABS_OK) return rc;
+  if (G == nullptr || O == nullptr) return set_error(ctx, ABS_ERR_INVALID_ARG, "G or O is null");
+  if ((g_dtype != ABS_F32 && g_dtype != ABS_BF16) || (o_dtype != ABS_F32 && o_dtype != ABS_BF16))
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "unknown dtype");
+  if (g_row_stride < cols || o_row_stride < cols ||
+      (count > 1 && (g_matrix_stride < (rows - 1) * g_row_stride + cols || o_matrix_stride < (rows - 1) * o_row_stride + cols)))
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "rows or matrices overlap: check the strides");
+  DeviceGuardNs guard(ctx->device);
+  if (!guard.ok) return set_error(ctx, ABS_ERR_CUDA, "cannot select device %d", ctx->device);
+  NsSource s = {};
+  s.G = G; s.src_bf16 = g_dtype == ABS_BF16; s.L = count; s.matrix_stride = g_matrix_stride;
+  s.row_stride = g_row_stride; s.rows = static_cast<int>(rows); s.cols = static_cast<int>(cols);
+  NsTarget t = {};
+  t.O = O; t.dst_bf16 = o_dtype == ABS_BF16; t.matrix_stride = o_matrix_stride; t.row_stride = o_row_stride;
+  return run_ns(ctx, s, t, count, cfg, scratch, scratch_bytes, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int local_muon_step(abs_ctx* ctx, float* X, float* Buf, const float* Gb, int M, int matrices, long long rows,
+                               long long cols, long long matrix_stride, long long replica_stride, const abs_muon_cfg* cfg,
+                               int average_after, void* scratch, size_t scratch_bytes, void* stream) {
+  if (ctx == nullptr) return ABS_ERR_INVALID_ARG;
+  if (cfg == nullptr) return set_error(ctx, ABS_ERR_INVALID_ARG, "cfg is null");
+  if (M < 1 || matrices < 1 || static_cast<long long>(M) * matrices > (1 << 24))
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "need M >= 1 and matrices >= 1 (M=%d matrices=%d)", M, matrices);
+  int rc = validate_ns(ctx, M * matrices, rows, cols, &cfg->ns);
+  if (rc != ABS_OK) return rc;
+  if (X == nullptr || Buf == nullptr || Gb == nullptr) return set_error(ctx, ABS_ERR_INVALID_ARG, "null tensor pointer");
+  if (!(cfg->momentum >= 0.f && cfg->momentum < 1.f) || !isfinite(cfg->lr) || !isfinite(cfg->weight_decay) || !isfinite(cfg->scale))
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "need momentum in [0, 1) and finite lr, weight_decay and scale");
+  const long long size = rows * cols;
+  if (matrices > 1 && matrix_stride < size)
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "matrix_stride %lld < rows * cols %lld", matrix_stride, size);
+  if (M > 1 && replica_stride < (matrices > 1 ? (matrices - 1) * matrix_stride : 0) + size)
+    return set_error(ctx, ABS_ERR_INVALID_ARG, "replica_stride %lld overlaps the previous replica", replica_stride);
+  DeviceGuardNs guard(ctx->device);
+  if (!guard.ok) return set_error(ctx, ABS_ERR_CUDA, "cannot select device %d", ctx->device);
+  NsSource s = {};
+  s.G = Gb; s.Buf = Buf; s.momentum = cfg->momentum; s.nesterov = cfg->nesterov ? 1 : 0; s.muon = 1; s.L = matrices;
+  s.replica_stride = replica_stride; s.matrix_stride = matrix_stride; s.row_stride = cols;
+  s.rows = static_cast<int>(rows); s.cols = static_cast<int>(cols);
+  NsTarget t = {};
+  t.X = X;
+  t.decay = static_cast<float>(1.0 - static_cast<double>(cfg->lr) * cfg->weight_decay);
+  t.step = static_cast<float>(static_cast<double>(cfg->lr) * cfg->scale);
+  t.replica_stride = replica_stride; t.matrix_stride = matrix_stride; t.row_stride = cols;
+  rc = run_ns(ctx, s, t, M * matrices, &cfg->ns, scratch, scratch_bytes, static_cast<cudaStream_t>(stream));
+  if (rc != ABS_OK || !average_after || M == 1) return rc;
+  if (matrices == 1 || matrix_stride == size) return replica_average(ctx, X, M, size * matrices, replica_stride, stream);
+  for (int l = 0; l < matrices; ++l) {
+    rc = replica_average(ctx, X + l * matrix_stride, M, size, replica_stride, stream);
+    if (rc != ABS_OK) return rc;
+  }
+  return ABS_OK;
+}

@@ -1,0 +1,48 @@
+// Newton-Schulz orthogonalisation: what the elementwise passes (abs_muon.cu) and the tensor-core
+// products (abs_ns_gemm.cu) share.
+//
+// One matrix is held with its short side as rows, X [m][n], m <= n (a tall matrix is transposed when
+// it is read and again when the result is written), as X = hi + lo in two fp16 matrices.  A step is
+//   A = X X',   B = b A + c A A,   X <- a X + B X,
+// three products whose operands are the fp16 (hi) values; the a X term takes hi + lo, so what 11
+// bits of an operand lose is always in proportion to B X and never fills directions that the
+// gradient does not have (see abs_muon.cu).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "abs_internal.cuh"
+
+namespace absk {
+
+constexpr int kNsMaxSteps = 32;
+
+// Powers of two by which a step's matrices are stored, so that fp16 neither overflows nor wastes its
+// range (largest possible entry at most 2^14).
+struct NsScales {
+  float sx[kNsMaxSteps + 1];   // X before step k (and after the last one)
+  float ta[kNsMaxSteps];       // A
+  float tb[kNsMaxSteps];       // B
+};
+
+// Device buffers of one group of Z matrices.  X is double-buffered: a step reads cur, writes cur ^ 1.
+struct NsBuffers {
+  int Z, m, n;
+  long long ldx, ldm;              // leading dimensions in elements, multiples of 8
+  __half* xh[2];
+  __half* xl[2];                   // low parts: the a X term and, with split operands, the products
+  __half* ah;
+  __half* al;                      // low parts of A and B: split operands only
+  __half* bh;
+  __half* bl;
+  double* part;                    // [Z][kNormParts] partial sums of squares
+};
+constexpr int kNormParts = 64;
+constexpr int kNsFlagWord = 8;     // word of abs_ctx::flags that a product whose wait ran out sets (cleared by every call)
+
+// One step's three products for the whole group.  split: both parts of every operand (three
+// tensor-core products, fp32-grade); else the fp16 values alone.
+int launch_ns_step(abs_ctx* ctx, const NsBuffers& w, int cur, float a, float b, float c, float sx, float ta, float tb,
+                   float sx_next, bool split, cudaStream_t st);
+
+}  // namespace absk
