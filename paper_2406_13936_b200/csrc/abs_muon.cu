@@ -20,8 +20,9 @@
 namespace absk {
 namespace {
 
-constexpr int kTile = 32;
+constexpr int kTile = 64;
 constexpr int kPassThreads = 256;
+constexpr int kTileVecs = kTile * kTile / 4 / kPassThreads;     // groups of four elements per thread
 
 // Where the matrices of a call live: matrix q is worker q / L, layer q % L.
 struct NsSource {
@@ -47,18 +48,57 @@ __device__ __forceinline__ long long matrix_base(int q, int L, long long replica
   const int m = q / L;
   return m * replica_stride + static_cast<long long>(q - m * L) * matrix_stride;
 }
-__device__ __forceinline__ float load_src(const NsSource& s, long long i) {
-  return s.src_bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short*>(s.G)[i]) << 16)
-                    : static_cast<const float*>(s.G)[i];
+template <int V>
+__device__ __forceinline__ void load_f32(const float* p, float (&v)[V]) {
+  if constexpr (V == 4) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    v[0] = *p;
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_f32(float* p, const float (&v)[V]) {
+  if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  else *p = v[0];
+}
+// V consecutive elements at index i of the source, fp32 or bf16.
+template <int V>
+__device__ __forceinline__ void load_src(const NsSource& s, long long i, float (&v)[V]) {
+  if (s.src_bf16) {
+    const unsigned short* p = static_cast<const unsigned short*>(s.G) + i;
+    if constexpr (V == 4) {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      v[0] = __uint_as_float(u.x << 16);
+      v[1] = __uint_as_float(u.x & 0xffff0000u);
+      v[2] = __uint_as_float(u.y << 16);
+      v[3] = __uint_as_float(u.y & 0xffff0000u);
+    } else {
+      v[0] = __uint_as_float(static_cast<uint32_t>(*p) << 16);
+    }
+  } else {
+    load_f32<V>(static_cast<const float*>(s.G) + i, v);
+  }
 }
 // The matrix to orthogonalise, after ns_norm_kernel has updated the momentum buffer.
-__device__ __forceinline__ float load_update(const NsSource& s, long long i) {
-  if (!s.muon) return load_src(s, i);
-  const float b = s.Buf[i];
-  return s.nesterov ? fmaf(s.momentum, b, load_src(s, i)) : b;
+template <int V>
+__device__ __forceinline__ void load_update(const NsSource& s, long long i, float (&u)[V]) {
+  if (!s.muon) {
+    load_src<V>(s, i, u);
+    return;
+  }
+  load_f32<V>(s.Buf + i, u);
+  if (s.nesterov) {
+    float g[V];
+    load_src<V>(s, i, g);
+#pragma unroll
+    for (int e = 0; e < V; ++e) u[e] = fmaf(s.momentum, u[e], g[e]);
+  }
 }
 
 // Momentum update (Muon) and partial sums of squares in fp64 (no overflow, no lost small entries).
+// V = 4: every group of four elements is 16-byte aligned and lies in one row.
+template <int V>
 __global__ void __launch_bounds__(kPassThreads)
 ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* flag) {
   __shared__ double red[kPassThreads / 32];
@@ -67,20 +107,33 @@ ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* fl
   pdl_wait();
   if (blockIdx.x == 0 && z == 0 && threadIdx.x == 0 && q0 == 0) *flag = 0u;
   const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
-  const long long count = static_cast<long long>(s.rows) * s.cols;
+  const bool flat = s.row_stride == s.cols;                    // one row of rows * cols elements
+  const int per_row = s.cols / V;
+  const long long count = static_cast<long long>(s.rows) * per_row;
   double sum = 0.0;
   for (long long e = static_cast<long long>(blockIdx.x) * kPassThreads + threadIdx.x; e < count;
        e += static_cast<long long>(gridDim.x) * kPassThreads) {
-    const long long r = e / s.cols, i = base + r * s.row_stride + (e - r * s.cols);
-    float u;
-    if (s.muon) {
-      const float g = load_src(s, i), b = fmaf(s.momentum, s.Buf[i], g);
-      s.Buf[i] = b;
-      u = s.nesterov ? fmaf(s.momentum, b, g) : b;
+    long long i = base;
+    if (flat) {
+      i += e * V;
     } else {
-      u = load_src(s, i);
+      const long long r = e / per_row;
+      i += r * s.row_stride + (e - r * per_row) * V;
     }
-    sum += static_cast<double>(u) * u;
+    float u[V];
+    load_src<V>(s, i, u);
+    if (s.muon) {
+      float b[V];
+      load_f32<V>(s.Buf + i, b);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        b[k] = fmaf(s.momentum, b[k], u[k]);
+        u[k] = s.nesterov ? fmaf(s.momentum, b[k], u[k]) : b[k];
+      }
+      store_f32<V>(s.Buf + i, b);
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) sum = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum);
   }
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -92,76 +145,143 @@ ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* fl
   }
 }
 
-// X_0 = U / (||U||_F + eps), scaled by sx, as hi + lo, transposed where U is taller than wide.
+// X_0 = U / (||U||_F + eps), scaled by sx, as hi + lo, transposed where U is taller than wide.  A CTA
+// takes a 64 x 64 tile of U; a warp reads and writes whole rows of it, four elements a lane.
+template <int V>
 __global__ void __launch_bounds__(kPassThreads)
-ns_split_kernel(const NsSource s, int q0, const NsBuffers w, float eps, float sx, int tiles_c) {
+ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float eps, float sx, int tiles_c) {
   __shared__ float tile[kTile][kTile + 1];
-  __shared__ double scale_s;
-  const int z = blockIdx.y, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  __shared__ double red[kPassThreads / 32];
+  const int z = blockIdx.y, tid = threadIdx.x;
   pdl_launch_dependents();
   pdl_wait();
-  if (threadIdx.x == 0) {
-    double sum = 0.0;
-    for (int k = 0; k < kNormParts; ++k) sum += w.part[static_cast<long long>(z) * kNormParts + k];
-    scale_s = static_cast<double>(sx) / (sqrt(sum) + static_cast<double>(eps));
-  }
-  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+  double sum = 0.0;
+  for (int k = tid; k < parts; k += kPassThreads) sum += w.part[static_cast<long long>(z) * kNormParts + k];
+  const bool tall = s.rows > s.cols;
+  const int tr = static_cast<int>(blockIdx.x) / tiles_c, tc = static_cast<int>(blockIdx.x) - tr * tiles_c;
   const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
-  const int c = tc * kTile + tx;
+  float u[kTileVecs][4];
 #pragma unroll
-  for (int k = 0; k < kTile; k += 8) {
-    const int r = tr * kTile + ty + k;
-    if (r < s.rows && c < s.cols) tile[ty + k][tx] = load_update(s, base + static_cast<long long>(r) * s.row_stride + c);
+  for (int k = 0; k < kTileVecs; ++k) {
+    const int r = tr * kTile + (tid >> 4) + 16 * k, c = tc * kTile + 4 * (tid & 15);
+    const long long i = base + static_cast<long long>(r) * s.row_stride + c;
+#pragma unroll
+    for (int e = 0; e < 4; e += V) {
+      float t[V];
+#pragma unroll
+      for (int x = 0; x < V; ++x) t[x] = 0.f;
+      if (r < s.rows && c + e < s.cols) load_update<V>(s, i + e, t);
+#pragma unroll
+      for (int x = 0; x < V; ++x) u[k][e + x] = t[x];
+    }
+  }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  if ((tid & 31) == 0) red[tid >> 5] = sum;
+  if (tall) {
+#pragma unroll
+    for (int k = 0; k < kTileVecs; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile[4 * (tid & 15) + e][(tid >> 4) + 16 * k] = u[k][e];
   }
   __syncthreads();
-  const double scale = scale_s;              // fp64: a tiny norm's inverse may pass the range of fp32
-  const bool tall = s.rows > s.cols;
+  sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < kPassThreads / 32; ++k) sum += red[k];
+  // fp64: a tiny norm's inverse may pass the range of fp32
+  const double scale = static_cast<double>(sx) / (sqrt(sum) + static_cast<double>(eps));
   const long long zoff = z * w.ldx * w.m;
 #pragma unroll
-  for (int k = 0; k < kTile; k += 8) {
-    const int i = (tall ? tc : tr) * kTile + ty + k, j = (tall ? tr : tc) * kTile + tx;      // row and column of X
-    if (i >= w.m || j >= w.n) continue;
-    const float v = static_cast<float>((tall ? tile[tx][ty + k] : tile[ty + k][tx]) * scale);
-    const __half h = __float2half_rn(v);
+  for (int k = 0; k < kTileVecs; ++k) {
+    const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
+    const int i = (tall ? tc : tr) * kTile + ri, j = (tall ? tr : tc) * kTile + cj;      // row and column of X
+    if (i >= w.m || j >= w.n) continue;                        // ldx is a multiple of 8: four columns stay in the row
+    __half2 h[2], l[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float a = static_cast<float>((tall ? tile[ri][cj + 2 * e] : u[k][2 * e]) * scale);
+      const float b = static_cast<float>((tall ? tile[ri][cj + 2 * e + 1] : u[k][2 * e + 1]) * scale);
+      h[e] = __floats2half2_rn(a, b);
+      const float2 f = __half22float2(h[e]);
+      l[e] = __floats2half2_rn(a - f.x, b - f.y);
+    }
     const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
-    w.xh[0][o] = h;
-    w.xl[0][o] = __float2half_rn(v - __half2float(h));
+    *reinterpret_cast<uint2*>(w.xh[0] + o) = *reinterpret_cast<const uint2*>(h);
+    *reinterpret_cast<uint2*>(w.xl[0] + o) = *reinterpret_cast<const uint2*>(l);
   }
 }
 
 // O = X / sx back in the caller's orientation: the result, or the parameter update.
+template <int V>
 __global__ void __launch_bounds__(kPassThreads)
 ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, int cur, float inv_sx, int tiles_c,
                  const unsigned* flag) {
   __shared__ float tile[kTile][kTile + 1];
-  const int z = blockIdx.y, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int z = blockIdx.y, tid = threadIdx.x;
   pdl_launch_dependents();
   pdl_wait();
-  const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
   const bool tall = s.rows > s.cols;
+  const int tr = static_cast<int>(blockIdx.x) / tiles_c, tc = static_cast<int>(blockIdx.x) - tr * tiles_c;
   const long long zoff = z * w.ldx * w.m;
   const float bad = *flag ? __int_as_float(0x7fc00000) : 0.f;          // a product whose wait ran out: nothing is valid
+  float u[kTileVecs][4];
 #pragma unroll
-  for (int k = 0; k < kTile; k += 8) {
-    const int i = (tall ? tc : tr) * kTile + ty + k, j = (tall ? tr : tc) * kTile + tx;
-    if (i >= w.m || j >= w.n) continue;
-    const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
-    const float v = (__half2float(w.xh[cur][o]) + __half2float(w.xl[cur][o])) * inv_sx + bad;
-    if (tall) tile[tx][ty + k] = v;
-    else tile[ty + k][tx] = v;
+  for (int k = 0; k < kTileVecs; ++k) {
+    const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
+    const int i = (tall ? tc : tr) * kTile + ri, j = (tall ? tr : tc) * kTile + cj;
+    uint2 h = make_uint2(0u, 0u), l = make_uint2(0u, 0u);
+    if (i < w.m && j < w.n) {
+      const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
+      h = *reinterpret_cast<const uint2*>(w.xh[cur] + o);
+      l = *reinterpret_cast<const uint2*>(w.xl[cur] + o);
+    }
+    const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y));
+    const float2 l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
+    u[k][0] = (h0.x + l0.x) * inv_sx + bad;
+    u[k][1] = (h0.y + l0.y) * inv_sx + bad;
+    u[k][2] = (h1.x + l1.x) * inv_sx + bad;
+    u[k][3] = (h1.y + l1.y) * inv_sx + bad;
+    if (tall) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile[cj + e][ri] = u[k][e];
+    }
   }
-  __syncthreads();
+  if (tall) __syncthreads();
   const long long base = matrix_base(q0 + z, s.L, t.replica_stride, t.matrix_stride);
-  const int c = tc * kTile + tx;
 #pragma unroll
-  for (int k = 0; k < kTile; k += 8) {
-    const int r = tr * kTile + ty + k;
-    if (r >= s.rows || c >= s.cols) continue;
+  for (int k = 0; k < kTileVecs; ++k) {
+    const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
+    const int r = tr * kTile + ri, c = tc * kTile + cj;
+    if (r >= s.rows) continue;
     const long long i = base + static_cast<long long>(r) * t.row_stride + c;
-    const float v = tile[ty + k][tx];
-    if (s.muon) t.X[i] = fmaf(-t.step, v, t.decay * t.X[i]);
-    else if (t.dst_bf16) static_cast<__nv_bfloat16*>(t.O)[i] = __float2bfloat16_rn(v);
-    else static_cast<float*>(t.O)[i] = v;
+    if (tall) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u[k][e] = tile[ri][cj + e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e += V) {
+      if (c + e >= s.cols) continue;
+      float v[V];
+#pragma unroll
+      for (int x = 0; x < V; ++x) v[x] = u[k][e + x];
+      if (s.muon) {
+        float x0[V];
+        load_f32<V>(t.X + i + e, x0);
+#pragma unroll
+        for (int x = 0; x < V; ++x) v[x] = fmaf(-t.step, v[x], t.decay * x0[x]);
+        store_f32<V>(t.X + i + e, v);
+      } else if (t.dst_bf16) {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(t.O) + i + e;
+        if constexpr (V == 4) {
+          __nv_bfloat162 p[2] = {__floats2bfloat162_rn(v[0], v[1]), __floats2bfloat162_rn(v[2], v[3])};
+          *reinterpret_cast<uint2*>(o) = *reinterpret_cast<const uint2*>(p);
+        } else {
+          *o = __float2bfloat16_rn(v[0]);
+        }
+      } else {
+        store_f32<V>(static_cast<float*>(t.O) + i + e, v);
+      }
+    }
   }
 }
 
@@ -248,9 +368,16 @@ NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
 int group_size(const NsPlan& p, int count) {
   long long z = static_cast<long long>(kGroupBytes / p.per_matrix());
   if (z < 1) z = 1;
-  if (z > count) z = count;
   if (z > 65535) z = 65535;
-  return static_cast<int>(z);
+  const long long groups = (count + z - 1) / z;
+  return static_cast<int>((count + groups - 1) / groups);      // groups of about the same size
+}
+
+// Whether four consecutive elements of a row can be moved at once everywhere (strides that are not used
+// are zero).
+bool vectors_of_four(const void* p, int bf16, long long row_stride, long long matrix_stride, long long replica_stride, int cols) {
+  return (reinterpret_cast<uintptr_t>(p) & (bf16 ? 7u : 15u)) == 0 &&
+         ((row_stride | matrix_stride | replica_stride | static_cast<long long>(cols)) & 3) == 0;
 }
 
 int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, const abs_ns_cfg* cfg, void* scratch,
@@ -274,6 +401,10 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
   }
   sc.sx[cfg->steps] = pow2_scale(hi);
 
+  const bool src_vec = vectors_of_four(src.G, src.src_bf16, src.row_stride, src.matrix_stride, src.replica_stride, src.cols) &&
+                       vectors_of_four(src.Buf, 0, src.row_stride, src.matrix_stride, src.replica_stride, src.cols);
+  const bool dst_vec = vectors_of_four(src.muon ? static_cast<const void*>(dst.X) : dst.O, dst.dst_bf16, dst.row_stride, dst.matrix_stride,
+                                       dst.replica_stride, src.cols);
   const int tiles_c = (src.cols + kTile - 1) / kTile, tiles_r = (src.rows + kTile - 1) / kTile;
   for (int q0 = 0; q0 < count; q0 += zmax) {
     NsBuffers w = {};
@@ -300,15 +431,23 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
     w.part = static_cast<double*>(take(static_cast<size_t>(zmax) * kNormParts * sizeof(double)));
 
     unsigned* flag = ctx->flags + kNsFlagWord;
-    ABS_CUDA_TRY(ctx, launch_dependent(ns_norm_kernel, dim3(kNormParts, w.Z), dim3(kPassThreads), 0, st, src, q0, w.part, flag));
+    // enough CTAs to fill the GPU, at least four groups of elements per thread
+    const long long vecs = static_cast<long long>(src.rows) * src.cols / 4;
+    long long parts = (static_cast<long long>(ctx->sm_count) * 8 + w.Z - 1) / w.Z;
+    if (parts > vecs / (4 * kPassThreads)) parts = vecs / (4 * kPassThreads);
+    if (parts < 1) parts = 1;
+    if (parts > kNormParts) parts = kNormParts;
+    ABS_CUDA_TRY(ctx, launch_dependent(src_vec ? ns_norm_kernel<4> : ns_norm_kernel<1>, dim3(static_cast<unsigned>(parts), w.Z),
+                                       dim3(kPassThreads), 0, st, src, q0, w.part, flag));
     const dim3 tiles(static_cast<unsigned>(tiles_c) * tiles_r, w.Z);
-    ABS_CUDA_TRY(ctx, launch_dependent(ns_split_kernel, tiles, dim3(kPassThreads), 0, st, src, q0, w, cfg->eps, sc.sx[0], tiles_c));
+    ABS_CUDA_TRY(ctx, launch_dependent(src_vec ? ns_split_kernel<4> : ns_split_kernel<1>, tiles, dim3(kPassThreads), 0, st, src,
+                                       q0, w, static_cast<int>(parts), cfg->eps, sc.sx[0], tiles_c));
     int cur = 0;
     for (int k = 0; k < cfg->steps; ++k, cur ^= 1) {
       const int rc = launch_ns_step(ctx, w, cur, cfg->a, cfg->b, cfg->c, sc.sx[k], sc.ta[k], sc.tb[k], sc.sx[k + 1], p.split, st);
       if (rc != ABS_OK) return rc;
     }
-    ABS_CUDA_TRY(ctx, launch_dependent(ns_finish_kernel, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur,
+    ABS_CUDA_TRY(ctx, launch_dependent(dst_vec ? ns_finish_kernel<4> : ns_finish_kernel<1>, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur,
                                        1.0f / sc.sx[cfg->steps], tiles_c, static_cast<const unsigned*>(flag)));
   }
   return ABS_OK;

@@ -37,7 +37,7 @@ struct NsBuffers {
   __half* bl;
   double* part;                    // [Z][kNormParts] partial sums of squares
 };
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 1184;
 constexpr int kNsFlagWord = 8;     // word of abs_ctx::flags that a product whose wait ran out sets (cleared by every call)
 
 // One step's three products for the whole group.  split: both parts of every operand (three

@@ -42,6 +42,7 @@ struct NsGemmParams {
   int drop_loads;             // test hook: nothing is loaded, so every wait must run out
 };
 
+__device__ __forceinline__ void fence_async_n() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tcn_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcn_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ bool elect_one_n() {
@@ -179,23 +180,67 @@ __device__ __forceinline__ void finish32(const NsGemmParams& p, int z, int r, in
   }
 }
 
+// The epilogue works through a tile in pieces of 32 columns: kPieces buffers of 16 KB in shared memory,
+// each two halves of 8 KB: what is read and written in place (fp16 values; remainders for kUpdate) or,
+// for a symmetric result, the values and their mirror image.  One thread of warp 2 moves the pieces by
+// TMA: it stores a finished piece, waits until the store has read the buffer, and loads the piece that
+// takes its place.
+constexpr int kPieces = 4;
+constexpr int kPieceCols = 32;
+constexpr uint32_t kHalfPiece = kBM * kPieceCols * 2;      // 8 KB
+constexpr uint32_t kPieceBytes = 2 * kHalfPiece;
+
+struct NsMaps {
+  CUtensorMap a, b;            // operands
+  CUtensorMap in_h, in_l;      // pieces of the matrix that the epilogue reads, 64-byte swizzle
+  CUtensorMap out_h, out_l;    // pieces of the result, 64-byte swizzle
+  CUtensorMap mirror;          // transposed pieces of a symmetric result, no swizzle
+};
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src),
+               "r"(x), "r"(y), "r"(z)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[j]);
+}
+__device__ __forceinline__ void sts128_n(uint32_t addr, const uint32_t (&v)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ void sts16_n(uint32_t addr, __half h) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(__half_as_ushort(h)) : "memory");
+}
+
 // BN: tile columns.  B_MN: the second operand is MN-major (kUpdate).
-template <int BN, bool B_MN>
+template <int BN, int MODE>
 __global__ void __launch_bounds__(kThreadsN, 1)
-ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-               const NsGemmParams p) {
+ns_gemm_kernel(const __grid_constant__ NsMaps maps, const NsGemmParams p) {
+  constexpr bool B_MN = MODE == kUpdate;
   constexpr uint32_t kBBytes = BN * 128;
   constexpr uint32_t kStage = kABytes + kBBytes;
-  constexpr int kStages = BN == 256 ? 4 : 6;
+  constexpr int kStages = BN == 256 ? 3 : 5;
+  constexpr int kTilePieces = BN / kPieceCols;
   extern __shared__ unsigned char smem_dyn[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t raw = smem_u32(smem_dyn), ring = (raw + 1023u) & ~1023u;
-  unsigned char* tail = smem_dyn + (ring - raw) + static_cast<size_t>(kStages) * kStage;
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(tail);     // full, empty, accfull[2], accempty[2], done
-  volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + 2 * kStages + 5);
+  const uint32_t pieces = ring + kStages * kStage;
+  unsigned char* tail = smem_dyn + (ring - raw) + static_cast<size_t>(kStages) * kStage + kPieces * kPieceBytes;
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(tail);
+  constexpr int kBars = 2 * kStages + 5 + 2 * kPieces;
+  volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   const uint32_t full = smem_u32(bars), empty = full + 8u * kStages, accfull = empty + 8u * kStages,
-                 accempty = accfull + 16u, done = accempty + 16u;
+                 accempty = accfull + 16u, done = accempty + 16u, ready = done + 8u, filled = ready + 8u * kPieces;
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + 8u * s, 1);
@@ -206,6 +251,10 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       mbar_init(accempty + 8u * k, kEpiWarpsN * 32);
     }
     mbar_init(done, 1);
+    for (int k = 0; k < kPieces; ++k) {
+      mbar_init(ready + 8u * k, 1);                      // the buffer is loaded (or free)
+      mbar_init(filled + 8u * k, kEpiWarpsN * 32);       // the piece is finished
+    }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -225,6 +274,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   const long long step = gridDim.x;
 
   if (warp == 0) {
+    // ---- operand loads ---------------------------------------------------------------------------
     if (elect_one_n()) {
       int s = 0;
       uint32_t pass = 0;
@@ -235,13 +285,13 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           if (pass > 0 && !mbar_wait(empty + 8u * s, (pass - 1) & 1u, abort_flag, p.timeout_cycles)) break;
           const uint32_t st = ring + static_cast<uint32_t>(s) * kStage;
           mbar_expect_tx(full + 8u * s, kStage);
-          tma_load_3d(st, &map_a, kb * kBK, i * kBM, z, full + 8u * s);
+          tma_load_3d(st, &maps.a, kb * kBK, i * kBM, z, full + 8u * s);
           if (B_MN) {
 #pragma unroll
             for (int q = 0; q < BN / 64; ++q)      // blocks of [64 values of k] x [64 columns]
-              tma_load_3d(st + kABytes + q * 8192u, &map_b, j * BN + q * 64, kb * kBK, z, full + 8u * s);
+              tma_load_3d(st + kABytes + q * 8192u, &maps.b, j * BN + q * 64, kb * kBK, z, full + 8u * s);
           } else {
-            tma_load_3d(st + kABytes, &map_b, kb * kBK, j * BN, z, full + 8u * s);
+            tma_load_3d(st + kABytes, &maps.b, kb * kBK, j * BN, z, full + 8u * s);
           }
           if (++s == kStages) {
             s = 0;
@@ -254,6 +304,7 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     __syncwarp();
   } else if (warp == 1) {
+    // ---- products ----------------------------------------------------------------------------------
     const uint32_t idesc = (1u << 4) | (B_MN ? (1u << 16) : 0u) | (static_cast<uint32_t>(BN >> 3) << 17) |
                            (static_cast<uint32_t>(kBM >> 4) << 24);
     // K-major, 128-byte swizzle: 8-row groups 1024 bytes apart, 16 values of k are 32 bytes.
@@ -295,30 +346,131 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncwarp();
     volatile unsigned ignore = 0u;
     mbar_wait(done, 0u, &ignore, p.timeout_cycles);           // no product in flight when tensor memory is freed
-  } else if (warp >= kFirstEpi) {
-    const int q = warp & 3, part = (warp - kFirstEpi) >> 2;
-    constexpr int kCols = BN / 2;
-    uint32_t it = 0;
-    for (long long t = blockIdx.x; t < p.tiles; t += step, ++it) {
-      int z, i, j;
-      tile_of(p, t, BN, z, i, j);
-      const uint32_t buf = it & 1u, use = it >> 1;
-      const bool arrived = mbar_wait(accfull + 8u * buf, use & 1u, abort_flag, p.timeout_cycles);
-      if (!__all_sync(0xffffffffu, arrived)) break;
-      tcn_after();
-      const int r = i * kBM + q * 32 + lane;
-      const uint32_t taddr = tmem + buf * BN + static_cast<uint32_t>(part * kCols) + (static_cast<uint32_t>(q * 32) << 16);
-#pragma unroll 1
-      for (int c32 = 0; c32 < kCols; c32 += 32) {
-        const int c = j * BN + part * kCols + c32;
-        const int col_block = c / kBM;
-        float v[32];
-        tmem_ld32(taddr + static_cast<uint32_t>(c32), v);
-        if (c >= p.n || (p.mode != kUpdate && col_block > i)) continue;      // the mirror image is stored elsewhere
-        finish32<false>(p, z, r, c, v, col_block < i);
+  } else if (warp == 2) {
+    // ---- pieces of the epilogue: store the finished one, load the one that takes its buffer ---------
+    if (elect_one_n()) {
+      long long t_in = blockIdx.x;                             // the piece that is loaded next
+      int piece_in = 0;
+      uint32_t issued = 0;
+      auto load_next = [&](uint32_t b) {
+        if (t_in >= p.tiles) return;
+        int z, i, j;
+        tile_of(p, t_in, BN, z, i, j);
+        const uint32_t at = pieces + b * kPieceBytes, bar = ready + 8u * b;
+        const int c = j * BN + piece_in * kPieceCols;
+        if (MODE == kGram || p.drop_loads) {
+          mbar_arrive(bar);
+        } else {
+          mbar_expect_tx(bar, MODE == kUpdate ? kPieceBytes : kHalfPiece);
+          tma_load_3d(at, &maps.in_h, c, i * kBM, z, bar);
+          if (MODE == kUpdate) tma_load_3d(at + kHalfPiece, &maps.in_l, c, i * kBM, z, bar);
+        }
+        ++issued;
+        if (++piece_in == kTilePieces) {
+          piece_in = 0;
+          t_in += step;
+        }
+      };
+      for (uint32_t b = 0; b < kPieces; ++b) load_next(b);
+      uint32_t n = 0;                                          // pieces stored so far
+      for (long long t = blockIdx.x; t < p.tiles; t += step) {
+        int z, i, j;
+        tile_of(p, t, BN, z, i, j);
+        bool ok = true;
+        for (int piece = 0; piece < kTilePieces && ok; ++piece, ++n) {
+          const uint32_t b = n % kPieces;
+          ok = mbar_wait(filled + 8u * b, (n / kPieces) & 1u, abort_flag, p.timeout_cycles);
+          if (!ok) break;
+          const uint32_t at = pieces + b * kPieceBytes;
+          const int c = j * BN + piece * kPieceCols;
+          tma_store_3d(&maps.out_h, at, c, i * kBM, z);
+          if (MODE == kUpdate) tma_store_3d(&maps.out_l, at + kHalfPiece, c, i * kBM, z);
+          else if (c / kBM < i) tma_store_3d(&maps.mirror, at + kHalfPiece, i * kBM, c, z);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          load_next(b);
+        }
+        if (!ok) break;
       }
-      tcn_before();
-      mbar_arrive(accempty + 8u * buf);
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      // no load in flight when the CTA exits (buffers are loaded in turn)
+      volatile unsigned ignore = 0u;
+      for (uint32_t b = 0; b < kPieces && b < issued; ++b) {
+        const uint32_t last = (issued - 1 - b) / kPieces;      // passes of buffer b, minus one
+        mbar_wait(ready + 8u * b, last & 1u, &ignore, p.timeout_cycles);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= kFirstEpi) {
+    // ---- epilogue: lanes are rows; the two warps of a quarter take 16 of a piece's 32 columns each ---
+    const int q = warp & 3, part = (warp - kFirstEpi) >> 2;
+    const uint32_t row = static_cast<uint32_t>(q * 32 + lane), sw = (row >> 1) & 3u;
+    uint32_t it = 0, n = 0;
+    bool ok = true;
+    for (long long t = blockIdx.x; t < p.tiles && ok; t += step, ++it) {
+      const uint32_t buf = it & 1u, use = it >> 1;
+      ok = __all_sync(0xffffffffu, mbar_wait(accfull + 8u * buf, use & 1u, abort_flag, p.timeout_cycles));
+      if (!ok) break;
+      tcn_after();
+      const uint32_t taddr = tmem + buf * BN + static_cast<uint32_t>(part * 16) + (static_cast<uint32_t>(q * 32) << 16);
+#pragma unroll 1
+      for (int piece = 0; piece < kTilePieces; ++piece, ++n) {
+        const uint32_t b = n % kPieces;
+        float v[16];
+        tmem_ld16(taddr + static_cast<uint32_t>(piece * kPieceCols), v);
+        if (piece == kTilePieces - 1) {                        // the accumulator is in registers: hand it back
+          tcn_before();
+          mbar_arrive(accempty + 8u * buf);
+        }
+        ok = __all_sync(0xffffffffu, mbar_wait(ready + 8u * b, (n / kPieces) & 1u, abort_flag, p.timeout_cycles));
+        if (!ok) break;
+        const uint32_t at = pieces + b * kPieceBytes;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {                          // 8 columns: one 16-byte chunk
+          const uint32_t chunk = static_cast<uint32_t>(part * 2 + g);
+          const uint32_t addr = at + row * 64u + ((chunk ^ sw) << 4);
+          float* w = v + 8 * g;
+          if (MODE == kGram) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] *= p.c_acc;
+          } else {
+            const uint4 h = lds128(addr);
+            const uint32_t hh[4] = {h.x, h.y, h.z, h.w};
+            uint4 l = make_uint4(0u, 0u, 0u, 0u);
+            if (MODE == kUpdate) l = lds128(addr + kHalfPiece);
+            const uint32_t ll[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 x = unpack_half2(hh[e]), y = unpack_half2(ll[e]);
+              w[2 * e] = fmaf(p.c_acc, w[2 * e], p.c_in * (x.x + y.x));
+              w[2 * e + 1] = fmaf(p.c_acc, w[2 * e + 1], p.c_in * (x.y + y.y));
+            }
+          }
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) h[e] = pack_half2(w[2 * e], w[2 * e + 1]);
+          sts128_n(addr, h);
+          if (MODE == kUpdate) {
+            uint32_t l[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = unpack_half2(h[e]);
+              l[e] = pack_half2(w[2 * e] - f.x, w[2 * e + 1] - f.y);
+            }
+            sts128_n(addr + kHalfPiece, l);
+          } else {                                             // mirror image: row = column, 256 bytes a row
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t base = at + kHalfPiece + (chunk * 8u + 2u * e) * 256u + row * 2u;
+              const __half2 hv = *reinterpret_cast<const __half2*>(&h[e]);
+              sts16_n(base, __low2half(hv));
+              sts16_n(base + 256u, __high2half(hv));
+            }
+          }
+        }
+        fence_async_n();
+        mbar_arrive(filled + 8u * b);
+      }
     }
   }
   tcn_before();
@@ -486,15 +638,15 @@ ns_gemm_split_kernel(const __grid_constant__ CUtensorMap map_ah, const __grid_co
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// [Z][rows][cols] fp16 matrix with boxes of [box_rows][64]; what lies outside reads as zero.
+// [Z][rows][cols] fp16 matrix with boxes of [box_rows][box_cols]; what lies outside reads as zero and is not written.
 int encode_half_map(abs_ctx* ctx, const __half* base, int Z, int rows, int cols, long long ld, int box_rows,
-                    CUtensorMap* map) {
+                    CUtensorMap* map, int box_cols = 64, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   const cuuint64_t gdim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(Z)};
   const cuuint64_t gstr[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * rows};
-  const cuuint32_t box[3] = {64u, static_cast<cuuint32_t>(box_rows), 1u};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   const CUresult r = encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), gdim, gstr, box,
-                                       estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                       estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS)
     return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (matrix) failed with code %d", static_cast<int>(r));
@@ -515,19 +667,30 @@ void count_tiles(NsGemmParams& p, int bn) {
 
 constexpr size_t ns_smem(int stages, uint32_t stage_bytes) { return static_cast<size_t>(stages) * stage_bytes + 1024 + 256; }
 
-template <int BN, bool B_MN>
+template <int BN, int MODE>
 int launch_plain(abs_ctx* ctx, NsGemmParams p, const __half* a, int a_rows, int a_cols, long long a_ld, const __half* b,
                  int b_rows, int b_cols, long long b_ld, cudaStream_t st) {
-  CUtensorMap ma, mb;
-  int rc = encode_half_map(ctx, a, p.Z, a_rows, a_cols, a_ld, kBM, &ma);
-  if (rc == ABS_OK) rc = encode_half_map(ctx, b, p.Z, b_rows, b_cols, b_ld, B_MN ? 64 : BN, &mb);
+  p.mode = MODE;
+  NsMaps maps;
+  const __half* in_h = MODE == kGram ? p.out_h : p.in_h;        // unused maps are given a valid matrix
+  const __half* in_l = MODE == kUpdate ? p.in_l : in_h;
+  const __half* out_l = MODE == kUpdate ? p.out_l : p.out_h;
+  const CUtensorMapSwizzle s64 = CU_TENSOR_MAP_SWIZZLE_64B;
+  int rc = encode_half_map(ctx, a, p.Z, a_rows, a_cols, a_ld, kBM, &maps.a);
+  if (rc == ABS_OK) rc = encode_half_map(ctx, b, p.Z, b_rows, b_cols, b_ld, MODE == kUpdate ? 64 : BN, &maps.b);
+  if (rc == ABS_OK) rc = encode_half_map(ctx, in_h, p.Z, p.m, p.n, p.ld, kBM, &maps.in_h, kPieceCols, s64);
+  if (rc == ABS_OK) rc = encode_half_map(ctx, in_l, p.Z, p.m, p.n, p.ld, kBM, &maps.in_l, kPieceCols, s64);
+  if (rc == ABS_OK) rc = encode_half_map(ctx, p.out_h, p.Z, p.m, p.n, p.ld, kBM, &maps.out_h, kPieceCols, s64);
+  if (rc == ABS_OK) rc = encode_half_map(ctx, out_l, p.Z, p.m, p.n, p.ld, kBM, &maps.out_l, kPieceCols, s64);
+  if (rc == ABS_OK)
+    rc = encode_half_map(ctx, p.out_h, p.Z, p.m, p.n, p.ld, kPieceCols, &maps.mirror, kBM, CU_TENSOR_MAP_SWIZZLE_NONE);
   if (rc != ABS_OK) return rc;
   count_tiles(p, BN);
-  const size_t smem = ns_smem(BN == 256 ? 4 : 6, kABytes + BN * 128);
-  auto kern = ns_gemm_kernel<BN, B_MN>;
+  const size_t smem = ns_smem(BN == 256 ? 3 : 5, kABytes + BN * 128) + kPieces * kPieceBytes;
+  auto kern = ns_gemm_kernel<BN, MODE>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
   const unsigned grid = static_cast<unsigned>(p.tiles < ctx->sm_count ? p.tiles : ctx->sm_count);
-  ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(grid), dim3(kThreadsN), smem, st, ma, mb, p));
+  ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(grid), dim3(kThreadsN), smem, st, maps, p));
   return ABS_OK;
 }
 
@@ -569,7 +732,7 @@ int launch_ns_step(abs_ctx* ctx, const NsBuffers& w, int cur, float a, float b, 
   p.c_acc = ta / (sx * sx);
   p.out_h = w.ah; p.out_l = w.al;
   int rc = split ? launch_split<false>(ctx, p, xh, xl, w.m, w.n, w.ldx, xh, xl, w.m, w.n, w.ldx, st)
-                 : launch_plain<128, false>(ctx, p, xh, w.m, w.n, w.ldx, xh, w.m, w.n, w.ldx, st);
+                 : launch_plain<128, kGram>(ctx, p, xh, w.m, w.n, w.ldx, xh, w.m, w.n, w.ldx, st);
   if (rc != ABS_OK) return rc;
   // B = b A + c A A
   p.mode = kPoly;
@@ -579,7 +742,7 @@ int launch_ns_step(abs_ctx* ctx, const NsBuffers& w, int cur, float a, float b, 
   p.c_in = b * (tb / ta);
   p.c_acc = c * (tb / (ta * ta));
   rc = split ? launch_split<false>(ctx, p, w.ah, w.al, w.m, w.m, w.ldm, w.ah, w.al, w.m, w.m, w.ldm, st)
-             : launch_plain<128, false>(ctx, p, w.ah, w.m, w.m, w.ldm, w.ah, w.m, w.m, w.ldm, st);
+             : launch_plain<128, kPoly>(ctx, p, w.ah, w.m, w.m, w.ldm, w.ah, w.m, w.m, w.ldm, st);
   if (rc != ABS_OK) return rc;
   // X <- a X + B X
   p.mode = kUpdate;
@@ -591,7 +754,7 @@ int launch_ns_step(abs_ctx* ctx, const NsBuffers& w, int cur, float a, float b, 
   p.c_in = a * (sx_next / sx);
   p.c_acc = sx_next / (tb * sx);
   if (split) return launch_split<true>(ctx, p, w.bh, w.bl, w.m, w.m, w.ldm, xh, xl, w.m, w.n, w.ldx, st);
-  return launch_plain<256, true>(ctx, p, w.bh, w.m, w.m, w.ldm, xh, w.m, w.n, w.ldx, st);
+  return launch_plain<256, kUpdate>(ctx, p, w.bh, w.m, w.m, w.ldm, xh, w.m, w.n, w.ldx, st);
 }
 
 }  // namespace absk
