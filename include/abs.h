@@ -89,7 +89,8 @@ const char* abs_last_error(const abs_ctx* ctx);
  * cluster and tcgen05 kernels issue no copies, abs_logreg_rounds_fused sends no
  * partial gradients and the tensor-core products of the MLP producer fill no
  * operand tile, so every wait runs out and the records come back flagged
- * ABS_STATUS_TIMEOUT; nothing traps or hangs),
+ * ABS_STATUS_TIMEOUT; the Newton-Schulz products load nothing and their results are
+ * NaN; nothing traps or hangs),
  * "stats_cluster_rows" (target rows per CTA of the cluster kernel, 16..512),
  * "stats_no_cluster" (1 = do not split the rows of a batch over a thread-block
  * cluster when b > 256),
@@ -103,6 +104,8 @@ const char* abs_last_error(const abs_ctx* ctx);
  * "stats_no_gram" (1 = do not use the tensor-core Gram kernels for bf16, b <= 256),
  * "stats_no_recheck" (1 = keep a Gram kernel's record even when its sums are
  * ill-conditioned, i.e. never recompute it with the tiled kernel),
+ * "ns_pair_tiles" (tiles of the Newton-Schulz products with fp16 operands: 1 =
+ * 128 x 128 on single CTAs, 2 = 256 x 256 on pairs of CTAs),
  * "stats_ctas_per_sm" (1: one CTA per SM, 64 KiB buffers, up to 16 rows per
  * thread; 2: two CTAs per SM, 32 KiB buffers, up to 8 rows per thread).
  * Unknown key or out-of-range value: ABS_ERR_INVALID_ARG. */

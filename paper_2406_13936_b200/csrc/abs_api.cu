@@ -196,6 +196,9 @@ extern "C" int abs_set_tuning(abs_ctx* ctx, const char* key, long long value) {
     ctx->tuning.stats_no_cluster = value ? 1 : 0;
   } else if (strcmp(key, "stats_no_gram") == 0) {
     ctx->tuning.stats_no_gram = value ? 1 : 0;
+  } else if (strcmp(key, "ns_pair_tiles") == 0) {
+    if (value > 2) return set_error(ctx, ABS_ERR_INVALID_ARG, "ns_pair_tiles must be 0, 1 or 2");
+    ctx->tuning.ns_pair_tiles = value;
   } else if (strcmp(key, "stats_ctas_per_sm") == 0) {
     if (value > 2) return set_error(ctx, ABS_ERR_INVALID_ARG, "stats_ctas_per_sm must be 0, 1 or 2");
     ctx->tuning.stats_ctas_per_sm = value;

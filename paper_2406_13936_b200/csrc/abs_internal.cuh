@@ -34,6 +34,7 @@ struct Tuning {
   long long stats_no_recheck = 0;          // 1: keep a Gram kernel's record whatever its conditioning
   long long stats_cluster_rows = 0;
   long long stats_timeout_cycles = 0;      // 0: about two seconds of SM clock
+  long long ns_pair_tiles = 0;             // Newton-Schulz products: 1 single-CTA tiles, 2 CTA-pair tiles
   long long stats_fault_drop_loads = 0;    // test hook: the tiled kernel's loader issues no copies
 };
 

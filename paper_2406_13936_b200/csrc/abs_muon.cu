@@ -100,12 +100,15 @@ __device__ __forceinline__ void load_update(const NsSource& s, long long i, floa
 // V = 4: every group of four elements is 16-byte aligned and lies in one row.
 template <int V>
 __global__ void __launch_bounds__(kPassThreads)
-ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* flag) {
+ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* __restrict__ progress, int counters,
+               unsigned* flag) {
   __shared__ double red[kPassThreads / 32];
   const int z = blockIdx.y;
   pdl_launch_dependents();
   pdl_wait();
   if (blockIdx.x == 0 && z == 0 && threadIdx.x == 0 && q0 == 0) *flag = 0u;
+  if (blockIdx.x == 0)
+    for (int k = threadIdx.x; k < counters; k += kPassThreads) progress[z * counters + k] = 0u;
   const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
   const bool flat = s.row_stride == s.cols;                    // one row of rows * cols elements
   const int per_row = s.cols / V;
@@ -344,7 +347,8 @@ struct NsPlan {
   long long ldx, ldm, x_halves, m_halves;    // per matrix
   bool split;
   size_t per_matrix() const {
-    return static_cast<size_t>(4 * x_halves + (split ? 4 : 2) * m_halves) * 2 + kNormParts * sizeof(double);
+    return static_cast<size_t>(4 * x_halves + (split ? 4 : 2) * m_halves) * 2 + kNormParts * sizeof(double) +
+           static_cast<size_t>(3 * ns_row_blocks(m)) * sizeof(unsigned);
   }
 };
 constexpr size_t kNsFixedBytes = 16 * 1024;       // alignment of the buffers
@@ -429,6 +433,7 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
       w.bl = static_cast<__half*>(take(mb));
     }
     w.part = static_cast<double*>(take(static_cast<size_t>(zmax) * kNormParts * sizeof(double)));
+    w.progress = static_cast<unsigned*>(take(static_cast<size_t>(zmax) * 3 * ns_row_blocks(p.m) * sizeof(unsigned)));
 
     unsigned* flag = ctx->flags + kNsFlagWord;
     // enough CTAs to fill the GPU, at least four groups of elements per thread
@@ -438,15 +443,13 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
     if (parts < 1) parts = 1;
     if (parts > kNormParts) parts = kNormParts;
     ABS_CUDA_TRY(ctx, launch_dependent(src_vec ? ns_norm_kernel<4> : ns_norm_kernel<1>, dim3(static_cast<unsigned>(parts), w.Z),
-                                       dim3(kPassThreads), 0, st, src, q0, w.part, flag));
+                                       dim3(kPassThreads), 0, st, src, q0, w.part, w.progress, 3 * ns_row_blocks(p.m), flag));
     const dim3 tiles(static_cast<unsigned>(tiles_c) * tiles_r, w.Z);
     ABS_CUDA_TRY(ctx, launch_dependent(src_vec ? ns_split_kernel<4> : ns_split_kernel<1>, tiles, dim3(kPassThreads), 0, st, src,
                                        q0, w, static_cast<int>(parts), cfg->eps, sc.sx[0], tiles_c));
-    int cur = 0;
-    for (int k = 0; k < cfg->steps; ++k, cur ^= 1) {
-      const int rc = launch_ns_step(ctx, w, cur, cfg->a, cfg->b, cfg->c, sc.sx[k], sc.ta[k], sc.tb[k], sc.sx[k + 1], p.split, st);
-      if (rc != ABS_OK) return rc;
-    }
+    const int rc = launch_ns_steps(ctx, w, cfg->steps, cfg->a, cfg->b, cfg->c, sc, p.split, st);
+    if (rc != ABS_OK) return rc;
+    const int cur = cfg->steps & 1;
     ABS_CUDA_TRY(ctx, launch_dependent(dst_vec ? ns_finish_kernel<4> : ns_finish_kernel<1>, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur,
                                        1.0f / sc.sx[cfg->steps], tiles_c, static_cast<const unsigned*>(flag)));
   }

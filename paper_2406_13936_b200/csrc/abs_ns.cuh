@@ -25,7 +25,7 @@ struct NsScales {
   float tb[kNsMaxSteps];       // B
 };
 
-// Device buffers of one group of Z matrices.  X is double-buffered: a step reads cur, writes cur ^ 1.
+// Device buffers of one group of Z matrices.  X is double-buffered: step k reads k & 1, writes the other.
 struct NsBuffers {
   int Z, m, n;
   long long ldx, ldm;              // leading dimensions in elements, multiples of 8
@@ -36,13 +36,15 @@ struct NsBuffers {
   __half* bh;
   __half* bl;
   double* part;                    // [Z][kNormParts] partial sums of squares
+  unsigned* progress;              // [Z][3][kNsRowBlocks(m)] finished tiles of X, A, B, zero before the products
 };
 constexpr int kNormParts = 1184;
 constexpr int kNsFlagWord = 8;     // word of abs_ctx::flags that a product whose wait ran out sets (cleared by every call)
+inline int ns_row_blocks(int m) { return (m + 127) / 128; }
 
-// One step's three products for the whole group.  split: both parts of every operand (three
-// tensor-core products, fp32-grade); else the fp16 values alone.
-int launch_ns_step(abs_ctx* ctx, const NsBuffers& w, int cur, float a, float b, float c, float sx, float ta, float tb,
-                   float sx_next, bool split, cudaStream_t st);
+// All steps of a group in one launch.  split: both parts of every operand (three tensor-core products,
+// fp32-grade); else the fp16 values alone.
+int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float b, float c, const NsScales& sc, bool split,
+                    cudaStream_t st);
 
 }  // namespace absk
