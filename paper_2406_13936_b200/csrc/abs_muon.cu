@@ -5,7 +5,7 @@
 //   A = X X',   X <- a X + (b A + c A^2) X          (on the short side, m <= n).
 //
 // Rounding.  The products run on fp16 operands (11 significant bits, fp32 accumulation); X itself is
-// carried as hi + lo (22 bits) and the linear term uses both.  Small singular values grow by a factor a
+// carried in fp32, which the linear term uses.  Small singular values grow by a factor a
 // in every step (3.4445^5 = 485), and only through the linear term: rounding X to 11 bits there would
 // lift the rounding noise of large directions into empty ones (fp16 simulation, 512 x 1024 of rank 8:
 // 4e-2 of the result's norm; bfloat16 0.35), while rounding inside B X stays in proportion to B X
@@ -199,18 +199,19 @@ ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float ep
     const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
     const int i = (tall ? tc : tr) * kTile + ri, j = (tall ? tr : tc) * kTile + cj;      // row and column of X
     if (i >= w.m || j >= w.n) continue;                        // ldx is a multiple of 8: four columns stay in the row
-    __half2 h[2], l[2];
+    float x[4];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float a = static_cast<float>((tall ? tile[ri][cj + 2 * e] : u[k][2 * e]) * scale);
-      const float b = static_cast<float>((tall ? tile[ri][cj + 2 * e + 1] : u[k][2 * e + 1]) * scale);
-      h[e] = __floats2half2_rn(a, b);
-      const float2 f = __half22float2(h[e]);
-      l[e] = __floats2half2_rn(a - f.x, b - f.y);
-    }
+    for (int e = 0; e < 4; ++e) x[e] = static_cast<float>((tall ? tile[ri][cj + e] : u[k][e]) * scale);
+    const __half2 h[2] = {__floats2half2_rn(x[0], x[1]), __floats2half2_rn(x[2], x[3])};
     const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
     *reinterpret_cast<uint2*>(w.xh[0] + o) = *reinterpret_cast<const uint2*>(h);
-    *reinterpret_cast<uint2*>(w.xl[0] + o) = *reinterpret_cast<const uint2*>(l);
+    if (w.xf != nullptr) {
+      *reinterpret_cast<float4*>(w.xf + o) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+      const float2 f0 = __half22float2(h[0]), f1 = __half22float2(h[1]);
+      const __half2 l[2] = {__floats2half2_rn(x[0] - f0.x, x[1] - f0.y), __floats2half2_rn(x[2] - f1.x, x[3] - f1.y)};
+      *reinterpret_cast<uint2*>(w.xl[0] + o) = *reinterpret_cast<const uint2*>(l);
+    }
   }
 }
 
@@ -232,18 +233,22 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
   for (int k = 0; k < kTileVecs; ++k) {
     const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
     const int i = (tall ? tc : tr) * kTile + ri, j = (tall ? tr : tc) * kTile + cj;
-    uint2 h = make_uint2(0u, 0u), l = make_uint2(0u, 0u);
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < w.m && j < w.n) {
       const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
-      h = *reinterpret_cast<const uint2*>(w.xh[cur] + o);
-      l = *reinterpret_cast<const uint2*>(w.xl[cur] + o);
+      if (w.xf != nullptr) {
+        x = *reinterpret_cast<const float4*>(w.xf + o);
+      } else {
+        const uint2 h = *reinterpret_cast<const uint2*>(w.xh[cur] + o), l = *reinterpret_cast<const uint2*>(w.xl[cur] + o);
+        const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x));
+        const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
+        x = make_float4(h0.x + l0.x, h0.y + l0.y, h1.x + l1.x, h1.y + l1.y);
+      }
     }
-    const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y));
-    const float2 l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
-    u[k][0] = (h0.x + l0.x) * inv_sx + bad;
-    u[k][1] = (h0.y + l0.y) * inv_sx + bad;
-    u[k][2] = (h1.x + l1.x) * inv_sx + bad;
-    u[k][3] = (h1.y + l1.y) * inv_sx + bad;
+    u[k][0] = x.x * inv_sx + bad;
+    u[k][1] = x.y * inv_sx + bad;
+    u[k][2] = x.z * inv_sx + bad;
+    u[k][3] = x.w * inv_sx + bad;
     if (tall) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) tile[cj + e][ri] = u[k][e];
@@ -351,9 +356,9 @@ struct NsPlan {
            static_cast<size_t>(3 * ns_row_blocks(m)) * sizeof(unsigned);
   }
 };
-constexpr size_t kNsFixedBytes = 16 * 1024;       // alignment of the buffers
+constexpr size_t kNsFixedBytes = 16 * 1024;       // alignment of the (at most ten) buffers
 // Matrices that are worked on together: as many as keep what a step reads and writes inside L2.
-constexpr size_t kGroupBytes = 96ull << 20;
+constexpr size_t kGroupBytes = 128ull << 20;
 
 NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
   NsPlan p;
@@ -422,9 +427,10 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
       return r;
     };
     const size_t xb = static_cast<size_t>(p.x_halves) * zmax * 2, mb = static_cast<size_t>(p.m_halves) * zmax * 2;
+    if (!p.split) w.xf = static_cast<float*>(take(2 * xb));
     for (int k = 0; k < 2; ++k) {
       w.xh[k] = static_cast<__half*>(take(xb));
-      w.xl[k] = static_cast<__half*>(take(xb));
+      if (p.split) w.xl[k] = static_cast<__half*>(take(xb));
     }
     w.ah = static_cast<__half*>(take(mb));
     w.bh = static_cast<__half*>(take(mb));

@@ -2,11 +2,12 @@
 // products (abs_ns_gemm.cu) share.
 //
 // One matrix is held with its short side as rows, X [m][n], m <= n (a tall matrix is transposed when
-// it is read and again when the result is written), as X = hi + lo in two fp16 matrices.  A step is
+// it is read and again when the result is written), in fp32 and, rounded, in fp16.  A step is
 //   A = X X',   B = b A + c A A,   X <- a X + B X,
-// three products whose operands are the fp16 (hi) values; the a X term takes hi + lo, so what 11
+// three products whose operands are the fp16 values; the a X term takes the fp32 ones, so what 11
 // bits of an operand lose is always in proportion to B X and never fills directions that the
-// gradient does not have (see abs_muon.cu).
+// gradient does not have (see abs_muon.cu).  With split operands every matrix is held as two fp16
+// matrices, values and remainders, and a product is three tensor-core products.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -25,15 +26,16 @@ struct NsScales {
   float tb[kNsMaxSteps];       // B
 };
 
-// Device buffers of one group of Z matrices.  X is double-buffered: step k reads k & 1, writes the other.
+// Device buffers of one group of Z matrices.  Step k reads the fp16 X (and remainders) of k & 1 and writes the other.
 struct NsBuffers {
   int Z, m, n;
   long long ldx, ldm;              // leading dimensions in elements, multiples of 8
+  float* xf;                       // X in fp32, changed in place (not with split operands)
   __half* xh[2];
-  __half* xl[2];                   // low parts: the a X term and, with split operands, the products
   __half* ah;
-  __half* al;                      // low parts of A and B: split operands only
   __half* bh;
+  __half* xl[2];                   // remainders: split operands only
+  __half* al;
   __half* bl;
   double* part;                    // [Z][kNormParts] partial sums of squares
   unsigned* progress;              // [Z][3][kNsRowBlocks(m)] finished tiles of X, A, B, zero before the products
@@ -42,8 +44,7 @@ constexpr int kNormParts = 1184;
 constexpr int kNsFlagWord = 8;     // word of abs_ctx::flags that a product whose wait ran out sets (cleared by every call)
 inline int ns_row_blocks(int m) { return (m + 127) / 128; }
 
-// All steps of a group in one launch.  split: both parts of every operand (three tensor-core products,
-// fp32-grade); else the fp16 values alone.
+// All steps of a group in one launch.
 int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float b, float c, const NsScales& sc, bool split,
                     cudaStream_t st);
 

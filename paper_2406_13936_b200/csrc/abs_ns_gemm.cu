@@ -1,9 +1,12 @@
 // All steps of the Newton-Schulz iteration of a group of matrices in one launch, on the tcgen05 tensor
 // cores.  A step is three products:
-//   kGram    A = X X'                      both operands K-major rows of X, result symmetric
-//   kPoly    B = b A + c A A               both operands K-major rows of A (A = A'), result symmetric
-//   kUpdate  X <- a X + B X                B K-major, X MN-major (its rows are the k index)
-// Symmetric results are computed for tiles on and below the diagonal and written to both places.
+//   kGram    A = X X'
+//   kPoly    B = b A + c A A
+//   kUpdate  X <- a X + B X
+// A and B are symmetric: only their tiles on and below the diagonal are computed and stored.  A block
+// above the diagonal is read as the transpose of the stored one, which the tensor core does by itself:
+// an operand whose k index runs along the rows of the stored matrix is MN-major (as X is in kUpdate),
+// one whose k index runs along the columns is K-major; the TMA box and the descriptor differ, no more.
 //
 // The tiles of all steps, products and matrices form one list, in that order; a resident grid walks it
 // with a fixed stride.  A tile starts when the row blocks that it reads are complete, which other CTAs
@@ -18,12 +21,17 @@
 // each CTA loads its 128 rows of the first operand and half the columns of the second, and holds its
 // 128 rows of the accumulator), which halves the operand bytes per product.
 //
+// An SM takes in about 64 bytes a clock from L2 (measured: a k-block of 64 of a 128 x 128 tile, 32 KB,
+// takes 556 clocks, its products 256), which is what a pair's tile needs at the tensor cores' full rate.
+//
 // Roles of a CTA's 12 warps: 0 loads operands by TMA into a ring of 32 KB stages, 1 issues the products
 // (fp32 accumulators in tensor memory, two of them, so the next tile's products run while this one is
-// read back), 8 warps read back, apply the step's coefficients and write pieces of 32 columns to shared
-// memory, 2 stores the pieces by TMA and announces finished tiles, 3 loads the pieces of X or A that the
-// coefficients apply to.  All waits are bounded; one that runs out raises the CTA's abort flag and the
-// call's flag word, every role falls through, copies in flight are waited for and tensor memory is freed.
+// read back), 4-7 and 8-11 are the two halves of the epilogue (each reads back half the tile's columns and
+// applies the coefficients in place, in shared memory), 2 and 3 move the units of one half each: they load
+// what the coefficients apply to, store the results by TMA and announce the half tile, so that no epilogue
+// warp waits for a copy to finish or for a fence.  All waits are bounded; one that runs out raises the
+// CTA's abort flag and the call's flag word, every role falls through, copies in flight are waited for and
+// tensor memory is freed.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
 
@@ -36,24 +44,24 @@ constexpr int kBM = 128;                     // rows of a CTA's tile
 constexpr int kEpiWarpsN = 8;
 constexpr int kFirstEpi = 4;
 constexpr int kThreadsN = (kFirstEpi + kEpiWarpsN) * 32;   // 384
-constexpr int kStagesN = 5;
+constexpr int kStagesN = 4;
 constexpr uint32_t kStageN = 32768;
-// Pieces of the epilogue: 32 columns of the tile's 128 rows, 8 KB per matrix.  Plain operands: 4 buffers of
-// two matrices (values and remainders of X, or a symmetric result and its mirror image).  Split operands:
-// 2 buffers of four (values, remainders and their mirror images).
-constexpr int kPieceCols = 32;
-constexpr uint32_t kHalfPiece = kBM * kPieceCols * 2;      // 8 KB
-constexpr uint32_t kPieceArea = 65536;
+// Units of the epilogue: 32 columns of the tile's 128 rows, changed in place in shared memory.  A unit takes
+// 8 KB as fp16 values (A, B), 16 KB as values and remainders (any matrix with split operands), and 16 + 8 KB as
+// X in fp32 and its fp16 values.  A half of the epilogue has 48 KB: all units of its half tile, or for X on CTA
+// pairs two of the four.
+constexpr int kUnitCols = 32;
+constexpr uint32_t kUnitBytes = kBM * kUnitCols * 2;       // 8 KB
+constexpr uint32_t kHalfArea = 6 * kUnitBytes;
 // Split operands: an accumulator of the main products takes kFold k-blocks of 32 (2 kFold additions) and is
 // then added, rounded to nearest, to sums in registers: the tensor core adds without rounding to nearest.
 constexpr int kFold = 8;
 
 struct NsMaps {
-  // operands: boxes of [128 rows][k-block] (K-major) and, for X as the second operand of kUpdate, of
-  // [k-block][64 columns]; _l: remainders (split operands)
-  CUtensorMap xk_h[2], xk_l[2], xm_h[2], xm_l[2], ak_h, ak_l, bk_h, bk_l;
-  // pieces: boxes of [128 rows][32 columns], and transposed ones of [32 rows][128 columns]
-  CUtensorMap xp_h[2], xp_l[2], ap_h, ap_l, bp_h, bp_l, at_h, at_l, bt_h, bt_l;
+  // operands: boxes of [128 rows][k-block] (K-major) and [k-block][64 columns] (MN-major); _l: remainders
+  CUtensorMap xk_h[2], xk_l[2], xm_h[2], xm_l[2], ak_h, ak_l, am_h, am_l, bk_h, bk_l, bm_h, bm_l;
+  // units of the epilogue: boxes of [128 rows][32 columns]
+  CUtensorMap xf, xu_h[2], xu_l[2], au_h, au_l, bu_h, bu_l;
 };
 struct NsCoef {
   float in, acc;              // result = in * (what the epilogue reads) + acc * accumulator
@@ -130,25 +138,30 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
                : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster) : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
-  uint32_t r[16];
+// 32 consecutive columns of this thread's lane; the values may be used after tmem_wait on the same registers.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr)
       : "memory");
-#pragma unroll
-  for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[j]);
+}
+__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+        "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+        "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+        "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+      :
+      : "memory");
 }
 __device__ __forceinline__ void sts128_n(uint32_t addr, const uint32_t (&v)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-__device__ __forceinline__ void sts16_n(uint32_t addr, __half h) {
-  asm volatile("st.shared.b16 [%0], %1;" ::"r"(addr), "h"(__half_as_ushort(h)) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_half2(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -186,6 +199,34 @@ __device__ __forceinline__ Tile tile_of(const NsStepsParams& p, long long t) {
   return q;
 }
 
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_f32x2(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+
+// Whether an operand's block at k0 is the transpose of the stored one (above the diagonal of A or B), or X in
+// kUpdate: its k index then runs along the rows of the stored matrix.
+__device__ __forceinline__ bool a_is_mn(const Tile& q, int k0, int bn) { return q.mode != kGram && k0 / bn > q.i; }
+__device__ __forceinline__ bool b_is_mn(const Tile& q, int k0, int bn) {
+  return q.mode == kUpdate || (q.mode == kPoly && k0 / bn > q.j);
+}
+
 // Waits (bounded) until the counter has reached `target`.
 __device__ __forceinline__ bool wait_count(const unsigned* c, unsigned target, const NsStepsParams& p, volatile unsigned* abort_flag) {
   const long long t0 = clock64();
@@ -200,19 +241,19 @@ __device__ __forceinline__ bool wait_count(const unsigned* c, unsigned target, c
     __nanosleep(32);
   }
 }
-// ... until the rows that a tile reads are complete.  Symmetric results: a row block is complete when all
-// row_blocks tiles that touch it are (its own row and, mirrored, the rows below).
+// ... until what a tile reads is complete.  Row block i of a symmetric result is read from the tiles of row
+// i and, transposed, of column i: row_blocks tiles.  Every CTA announces a tile twice (two epilogue halves).
 template <int CG>
 __device__ __forceinline__ bool wait_inputs(const NsStepsParams& p, const Tile& q, volatile unsigned* abort_flag) {
   const unsigned* base = p.progress + static_cast<long long>(q.z) * 3 * p.row_blocks;
   bool ok = true;
   if (q.mode == kGram) {
     if (q.step == 0) return true;
-    const unsigned target = static_cast<unsigned>(q.step) * p.col_tiles * CG;
+    const unsigned target = static_cast<unsigned>(q.step) * p.col_tiles * (2 * CG);
     ok = wait_count(base + q.i, target, p, abort_flag);
     if (ok && q.j != q.i) ok = wait_count(base + q.j, target, p, abort_flag);
   } else {
-    const unsigned target = static_cast<unsigned>(q.step + 1) * p.row_blocks * CG;
+    const unsigned target = static_cast<unsigned>(q.step + 1) * p.row_blocks * (2 * CG);
     const unsigned* c = base + (q.mode == kPoly ? 1 : 2) * p.row_blocks;
     ok = wait_count(c + q.i, target, p, abort_flag);
     if (ok && q.mode == kPoly && q.j != q.i) ok = wait_count(c + q.j, target, p, abort_flag);
@@ -220,7 +261,7 @@ __device__ __forceinline__ bool wait_inputs(const NsStepsParams& p, const Tile& 
   fence_async_all();                       // the copies that follow read what was announced
   return ok;
 }
-__device__ __forceinline__ void announce(unsigned* c) { asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(c) : "memory"); }
+__device__ __forceinline__ void announce(unsigned* c) { asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c) : "memory"); }
 
 // ---- the kernel ------------------------------------------------------------------------------------------
 template <int CG, bool SPLIT>
@@ -230,23 +271,21 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   constexpr int BN = 128 * CG;                               // columns of a tile
   constexpr int kBK = SPLIT ? 32 : 64;                       // k-block
   constexpr uint32_t kOperand = SPLIT ? 8192u : 16384u;      // bytes of one operand tile of a stage
-  constexpr int kPieces = SPLIT ? 2 : 4;
-  constexpr uint32_t kPieceBytes = kPieceArea / kPieces;
-  constexpr int kTilePieces = BN / kPieceCols;
+  constexpr int kUnits = BN / 2 / kUnitCols;                 // units of a tile per half of the epilogue
   extern __shared__ unsigned char smem_dyn[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t rank = 0;
   if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t raw = smem_u32(smem_dyn), ring = (raw + 1023u) & ~1023u;
-  const uint32_t pieces = ring + kStagesN * kStageN;
-  unsigned char* tail = smem_dyn + (ring - raw) + kStagesN * kStageN + kPieceArea;
+  const uint32_t epi_at = ring + kStagesN * kStageN;
+  constexpr int kHeld = SPLIT || CG == 1 ? kUnits : 2;        // units of X that fit in a half's area
+  unsigned char* tail = smem_dyn + (ring - raw) + kStagesN * kStageN + 2 * kHalfArea;
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(tail);
-  constexpr int kBars = 2 * kStagesN + 7 + 3 * kPieces;
+  constexpr int kBars = 2 * kStagesN + 7 + 4 * kUnits;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   const uint32_t full = smem_u32(bars), empty = full + 8u * kStagesN, accfull = empty + 8u * kStagesN, accempty = accfull + 16u,
-                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 8u * kPieces,
-                 freed = filled + 8u * kPieces;
+                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 16u * kUnits;
   if (tid == 0) {
     for (int s = 0; s < kStagesN; ++s) {
       mbar_init(full + 8u * s, 1);
@@ -258,10 +297,9 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       mbar_init(crossempty + 8u * k, kEpiWarpsN);
     }
     mbar_init(done, 1);
-    for (int k = 0; k < kPieces; ++k) {
-      mbar_init(ready + 8u * k, 1);                      // the buffer is loaded (or free)
-      mbar_init(filled + 8u * k, kEpiWarpsN * 32);       // the piece is finished
-      mbar_init(freed + 8u * k, 1);                      // ... and stored
+    for (int k = 0; k < 2 * kUnits; ++k) {               // per half and unit, each used once per tile
+      mbar_init(ready + 8u * k, 1);                      // loaded (or free)
+      mbar_init(filled + 8u * k, kEpiWarpsN / 2);        // finished
     }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -293,10 +331,6 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         const Tile q = tile_of(p, t);
         const int cur = q.step & 1;
         const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
-        const CUtensorMap* a_h = q.mode == kGram ? &maps.xk_h[cur] : q.mode == kPoly ? &maps.ak_h : &maps.bk_h;
-        const CUtensorMap* a_l = q.mode == kGram ? &maps.xk_l[cur] : q.mode == kPoly ? &maps.ak_l : &maps.bk_l;
-        const CUtensorMap* b_h = q.mode == kUpdate ? &maps.xm_h[cur] : a_h;
-        const CUtensorMap* b_l = q.mode == kUpdate ? &maps.xm_l[cur] : a_l;
         const int row = q.i * BN + row_in_tile, col = q.j * BN + row_in_tile;      // (the tile is square)
         if (!wait_inputs<CG>(p, q, abort_flag)) break;
         for (int kb = 0; kb < n_kb; ++kb) {
@@ -304,18 +338,24 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
           const uint32_t st = ring + static_cast<uint32_t>(s) * kStageN, bar = full0 + 8u * s;
           if (rank == 0) mbar_expect_tx(full + 8u * s, CG * kStageN);
           const int k0 = kb * kBK;
-          const uint32_t b_at = st + kOperand * (SPLIT ? 2u : 1u);
-          load_tile<CG>(st, a_h, k0, row, q.z, bar);
-          if (SPLIT) load_tile<CG>(st + kOperand, a_l, k0, row, q.z, bar);
-          if (q.mode == kUpdate) {                          // blocks of [k-block] x [64 columns]
-#pragma unroll
-            for (uint32_t h = 0; h < 2; ++h) {
-              load_tile<CG>(b_at + h * (kOperand / 2), b_h, col + 64 * static_cast<int>(h), k0, q.z, bar);
-              if (SPLIT) load_tile<CG>(b_at + kOperand + h * (kOperand / 2), b_l, col + 64 * static_cast<int>(h), k0, q.z, bar);
+          auto operand = [&](uint32_t at, const CUtensorMap* k_map, const CUtensorMap* m_map, int r, bool mn) {
+            if (mn) {                                       // two blocks of [k-block] x [64 columns]
+              load_tile<CG>(at, m_map, r, k0, q.z, bar);
+              load_tile<CG>(at + kOperand / 2, m_map, r + 64, k0, q.z, bar);
+            } else {
+              load_tile<CG>(at, k_map, k0, r, q.z, bar);
             }
-          } else {
-            load_tile<CG>(b_at, b_h, k0, col, q.z, bar);
-            if (SPLIT) load_tile<CG>(b_at + kOperand, b_l, k0, col, q.z, bar);
+          };
+          const bool mn_a = a_is_mn(q, k0, BN), mn_b = b_is_mn(q, k0, BN);
+          const CUtensorMap *ak = q.mode == kGram ? &maps.xk_h[cur] : q.mode == kPoly ? &maps.ak_h : &maps.bk_h;
+          const CUtensorMap *am = q.mode == kPoly ? &maps.am_h : &maps.bm_h;
+          operand(st, ak, am, row, mn_a);
+          operand(st + kOperand * (SPLIT ? 2u : 1u), ak, q.mode == kUpdate ? &maps.xm_h[cur] : am, col, mn_b);
+          if (SPLIT) {
+            const CUtensorMap *akl = q.mode == kGram ? &maps.xk_l[cur] : q.mode == kPoly ? &maps.ak_l : &maps.bk_l;
+            const CUtensorMap *aml = q.mode == kPoly ? &maps.am_l : &maps.bm_l;
+            operand(st + kOperand, akl, aml, row, mn_a);
+            operand(st + 3u * kOperand, akl, q.mode == kUpdate ? &maps.xm_l[cur] : aml, col, mn_b);
           }
           if (++s == kStagesN) {
             s = 0;
@@ -335,7 +375,7 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     __syncwarp();
   } else if (warp == 1 && rank == 0) {
     // ---- products ----------------------------------------------------------------------------------
-    // instruction descriptor: fp32 accumulator (bit 4), fp16 operands, second operand MN-major (bit 16),
+    // instruction descriptor: fp32 accumulator (bit 4), fp16 operands, MN-major operands (bits 15, 16),
     // N / 8 at bit 17, M / 16 at bit 24
     const uint32_t idesc0 = (1u << 4) | (static_cast<uint32_t>(BN >> 3) << 17) | (static_cast<uint32_t>(CG * kBM >> 4) << 24);
     // Operand descriptors in units of 16 bytes (version 1 at bit 46, swizzle at bits 61-63).
@@ -350,10 +390,6 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     for (long long t = first; t < p.tiles; t += step, ++it) {
       const Tile q = tile_of(p, t);
       const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
-      const bool mn = q.mode == kUpdate;
-      const uint32_t idesc = idesc0 | (mn ? 1u << 16 : 0u);
-      const uint64_t desc_b = mn ? desc_mn : desc_k;
-      const uint32_t step_b = mn ? 128u : 2u;
       if (SPLIT && it >= 2) mbar_wait(crossempty + 8u * (it & 1u), ((it >> 1) - 1) & 1u, abort_flag, p.timeout_cycles);
       const uint32_t cross = tmem + (2u + (it & 1u)) * BN;   // split operands only
       for (int kb = 0; kb < n_kb; ++kb) {
@@ -364,14 +400,18 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         mbar_wait(full + 8u * s, pass & 1u, abort_flag, p.timeout_cycles);
         tcn_after();
         const uint32_t base = ((ring + static_cast<uint32_t>(s) * kStageN) & 0x3ffffu) >> 4;
+        const bool mn_a = a_is_mn(q, kb * kBK, BN), mn_b = b_is_mn(q, kb * kBK, BN);
+        const uint32_t idesc = idesc0 | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u);
+        const uint64_t desc_a = mn_a ? desc_mn : desc_k, desc_b = mn_b ? desc_mn : desc_k;
+        const uint32_t step_a = mn_a ? 128u : 2u, step_b = mn_b ? 128u : 2u;
         const bool last = kb == n_kb - 1 || (SPLIT && in_fold == kFold - 1);
         if (elect_one_n()) {
 #pragma unroll
           for (int k = 0; k < kBK / 16; ++k) {
             constexpr uint32_t op = kOperand >> 4;
-            const uint64_t a_h = desc_k | static_cast<uint64_t>(base + 2u * k);
+            const uint64_t a_h = desc_a | static_cast<uint64_t>(base + step_a * k);
             if constexpr (SPLIT) {
-              const uint64_t a_l = desc_k | static_cast<uint64_t>(base + op + 2u * k);
+              const uint64_t a_l = desc_a | static_cast<uint64_t>(base + op + step_a * k);
               const uint64_t b_h = desc_b | static_cast<uint64_t>(base + 2u * op + step_b * k);
               const uint64_t b_l = desc_b | static_cast<uint64_t>(base + 3u * op + step_b * k);
               umma_f16<CG>(d, a_h, b_h, idesc, (in_fold | k) ? 1u : 0u);
@@ -399,87 +439,87 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     __syncwarp();
     volatile unsigned ignore = 0u;
     mbar_wait(done, 0u, &ignore, p.timeout_cycles);           // no product in flight when tensor memory is freed
-  } else if (warp == 2) {
-    // ---- stores of finished pieces -------------------------------------------------------------------
+  } else if (warp == 2 || warp == 3) {
+    // ---- units of one half of the epilogue: loads, stores, announcements --------------------------------
     if (elect_one_n()) {
-      uint32_t n = 0;
+      const uint32_t half = static_cast<uint32_t>(warp) - 2u;
+      const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
+      uint32_t it = 0, loaded = 0;                             // loaded: units of the last tile that were asked for
       bool ok = true;
-      for (long long t = first; t < p.tiles && ok; t += step) {
+      for (long long t = first; t < p.tiles && ok; t += step, ++it) {
         const Tile q = tile_of(p, t);
-        const int nxt = (q.step & 1) ^ 1, row = q.i * BN + row_in_tile;
-        const bool mirror = q.mode != kUpdate && q.j < q.i;
-        const CUtensorMap* o_h = q.mode == kGram ? &maps.ap_h : q.mode == kPoly ? &maps.bp_h : &maps.xp_h[nxt];
-        const CUtensorMap* o_l = q.mode == kGram ? &maps.ap_l : q.mode == kPoly ? &maps.bp_l : &maps.xp_l[nxt];
-        const CUtensorMap* t_h = q.mode == kGram ? &maps.at_h : &maps.bt_h;
-        const CUtensorMap* t_l = q.mode == kGram ? &maps.at_l : &maps.bt_l;
-        for (int piece = 0; piece < kTilePieces; ++piece, ++n) {
-          const uint32_t b = n % kPieces;
-          ok = mbar_wait(filled + 8u * b, (n / kPieces) & 1u, abort_flag, p.timeout_cycles);
+        const int cur = q.step & 1, row = q.i * BN + row_in_tile, col = q.j * BN + static_cast<int>(half) * (BN / 2);
+        const bool x = q.mode == kUpdate;
+        const uint32_t size = SPLIT ? 2u * kUnitBytes : x ? 3u * kUnitBytes : kUnitBytes;
+        const uint32_t held = x ? kHeld : kUnits;              // units in the area at a time
+        auto load_unit = [&](uint32_t u) {
+          const uint32_t at = area + (u % held) * size, bar = ready_h + 8u * u;
+          const int c = col + static_cast<int>(u) * kUnitCols;
+          if (q.mode == kGram || p.drop_loads) {
+            mbar_arrive(bar);
+          } else if (SPLIT) {
+            mbar_expect_tx(bar, 2u * kUnitBytes);
+            tma_load_3d(at, x ? &maps.xu_h[cur] : &maps.au_h, c, row, q.z, bar);
+            tma_load_3d(at + kUnitBytes, x ? &maps.xu_l[cur] : &maps.au_l, c, row, q.z, bar);
+          } else {
+            mbar_expect_tx(bar, x ? 2u * kUnitBytes : kUnitBytes);
+            tma_load_3d(at, x ? &maps.xf : &maps.au_h, c, row, q.z, bar);
+          }
+          loaded = u + 1;
+        };
+        if (q.mode != kGram && !p.drop_loads) ok = wait_inputs<CG>(p, q, abort_flag);
+        if (!ok) break;
+        loaded = 0;
+        for (uint32_t u = 0; u < held; ++u) load_unit(u);
+        const CUtensorMap* o_h = q.mode == kGram ? &maps.au_h : q.mode == kPoly ? &maps.bu_h : &maps.xu_h[cur ^ 1];
+        const CUtensorMap* o_l = q.mode == kGram ? &maps.au_l : q.mode == kPoly ? &maps.bu_l : &maps.xu_l[cur ^ 1];
+        for (uint32_t u = 0; u < kUnits; ++u) {
+          ok = mbar_wait(filled_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles);
           if (!ok) break;
-          const uint32_t at = pieces + b * kPieceBytes;
-          const int c = q.j * BN + piece * kPieceCols;
-          tma_store_3d(o_h, at, c, row, q.z);
-          if (SPLIT || q.mode == kUpdate) tma_store_3d(o_l, at + kHalfPiece, c, row, q.z);
-          if (mirror) {
-            tma_store_3d(t_h, at + (SPLIT ? 2u : 1u) * kHalfPiece, row, c, q.z);
-            if (SPLIT) tma_store_3d(t_l, at + 3u * kHalfPiece, row, c, q.z);
+          const uint32_t at = area + (u % held) * size;
+          const int c = col + static_cast<int>(u) * kUnitCols;
+          if (SPLIT) {
+            tma_store_3d(o_h, at, c, row, q.z);
+            tma_store_3d(o_l, at + kUnitBytes, c, row, q.z);
+          } else if (x) {
+            tma_store_3d(&maps.xf, at, c, row, q.z);
+            if (q.step + 1 < p.steps) tma_store_3d(o_h, at + 2u * kUnitBytes, c, row, q.z);      // nobody reads the last one
+          } else {
+            tma_store_3d(o_h, at, c, row, q.z);
           }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-          mbar_arrive(freed + 8u * b);
+          if (u + held < kUnits) {
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            load_unit(u + held);
+          }
         }
         if (!ok) break;
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        fence_async_all();
+        asm volatile("fence.acq_rel.gpu;" ::: "memory");       // the half tile, before its announcement
         unsigned* base = p.progress + static_cast<long long>(q.z) * 3 * p.row_blocks;
-        if (q.mode == kUpdate) {
+        if (x) {
           announce(base + q.i);
         } else {
           unsigned* c = base + (q.mode == kGram ? 1 : 2) * p.row_blocks;
           announce(c + q.i);
-          if (mirror) announce(c + q.j);
+          if (q.j < q.i) announce(c + q.j);
         }
       }
       asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    }
-    __syncwarp();
-  } else if (warp == 3) {
-    // ---- loads of the pieces that the coefficients apply to --------------------------------------------
-    if (elect_one_n()) {
-      uint32_t n = 0;
-      bool ok = true;
-      for (long long t = first; t < p.tiles && ok && !p.drop_loads; t += step) {
-        const Tile q = tile_of(p, t);
-        const int cur = q.step & 1, row = q.i * BN + row_in_tile;
-        const bool low = SPLIT || q.mode == kUpdate;
-        if (q.mode != kGram) ok = wait_inputs<CG>(p, q, abort_flag);
-        for (int piece = 0; piece < kTilePieces && ok; ++piece) {
-          const uint32_t b = n % kPieces, use = n / kPieces;
-          if (use > 0) ok = mbar_wait(freed + 8u * b, (use - 1) & 1u, abort_flag, p.timeout_cycles);
-          if (!ok) break;
-          const uint32_t at = pieces + b * kPieceBytes, bar = ready + 8u * b;
-          const int c = q.j * BN + piece * kPieceCols;
-          if (q.mode == kGram) {
-            mbar_arrive(bar);
-          } else {
-            mbar_expect_tx(bar, low ? 2u * kHalfPiece : kHalfPiece);
-            tma_load_3d(at, q.mode == kPoly ? &maps.ap_h : &maps.xp_h[cur], c, row, q.z, bar);
-            if (low) tma_load_3d(at + kHalfPiece, q.mode == kPoly ? &maps.ap_l : &maps.xp_l[cur], c, row, q.z, bar);
-          }
-          ++n;
-        }
-      }
       volatile unsigned ignore = 0u;
-      for (uint32_t b = 0; b < kPieces && b < n; ++b)          // no copy in flight when the CTA exits
-        mbar_wait(ready + 8u * b, ((n - 1 - b) / kPieces) & 1u, &ignore, p.timeout_cycles);
+      if (!ok)                                                 // left early: no load in flight when the CTA exits
+        for (uint32_t u = 0; u < loaded; ++u) mbar_wait(ready_h + 8u * u, it & 1u, &ignore, p.timeout_cycles);
     }
     __syncwarp();
   } else if (warp >= kFirstEpi) {
-    // ---- epilogue: lanes are rows; the two warps of a quarter take 16 of a piece's 32 columns each ---
-    const int q4 = warp & 3, part = (warp - kFirstEpi) >> 2;
-    const uint32_t row = static_cast<uint32_t>(q4 * 32 + lane), sw = (row >> 1) & 3u;
-    const uint32_t t_row = tmem + static_cast<uint32_t>(part * 16) + (static_cast<uint32_t>(q4 * 32) << 16);
+    // ---- epilogue: a thread owns a row of the tile and 32 columns of it at a time -----------------------
+    const int q4 = warp & 3;
+    const uint32_t half = static_cast<uint32_t>(warp - kFirstEpi) >> 2;
+    const uint32_t row = static_cast<uint32_t>(q4 * 32 + lane);
+    const uint32_t sw64 = (row >> 1) & 3u, sw128 = row & 7u;   // swizzles of rows of 64 and of 128 bytes
+    const uint32_t t_row = tmem + half * (BN / 2) + (static_cast<uint32_t>(q4 * 32) << 16);
     const uint32_t accempty0 = CG == 2 ? map_to_rank(accempty, 0) : accempty;
+    const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
     auto hand_back = [&](uint32_t buf) {                      // this warp has read its part of the accumulator
       tcn_before();
       __syncwarp();
@@ -488,112 +528,121 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         else mbar_arrive(accempty + 8u * buf);
       }
     };
-    uint32_t it = 0, n = 0, acc = 0;
+    uint32_t it = 0, acc = 0;
     bool ok = true;
     for (long long t = first; t < p.tiles && ok; t += step, ++it) {
       const Tile q = tile_of(p, t);
       const NsCoef coef = p.coef[q.step][q.mode];
-      const bool low = SPLIT || q.mode == kUpdate, mirror = q.mode != kUpdate && q.j < q.i;
-      float sum[SPLIT ? kTilePieces : 1][16];
+      const uint64_t c_in = pack_f32x2(coef.in, coef.in), c_acc = pack_f32x2(coef.acc, coef.acc);
+      uint32_t r[2][32];                                      // accumulator columns: this unit's and the next one's
+      float sum[SPLIT ? kUnits : 1][32];
       if constexpr (SPLIT) {
         const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK, folds = (n_kb + kFold - 1) / kFold;
 #pragma unroll
-        for (int k = 0; k < kTilePieces; ++k)
+        for (int k = 0; k < kUnits; ++k)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sum[k][e] = 0.f;
-        for (int f = 0; f < folds && ok; ++f, ++acc) {
-          ok = __all_sync(0xffffffffu, mbar_wait(accfull + 8u * (acc & 1u), (acc >> 1) & 1u, abort_flag, p.timeout_cycles));
-          if (!ok) break;
-          tcn_after();
-#pragma unroll
-          for (int k = 0; k < kTilePieces; ++k) {
-            float v[16];
-            tmem_ld16(t_row + (acc & 1u) * BN + k * kPieceCols, v);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) sum[k][e] += v[e];
+          for (int e = 0; e < 32; ++e) sum[k][e] = 0.f;
+        for (int f = 0; f <= folds && ok; ++f) {              // the last round adds the cross terms
+          const bool main = f < folds;
+          if (main) {
+            ok = __all_sync(0xffffffffu, mbar_wait(accfull + 8u * (acc & 1u), (acc >> 1) & 1u, abort_flag, p.timeout_cycles));
+            if (!ok) break;
+            tcn_after();
           }
-          hand_back(acc & 1u);
+          const uint32_t at = t_row + (main ? acc & 1u : 2u + (it & 1u)) * BN;
+#pragma unroll
+          for (int k = 0; k < kUnits; ++k) tmem_ld32(at + k * kUnitCols, r[k]);
+#pragma unroll
+          for (int k = 0; k < kUnits; ++k) {
+            tmem_wait(r[k]);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[k][e] += __uint_as_float(r[k][e]);
+          }
+          if (main) {
+            hand_back(acc & 1u);
+            ++acc;
+          } else {
+            tcn_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(crossempty + 8u * (it & 1u));
+          }
         }
         if (!ok) break;
-#pragma unroll
-        for (int k = 0; k < kTilePieces; ++k) {
-          float v[16];
-          tmem_ld16(t_row + (2u + (it & 1u)) * BN + k * kPieceCols, v);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sum[k][e] += v[e];
-        }
-        tcn_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(crossempty + 8u * (it & 1u));
       } else {
         ok = __all_sync(0xffffffffu, mbar_wait(accfull + 8u * (it & 1u), (it >> 1) & 1u, abort_flag, p.timeout_cycles));
         if (!ok) break;
         tcn_after();
+        tmem_ld32(t_row + (it & 1u) * BN, r[0]);
       }
-#pragma unroll(SPLIT ? kTilePieces : 1)
-      for (int piece = 0; piece < kTilePieces; ++piece, ++n) {
-        const uint32_t b = n % kPieces;
-        float v[16];
-        if constexpr (SPLIT) {
+      const uint32_t size = SPLIT ? 2u * kUnitBytes : q.mode == kUpdate ? 3u * kUnitBytes : kUnitBytes;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] = sum[piece][e];
-        } else {
-          tmem_ld16(t_row + (it & 1u) * BN + static_cast<uint32_t>(piece * kPieceCols), v);
-          if (piece == kTilePieces - 1) hand_back(it & 1u);
+      for (int u = 0; u < kUnits; ++u) {
+        const uint32_t at = area + (q.mode == kUpdate ? u % kHeld : u) * size;
+        const uint32_t h_at = at + (!SPLIT && q.mode == kUpdate ? 2u * kUnitBytes : 0u) + row * 64u;      // fp16 values
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(ready_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles));
+        uint64_t v[16];                                       // pairs of results
+        if constexpr (!SPLIT) tmem_wait(r[u & 1]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if constexpr (SPLIT) v[e] = mul_f32x2(c_acc, pack_f32x2(sum[u][2 * e], sum[u][2 * e + 1]));
+          else v[e] = mul_f32x2(c_acc, pack_f32x2(__uint_as_float(r[u & 1][2 * e]), __uint_as_float(r[u & 1][2 * e + 1])));
         }
-        ok = __all_sync(0xffffffffu, mbar_wait(ready + 8u * b, (n / kPieces) & 1u, abort_flag, p.timeout_cycles));
-        if (!ok) break;
-        const uint32_t at = pieces + b * kPieceBytes;
+        if constexpr (!SPLIT) {
+          if (u + 1 < kUnits) tmem_ld32(t_row + (it & 1u) * BN + (u + 1) * kUnitCols, r[(u + 1) & 1]);
+          else hand_back(it & 1u);
+        }
+        if (!SPLIT && q.mode == kUpdate) {                    // X in fp32
+          uint4 f[8];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {                          // 8 columns: one 16-byte chunk of the row
-          const uint32_t chunk = static_cast<uint32_t>(part * 2 + g);
-          const uint32_t addr = at + row * 64u + ((chunk ^ sw) << 4);
-          float* w = v + 8 * g;
-          if (q.mode == kGram) {
+          for (uint32_t c = 0; c < 8; ++c) f[c] = lds128(at + row * 128u + ((c ^ sw128) << 4));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] *= coef.acc;
-          } else {
-            const uint4 h4 = lds128(addr);
-            const uint32_t hh[4] = {h4.x, h4.y, h4.z, h4.w};
-            uint4 l4 = make_uint4(0u, 0u, 0u, 0u);
-            if (low) l4 = lds128(addr + kHalfPiece);
-            const uint32_t ll[4] = {l4.x, l4.y, l4.z, l4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 x = unpack_half2(hh[e]), y = unpack_half2(ll[e]);
-              w[2 * e] = fmaf(coef.acc, w[2 * e], coef.in * (x.x + y.x));
-              w[2 * e + 1] = fmaf(coef.acc, w[2 * e + 1], coef.in * (x.y + y.y));
-            }
+          for (uint32_t c = 0; c < 8; ++c) {
+            v[2 * c] = fma_f32x2(c_in, pack_f32x2(__uint_as_float(f[c].x), __uint_as_float(f[c].y)), v[2 * c]);
+            v[2 * c + 1] = fma_f32x2(c_in, pack_f32x2(__uint_as_float(f[c].z), __uint_as_float(f[c].w)), v[2 * c + 1]);
+            const float2 a = unpack_f32x2(v[2 * c]), b = unpack_f32x2(v[2 * c + 1]);
+            const uint32_t o[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
+            sts128_n(at + row * 128u + ((c ^ sw128) << 4), o);
           }
-          uint32_t h[4], l[4] = {0u, 0u, 0u, 0u};
+        } else if (q.mode != kGram) {                         // fp16 values, and remainders with split operands
+          uint4 h4[4], l4[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) h[e] = pack_half2(w[2 * e], w[2 * e + 1]);
-          sts128_n(addr, h);
-          if (low) {
+          for (uint32_t c = 0; c < 4; ++c) h4[c] = lds128(h_at + ((c ^ sw64) << 4));
+          if (SPLIT) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (uint32_t c = 0; c < 4; ++c) l4[c] = lds128(h_at + kUnitBytes + ((c ^ sw64) << 4));
+          }
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint4 h = h4[e >> 2];
+            const uint32_t hh = (e & 3) == 0 ? h.x : (e & 3) == 1 ? h.y : (e & 3) == 2 ? h.z : h.w;
+            float2 x = unpack_half2(hh);
+            if (SPLIT) {
+              const uint4 l = l4[e >> 2];
+              const float2 y = unpack_half2((e & 3) == 0 ? l.x : (e & 3) == 1 ? l.y : (e & 3) == 2 ? l.z : l.w);
+              x.x += y.x;
+              x.y += y.y;
+            }
+            v[e] = fma_f32x2(c_in, pack_f32x2(x.x, x.y), v[e]);
+          }
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+          uint32_t h[4], l[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 w = unpack_f32x2(v[4 * c + e]);
+            h[e] = pack_half2(w.x, w.y);
+            if (SPLIT) {
               const float2 f = unpack_half2(h[e]);
-              l[e] = pack_half2(w[2 * e] - f.x, w[2 * e + 1] - f.y);
-            }
-            sts128_n(addr + kHalfPiece, l);
-          }
-          if (mirror) {                                        // the mirror image: a row of 256 bytes per column
-            const uint32_t base = at + (SPLIT ? 2u : 1u) * kHalfPiece + chunk * 8u * 256u + row * 2u;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const __half2 hv = *reinterpret_cast<const __half2*>(&h[e]);
-              sts16_n(base + (2 * e) * 256u, __low2half(hv));
-              sts16_n(base + (2 * e + 1) * 256u, __high2half(hv));
-              if (SPLIT) {
-                const __half2 lv = *reinterpret_cast<const __half2*>(&l[e]);
-                sts16_n(base + kHalfPiece + (2 * e) * 256u, __low2half(lv));
-                sts16_n(base + kHalfPiece + (2 * e + 1) * 256u, __high2half(lv));
-              }
+              l[e] = pack_half2(w.x - f.x, w.y - f.y);
             }
           }
+          sts128_n(h_at + ((c ^ sw64) << 4), h);
+          if (SPLIT) sts128_n(h_at + kUnitBytes + ((c ^ sw64) << 4), l);
         }
         fence_async_n();
-        mbar_arrive(filled + 8u * b);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(filled_h + 8u * u);
       }
     }
   }
@@ -613,41 +662,46 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// [Z][rows][cols] fp16 matrices with boxes of [box_rows][box_cols]; what lies outside reads as zero and is not written.
-bool encode_half_map(const __half* base, int Z, int rows, int cols, long long ld, int box_rows, int box_cols,
-                     CUtensorMapSwizzle swizzle, CUtensorMap* map) {
+// [Z][rows][cols] fp16 or fp32 matrices with boxes of [box_rows][box_cols]; what lies outside reads as zero and
+// is not written.
+bool encode_map(const void* base, bool f32, int Z, int rows, int cols, long long ld, int box_rows, int box_cols,
+                CUtensorMapSwizzle swizzle, CUtensorMap* map) {
+  const cuuint64_t es = f32 ? 4 : 2;
   const cuuint64_t gdim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(Z)};
-  const cuuint64_t gstr[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * rows};
+  const cuuint64_t gstr[2] = {static_cast<cuuint64_t>(ld) * es, static_cast<cuuint64_t>(ld) * es * rows};
   const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
-  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), gdim, gstr, box, estr,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_tiled_fn()(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                           const_cast<void*>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int CG, bool SPLIT>
 int launch_steps(abs_ctx* ctx, const NsBuffers& w, NsStepsParams& p, cudaStream_t st) {
   constexpr int bk = SPLIT ? 32 : 64;
   const CUtensorMapSwizzle sk = SPLIT ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
-  const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B, s64 = CU_TENSOR_MAP_SWIZZLE_64B, s0 = CU_TENSOR_MAP_SWIZZLE_NONE;
+  const CUtensorMapSwizzle s128 = CU_TENSOR_MAP_SWIZZLE_128B, s64 = CU_TENSOR_MAP_SWIZZLE_64B;
   NsMaps maps;
   bool ok = true;
   for (int k = 0; k < 2; ++k) {
-    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_h[k]);
-    ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_l[k]);
-    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_h[k]);
-    ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_l[k]);
-    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, kBM, kPieceCols, s64, &maps.xp_h[k]);
-    ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, kBM, kPieceCols, s64, &maps.xp_l[k]);
+    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_h[k]);
+    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_h[k]);
+    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_h[k]);
+    if (SPLIT) {
+      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_l[k]);
+      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_l[k]);
+      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_l[k]);
+    }
   }
+  if (!SPLIT) ok = ok && encode_map(w.xf, true, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s128, &maps.xf);
   for (int k = 0; k < (SPLIT ? 2 : 1); ++k) {
     const __half *A = k ? w.al : w.ah, *B = k ? w.bl : w.bh;
-    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.ak_l : &maps.ak_h);
-    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.bk_l : &maps.bk_h);
-    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, kBM, kPieceCols, s64, k ? &maps.ap_l : &maps.ap_h);
-    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, kBM, kPieceCols, s64, k ? &maps.bp_l : &maps.bp_h);
-    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, kPieceCols, kBM, s0, k ? &maps.at_l : &maps.at_h);
-    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, kPieceCols, kBM, s0, k ? &maps.bt_l : &maps.bt_h);
+    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.ak_l : &maps.ak_h);
+    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.bk_l : &maps.bk_h);
+    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.am_l : &maps.am_h);
+    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.bm_l : &maps.bm_h);
+    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.au_l : &maps.au_h);
+    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.bu_l : &maps.bu_h);
   }
   if (!ok) return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (matrices of %d x %d) failed", w.m, w.n);
   constexpr int side = 128 * CG;
@@ -657,7 +711,7 @@ int launch_steps(abs_ctx* ctx, const NsBuffers& w, NsStepsParams& p, cudaStream_
   p.per_step = static_cast<long long>(w.Z) * (2ll * p.tri + static_cast<long long>(p.row_blocks) * p.col_tiles);
   p.tiles = p.per_step * p.steps;
 
-  const size_t smem = static_cast<size_t>(kStagesN) * kStageN + kPieceArea + 1024 + 256;
+  const size_t smem = static_cast<size_t>(kStagesN) * kStageN + 2 * kHalfArea + 1024 + 256;
   auto kern = ns_steps_kernel<CG, SPLIT>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
   const long long widest = static_cast<long long>(w.Z) * p.row_blocks * (p.row_blocks > p.col_tiles ? p.row_blocks : p.col_tiles);
