@@ -5,7 +5,7 @@
 //   A = X X',   X <- a X + (b A + c A^2) X          (on the short side, m <= n).
 //
 // Rounding.  The products run on fp16 operands (11 significant bits, fp32 accumulation); X itself is
-// carried in fp32, which the linear term uses.  Small singular values grow by a factor a
+// carried as value + remainder (22 bits) and the linear term uses both.  Small singular values grow by a factor a
 // in every step (3.4445^5 = 485), and only through the linear term: rounding X to 11 bits there would
 // lift the rounding noise of large directions into empty ones (fp16 simulation, 512 x 1024 of rank 8:
 // 4e-2 of the result's norm; bfloat16 0.35), while rounding inside B X stays in proportion to B X
@@ -205,20 +205,16 @@ ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float ep
     const __half2 h[2] = {__floats2half2_rn(x[0], x[1]), __floats2half2_rn(x[2], x[3])};
     const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
     *reinterpret_cast<uint2*>(w.xh[0] + o) = *reinterpret_cast<const uint2*>(h);
-    if (w.xf != nullptr) {
-      *reinterpret_cast<float4*>(w.xf + o) = make_float4(x[0], x[1], x[2], x[3]);
-    } else {
-      const float2 f0 = __half22float2(h[0]), f1 = __half22float2(h[1]);
-      const __half2 l[2] = {__floats2half2_rn(x[0] - f0.x, x[1] - f0.y), __floats2half2_rn(x[2] - f1.x, x[3] - f1.y)};
-      *reinterpret_cast<uint2*>(w.xl[0] + o) = *reinterpret_cast<const uint2*>(l);
-    }
+    const float2 f0 = __half22float2(h[0]), f1 = __half22float2(h[1]);
+    const __half2 l[2] = {__floats2half2_rn(x[0] - f0.x, x[1] - f0.y), __floats2half2_rn(x[2] - f1.x, x[3] - f1.y)};
+    *reinterpret_cast<uint2*>(w.xl[0] + o) = *reinterpret_cast<const uint2*>(l);
   }
 }
 
 // O = X / sx back in the caller's orientation: the result, or the parameter update.
 template <int V>
 __global__ void __launch_bounds__(kPassThreads)
-ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, int cur, float inv_sx, int tiles_c,
+ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, int cur, int low, float inv_sx, int tiles_c,
                  const unsigned* flag) {
   __shared__ float tile[kTile][kTile + 1];
   const int z = blockIdx.y, tid = threadIdx.x;
@@ -236,14 +232,10 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < w.m && j < w.n) {
       const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
-      if (w.xf != nullptr) {
-        x = *reinterpret_cast<const float4*>(w.xf + o);
-      } else {
-        const uint2 h = *reinterpret_cast<const uint2*>(w.xh[cur] + o), l = *reinterpret_cast<const uint2*>(w.xl[cur] + o);
-        const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x));
-        const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
-        x = make_float4(h0.x + l0.x, h0.y + l0.y, h1.x + l1.x, h1.y + l1.y);
-      }
+      const uint2 h = *reinterpret_cast<const uint2*>(w.xh[cur] + o), l = *reinterpret_cast<const uint2*>(w.xl[low] + o);
+      const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x));
+      const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
+      x = make_float4(h0.x + l0.x, h0.y + l0.y, h1.x + l1.x, h1.y + l1.y);
     }
     u[k][0] = x.x * inv_sx + bad;
     u[k][1] = x.y * inv_sx + bad;
@@ -352,7 +344,7 @@ struct NsPlan {
   long long ldx, ldm, x_halves, m_halves;    // per matrix
   bool split;
   size_t per_matrix() const {
-    return static_cast<size_t>(4 * x_halves + (split ? 4 : 2) * m_halves) * 2 + kNormParts * sizeof(double) +
+    return static_cast<size_t>((split ? 4 : 3) * x_halves + (split ? 4 : 2) * m_halves) * 2 + kNormParts * sizeof(double) +
            static_cast<size_t>(3 * ns_row_blocks(m)) * sizeof(unsigned);
   }
 };
@@ -427,10 +419,9 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
       return r;
     };
     const size_t xb = static_cast<size_t>(p.x_halves) * zmax * 2, mb = static_cast<size_t>(p.m_halves) * zmax * 2;
-    if (!p.split) w.xf = static_cast<float*>(take(2 * xb));
     for (int k = 0; k < 2; ++k) {
       w.xh[k] = static_cast<__half*>(take(xb));
-      if (p.split) w.xl[k] = static_cast<__half*>(take(xb));
+      if (p.split || k == 0) w.xl[k] = static_cast<__half*>(take(xb));
     }
     w.ah = static_cast<__half*>(take(mb));
     w.bh = static_cast<__half*>(take(mb));
@@ -456,7 +447,7 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
     const int rc = launch_ns_steps(ctx, w, cfg->steps, cfg->a, cfg->b, cfg->c, sc, p.split, st);
     if (rc != ABS_OK) return rc;
     const int cur = cfg->steps & 1;
-    ABS_CUDA_TRY(ctx, launch_dependent(dst_vec ? ns_finish_kernel<4> : ns_finish_kernel<1>, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur,
+    ABS_CUDA_TRY(ctx, launch_dependent(dst_vec ? ns_finish_kernel<4> : ns_finish_kernel<1>, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur, p.split ? cur : 0,
                                        1.0f / sc.sx[cfg->steps], tiles_c, static_cast<const unsigned*>(flag)));
   }
   return ABS_OK;

@@ -2,12 +2,13 @@
 // products (abs_ns_gemm.cu) share.
 //
 // One matrix is held with its short side as rows, X [m][n], m <= n (a tall matrix is transposed when
-// it is read and again when the result is written), in fp32 and, rounded, in fp16.  A step is
+// it is read and again when the result is written), as two fp16 matrices, values and remainders (22
+// bits).  A step is
 //   A = X X',   B = b A + c A A,   X <- a X + B X,
-// three products whose operands are the fp16 values; the a X term takes the fp32 ones, so what 11
+// three products whose operands are the values; the a X term takes the remainders too, so what 11
 // bits of an operand lose is always in proportion to B X and never fills directions that the
-// gradient does not have (see abs_muon.cu).  With split operands every matrix is held as two fp16
-// matrices, values and remainders, and a product is three tensor-core products.
+// gradient does not have (see abs_muon.cu).  With split operands A and B have remainders as well and
+// a product is three tensor-core products.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -26,16 +27,15 @@ struct NsScales {
   float tb[kNsMaxSteps];       // B
 };
 
-// Device buffers of one group of Z matrices.  Step k reads the fp16 X (and remainders) of k & 1 and writes the other.
+// Device buffers of one group of Z matrices.  Step k reads the X of k & 1 and writes the other.
 struct NsBuffers {
   int Z, m, n;
   long long ldx, ldm;              // leading dimensions in elements, multiples of 8
-  float* xf;                       // X in fp32, changed in place (not with split operands)
   __half* xh[2];
+  __half* xl[2];                   // remainders; without split operands only [0], changed in place
   __half* ah;
   __half* bh;
-  __half* xl[2];                   // remainders: split operands only
-  __half* al;
+  __half* al;                      // split operands only
   __half* bl;
   double* part;                    // [Z][kNormParts] partial sums of squares
   unsigned* progress;              // [Z][3][kNsRowBlocks(m)] finished tiles of X, A, B, zero before the products

@@ -8,14 +8,17 @@
 // an operand whose k index runs along the rows of the stored matrix is MN-major (as X is in kUpdate),
 // one whose k index runs along the columns is K-major; the TMA box and the descriptor differ, no more.
 //
-// The tiles of all steps, products and matrices form one list, in that order; a resident grid walks it
-// with a fixed stride.  A tile starts when the row blocks that it reads are complete, which other CTAs
-// announce in per-matrix counters (release / acquire in global memory), so a product's last tiles run
-// beside the next product's first ones and there is no launch, no grid barrier and no idle wave between
-// products.  Nothing that is still read is overwritten: a tile of product p needs the row blocks of
-// product p - 1, which need all of product p - 2 that touches them, and so on; written out, every tile
-// that reads a buffer is complete before the tile that writes the same rows of it again may start.  The
-// launch is cooperative, so every CTA that is waited for is resident.
+// The tiles of all steps, products and matrices form one list; a resident grid walks it with a fixed
+// stride.  A tile starts when the row blocks that it reads are complete, which other CTAs announce in
+// per-matrix counters (release / acquire in global memory): no launch, grid barrier or idle wave between
+// products.  The list runs in slots: the matrices are cut into three parts, and slot s has product s of the
+// first, s - 1 of the second and s - 2 of the third part, so a product and the one that reads it are a
+// third of a step's tiles apart, whichever they are.  (A tile is announced about 5000 clocks after its
+// last product; with all matrices in the same product the next wave stood still that long.)
+// Nothing that is still read is overwritten: a tile of a product needs the row blocks of the one before,
+// which need all of the one before that that touches them, and so on; written out, every tile that reads
+// a buffer is complete before the tile that writes the same rows of it again may start.  The launch is
+// cooperative, so every CTA that is waited for is resident.
 //
 // CG = 1: a CTA has 128 x 128 tiles.  CG = 2: a pair of CTAs has 256 x 256 tiles (tcgen05 cta_group::2:
 // each CTA loads its 128 rows of the first operand and half the columns of the second, and holds its
@@ -24,7 +27,8 @@
 // An SM takes in about 64 bytes a clock from L2 (measured: a k-block of 64 of a 128 x 128 tile, 32 KB,
 // takes 556 clocks, its products 256), which is what a pair's tile needs at the tensor cores' full rate.
 //
-// Roles of a CTA's 12 warps: 0 loads operands by TMA into a ring of 32 KB stages, 1 issues the products
+// Roles of a CTA's 13 warps: 0 loads operands by TMA into a ring of 32 KB stages, 12 looks out for the
+// inputs of the next tile meanwhile, 1 issues the products
 // (fp32 accumulators in tensor memory, two of them, so the next tile's products run while this one is
 // read back), 4-7 and 8-11 are the two halves of the epilogue (each reads back half the tile's columns and
 // applies the coefficients in place, in shared memory), 2 and 3 move the units of one half each: they load
@@ -43,16 +47,23 @@ enum { kGram = 0, kPoly = 1, kUpdate = 2 };
 constexpr int kBM = 128;                     // rows of a CTA's tile
 constexpr int kEpiWarpsN = 8;
 constexpr int kFirstEpi = 4;
-constexpr int kThreadsN = (kFirstEpi + kEpiWarpsN) * 32;   // 384
-constexpr int kStagesN = 4;
+constexpr int kLookout = kFirstEpi + kEpiWarpsN;
+constexpr int kThreadsN = (kLookout + 1) * 32;             // 416
 constexpr uint32_t kStageN = 32768;
-// Units of the epilogue: 32 columns of the tile's 128 rows, changed in place in shared memory.  A unit takes
-// 8 KB as fp16 values (A, B), 16 KB as values and remainders (any matrix with split operands), and 16 + 8 KB as
-// X in fp32 and its fp16 values.  A half of the epilogue has 48 KB: all units of its half tile, or for X on CTA
-// pairs two of the four.
+// Units of the epilogue: 32 columns of the tile's 128 rows, changed in place in shared memory: 8 KB of fp16
+// values (A, B) or 16 KB of values and remainders (X; with split operands any matrix).  A half of the epilogue
+// has room for all units of its half tile, except for X on pairs: three of four; the fourth takes the first
+// one's place when that has been stored.  (Room for four would cost a stage of the ring: 3 instead of 4 made
+// a step on 4096 x 4096 a tenth slower.)
 constexpr int kUnitCols = 32;
 constexpr uint32_t kUnitBytes = kBM * kUnitCols * 2;       // 8 KB
-constexpr uint32_t kHalfArea = 6 * kUnitBytes;
+template <int CG>
+struct Smem {
+  static constexpr int kStages = CG == 2 ? 4 : 5;
+  static constexpr int kHeld = CG == 2 ? 3 : 2;              // units of X in a half's area
+  static constexpr uint32_t kHalfArea = kHeld * 2 * kUnitBytes;
+  static constexpr size_t kBytes = static_cast<size_t>(kStages) * kStageN + 2 * kHalfArea + 1024 + 512;      // alignment, barriers
+};
 // Split operands: an accumulator of the main products takes kFold k-blocks of 32 (2 kFold additions) and is
 // then added, rounded to nearest, to sums in registers: the tensor core adds without rounding to nearest.
 constexpr int kFold = 8;
@@ -61,7 +72,7 @@ struct NsMaps {
   // operands: boxes of [128 rows][k-block] (K-major) and [k-block][64 columns] (MN-major); _l: remainders
   CUtensorMap xk_h[2], xk_l[2], xm_h[2], xm_l[2], ak_h, ak_l, am_h, am_l, bk_h, bk_l, bm_h, bm_l;
   // units of the epilogue: boxes of [128 rows][32 columns]
-  CUtensorMap xf, xu_h[2], xu_l[2], au_h, au_l, bu_h, bu_l;
+  CUtensorMap xu_h[2], xu_l[2], au_h, au_l, bu_h, bu_l;
 };
 struct NsCoef {
   float in, acc;              // result = in * (what the epilogue reads) + acc * accumulator
@@ -71,7 +82,9 @@ struct NsStepsParams {
   int row_blocks;             // of 128 CG rows
   int col_tiles;              // of 128 CG columns of X
   int tri;                    // tiles of a symmetric result
-  long long per_step, tiles;
+  int part_z[4];              // the matrices of part r: part_z[r] .. part_z[r + 1] - 1
+  long long tiles;
+  unsigned slot_at[3 * kNsMaxSteps + 3];      // first tile of every slot, and the end
   unsigned* progress;         // [Z][3][row_blocks]: X, A, B
   unsigned* flag;
   long long timeout_cycles;
@@ -173,28 +186,36 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t u) { return __half22floa
 struct Tile {
   int step, mode, z, i, j;
 };
-__device__ __forceinline__ Tile tile_of(const NsStepsParams& p, long long t) {
-  Tile q;
-  q.step = static_cast<int>(t / p.per_step);
-  long long r = t - q.step * p.per_step;
-  const long long sym = static_cast<long long>(p.Z) * p.tri;
-  if (r < 2 * sym) {
-    q.mode = r < sym ? kGram : kPoly;
-    if (q.mode == kPoly) r -= sym;
-    q.z = static_cast<int>(r / p.tri);
-    const int k = static_cast<int>(r - static_cast<long long>(q.z) * p.tri);
+// `slot`: a slot at or before the tile's (every role walks the list forwards and keeps it).
+__device__ __forceinline__ Tile tile_of(const NsStepsParams& p, long long t, int& slot) {
+  const unsigned at = static_cast<unsigned>(t);
+  while (at >= p.slot_at[slot + 1]) ++slot;
+  int k = static_cast<int>(at - p.slot_at[slot]);
+  const int upd = p.row_blocks * p.col_tiles;
+  Tile q = {};
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    const int product = slot - part;
+    if (product < 0 || product >= 3 * p.steps) continue;
+    q.step = product / 3;
+    q.mode = product - 3 * q.step;
+    const int per = q.mode == kUpdate ? upd : p.tri, here = (p.part_z[part + 1] - p.part_z[part]) * per;
+    if (k < here) {
+      q.z = k / per;
+      k -= q.z * per;
+      q.z += p.part_z[part];
+      break;
+    }
+    k -= here;
+  }
+  if (q.mode == kUpdate) {
+    q.i = k / p.col_tiles;
+    q.j = k - q.i * p.col_tiles;
+  } else {
     q.i = static_cast<int>((sqrtf(8.f * static_cast<float>(k) + 1.f) - 1.f) * 0.5f);      // corrected to i (i + 1) / 2 <= k
     while (q.i * (q.i + 1) / 2 > k) --q.i;
     while ((q.i + 1) * (q.i + 2) / 2 <= k) ++q.i;
     q.j = k - q.i * (q.i + 1) / 2;
-  } else {
-    r -= 2 * sym;
-    q.mode = kUpdate;
-    const int per = p.row_blocks * p.col_tiles;
-    q.z = static_cast<int>(r / per);
-    const int k = static_cast<int>(r - static_cast<long long>(q.z) * per);
-    q.i = k / p.col_tiles;
-    q.j = k - q.i * p.col_tiles;
   }
   return q;
 }
@@ -269,6 +290,7 @@ __global__ void __launch_bounds__(kThreadsN, 1)
 ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsStepsParams p) {
   static_assert(CG == 1 || !SPLIT, "split operands use single CTAs");
   constexpr int BN = 128 * CG;                               // columns of a tile
+  constexpr int kStagesN = Smem<CG>::kStages;
   constexpr int kBK = SPLIT ? 32 : 64;                       // k-block
   constexpr uint32_t kOperand = SPLIT ? 8192u : 16384u;      // bytes of one operand tile of a stage
   constexpr int kUnits = BN / 2 / kUnitCols;                 // units of a tile per half of the epilogue
@@ -278,14 +300,15 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t raw = smem_u32(smem_dyn), ring = (raw + 1023u) & ~1023u;
   const uint32_t epi_at = ring + kStagesN * kStageN;
-  constexpr int kHeld = SPLIT || CG == 1 ? kUnits : 2;        // units of X that fit in a half's area
+  constexpr uint32_t kHalfArea = Smem<CG>::kHalfArea, kHeld = Smem<CG>::kHeld;
   unsigned char* tail = smem_dyn + (ring - raw) + kStagesN * kStageN + 2 * kHalfArea;
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(tail);
-  constexpr int kBars = 2 * kStagesN + 7 + 4 * kUnits;
+  constexpr int kBars = 2 * kStagesN + 11 + 4 * kUnits;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   const uint32_t full = smem_u32(bars), empty = full + 8u * kStagesN, accfull = empty + 8u * kStagesN, accempty = accfull + 16u,
-                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 16u * kUnits;
+                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 16u * kUnits,
+                 inputs = filled + 16u * kUnits, taken = inputs + 16u;
   if (tid == 0) {
     for (int s = 0; s < kStagesN; ++s) {
       mbar_init(full + 8u * s, 1);
@@ -295,6 +318,8 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       mbar_init(accfull + 8u * k, 1);
       mbar_init(accempty + 8u * k, kEpiWarpsN * CG);
       mbar_init(crossempty + 8u * k, kEpiWarpsN);
+      mbar_init(inputs + 8u * k, 1);                       // a tile's inputs are complete
+      mbar_init(taken + 8u * k, 1);                        // ... and its loads begin
     }
     mbar_init(done, 1);
     for (int k = 0; k < 2 * kUnits; ++k) {               // per half and unit, each used once per tile
@@ -324,15 +349,17 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   if (warp == 0) {
     // ---- operand loads ---------------------------------------------------------------------------
     if (elect_one_n()) {
-      int s = 0;
-      uint32_t pass = 0;
+      int s = 0, slot = 0;
+      uint32_t pass = 0, it = 0;
       const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;       // the pair's barrier is its first CTA's
       for (long long t = first; t < p.tiles && !p.drop_loads; t += step) {
-        const Tile q = tile_of(p, t);
+        const Tile q = tile_of(p, t, slot);
         const int cur = q.step & 1;
         const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
         const int row = q.i * BN + row_in_tile, col = q.j * BN + row_in_tile;      // (the tile is square)
-        if (!wait_inputs<CG>(p, q, abort_flag)) break;
+        if (!mbar_wait(inputs + 8u * (it & 1u), (it >> 1) & 1u, abort_flag, p.timeout_cycles)) break;
+        mbar_arrive(taken + 8u * (it & 1u));
+        ++it;
         for (int kb = 0; kb < n_kb; ++kb) {
           if (pass > 0 && !mbar_wait(empty + 8u * s, (pass - 1) & 1u, abort_flag, p.timeout_cycles)) break;
           const uint32_t st = ring + static_cast<uint32_t>(s) * kStageN, bar = full0 + 8u * s;
@@ -385,10 +412,10 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     // 1024 bytes apart (stride offset), 16 values of k are 2048 bytes.
     const uint64_t desc_k = (1ull << 46) | (1ull << 16) | (SPLIT ? (32ull << 32) | (4ull << 61) : (64ull << 32) | (2ull << 61));
     const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(kBK * 8) << 16);
-    int s = 0;
+    int s = 0, slot = 0;
     uint32_t pass = 0, it = 0, acc = 0;                      // tiles, accumulators of the main products used so far
     for (long long t = first; t < p.tiles; t += step, ++it) {
-      const Tile q = tile_of(p, t);
+      const Tile q = tile_of(p, t, slot);
       const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
       if (SPLIT && it >= 2) mbar_wait(crossempty + 8u * (it & 1u), ((it >> 1) - 1) & 1u, abort_flag, p.timeout_cycles);
       const uint32_t cross = tmem + (2u + (it & 1u)) * BN;   // split operands only
@@ -444,56 +471,52 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     if (elect_one_n()) {
       const uint32_t half = static_cast<uint32_t>(warp) - 2u;
       const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
-      uint32_t it = 0, loaded = 0;                             // loaded: units of the last tile that were asked for
+      uint32_t it = 0;
+      int slot = 0;
       bool ok = true;
       for (long long t = first; t < p.tiles && ok; t += step, ++it) {
-        const Tile q = tile_of(p, t);
+        const Tile q = tile_of(p, t, slot);
         const int cur = q.step & 1, row = q.i * BN + row_in_tile, col = q.j * BN + static_cast<int>(half) * (BN / 2);
         const bool x = q.mode == kUpdate;
-        const uint32_t size = SPLIT ? 2u * kUnitBytes : x ? 3u * kUnitBytes : kUnitBytes;
-        const uint32_t held = x ? kHeld : kUnits;              // units in the area at a time
-        auto load_unit = [&](uint32_t u) {
-          const uint32_t at = area + (u % held) * size, bar = ready_h + 8u * u;
+        const bool low = SPLIT || x;                           // values and remainders
+        const uint32_t size = low ? 2u * kUnitBytes : kUnitBytes;
+        const int low_in = SPLIT ? cur : 0, low_out = SPLIT ? cur ^ 1 : 0;      // remainders of X stay where they are, unless operands
+        if (q.mode != kGram && !p.drop_loads) ok = wait_inputs<CG>(p, q, abort_flag);
+        if (!ok) break;
+        const uint32_t held = low && !SPLIT ? kHeld : kUnits;
+        uint32_t loaded = 0;
+        auto load_next = [&]() {
+          const uint32_t u = loaded++, at = area + (u % held) * size, bar = ready_h + 8u * u;
           const int c = col + static_cast<int>(u) * kUnitCols;
           if (q.mode == kGram || p.drop_loads) {
             mbar_arrive(bar);
-          } else if (SPLIT) {
-            mbar_expect_tx(bar, 2u * kUnitBytes);
-            tma_load_3d(at, x ? &maps.xu_h[cur] : &maps.au_h, c, row, q.z, bar);
-            tma_load_3d(at + kUnitBytes, x ? &maps.xu_l[cur] : &maps.au_l, c, row, q.z, bar);
           } else {
-            mbar_expect_tx(bar, x ? 2u * kUnitBytes : kUnitBytes);
-            tma_load_3d(at, x ? &maps.xf : &maps.au_h, c, row, q.z, bar);
+            mbar_expect_tx(bar, size);
+            tma_load_3d(at, x ? &maps.xu_h[cur] : &maps.au_h, c, row, q.z, bar);
+            if (low) tma_load_3d(at + kUnitBytes, x ? &maps.xu_l[low_in] : &maps.au_l, c, row, q.z, bar);
           }
-          loaded = u + 1;
         };
-        if (q.mode != kGram && !p.drop_loads) ok = wait_inputs<CG>(p, q, abort_flag);
-        if (!ok) break;
-        loaded = 0;
-        for (uint32_t u = 0; u < held; ++u) load_unit(u);
+        for (uint32_t u = 0; u < held; ++u) load_next();
         const CUtensorMap* o_h = q.mode == kGram ? &maps.au_h : q.mode == kPoly ? &maps.bu_h : &maps.xu_h[cur ^ 1];
-        const CUtensorMap* o_l = q.mode == kGram ? &maps.au_l : q.mode == kPoly ? &maps.bu_l : &maps.xu_l[cur ^ 1];
+        const CUtensorMap* o_l = q.mode == kGram ? &maps.au_l : q.mode == kPoly ? &maps.bu_l : &maps.xu_l[low_out];
         for (uint32_t u = 0; u < kUnits; ++u) {
           ok = mbar_wait(filled_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles);
           if (!ok) break;
           const uint32_t at = area + (u % held) * size;
           const int c = col + static_cast<int>(u) * kUnitCols;
-          if (SPLIT) {
-            tma_store_3d(o_h, at, c, row, q.z);
-            tma_store_3d(o_l, at + kUnitBytes, c, row, q.z);
-          } else if (x) {
-            tma_store_3d(&maps.xf, at, c, row, q.z);
-            if (q.step + 1 < p.steps) tma_store_3d(o_h, at + 2u * kUnitBytes, c, row, q.z);      // nobody reads the last one
-          } else {
-            tma_store_3d(o_h, at, c, row, q.z);
-          }
+          tma_store_3d(o_h, at, c, row, q.z);
+          if (low) tma_store_3d(o_l, at + kUnitBytes, c, row, q.z);
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          if (u + held < kUnits) {
+          if (loaded < kUnits) {
             asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            load_unit(u + held);
+            load_next();
           }
         }
-        if (!ok) break;
+        if (!ok) {                                             // no load in flight when the CTA exits
+          volatile unsigned ignore = 0u;
+          for (uint32_t u = 0; u < loaded; ++u) mbar_wait(ready_h + 8u * u, it & 1u, &ignore, p.timeout_cycles);
+          break;
+        }
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         asm volatile("fence.acq_rel.gpu;" ::: "memory");       // the half tile, before its announcement
         unsigned* base = p.progress + static_cast<long long>(q.z) * 3 * p.row_blocks;
@@ -506,17 +529,27 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         }
       }
       asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-      volatile unsigned ignore = 0u;
-      if (!ok)                                                 // left early: no load in flight when the CTA exits
-        for (uint32_t u = 0; u < loaded; ++u) mbar_wait(ready_h + 8u * u, it & 1u, &ignore, p.timeout_cycles);
     }
     __syncwarp();
-  } else if (warp >= kFirstEpi) {
+  } else if (warp == kLookout) {
+    // ---- waits for the inputs of the tile after the one that is being loaded -----------------------------
+    if (elect_one_n()) {
+      int slot = 0;
+      uint32_t it = 0;
+      for (long long t = first; t < p.tiles && !p.drop_loads; t += step, ++it) {
+        const Tile q = tile_of(p, t, slot);
+        if (it >= 2 && !mbar_wait(taken + 8u * (it & 1u), ((it >> 1) - 1) & 1u, abort_flag, p.timeout_cycles)) break;
+        if (!wait_inputs<CG>(p, q, abort_flag)) break;
+        mbar_arrive(inputs + 8u * (it & 1u));
+      }
+    }
+    __syncwarp();
+  } else if (warp >= kFirstEpi) {                            // (warp 1 of a pair's second CTA has nothing to do)
     // ---- epilogue: a thread owns a row of the tile and 32 columns of it at a time -----------------------
     const int q4 = warp & 3;
     const uint32_t half = static_cast<uint32_t>(warp - kFirstEpi) >> 2;
     const uint32_t row = static_cast<uint32_t>(q4 * 32 + lane);
-    const uint32_t sw64 = (row >> 1) & 3u, sw128 = row & 7u;   // swizzles of rows of 64 and of 128 bytes
+    const uint32_t sw64 = (row >> 1) & 3u;                     // swizzle of rows of 64 bytes
     const uint32_t t_row = tmem + half * (BN / 2) + (static_cast<uint32_t>(q4 * 32) << 16);
     const uint32_t accempty0 = CG == 2 ? map_to_rank(accempty, 0) : accempty;
     const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
@@ -529,9 +562,10 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       }
     };
     uint32_t it = 0, acc = 0;
+    int slot = 0;
     bool ok = true;
     for (long long t = first; t < p.tiles && ok; t += step, ++it) {
-      const Tile q = tile_of(p, t);
+      const Tile q = tile_of(p, t, slot);
       const NsCoef coef = p.coef[q.step][q.mode];
       const uint64_t c_in = pack_f32x2(coef.in, coef.in), c_acc = pack_f32x2(coef.acc, coef.acc);
       uint32_t r[2][32];                                      // accumulator columns: this unit's and the next one's
@@ -574,11 +608,10 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         tcn_after();
         tmem_ld32(t_row + (it & 1u) * BN, r[0]);
       }
-      const uint32_t size = SPLIT ? 2u * kUnitBytes : q.mode == kUpdate ? 3u * kUnitBytes : kUnitBytes;
+      const bool low = SPLIT || q.mode == kUpdate;            // values and remainders
 #pragma unroll
       for (int u = 0; u < kUnits; ++u) {
-        const uint32_t at = area + (q.mode == kUpdate ? u % kHeld : u) * size;
-        const uint32_t h_at = at + (!SPLIT && q.mode == kUpdate ? 2u * kUnitBytes : 0u) + row * 64u;      // fp16 values
+        const uint32_t h_at = area + (low && !SPLIT ? (u % kHeld) * 2u : low ? u * 2u : u) * kUnitBytes + row * 64u;
         ok = ok && __all_sync(0xffffffffu, mbar_wait(ready_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles));
         uint64_t v[16];                                       // pairs of results
         if constexpr (!SPLIT) tmem_wait(r[u & 1]);
@@ -591,54 +624,45 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
           if (u + 1 < kUnits) tmem_ld32(t_row + (it & 1u) * BN + (u + 1) * kUnitCols, r[(u + 1) & 1]);
           else hand_back(it & 1u);
         }
-        if (!SPLIT && q.mode == kUpdate) {                    // X in fp32
-          uint4 f[8];
-#pragma unroll
-          for (uint32_t c = 0; c < 8; ++c) f[c] = lds128(at + row * 128u + ((c ^ sw128) << 4));
-#pragma unroll
-          for (uint32_t c = 0; c < 8; ++c) {
-            v[2 * c] = fma_f32x2(c_in, pack_f32x2(__uint_as_float(f[c].x), __uint_as_float(f[c].y)), v[2 * c]);
-            v[2 * c + 1] = fma_f32x2(c_in, pack_f32x2(__uint_as_float(f[c].z), __uint_as_float(f[c].w)), v[2 * c + 1]);
-            const float2 a = unpack_f32x2(v[2 * c]), b = unpack_f32x2(v[2 * c + 1]);
-            const uint32_t o[4] = {__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
-            sts128_n(at + row * 128u + ((c ^ sw128) << 4), o);
-          }
-        } else if (q.mode != kGram) {                         // fp16 values, and remainders with split operands
+        if (q.mode != kGram) {
           uint4 h4[4], l4[4];
 #pragma unroll
           for (uint32_t c = 0; c < 4; ++c) h4[c] = lds128(h_at + ((c ^ sw64) << 4));
-          if (SPLIT) {
+          if (low) {
 #pragma unroll
             for (uint32_t c = 0; c < 4; ++c) l4[c] = lds128(h_at + kUnitBytes + ((c ^ sw64) << 4));
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint4 l = l4[e >> 2];
+              const float2 y = unpack_half2((e & 3) == 0 ? l.x : (e & 3) == 1 ? l.y : (e & 3) == 2 ? l.z : l.w);
+              v[e] = fma_f32x2(c_in, pack_f32x2(y.x, y.y), v[e]);
+            }
           }
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const uint4 h = h4[e >> 2];
-            const uint32_t hh = (e & 3) == 0 ? h.x : (e & 3) == 1 ? h.y : (e & 3) == 2 ? h.z : h.w;
-            float2 x = unpack_half2(hh);
-            if (SPLIT) {
-              const uint4 l = l4[e >> 2];
-              const float2 y = unpack_half2((e & 3) == 0 ? l.x : (e & 3) == 1 ? l.y : (e & 3) == 2 ? l.z : l.w);
-              x.x += y.x;
-              x.y += y.y;
-            }
+            const float2 x = unpack_half2((e & 3) == 0 ? h.x : (e & 3) == 1 ? h.y : (e & 3) == 2 ? h.z : h.w);
             v[e] = fma_f32x2(c_in, pack_f32x2(x.x, x.y), v[e]);
           }
         }
 #pragma unroll
         for (uint32_t c = 0; c < 4; ++c) {
-          uint32_t h[4], l[4];
+          uint32_t h[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float2 w = unpack_f32x2(v[4 * c + e]);
             h[e] = pack_half2(w.x, w.y);
-            if (SPLIT) {
-              const float2 f = unpack_half2(h[e]);
-              l[e] = pack_half2(w.x - f.x, w.y - f.y);
-            }
           }
           sts128_n(h_at + ((c ^ sw64) << 4), h);
-          if (SPLIT) sts128_n(h_at + kUnitBytes + ((c ^ sw64) << 4), l);
+          if (low) {
+            uint32_t l[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 w = unpack_f32x2(v[4 * c + e]), f = unpack_half2(h[e]);
+              l[e] = pack_half2(w.x - f.x, w.y - f.y);
+            }
+            sts128_n(h_at + kUnitBytes + ((c ^ sw64) << 4), l);
+          }
         }
         fence_async_n();
         __syncwarp();
@@ -662,18 +686,16 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// [Z][rows][cols] fp16 or fp32 matrices with boxes of [box_rows][box_cols]; what lies outside reads as zero and
-// is not written.
-bool encode_map(const void* base, bool f32, int Z, int rows, int cols, long long ld, int box_rows, int box_cols,
-                CUtensorMapSwizzle swizzle, CUtensorMap* map) {
-  const cuuint64_t es = f32 ? 4 : 2;
+// [Z][rows][cols] fp16 matrices with boxes of [box_rows][box_cols]; what lies outside reads as zero and is not written.
+bool encode_half_map(const __half* base, int Z, int rows, int cols, long long ld, int box_rows, int box_cols,
+                     CUtensorMapSwizzle swizzle, CUtensorMap* map) {
   const cuuint64_t gdim[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(Z)};
-  const cuuint64_t gstr[2] = {static_cast<cuuint64_t>(ld) * es, static_cast<cuuint64_t>(ld) * es * rows};
+  const cuuint64_t gstr[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * rows};
   const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 1u};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
-  return encode_tiled_fn()(map, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                           const_cast<void*>(base), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), gdim, gstr, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int CG, bool SPLIT>
@@ -684,34 +706,46 @@ int launch_steps(abs_ctx* ctx, const NsBuffers& w, NsStepsParams& p, cudaStream_
   NsMaps maps;
   bool ok = true;
   for (int k = 0; k < 2; ++k) {
-    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_h[k]);
-    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_h[k]);
-    ok = ok && encode_map(w.xh[k], false, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_h[k]);
+    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_h[k]);
+    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_h[k]);
+    ok = ok && encode_half_map(w.xh[k], w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_h[k]);
     if (SPLIT) {
-      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_l[k]);
-      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_l[k]);
-      ok = ok && encode_map(w.xl[k], false, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_l[k]);
+      ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, kBM, bk, sk, &maps.xk_l[k]);
+      ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, bk, 64, s128, &maps.xm_l[k]);
     }
+    if (SPLIT || k == 0) ok = ok && encode_half_map(w.xl[k], w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s64, &maps.xu_l[k]);
   }
-  if (!SPLIT) ok = ok && encode_map(w.xf, true, w.Z, w.m, w.n, w.ldx, kBM, kUnitCols, s128, &maps.xf);
   for (int k = 0; k < (SPLIT ? 2 : 1); ++k) {
     const __half *A = k ? w.al : w.ah, *B = k ? w.bl : w.bh;
-    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.ak_l : &maps.ak_h);
-    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.bk_l : &maps.bk_h);
-    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.am_l : &maps.am_h);
-    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.bm_l : &maps.bm_h);
-    ok = ok && encode_map(A, false, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.au_l : &maps.au_h);
-    ok = ok && encode_map(B, false, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.bu_l : &maps.bu_h);
+    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.ak_l : &maps.ak_h);
+    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, kBM, bk, sk, k ? &maps.bk_l : &maps.bk_h);
+    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.am_l : &maps.am_h);
+    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, bk, 64, s128, k ? &maps.bm_l : &maps.bm_h);
+    ok = ok && encode_half_map(A, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.au_l : &maps.au_h);
+    ok = ok && encode_half_map(B, w.Z, w.m, w.m, w.ldm, kBM, kUnitCols, s64, k ? &maps.bu_l : &maps.bu_h);
   }
   if (!ok) return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (matrices of %d x %d) failed", w.m, w.n);
   constexpr int side = 128 * CG;
   p.row_blocks = (w.m + side - 1) / side;
   p.col_tiles = (w.n + side - 1) / side;
   p.tri = p.row_blocks * (p.row_blocks + 1) / 2;
-  p.per_step = static_cast<long long>(w.Z) * (2ll * p.tri + static_cast<long long>(p.row_blocks) * p.col_tiles);
-  p.tiles = p.per_step * p.steps;
+  // three parts where a product of all matrices is a wave or more; else every product waits for the one before anyway
+  const bool parts = static_cast<long long>(w.Z) * p.tri >= ctx->sm_count / CG;
+  for (int r = 0; r <= 3; ++r) p.part_z[r] = r > 0 && !parts ? w.Z : static_cast<int>((static_cast<long long>(w.Z) * r + 2) / 3);
+  p.tiles = 0;
+  for (int s = 0; s <= 3 * p.steps + 1; ++s) {
+    p.slot_at[s] = static_cast<unsigned>(p.tiles);
+    for (int r = 0; r < 3; ++r) {
+      const int product = s - r;
+      if (product < 0 || product >= 3 * p.steps) continue;
+      p.tiles += static_cast<long long>(p.part_z[r + 1] - p.part_z[r]) *
+                 (product % 3 == kUpdate ? static_cast<long long>(p.row_blocks) * p.col_tiles : p.tri);
+    }
+  }
+  p.slot_at[3 * p.steps + 2] = static_cast<unsigned>(p.tiles);
+  if (p.tiles > 0x7fffffffll) return set_error(ctx, ABS_ERR_UNSUPPORTED, "too many tiles in %d matrices of %d x %d", w.Z, w.m, w.n);
 
-  const size_t smem = static_cast<size_t>(kStagesN) * kStageN + 2 * kHalfArea + 1024 + 256;
+  const size_t smem = Smem<CG>::kBytes;
   auto kern = ns_steps_kernel<CG, SPLIT>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
   const long long widest = static_cast<long long>(w.Z) * p.row_blocks * (p.row_blocks > p.col_tiles ? p.row_blocks : p.col_tiles);
