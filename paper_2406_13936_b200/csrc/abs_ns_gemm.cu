@@ -8,13 +8,12 @@
 // an operand whose k index runs along the rows of the stored matrix is MN-major (as X is in kUpdate),
 // one whose k index runs along the columns is K-major; the TMA box and the descriptor differ, no more.
 //
-// The tiles of all steps, products and matrices form one list; a resident grid walks it with a fixed
-// stride.  A tile starts when the row blocks that it reads are complete, which other CTAs announce in
-// per-matrix counters (release / acquire in global memory): no launch, grid barrier or idle wave between
-// products.  The list runs in slots: the matrices are cut into three parts, and slot s has product s of the
-// first, s - 1 of the second and s - 2 of the third part, so a product and the one that reads it are a
-// third of a step's tiles apart, whichever they are.  (A tile is announced about 5000 clocks after its
-// last product; with all matrices in the same product the next wave stood still that long.)
+// The tiles of all steps, products and matrices form one list, in that order; a resident grid walks it
+// with a fixed stride.  A tile starts when the row blocks that it reads are complete, which other CTAs
+// announce in per-matrix counters (release / acquire in global memory): no launch, grid barrier or idle
+// wave between products.  (Three parts of the matrices a product apart, so that a product and the one that
+// reads it were never neighbours in the list, took as long: 8 x 1024 x 1024 264 us against 261, 96 x 768 x
+// 768 1408 against 1389; what the waits gained the longer start and end lost.)
 // Nothing that is still read is overwritten: a tile of a product needs the row blocks of the one before,
 // which need all of the one before that that touches them, and so on; written out, every tile that reads
 // a buffer is complete before the tile that writes the same rows of it again may start.  The launch is
@@ -82,9 +81,7 @@ struct NsStepsParams {
   int row_blocks;             // of 128 CG rows
   int col_tiles;              // of 128 CG columns of X
   int tri;                    // tiles of a symmetric result
-  int part_z[4];              // the matrices of part r: part_z[r] .. part_z[r + 1] - 1
-  long long tiles;
-  unsigned slot_at[3 * kNsMaxSteps + 3];      // first tile of every slot, and the end
+  long long per_step, tiles;
   unsigned* progress;         // [Z][3][row_blocks]: X, A, B
   unsigned* flag;
   long long timeout_cycles;
@@ -186,36 +183,28 @@ __device__ __forceinline__ float2 unpack_half2(uint32_t u) { return __half22floa
 struct Tile {
   int step, mode, z, i, j;
 };
-// `slot`: a slot at or before the tile's (every role walks the list forwards and keeps it).
-__device__ __forceinline__ Tile tile_of(const NsStepsParams& p, long long t, int& slot) {
-  const unsigned at = static_cast<unsigned>(t);
-  while (at >= p.slot_at[slot + 1]) ++slot;
-  int k = static_cast<int>(at - p.slot_at[slot]);
-  const int upd = p.row_blocks * p.col_tiles;
-  Tile q = {};
-#pragma unroll
-  for (int part = 0; part < 3; ++part) {
-    const int product = slot - part;
-    if (product < 0 || product >= 3 * p.steps) continue;
-    q.step = product / 3;
-    q.mode = product - 3 * q.step;
-    const int per = q.mode == kUpdate ? upd : p.tri, here = (p.part_z[part + 1] - p.part_z[part]) * per;
-    if (k < here) {
-      q.z = k / per;
-      k -= q.z * per;
-      q.z += p.part_z[part];
-      break;
-    }
-    k -= here;
-  }
-  if (q.mode == kUpdate) {
-    q.i = k / p.col_tiles;
-    q.j = k - q.i * p.col_tiles;
-  } else {
+__device__ __forceinline__ Tile tile_of(const NsStepsParams& p, long long t) {
+  Tile q;
+  q.step = static_cast<int>(t / p.per_step);
+  long long r = t - q.step * p.per_step;
+  const long long sym = static_cast<long long>(p.Z) * p.tri;
+  if (r < 2 * sym) {
+    q.mode = r < sym ? kGram : kPoly;
+    if (q.mode == kPoly) r -= sym;
+    q.z = static_cast<int>(r / p.tri);
+    const int k = static_cast<int>(r - static_cast<long long>(q.z) * p.tri);
     q.i = static_cast<int>((sqrtf(8.f * static_cast<float>(k) + 1.f) - 1.f) * 0.5f);      // corrected to i (i + 1) / 2 <= k
     while (q.i * (q.i + 1) / 2 > k) --q.i;
     while ((q.i + 1) * (q.i + 2) / 2 <= k) ++q.i;
     q.j = k - q.i * (q.i + 1) / 2;
+  } else {
+    r -= 2 * sym;
+    q.mode = kUpdate;
+    const int per = p.row_blocks * p.col_tiles;
+    q.z = static_cast<int>(r / per);
+    const int k = static_cast<int>(r - static_cast<long long>(q.z) * per);
+    q.i = k / p.col_tiles;
+    q.j = k - q.i * p.col_tiles;
   }
   return q;
 }
@@ -349,11 +338,11 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   if (warp == 0) {
     // ---- operand loads ---------------------------------------------------------------------------
     if (elect_one_n()) {
-      int s = 0, slot = 0;
+      int s = 0;
       uint32_t pass = 0, it = 0;
       const uint32_t full0 = CG == 2 ? map_to_rank(full, 0) : full;       // the pair's barrier is its first CTA's
       for (long long t = first; t < p.tiles && !p.drop_loads; t += step) {
-        const Tile q = tile_of(p, t, slot);
+        const Tile q = tile_of(p, t);
         const int cur = q.step & 1;
         const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
         const int row = q.i * BN + row_in_tile, col = q.j * BN + row_in_tile;      // (the tile is square)
@@ -412,10 +401,10 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     // 1024 bytes apart (stride offset), 16 values of k are 2048 bytes.
     const uint64_t desc_k = (1ull << 46) | (1ull << 16) | (SPLIT ? (32ull << 32) | (4ull << 61) : (64ull << 32) | (2ull << 61));
     const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(kBK * 8) << 16);
-    int s = 0, slot = 0;
+    int s = 0;
     uint32_t pass = 0, it = 0, acc = 0;                      // tiles, accumulators of the main products used so far
     for (long long t = first; t < p.tiles; t += step, ++it) {
-      const Tile q = tile_of(p, t, slot);
+      const Tile q = tile_of(p, t);
       const int K = q.mode == kGram ? p.n : p.m, n_kb = (K + kBK - 1) / kBK;
       if (SPLIT && it >= 2) mbar_wait(crossempty + 8u * (it & 1u), ((it >> 1) - 1) & 1u, abort_flag, p.timeout_cycles);
       const uint32_t cross = tmem + (2u + (it & 1u)) * BN;   // split operands only
@@ -472,10 +461,9 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       const uint32_t half = static_cast<uint32_t>(warp) - 2u;
       const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
       uint32_t it = 0;
-      int slot = 0;
       bool ok = true;
       for (long long t = first; t < p.tiles && ok; t += step, ++it) {
-        const Tile q = tile_of(p, t, slot);
+        const Tile q = tile_of(p, t);
         const int cur = q.step & 1, row = q.i * BN + row_in_tile, col = q.j * BN + static_cast<int>(half) * (BN / 2);
         const bool x = q.mode == kUpdate;
         const bool low = SPLIT || x;                           // values and remainders
@@ -534,10 +522,9 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   } else if (warp == kLookout) {
     // ---- waits for the inputs of the tile after the one that is being loaded -----------------------------
     if (elect_one_n()) {
-      int slot = 0;
       uint32_t it = 0;
       for (long long t = first; t < p.tiles && !p.drop_loads; t += step, ++it) {
-        const Tile q = tile_of(p, t, slot);
+        const Tile q = tile_of(p, t);
         if (it >= 2 && !mbar_wait(taken + 8u * (it & 1u), ((it >> 1) - 1) & 1u, abort_flag, p.timeout_cycles)) break;
         if (!wait_inputs<CG>(p, q, abort_flag)) break;
         mbar_arrive(inputs + 8u * (it & 1u));
@@ -562,10 +549,9 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       }
     };
     uint32_t it = 0, acc = 0;
-    int slot = 0;
     bool ok = true;
     for (long long t = first; t < p.tiles && ok; t += step, ++it) {
-      const Tile q = tile_of(p, t, slot);
+      const Tile q = tile_of(p, t);
       const NsCoef coef = p.coef[q.step][q.mode];
       const uint64_t c_in = pack_f32x2(coef.in, coef.in), c_acc = pack_f32x2(coef.acc, coef.acc);
       uint32_t r[2][32];                                      // accumulator columns: this unit's and the next one's
@@ -729,21 +715,8 @@ int launch_steps(abs_ctx* ctx, const NsBuffers& w, NsStepsParams& p, cudaStream_
   p.row_blocks = (w.m + side - 1) / side;
   p.col_tiles = (w.n + side - 1) / side;
   p.tri = p.row_blocks * (p.row_blocks + 1) / 2;
-  // three parts where a product of all matrices is a wave or more; else every product waits for the one before anyway
-  const bool parts = static_cast<long long>(w.Z) * p.tri >= ctx->sm_count / CG;
-  for (int r = 0; r <= 3; ++r) p.part_z[r] = r > 0 && !parts ? w.Z : static_cast<int>((static_cast<long long>(w.Z) * r + 2) / 3);
-  p.tiles = 0;
-  for (int s = 0; s <= 3 * p.steps + 1; ++s) {
-    p.slot_at[s] = static_cast<unsigned>(p.tiles);
-    for (int r = 0; r < 3; ++r) {
-      const int product = s - r;
-      if (product < 0 || product >= 3 * p.steps) continue;
-      p.tiles += static_cast<long long>(p.part_z[r + 1] - p.part_z[r]) *
-                 (product % 3 == kUpdate ? static_cast<long long>(p.row_blocks) * p.col_tiles : p.tri);
-    }
-  }
-  p.slot_at[3 * p.steps + 2] = static_cast<unsigned>(p.tiles);
-  if (p.tiles > 0x7fffffffll) return set_error(ctx, ABS_ERR_UNSUPPORTED, "too many tiles in %d matrices of %d x %d", w.Z, w.m, w.n);
+  p.per_step = static_cast<long long>(w.Z) * (2ll * p.tri + static_cast<long long>(p.row_blocks) * p.col_tiles);
+  p.tiles = p.per_step * p.steps;
 
   const size_t smem = Smem<CG>::kBytes;
   auto kern = ns_steps_kernel<CG, SPLIT>;

@@ -156,13 +156,13 @@ def test_zero_and_non_finite_matrices(ctx):
 
 def test_groups_give_the_same_bits(ctx):
     """More matrices than are worked on together: each as if alone, and repeatable."""
-    G = matrices(9, 70, 300, 520)
+    G = matrices(9, 130, 300, 520)
     cfg = pkg.make_ns_cfg(precision="f32")
-    need = ctx.ns_scratch(70, 300, 520, cfg).numel()
-    assert need < 69 / 70 * ctx.ns_scratch(1, 300, 520, cfg).numel() * 70
+    one, all_ = (ctx.ns_scratch(k, 300, 520, cfg).numel() for k in (1, 130))
+    assert all_ < 0.6 * 130 * one                            # two groups
     O = orthogonalise(ctx, G, precision="f32")
     assert torch.equal(O, orthogonalise(ctx, G, precision="f32"))
-    for q in (0, 33, 69):
+    for q in (0, 64, 65, 129):
         assert torch.equal(O[q:q + 1], orthogonalise(ctx, G[q:q + 1], precision="f32"))
 
 
@@ -207,7 +207,7 @@ def test_muon_step(ctx, M, L, m, n, pad, nesterov, average):
 
 
 def test_muon_f32_precision_and_many_groups(ctx):
-    M, L, m, n = 4, 20, 300, 520
+    M, L, m, n = 4, 32, 300, 520
     X, _ = replicas(1, M, L, m, n, 0, 0.02)
     B, _ = replicas(2, M, L, m, n, 0, 5e-3)
     G, _ = replicas(3, M, L, m, n, 0, 1e-3)
