@@ -13,8 +13,6 @@
 // ABS_NS_F32 every operand is hi + lo and a product is three tensor-core products (fp32-grade).
 #include <math.h>
 
-#include <cuda_bf16.h>
-
 #include "abs_ns.cuh"
 
 namespace absk {
@@ -23,78 +21,6 @@ namespace {
 constexpr int kTile = 64;
 constexpr int kPassThreads = 256;
 constexpr int kTileVecs = kTile * kTile / 4 / kPassThreads;     // groups of four elements per thread
-
-// Where the matrices of a call live: matrix q is worker q / L, layer q % L.
-struct NsSource {
-  const void* G;          // orthogonalise: the input; Muon: the gradients
-  int src_bf16;
-  float* Buf;             // Muon: momentum buffers
-  float momentum;
-  int nesterov;
-  int muon;
-  int L;
-  long long replica_stride, matrix_stride, row_stride;
-  int rows, cols;
-};
-struct NsTarget {
-  void* O;                // orthogonalise: the result
-  int dst_bf16;
-  float* X;               // Muon: the parameters
-  float decay, step;      // x <- decay x - step o
-  long long replica_stride, matrix_stride, row_stride;
-};
-
-__device__ __forceinline__ long long matrix_base(int q, int L, long long replica_stride, long long matrix_stride) {
-  const int m = q / L;
-  return m * replica_stride + static_cast<long long>(q - m * L) * matrix_stride;
-}
-template <int V>
-__device__ __forceinline__ void load_f32(const float* p, float (&v)[V]) {
-  if constexpr (V == 4) {
-    const float4 f = *reinterpret_cast<const float4*>(p);
-    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
-  } else {
-    v[0] = *p;
-  }
-}
-template <int V>
-__device__ __forceinline__ void store_f32(float* p, const float (&v)[V]) {
-  if constexpr (V == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  else *p = v[0];
-}
-// V consecutive elements at index i of the source, fp32 or bf16.
-template <int V>
-__device__ __forceinline__ void load_src(const NsSource& s, long long i, float (&v)[V]) {
-  if (s.src_bf16) {
-    const unsigned short* p = static_cast<const unsigned short*>(s.G) + i;
-    if constexpr (V == 4) {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
-      v[0] = __uint_as_float(u.x << 16);
-      v[1] = __uint_as_float(u.x & 0xffff0000u);
-      v[2] = __uint_as_float(u.y << 16);
-      v[3] = __uint_as_float(u.y & 0xffff0000u);
-    } else {
-      v[0] = __uint_as_float(static_cast<uint32_t>(*p) << 16);
-    }
-  } else {
-    load_f32<V>(static_cast<const float*>(s.G) + i, v);
-  }
-}
-// The matrix to orthogonalise, after ns_norm_kernel has updated the momentum buffer.
-template <int V>
-__device__ __forceinline__ void load_update(const NsSource& s, long long i, float (&u)[V]) {
-  if (!s.muon) {
-    load_src<V>(s, i, u);
-    return;
-  }
-  load_f32<V>(s.Buf + i, u);
-  if (s.nesterov) {
-    float g[V];
-    load_src<V>(s, i, g);
-#pragma unroll
-    for (int e = 0; e < V; ++e) u[e] = fmaf(s.momentum, u[e], g[e]);
-  }
-}
 
 // Momentum update (Muon) and partial sums of squares in fp64 (no overflow, no lost small entries).
 // V = 4: every group of four elements is 16-byte aligned and lies in one row.
@@ -365,8 +291,14 @@ NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
   // Up to 64 rows the operands are split at either precision: with few rows the roundings of 11 bits do
   // not average out (simulated, worst of 200 Gaussian matrices: 2 x 2 1.8e-2, 4 x 4 6.5e-3, 10 x 1024
   // 2e-3), and a product of one row tile is bound by latency, not by its three tensor-core products.
+  // (Most such matrices are small ones, whose operands are always split.)
   p.split = cfg->precision == ABS_NS_F32 || p.m <= 64;
   return p;
+}
+int group_size(const NsPlan& p, int count);
+size_t scratch_need(const NsPlan& p, int count) {
+  if (ns_small_fits(p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
+  return kNsFixedBytes + group_size(p, count) * p.per_matrix();
 }
 int group_size(const NsPlan& p, int count) {
   long long z = static_cast<long long>(kGroupBytes / p.per_matrix());
@@ -387,7 +319,7 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
            size_t scratch_bytes, cudaStream_t st) {
   const NsPlan p = plan_ns(src.rows, src.cols, cfg);
   const int zmax = group_size(p, count);
-  const size_t need = kNsFixedBytes + zmax * p.per_matrix();
+  const size_t need = scratch_need(p, count);
   if (scratch == nullptr || scratch_bytes < need)
     return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes is too small: %zu needed", scratch_bytes, need);
   // scales of the stored matrices, from bounds on the singular values step by step
@@ -404,6 +336,8 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
   }
   sc.sx[cfg->steps] = pow2_scale(hi);
 
+  if (ns_small_fits(src.rows, src.cols))
+    return launch_ns_small(ctx, src, dst, count, cfg->eps, sc, cfg->steps, cfg->a, cfg->b, cfg->c, st);
   const bool src_vec = vectors_of_four(src.G, src.src_bf16, src.row_stride, src.matrix_stride, src.replica_stride, src.cols) &&
                        vectors_of_four(src.Buf, 0, src.row_stride, src.matrix_stride, src.replica_stride, src.cols);
   const bool dst_vec = vectors_of_four(src.muon ? static_cast<const void*>(dst.X) : dst.O, dst.dst_bf16, dst.row_stride, dst.matrix_stride,
@@ -477,7 +411,7 @@ extern "C" int abs_ns_scratch_bytes(int count, long long rows, long long cols, c
   const int rc = validate_ns(nullptr, count, rows, cols, cfg);
   if (rc != ABS_OK) return rc;
   const NsPlan p = plan_ns(rows, cols, cfg);
-  *out = kNsFixedBytes + group_size(p, count) * p.per_matrix();
+  *out = scratch_need(p, count);
   return ABS_OK;
 }
 

@@ -73,9 +73,6 @@ struct NsMaps {
   // units of the epilogue: boxes of [128 rows][32 columns]
   CUtensorMap xu_h[2], xu_l[2], au_h, au_l, bu_h, bu_l;
 };
-struct NsCoef {
-  float in, acc;              // result = in * (what the epilogue reads) + acc * accumulator
-};
 struct NsStepsParams {
   int Z, m, n, steps;
   int row_blocks;             // of 128 CG rows
@@ -766,12 +763,7 @@ int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float 
   p.flag = ctx->flags + kNsFlagWord;
   p.timeout_cycles = ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles;
   p.drop_loads = ctx->tuning.stats_fault_drop_loads ? 1 : 0;
-  for (int k = 0; k < steps; ++k) {
-    const float sx = sc.sx[k], ta = sc.ta[k], tb = sc.tb[k], next = sc.sx[k + 1];
-    p.coef[k][kGram] = {0.f, ta / (sx * sx)};
-    p.coef[k][kPoly] = {b * (tb / ta), c * (tb / (ta * ta))};
-    p.coef[k][kUpdate] = {a * (next / sx), next / (tb * sx)};
-  }
+  for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
   if (split) return launch_steps<1, true>(ctx, w, p, st);
   const int pairs = ctx->tuning.ns_pair_tiles ? ctx->tuning.ns_pair_tiles == 2 : w.m > 256;
   return pairs ? launch_steps<2, false>(ctx, w, p, st) : launch_steps<1, false>(ctx, w, p, st);

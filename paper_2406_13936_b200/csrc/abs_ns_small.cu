@@ -1,0 +1,468 @@
+// Newton-Schulz orthogonalisation and the Muon step of small matrices (short side m <= 128) in one launch:
+// momentum update, norm, all steps and the result, one thread-block cluster per matrix.
+//
+// X stays in shared memory as value + remainder (two fp16 numbers, 22 bits); a CTA of the cluster has up to
+// 256 of its columns (128 when m > 64 and there are several CTAs).  A step is three tcgen05 products
+// with a barrier after each: the time is latency, not arithmetic, so every product has split operands
+// (hi hi + hi lo + lo hi, fp32-grade) whatever precision is asked for.
+//   A = X X'          K-major rows of X twice; the CTAs' partial sums are added over the cluster: every CTA
+//                     adds its share of the elements, in rank order, and sends it to all
+//   B = b A + c A A   every CTA for itself, in the place of A
+//   X <- a X + B X    every CTA its own columns; X is MN-major here, in the same memory
+// The rows of X and A are padded with zeros to 64 or 128.  All waits are bounded; when one runs out the
+// results of the matrix are NaN.
+//
+// Measured (B200): 4 matrices of 64 x 192 and 8 of 10 x 1024, 5 steps, against the launches of the general
+// path (norm, split, all steps, finish): see the table of cases in the design notes of the product.
+#include "abs_ns.cuh"
+#include "abs_pipeline.cuh"
+
+namespace absk {
+namespace {
+
+constexpr int kWarpsS = 16;
+constexpr int kThreadsS = kWarpsS * 32;
+constexpr int kMaxCluster = 8;
+
+struct SmallParams {
+  NsSource s;
+  NsTarget t;
+  int m, n;            // short and long side
+  int R;               // rows of the stored matrices: 64 or 128
+  int W;               // columns of a CTA
+  int C;               // CTAs of a cluster
+  int steps;
+  float eps, sx, inv_sx;
+  long long timeout_cycles;
+  int drop;            // test hook: no product is issued, so the first wait must run out
+  NsCoef coef[kNsMaxSteps][3];
+};
+
+// ---- PTX ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tcs_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcs_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_s() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync_s() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void umma_s(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_s(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Eight columns of this thread's lane from each of the two accumulators, added.
+__device__ __forceinline__ void tmem_ld8_sum(uint32_t main, uint32_t cross, float (&v)[8]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(main), "r"(cross)
+      : "memory");
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[e]) + __uint_as_float(r[8 + e]);
+}
+__device__ __forceinline__ void sts128_s(uint32_t addr, const uint32_t (&v)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ void st_cluster128(uint32_t addr, const uint32_t (&v)[4]) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+               : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster128(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ double ld_cluster_f64(uint32_t addr) {
+  double v;
+  asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned ld_cluster_u32(uint32_t addr) {
+  unsigned v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// Byte offset of the 16-byte chunk that holds columns 8 ch .. 8 ch + 7 of row r in a matrix stored as blocks of
+// [R rows][64 columns] with the 128-byte swizzle.  The same memory is K-major (columns are k: 8-row groups 1024
+// bytes apart) and MN-major (rows are k: blocks of 64 columns R * 128 bytes apart).
+__device__ __forceinline__ uint32_t chunk_at(int R, int r, int ch) {
+  return static_cast<uint32_t>(ch >> 3) * (static_cast<uint32_t>(R) * 128u) + static_cast<uint32_t>(r) * 128u +
+         ((static_cast<uint32_t>(ch & 7) ^ static_cast<uint32_t>(r & 7)) << 4);
+}
+__device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&h)[4], uint32_t (&l)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 hv = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+    const float2 f = __half22float2(hv);
+    const __half2 lv = __floats2half2_rn(v[2 * e] - f.x, v[2 * e + 1] - f.y);
+    h[e] = *reinterpret_cast<const uint32_t*>(&hv);
+    l[e] = *reinterpret_cast<const uint32_t*>(&lv);
+  }
+}
+__device__ __forceinline__ void join8(const uint4 h, const uint4 l, float (&x)[8]) {
+  const uint32_t hh[4] = {h.x, h.y, h.z, h.w}, ll[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hh[e]));
+    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&ll[e]));
+    x[2 * e] = a.x + b.x;
+    x[2 * e + 1] = a.y + b.y;
+  }
+}
+
+__global__ void __launch_bounds__(kThreadsS, 1)
+ns_small_kernel(const __grid_constant__ SmallParams p) {
+  extern __shared__ unsigned char smem_dyn[];
+  __shared__ double red[kWarpsS];
+  __shared__ double norm_sq;
+  __shared__ unsigned long long bar_mem;
+  __shared__ unsigned abort_mem, tmem_slot;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int C = p.C, R = p.R;
+  const int q = blockIdx.x / C, rank = static_cast<int>(blockIdx.x) - q * C;     // matrix, place in its cluster
+  const int c0 = rank * p.W, wc = p.n - c0 < p.W ? p.n - c0 : p.W;               // this CTA's columns
+  const int Nm = (p.m + 15) & ~15, Nw = (wc + 15) & ~15;
+  const int blocks = (p.W + 63) / 64, mblocks = (p.m + 63) / 64;
+  const uint32_t block_bytes = static_cast<uint32_t>(R) * 128u;
+  const uint32_t raw = smem_u32(smem_dyn), base = (raw + 1023u) & ~1023u;
+  const uint32_t xh = base, xl = xh + blocks * block_bytes, ah = xl + blocks * block_bytes, al = ah + mblocks * block_bytes;
+  const uint32_t part = al + mblocks * block_bytes;                              // partial sums [m][Nm + 4] fp32 (C > 1)
+  const uint32_t pitch = static_cast<uint32_t>(Nm + 4) * 4u;
+  volatile unsigned* abort_flag = &abort_mem;
+  const uint32_t bar = smem_u32(&bar_mem);
+  const uint32_t cross_off = p.W > 128 ? 256u : 128u, tmem_cols = 2u * cross_off;
+  if (tid == 0) {
+    mbar_init(bar, 1);
+    abort_mem = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(tmem_cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // zero X and A (the pad rows and columns stay zero)
+  for (uint32_t o = tid * 16u; o < 2u * (blocks + mblocks) * block_bytes; o += kThreadsS * 16u) {
+    const uint32_t z[4] = {0u, 0u, 0u, 0u};
+    sts128_s(xh + o, z);
+  }
+  tcs_before();
+  __syncthreads();
+  tcs_after();
+  const uint32_t tmem = tmem_slot;
+
+  // ---- momentum update and norm, then X_0 ------------------------------------------------------------
+  // Elements of this CTA in the source's order: X[i][j] is row i, column j of U, or, where U is taller than
+  // wide, row j, column i; columns c0 .. c0 + wc - 1 of X.
+  const bool tall = p.s.rows > p.s.cols;
+  const int inner = tall ? p.m : wc, total = p.m * wc;
+  const long long src = matrix_base(q, p.s.L, p.s.replica_stride, p.s.matrix_stride);
+  auto place = [&](int e, int& i, int& j) {
+    const int o = e / inner, k = e - o * inner;
+    i = tall ? k : o;
+    j = tall ? o : k;                                            // within the CTA's columns
+    return src + static_cast<long long>(tall ? c0 + j : i) * p.s.row_stride + (tall ? i : c0 + j);
+  };
+  double sum = 0.0;
+  for (int e = tid; e < total; e += kThreadsS) {
+    int i, j;
+    const long long at = place(e, i, j);
+    float u[1];
+    load_src<1>(p.s, at, u);
+    if (p.s.muon) {
+      const float b = fmaf(p.s.momentum, p.s.Buf[at], u[0]);
+      p.s.Buf[at] = b;
+      u[0] = p.s.nesterov ? fmaf(p.s.momentum, b, u[0]) : b;
+    }
+    sum = fma(static_cast<double>(u[0]), static_cast<double>(u[0]), sum);
+  }
+  sum = warp_sum(sum);
+  if (lane == 0) red[warp] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    sum = 0.0;
+    for (int w = 0; w < kWarpsS; ++w) sum += red[w];
+    norm_sq = sum;
+  }
+  if (C > 1) cluster_sync_s();
+  else __syncthreads();
+  sum = 0.0;
+  if (C > 1) {
+    for (int r = 0; r < C; ++r) sum += ld_cluster_f64(map_to_rank(smem_u32(&norm_sq), static_cast<uint32_t>(r)));
+  } else {
+    sum = norm_sq;
+  }
+  const double scale = static_cast<double>(p.sx) / (sqrt(sum) + static_cast<double>(p.eps));
+  for (int e = tid; e < total; e += kThreadsS) {
+    int i, j;
+    const long long at = place(e, i, j);
+    float u[1];
+    load_update<1>(p.s, at, u);
+    const float v = static_cast<float>(u[0] * scale);
+    const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
+    const uint32_t o = chunk_at(R, i, j >> 3) + 2u * static_cast<uint32_t>(j & 7);
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(xh + o), "h"(__half_as_ushort(h)) : "memory");
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(xl + o), "h"(__half_as_ushort(l)) : "memory");
+  }
+
+  // ---- steps ---------------------------------------------------------------------------------------------
+  // instruction descriptor: fp32 accumulator, fp16 operands, MN-major second operand (bit 16), N, M = 128; operand
+  // descriptors: 128-byte swizzle, 8-row groups 1024 bytes apart, MN-major blocks of 64 columns block_bytes apart
+  const uint32_t idesc0 = (1u << 4) | (8u << 24);
+  const uint64_t desc_k = (1ull << 46) | (64ull << 32) | (2ull << 61) | (1ull << 16);
+  const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(block_bytes >> 4) << 16);
+  const uint32_t cross = tmem + cross_off;
+  uint32_t phase = 0;
+  // hi hi into the main accumulator; lo hi and hi lo (2^-11 of it) into one of their own
+  auto product16 = [&](uint32_t a_h, uint32_t a_l, uint64_t desc_b, uint32_t b_h, uint32_t b_l, uint32_t idesc, bool first) {
+    const uint64_t dah = desc_k | ((a_h & 0x3ffffu) >> 4), dal = desc_k | ((a_l & 0x3ffffu) >> 4);
+    const uint64_t dbh = desc_b | ((b_h & 0x3ffffu) >> 4), dbl = desc_b | ((b_l & 0x3ffffu) >> 4);
+    umma_s(tmem, dah, dbh, idesc, first ? 0u : 1u);
+    umma_s(cross, dal, dbh, idesc, first ? 0u : 1u);
+    umma_s(cross, dah, dbl, idesc, 1u);
+  };
+  auto wait_products = [&]() {
+    mbar_wait(bar, phase & 1u, abort_flag, p.timeout_cycles);
+    ++phase;
+    __syncwarp();
+    tcs_after();
+  };
+  // The products read what every thread wrote to shared memory and overwrite the accumulators that every warp read.
+  auto before_products = [&]() {
+    fence_proxy_s();
+    tcs_before();
+    __syncthreads();
+    tcs_after();
+  };
+  const int q4 = warp & 3, group = warp >> 2;                    // rows of this warp, its share of the chunks
+  const int row = q4 * 32 + lane;
+  const uint32_t t_row = static_cast<uint32_t>(q4 * 32) << 16;
+  const bool live = q4 * 32 < p.m;                               // (whole warps)
+
+  for (int step = 0; step < p.steps; ++step) {
+    // A = X X'
+    before_products();
+    if (tid == 0 && !p.drop) {
+      fence_proxy_s();
+      const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
+      for (int k = 0; k < Nw; k += 16) {
+        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
+        product16(xh + o, xl + o, desc_k, xh + o, xl + o, idesc, k == 0);
+      }
+      umma_commit_s(bar);
+    }
+    wait_products();
+    const NsCoef gram = p.coef[step][0], poly = p.coef[step][1], upd = p.coef[step][2];
+    if (live) {
+      for (int ch = group; ch < Nm / 8; ch += 4) {
+        float v[8];
+        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= gram.acc;
+        if (row < R) {
+          if (C > 1) {
+            if (row < p.m) {
+              const uint32_t at = part + static_cast<uint32_t>(row) * pitch + 32u * ch;
+              const uint32_t lo[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+              const uint32_t hi[4] = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+              sts128_s(at, lo);
+              sts128_s(at + 16u, hi);
+            }
+          } else {
+            uint32_t h[4], l[4];
+            split8(v, h, l);
+            sts128_s(ah + chunk_at(R, row, ch), h);
+            sts128_s(al + chunk_at(R, row, ch), l);
+          }
+        }
+      }
+    }
+    if (C > 1) {
+      cluster_sync_s();
+      const int per_row = Nm / 8;
+      for (int u = rank + C * tid; u < p.m * per_row; u += C * kThreadsS) {
+        const int r = u / per_row, ch = u - r * per_row;
+        const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < C; ++k) {
+          const uint32_t from = map_to_rank(at, static_cast<uint32_t>(k));
+          const float4 a = ld_cluster128(from), b = ld_cluster128(from + 16u);
+          v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+          v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
+        uint32_t h[4], l[4];
+        split8(v, h, l);
+        for (int k = 0; k < C; ++k) {
+          st_cluster128(map_to_rank(ah + chunk_at(R, r, ch), static_cast<uint32_t>(k)), h);
+          st_cluster128(map_to_rank(al + chunk_at(R, r, ch), static_cast<uint32_t>(k)), l);
+        }
+      }
+      fence_proxy_s();
+      cluster_sync_s();
+    }
+    // B = b A + c A A, in the place of A
+    before_products();
+    if (tid == 0 && !p.drop) {
+      fence_proxy_s();
+      const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
+      for (int k = 0; k < Nm; k += 16) {
+        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
+        product16(ah + o, al + o, desc_k, ah + o, al + o, idesc, k == 0);
+      }
+      umma_commit_s(bar);
+    }
+    wait_products();
+    if (live) {
+      for (int ch = group; ch < Nm / 8; ch += 4) {
+        float v[8], x[8];
+        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+        if (row < R) {
+          const uint32_t o = chunk_at(R, row, ch);
+          join8(lds128(ah + o), lds128(al + o), x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = row < p.m ? fmaf(poly.acc, v[e], poly.in * x[e]) : 0.f;
+          uint32_t h[4], l[4];
+          split8(v, h, l);
+          sts128_s(ah + o, h);
+          sts128_s(al + o, l);
+        }
+      }
+    }
+    // X <- a X + B X
+    before_products();
+    if (tid == 0 && !p.drop) {
+      fence_proxy_s();
+      const uint32_t idesc = idesc0 | (1u << 16) | (static_cast<uint32_t>(Nw >> 3) << 17);
+      for (int k = 0; k < Nm; k += 16) {
+        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
+        const uint32_t x = static_cast<uint32_t>(k) * 128u;      // 16 rows
+        product16(ah + o, al + o, desc_mn, xh + x, xl + x, idesc, k == 0);
+      }
+      umma_commit_s(bar);
+    }
+    wait_products();
+    if (live) {
+      for (int ch = group; ch < Nw / 8; ch += 4) {
+        float v[8], x[8];
+        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+        if (row < p.m) {
+          const uint32_t o = chunk_at(R, row, ch);
+          join8(lds128(xh + o), lds128(xl + o), x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = fmaf(upd.acc, v[e], upd.in * x[e]);
+          uint32_t h[4], l[4];
+          split8(v, h, l);
+          sts128_s(xh + o, h);
+          sts128_s(xl + o, l);
+        }
+      }
+    }
+  }
+  tcs_before();
+  __syncthreads();
+  if (warp == 0) {
+    tcs_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
+  }
+
+  // ---- the result ------------------------------------------------------------------------------------------
+  unsigned failed = abort_mem;
+  if (C > 1) {
+    cluster_sync_s();
+    for (int r = 0; r < C; ++r) failed |= ld_cluster_u32(map_to_rank(smem_u32(&abort_mem), static_cast<uint32_t>(r)));
+  }
+  const float bad = failed ? __int_as_float(0x7fc00000) : 0.f;
+  const long long dst = matrix_base(q, p.s.L, p.t.replica_stride, p.t.matrix_stride);
+  for (int e = tid; e < total; e += kThreadsS) {
+    const int o = e / inner, k = e - o * inner, i = tall ? k : o, j = tall ? o : k;
+    const uint32_t at = chunk_at(R, i, j >> 3) + 2u * static_cast<uint32_t>(j & 7);
+    unsigned short h, l;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(xh + at));
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(l) : "r"(xl + at));
+    const float v = (__half2float(__ushort_as_half(h)) + __half2float(__ushort_as_half(l))) * p.inv_sx + bad;
+    const long long to = dst + static_cast<long long>(tall ? c0 + j : i) * p.t.row_stride + (tall ? i : c0 + j);
+    if (p.s.muon) p.t.X[to] = fmaf(-p.t.step, v, p.t.decay * p.t.X[to]);
+    else if (p.t.dst_bf16) static_cast<__nv_bfloat16*>(p.t.O)[to] = __float2bfloat16_rn(v);
+    else static_cast<float*>(p.t.O)[to] = v;
+  }
+  if (C > 1) cluster_sync_s();                                   // a peer may still read this CTA's abort flag
+}
+
+struct SmallPlan {
+  int R, W, C;
+  size_t smem;
+};
+bool plan_small(long long rows, long long cols, SmallPlan* out) {
+  const int m = static_cast<int>(rows < cols ? rows : cols);
+  const long long n = rows < cols ? cols : rows;
+  if (m > 128) return false;
+  SmallPlan p;
+  p.R = m <= 64 ? 64 : 128;
+  const long long most = p.R == 64 || n <= 256 ? 256 : 128;      // columns of a CTA that fit beside A and the partial sums
+  const long long C = (n + most - 1) / most;
+  if (C > kMaxCluster) return false;
+  p.C = static_cast<int>(C);                                     // with W as below every CTA has columns: n > (C - 1) W
+  p.W = static_cast<int>(((n + C - 1) / C + 15) / 16 * 16);
+  const int Nm = (m + 15) & ~15;
+  const size_t block = static_cast<size_t>(p.R) * 128;
+  // with 64 rows the products read 128: what lies behind the last block has to be shared memory too
+  p.smem = 1024 + 2 * ((p.W + 63) / 64 + (m + 63) / 64) * block + (p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0) + 8192;
+  // One CTA per SM: two of them could want more tensor memory than there is, and a CTA that waits for it while
+  // its cluster waits for the CTA would wait for good.
+  if (p.smem < 120 * 1024) p.smem = 120 * 1024;
+  *out = p;
+  return true;
+}
+
+}  // namespace
+
+bool ns_small_fits(long long rows, long long cols) {
+  SmallPlan p;
+  return plan_small(rows, cols, &p);
+}
+
+int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int count, float eps, const NsScales& sc, int steps,
+                    float a, float b, float c, cudaStream_t st) {
+  SmallPlan plan;
+  if (!plan_small(s.rows, s.cols, &plan)) return ABS_ERR_UNSUPPORTED;
+  SmallParams p = {};
+  p.s = s; p.t = t;
+  p.m = s.rows < s.cols ? s.rows : s.cols;
+  p.n = s.rows < s.cols ? s.cols : s.rows;
+  p.R = plan.R; p.W = plan.W; p.C = plan.C;
+  p.steps = steps;
+  p.eps = eps;
+  p.sx = sc.sx[0];
+  p.inv_sx = 1.0f / sc.sx[steps];
+  p.timeout_cycles = ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles;
+  p.drop = ctx->tuning.stats_fault_drop_loads ? 1 : 0;
+  for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
+  auto kern = ns_small_kernel;
+  ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, plan.smem));
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(plan.C);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  lc.gridDim = dim3(static_cast<unsigned>(count) * plan.C);
+  lc.blockDim = dim3(kThreadsS);
+  lc.dynamicSmemBytes = plan.smem;
+  lc.stream = st;
+  lc.attrs = attr;
+  lc.numAttrs = 1;
+  ABS_CUDA_TRY(ctx, cudaLaunchKernelEx(&lc, kern, p));
+  return ABS_OK;
+}
+
+}  // namespace absk
