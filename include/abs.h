@@ -550,7 +550,8 @@ int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int M, long lon
  * takes them.  dX may be dY or X (same strides).  samples and tokens may be 0 (sums of nothing
  * are zero).  mean, rstd: [M][samples*tokens] as the forward pass wrote them.  All sums are fp32
  * in a fixed order: repeated calls give the same bits.
- * ABS_ERR_WORKSPACE if the context's workspace cannot hold one partial sum per replica.       */
+ * ABS_ERR_WORKSPACE if the context's workspace cannot hold two partial sums of 2d floats (one
+ * per replica, or per sample where only one of Gw and Gb is given, and one more).             */
 int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long dy_row_stride, long long dy_worker_stride,
                             const void* X, long long x_row_stride, long long x_worker_stride, abs_dtype dtype, int M,
                             long long samples, long long tokens, long long d, const float* mean, const float* rstd,

@@ -41,16 +41,24 @@ struct LnBackward {
   int M;
   long long samples, tokens;   // segments of a replica and rows of a segment
   int d;
-  // sums of `rows_per_chunk` rows of a segment: part[((m * samples + i) * chunks + c) * 2d + {0, d} + j]
+  // The rows of all segments in order, `rows_per_cta` to a CTA; the sums of a CTA over its rows of a segment go to
+  // part + part_slot() * 2d, or, where the segment lies within the CTA and both are given, to its rows of Gw and Gb.
   float* part;
-  int chunks;
-  long long rows_per_chunk;
+  long long rows_per_cta;
+  float* Gw;
+  float* Gb;
+  long long g_rs, g_ws;
 };
+// Place of CTA c's sums of segment s (counted over all replicas).  direct: only segments that do not lie within a CTA
+// have one, at most a CTA's first and last; else along the rows each step raises c or s, so no two share a place.
+__device__ __forceinline__ long long part_slot(bool direct, long long c, long long s, long long tokens, long long rows_per_cta) {
+  return direct ? 2 * c + (s * tokens > c * rows_per_cta ? 1 : 0) : c + s;
+}
 struct LnReduce {
   const float* part;
   int M;
-  long long samples;
-  int chunks, d;
+  long long samples, tokens, rows_per_cta;
+  int d, direct;               // direct: segments within one CTA are in G already
   float* Gw;
   float* Gb;
   long long g_rs, g_ws;
@@ -148,35 +156,43 @@ ln_dx_any_kernel(const LnBackward a) {
   }
 }
 
-// Partial sums of dw and db over one chunk of rows: a thread owns a column.
+// The sums of dw and db of any width, stride and alignment: a thread owns a column of one CTA's rows.
 template <typename T>
 __global__ void __launch_bounds__(kLnThreads)
 ln_params_any_kernel(const LnBackward a) {
   pdl_wait();
   const int col_tiles = (a.d + kLnThreads - 1) / kLnThreads;
-  const long long unit = blockIdx.x / col_tiles;                     // (m * samples + i) * chunks + c
-  const int j = static_cast<int>(blockIdx.x - unit * col_tiles) * kLnThreads + threadIdx.x;
-  const long long seg = unit / a.chunks, chunk = unit - seg * a.chunks;
-  const long long m = seg / a.samples, i = seg - m * a.samples;
-  const long long t0 = chunk * a.rows_per_chunk;
-  const long long t1 = t0 + a.rows_per_chunk < a.tokens ? t0 + a.rows_per_chunk : a.tokens;
+  const long long c = blockIdx.x / col_tiles;
+  const int j = static_cast<int>(blockIdx.x - c * col_tiles) * kLnThreads + threadIdx.x;
   if (j >= a.d) return;
-  const long long rows = a.samples * a.tokens;
-  float dw = 0.f, db = 0.f;
-  for (long long t = t0; t < t1; ++t) {
-    const long long r = i * a.tokens + t;
-    const float g = to_f32<T>(static_cast<const T*>(a.dY)[m * a.dy_ws + r * a.dy_rs + j]);
-    const float xh = (to_f32<T>(static_cast<const T*>(a.X)[m * a.x_ws + r * a.x_rs + j]) - a.mean[m * rows + r]) *
-                     a.rstd[m * rows + r];
-    dw = fmaf(g, xh, dw);
-    db += g;
+  const long long rows = a.samples * a.tokens, total = rows * a.M;
+  long long r = c * a.rows_per_cta;
+  const long long end = r + a.rows_per_cta < total ? r + a.rows_per_cta : total;
+  while (r < end) {
+    const long long seg = r / a.tokens, m = seg / a.samples;
+    const long long stop = (seg + 1) * a.tokens < end ? (seg + 1) * a.tokens : end;
+    float dw = 0.f, db = 0.f;
+    for (; r < stop; ++r) {
+      const long long q = r - m * rows;
+      const float g = to_f32<T>(static_cast<const T*>(a.dY)[m * a.dy_ws + q * a.dy_rs + j]);
+      const float xh = (to_f32<T>(static_cast<const T*>(a.X)[m * a.x_ws + q * a.x_rs + j]) - a.mean[r]) * a.rstd[r];
+      dw = fmaf(g, xh, dw);
+      db += g;
+    }
+    float* out_w = a.part + part_slot(a.Gw != nullptr, c, seg, a.tokens, a.rows_per_cta) * 2 * a.d;
+    float* out_b = out_w + a.d;
+    if (a.Gw != nullptr && seg * a.tokens >= c * a.rows_per_cta && stop == (seg + 1) * a.tokens) {
+      const long long g = m * a.g_ws + (seg - m * a.samples) * a.g_rs;
+      out_w = a.Gw + g;
+      out_b = a.Gb + g;
+    }
+    out_w[j] = dw;
+    out_b[j] = db;
   }
-  float* out = a.part + unit * 2 * a.d;
-  out[j] = dw;
-  out[a.d + j] = db;
 }
 
-// Chunks -> samples -> replica: 32 columns of one replica per CTA, 8 lanes of samples, fixed order.
+// Partial sums -> samples -> replica, in a fixed order: 32 columns of one replica per CTA.  Eight lanes share the
+// samples or, where there are few, the partial sums of each.
 __global__ void __launch_bounds__(kLnThreads)
 ln_reduce_kernel(const LnReduce a) {
   __shared__ float red[8][32];
@@ -188,14 +204,38 @@ ln_reduce_kernel(const LnReduce a) {
   const int j = is_b ? col - a.d : col;
   float* G = is_b ? a.Gb : a.Gw;
   float total = 0.f;
-  for (long long i = row; i < a.samples; i += 8) {
-    const float* p = a.part + (m * a.samples + i) * a.chunks * 2 * a.d + col;
+  const bool by_sample = a.samples >= 8 || a.tokens == 0;
+  for (long long i = by_sample ? row : 0; i < a.samples; i += by_sample ? 8 : 1) {
+    const long long seg = m * a.samples + i;
     float s = 0.f;
-    if (live)
-      for (int c = 0; c < a.chunks; ++c) s += p[static_cast<long long>(c) * 2 * a.d];
-    if (live && G) G[m * a.g_ws + i * a.g_rs + j] = s;
-    total += s;
+    if (a.tokens > 0) {
+      const long long c0 = seg * a.tokens / a.rows_per_cta, c1 = ((seg + 1) * a.tokens - 1) / a.rows_per_cta;
+      if (a.direct && c0 == c1) {
+        if (live && (by_sample || row == 0)) total += G[m * a.g_ws + i * a.g_rs + j];
+        continue;
+      }
+      if (live) {
+#pragma unroll 4
+        for (long long c = by_sample ? c0 : c0 + row; c <= c1; c += by_sample ? 1 : 8)
+          s += a.part[part_slot(a.direct, c, seg, a.tokens, a.rows_per_cta) * 2 * a.d + col];
+      }
+    }
+    if (!by_sample) {
+      __syncthreads();
+      red[row][lane] = s;
+      __syncthreads();
+      s = 0.f;
+      if (row == 0) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += red[k][lane];
+      }
+    }
+    if (live && (by_sample || row == 0)) {
+      if (G) G[m * a.g_ws + i * a.g_rs + j] = s;
+      total += s;
+    }
   }
+  __syncthreads();
   red[row][lane] = total;
   __syncthreads();
   float* out = is_b ? a.dB : a.dW;
@@ -204,6 +244,338 @@ ln_reduce_kernel(const LnReduce a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += red[k][lane];
     out[m * a.grad_stride + j] = s;
+  }
+}
+
+// ---- rows held in registers -----------------------------------------------------------------------------
+// A group of `tpr` threads (whole warps) has a row: thread t holds the pieces t, t + tpr, ... of V elements, NV
+// of them.  The next row's loads are issued before this row's arithmetic, weights (and, backward, the sums of
+// dw and db) stay in registers from row to row, and a row is read and written once.  Sums over a row: shuffles,
+// and through shared memory with a barrier of the group's own where it has several warps.
+constexpr int kFastThreads = 384;
+
+template <typename T, int V> struct Piece;       // V elements as one load
+template <> struct Piece<float, 4> { typedef uint4 Raw; };
+template <> struct Piece<float, 1> { typedef uint32_t Raw; };
+template <> struct Piece<__nv_bfloat16, 8> { typedef uint4 Raw; };
+template <> struct Piece<__nv_bfloat16, 2> { typedef uint32_t Raw; };
+template <> struct Piece<__nv_bfloat16, 1> { typedef unsigned short Raw; };
+
+__device__ __forceinline__ uint4 ld_once(const uint4* p) { return __ldcs(p); }
+__device__ __forceinline__ uint32_t ld_once(const uint32_t* p) { return __ldcs(p); }
+__device__ __forceinline__ unsigned short ld_once(const unsigned short* p) { return __ldcs(p); }
+template <typename R> __device__ __forceinline__ void st_once(R* p, const R& v) { __stcs(p, v); }
+__device__ __forceinline__ void zero_raw(uint4& r) { r = make_uint4(0u, 0u, 0u, 0u); }
+__device__ __forceinline__ void zero_raw(uint32_t& r) { r = 0u; }
+__device__ __forceinline__ void zero_raw(unsigned short& r) { r = 0; }
+
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const typename Piece<T, V>::Raw& r, float (&x)[V]) {
+  if constexpr (sizeof(T) == 4 && V == 4) {
+    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+  } else if constexpr (sizeof(T) == 4) {
+    x[0] = __uint_as_float(r);
+  } else if constexpr (V == 8) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  } else if constexpr (V == 2) {
+    x[0] = __uint_as_float(r << 16);
+    x[1] = __uint_as_float(r & 0xffff0000u);
+  } else {
+    x[0] = __uint_as_float(static_cast<uint32_t>(r) << 16);
+  }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T, int V>
+__device__ __forceinline__ typename Piece<T, V>::Raw pack(const float (&x)[V]) {
+  if constexpr (sizeof(T) == 4 && V == 4) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  } else if constexpr (sizeof(T) == 4) {
+    return __float_as_uint(x[0]);
+  } else if constexpr (V == 8) {
+    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  } else if constexpr (V == 2) {
+    return pack_bf16(x[0], x[1]);
+  } else {
+    return __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
+  }
+}
+
+// Sums over a group's threads, the same in each.  red: [2][32] of the group; the two halves alternate, so one
+// barrier a sum is enough.
+template <bool ONE_WARP>
+__device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int& flip, int group, int t, int tpr) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, off);
+    b += __shfl_xor_sync(0xffffffffu, b, off);
+  }
+  if constexpr (ONE_WARP) return make_float2(a, b);
+  float2* r = red + 32 * flip;
+  flip ^= 1;
+  if ((t & 31) == 0) r[t >> 5] = make_float2(a, b);
+  named_bar_sync(1 + group, tpr);
+  float2 s = make_float2(0.f, 0.f);
+  for (int w = 0; w < tpr / 32; ++w) {
+    s.x += r[w].x;
+    s.y += r[w].y;
+  }
+  return s;
+}
+
+template <int NV, int V>
+__device__ __forceinline__ void load_params(const float* p, float other, int t, int tpr, int pieces, float (&w)[NV][V]) {
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[k][e] = p != nullptr && v < pieces ? __ldg(p + v * V + e) : other;
+  }
+}
+
+template <typename T, int V, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(kFastThreads)
+ln_forward_kernel(const LnForward a, int tpr, long long per_group) {
+  typedef typename Piece<T, V>::Raw Raw;
+  __shared__ float2 red_mem[12][2][32];
+  const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
+  const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / V;
+  float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
+  int flip = 0;
+  const long long total = a.rows * a.M;
+  long long rr = (static_cast<long long>(blockIdx.x) * groups + group) * per_group;
+  const long long end = rr + per_group < total ? rr + per_group : total;
+  long long m = rr / a.rows, r = rr - m * a.rows;
+  pdl_wait();
+  Raw next[NV];
+  auto fetch = [&](long long mm, long long row) {
+    const T* x = static_cast<const T*>(a.X) + mm * a.x_ws + row * a.x_rs;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) next[k] = ld_once(reinterpret_cast<const Raw*>(x) + v);
+      else zero_raw(next[k]);
+    }
+  };
+  if (rr < end) fetch(m, r);
+  float w[NV][V], b[NV][V];
+  bool have = false;
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  for (; rr < end; ++rr) {
+    if (!have) {
+      load_params<NV, V>(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
+      load_params<NV, V>(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, t, tpr, pieces, b);
+      have = true;
+    }
+    float x[NV][V];
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      unpack<T, V>(next[k], x[k]);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s += x[k][e];
+    }
+    T* y = static_cast<T*>(a.Y) + m * a.y_ws + r * a.y_rs;
+    const bool same = r + 1 < a.rows;
+    if (same) {
+      ++r;
+    } else {
+      r = 0;
+      ++m;
+      have = a.p_stride == 0;
+    }
+    if (rr + 1 < end) fetch(m, r);
+    const float mean = group_sum2<ONE_WARP>(s, 0.f, red, flip, group, t, tpr).x * inv_d;
+    float q = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const bool in = t + k * tpr < pieces;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        x[k][e] -= mean;
+        if (in) q = fmaf(x[k][e], x[k][e], q);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(fmaf(group_sum2<ONE_WARP>(q, 0.f, red, flip, group, t, tpr).x, inv_d, a.eps));
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) {
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = fmaf(x[k][e] * rstd, w[k][e], b[k][e]);
+        st_once(reinterpret_cast<Raw*>(y) + v, pack<T, V>(o));
+      }
+    }
+    if (t == 0) {
+      if (a.mean) a.mean[rr] = mean;
+      if (a.rstd) a.rstd[rr] = rstd;
+    }
+  }
+}
+
+// A CTA has rows_per_cta rows in a run; its groups take them in turn.  Where a segment ends, the groups' sums are
+// added in order through shared memory and leave.
+template <typename T, int V, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(kFastThreads, (V * NV <= 8 ? 2 : 1))
+ln_backward_kernel(const LnBackward a, int tpr) {
+  typedef typename Piece<T, V>::Raw Raw;
+  extern __shared__ float sums[];                                     // [groups - 1][2 d]
+  __shared__ float2 red_mem[6][2][32];
+  const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
+  const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / V;
+  float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
+  int flip = 0;
+  const long long rows = a.samples * a.tokens, total = rows * a.M;    // of a replica, of all
+  const long long first = static_cast<long long>(blockIdx.x) * a.rows_per_cta;
+  const long long end = first + a.rows_per_cta < total ? first + a.rows_per_cta : total;
+  long long row = first + group;                                      // this group's row among all
+  long long m = row / rows, r = row - m * rows;                       // ... its replica and place there
+  pdl_wait();
+  Raw nx[NV], ng[NV];
+  float n_mean = 0.f, n_rstd = 0.f;
+  auto fetch = [&]() {
+    const Raw* x = reinterpret_cast<const Raw*>(static_cast<const T*>(a.X) + m * a.x_ws + r * a.x_rs);
+    const Raw* g = reinterpret_cast<const Raw*>(static_cast<const T*>(a.dY) + m * a.dy_ws + r * a.dy_rs);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) {
+        nx[k] = ld_once(x + v);
+        ng[k] = ld_once(g + v);
+      } else {
+        zero_raw(nx[k]);
+        zero_raw(ng[k]);
+      }
+    }
+    n_mean = __ldg(a.mean + row);
+    n_rstd = __ldg(a.rstd + row);
+  };
+  if (row < end) fetch();
+  float w[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[k][e] = db[k][e] = 0.f;
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  long long have = -1;                                                // the replica whose weight is in w
+  long long seg = first / a.tokens;
+  for (long long at = first; at < end; ++seg) {
+    const long long stop = (seg + 1) * a.tokens < end ? (seg + 1) * a.tokens : end;
+    const long long sm = seg / a.samples;                             // the segment's replica
+    if (sm != have) {
+      if (have < 0 || a.p_stride != 0)
+        load_params<NV, V>(a.weight ? a.weight + sm * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
+      have = sm;
+    }
+    while (row < stop) {
+      Raw cx[NV], cg[NV];
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        cx[k] = nx[k];
+        cg[k] = ng[k];
+      }
+      const float mean = n_mean, rstd = n_rstd;
+      Raw* o = reinterpret_cast<Raw*>(static_cast<T*>(a.dX) + m * a.dx_ws + r * a.dx_rs);
+      row += groups;
+      r += groups;
+      while (r >= rows) {
+        r -= rows;
+        ++m;
+      }
+      if (row < end) fetch();
+      float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        float x[V], g[V];
+        unpack<T, V>(cx[k], x);
+        unpack<T, V>(cg[k], g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float xh = (x[e] - mean) * rstd, y = g[e] * w[k][e];
+          s1 += y;
+          s2 = fmaf(y, xh, s2);
+          dw[k][e] = fmaf(g[e], xh, dw[k][e]);
+          db[k][e] += g[e];
+        }
+      }
+      if (a.dX != nullptr) {
+        const float2 s = group_sum2<ONE_WARP>(s1, s2, red, flip, group, t, tpr);
+        const float c1 = s.x * inv_d, c2 = s.y * inv_d;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int v = t + k * tpr;
+          float x[V], g[V], q[V];
+          unpack<T, V>(cx[k], x);
+          unpack<T, V>(cg[k], g);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float xh = (x[e] - mean) * rstd;
+            q[e] = rstd * (fmaf(g[e], w[k][e], -c1) - xh * c2);
+          }
+          if (v < pieces) st_once(o + v, pack<T, V>(q));
+        }
+      }
+    }
+    if (a.part != nullptr) {
+      // pieces past the row have zeros in dy: their sums are zero and not stored
+      float* out_w = a.part + part_slot(a.Gw != nullptr, blockIdx.x, seg, a.tokens, a.rows_per_cta) * 2 * a.d;
+      float* out_b = out_w + a.d;
+      if (a.Gw != nullptr && at == seg * a.tokens && stop == (seg + 1) * a.tokens) {
+        const long long g = sm * a.g_ws + (seg - sm * a.samples) * a.g_rs;
+        out_w = a.Gw + g;
+        out_b = a.Gb + g;
+      }
+      if (groups > 1) {
+        if (group > 0) {
+          float* p = sums + static_cast<long long>(group - 1) * 2 * a.d;
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            const int v = t + k * tpr;
+            if (v < pieces) {
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                p[v * V + e] = dw[k][e];
+                p[a.d + v * V + e] = db[k][e];
+              }
+            }
+          }
+        }
+        __syncthreads();
+      }
+      if (group == 0) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int v = t + k * tpr;
+          if (v < pieces) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              float sw = dw[k][e], sb = db[k][e];
+              for (int o = 0; o < groups - 1; ++o) {
+                const float* p = sums + static_cast<long long>(o) * 2 * a.d + v * V + e;
+                sw += p[0];
+                sb += p[a.d];
+              }
+              out_w[v * V + e] = sw;
+              out_b[v * V + e] = sb;
+            }
+          }
+        }
+      }
+      if (groups > 1) __syncthreads();
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[k][e] = db[k][e] = 0.f;
+    }
+    at = stop;
   }
 }
 
@@ -237,6 +609,98 @@ unsigned row_grid(const abs_ctx* ctx, long long rows) {
   return static_cast<unsigned>(rows < most ? rows : most);
 }
 
+
+// How a row of d elements is laid out over threads, or tpr = 0 where it does not fit: V elements a piece (16 bytes,
+// or what d and the alignment allow), the fewest threads (a divisor of the CTA's) that hold it in at most 4
+// pieces of 16 bytes (backward of bf16, where each element has two running sums, 3) or 16 elements each.
+struct RowPlan {
+  int V, NV, tpr;
+};
+RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits, int most16) {
+  const int es = dtype == ABS_F32 ? 4 : 2;
+  RowPlan p = {1, 0, 0};
+  align_bits |= static_cast<unsigned long long>(d) * es;
+  if ((align_bits & 15u) == 0) p.V = 16 / es;
+  else if (es == 2 && (align_bits & 3u) == 0) p.V = 2;
+  const long long pieces = d / p.V;
+  const int most = p.V * es == 16 ? most16 : 16 / p.V;
+  const int tprs[6] = {32, 64, 96, 128, 192, 384};
+  for (int k = 0; k < 6; ++k)
+    if (pieces <= static_cast<long long>(tprs[k]) * most) {
+      p.tpr = tprs[k];
+      p.NV = static_cast<int>((pieces + p.tpr - 1) / p.tpr);
+      break;
+    }
+  if (p.V * es != 16 && p.NV > 0) p.NV = most;                     // one variant of the narrow pieces
+  return p;
+}
+
+template <typename T, int V, int NV>
+cudaError_t run_forward(abs_ctx* ctx, const LnForward& a, int tpr, cudaStream_t st) {
+  const int groups = kFastThreads / tpr;
+  const long long total = a.rows * a.M;
+  const long long most = static_cast<long long>(ctx->sm_count) * 2 * groups;       // two CTAs per SM
+  const long long per = (total + most - 1) / most;
+  const long long used = (total + per - 1) / per;
+  const unsigned grid = static_cast<unsigned>((used + groups - 1) / groups);
+  if (tpr == 32) return launch_dependent(ln_forward_kernel<T, V, NV, true>, dim3(grid), dim3(kFastThreads), 0, st, a, tpr, per);
+  return launch_dependent(ln_forward_kernel<T, V, NV, false>, dim3(grid), dim3(kFastThreads), 0, st, a, tpr, per);
+}
+cudaError_t dispatch_forward(abs_ctx* ctx, const LnForward& a, abs_dtype dtype, const RowPlan& p, cudaStream_t st) {
+  if (dtype == ABS_F32) {
+    if (p.V == 1) return run_forward<float, 1, 16>(ctx, a, p.tpr, st);
+    switch (p.NV) {
+      case 1: return run_forward<float, 4, 1>(ctx, a, p.tpr, st);
+      case 2: return run_forward<float, 4, 2>(ctx, a, p.tpr, st);
+      case 3: return run_forward<float, 4, 3>(ctx, a, p.tpr, st);
+      default: return run_forward<float, 4, 4>(ctx, a, p.tpr, st);
+    }
+  }
+  if (p.V == 1) return run_forward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, st);
+  if (p.V == 2) return run_forward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, st);
+  switch (p.NV) {
+    case 1: return run_forward<__nv_bfloat16, 8, 1>(ctx, a, p.tpr, st);
+    case 2: return run_forward<__nv_bfloat16, 8, 2>(ctx, a, p.tpr, st);
+    case 3: return run_forward<__nv_bfloat16, 8, 3>(ctx, a, p.tpr, st);
+    default: return run_forward<__nv_bfloat16, 8, 4>(ctx, a, p.tpr, st);
+  }
+}
+
+template <typename T, int V, int NV>
+cudaError_t run_backward(abs_ctx* ctx, const LnBackward& a, int tpr, int groups, unsigned grid, cudaStream_t st) {
+  const size_t smem = a.part != nullptr ? static_cast<size_t>(groups - 1) * 2 * a.d * sizeof(float) : 0;
+  auto one = ln_backward_kernel<T, V, NV, true>;
+  auto many = ln_backward_kernel<T, V, NV, false>;
+  cudaError_t e = cudaSuccess;
+  if (smem > 40 * 1024) e = tpr == 32 ? ensure_dynamic_smem(ctx, one, smem) : ensure_dynamic_smem(ctx, many, smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(tpr == 32 ? one : many, dim3(grid), dim3(tpr * groups), smem, st, a, tpr);
+}
+cudaError_t dispatch_backward(abs_ctx* ctx, const LnBackward& a, abs_dtype dtype, const RowPlan& p, int groups, unsigned grid,
+                              cudaStream_t st) {
+  if (dtype == ABS_F32) {
+    if (p.V == 1) return run_backward<float, 1, 16>(ctx, a, p.tpr, groups, grid, st);
+    switch (p.NV) {
+      case 1: return run_backward<float, 4, 1>(ctx, a, p.tpr, groups, grid, st);
+      case 2: return run_backward<float, 4, 2>(ctx, a, p.tpr, groups, grid, st);
+      case 3: return run_backward<float, 4, 3>(ctx, a, p.tpr, groups, grid, st);
+      default: return run_backward<float, 4, 4>(ctx, a, p.tpr, groups, grid, st);
+    }
+  }
+  if (p.V == 1) return run_backward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, groups, grid, st);
+  if (p.V == 2) return run_backward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, groups, grid, st);
+  switch (p.NV) {
+    case 1: return run_backward<__nv_bfloat16, 8, 1>(ctx, a, p.tpr, groups, grid, st);
+    case 2: return run_backward<__nv_bfloat16, 8, 2>(ctx, a, p.tpr, groups, grid, st);
+    default: return run_backward<__nv_bfloat16, 8, 3>(ctx, a, p.tpr, groups, grid, st);
+  }
+}
+
+unsigned long long row_bits(const void* p, abs_dtype dtype, int M, long long rs, long long ws) {
+  const unsigned long long es = dtype == ABS_F32 ? 4 : 2;
+  return reinterpret_cast<uintptr_t>(p) | static_cast<unsigned long long>(rs) * es | (M > 1 ? static_cast<unsigned long long>(ws) * es : 0);
+}
+
 }  // namespace
 }  // namespace absk
 
@@ -261,6 +725,12 @@ extern "C" int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int 
   LnForward a{X, x_row_stride, x_worker_stride, weight, bias, param_stride, eps, Y, y_row_stride, y_worker_stride,
               mean, rstd, M, rows, static_cast<int>(d)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const RowPlan plan = plan_row(dtype, d, row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
+                                              row_bits(Y, dtype, M, y_row_stride, y_worker_stride), 4);
+  if (plan.tpr > 0) {
+    ABS_CUDA_TRY(ctx, dispatch_forward(ctx, a, dtype, plan, st));
+    return ABS_OK;
+  }
   const dim3 grid(row_grid(ctx, rows * M));
   if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_forward_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
   else ABS_CUDA_TRY(ctx, launch_dependent(ln_forward_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
@@ -301,39 +771,67 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
     tokens = rows;
   }
   LnBackward a{dY, dy_row_stride, dy_worker_stride, X, x_row_stride, x_worker_stride, mean, rstd, weight, param_stride,
-               dX, dx_row_stride, dx_worker_stride, M, samples, tokens, static_cast<int>(d), nullptr, 1, tokens};
-  const long long col_tiles = (d + kLnThreads - 1) / kLnThreads;
-  long long chunks = 0;
-  if (rows > 0 && (per_sample || totals)) {
-    const long long segments = samples * M;
-    const long long room = static_cast<long long>(ctx->workspace_bytes / (2 * sizeof(float))) / d;     // units
-    if (room < segments)
-      return set_error(ctx, ABS_ERR_WORKSPACE, "the workspace holds %lld partial sums of %lld needed", room, segments);
-    chunks = (static_cast<long long>(ctx->sm_count) * 8 + segments * col_tiles - 1) / (segments * col_tiles);
-    const long long by_rows = (tokens + 15) / 16;                    // at least 16 rows per chunk
-    if (chunks > by_rows) chunks = by_rows;
-    if (chunks > room / segments) chunks = room / segments;
-    if (chunks < 1) chunks = 1;
-    a.part = static_cast<float*>(ctx->workspace);
-    a.rows_per_chunk = (tokens + chunks - 1) / chunks;
-    chunks = (tokens + a.rows_per_chunk - 1) / a.rows_per_chunk;
-    a.chunks = static_cast<int>(chunks);
-    const long long blocks = segments * chunks * col_tiles;
-    if (blocks > 0x7fffffffll) return set_error(ctx, ABS_ERR_UNSUPPORTED, "too many samples (%lld) of width %lld", segments, d);
-    const dim3 grid(static_cast<unsigned>(blocks));
-    if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
-    else ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
+               dX, dx_row_stride, dx_worker_stride, M, samples, tokens, static_cast<int>(d), nullptr, 1, nullptr, nullptr, 0, 0};
+  const RowPlan plan = plan_row(dtype, d, row_bits(dY, dtype, M, dy_row_stride, dy_worker_stride) |
+                                              row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
+                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0),
+                                dtype == ABS_F32 ? 4 : 3);
+  const bool sums = per_sample || totals;
+  LnReduce red{static_cast<const float*>(ctx->workspace), M, samples, tokens, 1, static_cast<int>(d), 0, Gw, Gb, g_row_stride,
+               g_worker_stride, dW, dB, grad_stride};
+  if (rows > 0) {
+    const bool fast = plan.tpr > 0;
+    const long long total = rows * M, segments = samples * M;
+    // Groups of a CTA share segments; short ones (up to two rows a group) are better off with CTAs of one group.
+    int groups = 1;
+    long long ctas;
+    if (fast) {
+      groups = kFastThreads / plan.tpr;
+      if (tokens < 2 * groups && sums) groups = 1;
+      const int per_sm = groups > 1 || plan.tpr == kFastThreads ? (plan.V * plan.NV <= 8 ? 2 : 1)
+                                                                : (plan.V * plan.NV <= 8 ? 2 : 1) * kFastThreads / plan.tpr;
+      ctas = static_cast<long long>(ctx->sm_count) * per_sm;
+    } else {
+      ctas = static_cast<long long>(ctx->sm_count) * 8 * kLnThreads / (d < kLnThreads ? kLnThreads : d);
+      if (ctas < ctx->sm_count) ctas = ctx->sm_count;
+    }
+    const long long worth = (total + 2 * groups - 1) / (2 * groups);         // at least two rows a group
+    if (ctas > worth) ctas = worth;
+    if (sums) {
+      const long long room = static_cast<long long>(ctx->workspace_bytes / (2 * sizeof(float))) / d;     // partial sums
+      const bool direct = Gw != nullptr && Gb != nullptr;
+      const long long needed = direct ? 2 : segments + 1, most = direct ? room / 2 : room - segments;
+      if (room < needed)
+        return set_error(ctx, ABS_ERR_WORKSPACE, "the workspace holds %lld partial sums of %lld needed", room, needed);
+      if (ctas > most) ctas = most;
+      a.part = static_cast<float*>(ctx->workspace);
+      if (direct) {
+        a.Gw = Gw; a.Gb = Gb; a.g_rs = g_row_stride; a.g_ws = g_worker_stride;
+        red.direct = 1;
+      }
+    }
+    if (ctas < 1) ctas = 1;
+    a.rows_per_cta = (total + ctas - 1) / ctas;
+    if (groups == 1 && sums && a.rows_per_cta > tokens) a.rows_per_cta = a.rows_per_cta / tokens * tokens;      // whole segments
+    ctas = (total + a.rows_per_cta - 1) / a.rows_per_cta;
+    red.rows_per_cta = a.rows_per_cta;
+    if (fast) {
+      ABS_CUDA_TRY(ctx, dispatch_backward(ctx, a, dtype, plan, groups, static_cast<unsigned>(ctas), st));
+    } else {
+      if (sums) {
+        const dim3 grid(static_cast<unsigned>(ctas * ((d + kLnThreads - 1) / kLnThreads)));
+        if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
+        else ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
+      }
+      if (dX) {                    // after the sums: dX may take the place of dY or X
+        const dim3 grid(row_grid(ctx, total));
+        if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
+        else ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
+      }
+    }
   }
-  // after the sums: dX may take the place of dY or X
-  if (dX && rows > 0) {
-    const dim3 grid(row_grid(ctx, rows * M));
-    if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
-    else ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
-  }
-  if (!per_sample && !totals) return ABS_OK;
-  LnReduce r{static_cast<const float*>(ctx->workspace), M, samples, static_cast<int>(chunks), static_cast<int>(d), Gw, Gb,
-             g_row_stride, g_worker_stride, dW, dB, grad_stride};
-  ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M), dim3(kLnThreads), 0,
-                                     st, r));
+  if (sums)
+    ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M), dim3(kLnThreads), 0,
+                                       st, red));
   return ABS_OK;
 }
