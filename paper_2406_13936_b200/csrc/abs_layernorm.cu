@@ -248,45 +248,32 @@ ln_reduce_kernel(const LnReduce a) {
 }
 
 // ---- rows held in registers -----------------------------------------------------------------------------
-// A group of `tpr` threads (whole warps) has a row: thread t holds the pieces t, t + tpr, ... of V elements, NV
-// of them.  The next row's loads are issued before this row's arithmetic, weights (and, backward, the sums of
-// dw and db) stay in registers from row to row, and a row is read and written once.  Sums over a row: shuffles,
-// and through shared memory with a barrier of the group's own where it has several warps.
+// Rows that are not 16-byte aligned, in pieces of one element or, bf16, two.  A group of `tpr` threads (whole warps)
+// has a row: thread t holds the pieces t, t + tpr, ... of V elements, NV of them.  The next row's loads are issued before
+// this row's arithmetic, weights (and, backward, the sums of dw and db) stay in registers from row to row, and a row is
+// read and written once.  Sums over a row: shuffles, and through shared memory with a barrier of the group's own where
+// it has several warps.  (Narrow pieces through a ring of asynchronous copies, as below: 40000 x 1021 fp32 72 -> 92 us
+// forward, 121 -> 170 backward: each copy is an instruction and 4 bytes.)
 constexpr int kFastThreads = 384;
 
 template <typename T, int V> struct Piece;       // V elements as one load
-template <> struct Piece<float, 4> { typedef uint4 Raw; };
 template <> struct Piece<float, 1> { typedef uint32_t Raw; };
-template <> struct Piece<__nv_bfloat16, 8> { typedef uint4 Raw; };
 template <> struct Piece<__nv_bfloat16, 2> { typedef uint32_t Raw; };
 template <> struct Piece<__nv_bfloat16, 1> { typedef unsigned short Raw; };
 
-__device__ __forceinline__ uint4 ld_once(const uint4* p) { return __ldcs(p); }
 __device__ __forceinline__ uint32_t ld_once(const uint32_t* p) { return __ldcs(p); }
 __device__ __forceinline__ unsigned short ld_once(const unsigned short* p) { return __ldcs(p); }
 template <typename R> __device__ __forceinline__ void st_once(R* p, const R& v) { __stcs(p, v); }
-__device__ __forceinline__ void zero_raw(uint4& r) { r = make_uint4(0u, 0u, 0u, 0u); }
 __device__ __forceinline__ void zero_raw(uint32_t& r) { r = 0u; }
 __device__ __forceinline__ void zero_raw(unsigned short& r) { r = 0; }
 
 template <typename T, int V>
 __device__ __forceinline__ void unpack(const typename Piece<T, V>::Raw& r, float (&x)[V]) {
-  if constexpr (sizeof(T) == 4 && V == 4) {
-    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
-  } else if constexpr (sizeof(T) == 4) {
+  if constexpr (sizeof(T) == 4) {
     x[0] = __uint_as_float(r);
-  } else if constexpr (V == 8) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
-  } else if constexpr (V == 2) {
-    x[0] = __uint_as_float(r << 16);
-    x[1] = __uint_as_float(r & 0xffff0000u);
   } else {
     x[0] = __uint_as_float(static_cast<uint32_t>(r) << 16);
+    if constexpr (V == 2) x[1] = __uint_as_float(r & 0xffff0000u);
   }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -295,17 +282,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 template <typename T, int V>
 __device__ __forceinline__ typename Piece<T, V>::Raw pack(const float (&x)[V]) {
-  if constexpr (sizeof(T) == 4 && V == 4) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-  } else if constexpr (sizeof(T) == 4) {
-    return __float_as_uint(x[0]);
-  } else if constexpr (V == 8) {
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-  } else if constexpr (V == 2) {
-    return pack_bf16(x[0], x[1]);
-  } else {
-    return __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
-  }
+  if constexpr (sizeof(T) == 4) return __float_as_uint(x[0]);
+  else if constexpr (V == 2) return pack_bf16(x[0], x[1]);
+  else return __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
 }
 
 // Sums over a group's threads, the same in each.  red: [2][32] of the group; the two halves alternate, so one
@@ -424,7 +403,7 @@ ln_forward_kernel(const LnForward a, int tpr, long long per_group) {
 // A CTA has rows_per_cta rows in a run; its groups take them in turn.  Where a segment ends, the groups' sums are
 // added in order through shared memory and leave.
 template <typename T, int V, int NV, bool ONE_WARP>
-__global__ void __launch_bounds__(kFastThreads, (V * NV <= 8 ? 2 : 1))
+__global__ void __launch_bounds__(kFastThreads)
 ln_backward_kernel(const LnBackward a, int tpr) {
   typedef typename Piece<T, V>::Raw Raw;
   extern __shared__ float sums[];                                     // [groups - 1][2 d]
@@ -579,6 +558,428 @@ ln_backward_kernel(const LnBackward a, int tpr) {
   }
 }
 
+// ---- rows staged in shared memory ---------------------------------------------------------------------------
+// Rows whose pieces of 16 bytes are aligned.  A thread copies its own pieces of the rows ahead into its own places of a
+// ring with cp.async, so the bytes under way do not depend on registers and nobody waits for anybody else's copies.
+// (8 x 16384 x 768 bf16, forward / backward: with the next row in registers, 12 warps an SM, 95 / 167 us; with bulk
+// copies of whole rows and an mbarrier each 78 / 260 us.)  A group works on two rows at a time where it can: their sums
+// go through the same shuffles and barriers.  Arithmetic on pairs of elements (fma.rn.f32x2): at 2 bytes an element the
+// issue slots are the other limit.
+constexpr int kRingThreads = 384;
+constexpr int kAhead = 4;                          // rows under way besides the two that are worked on
+constexpr int kRing = kAhead + 2;
+constexpr int kBackRing = 4;                       // backward, with two tensors: one row at a time, three under way
+
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+  return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum2(uint64_t v) {
+  const float2 f = unpair(v);
+  return f.x + f.y;
+}
+// A piece of 16 bytes as pairs of fp32: 2 (fp32) or 4 (bf16).
+template <typename T>
+__device__ __forceinline__ void read_piece(uint32_t addr, uint64_t (&x)[8 / sizeof(T)]) {
+  const uint4 r = lds128(addr);
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  if constexpr (sizeof(T) == 4) {
+    x[0] = pair(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    x[1] = pair(__uint_as_float(w[2]), __uint_as_float(w[3]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = pair(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+  }
+}
+template <typename T>
+__device__ __forceinline__ void write_piece(void* p, const uint64_t (&x)[8 / sizeof(T)]) {
+  uint32_t w[4];
+  if constexpr (sizeof(T) == 4) {
+    const float2 a = unpair(x[0]), b = unpair(x[1]);
+    w[0] = __float_as_uint(a.x); w[1] = __float_as_uint(a.y); w[2] = __float_as_uint(b.x); w[3] = __float_as_uint(b.y);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = unpair(x[e]);
+      w[e] = pack_bf16(f.x, f.y);
+    }
+  }
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+}
+__device__ __forceinline__ void copy_ahead(uint32_t dst, const char* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// ... until all but the last kAhead rows' copies are done
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory"); }
+
+template <typename T, int NV>
+__device__ __forceinline__ void load_param_pairs(const float* p, float other, int t, int tpr, int pieces,
+                                                 uint64_t (&w)[NV][8 / sizeof(T)]) {
+  constexpr int P = 8 / sizeof(T);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+    const bool in = p != nullptr && v < pieces;
+#pragma unroll
+    for (int e = 0; e < P; ++e) w[k][e] = pair(in ? __ldg(p + (v * P + e) * 2) : other, in ? __ldg(p + (v * P + e) * 2 + 1) : other);
+  }
+}
+
+// A place in the ring of rows that a thread walks.
+struct Place {
+  uint32_t at, begin, end, step;
+  __device__ __forceinline__ void forward() {
+    at += step;
+    if (at == end) at = begin;
+  }
+};
+
+template <typename T, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(kRingThreads)
+ln_forward_ring_kernel(const LnForward a, int tpr, long long per_group) {
+  constexpr int P = 8 / sizeof(T);
+  constexpr long long es = sizeof(T);
+  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kRing][NV][threads] pieces
+  __shared__ float2 red_mem[ONE_WARP ? 1 : kRingThreads / 64][2][32];
+  const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
+  const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / (2 * P);
+  const uint32_t piece_step = blockDim.x * 16u, row_bytes = NV * piece_step;
+  const uint32_t mine = smem_u32(ring_mem) + threadIdx.x * 16u;
+  float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
+  int flip = 0;
+  const long long total = a.rows * a.M;
+  const long long first = (static_cast<long long>(blockIdx.x) * groups + group) * per_group;
+  const int count = static_cast<int>(total - first < per_group ? (total > first ? total - first : 0) : per_group);
+  // the row that is copied next: its number in the run, its address, the rows left of its replica
+  int copied = 0;
+  long long c_m = first / a.rows, c_left = a.rows - (first - c_m * a.rows);
+  const char* c_x = static_cast<const char*>(a.X) + (c_m * a.x_ws + (first - c_m * a.rows) * a.x_rs) * es + t * 16;
+  const long long x_step = a.x_rs * es, y_step = a.y_rs * es;
+  Place c_at = {mine, mine, mine + kRing * row_bytes, row_bytes}, x_at = c_at;
+  pdl_wait();
+  auto copy_until = [&](int n) {                                       // rows up to the n-th; past the run nothing
+    for (; copied < n; ++copied) {
+      if (copied < count) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+          if (t + k * tpr < pieces) copy_ahead(c_at.at + k * piece_step, c_x + k * tpr * 16);
+        c_x += x_step;
+        if (--c_left == 0) {
+          c_left = a.rows;
+          ++c_m;
+          c_x = static_cast<const char*>(a.X) + c_m * a.x_ws * es + t * 16;
+        }
+      }
+      copies_commit();
+      c_at.forward();
+    }
+  };
+  copy_until(kAhead);
+  uint64_t w[NV][P], b[NV][P];
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  long long m = first / a.rows, left = 0;                              // these rows' replica; rows left before the next
+  char* y = nullptr;
+  float* mean_out = a.mean ? a.mean + first : nullptr;
+  float* rstd_out = a.rstd ? a.rstd + first : nullptr;
+  for (int i = 0; i < count;) {
+    copy_until(i + kRing);                                             // into the places of the rows before
+    if (left == 0) {
+      const long long r = i == 0 ? first - m * a.rows : 0;
+      if (i > 0) ++m;
+      left = a.rows - r;
+      y = static_cast<char*>(a.Y) + (m * a.y_ws + r * a.y_rs) * es + 16 * t;
+      if (i == 0 || a.p_stride != 0) {
+        load_param_pairs<T, NV>(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
+        load_param_pairs<T, NV>(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, t, tpr, pieces, b);
+      }
+    }
+    const bool two = i + 1 < count && left > 1;                        // rows i and i + 1, of one replica
+    copies_wait();
+    uint64_t x[2][NV][P], sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (q == 0 || two) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (t + k * tpr < pieces) {
+            read_piece<T>(x_at.at + k * piece_step, x[q][k]);
+#pragma unroll
+            for (int e = 0; e < P; ++e) sum[q] = add2(sum[q], x[q][k][e]);
+          }
+        }
+        x_at.forward();
+      }
+    }
+    const float2 s = group_sum2<ONE_WARP>(sum2(sum[0]), sum2(sum[1]), red, flip, group, t, tpr);
+    const float mean[2] = {s.x * inv_d, s.y * inv_d};
+    uint64_t sq[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const uint64_t shift = pair(-mean[q], -mean[q]);
+      if (q == 0 || two) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (t + k * tpr < pieces) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+              x[q][k][e] = add2(x[q][k][e], shift);
+              sq[q] = fma2(x[q][k][e], x[q][k][e], sq[q]);
+            }
+          }
+        }
+      }
+    }
+    const float2 v = group_sum2<ONE_WARP>(sum2(sq[0]), sum2(sq[1]), red, flip, group, t, tpr);
+    const float rstd[2] = {1.0f / sqrtf(fmaf(v.x, inv_d, a.eps)), 1.0f / sqrtf(fmaf(v.y, inv_d, a.eps))};
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (q == 0 || two) {
+        const uint64_t scale = pair(rstd[q], rstd[q]);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (t + k * tpr < pieces) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) x[q][k][e] = fma2(mul2(x[q][k][e], scale), w[k][e], b[k][e]);
+            write_piece<T>(y + k * tpr * 16, x[q][k]);
+          }
+        }
+        y += y_step;
+        if (t == 0) {
+          if (mean_out) mean_out[i + q] = mean[q];
+          if (rstd_out) rstd_out[i + q] = rstd[q];
+        }
+      }
+    }
+    i += two ? 2 : 1;
+    left -= two ? 2 : 1;
+  }
+}
+
+// A CTA has rows_per_cta rows in a run; its groups take them in turn.  Where a segment ends, the groups' sums are
+// added in order through shared memory (`slots` of them at a time) and leave.
+template <typename T, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(kRingThreads, 1)
+ln_backward_ring_kernel(const LnBackward a, int tpr, int slots) {
+  constexpr int P = 8 / sizeof(T);
+  constexpr long long es = sizeof(T);
+  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kBackRing][x, dy][NV][threads] pieces, [slots][2 d] sums
+  __shared__ float2 red_mem[ONE_WARP ? 1 : kRingThreads / 64][2][32];
+  const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
+  const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / (2 * P);
+  const uint32_t piece_step = blockDim.x * 16u, half_bytes = NV * piece_step, row_bytes = 2u * half_bytes;
+  const uint32_t mine = smem_u32(ring_mem) + threadIdx.x * 16u;
+  float* sums = reinterpret_cast<float*>(ring_mem + static_cast<size_t>(kBackRing) * row_bytes);
+  float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
+  int flip = 0;
+  const long long rows = a.samples * a.tokens, total = rows * a.M;     // of a replica, of all
+  const long long first = static_cast<long long>(blockIdx.x) * a.rows_per_cta;
+  const int run = static_cast<int>(total - first < a.rows_per_cta ? total - first : a.rows_per_cta);      // this CTA's rows
+  const int count = run > group ? (run - group + groups - 1) / groups : 0;                                // ... this group's
+  // the row that is copied next: its number in the group's run, its address, the rows of its replica from it on
+  int copied = 0;
+  long long c_m = (first + group) / rows, c_left = rows - (first + group - c_m * rows);
+  const char *c_x, *c_g;
+  auto find = [&]() {
+    const long long r = rows - c_left;
+    c_x = static_cast<const char*>(a.X) + (c_m * a.x_ws + r * a.x_rs) * es + t * 16;
+    c_g = static_cast<const char*>(a.dY) + (c_m * a.dy_ws + r * a.dy_rs) * es + t * 16;
+  };
+  find();
+  const long long x_step = groups * a.x_rs * es, g_step = groups * a.dy_rs * es, o_step = groups * a.dx_rs * es;
+  Place c_at = {mine, mine, mine + kBackRing * row_bytes, row_bytes}, x_at = c_at;
+  pdl_wait();
+  auto copy_row = [&]() {
+    if (copied < count) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * tpr < pieces) {
+          copy_ahead(c_at.at + k * piece_step, c_x + k * tpr * 16);
+          copy_ahead(c_at.at + half_bytes + k * piece_step, c_g + k * tpr * 16);
+        }
+      }
+      ++copied;
+      c_x += x_step;
+      c_g += g_step;
+      c_left -= groups;
+      if (c_left <= 0) {
+        while (c_left <= 0) {
+          c_left += rows;
+          ++c_m;
+        }
+        find();
+      }
+    }
+    copies_commit();
+    c_at.forward();
+  };
+  for (int s = 0; s < kBackRing - 1; ++s) copy_row();
+  const float *mean_in = a.mean + first + group, *rstd_in = a.rstd + first + group;      // of this group's next row
+  float n_mean = 0.f, n_rstd = 0.f;
+  if (count > 0) {
+    n_mean = __ldg(mean_in);
+    n_rstd = __ldg(rstd_in);
+  }
+  uint64_t w[NV][P], dw[NV][P], db[NV][P];
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < P; ++e) dw[k][e] = db[k][e] = pair(0.f, 0.f);
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  long long have = -1;                                                 // the replica whose weight is in w
+  long long seg = first / a.tokens;
+  int next = group, done = 0;                                          // this group's next row in the run, rows done
+  for (int at = 0; at < run; ++seg) {
+    const long long seg_end = (seg + 1) * a.tokens - first;
+    const int stop = seg_end < run ? static_cast<int>(seg_end) : run;
+    const long long sm = seg / a.samples;                              // the segment's replica
+    if (sm != have) {
+      if (have < 0 || a.p_stride != 0)
+        load_param_pairs<T, NV>(a.weight ? a.weight + sm * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
+      have = sm;
+    }
+    char* o = static_cast<char*>(a.dX) + (sm * a.dx_ws + (first + next - sm * rows) * a.dx_rs) * es + 16 * t;
+    for (; next < stop; next += groups, o += o_step) {
+      copy_row();                                                      // into the place of the row before
+      const float mean = n_mean, rstd = n_rstd;
+      mean_in += groups;
+      rstd_in += groups;
+      if (++done < count) {
+        n_mean = __ldg(mean_in);
+        n_rstd = __ldg(rstd_in);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(kBackRing - 1) : "memory");
+      const uint32_t xp = x_at.at, gp = xp + half_bytes;
+      const uint64_t r2 = pair(rstd, rstd), shift = pair(-mean, -mean);
+      uint64_t s1 = pair(0.f, 0.f), s2 = pair(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * tpr < pieces) {
+          uint64_t x[P], g[P];
+          read_piece<T>(xp + k * piece_step, x);
+          read_piece<T>(gp + k * piece_step, g);
+#pragma unroll
+          for (int e = 0; e < P; ++e) {
+            const uint64_t xh = mul2(add2(x[e], shift), r2), y = mul2(g[e], w[k][e]);
+            s1 = add2(s1, y);
+            s2 = fma2(y, xh, s2);
+            dw[k][e] = fma2(g[e], xh, dw[k][e]);
+            db[k][e] = add2(db[k][e], g[e]);
+          }
+        }
+      }
+      if (a.dX != nullptr) {
+        const float2 c = group_sum2<ONE_WARP>(sum2(s1), sum2(s2), red, flip, group, t, tpr);
+        const float c1 = c.x * inv_d, c2 = c.y * inv_d;
+        const uint64_t nc1 = pair(-c1, -c1), nc2 = pair(-c2, -c2);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          if (t + k * tpr < pieces) {
+            uint64_t x[P], g[P];
+            read_piece<T>(xp + k * piece_step, x);
+            read_piece<T>(gp + k * piece_step, g);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+              const uint64_t xh = mul2(add2(x[e], shift), r2);
+              x[e] = mul2(r2, fma2(xh, nc2, fma2(g[e], w[k][e], nc1)));
+            }
+            write_piece<T>(o + k * tpr * 16, x);
+          }
+        }
+      }
+      x_at.forward();
+    }
+    if (a.part != nullptr) {
+      float* out_w = a.part + part_slot(a.Gw != nullptr, blockIdx.x, seg, a.tokens, a.rows_per_cta) * 2 * a.d;
+      float* out_b = out_w + a.d;
+      if (a.Gw != nullptr && first + at == seg * a.tokens && first + stop == (seg + 1) * a.tokens) {
+        const long long g = sm * a.g_ws + (seg - sm * a.samples) * a.g_rs;
+        out_w = a.Gw + g;
+        out_b = a.Gb + g;
+      }
+      for (int base = 1; base < groups; base += slots) {               // groups base .. base + slots - 1 hand theirs to group 0
+        if (group >= base && group < base + slots) {
+          float2* p = reinterpret_cast<float2*>(sums + static_cast<size_t>(group - base) * 2 * a.d);
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            const int v = t + k * tpr;
+            if (v < pieces) {
+#pragma unroll
+              for (int e = 0; e < P; ++e) {
+                p[v * P + e] = unpair(dw[k][e]);
+                p[a.d / 2 + v * P + e] = unpair(db[k][e]);
+              }
+            }
+          }
+        }
+        __syncthreads();
+        if (group == 0) {
+          const int n = groups - base < slots ? groups - base : slots;
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            const int v = t + k * tpr;
+            if (v < pieces) {
+              for (int g = 0; g < n; ++g) {
+                const float2* p = reinterpret_cast<const float2*>(sums + static_cast<size_t>(g) * 2 * a.d);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                  const float2 fw = p[v * P + e], fb = p[a.d / 2 + v * P + e];
+                  dw[k][e] = add2(dw[k][e], pair(fw.x, fw.y));
+                  db[k][e] = add2(db[k][e], pair(fb.x, fb.y));
+                }
+              }
+            }
+          }
+        }
+        __syncthreads();
+      }
+      if (group == 0) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int v = t + k * tpr;
+          if (v < pieces) {
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+              const float2 fw = unpair(dw[k][e]), fb = unpair(db[k][e]);
+              const int j = (v * P + e) * 2;
+              out_w[j] = fw.x;
+              out_w[j + 1] = fw.y;
+              out_b[j] = fb.x;
+              out_b[j + 1] = fb.y;
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < P; ++e) dw[k][e] = db[k][e] = pair(0.f, 0.f);
+    }
+    at = stop;
+  }
+}
+
 struct DeviceGuardLn {
   int prev = -1;
   bool ok = true;
@@ -610,28 +1011,30 @@ unsigned row_grid(const abs_ctx* ctx, long long rows) {
 }
 
 
-// How a row of d elements is laid out over threads, or tpr = 0 where it does not fit: V elements a piece (16 bytes,
-// or what d and the alignment allow), the fewest threads (a divisor of the CTA's) that hold it in at most 4
-// pieces of 16 bytes (backward of bf16, where each element has two running sums, 3) or 16 elements each.
+// How a row of d elements is laid out over threads, or tpr = 0 where it does not fit: the fewest threads (a divisor of
+// the CTA's) that hold it in at most NV pieces each.  Pieces are of 16 bytes (NV up to 4, fp32, or 3, bf16: 16 or 24
+// elements, each with a weight and a bias or two running sums), or, where the alignment does not allow them, of one
+// element or two bf16 (one variant each, 16 elements a thread).
 struct RowPlan {
+  bool wide;
   int V, NV, tpr;
 };
-RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits, int most16) {
+RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits) {
   const int es = dtype == ABS_F32 ? 4 : 2;
-  RowPlan p = {1, 0, 0};
+  RowPlan p = {false, 1, 0, 0};
   align_bits |= static_cast<unsigned long long>(d) * es;
-  if ((align_bits & 15u) == 0) p.V = 16 / es;
+  p.wide = (align_bits & 15u) == 0;
+  if (p.wide) p.V = 16 / es;
   else if (es == 2 && (align_bits & 3u) == 0) p.V = 2;
   const long long pieces = d / p.V;
-  const int most = p.V * es == 16 ? most16 : 16 / p.V;
+  const int most = p.wide ? (es == 4 ? 4 : 3) : 16 / p.V;
   const int tprs[6] = {32, 64, 96, 128, 192, 384};
   for (int k = 0; k < 6; ++k)
     if (pieces <= static_cast<long long>(tprs[k]) * most) {
       p.tpr = tprs[k];
-      p.NV = static_cast<int>((pieces + p.tpr - 1) / p.tpr);
+      p.NV = p.wide ? static_cast<int>((pieces + p.tpr - 1) / p.tpr) : most;
       break;
     }
-  if (p.V * es != 16 && p.NV > 0) p.NV = most;                     // one variant of the narrow pieces
   return p;
 }
 
@@ -639,60 +1042,80 @@ template <typename T, int V, int NV>
 cudaError_t run_forward(abs_ctx* ctx, const LnForward& a, int tpr, cudaStream_t st) {
   const int groups = kFastThreads / tpr;
   const long long total = a.rows * a.M;
-  const long long most = static_cast<long long>(ctx->sm_count) * 2 * groups;       // two CTAs per SM
+  const long long most = static_cast<long long>(ctx->sm_count) * groups;
   const long long per = (total + most - 1) / most;
   const long long used = (total + per - 1) / per;
   const unsigned grid = static_cast<unsigned>((used + groups - 1) / groups);
-  if (tpr == 32) return launch_dependent(ln_forward_kernel<T, V, NV, true>, dim3(grid), dim3(kFastThreads), 0, st, a, tpr, per);
-  return launch_dependent(ln_forward_kernel<T, V, NV, false>, dim3(grid), dim3(kFastThreads), 0, st, a, tpr, per);
+  auto kern = tpr == 32 ? ln_forward_kernel<T, V, NV, true> : ln_forward_kernel<T, V, NV, false>;
+  return launch_dependent(kern, dim3(grid), dim3(kFastThreads), 0, st, a, tpr, per);
+}
+template <typename T, int NV>
+cudaError_t run_forward_ring(abs_ctx* ctx, const LnForward& a, int tpr, cudaStream_t st) {
+  const long long total = a.rows * a.M;
+  const int groups = kRingThreads / tpr;
+  const size_t smem = static_cast<size_t>(kRing) * NV * kRingThreads * 16;
+  const long long most = static_cast<long long>(ctx->sm_count) * groups;
+  long long per = (total + most - 1) / most;
+  if (per > (1ll << 30)) per = 1ll << 30;                              // a group counts its rows in 32 bits
+  const long long used = (total + per - 1) / per;
+  const unsigned grid = static_cast<unsigned>((used + groups - 1) / groups);
+  auto kern = tpr == 32 ? ln_forward_ring_kernel<T, NV, true> : ln_forward_ring_kernel<T, NV, false>;
+  const cudaError_t e = ensure_dynamic_smem(ctx, kern, smem);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kern, dim3(grid), dim3(kRingThreads), smem, st, a, tpr, per);
 }
 cudaError_t dispatch_forward(abs_ctx* ctx, const LnForward& a, abs_dtype dtype, const RowPlan& p, cudaStream_t st) {
-  if (dtype == ABS_F32) {
-    if (p.V == 1) return run_forward<float, 1, 16>(ctx, a, p.tpr, st);
-    switch (p.NV) {
-      case 1: return run_forward<float, 4, 1>(ctx, a, p.tpr, st);
-      case 2: return run_forward<float, 4, 2>(ctx, a, p.tpr, st);
-      case 3: return run_forward<float, 4, 3>(ctx, a, p.tpr, st);
-      default: return run_forward<float, 4, 4>(ctx, a, p.tpr, st);
-    }
+  const bool f = dtype == ABS_F32;
+  if (!p.wide) {
+    if (f) return run_forward<float, 1, 16>(ctx, a, p.tpr, st);
+    return p.V == 2 ? run_forward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, st) : run_forward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, st);
   }
-  if (p.V == 1) return run_forward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, st);
-  if (p.V == 2) return run_forward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, st);
   switch (p.NV) {
-    case 1: return run_forward<__nv_bfloat16, 8, 1>(ctx, a, p.tpr, st);
-    case 2: return run_forward<__nv_bfloat16, 8, 2>(ctx, a, p.tpr, st);
-    case 3: return run_forward<__nv_bfloat16, 8, 3>(ctx, a, p.tpr, st);
-    default: return run_forward<__nv_bfloat16, 8, 4>(ctx, a, p.tpr, st);
+    case 1: return f ? run_forward_ring<float, 1>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 1>(ctx, a, p.tpr, st);
+    case 2: return f ? run_forward_ring<float, 2>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 2>(ctx, a, p.tpr, st);
+    case 3: return f ? run_forward_ring<float, 3>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 3>(ctx, a, p.tpr, st);
+    default: return run_forward_ring<float, 4>(ctx, a, p.tpr, st);
   }
 }
 
 template <typename T, int V, int NV>
 cudaError_t run_backward(abs_ctx* ctx, const LnBackward& a, int tpr, int groups, unsigned grid, cudaStream_t st) {
   const size_t smem = a.part != nullptr ? static_cast<size_t>(groups - 1) * 2 * a.d * sizeof(float) : 0;
-  auto one = ln_backward_kernel<T, V, NV, true>;
-  auto many = ln_backward_kernel<T, V, NV, false>;
-  cudaError_t e = cudaSuccess;
-  if (smem > 40 * 1024) e = tpr == 32 ? ensure_dynamic_smem(ctx, one, smem) : ensure_dynamic_smem(ctx, many, smem);
+  auto kern = tpr == 32 ? ln_backward_kernel<T, V, NV, true> : ln_backward_kernel<T, V, NV, false>;
+  if (smem > 40 * 1024) {
+    const cudaError_t e = ensure_dynamic_smem(ctx, kern, smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_dependent(kern, dim3(grid), dim3(tpr * groups), smem, st, a, tpr);
+}
+template <typename T, int NV>
+cudaError_t run_backward_ring(abs_ctx* ctx, const LnBackward& a, int tpr, int groups, unsigned grid, cudaStream_t st) {
+  const size_t sum = 2 * static_cast<size_t>(a.d) * sizeof(float);
+  int slots = 0;
+  if (a.part != nullptr && groups > 1) {             // sums of as many groups at a time as fit in 24 KB
+    slots = static_cast<int>(24 * 1024 / sum);
+    if (slots > groups - 1) slots = groups - 1;
+    if (slots < 1) slots = 1;
+  }
+  const size_t smem = static_cast<size_t>(kBackRing) * 2 * NV * (tpr * groups) * 16 + slots * sum;
+  auto kern = tpr == 32 ? ln_backward_ring_kernel<T, NV, true> : ln_backward_ring_kernel<T, NV, false>;
+  const cudaError_t e = ensure_dynamic_smem(ctx, kern, smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(tpr == 32 ? one : many, dim3(grid), dim3(tpr * groups), smem, st, a, tpr);
+  return launch_dependent(kern, dim3(grid), dim3(tpr * groups), smem, st, a, tpr, slots);
 }
 cudaError_t dispatch_backward(abs_ctx* ctx, const LnBackward& a, abs_dtype dtype, const RowPlan& p, int groups, unsigned grid,
                               cudaStream_t st) {
-  if (dtype == ABS_F32) {
-    if (p.V == 1) return run_backward<float, 1, 16>(ctx, a, p.tpr, groups, grid, st);
-    switch (p.NV) {
-      case 1: return run_backward<float, 4, 1>(ctx, a, p.tpr, groups, grid, st);
-      case 2: return run_backward<float, 4, 2>(ctx, a, p.tpr, groups, grid, st);
-      case 3: return run_backward<float, 4, 3>(ctx, a, p.tpr, groups, grid, st);
-      default: return run_backward<float, 4, 4>(ctx, a, p.tpr, groups, grid, st);
-    }
+  const bool f = dtype == ABS_F32;
+  if (!p.wide) {
+    if (f) return run_backward<float, 1, 16>(ctx, a, p.tpr, groups, grid, st);
+    return p.V == 2 ? run_backward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, groups, grid, st)
+                    : run_backward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, groups, grid, st);
   }
-  if (p.V == 1) return run_backward<__nv_bfloat16, 1, 16>(ctx, a, p.tpr, groups, grid, st);
-  if (p.V == 2) return run_backward<__nv_bfloat16, 2, 8>(ctx, a, p.tpr, groups, grid, st);
   switch (p.NV) {
-    case 1: return run_backward<__nv_bfloat16, 8, 1>(ctx, a, p.tpr, groups, grid, st);
-    case 2: return run_backward<__nv_bfloat16, 8, 2>(ctx, a, p.tpr, groups, grid, st);
-    default: return run_backward<__nv_bfloat16, 8, 3>(ctx, a, p.tpr, groups, grid, st);
+    case 1: return f ? run_backward_ring<float, 1>(ctx, a, p.tpr, groups, grid, st) : run_backward_ring<__nv_bfloat16, 1>(ctx, a, p.tpr, groups, grid, st);
+    case 2: return f ? run_backward_ring<float, 2>(ctx, a, p.tpr, groups, grid, st) : run_backward_ring<__nv_bfloat16, 2>(ctx, a, p.tpr, groups, grid, st);
+    case 3: return f ? run_backward_ring<float, 3>(ctx, a, p.tpr, groups, grid, st) : run_backward_ring<__nv_bfloat16, 3>(ctx, a, p.tpr, groups, grid, st);
+    default: return run_backward_ring<float, 4>(ctx, a, p.tpr, groups, grid, st);
   }
 }
 
@@ -726,7 +1149,7 @@ extern "C" int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int 
               mean, rstd, M, rows, static_cast<int>(d)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const RowPlan plan = plan_row(dtype, d, row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
-                                              row_bits(Y, dtype, M, y_row_stride, y_worker_stride), 4);
+                                              row_bits(Y, dtype, M, y_row_stride, y_worker_stride));
   if (plan.tpr > 0) {
     ABS_CUDA_TRY(ctx, dispatch_forward(ctx, a, dtype, plan, st));
     return ABS_OK;
@@ -774,8 +1197,7 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
                dX, dx_row_stride, dx_worker_stride, M, samples, tokens, static_cast<int>(d), nullptr, 1, nullptr, nullptr, 0, 0};
   const RowPlan plan = plan_row(dtype, d, row_bits(dY, dtype, M, dy_row_stride, dy_worker_stride) |
                                               row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
-                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0),
-                                dtype == ABS_F32 ? 4 : 3);
+                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0));
   const bool sums = per_sample || totals;
   LnReduce red{static_cast<const float*>(ctx->workspace), M, samples, tokens, 1, static_cast<int>(d), 0, Gw, Gb, g_row_stride,
                g_worker_stride, dW, dB, grad_stride};
@@ -786,11 +1208,9 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
     int groups = 1;
     long long ctas;
     if (fast) {
-      groups = kFastThreads / plan.tpr;
-      if (tokens < 2 * groups && sums) groups = 1;
-      const int per_sm = groups > 1 || plan.tpr == kFastThreads ? (plan.V * plan.NV <= 8 ? 2 : 1)
-                                                                : (plan.V * plan.NV <= 8 ? 2 : 1) * kFastThreads / plan.tpr;
-      ctas = static_cast<long long>(ctx->sm_count) * per_sm;
+      const int full = kRingThreads / plan.tpr;
+      if (tokens >= 2 * full || !sums) groups = full;
+      ctas = static_cast<long long>(ctx->sm_count) * (full / groups);
     } else {
       ctas = static_cast<long long>(ctx->sm_count) * 8 * kLnThreads / (d < kLnThreads ? kLnThreads : d);
       if (ctas < ctx->sm_count) ctas = ctx->sm_count;
@@ -810,7 +1230,7 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
         red.direct = 1;
       }
     }
-    if (ctas < 1) ctas = 1;
+    if (ctas < (total >> 30) + 1) ctas = (total >> 30) + 1;                  // a CTA counts its rows in 32 bits
     a.rows_per_cta = (total + ctas - 1) / ctas;
     if (groups == 1 && sums && a.rows_per_cta > tokens) a.rows_per_cta = a.rows_per_cta / tokens * tokens;      // whole segments
     ctas = (total + a.rows_per_cta - 1) / a.rows_per_cta;
