@@ -59,6 +59,9 @@ struct LnReduce {
   int M;
   long long samples, tokens, rows_per_cta;
   int d, direct;               // direct: segments within one CTA are in G already
+  int whole;                   // ... and all of them lie within one
+  long long per_cta;           // samples of a CTA (blockIdx.z)
+  float* totals;               // [M][gridDim.z][2 d] where there are several, else NULL
   float* Gw;
   float* Gb;
   long long g_rs, g_ws;
@@ -205,7 +208,14 @@ ln_reduce_kernel(const LnReduce a) {
   float* G = is_b ? a.Gb : a.Gw;
   float total = 0.f;
   const bool by_sample = a.samples >= 8 || a.tokens == 0;
-  for (long long i = by_sample ? row : 0; i < a.samples; i += by_sample ? 8 : 1) {
+  const long long i0 = blockIdx.z * a.per_cta, i1 = i0 + a.per_cta < a.samples ? i0 + a.per_cta : a.samples;
+  if (a.whole) {
+    if (live) {
+      const float* p = G + m * a.g_ws + j;
+#pragma unroll 8
+      for (long long i = i0 + row; i < i1; i += 8) total += p[i * a.g_rs];
+    }
+  } else for (long long i = i0 + (by_sample ? row : 0); i < i1; i += by_sample ? 8 : 1) {
     const long long seg = m * a.samples + i;
     float s = 0.f;
     if (a.tokens > 0) {
@@ -239,12 +249,28 @@ ln_reduce_kernel(const LnReduce a) {
   red[row][lane] = total;
   __syncthreads();
   float* out = is_b ? a.dB : a.dW;
-  if (row == 0 && live && out) {
+  if (row == 0 && live && (out || a.totals)) {
     float s = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += red[k][lane];
-    out[m * a.grad_stride + j] = s;
+    if (a.totals) a.totals[(m * gridDim.z + blockIdx.z) * 2 * a.d + col] = s;
+    else out[m * a.grad_stride + j] = s;
   }
+}
+
+__global__ void __launch_bounds__(kLnThreads)
+ln_total_kernel(const LnReduce a, int n) {
+  const int col = blockIdx.x * kLnThreads + threadIdx.x;
+  const long long m = blockIdx.y;
+  pdl_wait();
+  if (col >= 2 * a.d) return;
+  const bool is_b = col >= a.d;
+  float* out = is_b ? a.dB : a.dW;
+  if (out == nullptr) return;
+  float s = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < n; ++k) s += a.totals[(m * n + k) * 2 * a.d + col];
+  out[m * a.grad_stride + (is_b ? col - a.d : col)] = s;
 }
 
 // ---- rows held in registers -----------------------------------------------------------------------------
@@ -305,6 +331,28 @@ __device__ __forceinline__ float2 group_sum2(float a, float b, float2* red, int&
   for (int w = 0; w < tpr / 32; ++w) {
     s.x += r[w].x;
     s.y += r[w].y;
+  }
+  return s;
+}
+
+template <bool ONE_WARP>
+__device__ __forceinline__ float4 group_sum4(float4 v, float4* red, int& flip, int group, int t, int tpr) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, off);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, off);
+    v.z += __shfl_xor_sync(0xffffffffu, v.z, off);
+    v.w += __shfl_xor_sync(0xffffffffu, v.w, off);
+  }
+  if constexpr (ONE_WARP) return v;
+  float4* r = red + 32 * flip;
+  flip ^= 1;
+  if ((t & 31) == 0) r[t >> 5] = v;
+  named_bar_sync(1 + group, tpr);
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = 0; w < tpr / 32; ++w) {
+    const float4 q = r[w];
+    s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
   }
   return s;
 }
@@ -566,9 +614,8 @@ ln_backward_kernel(const LnBackward a, int tpr) {
 // go through the same shuffles and barriers.  Arithmetic on pairs of elements (fma.rn.f32x2): at 2 bytes an element the
 // issue slots are the other limit.
 constexpr int kRingThreads = 384;
-constexpr int kAhead = 4;                          // rows under way besides the two that are worked on
+constexpr int kAhead = 2;                          // rows under way besides the two that are worked on
 constexpr int kRing = kAhead + 2;
-constexpr int kBackRing = 4;                       // backward, with two tensors: one row at a time, three under way
 
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t r;
@@ -634,16 +681,33 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 // ... until all but the last kAhead rows' copies are done
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory"); }
 
-template <typename T, int NV>
-__device__ __forceinline__ void load_param_pairs(const float* p, float other, int t, int tpr, int pieces,
-                                                 uint64_t (&w)[NV][8 / sizeof(T)]) {
-  constexpr int P = 8 / sizeof(T);
+// A replica's weight (or bias) into shared memory: element j of piece v = j / 2P lies in the piece's quarter q, [Q][pieces]
+// of 16 bytes, so that a warp's reads of one quarter are contiguous.
+template <typename T>
+__device__ __forceinline__ void stage_params(float* to, const float* from, float other, int d) {
+  constexpr int E = 16 / sizeof(T);
+  const int pieces = d / E;
+  for (int j = threadIdx.x; j < d; j += blockDim.x) {
+    const int v = j / E, q = (j - v * E) / 4;
+    to[(q * pieces + v) * 4 + (j & 3)] = from ? __ldg(from + j) : other;
+  }
+}
+__device__ __forceinline__ void read_params(uint32_t addr, uint64_t& a, uint64_t& b) {
+  const uint4 v = lds128(addr);
+  a = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+  b = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+}
+// Pairs of sums to consecutive floats; `wide`: p is 16-byte aligned.
+template <int P>
+__device__ __forceinline__ void store_sums(float* p, const uint64_t (&x)[P], bool wide) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = t + k * tpr;
-    const bool in = p != nullptr && v < pieces;
-#pragma unroll
-    for (int e = 0; e < P; ++e) w[k][e] = pair(in ? __ldg(p + (v * P + e) * 2) : other, in ? __ldg(p + (v * P + e) * 2 + 1) : other);
+  for (int e = 0; e < P; e += 2) {
+    const float2 a = unpair(x[e]), b = unpair(x[e + 1]);
+    if (wide) {
+      *reinterpret_cast<float4*>(p + 2 * e) = make_float4(a.x, a.y, b.x, b.y);
+    } else {
+      p[2 * e] = a.x; p[2 * e + 1] = a.y; p[2 * e + 2] = b.x; p[2 * e + 3] = b.y;
+    }
   }
 }
 
@@ -656,27 +720,32 @@ struct Place {
   }
 };
 
+// A CTA has rows_per_cta rows in a run, its groups take them in turn; weight and bias of the replica lie in shared
+// memory.
 template <typename T, int NV, bool ONE_WARP>
-__global__ void __launch_bounds__(kRingThreads)
-ln_forward_ring_kernel(const LnForward a, int tpr, long long per_group) {
-  constexpr int P = 8 / sizeof(T);
+__global__ void __launch_bounds__(kRingThreads, 1)
+ln_forward_ring_kernel(const LnForward a, int tpr, long long rows_per_cta) {
+  constexpr int P = 8 / sizeof(T), Q = P / 2;                          // a piece's weights are Q times 16 bytes
   constexpr long long es = sizeof(T);
-  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kRing][NV][threads] pieces
+  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kRing][NV][threads] pieces, weight, bias [Q][pieces]
   __shared__ float2 red_mem[ONE_WARP ? 1 : kRingThreads / 64][2][32];
   const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
   const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / (2 * P);
   const uint32_t piece_step = blockDim.x * 16u, row_bytes = NV * piece_step;
   const uint32_t mine = smem_u32(ring_mem) + threadIdx.x * 16u;
+  float* params = reinterpret_cast<float*>(ring_mem + static_cast<size_t>(kRing) * row_bytes);
+  const uint32_t w_at = smem_u32(params) + 16u * t, b_at = w_at + Q * pieces * 16u;
   float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
   int flip = 0;
   const long long total = a.rows * a.M;
-  const long long first = (static_cast<long long>(blockIdx.x) * groups + group) * per_group;
-  const int count = static_cast<int>(total - first < per_group ? (total > first ? total - first : 0) : per_group);
-  // the row that is copied next: its number in the run, its address, the rows left of its replica
+  const long long first = static_cast<long long>(blockIdx.x) * rows_per_cta;
+  const int run = static_cast<int>(total - first < rows_per_cta ? total - first : rows_per_cta);      // this CTA's rows
+  const int count = run > group ? (run - group + groups - 1) / groups : 0;                            // ... this group's
+  // the row that is copied next: its number in the group's run, its address, the rows of its replica from it on
   int copied = 0;
-  long long c_m = first / a.rows, c_left = a.rows - (first - c_m * a.rows);
-  const char* c_x = static_cast<const char*>(a.X) + (c_m * a.x_ws + (first - c_m * a.rows) * a.x_rs) * es + t * 16;
-  const long long x_step = a.x_rs * es, y_step = a.y_rs * es;
+  long long c_m = (first + group) / a.rows, c_left = a.rows - (first + group - c_m * a.rows);
+  const char* c_x = static_cast<const char*>(a.X) + (c_m * a.x_ws + (a.rows - c_left) * a.x_rs) * es + t * 16;
+  const long long x_step = groups * a.x_rs * es, y_step = groups * a.y_rs * es;
   Place c_at = {mine, mine, mine + kRing * row_bytes, row_bytes}, x_at = c_at;
   pdl_wait();
   auto copy_until = [&](int n) {                                       // rows up to the n-th; past the run nothing
@@ -686,10 +755,13 @@ ln_forward_ring_kernel(const LnForward a, int tpr, long long per_group) {
         for (int k = 0; k < NV; ++k)
           if (t + k * tpr < pieces) copy_ahead(c_at.at + k * piece_step, c_x + k * tpr * 16);
         c_x += x_step;
-        if (--c_left == 0) {
-          c_left = a.rows;
-          ++c_m;
-          c_x = static_cast<const char*>(a.X) + c_m * a.x_ws * es + t * 16;
+        c_left -= groups;
+        if (c_left <= 0) {
+          while (c_left <= 0) {
+            c_left += a.rows;
+            ++c_m;
+          }
+          c_x = static_cast<const char*>(a.X) + (c_m * a.x_ws + (a.rows - c_left) * a.x_rs) * es + t * 16;
         }
       }
       copies_commit();
@@ -697,83 +769,99 @@ ln_forward_ring_kernel(const LnForward a, int tpr, long long per_group) {
     }
   };
   copy_until(kAhead);
-  uint64_t w[NV][P], b[NV][P];
   const float inv_d = 1.0f / static_cast<float>(a.d);
-  long long m = first / a.rows, left = 0;                              // these rows' replica; rows left before the next
-  char* y = nullptr;
-  float* mean_out = a.mean ? a.mean + first : nullptr;
-  float* rstd_out = a.rstd ? a.rstd + first : nullptr;
-  for (int i = 0; i < count;) {
-    copy_until(i + kRing);                                             // into the places of the rows before
-    if (left == 0) {
-      const long long r = i == 0 ? first - m * a.rows : 0;
-      if (i > 0) ++m;
-      left = a.rows - r;
-      y = static_cast<char*>(a.Y) + (m * a.y_ws + r * a.y_rs) * es + 16 * t;
-      if (i == 0 || a.p_stride != 0) {
-        load_param_pairs<T, NV>(a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
-        load_param_pairs<T, NV>(a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, t, tpr, pieces, b);
-      }
+  long long m = first / a.rows;
+  int next = group, done = 0;                                          // this group's next row in the run, rows done
+  for (int at = 0; at < run; ++m) {                                    // the run's rows of replica m
+    const long long m_end = (m + 1) * a.rows - first;
+    const int stop = m_end < run ? static_cast<int>(m_end) : run;
+    if (at == 0 || a.p_stride != 0) {
+      if (at > 0) __syncthreads();
+      stage_params<T>(params, a.weight ? a.weight + m * a.p_stride : nullptr, 1.f, a.d);
+      stage_params<T>(params + a.d, a.bias ? a.bias + m * a.p_stride : nullptr, 0.f, a.d);
+      __syncthreads();
     }
-    const bool two = i + 1 < count && left > 1;                        // rows i and i + 1, of one replica
-    copies_wait();
-    uint64_t x[2][NV][P], sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+    const long long row = first + next;                                // of all
+    char* y = static_cast<char*>(a.Y) + (m * a.y_ws + (row - m * a.rows) * a.y_rs) * es + 16 * t;
+    float* mean_out = a.mean ? a.mean + row : nullptr;
+    float* rstd_out = a.rstd ? a.rstd + row : nullptr;
+    while (next < stop) {
+      copy_until(done + kRing);                                        // into the places of the rows before
+      const bool two = next + groups < stop;                           // this group's next two rows
+      copies_wait();
+      uint64_t x[2][NV][P], sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      if (q == 0 || two) {
+      for (int q = 0; q < 2; ++q) {
+        if (q == 0 || two) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          if (t + k * tpr < pieces) {
-            read_piece<T>(x_at.at + k * piece_step, x[q][k]);
+          for (int k = 0; k < NV; ++k) {
+            if (t + k * tpr < pieces) {
+              read_piece<T>(x_at.at + k * piece_step, x[q][k]);
 #pragma unroll
-            for (int e = 0; e < P; ++e) sum[q] = add2(sum[q], x[q][k][e]);
+              for (int e = 0; e < P; ++e) sum[q] = add2(sum[q], x[q][k][e]);
+            }
           }
+          x_at.forward();
         }
-        x_at.forward();
       }
-    }
-    const float2 s = group_sum2<ONE_WARP>(sum2(sum[0]), sum2(sum[1]), red, flip, group, t, tpr);
-    const float mean[2] = {s.x * inv_d, s.y * inv_d};
-    uint64_t sq[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+      const float2 s = group_sum2<ONE_WARP>(sum2(sum[0]), sum2(sum[1]), red, flip, group, t, tpr);
+      const float mean[2] = {s.x * inv_d, s.y * inv_d};
+      uint64_t sq[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const uint64_t shift = pair(-mean[q], -mean[q]);
-      if (q == 0 || two) {
+      for (int q = 0; q < 2; ++q) {
+        const uint64_t shift = pair(-mean[q], -mean[q]);
+        if (q == 0 || two) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          if (t + k * tpr < pieces) {
+          for (int k = 0; k < NV; ++k) {
+            if (t + k * tpr < pieces) {
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-              x[q][k][e] = add2(x[q][k][e], shift);
-              sq[q] = fma2(x[q][k][e], x[q][k][e], sq[q]);
+              for (int e = 0; e < P; ++e) {
+                x[q][k][e] = add2(x[q][k][e], shift);
+                sq[q] = fma2(x[q][k][e], x[q][k][e], sq[q]);
+              }
             }
           }
         }
       }
-    }
-    const float2 v = group_sum2<ONE_WARP>(sum2(sq[0]), sum2(sq[1]), red, flip, group, t, tpr);
-    const float rstd[2] = {1.0f / sqrtf(fmaf(v.x, inv_d, a.eps)), 1.0f / sqrtf(fmaf(v.y, inv_d, a.eps))};
+      const float2 v = group_sum2<ONE_WARP>(sum2(sq[0]), sum2(sq[1]), red, flip, group, t, tpr);
+      const float rstd[2] = {rsqrtf(fmaf(v.x, inv_d, a.eps)), rsqrtf(fmaf(v.y, inv_d, a.eps))};      // (within 2 ulp)
+      const uint64_t scale[2] = {pair(rstd[0], rstd[0]), pair(rstd[1], rstd[1])};
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      if (q == 0 || two) {
-        const uint64_t scale = pair(rstd[q], rstd[q]);
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * tpr < pieces) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          if (t + k * tpr < pieces) {
+          for (int q = 0; q < Q; ++q) {
+            uint64_t w0, w1, b0, b1;
+            read_params(w_at + (q * pieces + k * tpr) * 16u, w0, w1);
+            read_params(b_at + (q * pieces + k * tpr) * 16u, b0, b1);
 #pragma unroll
-            for (int e = 0; e < P; ++e) x[q][k][e] = fma2(mul2(x[q][k][e], scale), w[k][e], b[k][e]);
-            write_piece<T>(y + k * tpr * 16, x[q][k]);
+            for (int r = 0; r < 2; ++r) {
+              x[r][k][2 * q] = fma2(mul2(x[r][k][2 * q], scale[r]), w0, b0);
+              x[r][k][2 * q + 1] = fma2(mul2(x[r][k][2 * q + 1], scale[r]), w1, b1);
+            }
           }
-        }
-        y += y_step;
-        if (t == 0) {
-          if (mean_out) mean_out[i + q] = mean[q];
-          if (rstd_out) rstd_out[i + q] = rstd[q];
+          write_piece<T>(y + k * tpr * 16, x[0][k]);
+          if (two) write_piece<T>(y + y_step + k * tpr * 16, x[1][k]);
         }
       }
+      if (t == 0) {
+        if (mean_out) {
+          mean_out[0] = mean[0];
+          if (two) mean_out[groups] = mean[1];
+        }
+        if (rstd_out) {
+          rstd_out[0] = rstd[0];
+          if (two) rstd_out[groups] = rstd[1];
+        }
+      }
+      const int n = two ? 2 : 1;
+      done += n;
+      next += n * groups;
+      y += n * y_step;
+      if (mean_out) mean_out += n * groups;
+      if (rstd_out) rstd_out += n * groups;
     }
-    i += two ? 2 : 1;
-    left -= two ? 2 : 1;
+    at = stop;
   }
 }
 
@@ -782,16 +870,18 @@ ln_forward_ring_kernel(const LnForward a, int tpr, long long per_group) {
 template <typename T, int NV, bool ONE_WARP>
 __global__ void __launch_bounds__(kRingThreads, 1)
 ln_backward_ring_kernel(const LnBackward a, int tpr, int slots) {
-  constexpr int P = 8 / sizeof(T);
+  constexpr int P = 8 / sizeof(T), Q = P / 2;                          // a piece's weights are Q times 16 bytes
   constexpr long long es = sizeof(T);
-  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kBackRing][x, dy][NV][threads] pieces, [slots][2 d] sums
-  __shared__ float2 red_mem[ONE_WARP ? 1 : kRingThreads / 64][2][32];
+  extern __shared__ __align__(128) unsigned char ring_mem[];           // [kRing][x, dy][NV][threads] pieces, weight, [slots][2 d] sums
+  __shared__ float4 red_mem[ONE_WARP ? 1 : kRingThreads / 64][2][32];
   const int group = static_cast<int>(threadIdx.x) / tpr, t = static_cast<int>(threadIdx.x) - group * tpr;
   const int groups = static_cast<int>(blockDim.x) / tpr, pieces = a.d / (2 * P);
   const uint32_t piece_step = blockDim.x * 16u, half_bytes = NV * piece_step, row_bytes = 2u * half_bytes;
   const uint32_t mine = smem_u32(ring_mem) + threadIdx.x * 16u;
-  float* sums = reinterpret_cast<float*>(ring_mem + static_cast<size_t>(kBackRing) * row_bytes);
-  float2* red = &red_mem[ONE_WARP ? 0 : group][0][0];
+  float* params = reinterpret_cast<float*>(ring_mem + static_cast<size_t>(kRing) * row_bytes);
+  float* sums = params + a.d;
+  const uint32_t w_at = smem_u32(params) + 16u * t;
+  float4* red = &red_mem[ONE_WARP ? 0 : group][0][0];
   int flip = 0;
   const long long rows = a.samples * a.tokens, total = rows * a.M;     // of a replica, of all
   const long long first = static_cast<long long>(blockIdx.x) * a.rows_per_cta;
@@ -808,7 +898,7 @@ ln_backward_ring_kernel(const LnBackward a, int tpr, int slots) {
   };
   find();
   const long long x_step = groups * a.x_rs * es, g_step = groups * a.dy_rs * es, o_step = groups * a.dx_rs * es;
-  Place c_at = {mine, mine, mine + kBackRing * row_bytes, row_bytes}, x_at = c_at;
+  Place c_at = {mine, mine, mine + kRing * row_bytes, row_bytes}, x_at = c_at;
   pdl_wait();
   auto copy_row = [&]() {
     if (copied < count) {
@@ -834,81 +924,117 @@ ln_backward_ring_kernel(const LnBackward a, int tpr, int slots) {
     copies_commit();
     c_at.forward();
   };
-  for (int s = 0; s < kBackRing - 1; ++s) copy_row();
+  for (int s = 0; s < kAhead; ++s) copy_row();
   const float *mean_in = a.mean + first + group, *rstd_in = a.rstd + first + group;      // of this group's next row
-  float n_mean = 0.f, n_rstd = 0.f;
-  if (count > 0) {
-    n_mean = __ldg(mean_in);
-    n_rstd = __ldg(rstd_in);
-  }
-  uint64_t w[NV][P], dw[NV][P], db[NV][P];
+  // of its next two rows, asked for an iteration early
+  float n_mean[2] = {0.f, 0.f}, n_rstd[2] = {0.f, 0.f};
+  int done = 0;                                                        // rows of this group that are done
+  auto next_statistics = [&]() {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (done + q < count) {
+        n_mean[q] = __ldg(mean_in + q * groups);
+        n_rstd[q] = __ldg(rstd_in + q * groups);
+      }
+    }
+  };
+  next_statistics();
+  uint64_t dw[NV][P], db[NV][P];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
     for (int e = 0; e < P; ++e) dw[k][e] = db[k][e] = pair(0.f, 0.f);
   const float inv_d = 1.0f / static_cast<float>(a.d);
-  long long have = -1;                                                 // the replica whose weight is in w
+  long long have = -1;                                                 // the replica whose weight is in shared memory
   long long seg = first / a.tokens;
-  int next = group, done = 0;                                          // this group's next row in the run, rows done
+  int next = group;                                                    // this group's next row in the run
   for (int at = 0; at < run; ++seg) {
     const long long seg_end = (seg + 1) * a.tokens - first;
     const int stop = seg_end < run ? static_cast<int>(seg_end) : run;
     const long long sm = seg / a.samples;                              // the segment's replica
     if (sm != have) {
-      if (have < 0 || a.p_stride != 0)
-        load_param_pairs<T, NV>(a.weight ? a.weight + sm * a.p_stride : nullptr, 1.f, t, tpr, pieces, w);
+      if (have < 0 || a.p_stride != 0) {
+        if (have >= 0) __syncthreads();
+        stage_params<T>(params, a.weight ? a.weight + sm * a.p_stride : nullptr, 1.f, a.d);
+        __syncthreads();
+      }
       have = sm;
     }
     char* o = static_cast<char*>(a.dX) + (sm * a.dx_ws + (first + next - sm * rows) * a.dx_rs) * es + 16 * t;
-    for (; next < stop; next += groups, o += o_step) {
-      copy_row();                                                      // into the place of the row before
-      const float mean = n_mean, rstd = n_rstd;
-      mean_in += groups;
-      rstd_in += groups;
-      if (++done < count) {
-        n_mean = __ldg(mean_in);
-        n_rstd = __ldg(rstd_in);
-      }
-      asm volatile("cp.async.wait_group %0;" ::"n"(kBackRing - 1) : "memory");
-      const uint32_t xp = x_at.at, gp = xp + half_bytes;
-      const uint64_t r2 = pair(rstd, rstd), shift = pair(-mean, -mean);
-      uint64_t s1 = pair(0.f, 0.f), s2 = pair(0.f, 0.f);
+    while (next < stop) {
+      const bool two = next + groups < stop;                           // this group's next two rows, of one segment
+      copy_row();                                                      // into the places of the rows before
+      if (two) copy_row();
+      const float mean[2] = {n_mean[0], n_mean[1]}, rstd[2] = {n_rstd[0], n_rstd[1]};
+      const int n = two ? 2 : 1;
+      done += n;
+      mean_in += n * groups;
+      rstd_in += n * groups;
+      next_statistics();
+      copies_wait();
+      const uint32_t xp0 = x_at.at;
+      x_at.forward();
+      const uint32_t xp1 = x_at.at;
+      if (two) x_at.forward();
+      const uint64_t r2[2] = {pair(rstd[0], rstd[0]), pair(rstd[1], rstd[1])};
+      const uint64_t shift[2] = {pair(-mean[0], -mean[0]), pair(-mean[1], -mean[1])};
+      uint64_t s1[2] = {pair(0.f, 0.f), pair(0.f, 0.f)}, s2[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         if (t + k * tpr < pieces) {
-          uint64_t x[P], g[P];
-          read_piece<T>(xp + k * piece_step, x);
-          read_piece<T>(gp + k * piece_step, g);
+          uint64_t w[P];
 #pragma unroll
-          for (int e = 0; e < P; ++e) {
-            const uint64_t xh = mul2(add2(x[e], shift), r2), y = mul2(g[e], w[k][e]);
-            s1 = add2(s1, y);
-            s2 = fma2(y, xh, s2);
-            dw[k][e] = fma2(g[e], xh, dw[k][e]);
-            db[k][e] = add2(db[k][e], g[e]);
+          for (int e = 0; e < Q; ++e) read_params(w_at + (e * pieces + k * tpr) * 16u, w[2 * e], w[2 * e + 1]);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            if (q == 0 || two) {
+              const uint32_t xp = q == 0 ? xp0 : xp1;
+              uint64_t x[P], g[P];
+              read_piece<T>(xp + k * piece_step, x);
+              read_piece<T>(xp + half_bytes + k * piece_step, g);
+#pragma unroll
+              for (int e = 0; e < P; ++e) {
+                const uint64_t xh = mul2(add2(x[e], shift[q]), r2[q]), y = mul2(g[e], w[e]);
+                s1[q] = add2(s1[q], y);
+                s2[q] = fma2(y, xh, s2[q]);
+                dw[k][e] = fma2(g[e], xh, dw[k][e]);
+                db[k][e] = add2(db[k][e], g[e]);
+              }
+            }
           }
         }
       }
       if (a.dX != nullptr) {
-        const float2 c = group_sum2<ONE_WARP>(sum2(s1), sum2(s2), red, flip, group, t, tpr);
-        const float c1 = c.x * inv_d, c2 = c.y * inv_d;
-        const uint64_t nc1 = pair(-c1, -c1), nc2 = pair(-c2, -c2);
+        float4 c = make_float4(sum2(s1[0]), sum2(s2[0]), sum2(s1[1]), sum2(s2[1]));
+        c = group_sum4<ONE_WARP>(c, red, flip, group, t, tpr);
+        const uint64_t nc1[2] = {pair(-c.x * inv_d, -c.x * inv_d), pair(-c.z * inv_d, -c.z * inv_d)};
+        const uint64_t nc2[2] = {pair(-c.y * inv_d, -c.y * inv_d), pair(-c.w * inv_d, -c.w * inv_d)};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
           if (t + k * tpr < pieces) {
-            uint64_t x[P], g[P];
-            read_piece<T>(xp + k * piece_step, x);
-            read_piece<T>(gp + k * piece_step, g);
+            uint64_t w[P];
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-              const uint64_t xh = mul2(add2(x[e], shift), r2);
-              x[e] = mul2(r2, fma2(xh, nc2, fma2(g[e], w[k][e], nc1)));
+            for (int e = 0; e < Q; ++e) read_params(w_at + (e * pieces + k * tpr) * 16u, w[2 * e], w[2 * e + 1]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              if (q == 0 || two) {
+                const uint32_t xp = q == 0 ? xp0 : xp1;
+                uint64_t x[P], g[P];
+                read_piece<T>(xp + k * piece_step, x);
+                read_piece<T>(xp + half_bytes + k * piece_step, g);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                  const uint64_t xh = mul2(add2(x[e], shift[q]), r2[q]);
+                  x[e] = mul2(r2[q], fma2(xh, nc2[q], fma2(g[e], w[e], nc1[q])));
+                }
+                write_piece<T>(o + q * o_step + k * tpr * 16, x);
+              }
             }
-            write_piece<T>(o + k * tpr * 16, x);
           }
         }
       }
-      x_at.forward();
+      next += n * groups;
+      o += n * o_step;
     }
     if (a.part != nullptr) {
       float* out_w = a.part + part_slot(a.Gw != nullptr, blockIdx.x, seg, a.tokens, a.rows_per_cta) * 2 * a.d;
@@ -955,19 +1081,13 @@ ln_backward_ring_kernel(const LnBackward a, int tpr, int slots) {
         __syncthreads();
       }
       if (group == 0) {
+        const bool wide = ((reinterpret_cast<uintptr_t>(out_w) | reinterpret_cast<uintptr_t>(out_b)) & 15u) == 0;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
           const int v = t + k * tpr;
           if (v < pieces) {
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-              const float2 fw = unpair(dw[k][e]), fb = unpair(db[k][e]);
-              const int j = (v * P + e) * 2;
-              out_w[j] = fw.x;
-              out_w[j + 1] = fw.y;
-              out_b[j] = fb.x;
-              out_b[j + 1] = fb.y;
-            }
+            store_sums<P>(out_w + v * 2 * P, dw[k], wide);
+            store_sums<P>(out_b + v * 2 * P, db[k], wide);
           }
         }
       }
@@ -1012,14 +1132,17 @@ unsigned row_grid(const abs_ctx* ctx, long long rows) {
 
 
 // How a row of d elements is laid out over threads, or tpr = 0 where it does not fit: the fewest threads (a divisor of
-// the CTA's) that hold it in at most NV pieces each.  Pieces are of 16 bytes (NV up to 4, fp32, or 3, bf16: 16 or 24
-// elements, each with a weight and a bias or two running sums), or, where the alignment does not allow them, of one
-// element or two bf16 (one variant each, 16 elements a thread).
+// the CTA's) that hold it in at most NV pieces each; few, because what a row costs a warp besides its elements is half
+// of the instructions.  Pieces are of 16 bytes (NV up to most_wide: forward 6, where two rows' elements are in
+// registers; backward 4 of fp32 or 3 of bf16, where each element has two running sums), or, where the alignment does not allow them, of
+// one element or two bf16 (one variant each, 16 elements a thread).
 struct RowPlan {
   bool wide;
   int V, NV, tpr;
 };
-RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits) {
+constexpr size_t kRingBytes = 220 * 1024;          // dynamic shared memory of the ring kernels, at most
+size_t ring_smem(int NV, int threads, int tensors) { return static_cast<size_t>(kRing) * tensors * NV * threads * 16; }
+RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits, int most_wide, int tensors) {
   const int es = dtype == ABS_F32 ? 4 : 2;
   RowPlan p = {false, 1, 0, 0};
   align_bits |= static_cast<unsigned long long>(d) * es;
@@ -1027,14 +1150,18 @@ RowPlan plan_row(abs_dtype dtype, long long d, unsigned long long align_bits) {
   if (p.wide) p.V = 16 / es;
   else if (es == 2 && (align_bits & 3u) == 0) p.V = 2;
   const long long pieces = d / p.V;
-  const int most = p.wide ? (es == 4 ? 4 : 3) : 16 / p.V;
+  const int most = p.wide ? most_wide : 16 / p.V;
   const int tprs[6] = {32, 64, 96, 128, 192, 384};
-  for (int k = 0; k < 6; ++k)
-    if (pieces <= static_cast<long long>(tprs[k]) * most) {
-      p.tpr = tprs[k];
-      p.NV = p.wide ? static_cast<int>((pieces + p.tpr - 1) / p.tpr) : most;
-      break;
-    }
+  for (int k = 0; k < 6; ++k) {
+    if (pieces > static_cast<long long>(tprs[k]) * most) continue;
+    const int NV = p.wide ? static_cast<int>((pieces + tprs[k] - 1) / tprs[k]) : most;
+    // the ring, the parameters (two vectors forward, one backward) and, backward, one group's sums
+    const size_t vectors = tensors == 1 ? 2 : tprs[k] < kRingThreads ? 3 : 1;
+    if (p.wide && ring_smem(NV, kRingThreads, tensors) + vectors * static_cast<size_t>(d) * sizeof(float) > kRingBytes) continue;
+    p.tpr = tprs[k];
+    p.NV = NV;
+    break;
+  }
   return p;
 }
 
@@ -1053,12 +1180,12 @@ template <typename T, int NV>
 cudaError_t run_forward_ring(abs_ctx* ctx, const LnForward& a, int tpr, cudaStream_t st) {
   const long long total = a.rows * a.M;
   const int groups = kRingThreads / tpr;
-  const size_t smem = static_cast<size_t>(kRing) * NV * kRingThreads * 16;
-  const long long most = static_cast<long long>(ctx->sm_count) * groups;
+  const size_t smem = ring_smem(NV, kRingThreads, 1) + 2 * static_cast<size_t>(a.d) * sizeof(float);
+  const long long most = static_cast<long long>(ctx->sm_count);
   long long per = (total + most - 1) / most;
-  if (per > (1ll << 30)) per = 1ll << 30;                              // a group counts its rows in 32 bits
-  const long long used = (total + per - 1) / per;
-  const unsigned grid = static_cast<unsigned>((used + groups - 1) / groups);
+  if (per < groups) per = groups < total ? groups : total;             // a row for every group before a second CTA
+  if (per > (1ll << 30)) per = 1ll << 30;                              // a CTA counts its rows in 32 bits
+  const unsigned grid = static_cast<unsigned>((total + per - 1) / per);
   auto kern = tpr == 32 ? ln_forward_ring_kernel<T, NV, true> : ln_forward_ring_kernel<T, NV, false>;
   const cudaError_t e = ensure_dynamic_smem(ctx, kern, smem);
   if (e != cudaSuccess) return e;
@@ -1074,7 +1201,9 @@ cudaError_t dispatch_forward(abs_ctx* ctx, const LnForward& a, abs_dtype dtype, 
     case 1: return f ? run_forward_ring<float, 1>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 1>(ctx, a, p.tpr, st);
     case 2: return f ? run_forward_ring<float, 2>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 2>(ctx, a, p.tpr, st);
     case 3: return f ? run_forward_ring<float, 3>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 3>(ctx, a, p.tpr, st);
-    default: return run_forward_ring<float, 4>(ctx, a, p.tpr, st);
+    case 4: return f ? run_forward_ring<float, 4>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 4>(ctx, a, p.tpr, st);
+    case 5: return f ? run_forward_ring<float, 5>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 5>(ctx, a, p.tpr, st);
+    default: return f ? run_forward_ring<float, 6>(ctx, a, p.tpr, st) : run_forward_ring<__nv_bfloat16, 6>(ctx, a, p.tpr, st);
   }
 }
 
@@ -1092,12 +1221,14 @@ template <typename T, int NV>
 cudaError_t run_backward_ring(abs_ctx* ctx, const LnBackward& a, int tpr, int groups, unsigned grid, cudaStream_t st) {
   const size_t sum = 2 * static_cast<size_t>(a.d) * sizeof(float);
   int slots = 0;
-  if (a.part != nullptr && groups > 1) {             // sums of as many groups at a time as fit in 24 KB
-    slots = static_cast<int>(24 * 1024 / sum);
+  const size_t ring = ring_smem(NV, tpr * groups, 2) + static_cast<size_t>(a.d) * sizeof(float);
+  if (a.part != nullptr && groups > 1) {             // sums of as many groups at a time as there is room for, up to 48 KB
+    const size_t room = kRingBytes - ring;
+    slots = static_cast<int>((room < 48 * 1024 ? room : 48 * 1024) / sum);
     if (slots > groups - 1) slots = groups - 1;
     if (slots < 1) slots = 1;
   }
-  const size_t smem = static_cast<size_t>(kBackRing) * 2 * NV * (tpr * groups) * 16 + slots * sum;
+  const size_t smem = ring + slots * sum;
   auto kern = tpr == 32 ? ln_backward_ring_kernel<T, NV, true> : ln_backward_ring_kernel<T, NV, false>;
   const cudaError_t e = ensure_dynamic_smem(ctx, kern, smem);
   if (e != cudaSuccess) return e;
@@ -1149,7 +1280,7 @@ extern "C" int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int 
               mean, rstd, M, rows, static_cast<int>(d)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const RowPlan plan = plan_row(dtype, d, row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
-                                              row_bits(Y, dtype, M, y_row_stride, y_worker_stride));
+                                              row_bits(Y, dtype, M, y_row_stride, y_worker_stride), 6, 1);
   if (plan.tpr > 0) {
     ABS_CUDA_TRY(ctx, dispatch_forward(ctx, a, dtype, plan, st));
     return ABS_OK;
@@ -1197,10 +1328,12 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
                dX, dx_row_stride, dx_worker_stride, M, samples, tokens, static_cast<int>(d), nullptr, 1, nullptr, nullptr, 0, 0};
   const RowPlan plan = plan_row(dtype, d, row_bits(dY, dtype, M, dy_row_stride, dy_worker_stride) |
                                               row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
-                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0));
+                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0), dtype == ABS_F32 ? 4 : 3, 2);
   const bool sums = per_sample || totals;
-  LnReduce red{static_cast<const float*>(ctx->workspace), M, samples, tokens, 1, static_cast<int>(d), 0, Gw, Gb, g_row_stride,
-               g_worker_stride, dW, dB, grad_stride};
+  LnReduce red{static_cast<const float*>(ctx->workspace), M, samples, tokens, 1, static_cast<int>(d), 0, 0, samples > 0 ? samples : 1,
+               nullptr, Gw, Gb, g_row_stride, g_worker_stride, dW, dB, grad_stride};
+  const long long room = static_cast<long long>(ctx->workspace_bytes / (2 * sizeof(float))) / d;     // of the workspace, in partial sums
+  long long used = 0, parts = 1;                                       // ... in use; CTAs that share a column's samples
   if (rows > 0) {
     const bool fast = plan.tpr > 0;
     const long long total = rows * M, segments = samples * M;
@@ -1218,7 +1351,6 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
     const long long worth = (total + 2 * groups - 1) / (2 * groups);         // at least two rows a group
     if (ctas > worth) ctas = worth;
     if (sums) {
-      const long long room = static_cast<long long>(ctx->workspace_bytes / (2 * sizeof(float))) / d;     // partial sums
       const bool direct = Gw != nullptr && Gb != nullptr;
       const long long needed = direct ? 2 : segments + 1, most = direct ? room / 2 : room - segments;
       if (room < needed)
@@ -1235,6 +1367,19 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
     if (groups == 1 && sums && a.rows_per_cta > tokens) a.rows_per_cta = a.rows_per_cta / tokens * tokens;      // whole segments
     ctas = (total + a.rows_per_cta - 1) / a.rows_per_cta;
     red.rows_per_cta = a.rows_per_cta;
+    red.whole = red.direct && a.rows_per_cta % tokens == 0;
+    used = red.direct ? 2 * ctas : ctas + segments;
+    // 32 samples a CTA, where that fills the GPU no further than needed
+    if (per_sample) {
+      parts = (samples + 31) / 32;
+      const long long most = 1 + 16ll * ctx->sm_count * 32 / (2 * d * M), fit = totals ? (room - used) / M : parts;
+      if (parts > most) parts = most;
+      if (parts > fit) parts = fit;
+      if (parts < 1) parts = 1;
+      red.per_cta = (samples + parts - 1) / parts;
+      parts = (samples + red.per_cta - 1) / red.per_cta;
+      if (parts > 1 && totals) red.totals = static_cast<float*>(ctx->workspace) + used * 2 * d;
+    }
     if (fast) {
       ABS_CUDA_TRY(ctx, dispatch_backward(ctx, a, dtype, plan, groups, static_cast<unsigned>(ctas), st));
     } else {
@@ -1250,8 +1395,11 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
       }
     }
   }
-  if (sums)
-    ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M), dim3(kLnThreads), 0,
-                                       st, red));
+  if (!sums || (red.whole && !totals)) return ABS_OK;
+  ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M, static_cast<unsigned>(parts)),
+                                     dim3(kLnThreads), 0, st, red));
+  if (red.totals)
+    ABS_CUDA_TRY(ctx, launch_dependent(ln_total_kernel, dim3(static_cast<unsigned>((2 * d + kLnThreads - 1) / kLnThreads), M),
+                                       dim3(kLnThreads), 0, st, red, static_cast<int>(parts)));
   return ABS_OK;
 }
