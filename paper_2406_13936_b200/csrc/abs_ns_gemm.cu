@@ -26,15 +26,14 @@
 // An SM takes in about 64 bytes a clock from L2 (measured: a k-block of 64 of a 128 x 128 tile, 32 KB,
 // takes 556 clocks, its products 256), which is what a pair's tile needs at the tensor cores' full rate.
 //
-// Roles of a CTA's 13 warps: 0 loads operands by TMA into a ring of 32 KB stages, 12 looks out for the
-// inputs of the next tile meanwhile, 1 issues the products
-// (fp32 accumulators in tensor memory, two of them, so the next tile's products run while this one is
-// read back), 4-7 and 8-11 are the two halves of the epilogue (each reads back half the tile's columns and
-// applies the coefficients in place, in shared memory), 2 and 3 move the units of one half each: they load
-// what the coefficients apply to, store the results by TMA and announce the half tile, so that no epilogue
-// warp waits for a copy to finish or for a fence.  All waits are bounded; one that runs out raises the
-// CTA's abort flag and the call's flag word, every role falls through, copies in flight are waited for and
-// tensor memory is freed.
+// Roles of a CTA's 14 warps: 0 loads operands by TMA into a ring of 32 KB stages, 12 looks out for the inputs of
+// the next tile meanwhile, 1 issues the products (fp32 accumulators in tensor memory, two of them, so the next
+// tile's products run while this one is read back), 4-7 and 8-11 are the two halves of the epilogue (each reads back
+// half the tile's columns and applies the coefficients in place, in shared memory), 2 loads what the
+// coefficients apply to, 3 and 13 store one half's results by TMA and announce the half tile.  Loads, stores and
+// announcements (a fence of 1000 to 4000 clocks) have threads of their own because one after the other they took
+// longer than a tile's products.  All waits are bounded; one that runs out raises the CTA's abort flag and the call's
+// flag word, every role falls through, copies in flight are waited for and tensor memory is freed.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
 
@@ -47,22 +46,17 @@ constexpr int kBM = 128;                     // rows of a CTA's tile
 constexpr int kEpiWarpsN = 8;
 constexpr int kFirstEpi = 4;
 constexpr int kLookout = kFirstEpi + kEpiWarpsN;
-constexpr int kThreadsN = (kLookout + 1) * 32;             // 416
+constexpr int kThreadsN = (kLookout + 2) * 32;             // 448
 constexpr uint32_t kStageN = 32768;
 // Units of the epilogue: 32 columns of the tile's 128 rows, changed in place in shared memory: 8 KB of fp16
-// values (A, B) or 16 KB of values and remainders (X; with split operands any matrix).  A half of the epilogue
-// has room for all units of its half tile, except for X on pairs: three of four; the fourth takes the first
-// one's place when that has been stored.  (Room for four would cost a stage of the ring: 3 instead of 4 made
-// a step on 4096 x 4096 a tenth slower.)
+// values (A, B) or 16 KB of values and remainders (X; with split operands any matrix).  Each half of the epilogue has
+// a ring of three places for them, which runs on from tile to tile.
 constexpr int kUnitCols = 32;
 constexpr uint32_t kUnitBytes = kBM * kUnitCols * 2;       // 8 KB
-template <int CG>
-struct Smem {
-  static constexpr int kStages = CG == 2 ? 4 : 5;
-  static constexpr int kHeld = CG == 2 ? 3 : 2;              // units of X in a half's area
-  static constexpr uint32_t kHalfArea = kHeld * 2 * kUnitBytes;
-  static constexpr size_t kBytes = static_cast<size_t>(kStages) * kStageN + 2 * kHalfArea + 1024 + 512;      // alignment, barriers
-};
+constexpr int kStagesN = 4;
+constexpr uint32_t kPlaces = 3;
+constexpr uint32_t kHalfArea = kPlaces * 2 * kUnitBytes;
+constexpr size_t kSmemN = static_cast<size_t>(kStagesN) * kStageN + 2 * kHalfArea + 1024 + 512;      // alignment, barriers
 // Split operands: an accumulator of the main products takes kFold k-blocks of 32 (2 kFold additions) and is
 // then added, rounded to nearest, to sums in registers: the tensor core adds without rounding to nearest.
 constexpr int kFold = 8;
@@ -276,7 +270,6 @@ __global__ void __launch_bounds__(kThreadsN, 1)
 ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsStepsParams p) {
   static_assert(CG == 1 || !SPLIT, "split operands use single CTAs");
   constexpr int BN = 128 * CG;                               // columns of a tile
-  constexpr int kStagesN = Smem<CG>::kStages;
   constexpr int kBK = SPLIT ? 32 : 64;                       // k-block
   constexpr uint32_t kOperand = SPLIT ? 8192u : 16384u;      // bytes of one operand tile of a stage
   constexpr int kUnits = BN / 2 / kUnitCols;                 // units of a tile per half of the epilogue
@@ -286,15 +279,14 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
   if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t raw = smem_u32(smem_dyn), ring = (raw + 1023u) & ~1023u;
   const uint32_t epi_at = ring + kStagesN * kStageN;
-  constexpr uint32_t kHalfArea = Smem<CG>::kHalfArea, kHeld = Smem<CG>::kHeld;
   unsigned char* tail = smem_dyn + (ring - raw) + kStagesN * kStageN + 2 * kHalfArea;
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(tail);
-  constexpr int kBars = 2 * kStagesN + 11 + 4 * kUnits;
+  constexpr int kBars = 2 * kStagesN + 11 + 6 * kPlaces;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   const uint32_t full = smem_u32(bars), empty = full + 8u * kStagesN, accfull = empty + 8u * kStagesN, accempty = accfull + 16u,
-                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 16u * kUnits,
-                 inputs = filled + 16u * kUnits, taken = inputs + 16u;
+                 crossempty = accempty + 16u, done = crossempty + 16u, ready = done + 8u, filled = ready + 16u * kPlaces,
+                 freed = filled + 16u * kPlaces, inputs = freed + 16u * kPlaces, taken = inputs + 16u;
   if (tid == 0) {
     for (int s = 0; s < kStagesN; ++s) {
       mbar_init(full + 8u * s, 1);
@@ -305,12 +297,13 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       mbar_init(accempty + 8u * k, kEpiWarpsN * CG);
       mbar_init(crossempty + 8u * k, kEpiWarpsN);
       mbar_init(inputs + 8u * k, 1);                       // a tile's inputs are complete
-      mbar_init(taken + 8u * k, 1);                        // ... and its loads begin
+      mbar_init(taken + 8u * k, 2);                        // ... and both loaders know
     }
     mbar_init(done, 1);
-    for (int k = 0; k < 2 * kUnits; ++k) {               // per half and unit, each used once per tile
+    for (uint32_t k = 0; k < 2 * kPlaces; ++k) {         // per half and place
       mbar_init(ready + 8u * k, 1);                      // loaded (or free)
       mbar_init(filled + 8u * k, kEpiWarpsN / 2);        // finished
+      mbar_init(freed + 8u * k, 1);                      // ... and stored
     }
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -452,56 +445,71 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     __syncwarp();
     volatile unsigned ignore = 0u;
     mbar_wait(done, 0u, &ignore, p.timeout_cycles);           // no product in flight when tensor memory is freed
-  } else if (warp == 2 || warp == 3) {
-    // ---- units of one half of the epilogue: loads, stores, announcements --------------------------------
+  } else if (warp == 2) {
+    // ---- loads of the units that the coefficients apply to --------------------------------------------
     if (elect_one_n()) {
-      const uint32_t half = static_cast<uint32_t>(warp) - 2u;
-      const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
-      uint32_t it = 0;
+      uint32_t it = 0, n = 0;                                  // n: units of each half so far
       bool ok = true;
-      for (long long t = first; t < p.tiles && ok; t += step, ++it) {
+      for (long long t = first; t < p.tiles && ok && !p.drop_loads; t += step, ++it) {
         const Tile q = tile_of(p, t);
-        const int cur = q.step & 1, row = q.i * BN + row_in_tile, col = q.j * BN + static_cast<int>(half) * (BN / 2);
-        const bool x = q.mode == kUpdate;
-        const bool low = SPLIT || x;                           // values and remainders
-        const uint32_t size = low ? 2u * kUnitBytes : kUnitBytes;
-        const int low_in = SPLIT ? cur : 0, low_out = SPLIT ? cur ^ 1 : 0;      // remainders of X stay where they are, unless operands
-        if (q.mode != kGram && !p.drop_loads) ok = wait_inputs<CG>(p, q, abort_flag);
+        const int cur = q.step & 1, row = q.i * BN + row_in_tile;
+        const bool x = q.mode == kUpdate, low = SPLIT || x;    // low: values and remainders
+        const CUtensorMap* m_h = x ? &maps.xu_h[cur] : &maps.au_h;
+        const CUtensorMap* m_l = x ? &maps.xu_l[SPLIT ? cur : 0] : &maps.au_l;      // remainders of X stay in place, unless operands
+        ok = mbar_wait(inputs + 8u * (it & 1u), (it >> 1) & 1u, abort_flag, p.timeout_cycles);
         if (!ok) break;
-        const uint32_t held = low && !SPLIT ? kHeld : kUnits;
-        uint32_t loaded = 0;
-        auto load_next = [&]() {
-          const uint32_t u = loaded++, at = area + (u % held) * size, bar = ready_h + 8u * u;
-          const int c = col + static_cast<int>(u) * kUnitCols;
-          if (q.mode == kGram || p.drop_loads) {
-            mbar_arrive(bar);
-          } else {
-            mbar_expect_tx(bar, size);
-            tma_load_3d(at, x ? &maps.xu_h[cur] : &maps.au_h, c, row, q.z, bar);
-            if (low) tma_load_3d(at + kUnitBytes, x ? &maps.xu_l[low_in] : &maps.au_l, c, row, q.z, bar);
+        mbar_arrive(taken + 8u * (it & 1u));
+        for (int u = 0; u < kUnits && ok; ++u, ++n) {
+          const uint32_t place = n % kPlaces;
+          for (uint32_t half = 0; half < 2; ++half) {
+            const uint32_t k = half * kPlaces + place, at = epi_at + k * 2u * kUnitBytes, bar = ready + 8u * k;
+            if (n >= kPlaces) ok = mbar_wait(freed + 8u * k, (n / kPlaces - 1u) & 1u, abort_flag, p.timeout_cycles);
+            if (!ok) break;
+            if (q.mode == kGram) {
+              mbar_arrive(bar);
+            } else {
+              const int c = q.j * BN + static_cast<int>(half) * (BN / 2) + u * kUnitCols;
+              mbar_expect_tx(bar, low ? 2u * kUnitBytes : kUnitBytes);
+              tma_load_3d(at, m_h, c, row, q.z, bar);
+              if (low) tma_load_3d(at + kUnitBytes, m_l, c, row, q.z, bar);
+            }
           }
-        };
-        for (uint32_t u = 0; u < held; ++u) load_next();
-        const CUtensorMap* o_h = q.mode == kGram ? &maps.au_h : q.mode == kPoly ? &maps.bu_h : &maps.xu_h[cur ^ 1];
-        const CUtensorMap* o_l = q.mode == kGram ? &maps.au_l : q.mode == kPoly ? &maps.bu_l : &maps.xu_l[low_out];
-        for (uint32_t u = 0; u < kUnits; ++u) {
-          ok = mbar_wait(filled_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles);
           if (!ok) break;
-          const uint32_t at = area + (u % held) * size;
-          const int c = col + static_cast<int>(u) * kUnitCols;
+        }
+      }
+      if (!ok) {                                               // no load in flight when the CTA exits
+        volatile unsigned ignore = 0u;
+        for (uint32_t k = n > kPlaces ? n - kPlaces : 0u; k < n; ++k)
+          for (uint32_t half = 0; half < 2; ++half)
+            mbar_wait(ready + 8u * (half * kPlaces + k % kPlaces), (k / kPlaces) & 1u, &ignore, p.timeout_cycles);
+        mbar_wait(ready + 8u * (n % kPlaces), (n / kPlaces) & 1u, &ignore, 100000);      // (the first half's, if it was asked for)
+      }
+    }
+    __syncwarp();
+  } else if (warp == 3 || warp == kLookout + 1) {
+    // ---- stores of one half's units, announcements ----------------------------------------------------
+    if (elect_one_n()) {
+      const uint32_t half = warp == 3 ? 0u : 1u;
+      uint32_t n = 0;
+      bool ok = true;
+      for (long long t = first; t < p.tiles && ok; t += step) {
+        const Tile q = tile_of(p, t);
+        const int nxt = (q.step & 1) ^ 1, row = q.i * BN + row_in_tile, col = q.j * BN + static_cast<int>(half) * (BN / 2);
+        const bool x = q.mode == kUpdate, low = SPLIT || x;
+        const CUtensorMap* o_h = q.mode == kGram ? &maps.au_h : q.mode == kPoly ? &maps.bu_h : &maps.xu_h[nxt];
+        const CUtensorMap* o_l = q.mode == kGram ? &maps.au_l : q.mode == kPoly ? &maps.bu_l : &maps.xu_l[SPLIT ? nxt : 0];
+        for (int u = 0; u < kUnits; ++u, ++n) {
+          const uint32_t k = half * kPlaces + n % kPlaces, at = epi_at + k * 2u * kUnitBytes;
+          ok = mbar_wait(filled + 8u * k, (n / kPlaces) & 1u, abort_flag, p.timeout_cycles);
+          if (!ok) break;
+          const int c = col + u * kUnitCols;
           tma_store_3d(o_h, at, c, row, q.z);
           if (low) tma_store_3d(o_l, at + kUnitBytes, c, row, q.z);
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          if (loaded < kUnits) {
-            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-            load_next();
-          }
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          mbar_arrive(freed + 8u * k);
         }
-        if (!ok) {                                             // no load in flight when the CTA exits
-          volatile unsigned ignore = 0u;
-          for (uint32_t u = 0; u < loaded; ++u) mbar_wait(ready_h + 8u * u, it & 1u, &ignore, p.timeout_cycles);
-          break;
-        }
+        if (!ok) break;
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         asm volatile("fence.acq_rel.gpu;" ::: "memory");       // the half tile, before its announcement
         unsigned* base = p.progress + static_cast<long long>(q.z) * 3 * p.row_blocks;
@@ -528,7 +536,7 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       }
     }
     __syncwarp();
-  } else if (warp >= kFirstEpi) {                            // (warp 1 of a pair's second CTA has nothing to do)
+  } else if (warp >= kFirstEpi && warp < kLookout) {        // (warp 1 of a pair's second CTA has nothing to do)
     // ---- epilogue: a thread owns a row of the tile and 32 columns of it at a time -----------------------
     const int q4 = warp & 3;
     const uint32_t half = static_cast<uint32_t>(warp - kFirstEpi) >> 2;
@@ -536,7 +544,6 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
     const uint32_t sw64 = (row >> 1) & 3u;                     // swizzle of rows of 64 bytes
     const uint32_t t_row = tmem + half * (BN / 2) + (static_cast<uint32_t>(q4 * 32) << 16);
     const uint32_t accempty0 = CG == 2 ? map_to_rank(accempty, 0) : accempty;
-    const uint32_t area = epi_at + half * kHalfArea, ready_h = ready + 8u * kUnits * half, filled_h = filled + 8u * kUnits * half;
     auto hand_back = [&](uint32_t buf) {                      // this warp has read its part of the accumulator
       tcn_before();
       __syncwarp();
@@ -545,7 +552,7 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         else mbar_arrive(accempty + 8u * buf);
       }
     };
-    uint32_t it = 0, acc = 0;
+    uint32_t it = 0, acc = 0, n = 0;                          // n: units so far
     bool ok = true;
     for (long long t = first; t < p.tiles && ok; t += step, ++it) {
       const Tile q = tile_of(p, t);
@@ -593,9 +600,9 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
       }
       const bool low = SPLIT || q.mode == kUpdate;            // values and remainders
 #pragma unroll
-      for (int u = 0; u < kUnits; ++u) {
-        const uint32_t h_at = area + (low && !SPLIT ? (u % kHeld) * 2u : low ? u * 2u : u) * kUnitBytes + row * 64u;
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(ready_h + 8u * u, it & 1u, abort_flag, p.timeout_cycles));
+      for (int u = 0; u < kUnits; ++u, ++n) {
+        const uint32_t place = half * kPlaces + n % kPlaces, h_at = epi_at + place * 2u * kUnitBytes + row * 64u;
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(ready + 8u * place, (n / kPlaces) & 1u, abort_flag, p.timeout_cycles));
         uint64_t v[16];                                       // pairs of results
         if constexpr (!SPLIT) tmem_wait(r[u & 1]);
 #pragma unroll
@@ -649,7 +656,7 @@ ns_steps_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsS
         }
         fence_async_n();
         __syncwarp();
-        if (lane == 0) mbar_arrive(filled_h + 8u * u);
+        if (lane == 0) mbar_arrive(filled + 8u * place);
       }
     }
   }
@@ -715,7 +722,7 @@ int launch_steps(abs_ctx* ctx, const NsBuffers& w, NsStepsParams& p, cudaStream_
   p.per_step = static_cast<long long>(w.Z) * (2ll * p.tri + static_cast<long long>(p.row_blocks) * p.col_tiles);
   p.tiles = p.per_step * p.steps;
 
-  const size_t smem = Smem<CG>::kBytes;
+  const size_t smem = kSmemN;
   auto kern = ns_steps_kernel<CG, SPLIT>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
   const long long widest = static_cast<long long>(w.Z) * p.row_blocks * (p.row_blocks > p.col_tiles ? p.row_blocks : p.col_tiles);
