@@ -192,13 +192,13 @@ def load_library():
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
+    return t.data_ptr() if t is not None else None
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    if stream is None:                     # the current stream's handle, without making a Stream object for it
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _dtype_code(t):
@@ -387,24 +387,26 @@ class Context:
     def _rows(t, what):
         """(row stride, worker stride) of [M, rows, d]; the strides of dimensions of one element are free."""
         M, rows, d = t.shape
-        if t.stride(2) != 1 and d > 1:
+        worker, row, one = t.stride()
+        if one != 1 and d > 1:
             raise AbsError("the last dimension of %s must be contiguous" % what)
-        row = t.stride(1) if rows > 1 else d
-        return row, t.stride(0) if M > 1 else row * rows
+        if rows <= 1:
+            row = d
+        return row, worker if M > 1 else row * rows
 
     @staticmethod
-    def _params(t, M, d, what):
-        """Checks [M, d] fp32 parameters (a replica each) and returns their stride."""
-        if t.dtype != torch.float32 or t.shape != (M, d) or (d > 1 and t.stride(1) != 1):
-            raise AbsError("%s must be float32 [%d, %d] with contiguous rows" % (what, M, d))
-        return t.stride(0) if M > 1 else d
-
-    @classmethod
-    def _same_stride(cls, tensors, M, d, what):
-        strides = {cls._params(t, M, d, what) for t in tensors if t is not None}
-        if len(strides) > 1:
-            raise AbsError("%s must share the replica stride" % what)
-        return strides.pop() if strides else d
+    def _same_stride(tensors, M, d, what):
+        """Checks [M, d] fp32 parameters (a replica each; None: absent) and returns their stride."""
+        stride = None
+        for t in tensors:
+            if t is not None:
+                if t.dtype != torch.float32 or t.shape != (M, d) or (d > 1 and t.stride(1) != 1):
+                    raise AbsError("%s must be float32 [%d, %d] with contiguous rows" % (what, M, d))
+                own = t.stride(0) if M > 1 else d
+                if stride is not None and own != stride:
+                    raise AbsError("%s must share the replica stride" % what)
+                stride = own
+        return d if stride is None else stride
 
     def abs_layer_norm(self, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
         """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight, bias: [M, d] (or [d]) fp32 or None; mean, rstd:
@@ -412,9 +414,10 @@ class Context:
         if X.dim() == 2:
             X, Y = X.unsqueeze(0), Y.unsqueeze(0)
             weight, bias = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, bias))
-        if X.dim() != 3 or X.shape != Y.shape or X.dtype != Y.dtype:
+        shape = X.shape
+        if len(shape) != 3 or Y.shape != shape or X.dtype != Y.dtype:
             raise AbsError("X and Y must be [M, rows, d] of one type")
-        M, rows, d = X.shape
+        M, rows, d = shape
         p_stride = self._same_stride((weight, bias), M, d, "weight and bias")
         self._statistics((mean, rstd), M * rows)
         x_rs, x_ws = self._rows(X, "X")
@@ -439,25 +442,26 @@ class Context:
             dY, X, dX = (t if t is None else t.unsqueeze(0) for t in (dY, X, dX))
             weight, dW, dB = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, dW, dB))
             Gw, Gb = (t if t is None or t.dim() == 3 else t.unsqueeze(0) for t in (Gw, Gb))
-        for t in (dY, X, dX):
-            if t is not None and (t.dim() != 3 or t.shape != X.shape or t.dtype != X.dtype):
-                raise AbsError("dY, X and dX must be [M, rows, d] of one type")
-        M, rows, d = X.shape
+        shape, dtype = X.shape, X.dtype
+        if len(shape) != 3 or any(t is not None and (t.shape != shape or t.dtype != dtype) for t in (dY, dX)):
+            raise AbsError("dY, X and dX must be [M, rows, d] of one type")
+        M, rows, d = shape
         samples = int(samples)
         if samples < 0 or (samples == 0 and rows) or (samples and rows % samples):
             raise AbsError("%d rows are not %d samples of equal length" % (rows, samples))
         p_stride = self._same_stride((weight,), M, d, "weight")
         grad_stride = self._same_stride((dW, dB), M, d, "dW and dB")
         self._statistics((mean, rstd), M * rows)
-        g_strides = set()
+        g_strides = None
         for t in (Gw, Gb):
             if t is not None:
                 if t.dtype != torch.float32 or t.shape != (M, samples, d):
                     raise AbsError("Gw and Gb must be float32 [%d, %d, %d]" % (M, samples, d))
-                g_strides.add(self._rows(t, "Gw and Gb"))
-        if len(g_strides) > 1:
-            raise AbsError("Gw and Gb must share their strides")
-        g_rs, g_ws = g_strides.pop() if g_strides else (d, d * samples)
+                own = self._rows(t, "Gw and Gb")
+                if g_strides is not None and own != g_strides:
+                    raise AbsError("Gw and Gb must share their strides")
+                g_strides = own
+        g_rs, g_ws = g_strides or (d, d * samples)
         y_rs, y_ws = self._rows(dY, "dY")
         x_rs, x_ws = self._rows(X, "X")
         dx_rs, dx_ws = self._rows(dX, "dX") if dX is not None else (d, d)

@@ -124,7 +124,7 @@ ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float ep
   for (int k = 0; k < kTileVecs; ++k) {
     const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
     const int i = (tall ? tc : tr) * kTile + ri, j = (tall ? tr : tc) * kTile + cj;      // row and column of X
-    if (i >= w.m || j >= w.n) continue;                        // ldx is a multiple of 8: four columns stay in the row
+    if (i >= w.m || j >= w.n) continue;                        // ldx is a multiple of 64: four columns stay in the row
     float x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = static_cast<float>((tall ? tile[ri][cj + e] : u[k][e]) * scale);
@@ -284,8 +284,8 @@ NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
   NsPlan p;
   p.m = static_cast<int>(rows < cols ? rows : cols);
   p.n = static_cast<int>(rows < cols ? cols : rows);
-  p.ldx = align_up(p.n, 8);
-  p.ldm = align_up(p.m, 8);
+  p.ldx = align_up(p.n, 64);      // rows of whole 128-byte lines: 8 of 784 x 1024 44 us a step in pairs, 48 with rows of 8 halves
+  p.ldm = align_up(p.m, 64);
   p.x_halves = p.ldx * p.m;
   p.m_halves = p.ldm * p.m;
   // Up to 64 rows the operands are split at either precision: with few rows the roundings of 11 bits do

@@ -31,7 +31,7 @@ struct NsScales {
 // Device buffers of one group of Z matrices.  Step k reads the X of k & 1 and writes the other.
 struct NsBuffers {
   int Z, m, n;
-  long long ldx, ldm;              // leading dimensions in elements, multiples of 8
+  long long ldx, ldm;              // leading dimensions in elements, multiples of 64
   __half* xh[2];
   __half* xl[2];                   // remainders; without split operands only [0], changed in place
   __half* ah;

@@ -772,7 +772,19 @@ int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float 
   p.drop_loads = ctx->tuning.stats_fault_drop_loads ? 1 : 0;
   for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
   if (split) return launch_steps<1, true>(ctx, w, p, st);
-  const int pairs = ctx->tuning.ns_pair_tiles ? ctx->tuning.ns_pair_tiles == 2 : w.m > 256;
+  // Single CTAs or pairs.  A pair's 256 x 256 tile takes about as long as a single CTA's 128 x 128 (each is bound by
+  // what its SMs fetch), so a step of T1 or T2 tiles takes T1 / 148 or T2 / 74 of that time: pairs are up to twice as fast, less
+  // what the last row and column blocks pad.  A larger tile has the longer epilogue, which counts where matrices are small
+  // or few.  us a step, pairs and single CTAs (T1 / T2): 4096 x 4096 221, 353 (3.94); 2000 x 1500 40, 50 (3.87); 8 of
+  // 1024 x 1024 38, 48 (3.78); 14 of 768 x 768 33, 37 (3.71); 56 of 256 x 1024 34, 36 and 24 of 200 x 1000 26, 23 (3.67);
+  // 16 of 512 x 512 25, 24 (3.6); 8 of 784 x 1024 44, 43 (3.1); 64 of 300 x 520 54, 38 (2.25); and with fewer tiles than pairs
+  // 1024 x 1024 40, 29.
+  auto tiles = [&](long long side) {
+    const long long rb = (w.m + side - 1) / side, cb = (w.n + side - 1) / side;
+    return w.Z * (rb * (rb + 1) + rb * cb);
+  };
+  const long long t1 = tiles(128), t2 = tiles(256);
+  const bool pairs = ctx->tuning.ns_pair_tiles ? ctx->tuning.ns_pair_tiles == 2 : 10 * t1 > 37 * t2 && 2 * t2 >= ctx->sm_count;
   return pairs ? launch_steps<2, false>(ctx, w, p, st) : launch_steps<1, false>(ctx, w, p, st);
 }
 
