@@ -77,15 +77,13 @@ ns_norm_kernel(const NsSource s, int q0, double* __restrict__ part, unsigned* __
 // X_0 = U / (||U||_F + eps), scaled by sx, as hi + lo, transposed where U is taller than wide.  A CTA
 // takes a 64 x 64 tile of U; a warp reads and writes whole rows of it, four elements a lane.
 template <int V>
-__global__ void __launch_bounds__(kPassThreads)
+__global__ void __launch_bounds__(kPassThreads, 6)
 ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float eps, float sx, int tiles_c) {
   __shared__ float tile[kTile][kTile + 1];
   __shared__ double red[kPassThreads / 32];
   const int z = blockIdx.y, tid = threadIdx.x;
   pdl_launch_dependents();
   pdl_wait();
-  double sum = 0.0;
-  for (int k = tid; k < parts; k += kPassThreads) sum += w.part[static_cast<long long>(z) * kNormParts + k];
   const bool tall = s.rows > s.cols;
   const int tr = static_cast<int>(blockIdx.x) / tiles_c, tc = static_cast<int>(blockIdx.x) - tr * tiles_c;
   const long long base = matrix_base(q0 + z, s.L, s.replica_stride, s.matrix_stride);
@@ -104,6 +102,8 @@ ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float ep
       for (int x = 0; x < V; ++x) u[k][e + x] = t[x];
     }
   }
+  double sum = 0.0;
+  for (int k = tid; k < parts; k += kPassThreads) sum += w.part[static_cast<long long>(z) * kNormParts + k];
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
   if ((tid & 31) == 0) red[tid >> 5] = sum;
@@ -138,8 +138,8 @@ ns_split_kernel(const NsSource s, int q0, const NsBuffers w, int parts, float ep
 }
 
 // O = X / sx back in the caller's orientation: the result, or the parameter update.
-template <int V>
-__global__ void __launch_bounds__(kPassThreads)
+template <int V, bool MUON>
+__global__ void __launch_bounds__(kPassThreads, MUON ? 5 : 6)
 ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, int cur, int low, float inv_sx, int tiles_c,
                  const unsigned* flag) {
   __shared__ float tile[kTile][kTile + 1];
@@ -150,6 +150,23 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
   const int tr = static_cast<int>(blockIdx.x) / tiles_c, tc = static_cast<int>(blockIdx.x) - tr * tiles_c;
   const long long zoff = z * w.ldx * w.m;
   const float bad = *flag ? __int_as_float(0x7fc00000) : 0.f;          // a product whose wait ran out: nothing is valid
+  // Every load before the first store, which may be to the same place as far as the compiler knows, and few enough
+  // registers for five or six CTAs an SM: 32 of 768 x 768 in 34 us (Muon 49), without 51 (56).
+  const long long base = matrix_base(q0 + z, s.L, t.replica_stride, t.matrix_stride);
+  float x0[kTileVecs][4];
+#pragma unroll
+  for (int k = 0; k < kTileVecs; ++k) {
+    const int r = tr * kTile + (tid >> 4) + 16 * k, c = tc * kTile + 4 * (tid & 15);
+#pragma unroll
+    for (int e = 0; e < 4; e += V) {
+      float x[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = 0.f;
+      if (MUON && r < s.rows && c + e < s.cols) load_f32<V>(t.X + base + static_cast<long long>(r) * t.row_stride + c + e, x);
+#pragma unroll
+      for (int v = 0; v < V; ++v) x0[k][e + v] = x[v];
+    }
+  }
   float u[kTileVecs][4];
 #pragma unroll
   for (int k = 0; k < kTileVecs; ++k) {
@@ -158,7 +175,7 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < w.m && j < w.n) {
       const long long o = zoff + static_cast<long long>(i) * w.ldx + j;
-      const uint2 h = *reinterpret_cast<const uint2*>(w.xh[cur] + o), l = *reinterpret_cast<const uint2*>(w.xl[low] + o);
+      const uint2 h = *reinterpret_cast<const uint2*>((cur ? w.xh[1] : w.xh[0]) + o), l = *reinterpret_cast<const uint2*>((low ? w.xl[1] : w.xl[0]) + o);
       const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&h.x)), l0 = __half22float2(*reinterpret_cast<const __half2*>(&l.x));
       const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&h.y)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&l.y));
       x = make_float4(h0.x + l0.x, h0.y + l0.y, h1.x + l1.x, h1.y + l1.y);
@@ -173,7 +190,6 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
     }
   }
   if (tall) __syncthreads();
-  const long long base = matrix_base(q0 + z, s.L, t.replica_stride, t.matrix_stride);
 #pragma unroll
   for (int k = 0; k < kTileVecs; ++k) {
     const int ri = (tid >> 4) + 16 * k, cj = 4 * (tid & 15);
@@ -190,11 +206,9 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
       float v[V];
 #pragma unroll
       for (int x = 0; x < V; ++x) v[x] = u[k][e + x];
-      if (s.muon) {
-        float x0[V];
-        load_f32<V>(t.X + i + e, x0);
+      if (MUON) {
 #pragma unroll
-        for (int x = 0; x < V; ++x) v[x] = fmaf(-t.step, v[x], t.decay * x0[x]);
+        for (int x = 0; x < V; ++x) v[x] = fmaf(-t.step, v[x], t.decay * x0[k][e + x]);
         store_f32<V>(t.X + i + e, v);
       } else if (t.dst_bf16) {
         __nv_bfloat16* o = static_cast<__nv_bfloat16*>(t.O) + i + e;
@@ -383,7 +397,9 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
     const int rc = launch_ns_steps(ctx, w, cfg->steps, cfg->a, cfg->b, cfg->c, sc, p.split, st);
     if (rc != ABS_OK) return rc;
     const int cur = cfg->steps & 1;
-    ABS_CUDA_TRY(ctx, launch_dependent(dst_vec ? ns_finish_kernel<4> : ns_finish_kernel<1>, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur, p.split ? cur : 0,
+    auto finish = src.muon ? (dst_vec ? ns_finish_kernel<4, true> : ns_finish_kernel<1, true>)
+                           : (dst_vec ? ns_finish_kernel<4, false> : ns_finish_kernel<1, false>);
+    ABS_CUDA_TRY(ctx, launch_dependent(finish, tiles, dim3(kPassThreads), 0, st, src, dst, q0, w, cur, p.split ? cur : 0,
                                        1.0f / sc.sx[cfg->steps], tiles_c, static_cast<const unsigned*>(flag)));
   }
   return ABS_OK;
