@@ -23,6 +23,7 @@ namespace {
 constexpr int kWarpsS = 16;
 constexpr int kThreadsS = kWarpsS * 32;
 constexpr int kMaxCluster = 8;
+constexpr int kBatch = 2;            // groups of eight elements that a thread loads at a time
 
 struct SmallParams {
   NsSource s;
@@ -34,6 +35,7 @@ struct SmallParams {
   int steps;
   float eps, sx, inv_sx;
   long long timeout_cycles;
+  int vec_src, vec_dst;   // groups of eight are 16-byte aligned in global memory
   int drop;            // test hook: no product is issued, so the first wait must run out
   NsCoef coef[kNsMaxSteps][3];
 };
@@ -121,6 +123,83 @@ __device__ __forceinline__ void join8(const uint4 h, const uint4 l, float (&x)[8
   }
 }
 
+// n <= 8 consecutive elements of a matrix in global memory (zeros behind them); vec: 16-byte aligned.
+__device__ __forceinline__ void load8(const float* p, int n, bool vec, float (&v)[8]) {
+  if (vec && n == 8) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, bool vec, float (&v)[8]) {
+  if (vec && n == 8) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e]) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int n, bool vec, const float (&v)[8]) {
+  if (vec && n == 8) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = v[e];
+  }
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int n, bool vec, const float (&v)[8]) {
+  if (vec && n == 8) {
+    __nv_bfloat162 w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(w);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = __float2bfloat16_rn(v[e]);
+  }
+}
+// Eight 16-bit values to or from a stored matrix: a chunk of row o, or rows 8 g .. 8 g + 7 of column o (the first n).
+__device__ __forceinline__ void put8(uint32_t matrix, int R, bool tall, int o, int g, int n, const uint32_t (&v)[4]) {
+  if (!tall) {
+    sts128_s(matrix + chunk_at(R, o, g), v);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (e < n)
+      asm volatile("st.shared.b16 [%0], %1;" ::"r"(matrix + chunk_at(R, 8 * g + e, o >> 3) + 2u * static_cast<uint32_t>(o & 7)),
+                   "h"(static_cast<unsigned short>(e & 1 ? v[e >> 1] >> 16 : v[e >> 1]))
+                   : "memory");
+  }
+}
+__device__ __forceinline__ void get8(uint32_t matrix, int R, bool tall, int o, int g, uint32_t (&v)[4]) {
+  if (!tall) {
+    const uint4 a = lds128(matrix + chunk_at(R, o, g));
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {                                  // (rows up to the next multiple of eight are there)
+    unsigned short a, b;
+    const uint32_t at = 2u * static_cast<uint32_t>(o & 7);
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(a) : "r"(matrix + chunk_at(R, 8 * g + 2 * e, o >> 3) + at));
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(matrix + chunk_at(R, 8 * g + 2 * e + 1, o >> 3) + at));
+    v[e] = static_cast<uint32_t>(a) | (static_cast<uint32_t>(b) << 16);
+  }
+}
+
 __global__ void __launch_bounds__(kThreadsS, 1)
 ns_small_kernel(const __grid_constant__ SmallParams p) {
   extern __shared__ unsigned char smem_dyn[];
@@ -163,29 +242,64 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   const uint32_t tmem = tmem_slot;
 
   // ---- momentum update and norm, then X_0 ------------------------------------------------------------
-  // Elements of this CTA in the source's order: X[i][j] is row i, column j of U, or, where U is taller than
-  // wide, row j, column i; columns c0 .. c0 + wc - 1 of X.
+  // This CTA's part of U goes to X's place in groups of eight elements that are consecutive in U: of columns, or, where
+  // U is taller than wide, of rows of X.  (Element by element, at some 120 instructions each, the passes over the matrix
+  // took longer than two steps.)
   const bool tall = p.s.rows > p.s.cols;
-  const int inner = tall ? p.m : wc, total = p.m * wc;
-  const long long src = matrix_base(q, p.s.L, p.s.replica_stride, p.s.matrix_stride);
-  auto place = [&](int e, int& i, int& j) {
-    const int o = e / inner, k = e - o * inner;
-    i = tall ? k : o;
-    j = tall ? o : k;                                            // within the CTA's columns
-    return src + static_cast<long long>(tall ? c0 + j : i) * p.s.row_stride + (tall ? i : c0 + j);
-  };
-  double sum = 0.0;
-  for (int e = tid; e < total; e += kThreadsS) {
-    int i, j;
-    const long long at = place(e, i, j);
-    float u[1];
-    load_src<1>(p.s, at, u);
-    if (p.s.muon) {
-      const float b = fmaf(p.s.momentum, p.s.Buf[at], u[0]);
-      p.s.Buf[at] = b;
-      u[0] = p.s.nesterov ? fmaf(p.s.momentum, b, u[0]) : b;
+  const int groups = ((tall ? p.m : wc) + 7) / 8, lines = tall ? wc : p.m, units = groups * lines;
+  auto unit = [&](int u, int& o, int& g, int& n) {               // line, group of eight in it and elements of that
+    if (tall) {                                                  // lanes next to one another: columns of X
+      g = u / lines;
+      o = u - g * lines;
+      n = p.m - 8 * g;
+    } else {
+      o = u / groups;
+      g = u - o * groups;
+      n = wc - 8 * g;
     }
-    sum = fma(static_cast<double>(u[0]), static_cast<double>(u[0]), sum);
+    if (n > 8) n = 8;
+  };
+  auto in_matrix = [&](int o, int g, long long row_stride) {
+    return (tall ? c0 + o : o) * row_stride + (tall ? 0 : c0) + 8 * g;
+  };
+  const long long src = matrix_base(q, p.s.L, p.s.replica_stride, p.s.matrix_stride);
+  double sum = 0.0;
+  for (int u0 = tid; u0 < units; u0 += kBatch * kThreadsS) {
+    int o[kBatch], g[kBatch], n[kBatch];
+    float u[kBatch][8], b[kBatch][8];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      n[x] = 0;
+      if (u0 + x * kThreadsS >= units) continue;
+      unit(u0 + x * kThreadsS, o[x], g[x], n[x]);
+      const long long at = src + in_matrix(o[x], g[x], p.s.row_stride);
+      if (p.s.src_bf16) load8(static_cast<const __nv_bfloat16*>(p.s.G) + at, n[x], p.vec_src, u[x]);
+      else load8(static_cast<const float*>(p.s.G) + at, n[x], p.vec_src, u[x]);
+      if (p.s.muon) load8(p.s.Buf + at, n[x], p.vec_src, b[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      if (n[x] == 0) continue;
+      if (p.s.muon) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          b[x][e] = fmaf(p.s.momentum, b[x][e], u[x][e]);
+          u[x][e] = p.s.nesterov ? fmaf(p.s.momentum, b[x][e], u[x][e]) : b[x][e];
+        }
+        store8(p.s.Buf + src + in_matrix(o[x], g[x], p.s.row_stride), n[x], p.vec_src, b[x]);
+      }
+      uint32_t hi[4], lo[4];                                     // as it is for now: upper and lower halves of fp32
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma(static_cast<double>(u[x][e]), static_cast<double>(u[x][e]), sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t f = __float_as_uint(u[x][2 * e]), s2 = __float_as_uint(u[x][2 * e + 1]);
+        hi[e] = __byte_perm(f, s2, 0x7632);
+        lo[e] = __byte_perm(f, s2, 0x5410);
+      }
+      put8(xh, R, tall, o[x], g[x], n[x], hi);
+      put8(xl, R, tall, o[x], g[x], n[x], lo);
+    }
   }
   sum = warp_sum(sum);
   if (lane == 0) red[warp] = sum;
@@ -204,16 +318,19 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     sum = norm_sq;
   }
   const double scale = static_cast<double>(p.sx) / (sqrt(sum) + static_cast<double>(p.eps));
-  for (int e = tid; e < total; e += kThreadsS) {
-    int i, j;
-    const long long at = place(e, i, j);
-    float u[1];
-    load_update<1>(p.s, at, u);
-    const float v = static_cast<float>(u[0] * scale);
-    const __half h = __float2half_rn(v), l = __float2half_rn(v - __half2float(h));
-    const uint32_t o = chunk_at(R, i, j >> 3) + 2u * static_cast<uint32_t>(j & 7);
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(xh + o), "h"(__half_as_ushort(h)) : "memory");
-    asm volatile("st.shared.b16 [%0], %1;" ::"r"(xl + o), "h"(__half_as_ushort(l)) : "memory");
+  for (uint32_t o = tid * 16u; o < blocks * block_bytes; o += kThreadsS * 16u) {
+    const uint4 a = lds128(xh + o), b = lds128(xl + o);
+    const uint32_t hi[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = static_cast<float>(__uint_as_float((hi[e] << 16) | (lo[e] & 0xffffu)) * scale);
+      v[2 * e + 1] = static_cast<float>(__uint_as_float((hi[e] & 0xffff0000u) | (lo[e] >> 16)) * scale);
+    }
+    uint32_t h[4], l[4];
+    split8(v, h, l);
+    sts128_s(xh + o, h);
+    sts128_s(xl + o, l);
   }
 
   // ---- steps ---------------------------------------------------------------------------------------------
@@ -295,11 +412,19 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int k = 0; k < C; ++k) {
+        float4 a[kMaxCluster], b[kMaxCluster];                     // all under way before the first is used
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+          if (k >= C) continue;
           const uint32_t from = map_to_rank(at, static_cast<uint32_t>(k));
-          const float4 a = ld_cluster128(from), b = ld_cluster128(from + 16u);
-          v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-          v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+          a[k] = ld_cluster128(from);
+          b[k] = ld_cluster128(from + 16u);
+        }
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+          if (k >= C) continue;
+          v[0] += a[k].x; v[1] += a[k].y; v[2] += a[k].z; v[3] += a[k].w;
+          v[4] += b[k].x; v[5] += b[k].y; v[6] += b[k].z; v[7] += b[k].w;
         }
         uint32_t h[4], l[4];
         split8(v, h, l);
@@ -384,17 +509,34 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   }
   const float bad = failed ? __int_as_float(0x7fc00000) : 0.f;
   const long long dst = matrix_base(q, p.s.L, p.t.replica_stride, p.t.matrix_stride);
-  for (int e = tid; e < total; e += kThreadsS) {
-    const int o = e / inner, k = e - o * inner, i = tall ? k : o, j = tall ? o : k;
-    const uint32_t at = chunk_at(R, i, j >> 3) + 2u * static_cast<uint32_t>(j & 7);
-    unsigned short h, l;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(xh + at));
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(l) : "r"(xl + at));
-    const float v = (__half2float(__ushort_as_half(h)) + __half2float(__ushort_as_half(l))) * p.inv_sx + bad;
-    const long long to = dst + static_cast<long long>(tall ? c0 + j : i) * p.t.row_stride + (tall ? i : c0 + j);
-    if (p.s.muon) p.t.X[to] = fmaf(-p.t.step, v, p.t.decay * p.t.X[to]);
-    else if (p.t.dst_bf16) static_cast<__nv_bfloat16*>(p.t.O)[to] = __float2bfloat16_rn(v);
-    else static_cast<float*>(p.t.O)[to] = v;
+  for (int u0 = tid; u0 < units; u0 += kBatch * kThreadsS) {
+    int o[kBatch], g[kBatch], n[kBatch];
+    float x0[kBatch][8];
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      n[x] = 0;
+      if (u0 + x * kThreadsS >= units) continue;
+      unit(u0 + x * kThreadsS, o[x], g[x], n[x]);
+      if (p.s.muon) load8(p.t.X + dst + in_matrix(o[x], g[x], p.t.row_stride), n[x], p.vec_dst, x0[x]);
+    }
+#pragma unroll
+    for (int x = 0; x < kBatch; ++x) {
+      if (n[x] == 0) continue;
+      const long long at = dst + in_matrix(o[x], g[x], p.t.row_stride);
+      uint32_t h[4], l[4];
+      get8(xh, R, tall, o[x], g[x], h);
+      get8(xl, R, tall, o[x], g[x], l);
+      float v[8];
+      join8(make_uint4(h[0], h[1], h[2], h[3]), make_uint4(l[0], l[1], l[2], l[3]), v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = v[e] * p.inv_sx + bad;
+        if (p.s.muon) v[e] = fmaf(-p.t.step, v[e], p.t.decay * x0[x][e]);
+      }
+      if (p.s.muon) store8(p.t.X + at, n[x], p.vec_dst, v);
+      else if (p.t.dst_bf16) store8(static_cast<__nv_bfloat16*>(p.t.O) + at, n[x], p.vec_dst, v);
+      else store8(static_cast<float*>(p.t.O) + at, n[x], p.vec_dst, v);
+    }
   }
   if (C > 1) cluster_sync_s();                                   // a peer may still read this CTA's abort flag
 }
@@ -441,6 +583,12 @@ int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int coun
   p.m = s.rows < s.cols ? s.rows : s.cols;
   p.n = s.rows < s.cols ? s.cols : s.rows;
   p.R = plan.R; p.W = plan.W; p.C = plan.C;
+  auto aligned = [](const void* a, int es, long long rs, long long ms, long long ls) {
+    return ((reinterpret_cast<uintptr_t>(a) | static_cast<uintptr_t>(rs * es) | static_cast<uintptr_t>(ms * es) | static_cast<uintptr_t>(ls * es)) & 15u) == 0;
+  };
+  p.vec_src = aligned(s.G, s.src_bf16 ? 2 : 4, s.row_stride, s.matrix_stride, s.replica_stride) &&
+              aligned(s.Buf, 4, s.row_stride, s.matrix_stride, s.replica_stride);
+  p.vec_dst = aligned(s.muon ? static_cast<const void*>(t.X) : t.O, !s.muon && t.dst_bf16 ? 2 : 4, t.row_stride, t.matrix_stride, t.replica_stride);
   p.steps = steps;
   p.eps = eps;
   p.sx = sc.sx[0];
