@@ -43,7 +43,8 @@ struct SmallParams {
 // ---- PTX ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tcs_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcs_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_proxy_s() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_s() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_cluster_s() { asm volatile("fence.proxy.async.shared::cluster;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync_s() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -58,19 +59,21 @@ __device__ __forceinline__ void umma_s(uint32_t d, uint64_t a, uint64_t b, uint3
 __device__ __forceinline__ void umma_commit_s(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// Eight columns of this thread's lane from each of the two accumulators, added.
-__device__ __forceinline__ void tmem_ld8_sum(uint32_t main, uint32_t cross, float (&v)[8]) {
-  uint32_t r[16];
+// Sixteen columns of this thread's lane from each of the two accumulators, added.
+__device__ __forceinline__ void tmem_ld16_sum(uint32_t main, uint32_t cross, float (&v)[2][8]) {
+  uint32_t r[32];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(main), "r"(cross)
       : "memory");
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[e]) + __uint_as_float(r[8 + e]);
+  for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = __uint_as_float(r[e]) + __uint_as_float(r[16 + e]);
 }
 __device__ __forceinline__ void sts128_s(uint32_t addr, const uint32_t (&v)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
@@ -341,13 +344,29 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(block_bytes >> 4) << 16);
   const uint32_t cross = tmem + cross_off;
   uint32_t phase = 0;
-  // hi hi into the main accumulator; lo hi and hi lo (2^-11 of it) into one of their own
-  auto product16 = [&](uint32_t a_h, uint32_t a_l, uint64_t desc_b, uint32_t b_h, uint32_t b_l, uint32_t idesc, bool first) {
-    const uint64_t dah = desc_k | ((a_h & 0x3ffffu) >> 4), dal = desc_k | ((a_l & 0x3ffffu) >> 4);
-    const uint64_t dbh = desc_b | ((b_h & 0x3ffffu) >> 4), dbl = desc_b | ((b_l & 0x3ffffu) >> 4);
-    umma_s(tmem, dah, dbh, idesc, first ? 0u : 1u);
-    umma_s(cross, dal, dbh, idesc, first ? 0u : 1u);
-    umma_s(cross, dah, dbl, idesc, 1u);
+  // A product over K = 16 steps, hi hi into the main accumulator, lo hi and hi lo (2^-11 of it) into one of their own.
+  // First operand: K-major, `second` + what advances by step_b bytes per 16 of K within a block of 64 columns of
+  // the first operand, and block_b from block to block.  One thread issues them all, so its instructions count: the
+  // descriptors of a block are made once.
+  auto products = [&](uint32_t a_h, uint32_t a_l, uint64_t desc_b, uint32_t b_h, uint32_t b_l, uint32_t step_b, uint32_t block_b,
+                      uint32_t idesc, int K) {
+    uint64_t dah = desc_k | ((a_h & 0x3ffffu) >> 4), dal = desc_k | ((a_l & 0x3ffffu) >> 4);
+    uint64_t dbh = desc_b | ((b_h & 0x3ffffu) >> 4), dbl = desc_b | ((b_l & 0x3ffffu) >> 4);
+    for (int k0 = 0; k0 < K; k0 += 64) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k0 + 16 * k >= K) break;
+        const uint64_t sa = 2u * k, sb = static_cast<uint64_t>(step_b >> 4) * k;
+        umma_s(tmem, dah + sa, dbh + sb, idesc, (k0 | k) ? 1u : 0u);
+        umma_s(cross, dal + sa, dbh + sb, idesc, (k0 | k) ? 1u : 0u);
+        umma_s(cross, dah + sa, dbl + sb, idesc, 1u);
+      }
+      dah += block_bytes >> 4;
+      dal += block_bytes >> 4;
+      dbh += block_b >> 4;
+      dbl += block_b >> 4;
+    }
+    umma_commit_s(bar);
   };
   auto wait_products = [&]() {
     mbar_wait(bar, phase & 1u, abort_flag, p.timeout_cycles);
@@ -373,21 +392,20 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
       const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
-      for (int k = 0; k < Nw; k += 16) {
-        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
-        product16(xh + o, xl + o, desc_k, xh + o, xl + o, idesc, k == 0);
-      }
-      umma_commit_s(bar);
+      products(xh, xl, desc_k, xh, xl, 32u, block_bytes, idesc, Nw);
     }
     wait_products();
     const NsCoef gram = p.coef[step][0], poly = p.coef[step][1], upd = p.coef[step][2];
     if (live) {
-      for (int ch = group; ch < Nm / 8; ch += 4) {
-        float v[8];
-        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+      for (int ch2 = 2 * group; ch2 < Nm / 8; ch2 += 8) {
+        float w[2][8];
+        tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= gram.acc;
-        if (row < R) {
+        for (int x = 0; x < 2; ++x) {
+          const int ch = ch2 + x;
+          float (&v)[8] = w[x];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= gram.acc;
           if (C > 1) {
             if (row < p.m) {
               const uint32_t at = part + static_cast<uint32_t>(row) * pitch + 32u * ch;
@@ -396,7 +414,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
               sts128_s(at, lo);
               sts128_s(at + 16u, hi);
             }
-          } else {
+          } else if (row < R) {
             uint32_t h[4], l[4];
             split8(v, h, l);
             sts128_s(ah + chunk_at(R, row, ch), h);
@@ -407,8 +425,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     }
     if (C > 1) {
       cluster_sync_s();
-      const int per_row = Nm / 8;
-      for (int u = rank + C * tid; u < p.m * per_row; u += C * kThreadsS) {
+      const int per_row = Nm / 8, all = p.m * per_row, share = (all + C - 1) / C, stop = (rank + 1) * share < all ? (rank + 1) * share : all;
+      for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10 us, interleaved XX
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -433,7 +451,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
           st_cluster128(map_to_rank(al + chunk_at(R, r, ch), static_cast<uint32_t>(k)), l);
         }
       }
-      fence_proxy_s();
+      fence_proxy_cluster_s();
       cluster_sync_s();
     }
     // B = b A + c A A, in the place of A
@@ -441,26 +459,26 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
       const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
-      for (int k = 0; k < Nm; k += 16) {
-        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
-        product16(ah + o, al + o, desc_k, ah + o, al + o, idesc, k == 0);
-      }
-      umma_commit_s(bar);
+      products(ah, al, desc_k, ah, al, 32u, block_bytes, idesc, Nm);
     }
     wait_products();
     if (live) {
-      for (int ch = group; ch < Nm / 8; ch += 4) {
-        float v[8], x[8];
-        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+      for (int ch2 = 2 * group; ch2 < Nm / 8; ch2 += 8) {
+        float w[2][8];
+        tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
         if (row < R) {
-          const uint32_t o = chunk_at(R, row, ch);
-          join8(lds128(ah + o), lds128(al + o), x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = row < p.m ? fmaf(poly.acc, v[e], poly.in * x[e]) : 0.f;
-          uint32_t h[4], l[4];
-          split8(v, h, l);
-          sts128_s(ah + o, h);
-          sts128_s(al + o, l);
+          for (int q2 = 0; q2 < 2; ++q2) {
+            const uint32_t o = chunk_at(R, row, ch2 + q2);
+            float (&v)[8] = w[q2], x[8];
+            join8(lds128(ah + o), lds128(al + o), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = row < p.m ? fmaf(poly.acc, v[e], poly.in * x[e]) : 0.f;
+            uint32_t h[4], l[4];
+            split8(v, h, l);
+            sts128_s(ah + o, h);
+            sts128_s(al + o, l);
+          }
         }
       }
     }
@@ -469,27 +487,26 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
       const uint32_t idesc = idesc0 | (1u << 16) | (static_cast<uint32_t>(Nw >> 3) << 17);
-      for (int k = 0; k < Nm; k += 16) {
-        const uint32_t o = static_cast<uint32_t>(k >> 6) * block_bytes + static_cast<uint32_t>(k & 63) * 2u;
-        const uint32_t x = static_cast<uint32_t>(k) * 128u;      // 16 rows
-        product16(ah + o, al + o, desc_mn, xh + x, xl + x, idesc, k == 0);
-      }
-      umma_commit_s(bar);
+      products(ah, al, desc_mn, xh, xl, 16u * 128u, 64u * 128u, idesc, Nm);      // (16 rows)
     }
     wait_products();
     if (live) {
-      for (int ch = group; ch < Nw / 8; ch += 4) {
-        float v[8], x[8];
-        tmem_ld8_sum(tmem + t_row + 8u * ch, cross + t_row + 8u * ch, v);
+      for (int ch2 = 2 * group; ch2 < Nw / 8; ch2 += 8) {
+        float w[2][8];
+        tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
         if (row < p.m) {
-          const uint32_t o = chunk_at(R, row, ch);
-          join8(lds128(xh + o), lds128(xl + o), x);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = fmaf(upd.acc, v[e], upd.in * x[e]);
-          uint32_t h[4], l[4];
-          split8(v, h, l);
-          sts128_s(xh + o, h);
-          sts128_s(xl + o, l);
+          for (int q2 = 0; q2 < 2; ++q2) {
+            const uint32_t o = chunk_at(R, row, ch2 + q2);
+            float (&v)[8] = w[q2], x[8];
+            join8(lds128(xh + o), lds128(xl + o), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(upd.acc, v[e], upd.in * x[e]);
+            uint32_t h[4], l[4];
+            split8(v, h, l);
+            sts128_s(xh + o, h);
+            sts128_s(xl + o, l);
+          }
         }
       }
     }
