@@ -126,6 +126,28 @@ __device__ __forceinline__ void join8(const uint4 h, const uint4 l, float (&x)[8
   }
 }
 
+// y <- in y + acc w for two chunks of a row; both are loaded before the first is used (a chunk alone takes
+// 260 clocks from its load to its store).
+__device__ __forceinline__ void apply16(uint32_t yh, uint32_t yl, int R, int row, int ch, float acc, float in, float (&w)[2][8]) {
+  const uint32_t o[2] = {chunk_at(R, row, ch), chunk_at(R, row, ch + 1)};
+  const uint4 h0 = lds128(yh + o[0]), l0 = lds128(yl + o[0]), h1 = lds128(yh + o[1]), l1 = lds128(yl + o[1]);
+  float x[2][8];
+  join8(h0, l0, x[0]);
+  join8(h1, l1, x[1]);
+  uint32_t h[2][4], l[2][4];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[k][e] = fmaf(acc, w[k][e], in * x[k][e]);
+    split8(w[k], h[k], l[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    sts128_s(yh + o[k], h[k]);
+    sts128_s(yl + o[k], l[k]);
+  }
+}
+
 // n <= 8 consecutive elements of a matrix in global memory (zeros behind them); vec: 16-byte aligned.
 __device__ __forceinline__ void load8(const float* p, int n, bool vec, float (&v)[8]) {
   if (vec && n == 8) {
@@ -267,6 +289,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   };
   const long long src = matrix_base(q, p.s.L, p.s.replica_stride, p.s.matrix_stride);
   double sum = 0.0;
+#pragma unroll 1
   for (int u0 = tid; u0 < units; u0 += kBatch * kThreadsS) {
     int o[kBatch], g[kBatch], n[kBatch];
     float u[kBatch][8], b[kBatch][8];
@@ -321,6 +344,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     sum = norm_sq;
   }
   const double scale = static_cast<double>(p.sx) / (sqrt(sum) + static_cast<double>(p.eps));
+#pragma unroll 1
   for (uint32_t o = tid * 16u; o < blocks * block_bytes; o += kThreadsS * 16u) {
     const uint4 a = lds128(xh + o), b = lds128(xl + o);
     const uint32_t hi[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
@@ -352,6 +376,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
                       uint32_t idesc, int K) {
     uint64_t dah = desc_k | ((a_h & 0x3ffffu) >> 4), dal = desc_k | ((a_l & 0x3ffffu) >> 4);
     uint64_t dbh = desc_b | ((b_h & 0x3ffffu) >> 4), dbl = desc_b | ((b_l & 0x3ffffu) >> 4);
+#pragma unroll 1
     for (int k0 = 0; k0 < K; k0 += 64) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -397,6 +422,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     wait_products();
     const NsCoef gram = p.coef[step][0], poly = p.coef[step][1], upd = p.coef[step][2];
     if (live) {
+#pragma unroll 1
       for (int ch2 = 2 * group; ch2 < Nm / 8; ch2 += 8) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
@@ -426,6 +452,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (C > 1) {
       cluster_sync_s();
       const int per_row = Nm / 8, all = p.m * per_row, share = (all + C - 1) / C, stop = (rank + 1) * share < all ? (rank + 1) * share : all;
+#pragma unroll 1
       for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10 us, interleaved XX
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
@@ -463,22 +490,12 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     }
     wait_products();
     if (live) {
+#pragma unroll 1
       for (int ch2 = 2 * group; ch2 < Nm / 8; ch2 += 8) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
         if (row < R) {
-#pragma unroll
-          for (int q2 = 0; q2 < 2; ++q2) {
-            const uint32_t o = chunk_at(R, row, ch2 + q2);
-            float (&v)[8] = w[q2], x[8];
-            join8(lds128(ah + o), lds128(al + o), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = row < p.m ? fmaf(poly.acc, v[e], poly.in * x[e]) : 0.f;
-            uint32_t h[4], l[4];
-            split8(v, h, l);
-            sts128_s(ah + o, h);
-            sts128_s(al + o, l);
-          }
+          apply16(ah, al, R, row, ch2, row < p.m ? poly.acc : 0.f, row < p.m ? poly.in : 0.f, w);
         }
       }
     }
@@ -491,22 +508,12 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     }
     wait_products();
     if (live) {
+#pragma unroll 1
       for (int ch2 = 2 * group; ch2 < Nw / 8; ch2 += 8) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
         if (row < p.m) {
-#pragma unroll
-          for (int q2 = 0; q2 < 2; ++q2) {
-            const uint32_t o = chunk_at(R, row, ch2 + q2);
-            float (&v)[8] = w[q2], x[8];
-            join8(lds128(xh + o), lds128(xl + o), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = fmaf(upd.acc, v[e], upd.in * x[e]);
-            uint32_t h[4], l[4];
-            split8(v, h, l);
-            sts128_s(xh + o, h);
-            sts128_s(xl + o, l);
-          }
+          apply16(xh, xl, R, row, ch2, upd.acc, upd.in, w);
         }
       }
     }
@@ -526,6 +533,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   }
   const float bad = failed ? __int_as_float(0x7fc00000) : 0.f;
   const long long dst = matrix_base(q, p.s.L, p.t.replica_stride, p.t.matrix_stride);
+#pragma unroll 1
   for (int u0 = tid; u0 < units; u0 += kBatch * kThreadsS) {
     int o[kBatch], g[kBatch], n[kBatch];
     float x0[kBatch][8];
