@@ -9,11 +9,13 @@
 //                     adds its share of the elements, in rank order, and sends it to all
 //   B = b A + c A A   every CTA for itself, in the place of A
 //   X <- a X + B X    every CTA its own columns; X is MN-major here, in the same memory
-// The rows of X and A are padded with zeros to 64 or 128.  All waits are bounded; when one runs out the
+// The rows of X are padded with zeros to 64 or 128, A has 128 rows.  All waits are bounded; when one runs out the
 // results of the matrix are NaN.
 //
-// Measured (B200): 4 matrices of 64 x 192 and 8 of 10 x 1024, 5 steps, against the launches of the general
-// path (norm, split, all steps, finish): see the table of cases in the design notes of the product.
+// Measured (B200): a step takes 1.8 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 4.3 for 8 of 10 x 1024 (of which 0.6 the
+// two cluster barriers and 0.6 the exchange), 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is
+// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 30 us;
+// with the launches of the general path (norm, split, steps, finish) 101 and 147.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
 
@@ -75,6 +77,18 @@ __device__ __forceinline__ void tmem_ld16_sum(uint32_t main, uint32_t cross, flo
 #pragma unroll
   for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = __uint_as_float(r[e]) + __uint_as_float(r[16 + e]);
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[2][8]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = __uint_as_float(r[e]);
+}
 __device__ __forceinline__ void sts128_s(uint32_t addr, const uint32_t (&v)[4]) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
@@ -99,10 +113,10 @@ __device__ __forceinline__ unsigned ld_cluster_u32(uint32_t addr) {
 }
 
 // Byte offset of the 16-byte chunk that holds columns 8 ch .. 8 ch + 7 of row r in a matrix stored as blocks of
-// [R rows][64 columns] with the 128-byte swizzle.  The same memory is K-major (columns are k: 8-row groups 1024
-// bytes apart) and MN-major (rows are k: blocks of 64 columns R * 128 bytes apart).
-__device__ __forceinline__ uint32_t chunk_at(int R, int r, int ch) {
-  return static_cast<uint32_t>(ch >> 3) * (static_cast<uint32_t>(R) * 128u) + static_cast<uint32_t>(r) * 128u +
+// 64 columns, `block` bytes apart, with the 128-byte swizzle.  The same memory is K-major (columns are k: 8-row
+// groups 1024 bytes apart) and MN-major (rows are k).
+__device__ __forceinline__ uint32_t chunk_at(uint32_t block, int r, int ch) {
+  return static_cast<uint32_t>(ch >> 3) * block + static_cast<uint32_t>(r) * 128u +
          ((static_cast<uint32_t>(ch & 7) ^ static_cast<uint32_t>(r & 7)) << 4);
 }
 __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&h)[4], uint32_t (&l)[4]) {
@@ -126,10 +140,11 @@ __device__ __forceinline__ void join8(const uint4 h, const uint4 l, float (&x)[8
   }
 }
 
-// y <- in y + acc w for two chunks of a row; both are loaded before the first is used (a chunk alone takes
-// 260 clocks from its load to its store).
-__device__ __forceinline__ void apply16(uint32_t yh, uint32_t yl, int R, int row, int ch, float acc, float in, float (&w)[2][8]) {
-  const uint32_t o[2] = {chunk_at(R, row, ch), chunk_at(R, row, ch + 1)};
+// y <- in y + acc w for two chunks of a row, stored to `copies` rows copy_rows apart; both chunks are loaded before the
+// first is used (one alone takes 260 clocks from its load to its store).
+__device__ __forceinline__ void apply16(uint32_t yh, uint32_t yl, uint32_t block, int row, int ch, float acc, float in,
+                                        float (&w)[2][8], int copies, int copy_rows) {
+  const uint32_t o[2] = {chunk_at(block, row, ch), chunk_at(block, row, ch + 1)};
   const uint4 h0 = lds128(yh + o[0]), l0 = lds128(yl + o[0]), h1 = lds128(yh + o[1]), l1 = lds128(yl + o[1]);
   float x[2][8];
   join8(h0, l0, x[0]);
@@ -141,10 +156,14 @@ __device__ __forceinline__ void apply16(uint32_t yh, uint32_t yl, int R, int row
     for (int e = 0; e < 8; ++e) w[k][e] = fmaf(acc, w[k][e], in * x[k][e]);
     split8(w[k], h[k], l[k]);
   }
+#pragma unroll 1
+  for (int c = 0; c < copies; ++c) {                             // (the swizzle is the same: copy_rows is a multiple of 8)
+    const uint32_t to = static_cast<uint32_t>(c * copy_rows) * 128u;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    sts128_s(yh + o[k], h[k]);
-    sts128_s(yl + o[k], l[k]);
+    for (int k = 0; k < 2; ++k) {
+      sts128_s(yh + o[k] + to, h[k]);
+      sts128_s(yl + o[k] + to, l[k]);
+    }
   }
 }
 
@@ -196,22 +215,22 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, int n, bool vec, const 
   }
 }
 // Eight 16-bit values to or from a stored matrix: a chunk of row o, or rows 8 g .. 8 g + 7 of column o (the first n).
-__device__ __forceinline__ void put8(uint32_t matrix, int R, bool tall, int o, int g, int n, const uint32_t (&v)[4]) {
+__device__ __forceinline__ void put8(uint32_t matrix, uint32_t block, bool tall, int o, int g, int n, const uint32_t (&v)[4]) {
   if (!tall) {
-    sts128_s(matrix + chunk_at(R, o, g), v);
+    sts128_s(matrix + chunk_at(block, o, g), v);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (e < n)
-      asm volatile("st.shared.b16 [%0], %1;" ::"r"(matrix + chunk_at(R, 8 * g + e, o >> 3) + 2u * static_cast<uint32_t>(o & 7)),
+      asm volatile("st.shared.b16 [%0], %1;" ::"r"(matrix + chunk_at(block, 8 * g + e, o >> 3) + 2u * static_cast<uint32_t>(o & 7)),
                    "h"(static_cast<unsigned short>(e & 1 ? v[e >> 1] >> 16 : v[e >> 1]))
                    : "memory");
   }
 }
-__device__ __forceinline__ void get8(uint32_t matrix, int R, bool tall, int o, int g, uint32_t (&v)[4]) {
+__device__ __forceinline__ void get8(uint32_t matrix, uint32_t block, bool tall, int o, int g, uint32_t (&v)[4]) {
   if (!tall) {
-    const uint4 a = lds128(matrix + chunk_at(R, o, g));
+    const uint4 a = lds128(matrix + chunk_at(block, o, g));
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
     return;
   }
@@ -219,8 +238,8 @@ __device__ __forceinline__ void get8(uint32_t matrix, int R, bool tall, int o, i
   for (int e = 0; e < 4; ++e) {                                  // (rows up to the next multiple of eight are there)
     unsigned short a, b;
     const uint32_t at = 2u * static_cast<uint32_t>(o & 7);
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(a) : "r"(matrix + chunk_at(R, 8 * g + 2 * e, o >> 3) + at));
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(matrix + chunk_at(R, 8 * g + 2 * e + 1, o >> 3) + at));
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(a) : "r"(matrix + chunk_at(block, 8 * g + 2 * e, o >> 3) + at));
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(b) : "r"(matrix + chunk_at(block, 8 * g + 2 * e + 1, o >> 3) + at));
     v[e] = static_cast<uint32_t>(a) | (static_cast<uint32_t>(b) << 16);
   }
 }
@@ -240,8 +259,10 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   const int blocks = (p.W + 63) / 64, mblocks = (p.m + 63) / 64;
   const uint32_t block_bytes = static_cast<uint32_t>(R) * 128u;
   const uint32_t raw = smem_u32(smem_dyn), base = (raw + 1023u) & ~1023u;
-  const uint32_t xh = base, xl = xh + blocks * block_bytes, ah = xl + blocks * block_bytes, al = ah + mblocks * block_bytes;
-  const uint32_t part = al + mblocks * block_bytes;                              // partial sums [m][Nm + 4] fp32 (C > 1)
+  // X: a block's values, its remainders, the next block's values, ...; A: values, remainders
+  const uint32_t x_block = 2u * block_bytes, a_block = 128u * 128u;
+  const uint32_t xh = base, xl = xh + block_bytes, ah = xh + blocks * x_block, al = ah + mblocks * a_block;
+  const uint32_t part = al + mblocks * a_block;                              // partial sums [m][Nm + 4] fp32 (C > 1)
   const uint32_t pitch = static_cast<uint32_t>(Nm + 4) * 4u;
   volatile unsigned* abort_flag = &abort_mem;
   const uint32_t bar = smem_u32(&bar_mem);
@@ -257,7 +278,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   // zero X and A (the pad rows and columns stay zero)
-  for (uint32_t o = tid * 16u; o < 2u * (blocks + mblocks) * block_bytes; o += kThreadsS * 16u) {
+  for (uint32_t o = tid * 16u; o < blocks * x_block + 2u * mblocks * a_block; o += kThreadsS * 16u) {
     const uint32_t z[4] = {0u, 0u, 0u, 0u};
     sts128_s(xh + o, z);
   }
@@ -323,8 +344,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         hi[e] = __byte_perm(f, s2, 0x7632);
         lo[e] = __byte_perm(f, s2, 0x5410);
       }
-      put8(xh, R, tall, o[x], g[x], n[x], hi);
-      put8(xl, R, tall, o[x], g[x], n[x], lo);
+      put8(xh, x_block, tall, o[x], g[x], n[x], hi);
+      put8(xl, x_block, tall, o[x], g[x], n[x], lo);
     }
   }
   sum = warp_sum(sum);
@@ -345,7 +366,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   }
   const double scale = static_cast<double>(p.sx) / (sqrt(sum) + static_cast<double>(p.eps));
 #pragma unroll 1
-  for (uint32_t o = tid * 16u; o < blocks * block_bytes; o += kThreadsS * 16u) {
+  for (uint32_t k = tid * 16u; k < blocks * block_bytes; k += kThreadsS * 16u) {
+    const uint32_t o = k + (k & ~(block_bytes - 1u));            // blocks of values are x_block apart
     const uint4 a = lds128(xh + o), b = lds128(xl + o);
     const uint32_t hi[4] = {a.x, a.y, a.z, a.w}, lo[4] = {b.x, b.y, b.z, b.w};
     float v[8];
@@ -365,17 +387,18 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   // descriptors: 128-byte swizzle, 8-row groups 1024 bytes apart, MN-major blocks of 64 columns block_bytes apart
   const uint32_t idesc0 = (1u << 4) | (8u << 24);
   const uint64_t desc_k = (1ull << 46) | (64ull << 32) | (2ull << 61) | (1ull << 16);
-  const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(block_bytes >> 4) << 16);
+  const uint64_t desc_mn = (1ull << 46) | (64ull << 32) | (2ull << 61) | (static_cast<uint64_t>(x_block >> 4) << 16);
   const uint32_t cross = tmem + cross_off;
   uint32_t phase = 0;
-  // A product over K = 16 steps, hi hi into the main accumulator, lo hi and hi lo (2^-11 of it) into one of their own.
-  // First operand: K-major, `second` + what advances by step_b bytes per 16 of K within a block of 64 columns of
-  // the first operand, and block_b from block to block.  One thread issues them all, so its instructions count: the
-  // descriptors of a block are made once.
-  auto products = [&](uint32_t a_h, uint32_t a_l, uint64_t desc_b, uint32_t b_h, uint32_t b_l, uint32_t step_b, uint32_t block_b,
-                      uint32_t idesc, int K) {
-    uint64_t dah = desc_k | ((a_h & 0x3ffffu) >> 4), dal = desc_k | ((a_l & 0x3ffffu) >> 4);
-    uint64_t dbh = desc_b | ((b_h & 0x3ffffu) >> 4), dbl = desc_b | ((b_l & 0x3ffffu) >> 4);
+  // The products of split operands over K: hi hi into the main accumulator, lo hi and hi lo (2^-11 of it) into one of
+  // their own.  `first` and `second` (its descriptor: desc_b) are the addresses of the values, remainders are
+  // first_l and second_l bytes behind.  16 of K are 32 bytes of the first operand and step_b bytes of the second; blocks of
+  // 64 of K are first_block and second_block bytes apart.  One thread issues them all, so its
+  // instructions count: the descriptors of a block are made once.
+  auto products = [&](uint32_t first, uint32_t first_l, uint32_t first_block, uint64_t desc_b, uint32_t second, uint32_t second_l,
+                      uint32_t step_b, uint32_t second_block, uint32_t idesc, int K) {
+    uint64_t dah = desc_k | ((first & 0x3ffffu) >> 4), dal = dah + (first_l >> 4);
+    uint64_t dbh = desc_b | ((second & 0x3ffffu) >> 4), dbl = dbh + (second_l >> 4);
 #pragma unroll 1
     for (int k0 = 0; k0 < K; k0 += 64) {
 #pragma unroll
@@ -386,10 +409,29 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         umma_s(cross, dal + sa, dbh + sb, idesc, (k0 | k) ? 1u : 0u);
         umma_s(cross, dah + sa, dbl + sb, idesc, 1u);
       }
-      dah += block_bytes >> 4;
-      dal += block_bytes >> 4;
-      dbh += block_b >> 4;
-      dbl += block_b >> 4;
+      dah += first_block >> 4;
+      dal += first_block >> 4;
+      dbh += second_block >> 4;
+      dbl += second_block >> 4;
+    }
+    umma_commit_s(bar);
+  };
+  // X X' where X's remainders lie 64 rows behind its values: hi hi and hi lo are one product of twice the width.  One of up
+  // to 128 columns costs 61 clocks (what the first operand's 128 rows take to fetch), so two of
+  // them are a third faster than three: 10 x 1024 on 4 CTAs 2200 clocks, 2950.
+  auto gram_products = [&](uint32_t idesc) {
+    const uint32_t wide = idesc + (64u >> 3 << 17);
+    uint64_t dh = desc_k | ((xh & 0x3ffffu) >> 4), dl = dh + (block_bytes >> 4);
+#pragma unroll 1
+    for (int k0 = 0; k0 < Nw; k0 += 64) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k0 + 16 * k >= Nw) break;
+        umma_s(tmem, dh + 2u * k, dh + 2u * k, wide, (k0 | k) ? 1u : 0u);
+        umma_s(cross, dl + 2u * k, dh + 2u * k, idesc, (k0 | k) ? 1u : 0u);
+      }
+      dh += x_block >> 4;
+      dl += x_block >> 4;
     }
     umma_commit_s(bar);
   };
@@ -410,6 +452,12 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   const int row = q4 * 32 + lane;
   const uint32_t t_row = static_cast<uint32_t>(q4 * 32) << 16;
   const bool live = q4 * 32 < p.m;                               // (whole warps)
+  // Up to 64 rows B's rows are stored two or four times, so that all 128 lanes of the accumulator hold
+  // B X and every warp (its lanes are the rows q4 * 32 ...) has columns to bring back: 10 x 1024, 256 columns a CTA, 3900
+  // clocks with one copy, 1250 with four.
+  const int copies = p.m <= 32 ? 4 : p.m <= 64 ? 2 : 1, copy_rows = 128 / copies, quarters = 4 / copies;
+  const int x_row = q4 % quarters * 32 + lane, x_share = q4 / quarters * 4 + group;
+  const bool joined = R == 64;
 
   for (int step = 0; step < p.steps; ++step) {
     // A = X X'
@@ -417,7 +465,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
       const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
-      products(xh, xl, desc_k, xh, xl, 32u, block_bytes, idesc, Nw);
+      if (joined) gram_products(idesc);
+      else products(xh, block_bytes, x_block, desc_k, xh, block_bytes, 32u, x_block, idesc, Nw);
     }
     wait_products();
     const NsCoef gram = p.coef[step][0], poly = p.coef[step][1], upd = p.coef[step][2];
@@ -426,6 +475,12 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
       for (int ch2 = 2 * group; ch2 < Nm / 8; ch2 += 8) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
+        if (joined) {
+          float z[2][8];
+          tmem_ld16(tmem + 64u + t_row + 8u * ch2, z);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e >> 3][e & 7] += z[e >> 3][e & 7];
+        }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int ch = ch2 + x;
@@ -443,8 +498,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
           } else if (row < R) {
             uint32_t h[4], l[4];
             split8(v, h, l);
-            sts128_s(ah + chunk_at(R, row, ch), h);
-            sts128_s(al + chunk_at(R, row, ch), l);
+            sts128_s(ah + chunk_at(a_block, row, ch), h);
+            sts128_s(al + chunk_at(a_block, row, ch), l);
           }
         }
       }
@@ -453,7 +508,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
       cluster_sync_s();
       const int per_row = Nm / 8, all = p.m * per_row, share = (all + C - 1) / C, stop = (rank + 1) * share < all ? (rank + 1) * share : all;
 #pragma unroll 1
-      for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10 us, interleaved XX
+      for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10000 clocks, interleaved 19000
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -474,8 +529,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         uint32_t h[4], l[4];
         split8(v, h, l);
         for (int k = 0; k < C; ++k) {
-          st_cluster128(map_to_rank(ah + chunk_at(R, r, ch), static_cast<uint32_t>(k)), h);
-          st_cluster128(map_to_rank(al + chunk_at(R, r, ch), static_cast<uint32_t>(k)), l);
+          st_cluster128(map_to_rank(ah + chunk_at(a_block, r, ch), static_cast<uint32_t>(k)), h);
+          st_cluster128(map_to_rank(al + chunk_at(a_block, r, ch), static_cast<uint32_t>(k)), l);
         }
       }
       fence_proxy_cluster_s();
@@ -485,8 +540,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     before_products();
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
-      const uint32_t idesc = idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17);
-      products(ah, al, desc_k, ah, al, 32u, block_bytes, idesc, Nm);
+      products(ah, al - ah, a_block, desc_k, ah, al - ah, 32u, a_block, idesc0 | (static_cast<uint32_t>(Nm >> 3) << 17), Nm);
     }
     wait_products();
     if (live) {
@@ -495,7 +549,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
         if (row < R) {
-          apply16(ah, al, R, row, ch2, row < p.m ? poly.acc : 0.f, row < p.m ? poly.in : 0.f, w);
+          apply16(ah, al, a_block, row, ch2, row < p.m ? poly.acc : 0.f, row < p.m ? poly.in : 0.f, w, copies, copy_rows);
         }
       }
     }
@@ -504,17 +558,15 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     if (tid == 0 && !p.drop) {
       fence_proxy_s();
       const uint32_t idesc = idesc0 | (1u << 16) | (static_cast<uint32_t>(Nw >> 3) << 17);
-      products(ah, al, desc_mn, xh, xl, 16u * 128u, 64u * 128u, idesc, Nm);      // (16 rows)
+      products(ah, al - ah, a_block, desc_mn, xh, block_bytes, 16u * 128u, 64u * 128u, idesc, Nm);      // (16 rows)
     }
     wait_products();
-    if (live) {
+    if (q4 % quarters * 32 < p.m) {
 #pragma unroll 1
-      for (int ch2 = 2 * group; ch2 < Nw / 8; ch2 += 8) {
+      for (int ch2 = 2 * x_share; ch2 < Nw / 8; ch2 += 8 * copies) {
         float w[2][8];
         tmem_ld16_sum(tmem + t_row + 8u * ch2, cross + t_row + 8u * ch2, w);
-        if (row < p.m) {
-          apply16(xh, xl, R, row, ch2, upd.acc, upd.in, w);
-        }
+        if (x_row < p.m) apply16(xh, xl, x_block, x_row, ch2, upd.acc, upd.in, w, 1, 0);
       }
     }
   }
@@ -549,8 +601,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
       if (n[x] == 0) continue;
       const long long at = dst + in_matrix(o[x], g[x], p.t.row_stride);
       uint32_t h[4], l[4];
-      get8(xh, R, tall, o[x], g[x], h);
-      get8(xl, R, tall, o[x], g[x], l);
+      get8(xh, x_block, tall, o[x], g[x], h);
+      get8(xl, x_block, tall, o[x], g[x], l);
       float v[8];
       join8(make_uint4(h[0], h[1], h[2], h[3]), make_uint4(l[0], l[1], l[2], l[3]), v);
 #pragma unroll
@@ -583,8 +635,8 @@ bool plan_small(long long rows, long long cols, SmallPlan* out) {
   p.W = static_cast<int>(((n + C - 1) / C + 15) / 16 * 16);
   const int Nm = (m + 15) & ~15;
   const size_t block = static_cast<size_t>(p.R) * 128;
-  // with 64 rows the products read 128: what lies behind the last block has to be shared memory too
-  p.smem = 1024 + 2 * ((p.W + 63) / 64 + (m + 63) / 64) * block + (p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0) + 8192;
+  // with 64 rows the products read 128 of X: behind the last block lies A
+  p.smem = 1024 + 2 * ((p.W + 63) / 64 * block + (m + 63) / 64 * 16384) + (p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0);
   // One CTA per SM: two of them could want more tensor memory than there is, and a CTA that waits for it while
   // its cluster waits for the CTA would wait for good.
   if (p.smem < 120 * 1024) p.smem = 120 * 1024;
