@@ -82,6 +82,72 @@ def test_shapes(ctx, count, m, n, precision, tol):
     check(orthogonalise(ctx, G, precision=precision), ref_ns(G), tol)
 
 
+@pytest.fixture
+def tiles(ctx):
+    """Forces 128 x 128 tiles of single CTAs (1) or 256 x 256 tiles of pairs (2)."""
+    yield lambda kind: ctx.set_tuning("ns_pair_tiles", kind)
+    ctx.set_tuning("ns_pair_tiles", 0)
+
+
+# sides just over and under the tiles' (a last block of 1, 2, 127 or 255 rows), far more tiles than CTAs
+TILED = [(1, 129, 129), (2, 255, 257), (1, 257, 130), (3, 256, 256), (2, 383, 640), (1, 513, 2000), (1, 1500, 1100), (12, 770, 768),
+         (30, 512, 300), (1, 2304, 2300)]
+
+
+@pytest.mark.parametrize("kind", [1, 2])
+@pytest.mark.parametrize("count,m,n", TILED)
+def test_both_tile_shapes(ctx, tiles, count, m, n, kind):
+    tiles(kind)
+    G = matrices(21, count, m, n, scale=1e-2)
+    check(orthogonalise(ctx, G), ref_ns(G), 4e-3)
+
+
+@pytest.mark.parametrize("kind", [1, 2])
+def test_both_tile_shapes_repeat_their_bits_and_end_when_a_wait_runs_out(ctx, tiles, kind):
+    tiles(kind)
+    G = matrices(22, 3, 400, 700)
+    want = orthogonalise(ctx, G)
+    for _ in range(5):
+        assert torch.equal(orthogonalise(ctx, G), want)
+    ctx.set_tuning("stats_timeout_cycles", 200000)
+    ctx.set_tuning("stats_fault_drop_loads", 1)
+    try:
+        lost = orthogonalise(ctx, G)
+        torch.cuda.synchronize()
+    finally:
+        ctx.set_tuning("stats_fault_drop_loads", 0)
+        ctx.set_tuning("stats_timeout_cycles", 0)
+    assert torch.isnan(lost).all()
+    assert torch.equal(orthogonalise(ctx, G), want)
+
+
+# Short sides around what changes the layout of a small matrix: 16 (columns of a product), 32 and 64 (copies of B), 128;
+# long sides with one CTA and clusters of 2 to 8, with a last CTA of few columns
+SMALL = [(7, 2048), (16, 250), (17, 259), (31, 513), (32, 1030), (33, 300), (64, 257), (64, 1799), (65, 140), (65, 260), (100, 90),
+         (113, 400), (128, 1000), (128, 200)]
+
+
+@pytest.mark.parametrize("src", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [0, 3, 8])
+@pytest.mark.parametrize("tall", [False, True])
+@pytest.mark.parametrize("m,n", SMALL)
+def test_small_matrices_in_wider_rows(ctx, m, n, tall, pad, src):
+    """Their products have split operands at either precision."""
+    if tall:
+        m, n = n, m
+    G = matrices(23, 3, m, n).to(TYPES[src])
+    wide = torch.full((3, m, n + pad), 5.0, device="cuda", dtype=TYPES[src])
+    wide[:, :, :n] = G
+    out = torch.full((3, m, n + pad), 5.0, device="cuda")
+    cfg = pkg.make_ns_cfg()
+    ctx.abs_orthogonalise(wide[:, :, :n], out[:, :, :n], cfg, ctx.ns_scratch(3, m, n, cfg))
+    check(out[:, :, :n], ref_ns(G), 2e-5)
+    assert bool((out[:, :, n:] == 5.0).all()) and torch.equal(wide[:, :, :n], G)
+    again = torch.empty_like(G, dtype=torch.float32)
+    ctx.abs_orthogonalise(G, again, cfg, ctx.ns_scratch(3, m, n, cfg))
+    assert torch.equal(again, out[:, :, :n])                   # alignment changes the loads, not the result
+
+
 @pytest.mark.parametrize("src", ["f32", "bf16"])
 @pytest.mark.parametrize("dst", ["f32", "bf16"])
 @pytest.mark.parametrize("precision,tol", [("f16", 4e-3), ("f32", 2e-5)])
