@@ -290,8 +290,8 @@ struct NsPlan {
 };
 constexpr size_t kNsFixedBytes = 16 * 1024;       // alignment of the (at most ten) buffers
 // Matrices that are worked on together.  More of them hide the waits between products, fewer keep what a step
-// reads and writes inside L2 (126 MB): 96 matrices of 768 x 768 in groups of 10, 20, 32, 48 and 96 took 1699,
-// 1389, 1396, 1443 and 1459 us, 28 of them in groups of 10, 14 and 28 791, 526 and 397.
+// reads and writes inside L2 (126 MB).  us with groups of 100, 200, 300 and 600 MB: 96 matrices of 768 x 768 1320, 1303,
+// 1310, 1326; 28 of them 450, 394, 394, 420; 16 of 2048 x 2048 2723, 2528, 2624, 2578.
 constexpr size_t kGroupBytes = 200ull << 20;
 
 NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
