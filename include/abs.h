@@ -353,8 +353,8 @@ typedef struct {
 } abs_ns_cfg;           /* 24 bytes */
 
 /* Bytes of device scratch that abs_orthogonalise (count matrices) or local_muon_step
- * (count = M * matrices) needs; matrices are worked on in groups, so this stays near
- * 100 MB however many there are.  cfg is a HOST pointer; needs no context.           */
+ * (count = M * matrices) needs; matrices are worked on in groups, so past about
+ * 200 MB (or one matrix, if that is more) it stops growing with their number.  cfg is a HOST pointer; needs no context.           */
 int abs_ns_scratch_bytes(int count, long long rows, long long cols, const abs_ns_cfg* cfg, size_t* out);
 
 /* O[q] = the iterate after cfg->steps steps from G[q], q < count.  Element (q, r, c) of G at
