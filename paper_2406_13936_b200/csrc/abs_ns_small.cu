@@ -5,16 +5,16 @@
 // 256 of its columns (128 when m > 64 and there are several CTAs).  A step is three tcgen05 products
 // with a barrier after each: the time is latency, not arithmetic, so every product has split operands
 // (hi hi + hi lo + lo hi, fp32-grade) whatever precision is asked for.
-//   A = X X'          K-major rows of X twice; the CTAs' partial sums are added over the cluster: every CTA
-//                     adds its share of the elements, in rank order, and sends it to all
+//   A = X X'          K-major rows of X twice; the CTAs' partial sums are added over the cluster, in rank order: every CTA
+//                     receives all of them or, where that is too much, adds its share of the elements and sends it to all
 //   B = b A + c A A   every CTA for itself, in the place of A
 //   X <- a X + B X    every CTA its own columns; X is MN-major here, in the same memory
 // The rows of X are padded with zeros to 64 or 128, A has 128 rows.  All waits are bounded; when one runs out the
 // results of the matrix are NaN.
 //
-// Measured (B200): a step takes 1.8 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 4.3 for 8 of 10 x 1024 (of which 0.6 the
-// two cluster barriers and 0.6 the exchange), 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is
-// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 30 us;
+// Measured (B200): a step takes 1.8 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 3.9 for 8 of 10 x 1024 (of which 1 the
+// exchange), 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is
+// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 29 us;
 // with the launches of the general path (norm, split, steps, finish) 101 and 147.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
@@ -37,6 +37,7 @@ struct SmallParams {
   int steps;
   float eps, sx, inv_sx;
   long long timeout_cycles;
+  int gather;          // every CTA sends its partial sums of A to all (else: two-part exchange)
   int vec_src, vec_dst;   // groups of eight are 16-byte aligned in global memory
   int drop;            // test hook: no product is issued, so the first wait must run out
   NsCoef coef[kNsMaxSteps][3];
@@ -262,8 +263,9 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   // X: a block's values, its remainders, the next block's values, ...; A: values, remainders
   const uint32_t x_block = 2u * block_bytes, a_block = 128u * 128u;
   const uint32_t xh = base, xl = xh + block_bytes, ah = xh + blocks * x_block, al = ah + mblocks * a_block;
-  const uint32_t part = al + mblocks * a_block;                              // partial sums [m][Nm + 4] fp32 (C > 1)
-  const uint32_t pitch = static_cast<uint32_t>(Nm + 4) * 4u;
+  // partial sums (C > 1): one matrix [m][Nm + 4] fp32, or two sets of one of every CTA
+  const uint32_t part = al + mblocks * a_block;
+  const uint32_t pitch = static_cast<uint32_t>(Nm + 4) * 4u, part_bytes = static_cast<uint32_t>(p.m) * pitch;
   volatile unsigned* abort_flag = &abort_mem;
   const uint32_t bar = smem_u32(&bar_mem);
   const uint32_t cross_off = p.W > 128 ? 256u : 128u, tmem_cols = 2u * cross_off;
@@ -492,8 +494,17 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
               const uint32_t at = part + static_cast<uint32_t>(row) * pitch + 32u * ch;
               const uint32_t lo[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
               const uint32_t hi[4] = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-              sts128_s(at, lo);
-              sts128_s(at + 16u, hi);
+              if (p.gather) {
+                const uint32_t mine = at + static_cast<uint32_t>((step & 1) * C + rank) * part_bytes;
+                for (int k = 0; k < C; ++k) {
+                  const uint32_t to = map_to_rank(mine, static_cast<uint32_t>(k));
+                  st_cluster128(to, lo);
+                  st_cluster128(to + 16u, hi);
+                }
+              } else {
+                sts128_s(at, lo);
+                sts128_s(at + 16u, hi);
+              }
             }
           } else if (row < R) {
             uint32_t h[4], l[4];
@@ -504,8 +515,29 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         }
       }
     }
-    if (C > 1) {
-      cluster_sync_s();
+    if (C > 1) cluster_sync_s();
+    if (C > 1 && p.gather) {
+      // A CTA may write a set of step s + 2 once it has passed the barrier of step s + 1, which every CTA reaches with
+      // the set of step s read.
+      const int per_row = Nm / 8;
+#pragma unroll 1
+      for (int u = tid; u < p.m * per_row; u += kThreadsS) {
+        const int r = u / per_row, ch = u - r * per_row;
+        const uint32_t at = part + static_cast<uint32_t>((step & 1) * C) * part_bytes + static_cast<uint32_t>(r) * pitch + 32u * ch;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+          if (k >= C) break;
+          const uint4 a = lds128(at + static_cast<uint32_t>(k) * part_bytes), b = lds128(at + static_cast<uint32_t>(k) * part_bytes + 16u);
+          v[0] += __uint_as_float(a.x); v[1] += __uint_as_float(a.y); v[2] += __uint_as_float(a.z); v[3] += __uint_as_float(a.w);
+          v[4] += __uint_as_float(b.x); v[5] += __uint_as_float(b.y); v[6] += __uint_as_float(b.z); v[7] += __uint_as_float(b.w);
+        }
+        uint32_t h[4], l[4];
+        split8(v, h, l);
+        sts128_s(ah + chunk_at(a_block, r, ch), h);
+        sts128_s(al + chunk_at(a_block, r, ch), l);
+      }
+    } else if (C > 1) {
       const int per_row = Nm / 8, all = p.m * per_row, share = (all + C - 1) / C, stop = (rank + 1) * share < all ? (rank + 1) * share : all;
 #pragma unroll 1
       for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10000 clocks, interleaved 19000
@@ -619,7 +651,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
 }
 
 struct SmallPlan {
-  int R, W, C;
+  int R, W, C, gather;
   size_t smem;
 };
 bool plan_small(long long rows, long long cols, SmallPlan* out) {
@@ -636,7 +668,13 @@ bool plan_small(long long rows, long long cols, SmallPlan* out) {
   const int Nm = (m + 15) & ~15;
   const size_t block = static_cast<size_t>(p.R) * 128;
   // with 64 rows the products read 128 of X: behind the last block lies A
-  p.smem = 1024 + 2 * ((p.W + 63) / 64 * block + (m + 63) / 64 * 16384) + (p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0);
+  p.smem = 1024 + 2 * ((p.W + 63) / 64 * block + (m + 63) / 64 * 16384);
+  // Up to 20 KB of partial sums go to all CTAs, with one barrier a step; beyond that every CTA adds its share and sends it
+  // on, with two.  us a step that way and the other: 10 x 1024 on 4 CTAs (3 KB) 3.9, 4.4; 32 x 500 on 2 (9 KB) 4.2, 4.9;
+  // 32 x 1000 on 4 (18 KB) 4.7, 5.0; 24 x 1500 on 6 (20 KB) 5.1, 5.1; 48 x 1000 on 4 (39 KB) 6.8, 6.4.
+  const size_t part = p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0;
+  p.gather = p.C * part <= 20 * 1024;
+  p.smem += p.gather ? 2 * p.C * part : part;
   // One CTA per SM: two of them could want more tensor memory than there is, and a CTA that waits for it while
   // its cluster waits for the CTA would wait for good.
   if (p.smem < 120 * 1024) p.smem = 120 * 1024;
@@ -659,7 +697,7 @@ int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int coun
   p.s = s; p.t = t;
   p.m = s.rows < s.cols ? s.rows : s.cols;
   p.n = s.rows < s.cols ? s.cols : s.rows;
-  p.R = plan.R; p.W = plan.W; p.C = plan.C;
+  p.R = plan.R; p.W = plan.W; p.C = plan.C; p.gather = plan.gather;
   auto aligned = [](const void* a, int es, long long rs, long long ms, long long ls) {
     return ((reinterpret_cast<uintptr_t>(a) | static_cast<uintptr_t>(rs * es) | static_cast<uintptr_t>(ms * es) | static_cast<uintptr_t>(ls * es)) & 15u) == 0;
   };
