@@ -201,12 +201,14 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+_DTYPE_CODES = {torch.float32: ABS_F32, torch.bfloat16: ABS_BF16}
+
+
 def _dtype_code(t):
-    if t.dtype == torch.float32:
-        return ABS_F32
-    if t.dtype == torch.bfloat16:
-        return ABS_BF16
-    raise AbsError("G must be float32 or bfloat16, got %s" % t.dtype)
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
+        raise AbsError("G must be float32 or bfloat16, got %s" % t.dtype)
+    return code
 
 
 class Context:
@@ -383,10 +385,10 @@ class Context:
                                               scratch.numel(), _stream(stream)), "local_muon_step")
 
     # ---- layer norm ------------------------------------------------------------------------------
+    # (A call on a few rows takes less time on the GPU than its checks here, so these are written out for speed.)
     @staticmethod
-    def _rows(t, what):
+    def _rows(t, M, rows, d, what):
         """(row stride, worker stride) of [M, rows, d]; the strides of dimensions of one element are free."""
-        M, rows, d = t.shape
         worker, row, one = t.stride()
         if one != 1 and d > 1:
             raise AbsError("the last dimension of %s must be contiguous" % what)
@@ -395,80 +397,89 @@ class Context:
         return row, worker if M > 1 else row * rows
 
     @staticmethod
-    def _same_stride(tensors, M, d, what):
+    def _same_stride(one, two, M, d, what):
         """Checks [M, d] fp32 parameters (a replica each; None: absent) and returns their stride."""
         stride = None
-        for t in tensors:
+        for t in (one, two):
             if t is not None:
-                if t.dtype != torch.float32 or t.shape != (M, d) or (d > 1 and t.stride(1) != 1):
+                own, last = t.stride() if t.shape == (M, d) and t.dtype == torch.float32 else (0, -1)
+                if last != 1 and (d > 1 or last == -1):
                     raise AbsError("%s must be float32 [%d, %d] with contiguous rows" % (what, M, d))
-                own = t.stride(0) if M > 1 else d
-                if stride is not None and own != stride:
-                    raise AbsError("%s must share the replica stride" % what)
-                stride = own
+                if M > 1:
+                    if stride is not None and own != stride:
+                        raise AbsError("%s must share the replica stride" % what)
+                    stride = own
         return d if stride is None else stride
+
+    @staticmethod
+    def _statistics(mean, rstd, n):
+        for t in (mean, rstd):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
+                raise AbsError("mean and rstd must be contiguous float32 tensors of %d values" % n)
 
     def abs_layer_norm(self, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
         """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight, bias: [M, d] (or [d]) fp32 or None; mean, rstd:
         contiguous fp32 [M, rows] or None.  Y may be X."""
-        if X.dim() == 2:
+        shape = X.shape
+        if len(shape) == 2:
             X, Y = X.unsqueeze(0), Y.unsqueeze(0)
             weight, bias = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, bias))
-        shape = X.shape
+            shape = X.shape
         if len(shape) != 3 or Y.shape != shape or X.dtype != Y.dtype:
             raise AbsError("X and Y must be [M, rows, d] of one type")
         M, rows, d = shape
-        p_stride = self._same_stride((weight, bias), M, d, "weight and bias")
-        self._statistics((mean, rstd), M * rows)
-        x_rs, x_ws = self._rows(X, "X")
-        y_rs, y_ws = self._rows(Y, "Y")
-        self._check(self._lib.abs_layer_norm(self._h, _ptr(X), _dtype_code(X), M, rows, d, x_rs, x_ws, _ptr(weight),
-                                             _ptr(bias), p_stride, float(eps), _ptr(Y), y_rs, y_ws, _ptr(mean), _ptr(rstd),
-                                             _stream(stream)), "abs_layer_norm")
+        p_stride = self._same_stride(weight, bias, M, d, "weight and bias")
+        self._statistics(mean, rstd, M * rows)
+        x_rs, x_ws = self._rows(X, M, rows, d, "X")
+        y_rs, y_ws = self._rows(Y, M, rows, d, "Y")
+        rc = self._lib.abs_layer_norm(self._h, X.data_ptr(), _dtype_code(X), M, rows, d, x_rs, x_ws, _ptr(weight),
+                                      _ptr(bias), p_stride, eps, Y.data_ptr(), y_rs, y_ws, _ptr(mean), _ptr(rstd),
+                                      _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_layer_norm")
         return Y
-
-    @staticmethod
-    def _statistics(tensors, n):
-        for t in tensors:
-            if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
-                raise AbsError("mean and rstd must be contiguous float32 tensors of %d values" % n)
 
     def abs_layer_norm_backward(self, dY, X, mean, rstd, weight, dX=None, dW=None, dB=None, samples=1, Gw=None, Gb=None,
                                 stream=None):
         """dY, X, dX: [M, samples * tokens, d] (or [rows, d]); mean, rstd as abs_layer_norm wrote them; weight [M, d] or
         None.  dW, dB: fp32 [M, d]; Gw, Gb: fp32 [M, samples, d] per-sample gradients with a shared row stride (two
         parts of the rows that abs_test_stats takes).  Every output may be None."""
-        if X.dim() == 2:
+        shape, dtype = X.shape, X.dtype
+        if len(shape) == 2:
             dY, X, dX = (t if t is None else t.unsqueeze(0) for t in (dY, X, dX))
             weight, dW, dB = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, dW, dB))
             Gw, Gb = (t if t is None or t.dim() == 3 else t.unsqueeze(0) for t in (Gw, Gb))
-        shape, dtype = X.shape, X.dtype
-        if len(shape) != 3 or any(t is not None and (t.shape != shape or t.dtype != dtype) for t in (dY, dX)):
+            shape = X.shape
+        if len(shape) != 3 or dY.shape != shape or dY.dtype != dtype or (
+                dX is not None and (dX.shape != shape or dX.dtype != dtype)):
             raise AbsError("dY, X and dX must be [M, rows, d] of one type")
         M, rows, d = shape
         samples = int(samples)
         if samples < 0 or (samples == 0 and rows) or (samples and rows % samples):
             raise AbsError("%d rows are not %d samples of equal length" % (rows, samples))
-        p_stride = self._same_stride((weight,), M, d, "weight")
-        grad_stride = self._same_stride((dW, dB), M, d, "dW and dB")
-        self._statistics((mean, rstd), M * rows)
-        g_strides = None
+        p_stride = self._same_stride(weight, None, M, d, "weight")
+        grad_stride = self._same_stride(dW, dB, M, d, "dW and dB")
+        self._statistics(mean, rstd, M * rows)
+        g_rs = g_ws = None
         for t in (Gw, Gb):
             if t is not None:
                 if t.dtype != torch.float32 or t.shape != (M, samples, d):
                     raise AbsError("Gw and Gb must be float32 [%d, %d, %d]" % (M, samples, d))
-                own = self._rows(t, "Gw and Gb")
-                if g_strides is not None and own != g_strides:
+                row, worker = self._rows(t, M, samples, d, "Gw and Gb")
+                if g_rs is not None and (row != g_rs or worker != g_ws):
                     raise AbsError("Gw and Gb must share their strides")
-                g_strides = own
-        g_rs, g_ws = g_strides or (d, d * samples)
-        y_rs, y_ws = self._rows(dY, "dY")
-        x_rs, x_ws = self._rows(X, "X")
-        dx_rs, dx_ws = self._rows(dX, "dX") if dX is not None else (d, d)
-        self._check(self._lib.abs_layer_norm_backward(
-            self._h, _ptr(dY), y_rs, y_ws, _ptr(X), x_rs, x_ws, _dtype_code(X), M, samples,
+                g_rs, g_ws = row, worker
+        if g_rs is None:
+            g_rs, g_ws = d, d * samples
+        y_rs, y_ws = self._rows(dY, M, rows, d, "dY")
+        x_rs, x_ws = self._rows(X, M, rows, d, "X")
+        dx_rs, dx_ws = self._rows(dX, M, rows, d, "dX") if dX is not None else (d, d)
+        rc = self._lib.abs_layer_norm_backward(
+            self._h, dY.data_ptr(), y_rs, y_ws, X.data_ptr(), x_rs, x_ws, _dtype_code(X), M, samples,
             rows // samples if samples else 0, d, _ptr(mean), _ptr(rstd), _ptr(weight), p_stride, _ptr(dX), dx_rs, dx_ws,
-            _ptr(dW), _ptr(dB), grad_stride, _ptr(Gw), _ptr(Gb), g_rs, g_ws, _stream(stream)), "abs_layer_norm_backward")
+            _ptr(dW), _ptr(dB), grad_stride, _ptr(Gw), _ptr(Gb), g_rs, g_ws, _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_layer_norm_backward")
 
     # ---- producers and rounds ----------------------------------------------------------------
     def abs_logreg_grads(self, A, y, idx, X, b, G, stream=None):
