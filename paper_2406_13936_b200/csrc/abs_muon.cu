@@ -311,7 +311,7 @@ NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
 }
 int group_size(const NsPlan& p, int count);
 size_t scratch_need(const NsPlan& p, int count) {
-  if (ns_small_fits(p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
+  if (ns_small_fits(count, p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
   return kNsFixedBytes + group_size(p, count) * p.per_matrix();
 }
 int group_size(const NsPlan& p, int count) {
@@ -350,7 +350,7 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
   }
   sc.sx[cfg->steps] = pow2_scale(hi);
 
-  if (ns_small_fits(src.rows, src.cols))
+  if (ns_small_fits(count, src.rows, src.cols))
     return launch_ns_small(ctx, src, dst, count, cfg->eps, sc, cfg->steps, cfg->a, cfg->b, cfg->c, st);
   const bool src_vec = vectors_of_four(src.G, src.src_bf16, src.row_stride, src.matrix_stride, src.replica_stride, src.cols) &&
                        vectors_of_four(src.Buf, 0, src.row_stride, src.matrix_stride, src.replica_stride, src.cols);

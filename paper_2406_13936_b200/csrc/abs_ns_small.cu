@@ -2,7 +2,7 @@
 // momentum update, norm, all steps and the result, one thread-block cluster per matrix.
 //
 // X stays in shared memory as value + remainder (two fp16 numbers, 22 bits); a CTA of the cluster has up to
-// 256 of its columns (128 when m > 64 and there are several CTAs).  A step is three tcgen05 products
+// 256 of its columns (192 or 128 where A and the partial sums leave no room for more).  A step is three tcgen05 products
 // with a barrier after each: the time is latency, not arithmetic, so every product has split operands
 // (hi hi + hi lo + lo hi, fp32-grade) whatever precision is asked for.
 //   A = X X'          K-major rows of X twice; the CTAs' partial sums are added over the cluster, in rank order: every CTA
@@ -24,7 +24,9 @@ namespace {
 
 constexpr int kWarpsS = 16;
 constexpr int kThreadsS = kWarpsS * 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;      // (beyond 8 by the non-portable attribute)
+constexpr int kTogether = 8;         // CTAs whose sums a thread fetches together
+constexpr size_t kSmallSmem = 224 * 1024;      // dynamic shared memory, at most
 constexpr int kBatch = 2;            // groups of eight elements that a thread loads at a time
 
 struct SmallParams {
@@ -525,9 +527,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>((step & 1) * C) * part_bytes + static_cast<uint32_t>(r) * pitch + 32u * ch;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < kMaxCluster; ++k) {
-          if (k >= C) break;
+#pragma unroll 4
+        for (int k = 0; k < C; ++k) {
           const uint4 a = lds128(at + static_cast<uint32_t>(k) * part_bytes), b = lds128(at + static_cast<uint32_t>(k) * part_bytes + 16u);
           v[0] += __uint_as_float(a.x); v[1] += __uint_as_float(a.y); v[2] += __uint_as_float(a.z); v[3] += __uint_as_float(a.w);
           v[4] += __uint_as_float(b.x); v[5] += __uint_as_float(b.y); v[6] += __uint_as_float(b.z); v[7] += __uint_as_float(b.w);
@@ -544,19 +545,22 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         const int r = u / per_row, ch = u - r * per_row;
         const uint32_t at = part + static_cast<uint32_t>(r) * pitch + 32u * ch;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        float4 a[kMaxCluster], b[kMaxCluster];                     // all under way before the first is used
+#pragma unroll 1
+        for (int k0 = 0; k0 < C; k0 += kTogether) {
+          float4 a[kTogether], b[kTogether];
 #pragma unroll
-        for (int k = 0; k < kMaxCluster; ++k) {
-          if (k >= C) continue;
-          const uint32_t from = map_to_rank(at, static_cast<uint32_t>(k));
-          a[k] = ld_cluster128(from);
-          b[k] = ld_cluster128(from + 16u);
-        }
+          for (int k = 0; k < kTogether; ++k) {
+            if (k0 + k >= C) continue;
+            const uint32_t from = map_to_rank(at, static_cast<uint32_t>(k0 + k));
+            a[k] = ld_cluster128(from);
+            b[k] = ld_cluster128(from + 16u);
+          }
 #pragma unroll
-        for (int k = 0; k < kMaxCluster; ++k) {
-          if (k >= C) continue;
-          v[0] += a[k].x; v[1] += a[k].y; v[2] += a[k].z; v[3] += a[k].w;
-          v[4] += b[k].x; v[5] += b[k].y; v[6] += b[k].z; v[7] += b[k].w;
+          for (int k = 0; k < kTogether; ++k) {
+            if (k0 + k >= C) continue;
+            v[0] += a[k].x; v[1] += a[k].y; v[2] += a[k].z; v[3] += a[k].w;
+            v[4] += b[k].x; v[5] += b[k].y; v[6] += b[k].z; v[7] += b[k].w;
+          }
         }
         uint32_t h[4], l[4];
         split8(v, h, l);
@@ -654,45 +658,58 @@ struct SmallPlan {
   int R, W, C, gather;
   size_t smem;
 };
-bool plan_small(long long rows, long long cols, SmallPlan* out) {
+// `narrow`: at most 128 columns a CTA.
+bool plan_columns(int count, long long rows, long long cols, bool narrow, SmallPlan* out) {
   const int m = static_cast<int>(rows < cols ? rows : cols);
   const long long n = rows < cols ? cols : rows;
-  if (m > 128) return false;
+  if (m > 128 || n > 256 * kMaxCluster) return false;
   SmallPlan p;
   p.R = m <= 64 ? 64 : 128;
-  const long long most = p.R == 64 || n <= 256 ? 256 : 128;      // columns of a CTA that fit beside A and the partial sums
+  const int Nm = (m + 15) & ~15;
+  const size_t block = static_cast<size_t>(p.R) * 128, part = static_cast<size_t>(m) * (Nm + 4) * 4;
+  // with 64 rows the products read 128 of X: behind the last block lies A
+  auto smem = [&](int W) { return 1024 + 2 * (static_cast<size_t>((W + 63) / 64) * block + static_cast<size_t>((m + 63) / 64) * 16384); };
+  int most = narrow ? 128 : 256;                                 // columns of a CTA that fit beside A and the partial sums
+  while (most > 64 && smem(most) + (n > most ? part : 0) > kSmallSmem) most -= 64;
   const long long C = (n + most - 1) / most;
-  if (C > kMaxCluster) return false;
+  // A cluster of more than 8 CTAs has a GPC of its own, so few matrices are under way at a time.  5 steps there and on the
+  // general path, us: 7 of 18 x 2474 (10 CTAs) 41, 243; 4 of 64 x 4000 (16) 62, 345; 3 of 86 x 2085 (11) 85, 128;
+  // 128 x 2048 (16) 105, 122; but 8 of 128 x 1500 (12) 195, 115.
+  if (C > kMaxCluster || (C > 8 && count > (m > 64 ? 4 : 32))) return false;
   p.C = static_cast<int>(C);                                     // with W as below every CTA has columns: n > (C - 1) W
   p.W = static_cast<int>(((n + C - 1) / C + 15) / 16 * 16);
-  const int Nm = (m + 15) & ~15;
-  const size_t block = static_cast<size_t>(p.R) * 128;
-  // with 64 rows the products read 128 of X: behind the last block lies A
-  p.smem = 1024 + 2 * ((p.W + 63) / 64 * block + (m + 63) / 64 * 16384);
+  p.smem = smem(p.W);
   // Up to 20 KB of partial sums go to all CTAs, with one barrier a step; beyond that every CTA adds its share and sends it
   // on, with two.  us a step that way and the other: 10 x 1024 on 4 CTAs (3 KB) 3.9, 4.4; 32 x 500 on 2 (9 KB) 4.2, 4.9;
   // 32 x 1000 on 4 (18 KB) 4.7, 5.0; 24 x 1500 on 6 (20 KB) 5.1, 5.1; 48 x 1000 on 4 (39 KB) 6.8, 6.4.
-  const size_t part = p.C > 1 ? static_cast<size_t>(m) * (Nm + 4) * 4 : 0;
   p.gather = p.C * part <= 20 * 1024;
-  p.smem += p.gather ? 2 * p.C * part : part;
+  if (p.C > 1) p.smem += p.gather ? 2 * p.C * part : part;
   // One CTA per SM: two of them could want more tensor memory than there is, and a CTA that waits for it while
   // its cluster waits for the CTA would wait for good.
   if (p.smem < 120 * 1024) p.smem = 120 * 1024;
   *out = p;
   return true;
 }
+// With SMs to spare, CTAs of fewer columns, where there are several anyway: 8 of 10 x 1024 (8 CTAs for 4) 28.3 -> 27.1 us,
+// 64 x 1000 47.8 -> 43.6; 16 of 32 x 1000, whose 16 clusters of 8 do not fit at a time, 34 -> 64, 4 of 64 x 192 (2 for 1) 31.7 -> 35.4.
+bool plan_small(int count, long long rows, long long cols, SmallPlan* out) {
+  if (!plan_columns(count, rows, cols, false, out)) return false;
+  SmallPlan narrow;
+  if (out->C > 2 && plan_columns(count, rows, cols, true, &narrow) && narrow.C <= 8 && count * narrow.C <= 64) *out = narrow;
+  return true;
+}
 
 }  // namespace
 
-bool ns_small_fits(long long rows, long long cols) {
+bool ns_small_fits(int count, long long rows, long long cols) {
   SmallPlan p;
-  return plan_small(rows, cols, &p);
+  return plan_small(count, rows, cols, &p);
 }
 
 int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int count, float eps, const NsScales& sc, int steps,
                     float a, float b, float c, cudaStream_t st) {
   SmallPlan plan;
-  if (!plan_small(s.rows, s.cols, &plan)) return ABS_ERR_UNSUPPORTED;
+  if (!plan_small(count, s.rows, s.cols, &plan)) return ABS_ERR_UNSUPPORTED;
   SmallParams p = {};
   p.s = s; p.t = t;
   p.m = s.rows < s.cols ? s.rows : s.cols;
@@ -713,6 +730,7 @@ int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int coun
   for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
   auto kern = ns_small_kernel;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, plan.smem));
+  if (plan.C > 8) ABS_CUDA_TRY(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -124,7 +124,7 @@ def test_both_tile_shapes_repeat_their_bits_and_end_when_a_wait_runs_out(ctx, ti
 # Short sides around what changes the layout of a small matrix: 16 (columns of a product), 32 and 64 (copies of B), 128;
 # long sides with one CTA and clusters of 2 to 8, with a last CTA of few columns
 SMALL = [(7, 2048), (16, 250), (17, 259), (31, 513), (32, 1030), (33, 300), (64, 257), (64, 1799), (65, 140), (65, 260), (100, 90),
-         (113, 400), (128, 1000), (128, 200)]
+         (113, 400), (128, 1000), (128, 200), (18, 2474), (64, 4096), (86, 2085), (128, 2048), (97, 1300)]
 
 
 @pytest.mark.parametrize("src", ["f32", "bf16"])
