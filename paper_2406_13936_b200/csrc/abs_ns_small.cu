@@ -14,7 +14,7 @@
 //
 // Measured (B200): a step takes 1.8 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 3.9 for 8 of 10 x 1024 (of which 1 the
 // exchange), 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is
-// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 29 us;
+// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 26 us;
 // with the launches of the general path (norm, split, steps, finish) 101 and 147.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
@@ -247,6 +247,9 @@ __device__ __forceinline__ void get8(uint32_t matrix, uint32_t block, bool tall,
   }
 }
 
+// CLUSTER: several CTAs a matrix.  (A kernel of its own for one CTA: what it does not need is not in its way; 4 of
+// 64 x 192 30.8 us, 32.8 with one kernel for both.)
+template <bool CLUSTER>
 __global__ void __launch_bounds__(kThreadsS, 1)
 ns_small_kernel(const __grid_constant__ SmallParams p) {
   extern __shared__ unsigned char smem_dyn[];
@@ -255,7 +258,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   __shared__ unsigned long long bar_mem;
   __shared__ unsigned abort_mem, tmem_slot;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int C = p.C, R = p.R;
+  const int C = CLUSTER ? p.C : 1, R = p.R;
   const int q = blockIdx.x / C, rank = static_cast<int>(blockIdx.x) - q * C;     // matrix, place in its cluster
   const int c0 = rank * p.W, wc = p.n - c0 < p.W ? p.n - c0 : p.W;               // this CTA's columns
   const int Nm = (p.m + 15) & ~15, Nw = (wc + 15) & ~15;
@@ -360,10 +363,10 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
     for (int w = 0; w < kWarpsS; ++w) sum += red[w];
     norm_sq = sum;
   }
-  if (C > 1) cluster_sync_s();
+  if constexpr (CLUSTER) cluster_sync_s();
   else __syncthreads();
   sum = 0.0;
-  if (C > 1) {
+  if constexpr (CLUSTER) {
     for (int r = 0; r < C; ++r) sum += ld_cluster_f64(map_to_rank(smem_u32(&norm_sq), static_cast<uint32_t>(r)));
   } else {
     sum = norm_sq;
@@ -491,7 +494,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
           float (&v)[8] = w[x];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= gram.acc;
-          if (C > 1) {
+          if constexpr (CLUSTER) {
             if (row < p.m) {
               const uint32_t at = part + static_cast<uint32_t>(row) * pitch + 32u * ch;
               const uint32_t lo[4] = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
@@ -517,8 +520,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         }
       }
     }
-    if (C > 1) cluster_sync_s();
-    if (C > 1 && p.gather) {
+    if constexpr (CLUSTER) cluster_sync_s();
+    if (CLUSTER && p.gather) {
       // A CTA may write a set of step s + 2 once it has passed the barrier of step s + 1, which every CTA reaches with
       // the set of step s read.
       const int per_row = Nm / 8;
@@ -538,7 +541,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
         sts128_s(ah + chunk_at(a_block, r, ch), h);
         sts128_s(al + chunk_at(a_block, r, ch), l);
       }
-    } else if (C > 1) {
+    } else if constexpr (CLUSTER) {
       const int per_row = Nm / 8, all = p.m * per_row, share = (all + C - 1) / C, stop = (rank + 1) * share < all ? (rank + 1) * share : all;
 #pragma unroll 1
       for (int u = rank * share + tid; u < stop; u += kThreadsS) {      // one after the other: 128 x 512 on 4 CTAs 10000 clocks, interleaved 19000
@@ -615,7 +618,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
 
   // ---- the result ------------------------------------------------------------------------------------------
   unsigned failed = abort_mem;
-  if (C > 1) {
+  if constexpr (CLUSTER) {
     cluster_sync_s();
     for (int r = 0; r < C; ++r) failed |= ld_cluster_u32(map_to_rank(smem_u32(&abort_mem), static_cast<uint32_t>(r)));
   }
@@ -651,7 +654,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
       else store8(static_cast<float*>(p.t.O) + at, n[x], p.vec_dst, v);
     }
   }
-  if (C > 1) cluster_sync_s();                                   // a peer may still read this CTA's abort flag
+  if constexpr (CLUSTER) cluster_sync_s();                                   // a peer may still read this CTA's abort flag
 }
 
 struct SmallPlan {
@@ -728,7 +731,7 @@ int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int coun
   p.timeout_cycles = ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles;
   p.drop = ctx->tuning.stats_fault_drop_loads ? 1 : 0;
   for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
-  auto kern = ns_small_kernel;
+  auto kern = plan.C > 1 ? ns_small_kernel<true> : ns_small_kernel<false>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, plan.smem));
   if (plan.C > 8) ABS_CUDA_TRY(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t lc = {};
