@@ -426,6 +426,8 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
   // X X' where X's remainders lie 64 rows behind its values: hi hi and hi lo are one product of twice the width.  One of up
   // to 128 columns costs 61 clocks (what the first operand's 128 rows take to fetch), so two of
   // them are a third faster than three: 10 x 1024 on 4 CTAs 2200 clocks, 2950.
+  // Columns 128 .. 255 have an accumulator of their own: the tensor core does not round its sums to nearest, and shorter ones
+  // are nearer (4 of 64 x 256, error against 64 bits 2.0e-6 with one, 1.8e-6 with two, plain fp32 1.2e-6).
   auto gram_products = [&](uint32_t idesc) {
     const uint32_t wide = idesc + (64u >> 3 << 17);
     uint64_t dh = desc_k | ((xh & 0x3ffffu) >> 4), dl = dh + (block_bytes >> 4);
@@ -434,7 +436,7 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (k0 + 16 * k >= Nw) break;
-        umma_s(tmem, dh + 2u * k, dh + 2u * k, wide, (k0 | k) ? 1u : 0u);
+        umma_s(tmem + (k0 < 128 ? 0u : 128u), dh + 2u * k, dh + 2u * k, wide, ((k0 & 127) | k) ? 1u : 0u);
         umma_s(cross, dl + 2u * k, dh + 2u * k, idesc, (k0 | k) ? 1u : 0u);
       }
       dh += x_block >> 4;
@@ -487,6 +489,11 @@ ns_small_kernel(const __grid_constant__ SmallParams p) {
           tmem_ld16(tmem + 64u + t_row + 8u * ch2, z);
 #pragma unroll
           for (int e = 0; e < 16; ++e) w[e >> 3][e & 7] += z[e >> 3][e & 7];
+          if (Nw > 128) {
+            tmem_ld16_sum(tmem + 128u + t_row + 8u * ch2, tmem + 192u + t_row + 8u * ch2, z);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e >> 3][e & 7] += z[e >> 3][e & 7];
+          }
         }
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
