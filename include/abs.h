@@ -551,13 +551,38 @@ int abs_layer_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int M, long lon
  * are zero).  mean, rstd: [M][samples*tokens] as the forward pass wrote them.  All sums are fp32
  * in a fixed order: repeated calls give the same bits.
  * ABS_ERR_WORKSPACE if the context's workspace cannot hold two partial sums of 2d floats (one
- * per replica, or per sample where only one of Gw and Gb is given, and one more).             */
+ * per replica, or per sample where only one of Gw and Gb is given, and one more); past 2^30 rows
+ * of all replicas twice (or one more) for every 2^30.                                         */
 int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long dy_row_stride, long long dy_worker_stride,
                             const void* X, long long x_row_stride, long long x_worker_stride, abs_dtype dtype, int M,
                             long long samples, long long tokens, long long d, const float* mean, const float* rstd,
                             const float* weight, long long param_stride, void* dX, long long dx_row_stride,
                             long long dx_worker_stride, float* dW, float* dB, long long grad_stride, float* Gw,
                             float* Gb, long long g_row_stride, long long g_worker_stride, void* stream);
+
+/* How abs_layer_norm_backward would share out its rows and its workspace for a shape: the host-side
+ * planning, exposed for inspection and for tests that need no GPU.  aligned != 0 means base addresses and
+ * strides are multiples of 16 bytes (else of one element).  The M*samples segments of `tokens` rows (without
+ * Gw and Gb: one a replica) lie one after the other; CTA c has rows c*rows_per_cta and on.  Its sums of
+ * segment s go to the workspace's place c + s, or, direct: to Gw and Gb themselves where the CTA has the whole
+ * segment, else to place 2c (its first) or 2c + 1.  M*parts places from `used` on follow where parts > 1 and
+ * the totals are asked for.  ABS_ERR_WORKSPACE: room < needed, and ctas to used are not set.              */
+typedef struct {
+  int route;              /* 0 rows staged in shared memory, 1 rows in registers, 2 any width          */
+  int groups;             /* groups of threads of a CTA, each with rows of its own                     */
+  long long samples;      /* segments of a replica                                                     */
+  long long tokens;       /* rows of a segment                                                         */
+  long long ctas;
+  long long rows_per_cta;
+  int direct;
+  int parts;              /* CTAs that add up a column's segments                                      */
+  long long room;         /* places of 2d floats in the workspace                                      */
+  long long needed;
+  long long used;
+} abs_ln_backward_plan;   /* 72 bytes */
+int abs_plan_layer_norm_backward(abs_dtype dtype, int M, long long samples, long long tokens, long long d, int aligned,
+                                 int with_gw, int with_gb, int with_totals, int sm_count, size_t workspace_bytes,
+                                 abs_ln_backward_plan* out);
 
 /* Three-layer ReLU MLP with softmax cross-entropy (the second synthetic problem).
  * dims = {n0, n1, n2, n3} layer widths.  One replica's parameters are a flat fp32

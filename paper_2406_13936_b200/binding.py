@@ -60,6 +60,12 @@ class MuonCfg(ctypes.Structure):
                 ("scale", ctypes.c_float), ("nesterov", ctypes.c_int), ("reserved", ctypes.c_int), ("ns", NsCfg)]
 
 
+class LnBackwardPlan(ctypes.Structure):
+    _fields_ = [("route", ctypes.c_int), ("groups", ctypes.c_int), ("samples", ctypes.c_longlong), ("tokens", ctypes.c_longlong),
+                ("ctas", ctypes.c_longlong), ("rows_per_cta", ctypes.c_longlong), ("direct", ctypes.c_int), ("parts", ctypes.c_int),
+                ("room", ctypes.c_longlong), ("needed", ctypes.c_longlong), ("used", ctypes.c_longlong)]
+
+
 class StatsPlan(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in
                 ("route", "lanes_per_row", "warps_per_box", "boxes_per_stage", "stages", "box_rows", "row_boxes",
@@ -160,6 +166,9 @@ EXPORTS = {
                                 ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
                                 ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p,
                                 ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p],
+    "abs_plan_layer_norm_backward": [ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
+                                     ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_size_t,
+                                     ctypes.POINTER(LnBackwardPlan)],
 }
 
 _lib = None
@@ -651,6 +660,19 @@ def plan_stats(dtype, b, aligned=True, sm_count=148, smem_optin=232448):
     if rc != 0:
         raise AbsError("abs_plan_stats failed (%d)" % rc)
     return {name: getattr(plan, name) for name, _ in StatsPlan._fields_ if name != "reserved"}
+
+
+def plan_layer_norm_backward(dtype, M, samples, tokens, d, aligned=True, with_gw=False, with_gb=False, with_totals=False,
+                             sm_count=148, workspace_bytes=64 << 20):
+    """How abs_layer_norm_backward would share out its rows and its workspace; needs no GPU."""
+    lib = load_library()
+    plan = LnBackwardPlan()
+    rc = lib.abs_plan_layer_norm_backward({"f32": ABS_F32, "bf16": ABS_BF16}[dtype], int(M), int(samples), int(tokens), int(d),
+                                          int(bool(aligned)), int(bool(with_gw)), int(bool(with_gb)), int(bool(with_totals)),
+                                          int(sm_count), int(workspace_bytes), ctypes.byref(plan))
+    if rc != 0:
+        raise AbsError("abs_plan_layer_norm_backward failed (%d)" % rc)
+    return {name: getattr(plan, name) for name, _ in LnBackwardPlan._fields_}
 
 
 def _record_to_dict(r):

@@ -1255,6 +1255,82 @@ unsigned long long row_bits(const void* p, abs_dtype dtype, int M, long long rs,
   return reinterpret_cast<uintptr_t>(p) | static_cast<unsigned long long>(rs) * es | (M > 1 ? static_cast<unsigned long long>(ws) * es : 0);
 }
 
+// How a backward pass shares out its rows and what it keeps in the workspace, counted in partial sums of 2 d floats: those of
+// the CTAs at part_slot(), `used` places, then the totals of ln_reduce_kernel's CTAs.  Host arithmetic alone.
+struct BackwardPlan {
+  RowPlan row;
+  bool sums, direct, whole;
+  int groups;
+  long long samples, tokens;             // segments of a replica and rows of one
+  long long ctas, rows_per_cta;
+  long long room, needed, used;          // places of the workspace, those that the pass cannot do without, those of the CTAs
+  long long parts, per_cta;              // CTAs that share a column's samples, samples of one
+};
+BackwardPlan plan_backward(abs_dtype dtype, int M, long long samples, long long tokens, long long d, unsigned long long align_bits,
+                           bool with_gw, bool with_gb, bool totals, int sm_count, size_t workspace_bytes) {
+  BackwardPlan p = {};
+  const bool per_sample = with_gw || with_gb;
+  const long long rows = samples * tokens;
+  if (!per_sample) {               // only the totals: a replica's rows are one segment
+    samples = rows > 0 ? 1 : 0;
+    tokens = rows;
+  }
+  p.row = plan_row(dtype, d, align_bits, dtype == ABS_F32 ? 4 : 3, 2);
+  p.sums = per_sample || totals;
+  p.samples = samples;
+  p.tokens = tokens;
+  p.groups = 1;
+  p.rows_per_cta = 1;
+  p.parts = 1;
+  p.per_cta = samples > 0 ? samples : 1;
+  p.room = static_cast<long long>(workspace_bytes / (2 * sizeof(float))) / d;
+  if (rows == 0) return p;
+  const bool fast = p.row.tpr > 0;
+  const long long total = rows * M, segments = samples * M;
+  // Groups of a CTA share segments; short ones (up to two rows a group) are better off with CTAs of one group.
+  if (fast) {
+    const int full = kRingThreads / p.row.tpr;
+    if (tokens >= 2 * full || !p.sums) p.groups = full;
+    p.ctas = static_cast<long long>(sm_count) * (full / p.groups);
+  } else {
+    p.ctas = static_cast<long long>(sm_count) * 8 * kLnThreads / (d < kLnThreads ? kLnThreads : d);
+    if (p.ctas < sm_count) p.ctas = sm_count;
+  }
+  const long long worth = (total + 2 * p.groups - 1) / (2 * p.groups);         // at least two rows a group
+  if (p.ctas > worth) p.ctas = worth;
+  const long long fewest = (total >> 30) + 1;                                  // a CTA counts its rows in 32 bits
+  if (p.ctas < fewest) p.ctas = fewest;
+  if (p.sums) {
+    p.direct = with_gw && with_gb;
+    p.needed = p.direct ? 2 * fewest : segments + fewest;
+    if (p.room < p.needed) return p;
+    const long long most = p.direct ? p.room / 2 : p.room - segments;          // (never below fewest)
+    if (p.ctas > most) p.ctas = most;
+  }
+  p.rows_per_cta = (total + p.ctas - 1) / p.ctas;
+  if (p.groups == 1 && p.sums && p.rows_per_cta > tokens) {
+    // Whole segments.  Rounded down they take more CTAs, whose places the workspace has to have (direct: none is used then);
+    // rounded up they never do.
+    const long long down = p.rows_per_cta / tokens * tokens;
+    const bool fits = p.direct || (total + down - 1) / down + segments <= p.room;
+    p.rows_per_cta = fits || down == p.rows_per_cta ? down : down + tokens;
+  }
+  p.ctas = (total + p.rows_per_cta - 1) / p.rows_per_cta;
+  p.whole = p.direct && p.rows_per_cta % tokens == 0;
+  if (p.sums) p.used = p.whole ? 0 : p.direct ? 2 * p.ctas : p.ctas + segments;
+  // 32 samples a CTA, where that fills the GPU no further than needed
+  if (per_sample) {
+    p.parts = (samples + 31) / 32;
+    const long long most = 1 + 16ll * sm_count * 32 / (2 * d * M), fit = totals ? (p.room - p.used) / M : p.parts;
+    if (p.parts > most) p.parts = most;
+    if (p.parts > fit) p.parts = fit;
+    if (p.parts < 1) p.parts = 1;
+    p.per_cta = (samples + p.parts - 1) / p.parts;
+    p.parts = (samples + p.per_cta - 1) / p.per_cta;
+  }
+  return p;
+}
+
 }  // namespace
 }  // namespace absk
 
@@ -1320,86 +1396,67 @@ extern "C" int abs_layer_norm_backward(abs_ctx* ctx, const void* dY, long long d
   DeviceGuardLn guard(ctx->device);
   if (!guard.ok) return set_error(ctx, ABS_ERR_CUDA, "cannot select device %d", ctx->device);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (!per_sample) {               // only the totals: a replica's rows are one segment
-    samples = rows > 0 ? 1 : 0;
-    tokens = rows;
-  }
+  const unsigned long long align_bits = row_bits(dY, dtype, M, dy_row_stride, dy_worker_stride) |
+                                        row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
+                                        (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0);
+  const BackwardPlan p = plan_backward(dtype, M, samples, tokens, d, align_bits, Gw != nullptr, Gb != nullptr, totals, ctx->sm_count,
+                                       ctx->workspace_bytes);
+  if (p.room < p.needed)
+    return set_error(ctx, ABS_ERR_WORKSPACE, "the workspace holds %lld partial sums of %lld needed", p.room, p.needed);
   LnBackward a{dY, dy_row_stride, dy_worker_stride, X, x_row_stride, x_worker_stride, mean, rstd, weight, param_stride,
-               dX, dx_row_stride, dx_worker_stride, M, samples, tokens, static_cast<int>(d), nullptr, 1, nullptr, nullptr, 0, 0};
-  const RowPlan plan = plan_row(dtype, d, row_bits(dY, dtype, M, dy_row_stride, dy_worker_stride) |
-                                              row_bits(X, dtype, M, x_row_stride, x_worker_stride) |
-                                              (dX ? row_bits(dX, dtype, M, dx_row_stride, dx_worker_stride) : 0), dtype == ABS_F32 ? 4 : 3, 2);
-  const bool sums = per_sample || totals;
-  LnReduce red{static_cast<const float*>(ctx->workspace), M, samples, tokens, 1, static_cast<int>(d), 0, 0, samples > 0 ? samples : 1,
-               nullptr, Gw, Gb, g_row_stride, g_worker_stride, dW, dB, grad_stride};
-  const long long room = static_cast<long long>(ctx->workspace_bytes / (2 * sizeof(float))) / d;     // of the workspace, in partial sums
-  long long used = 0, parts = 1;                                       // ... in use; CTAs that share a column's samples
+               dX, dx_row_stride, dx_worker_stride, M, p.samples, p.tokens, static_cast<int>(d), nullptr, p.rows_per_cta, nullptr,
+               nullptr, 0, 0};
+  LnReduce red{static_cast<const float*>(ctx->workspace), M, p.samples, p.tokens, p.rows_per_cta, static_cast<int>(d), p.direct,
+               p.whole, p.per_cta, nullptr, Gw, Gb, g_row_stride, g_worker_stride, dW, dB, grad_stride};
   if (rows > 0) {
-    const bool fast = plan.tpr > 0;
-    const long long total = rows * M, segments = samples * M;
-    // Groups of a CTA share segments; short ones (up to two rows a group) are better off with CTAs of one group.
-    int groups = 1;
-    long long ctas;
-    if (fast) {
-      const int full = kRingThreads / plan.tpr;
-      if (tokens >= 2 * full || !sums) groups = full;
-      ctas = static_cast<long long>(ctx->sm_count) * (full / groups);
+    if (p.sums) a.part = static_cast<float*>(ctx->workspace);
+    if (p.direct) {
+      a.Gw = Gw; a.Gb = Gb; a.g_rs = g_row_stride; a.g_ws = g_worker_stride;
+    }
+    if (p.parts > 1 && totals) red.totals = static_cast<float*>(ctx->workspace) + p.used * 2 * d;
+    if (p.row.tpr > 0) {
+      ABS_CUDA_TRY(ctx, dispatch_backward(ctx, a, dtype, p.row, p.groups, static_cast<unsigned>(p.ctas), st));
     } else {
-      ctas = static_cast<long long>(ctx->sm_count) * 8 * kLnThreads / (d < kLnThreads ? kLnThreads : d);
-      if (ctas < ctx->sm_count) ctas = ctx->sm_count;
-    }
-    const long long worth = (total + 2 * groups - 1) / (2 * groups);         // at least two rows a group
-    if (ctas > worth) ctas = worth;
-    if (sums) {
-      const bool direct = Gw != nullptr && Gb != nullptr;
-      const long long needed = direct ? 2 : segments + 1, most = direct ? room / 2 : room - segments;
-      if (room < needed)
-        return set_error(ctx, ABS_ERR_WORKSPACE, "the workspace holds %lld partial sums of %lld needed", room, needed);
-      if (ctas > most) ctas = most;
-      a.part = static_cast<float*>(ctx->workspace);
-      if (direct) {
-        a.Gw = Gw; a.Gb = Gb; a.g_rs = g_row_stride; a.g_ws = g_worker_stride;
-        red.direct = 1;
-      }
-    }
-    if (ctas < (total >> 30) + 1) ctas = (total >> 30) + 1;                  // a CTA counts its rows in 32 bits
-    a.rows_per_cta = (total + ctas - 1) / ctas;
-    if (groups == 1 && sums && a.rows_per_cta > tokens) a.rows_per_cta = a.rows_per_cta / tokens * tokens;      // whole segments
-    ctas = (total + a.rows_per_cta - 1) / a.rows_per_cta;
-    red.rows_per_cta = a.rows_per_cta;
-    red.whole = red.direct && a.rows_per_cta % tokens == 0;
-    used = red.direct ? 2 * ctas : ctas + segments;
-    // 32 samples a CTA, where that fills the GPU no further than needed
-    if (per_sample) {
-      parts = (samples + 31) / 32;
-      const long long most = 1 + 16ll * ctx->sm_count * 32 / (2 * d * M), fit = totals ? (room - used) / M : parts;
-      if (parts > most) parts = most;
-      if (parts > fit) parts = fit;
-      if (parts < 1) parts = 1;
-      red.per_cta = (samples + parts - 1) / parts;
-      parts = (samples + red.per_cta - 1) / red.per_cta;
-      if (parts > 1 && totals) red.totals = static_cast<float*>(ctx->workspace) + used * 2 * d;
-    }
-    if (fast) {
-      ABS_CUDA_TRY(ctx, dispatch_backward(ctx, a, dtype, plan, groups, static_cast<unsigned>(ctas), st));
-    } else {
-      if (sums) {
-        const dim3 grid(static_cast<unsigned>(ctas * ((d + kLnThreads - 1) / kLnThreads)));
+      if (p.sums) {
+        const dim3 grid(static_cast<unsigned>(p.ctas * ((d + kLnThreads - 1) / kLnThreads)));
         if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
         else ABS_CUDA_TRY(ctx, launch_dependent(ln_params_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
       }
       if (dX) {                    // after the sums: dX may take the place of dY or X
-        const dim3 grid(row_grid(ctx, total));
+        const dim3 grid(row_grid(ctx, rows * M));
         if (dtype == ABS_F32) ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<float>, grid, dim3(kLnThreads), 0, st, a));
         else ABS_CUDA_TRY(ctx, launch_dependent(ln_dx_any_kernel<__nv_bfloat16>, grid, dim3(kLnThreads), 0, st, a));
       }
     }
   }
-  if (!sums || (red.whole && !totals)) return ABS_OK;
-  ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M, static_cast<unsigned>(parts)),
+  if (!p.sums || (p.whole && !totals)) return ABS_OK;
+  ABS_CUDA_TRY(ctx, launch_dependent(ln_reduce_kernel, dim3(static_cast<unsigned>((2 * d + 31) / 32), M, static_cast<unsigned>(p.parts)),
                                      dim3(kLnThreads), 0, st, red));
   if (red.totals)
     ABS_CUDA_TRY(ctx, launch_dependent(ln_total_kernel, dim3(static_cast<unsigned>((2 * d + kLnThreads - 1) / kLnThreads), M),
-                                       dim3(kLnThreads), 0, st, red, static_cast<int>(parts)));
+                                       dim3(kLnThreads), 0, st, red, static_cast<int>(p.parts)));
   return ABS_OK;
+}
+
+extern "C" int abs_plan_layer_norm_backward(abs_dtype dtype, int M, long long samples, long long tokens, long long d, int aligned,
+                                            int with_gw, int with_gb, int with_totals, int sm_count, size_t workspace_bytes,
+                                            abs_ln_backward_plan* out) {
+  if (out == nullptr || M < 1 || samples < 0 || tokens < 0 || d < 1 || sm_count < 1 || (dtype != ABS_F32 && dtype != ABS_BF16) ||
+      d > (1 << 24) || M > 65535 || (tokens > 0 && samples > (1ll << 40) / tokens))
+    return ABS_ERR_INVALID_ARG;
+  const BackwardPlan p = plan_backward(dtype, M, samples, tokens, d, aligned ? 0u : (dtype == ABS_F32 ? 4u : 2u), with_gw != 0,
+                                       with_gb != 0, with_totals != 0, sm_count, workspace_bytes);
+  memset(out, 0, sizeof(*out));
+  out->route = p.row.tpr == 0 ? 2 : p.row.wide ? 0 : 1;
+  out->groups = p.groups;
+  out->samples = p.samples;
+  out->tokens = p.tokens;
+  out->ctas = p.ctas;
+  out->rows_per_cta = p.rows_per_cta;
+  out->direct = p.direct;
+  out->parts = static_cast<int>(p.parts);
+  out->room = p.room;
+  out->needed = p.needed;
+  out->used = p.used;
+  return p.room < p.needed ? ABS_ERR_WORKSPACE : ABS_OK;
 }

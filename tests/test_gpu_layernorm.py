@@ -366,3 +366,50 @@ def test_refusals(ctx):
     finally:
         small.close()
     assert np.isfinite(dW.sum().item())
+
+
+# (M, samples, tokens, d, offset, spare places of the workspace): rows staged in shared memory, in registers, of any width
+TIGHT = [(1, 64, 2, 96, 0, 3), (1, 300, 23, 512, 0, 7), (3, 50, 5, 257, 0, 7), (2, 1000, 11, 96, 1, 40), (1, 40, 3, 9000, 0, 2),
+         (4, 7, 1, 768, 0, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,S,T,d,offset,spare", TIGHT)
+def test_a_workspace_with_barely_enough_places(ctx, M, S, T, d, offset, spare, dtype):
+    """One of the two per-sample gradients of short samples, or both, or the totals alone."""
+    x, dy = rows_of(31, M, S * T, d, 0, offset, dtype), rows_of(32, M, S * T, d, 0, offset, dtype, 1e-2, 1e-3)
+    w, _ = params_of(33, M, d)
+    _, rm, rr = ref_forward(x, None, None)
+    mean, rstd = rm.float(), rr.float()
+    _, tw, tb = ref_backward(dy, x, mean, rstd, w, S)
+    for gw, gb, totals in ((1, 0, 0), (0, 1, 1), (1, 1, 1), (0, 0, 1)):
+        places = 2 if gw and gb else M * (S if gw or gb else 1) + 1
+        small = pkg.Context(0, workspace_bytes=(places + spare - 1) * 8 * d)
+        try:
+            G, H = (torch.full((M, S, d), 7.0, device="cuda") for _ in range(2))
+            dW, dB = (torch.full((M, d), 7.0, device="cuda") for _ in range(2))
+            small.abs_layer_norm_backward(dy, x, mean, rstd, w, None, dW if totals else None, dB if totals else None, samples=S,
+                                          Gw=G if gw else None, Gb=H if gb else None)
+            for wanted, got, terms, dim in ((gw, G, tw, 2), (gb, H, tb, 2), (totals, dW, tw, (1, 2)), (totals, dB, tb, (1, 2))):
+                if wanted:
+                    check_sum(got, terms, dim)
+            if places > 2:
+                with pytest.raises(pkg.AbsError, match="workspace"):
+                    tiny = pkg.Context(0, workspace_bytes=(places - 1) * 8 * d)
+                    tiny.abs_layer_norm_backward(dy, x, mean, rstd, w, None, dW if totals else None, dB if totals else None,
+                                                 samples=S, Gw=G if gw else None, Gb=H if gb else None)
+        finally:
+            small.close()
+
+
+@pytest.mark.parametrize("which", ["Gw", "Gb"])
+def test_one_gradient_of_many_short_samples(ctx, which):
+    """14738 samples of 23 rows of 512: their places and the CTAs' nearly fill the default workspace."""
+    S, T, d = 14738, 23, 512
+    x, dy = rows_of(34, 1, S * T, d), rows_of(35, 1, S * T, d, scale=1e-2, shift=1e-3)
+    mean, rstd = (t.float() for t in ref_forward(x, None, None)[1:])
+    G = torch.full((1, S + 1, d), 7.0, device="cuda")
+    ctx.abs_layer_norm_backward(dy, x, mean, rstd, None, samples=S, **{which: G[:, :S]})
+    _, tw, tb = ref_backward(dy, x, mean, rstd, None, S)
+    check_sum(G[:, :S], tw if which == "Gw" else tb, 2)
+    assert bool((G[:, S:] == 7.0).all())
