@@ -352,9 +352,11 @@ typedef struct {
   int precision;        /* abs_ns_precision                                                              */
 } abs_ns_cfg;           /* 24 bytes */
 
-/* Bytes of device scratch that abs_orthogonalise (count matrices) or local_muon_step
- * (count = M * matrices) needs; matrices are worked on in groups, so past about
- * 200 MB (or one matrix, if that is more) it stops growing with their number.  cfg is a HOST pointer; needs no context.           */
+/* Bytes of device scratch for abs_orthogonalise (count matrices) or local_muon_step (count = M *
+ * matrices).  Matrices are worked on in groups, so past about 200 MB (or one matrix, if that is more) it stops
+ * growing with their number; there it also falls, as groups are of equal size.  Both calls take less than this, down to
+ * what one matrix needs, in smaller groups (more launches): scratch for some number of matrices serves every
+ * smaller one.  cfg is a HOST pointer; needs no context.                                           */
 int abs_ns_scratch_bytes(int count, long long rows, long long cols, const abs_ns_cfg* cfg, size_t* out);
 
 /* O[q] = the iterate after cfg->steps steps from G[q], q < count.  Element (q, r, c) of G at

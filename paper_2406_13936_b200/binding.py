@@ -341,7 +341,7 @@ class Context:
 
     # ---- orthogonalisation and the Muon step -------------------------------------------------
     def ns_scratch(self, count, rows, cols, cfg):
-        """Device scratch tensor (uint8) for abs_orthogonalise / local_muon_step on `count` matrices."""
+        """Device scratch tensor (uint8) for abs_orthogonalise / local_muon_step on up to `count` matrices."""
         out = ctypes.c_size_t()
         rc = self._lib.abs_ns_scratch_bytes(int(count), int(rows), int(cols), ctypes.byref(cfg), ctypes.byref(out))
         if rc != 0:

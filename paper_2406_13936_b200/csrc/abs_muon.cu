@@ -309,17 +309,20 @@ NsPlan plan_ns(long long rows, long long cols, const abs_ns_cfg* cfg) {
   p.split = cfg->precision == ABS_NS_F32 || p.m <= 64;
   return p;
 }
-int group_size(const NsPlan& p, int count);
-size_t scratch_need(const NsPlan& p, int count) {
-  if (ns_small_fits(count, p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
-  return kNsFixedBytes + group_size(p, count) * p.per_matrix();
-}
-int group_size(const NsPlan& p, int count) {
-  long long z = static_cast<long long>(kGroupBytes / p.per_matrix());
+// Matrices worked on together where `bytes` of scratch hold them: groups of about the same size, so that 36 matrices with room
+// for 35 are two groups of 18.
+int group_size(const NsPlan& p, int count, size_t bytes) {
+  long long z = static_cast<long long>((bytes < kGroupBytes ? bytes : kGroupBytes) / p.per_matrix());
   if (z < 1) z = 1;
   if (z > 65535) z = 65535;
   const long long groups = (count + z - 1) / z;
-  return static_cast<int>((count + groups - 1) / groups);      // groups of about the same size
+  return static_cast<int>((count + groups - 1) / groups);
+}
+// What the call asks for.  One group's size is not monotone in the number of matrices (35 of 768 x 768 207 MB, 36 106 MB),
+// so any call takes what it gets from one matrix's up, in smaller groups: scratch for some number serves every smaller one.
+size_t scratch_need(const NsPlan& p, int count) {
+  if (ns_small_fits(count, p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
+  return kNsFixedBytes + group_size(p, count, kGroupBytes) * p.per_matrix();
 }
 
 // Whether four consecutive elements of a row can be moved at once everywhere (strides that are not used
@@ -332,10 +335,10 @@ bool vectors_of_four(const void* p, int bf16, long long row_stride, long long ma
 int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, const abs_ns_cfg* cfg, void* scratch,
            size_t scratch_bytes, cudaStream_t st) {
   const NsPlan p = plan_ns(src.rows, src.cols, cfg);
-  const int zmax = group_size(p, count);
-  const size_t need = scratch_need(p, count);
-  if (scratch == nullptr || scratch_bytes < need)
-    return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes is too small: %zu needed", scratch_bytes, need);
+  const size_t least = kNsFixedBytes + (ns_small_fits(count, src.rows, src.cols) ? 0 : p.per_matrix());
+  if (scratch == nullptr || scratch_bytes < least)
+    return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes is too small: at least %zu needed", scratch_bytes, least);
+  const int zmax = group_size(p, count, scratch_bytes - kNsFixedBytes);
   // scales of the stored matrices, from bounds on the singular values step by step
   NsScales sc;
   double hi = 1.0;

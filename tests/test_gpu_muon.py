@@ -356,3 +356,36 @@ def test_refusals(ctx):
                 lambda: ctx.local_muon_step(X, X.clone(), X.clone(), muon, scratch[:64])):
         with pytest.raises(pkg.AbsError):
             bad()
+
+
+@pytest.mark.parametrize("m,n,precision,most,fewer", [(300, 520, "f32", 98, (97, 60, 1)), (768, 768, "f16", 36, (35, 2)),
+                                                      (64, 4000, "f16", 33, (32, 5)), (200, 140, "f32", 3, (2, 1))])
+def test_scratch_for_some_number_serves_every_smaller_one(ctx, m, n, precision, most, fewer):
+    """Past one group the scratch of one matrix more is that of half as many: 98 of 300 x 520 ask for 106 MB, 97 for 209."""
+    cfg = pkg.make_ns_cfg(steps=2, precision=precision)
+    scratch = ctx.ns_scratch(most, m, n, cfg)
+    G = matrices(41, 2, m, n).repeat(most // 2 + 1, 1, 1)
+    for count in (most,) + fewer:
+        O = torch.full((count, m, n), 7.0, device="cuda")
+        ctx.abs_orthogonalise(G[:count], O, cfg, scratch)
+        check(O[:2], ref_ns(G[:min(2, count)], steps=2), 4e-3 if precision == "f16" else 2e-5)
+        assert torch.equal(O, O[:2].repeat(count // 2 + 1, 1, 1)[:count])
+
+
+def test_less_scratch_makes_smaller_groups(ctx):
+    cfg = pkg.make_ns_cfg(precision="f32")
+    G = matrices(42, 7, 200, 300)
+    want = orthogonalise(ctx, G, precision="f32")
+    one, three = (ctx.ns_scratch(k, 200, 300, cfg) for k in (1, 3))
+    for scratch in (one, three, three[:-1]):
+        O = torch.empty_like(G)
+        ctx.abs_orthogonalise(G, O, cfg, scratch)
+        assert torch.equal(O, want)
+    X, Buf, Gb = (matrices(k, 7, 200, 300).view(7, 1, 200, 300) for k in (43, 44, 45))
+    muon = pkg.make_muon_cfg(0.1, ns=cfg)
+    X2, Buf2 = X.clone(), Buf.clone()
+    ctx.local_muon_step(X, Buf, Gb, muon, one, average_after=True)
+    ctx.local_muon_step(X2, Buf2, Gb, muon, ctx.ns_scratch(7, 200, 300, cfg), average_after=True)
+    assert torch.equal(X, X2) and torch.equal(Buf, Buf2)
+    with pytest.raises(pkg.AbsError, match="scratch"):
+        ctx.abs_orthogonalise(G, torch.empty_like(G), cfg, one[:-1])

@@ -57,3 +57,11 @@ def test_scratch_refusals(count, rows, cols, kw):
 def test_unknown_precision():
     with pytest.raises(KeyError):
         pkg.make_ns_cfg(precision="f8")
+
+
+@pytest.mark.parametrize("m,n,precision", [(300, 520, "f32"), (768, 768, "f16"), (18, 2474, "f16"), (10, 1024, "f32"), (4096, 4096, "f16"),
+                                           (129, 129, "f16"), (86, 2085, "f32")])
+def test_scratch_of_any_number_is_enough_for_one(m, n, precision):
+    """... which is the least that a call takes: whatever scratch was made for, fewer matrices can use it."""
+    one = scratch(1, m, n, precision=precision)[1]
+    assert all(scratch(count, m, n, precision=precision)[1] >= one for count in list(range(1, 120)) + [1000, 1 << 20])
