@@ -106,6 +106,8 @@ const char* abs_last_error(const abs_ctx* ctx);
  * ill-conditioned, i.e. never recompute it with the tiled kernel),
  * "ns_pair_tiles" (tiles of the Newton-Schulz products with fp16 operands: 1 =
  * 128 x 128 on single CTAs, 2 = 256 x 256 on pairs of CTAs),
+ * "ns_max_cluster" (8..16: matrices with a side up to 128 use no larger thread-block clusters, as on a
+ * device that cannot hold them, and take the general path instead),
  * "stats_ctas_per_sm" (1: one CTA per SM, 64 KiB buffers, up to 16 rows per
  * thread; 2: two CTAs per SM, 32 KiB buffers, up to 8 rows per thread).
  * Unknown key or out-of-range value: ABS_ERR_INVALID_ARG. */

@@ -199,6 +199,9 @@ extern "C" int abs_set_tuning(abs_ctx* ctx, const char* key, long long value) {
   } else if (strcmp(key, "ns_pair_tiles") == 0) {
     if (value > 2) return set_error(ctx, ABS_ERR_INVALID_ARG, "ns_pair_tiles must be 0, 1 or 2");
     ctx->tuning.ns_pair_tiles = value;
+  } else if (strcmp(key, "ns_max_cluster") == 0) {
+    if (value != 0 && (value < 8 || value > 16)) return set_error(ctx, ABS_ERR_INVALID_ARG, "ns_max_cluster must be 0 or 8..16");
+    ctx->tuning.ns_max_cluster = value;
   } else if (strcmp(key, "stats_ctas_per_sm") == 0) {
     if (value > 2) return set_error(ctx, ABS_ERR_INVALID_ARG, "stats_ctas_per_sm must be 0, 1 or 2");
     ctx->tuning.stats_ctas_per_sm = value;

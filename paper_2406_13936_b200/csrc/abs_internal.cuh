@@ -35,6 +35,7 @@ struct Tuning {
   long long stats_cluster_rows = 0;
   long long stats_timeout_cycles = 0;      // 0: about two seconds of SM clock
   long long ns_pair_tiles = 0;             // Newton-Schulz products: 1 single-CTA tiles, 2 CTA-pair tiles
+  long long ns_max_cluster = 0;            // Newton-Schulz of small matrices: 8..16, no larger clusters than that
   long long stats_fault_drop_loads = 0;    // test hook: the tiled kernel's loader issues no copies
 };
 
@@ -79,6 +80,7 @@ struct abs_ctx {
   size_t staging_out_bytes = 0;
   absk::Tuning tuning;
   absk::FnCache fn_cache;
+  signed char ns_clusters[17] = {};  // clusters of the small Newton-Schulz kernel: 1 the device holds them, -1 not, 0 not asked
   char err[512] = {0};
 };
 

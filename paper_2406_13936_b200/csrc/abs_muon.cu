@@ -321,7 +321,9 @@ int group_size(const NsPlan& p, int count, size_t bytes) {
 // What the call asks for.  One group's size is not monotone in the number of matrices (35 of 768 x 768 207 MB, 36 106 MB),
 // so any call takes what it gets from one matrix's up, in smaller groups: scratch for some number serves every smaller one.
 size_t scratch_need(const NsPlan& p, int count) {
-  if (ns_small_fits(count, p.m, p.n)) return kNsFixedBytes;         // everything stays in shared memory
+  const int cluster = ns_small_cluster(count, p.m, p.n);
+  // Everything stays in shared memory.  (Larger clusters may have to take the general path.)
+  if (cluster > 0 && cluster <= kPortableCluster) return kNsFixedBytes;
   return kNsFixedBytes + group_size(p, count, kGroupBytes) * p.per_matrix();
 }
 
@@ -335,7 +337,9 @@ bool vectors_of_four(const void* p, int bf16, long long row_stride, long long ma
 int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, const abs_ns_cfg* cfg, void* scratch,
            size_t scratch_bytes, cudaStream_t st) {
   const NsPlan p = plan_ns(src.rows, src.cols, cfg);
-  const size_t least = kNsFixedBytes + (ns_small_fits(count, src.rows, src.cols) ? 0 : p.per_matrix());
+  const int cluster = ns_small_cluster(count, src.rows, src.cols);
+  const bool small = cluster > 0 && ns_small_resident(ctx, cluster);
+  const size_t least = kNsFixedBytes + (small ? 0 : p.per_matrix());
   if (scratch == nullptr || scratch_bytes < least)
     return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes is too small: at least %zu needed", scratch_bytes, least);
   const int zmax = group_size(p, count, scratch_bytes - kNsFixedBytes);
@@ -353,7 +357,7 @@ int run_ns(abs_ctx* ctx, const NsSource& src, const NsTarget& dst, int count, co
   }
   sc.sx[cfg->steps] = pow2_scale(hi);
 
-  if (ns_small_fits(count, src.rows, src.cols))
+  if (small)
     return launch_ns_small(ctx, src, dst, count, cfg->eps, sc, cfg->steps, cfg->a, cfg->b, cfg->c, st);
   const bool src_vec = vectors_of_four(src.G, src.src_bf16, src.row_stride, src.matrix_stride, src.replica_stride, src.cols) &&
                        vectors_of_four(src.Buf, 0, src.row_stride, src.matrix_stride, src.replica_stride, src.cols);

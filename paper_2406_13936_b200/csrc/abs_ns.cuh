@@ -133,7 +133,10 @@ __device__ __forceinline__ void load_update(const NsSource& s, long long i, floa
 // shared memory), or ABS_ERR_UNSUPPORTED where they do not fit.
 int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int count, float eps, const NsScales& sc, int steps,
                     float a, float b, float c, cudaStream_t st);
-bool ns_small_fits(int count, long long rows, long long cols);
+// CTAs of its clusters, 0 where the matrices do not fit; clusters beyond kPortableCluster are the device's to hold or not.
+int ns_small_cluster(int count, long long rows, long long cols);
+constexpr int kPortableCluster = 8;
+bool ns_small_resident(abs_ctx* ctx, int cluster);
 
 // All steps of a group in one launch.
 int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float b, float c, const NsScales& sc, bool split,

@@ -711,15 +711,41 @@ bool plan_small(int count, long long rows, long long cols, SmallPlan* out) {
 
 }  // namespace
 
-bool ns_small_fits(int count, long long rows, long long cols) {
+int ns_small_cluster(int count, long long rows, long long cols) {
   SmallPlan p;
-  return plan_small(count, rows, cols, &p);
+  return plan_small(count, rows, cols, &p) ? p.C : 0;
+}
+
+// Whether the device can hold a cluster of that many CTAs (of a whole SM each); asked once.
+bool ns_small_resident(abs_ctx* ctx, int cluster) {
+  if (cluster <= kPortableCluster) return true;
+  if (ctx->tuning.ns_max_cluster != 0 && cluster > ctx->tuning.ns_max_cluster) return false;
+  if (ctx->ns_clusters[cluster] == 0) {
+    auto kern = ns_small_kernel<true>;
+    cudaLaunchConfig_t lc = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    lc.gridDim = dim3(static_cast<unsigned>(cluster));
+    lc.blockDim = dim3(kThreadsS);
+    lc.dynamicSmemBytes = kSmallSmem;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    int clusters = 0;
+    const bool ok = ensure_dynamic_smem(ctx, kern, kSmallSmem) == cudaSuccess &&
+                    cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&clusters, reinterpret_cast<const void*>(kern), &lc) == cudaSuccess && clusters > 0;
+    if (!ok) cudaGetLastError();
+    ctx->ns_clusters[cluster] = ok ? 1 : -1;
+  }
+  return ctx->ns_clusters[cluster] > 0;
 }
 
 int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int count, float eps, const NsScales& sc, int steps,
                     float a, float b, float c, cudaStream_t st) {
   SmallPlan plan;
-  if (!plan_small(count, s.rows, s.cols, &plan)) return ABS_ERR_UNSUPPORTED;
+  if (!plan_small(count, s.rows, s.cols, &plan) || !ns_small_resident(ctx, plan.C)) return ABS_ERR_UNSUPPORTED;
   SmallParams p = {};
   p.s = s; p.t = t;
   p.m = s.rows < s.cols ? s.rows : s.cols;
@@ -740,7 +766,6 @@ int launch_ns_small(abs_ctx* ctx, const NsSource& s, const NsTarget& t, int coun
   for (int k = 0; k < steps; ++k) ns_coefs(p.coef[k], a, b, c, sc, k);
   auto kern = plan.C > 1 ? ns_small_kernel<true> : ns_small_kernel<false>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, plan.smem));
-  if (plan.C > 8) ABS_CUDA_TRY(ctx, cudaFuncSetAttribute(reinterpret_cast<const void*>(kern), cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -389,3 +389,24 @@ def test_less_scratch_makes_smaller_groups(ctx):
     assert torch.equal(X, X2) and torch.equal(Buf, Buf2)
     with pytest.raises(pkg.AbsError, match="scratch"):
         ctx.abs_orthogonalise(G, torch.empty_like(G), cfg, one[:-1])
+
+
+@pytest.mark.parametrize("m,n", [(18, 2474), (64, 4096), (2048, 128), (97, 1300)])
+def test_clusters_that_the_device_does_not_hold(ctx, m, n):
+    """Without clusters beyond 8 CTAs such matrices take the general path, with the scratch that was asked for."""
+    G = matrices(46, 3, m, n)
+    want = ref_ns(G)
+    cfg = pkg.make_ns_cfg(precision="f32")
+    ctx.set_tuning("ns_max_cluster", 8)
+    try:
+        O = orthogonalise(ctx, G, precision="f32")
+        X, Buf = G.clone().unsqueeze(1), torch.zeros_like(G).unsqueeze(1)
+        ctx.local_muon_step(X, Buf, G.unsqueeze(1), pkg.make_muon_cfg(1.0, nesterov=False, ns=cfg), ctx.ns_scratch(3, m, n, cfg))
+    finally:
+        ctx.set_tuning("ns_max_cluster", 0)
+    check(O, want, 2e-5)
+    check(G - X[:, 0], want, 2e-5 + 2.0 ** -22 * (G.norm() / want.norm()).item())
+    check(orthogonalise(ctx, G, precision="f32"), want, 2e-5)
+    for bad in (7, 17):
+        with pytest.raises(pkg.AbsError):
+            ctx.set_tuning("ns_max_cluster", bad)
