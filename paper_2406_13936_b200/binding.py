@@ -350,7 +350,8 @@ class Context:
 
     def abs_orthogonalise(self, G, O, cfg, scratch, stream=None):
         """G, O: [count, rows, cols] or [rows, cols] device tensors (fp32 or bf16, last dim contiguous; O may be
-        G); cfg from make_ns_cfg; scratch from ns_scratch(count, rows, cols, cfg)."""
+        G); cfg from make_ns_cfg; scratch from ns_scratch(count, rows, cols, cfg).  Returns O."""
+        given = O
         if G.dim() == 2:
             G = G.unsqueeze(0)
         if O.dim() == 2:
@@ -363,7 +364,7 @@ class Context:
         self._check(self._lib.abs_orthogonalise(self._h, _ptr(G), _dtype_code(G), count, rows, cols, g_row, g_mat, _ptr(O),
                                                 _dtype_code(O), o_row, o_mat, ctypes.byref(cfg), _ptr(scratch),
                                                 scratch.numel(), _stream(stream)), "abs_orthogonalise")
-        return O
+        return given
 
     @staticmethod
     def _matrix_strides(G):
@@ -428,8 +429,8 @@ class Context:
 
     def abs_layer_norm(self, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
         """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight, bias: [M, d] (or [d]) fp32 or None; mean, rstd:
-        contiguous fp32 [M, rows] or None.  Y may be X."""
-        shape = X.shape
+        contiguous fp32 [M, rows] or None.  Y may be X.  Returns Y."""
+        shape, given = X.shape, Y
         if len(shape) == 2:
             X, Y = X.unsqueeze(0), Y.unsqueeze(0)
             weight, bias = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, bias))
@@ -446,7 +447,7 @@ class Context:
                                       _stream(stream))
         if rc != 0:
             self._check(rc, "abs_layer_norm")
-        return Y
+        return given
 
     def abs_layer_norm_backward(self, dY, X, mean, rstd, weight, dX=None, dW=None, dB=None, samples=1, Gw=None, Gb=None,
                                 stream=None):

@@ -4,6 +4,7 @@ import os
 import re
 
 import pytest
+import torch
 
 import paper_2406_13936_b200 as pkg
 from paper_2406_13936_b200 import binding
@@ -65,3 +66,29 @@ def test_scratch_of_any_number_is_enough_for_one(m, n, precision):
     """... which is the least that a call takes: whatever scratch was made for, fewer matrices can use it."""
     one = scratch(1, m, n, precision=precision)[1]
     assert all(scratch(count, m, n, precision=precision)[1] >= one for count in list(range(1, 120)) + [1000, 1 << 20])
+
+
+class _Library:
+    """Takes every call and does nothing."""
+
+    def __getattr__(self, name):
+        return lambda *args: 0
+
+
+def context():
+    """A context whose library does nothing; its device is the CPU's, so its tensors may be there."""
+    ctx = pkg.Context.__new__(pkg.Context)
+    ctx._lib, ctx._h, ctx.device = _Library(), None, -1
+    return ctx
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+def test_calls_return_the_tensor_that_they_were_given():
+    ctx, s = context(), _Stream()
+    for shape in ((4, 8), (2, 4, 8)):
+        x, y = torch.zeros(shape), torch.zeros(shape)
+        assert ctx.abs_layer_norm(x, None, None, 1e-5, y, stream=s) is y
+        assert ctx.abs_orthogonalise(x, y, pkg.make_ns_cfg(), torch.zeros(10, dtype=torch.uint8), stream=s) is y
