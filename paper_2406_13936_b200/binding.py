@@ -380,6 +380,8 @@ class Context:
         contiguous; cfg from make_muon_cfg; scratch from ns_scratch(M * L, rows, cols, cfg.ns)."""
         if X.dim() == 3:
             X, Buf, Gb = X.unsqueeze(1), Buf.unsqueeze(1), Gb.unsqueeze(1)
+        if X.dim() != 4:
+            raise AbsError("X must be [M, L, rows, cols] or [M, rows, cols], got %s" % (tuple(X.shape),))
         M, L, rows, cols = X.shape
         strides = X.stride()
         if (cols > 1 and strides[3] != 1) or (rows > 1 and strides[2] != cols):

@@ -92,3 +92,10 @@ def test_calls_return_the_tensor_that_they_were_given():
         x, y = torch.zeros(shape), torch.zeros(shape)
         assert ctx.abs_layer_norm(x, None, None, 1e-5, y, stream=s) is y
         assert ctx.abs_orthogonalise(x, y, pkg.make_ns_cfg(), torch.zeros(10, dtype=torch.uint8), stream=s) is y
+
+
+@pytest.mark.parametrize("shape", [(8, 8), (8,), (1, 2, 2, 4, 4)])
+def test_muon_refuses_other_dimensions(shape):
+    x = torch.zeros(shape)
+    with pytest.raises(pkg.AbsError, match="M, L, rows, cols"):
+        context().local_muon_step(x, x, x, pkg.make_muon_cfg(0.1), torch.zeros(10, dtype=torch.uint8), stream=_Stream())
