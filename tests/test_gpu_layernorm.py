@@ -413,3 +413,62 @@ def test_one_gradient_of_many_short_samples(ctx, which):
     _, tw, tb = ref_backward(dy, x, mean, rstd, None, S)
     check_sum(G[:, :S], tw if which == "Gw" else tb, 2)
     assert bool((G[:, S:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 768), ("f32", 257), ("f32", 9000)])
+def test_in_a_graph(ctx, dtype, d):
+    """Forward and backward captured once, replayed on new inputs (rows in shared memory, in registers, of any width)."""
+    M, S, T = 2, 40, 9
+    x, dy = rows_of(51, M, S * T, d, dtype=dtype), rows_of(52, M, S * T, d, dtype=dtype)
+    w, b = params_of(53, M, d)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty((M, S * T), device="cuda") for _ in range(2))
+    dW, dB = (torch.empty((M, d), device="cuda") for _ in range(2))
+    G = torch.empty((M, S, 2 * d), device="cuda")
+    outputs = (y, dx, mean, rstd, dW, dB, G)
+
+    def run():
+        ctx.abs_layer_norm(x, w, b, EPS, y, mean, rstd)
+        ctx.abs_layer_norm_backward(dy, x, mean, rstd, w, dx, dW, dB, samples=S, Gw=G[:, :, :d], Gb=G[:, :, d:])
+
+    run()                                                # what a context does once is not captured
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in (54, 55):
+        x.copy_(rows_of(seed, M, S * T, d, dtype=dtype))
+        for t in outputs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in outputs]
+        run()
+        for got, want in zip(replayed, outputs):
+            assert torch.equal(got, want)
+    check_dx(dx, ref_backward(dy, x, mean, rstd, w, S)[0], x, dy, w, mean, rstd, dtype)
+
+
+# the last widths of the kernels that hold a row in one CTA and the first ones past them, aligned and not
+@pytest.mark.parametrize("dtype,d", [("f32", 6144), ("f32", 6148), ("f32", 9216), ("f32", 9220), ("bf16", 9216), ("bf16", 9224),
+                                     ("bf16", 12800), ("bf16", 12808), ("bf16", 18432), ("f32", 6143), ("f32", 6145), ("bf16", 6143),
+                                     ("bf16", 6146)])
+def test_widths_around_the_limits(ctx, dtype, d):
+    x, dy = rows_of(56, 2, 11, d, dtype=dtype), rows_of(57, 2, 11, d, dtype=dtype, scale=1e-2, shift=1e-3)
+    w, b = params_of(58, 2, d)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = (torch.empty((2, 11), device="cuda") for _ in range(2))
+    dW, dB = (torch.empty((2, d), device="cuda") for _ in range(2))
+    ctx.abs_layer_norm(x, w, b, EPS, y, mean, rstd)
+    ry, rm, rr = ref_forward(x, w, b)
+    k = (1 + rm.abs() * rr)[:, :, None]
+    xh = (ry - b.double()[:, None]).abs() + w.double().abs()[:, None]
+    tol = 24 * U * k * xh + 4 * U * b.double().abs()[:, None]
+    if dtype == "bf16":
+        tol = tol + V * ry.abs() * (1 + 4 * V)
+    assert bool(((y.double() - ry).abs() <= tol).all())
+    ctx.abs_layer_norm_backward(dy, x, mean, rstd, w, dx, dW, dB)
+    rdx, tw, tb = ref_backward(dy, x, mean, rstd, w, 1)
+    check_dx(dx, rdx, x, dy, w, mean, rstd, dtype)
+    check_sum(dW, tw, (1, 2))
+    check_sum(dB, tb, (1, 2))

@@ -123,6 +123,7 @@ def test_both_tile_shapes_repeat_their_bits_and_end_when_a_wait_runs_out(ctx, ti
 
 # Short sides around what changes the layout of a small matrix: 16 (columns of a product), 32 and 64 (copies of B), 128;
 # long sides with one CTA and clusters of 2 to 8, with a last CTA of few columns
+# (and, the wide ones of the last row, clusters of 10, 11 and 16)
 SMALL = [(7, 2048), (16, 250), (17, 259), (31, 513), (32, 1030), (33, 300), (64, 257), (64, 1799), (65, 140), (65, 260), (100, 90),
          (113, 400), (128, 1000), (128, 200), (18, 2474), (64, 4096), (86, 2085), (128, 2048), (97, 1300)]
 
@@ -410,3 +411,17 @@ def test_clusters_that_the_device_does_not_hold(ctx, m, n):
     for bad in (7, 17):
         with pytest.raises(pkg.AbsError):
             ctx.set_tuning("ns_max_cluster", bad)
+
+
+@pytest.mark.parametrize("count,m,n", [(100, 128, 500), (90, 10, 1024), (50, 64, 1000), (40, 100, 700), (300, 24, 40), (32, 18, 2474),
+                                       (33, 18, 2474), (4, 128, 2048), (5, 128, 2048)])
+def test_more_small_matrices_than_fit_at_a_time(ctx, count, m, n):
+    """Clusters of 4 to 16 CTAs in several waves; numbers on either side of what sends wide ones to the general path."""
+    G = matrices(47, count, m, n)
+    O = orthogonalise(ctx, G, precision="f32")
+    check(O, ref_ns(G), 2e-5)
+    assert torch.equal(O, orthogonalise(ctx, G, precision="f32"))
+    X, Buf, Gb = G.view(count, 1, m, n).clone(), torch.zeros((count, 1, m, n), device="cuda"), G.view(count, 1, m, n)
+    cfg = pkg.make_muon_cfg(1.0, nesterov=False, ns=pkg.make_ns_cfg(precision="f32"))
+    ctx.local_muon_step(X, Buf, Gb, cfg, ctx.ns_scratch(count, m, n, cfg.ns))
+    assert torch.equal(Buf[:, 0], G) and torch.equal(X[:, 0], G - O)
