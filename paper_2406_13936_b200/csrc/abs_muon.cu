@@ -151,7 +151,8 @@ ns_finish_kernel(const NsSource s, const NsTarget t, int q0, const NsBuffers w, 
   const long long zoff = z * w.ldx * w.m;
   const float bad = *flag ? __int_as_float(0x7fc00000) : 0.f;          // a product whose wait ran out: nothing is valid
   // Every load before the first store, which may be to the same place as far as the compiler knows, and few enough
-  // registers for five or six CTAs an SM: 32 of 768 x 768 in 34 us (Muon 49), without 51 (56).
+  // registers for five or six CTAs an SM: 32 of 768 x 768 in 34 us (Muon 49), without 51 (56).  (At five the Muon kernel has 48
+  // registers and spills 108 bytes a thread, with single elements 16; the times are with that.)
   const long long base = matrix_base(q0 + z, s.L, t.replica_stride, t.matrix_stride);
   float x0[kTileVecs][4];
 #pragma unroll

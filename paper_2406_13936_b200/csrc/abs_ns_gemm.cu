@@ -779,9 +779,12 @@ int launch_ns_steps(abs_ctx* ctx, const NsBuffers& w, int steps, float a, float 
   // what its SMs fetch), so a step of T1 or T2 tiles takes T1 / 148 or T2 / 74 of that time: pairs are up to twice as fast, less
   // what the last row and column blocks pad.  A larger tile has the longer epilogue, which counts where matrices are small
   // or few.  us a step, pairs and single CTAs (T1 / T2): 4096 x 4096 221, 353 (3.94); 2000 x 1500 40, 50 (3.87); 8 of
-  // 1024 x 1024 38, 48 (3.78); 14 of 768 x 768 33, 37 (3.71); 56 of 256 x 1024 34, 36 and 24 of 200 x 1000 26, 23 (3.67);
+  // 1024 x 1024 38, 48 (3.78); 14 of 768 x 768 33, 39 (3.71); 24 of 256 x 1024 24, 22 and of 200 x 1000 25, 22 (3.67);
   // 16 of 512 x 512 25, 24 (3.6); 8 of 784 x 1024 44, 43 (3.1); 64 of 300 x 520 54, 38 (2.25); and with fewer tiles than pairs
   // 1024 x 1024 40, 29.
+  // The limit of 3.7 is right for a few waves of tiles.  With many, pairs are better below it too, the more so the longer the
+  // products are, and this rule, which knows neither, gives these to single CTAs: 112 of 256 x 1024 61, 64, of 512 x 512 96, 117 and
+  // 24 of 784 x 1024 88, 135.
   auto tiles = [&](long long side) {
     const long long rb = (w.m + side - 1) / side, cb = (w.n + side - 1) / side;
     return w.Z * (rb * (rb + 1) + rb * cb);

@@ -9,13 +9,14 @@
 //                     receives all of them or, where that is too much, adds its share of the elements and sends it to all
 //   B = b A + c A A   every CTA for itself, in the place of A
 //   X <- a X + B X    every CTA its own columns; X is MN-major here, in the same memory
-// The rows of X are padded with zeros to 64 or 128, A has 128 rows.  All waits are bounded; when one runs out the
-// results of the matrix are NaN.
+// The rows of X are padded with zeros to 64 or 128, A has 128 rows.  The waits for products are bounded; when one runs out
+// the results of the matrix are NaN.  The cluster barriers have no limit of their own: every CTA of a cluster reaches each of
+// them, whether or not a wait of its own ran out before.
 //
-// Measured (B200): a step takes 1.8 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 3.9 for 8 of 10 x 1024 (of which 1 the
-// exchange), 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is
-// not steps (launch, momentum, norm, result) 5 to 12 us.  5 steps on 4 of 64 x 192 take 31 us, 8 of 10 x 1024 26 us;
-// with the launches of the general path (norm, split, steps, finish) 101 and 147.
+// Measured (B200): a step takes 1.7 us for one 8 x 8 matrix, 4.5 for 4 of 64 x 192, 3.7 for 8 of 10 x 1024 (8 CTAs each),
+// 13 for 8 of 128 x 512 (5 of them the exchange of 64 KB a CTA over the cluster); what is not steps (launch, momentum, norm,
+// result) 6 to 14 us.  A call of 5 steps takes 32.7 us on 4 of 64 x 192 (a Muon step 32.8) and 28.7 on 8 of 10 x 1024; with
+// the launches of the general path (norm, split, steps, finish) the Muon step took 101 and the orthogonalisation 147.
 #include "abs_ns.cuh"
 #include "abs_pipeline.cuh"
 
@@ -248,7 +249,7 @@ __device__ __forceinline__ void get8(uint32_t matrix, uint32_t block, bool tall,
 }
 
 // CLUSTER: several CTAs a matrix.  (A kernel of its own for one CTA: what it does not need is not in its way; 4 of
-// 64 x 192 30.8 us, 32.8 with one kernel for both.)
+// 64 x 192 32.8 us, 41.0 with one kernel for both.)
 template <bool CLUSTER>
 __global__ void __launch_bounds__(kThreadsS, 1)
 ns_small_kernel(const __grid_constant__ SmallParams p) {
@@ -682,15 +683,17 @@ bool plan_columns(int count, long long rows, long long cols, bool narrow, SmallP
   int most = narrow ? 128 : 256;                                 // columns of a CTA that fit beside A and the partial sums
   while (most > 64 && smem(most) + (n > most ? part : 0) > kSmallSmem) most -= 64;
   const long long C = (n + most - 1) / most;
-  // A cluster of more than 8 CTAs has a GPC of its own, so few matrices are under way at a time.  5 steps there and on the
-  // general path, us: 7 of 18 x 2474 (10 CTAs) 41, 243; 4 of 64 x 4000 (16) 62, 345; 3 of 86 x 2085 (11) 85, 128;
-  // 128 x 2048 (16) 105, 122; but 8 of 128 x 1500 (12) 195, 115.
+  // A cluster of more than 8 CTAs has a GPC of its own, so five to eight matrices are under way at a time.  5 steps there and
+  // on the general path, us.  Up to 64 rows: 18 x 2474 (10 CTAs), 8 matrices 41, 253, 16 81, 263, 32 123, 298, 48 201, 333,
+  // 64 245, 380; 64 x 4000 (16), 4 60, 355, 32 296, 464, 48 417, 544; 40 x 3000 (12), 32 240, 355, 64 477, 466: the limit
+  // of 32 is below where the two meet (about 64).  Up to 128 rows: 86 x 2085 (11), 5 matrices 83, 130, 8 164, 134; 128 x 2048 (16),
+  // 5 102, 127, 8 201, 131: the limit of 4 is below the first number that needs a second wave.
   if (C > kMaxCluster || (C > 8 && count > (m > 64 ? 4 : 32))) return false;
   p.C = static_cast<int>(C);                                     // with W as below every CTA has columns: n > (C - 1) W
   p.W = static_cast<int>(((n + C - 1) / C + 15) / 16 * 16);
   p.smem = smem(p.W);
   // Up to 20 KB of partial sums go to all CTAs, with one barrier a step; beyond that every CTA adds its share and sends it
-  // on, with two.  us a step that way and the other: 10 x 1024 on 4 CTAs (3 KB) 3.9, 4.4; 32 x 500 on 2 (9 KB) 4.2, 4.9;
+  // on, with two.  us a step that way and the other: 10 x 1024 as it would be on 4 CTAs (3 KB) 3.9, 4.4; 32 x 500 on 2 (9 KB) 4.2, 4.9;
   // 32 x 1000 on 4 (18 KB) 4.7, 5.0; 24 x 1500 on 6 (20 KB) 5.1, 5.1; 48 x 1000 on 4 (39 KB) 6.8, 6.4.
   p.gather = p.C * part <= 20 * 1024;
   if (p.C > 1) p.smem += p.gather ? 2 * p.C * part : part;
@@ -700,8 +703,10 @@ bool plan_columns(int count, long long rows, long long cols, bool narrow, SmallP
   *out = p;
   return true;
 }
-// With SMs to spare, CTAs of fewer columns, where there are several anyway: 8 of 10 x 1024 (8 CTAs for 4) 28.3 -> 27.1 us,
-// 64 x 1000 47.8 -> 43.6; 16 of 32 x 1000, whose 16 clusters of 8 do not fit at a time, 34 -> 64, 4 of 64 x 192 (2 for 1) 31.7 -> 35.4.
+// With SMs to spare, CTAs of fewer columns, where there are several anyway, us wide and narrow: 8 of 10 x 1024 (8 CTAs for 4) 30.8,
+// 28.7; of 64 x 1000 50, 42; of 100 x 700 (6 for 4) 73, 68; but 4 of 64 x 192 (2 for 1) 31.7, 35.4.  The limit of 64 CTAs is on the safe
+// side of how many clusters fit at a time: 10 of 64 x 1000 (80) 50, 43, 16 (128) 50, 82; 10 of 100 x 700 (60) 73, 71, 16 (96) 74, 75;
+// 20 of 64 x 640 (100, clusters of 5) 48, 41, 32 (160) 49, 80.
 bool plan_small(int count, long long rows, long long cols, SmallPlan* out) {
   if (!plan_columns(count, rows, cols, false, out)) return false;
   SmallPlan narrow;
