@@ -19,6 +19,12 @@
  *   abs_layer_norm, abs_layer_norm_backward
  *                      layer norm; its backward pass also gives per-sample gradient
  *                      rows of weight and bias for the test
+ *   abs_rms_norm, abs_rms_norm_backward
+ *                      root-mean-square norm with the residual's addition
+ *   abs_attention, abs_attention_backward
+ *                      causal attention with grouped heads over packed sequences
+ *   abs_embedding, abs_embedding_backward
+ *                      token embedding of the replicas
  *
  * Conventions
  *   - Every function returns an int: ABS_OK (0) or a negative ABS_ERR_* code.
@@ -589,6 +595,116 @@ typedef struct {
 int abs_plan_layer_norm_backward(abs_dtype dtype, int M, long long samples, long long tokens, long long d, int aligned,
                                  int with_gw, int with_gb, int with_totals, int sm_count, size_t workspace_bytes,
                                  abs_ln_backward_plan* out);
+
+/* ---- root-mean-square norm -----------------------------------------------------------------
+ * Rows of d features, fp32 or bf16, for M replicas with a weight of their own (fp32):
+ *   h_j = x_j + r_j (rounded to the type once; h = x without R),
+ *   rstd = 1 / sqrt( (1/d) sum_j h_j^2 + eps ),   y_j = h_j rstd weight_j
+ *   X, R, H, Y  row r of replica m at + m*worker_stride + r*row_stride (>= d; replicas disjoint; the
+ *               worker strides are ignored for M == 1).  R (the residual stream) and H (its new
+ *               value) are NULL or of X's type.  H may be R or X, Y may be X (same strides each).
+ *   Q, scales   NULL, or the rows in 8 bits (e4m3, one byte an element, strides in bytes) and
+ *               [M][rows] fp32: scales = max_j |y_j| / 448 (1 for a row of zeros), Q = y / scales
+ *               rounded to nearest.  Y may be NULL then.  A row with a NaN or an infinity gives
+ *               NaN scales and NaN in Q.
+ *   weight      replica m at + m*param_stride (0: all replicas share it), or NULL (ones)
+ *   rstd        [M][rows] fp32 for the backward pass, or NULL
+ *   rows may be 0.  Sums and y are fp32; y is rounded once.                                     */
+int abs_rms_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int M, long long rows, long long d,
+                 long long x_row_stride, long long x_worker_stride, const void* R, long long r_row_stride,
+                 long long r_worker_stride, void* H, long long h_row_stride, long long h_worker_stride,
+                 const float* weight, long long param_stride, float eps, void* Y, long long y_row_stride,
+                 long long y_worker_stride, void* Q, long long q_row_stride, long long q_worker_stride, float* scales,
+                 float* rstd, void* stream);
+
+/* Its backward pass.  A replica's rows are `samples` samples of `tokens` consecutive rows.  With
+ * xh = h rstd and a = weight dy:
+ *   dx = dh + rstd ( a - xh (1/d) sum_j a_j xh_j )      (the gradient of X and of R alike)
+ *   per-sample gradients:  Gw[i] = sum_t dy xh          at + m*g_worker_stride + i*g_row_stride
+ *   and their sum over the samples, dW, at + m*grad_stride.
+ * dH: the gradient that reaches the residual stream behind the norm, or NULL (zero).  dX, dW and Gw may each
+ * be NULL.  dX may be dY, H or dH (same strides).  samples and tokens may be 0 (sums of nothing are
+ * zero).  H: what was normalised; rstd as the forward pass wrote it.  All sums are fp32 in a fixed order:
+ * repeated calls give the same bits.  Uses the context's workspace as far as it goes.              */
+int abs_rms_norm_backward(abs_ctx* ctx, const void* dY, long long dy_row_stride, long long dy_worker_stride,
+                          const void* H, long long h_row_stride, long long h_worker_stride, const void* dH,
+                          long long dh_row_stride, long long dh_worker_stride, abs_dtype dtype, int M, long long samples,
+                          long long tokens, long long d, const float* rstd, const float* weight,
+                          long long param_stride, void* dX, long long dx_row_stride, long long dx_worker_stride,
+                          float* dW, long long grad_stride, float* Gw, long long g_row_stride,
+                          long long g_worker_stride, void* stream);
+
+/* ---- attention -------------------------------------------------------------------------------
+ * Causal attention with grouped heads over packed sequences, fp32 or bf16.  The tokens of all sequences (of all
+ * replicas, where there are several) are rows of one tensor, total of them; sequence i has the rows offsets[i] to
+ * offsets[i+1] - 1.  Row t of a sequence sees the rows of that sequence up to its own; query head h reads the
+ * keys and values of head h / (q_heads / kv_heads):
+ *   s_tj = scale <q_t, k_j>,  lse_t = log sum_j exp(s_tj),  o_t = sum_j exp(s_tj - lse_t) v_j
+ * Rows outside all sequences (in front of the first, behind the last) are neither computed nor written, and nothing in
+ * them reaches a result; neither do the rows of one sequence reach another's.  Inside a sequence an infinity or a NaN in V
+ * (backward: in Q, K, V, dO) may reach earlier rows than its own.
+ * Sequences may be empty.  head_dim <= 128.
+ *
+ * A tensor is a HOST struct: token t, head h at data + t*row_stride + h*head_stride, head_dim contiguous elements, no two
+ * of these overlapping.  Views of a fused [total][(q_heads + 2 kv_heads) head_dim] tensor are such tensors.
+ * bf16 runs on the tensor cores where every tensor's base and strides are multiples of 16 bytes and head_dim is one of 8
+ * elements; other layouts and fp32 run on the CUDA cores.                                          */
+typedef struct {
+  void* data;
+  long long row_stride;
+  long long head_stride;
+} abs_heads;   /* 24 bytes */
+
+/* The plan of a batch: the tiles of its sequences in the order in which they are worked off.  Made once a batch, read by
+ * the calls of every layer.  offsets: DEVICE int32 [sequences + 1]; values outside [0, total] are clamped and one
+ * below its predecessor is raised to it, which sets the plan's third int32 to 1 (else 0).  plan: device memory of
+ * abs_attention_plan_bytes, 16-byte aligned.  A plan for other offsets of as many sequences and the same total may be written over it, also
+ * between replays of a graph that captured the calls that read it.
+ * sequences <= 2^24, total <= 2^30.                                                                  */
+int abs_attention_plan_bytes(int sequences, long long total, size_t* out);
+int abs_attention_plan(abs_ctx* ctx, const int* offsets, int sequences, long long total, void* plan, size_t plan_bytes,
+                       void* stream);
+
+/* lse: fp32 [q_heads][total], or NULL.  q_heads <= 4096 and total * q_heads <= 2^32.  O overlaps no input.     */
+int abs_attention(abs_ctx* ctx, const abs_heads* Q, const abs_heads* K, const abs_heads* V, abs_dtype dtype, const void* plan,
+                  int sequences, long long total, int q_heads, int kv_heads, int head_dim, float scale, const abs_heads* O,
+                  float* lse, void* stream);
+
+/* Its backward pass.  O, lse: as the forward pass wrote them.  With p_tj = exp(s_tj - lse_t):
+ *   ds_tj = p_tj (<do_t, v_j> - <do_t, o_t>)
+ *   dv_j = sum_t p_tj do_t,   dk_j = scale sum_t ds_tj q_t,   dq_t = scale sum_j ds_tj k_j
+ * with the sums over t of dk and dv running over all query heads of the group.  Sums are fp32 in a fixed order:
+ * repeated calls give the same bits.  The outputs overlap no input and not one another.
+ * scratch: device memory of abs_attention_scratch_bytes, 256-byte aligned; calls that may overlap have scratch of their own.  */
+int abs_attention_scratch_bytes(long long total, int q_heads, int kv_heads, int head_dim, int sequences, size_t* out);
+int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const abs_heads* Q, const abs_heads* K, const abs_heads* V,
+                           const abs_heads* O, const float* lse, abs_dtype dtype, const void* plan, int sequences,
+                           long long total, int q_heads, int kv_heads, int head_dim, float scale, const abs_heads* dQ,
+                           const abs_heads* dK, const abs_heads* dV, void* scratch, size_t scratch_bytes, void* stream);
+
+/* ---- token embedding -------------------------------------------------------------------------
+ * y_t = scale E[token_t], rounded once to Y's type (fp32 or bf16).
+ *   E       [M] fp32 tables of vocab rows of d: row v of replica m at + m*e_worker_stride + v*e_row_stride
+ *           (>= d).  e_worker_stride 0: all replicas share one table.
+ *   tokens  int32, token t of replica m at + m*tokens_stride + t (0: all replicas share them).  A token outside
+ *           [0, vocab) gives a row of zeros and no gradient.
+ *   Y       row t of replica m at + m*y_worker_stride + t*y_row_stride
+ * Worker strides are ignored for M == 1.  rows may be 0.                                            */
+int abs_embedding(abs_ctx* ctx, const float* E, int M, long long vocab, long long d, long long e_row_stride,
+                  long long e_worker_stride, const int* tokens, long long tokens_stride, long long rows, float scale, void* Y,
+                  abs_dtype y_dtype, long long y_row_stride, long long y_worker_stride, void* stream);
+
+/* Its backward pass: dE[v] = scale sum_{t: token_t = v} dy_t for every row v of every replica's table, zeros for
+ * tokens that do not occur; accumulate != 0: added to what dE holds (rows of other tokens are not touched).
+ * The tokens are sorted on the way; sums are fp32 in a fixed order: repeated calls give the same bits.
+ * dE: fp32, replica m at + m*e_worker_stride (replicas disjoint).  scratch: device memory of
+ * abs_embedding_scratch_bytes, 256-byte aligned; calls that may overlap have scratch of their own.
+ * vocab < 2^24, d <= 2^24, rows <= 2^28, M <= 65535, M * rows <= 2^31, M * vocab <= 2^36 (of the forward pass too).  */
+int abs_embedding_scratch_bytes(int M, long long rows, long long vocab, long long d, size_t* out);
+int abs_embedding_backward(abs_ctx* ctx, const void* dY, abs_dtype dtype, int M, long long rows, long long d,
+                           long long dy_row_stride, long long dy_worker_stride, const int* tokens, long long tokens_stride,
+                           long long vocab, float scale, float* dE, long long e_row_stride, long long e_worker_stride,
+                           int accumulate, void* scratch, size_t scratch_bytes, void* stream);
 
 /* Three-layer ReLU MLP with softmax cross-entropy (the second synthetic problem).
  * dims = {n0, n1, n2, n3} layer widths.  One replica's parameters are a flat fp32

@@ -66,6 +66,10 @@ class LnBackwardPlan(ctypes.Structure):
                 ("room", ctypes.c_longlong), ("needed", ctypes.c_longlong), ("used", ctypes.c_longlong)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong)]
+
+
 class StatsPlan(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int) for name in
                 ("route", "lanes_per_row", "warps_per_box", "boxes_per_stage", "stages", "box_rows", "row_boxes",
@@ -169,6 +173,37 @@ EXPORTS = {
     "abs_plan_layer_norm_backward": [ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
                                      ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_size_t,
                                      ctypes.POINTER(LnBackwardPlan)],
+    "abs_rms_norm": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong,
+                     ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
+                     ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_float,
+                     ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong,
+                     ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
+    "abs_rms_norm_backward": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p,
+                              ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
+                              ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
+                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong,
+                              ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong,
+                              ctypes.c_longlong, ctypes.c_void_p],
+    "abs_attention_plan_bytes": [ctypes.c_int, ctypes.c_longlong, ctypes.POINTER(ctypes.c_size_t)],
+    "abs_attention_plan": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_size_t,
+                           ctypes.c_void_p],
+    "abs_attention": [ctypes.c_void_p] + [ctypes.POINTER(Heads)] * 3 + [ctypes.c_int, ctypes.c_void_p, ctypes.c_int,
+                      ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.POINTER(Heads),
+                      ctypes.c_void_p, ctypes.c_void_p],
+    "abs_attention_scratch_bytes": [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                    ctypes.POINTER(ctypes.c_size_t)],
+    "abs_attention_backward": [ctypes.c_void_p] + [ctypes.POINTER(Heads)] * 5 + [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p,
+                               ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_float] +
+                              [ctypes.POINTER(Heads)] * 3 + [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+    "abs_embedding": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
+                      ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_float, ctypes.c_void_p,
+                      ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p],
+    "abs_embedding_scratch_bytes": [ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_longlong,
+                                    ctypes.POINTER(ctypes.c_size_t)],
+    "abs_embedding_backward": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_longlong, ctypes.c_longlong,
+                               ctypes.c_longlong, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong,
+                               ctypes.c_float, ctypes.c_void_p, ctypes.c_longlong, ctypes.c_longlong, ctypes.c_int,
+                               ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
 }
 
 _lib = None
@@ -424,10 +459,10 @@ class Context:
         return d if stride is None else stride
 
     @staticmethod
-    def _statistics(mean, rstd, n):
+    def _statistics(mean, rstd, n, what="mean and rstd"):
         for t in (mean, rstd):
             if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
-                raise AbsError("mean and rstd must be contiguous float32 tensors of %d values" % n)
+                raise AbsError("%s must be contiguous float32 tensors of %d values" % (what, n))
 
     def abs_layer_norm(self, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
         """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight, bias: [M, d] (or [d]) fp32 or None; mean, rstd:
@@ -492,6 +527,213 @@ class Context:
             _ptr(dW), _ptr(dB), grad_stride, _ptr(Gw), _ptr(Gb), g_rs, g_ws, _stream(stream))
         if rc != 0:
             self._check(rc, "abs_layer_norm_backward")
+
+    # ---- root-mean-square norm -------------------------------------------------------------------
+    def abs_rms_norm(self, X, weight, eps, Y, residual=None, summed=None, rstd=None, Q=None, scales=None, stream=None):
+        """X, Y: [M, rows, d] (or [rows, d]) fp32 or bf16; weight: [M, d] (or [d]) fp32 or None.  residual: added to X first, of
+        X's shape and type; summed: takes the sum (may be residual or X).  rstd: contiguous fp32 [M, rows] or None.  Q
+        (float8_e4m3fn or uint8, X's shape) and scales (contiguous fp32 [M, rows]): the rows in 8 bits; Y may be None then.
+        Returns Y, or Q without it."""
+        shape, dtype, given = X.shape, X.dtype, Y if Y is not None else Q
+        if len(shape) == 2:
+            X, Y, residual, summed, Q = (t if t is None else t.unsqueeze(0) for t in (X, Y, residual, summed, Q))
+            if weight is not None and weight.dim() == 1:
+                weight = weight.unsqueeze(0)
+            shape = X.shape
+        if len(shape) != 3:
+            raise AbsError("X must be [M, rows, d] or [rows, d], got %s" % (tuple(shape),))
+        M, rows, d = shape
+        strides = []
+        for what, t in (("X", X), ("residual", residual), ("summed", summed), ("Y", Y)):
+            if t is None:
+                strides += [None, d, d * rows]
+            else:
+                if t.shape != shape or t.dtype != dtype:
+                    raise AbsError("X, residual, summed and Y must be [M, rows, d] of one type")
+                strides += [t.data_ptr(), *self._rows(t, M, rows, d, what)]
+        if Y is None and Q is None:
+            raise AbsError("Y or Q must be given")
+        if (Q is None) != (scales is None):
+            raise AbsError("Q and scales go together")
+        q = (None, d, d * rows)
+        if Q is not None:
+            if Q.shape != shape or Q.dtype not in (torch.float8_e4m3fn, torch.uint8):
+                raise AbsError("Q must be float8_e4m3fn (or uint8) of X's shape")
+            q = (Q.data_ptr(), *self._rows(Q, M, rows, d, "Q"))
+        p_stride = self._same_stride(weight, None, M, d, "weight")
+        self._statistics(rstd, scales, M * rows, "rstd and scales")
+        rc = self._lib.abs_rms_norm(self._h, strides[0], _dtype_code(X), M, rows, d, *strides[1:9], _ptr(weight), p_stride, eps,
+                                    *strides[9:], *q, _ptr(scales), _ptr(rstd), _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_rms_norm")
+        return given
+
+    def abs_rms_norm_backward(self, dY, H, rstd, weight, dX=None, dH=None, dW=None, samples=1, Gw=None, stream=None):
+        """dY, H, dX, dH: [M, samples * tokens, d] (or [rows, d]) of one type; H: what was normalised (the sum, where there was
+        a residual); dH: the gradient that reaches the sum past the norm, or None; rstd as abs_rms_norm wrote it; weight [M, d] or
+        None.  dW: fp32 [M, d]; Gw: fp32 [M, samples, d] per-sample gradients (rows that abs_test_stats takes).  Every output
+        may be None."""
+        shape, dtype = H.shape, H.dtype
+        if len(shape) == 2:
+            dY, H, dX, dH = (t if t is None else t.unsqueeze(0) for t in (dY, H, dX, dH))
+            weight, dW = (t if t is None or t.dim() == 2 else t.unsqueeze(0) for t in (weight, dW))
+            Gw = Gw if Gw is None or Gw.dim() == 3 else Gw.unsqueeze(0)
+            shape = H.shape
+        if len(shape) != 3:
+            raise AbsError("H must be [M, rows, d] or [rows, d], got %s" % (tuple(shape),))
+        M, rows, d = shape
+        samples = int(samples)
+        if samples < 0 or (samples == 0 and rows) or (samples and rows % samples):
+            raise AbsError("%d rows are not %d samples of equal length" % (rows, samples))
+        args = []
+        for what, t in (("dY", dY), ("H", H), ("dH", dH), ("dX", dX)):
+            if t is None:
+                args.append((None, d, d * rows))
+            else:
+                if t.shape != shape or t.dtype != dtype:
+                    raise AbsError("dY, H, dH and dX must be [M, rows, d] of one type")
+                args.append((t.data_ptr(), *self._rows(t, M, rows, d, what)))
+        p_stride = self._same_stride(weight, None, M, d, "weight")
+        grad_stride = self._same_stride(dW, None, M, d, "dW")
+        self._statistics(rstd, None, M * rows, "rstd")
+        g = (None, d, d * samples)
+        if Gw is not None:
+            if Gw.dtype != torch.float32 or Gw.shape != (M, samples, d):
+                raise AbsError("Gw must be float32 [%d, %d, %d]" % (M, samples, d))
+            g = (Gw.data_ptr(), *self._rows(Gw, M, samples, d, "Gw"))
+        rc = self._lib.abs_rms_norm_backward(self._h, *args[0], *args[1], *args[2], _dtype_code(H), M, samples,
+                                             rows // samples if samples else 0, d, _ptr(rstd), _ptr(weight), p_stride, *args[3],
+                                             _ptr(dW), grad_stride, *g, _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_rms_norm_backward")
+
+    # ---- attention -------------------------------------------------------------------------------
+    def attention_plan(self, offsets, total, plan=None, stream=None):
+        """The plan of a batch of packed sequences: offsets int32 device tensor [sequences + 1], sequence i has the rows
+        offsets[i] .. offsets[i + 1] - 1 of `total`.  Every layer's abs_attention and abs_attention_backward take it.  plan: an
+        earlier plan of as many sequences and the same total to write over.  Returns the plan."""
+        if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.numel() < 1 or not offsets.is_contiguous():
+            raise AbsError("offsets must be a contiguous int32 tensor [sequences + 1]")
+        n, total = offsets.numel() - 1, int(total)
+        need = ctypes.c_size_t()
+        rc = self._lib.abs_attention_plan_bytes(n, total, ctypes.byref(need))
+        if rc != 0:
+            raise AbsError("abs_attention_plan_bytes failed (%d): %s" % (rc, self._lib.abs_last_error(None).decode()))
+        if plan is None:
+            plan = AttentionPlan(torch.empty(need.value // 4, dtype=torch.int32, device="cuda:%d" % self.device), n, total)
+        elif plan.sequences != n or plan.total != total:
+            raise AbsError("the plan is for %d sequences and %d rows" % (plan.sequences, plan.total))
+        self._check(self._lib.abs_attention_plan(self._h, _ptr(offsets), n, total, _ptr(plan.words), plan.words.numel() * 4,
+                                                 _stream(stream)), "abs_attention_plan")
+        return plan
+
+    def attention_scratch(self, total, q_heads, kv_heads, head_dim, sequences):
+        """Device scratch tensor (uint8) for abs_attention_backward."""
+        out = ctypes.c_size_t()
+        rc = self._lib.abs_attention_scratch_bytes(int(total), int(q_heads), int(kv_heads), int(head_dim), int(sequences),
+                                                   ctypes.byref(out))
+        if rc != 0:
+            raise AbsError("abs_attention_scratch_bytes failed (%d): %s" % (rc, self._lib.abs_last_error(None).decode()))
+        return torch.empty(out.value, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    @staticmethod
+    def _heads(t, what, shape, dtype):
+        if t.shape != shape or t.dtype != dtype:
+            raise AbsError("%s must be %s of type %s, got %s of %s" % (what, tuple(shape), dtype, tuple(t.shape), t.dtype))
+        row, head, one = t.stride()
+        if one != 1 and shape[2] > 1:
+            raise AbsError("the last dimension of %s must be contiguous" % what)
+        if shape[1] == 1:                                  # the strides of dimensions of one element are free
+            head = shape[2]
+        if shape[0] == 1:
+            row = head * shape[1]
+        return Heads(t.data_ptr(), row, head)
+
+    def _attention_shapes(self, Q, K, plan, lse):
+        if Q.dim() != 3 or K.dim() != 3:
+            raise AbsError("Q and K must be [total, heads, head_dim], got %s and %s" % (tuple(Q.shape), tuple(K.shape)))
+        total, hq, hd = Q.shape
+        if plan.total != total:
+            raise AbsError("the plan is for %d rows, Q has %d" % (plan.total, total))
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != (hq, total) or not lse.is_contiguous()):
+            raise AbsError("lse must be a contiguous float32 tensor [%d, %d]" % (hq, total))
+        return total, hq, K.shape[1], hd
+
+    def abs_attention(self, Q, K, V, plan, O, lse=None, scale=None, stream=None):
+        """Causal attention over packed sequences.  Q, O: [total, q_heads, head_dim], K, V: [total, kv_heads, head_dim], fp32 or
+        bf16, the last dimension contiguous (views of a fused tensor are fine); plan from attention_plan; lse: contiguous fp32
+        [q_heads, total] for the backward pass, or None; scale: 1 / sqrt(head_dim) by default.  Returns O."""
+        total, hq, hk, hd = self._attention_shapes(Q, K, plan, lse)
+        kv = (total, hk, hd)
+        q, k, v, o = (self._heads(t, what, shape, Q.dtype) for t, what, shape in
+                      ((Q, "Q", Q.shape), (K, "K", kv), (V, "V", kv), (O, "O", Q.shape)))
+        rc = self._lib.abs_attention(self._h, q, k, v, _dtype_code(Q), plan.words.data_ptr(), plan.sequences, total, hq, hk, hd,
+                                     hd ** -0.5 if scale is None else scale, o, _ptr(lse), _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_attention")
+        return O
+
+    def abs_attention_backward(self, dO, Q, K, V, O, lse, plan, dQ, dK, dV, scratch, scale=None, stream=None):
+        """Gradients of abs_attention: dO, dQ like Q, dK and dV like K; O and lse as the forward pass wrote them; scratch from
+        attention_scratch."""
+        if lse is None:
+            raise AbsError("the backward pass needs lse")
+        total, hq, hk, hd = self._attention_shapes(Q, K, plan, lse)
+        q, kv = Q.shape, (total, hk, hd)
+        do, q_, k, v, o, dq, dk, dv = (self._heads(t, what, shape, Q.dtype) for t, what, shape in
+                                       ((dO, "dO", q), (Q, "Q", q), (K, "K", kv), (V, "V", kv), (O, "O", q), (dQ, "dQ", q),
+                                        (dK, "dK", kv), (dV, "dV", kv)))
+        rc = self._lib.abs_attention_backward(self._h, do, q_, k, v, o, lse.data_ptr(), _dtype_code(Q), plan.words.data_ptr(),
+                                              plan.sequences, total, hq, hk, hd, hd ** -0.5 if scale is None else scale, dq, dk, dv,
+                                              scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_attention_backward")
+
+    # ---- token embedding ---------------------------------------------------------------------------
+    def _embedding_shapes(self, E, tokens, Y, what):
+        if E.dim() == 2:
+            E, Y = E.unsqueeze(0), Y.unsqueeze(0)
+            tokens = tokens.unsqueeze(0) if tokens.dim() == 1 else tokens
+        if E.dim() != 3 or Y.dim() != 3 or E.dtype != torch.float32 or Y.shape[0] != E.shape[0] or Y.shape[2] != E.shape[2]:
+            raise AbsError("%s must be float32 [M, vocab, d] and the rows [M, rows, d]" % what)
+        M, vocab, d = E.shape
+        rows = Y.shape[1]
+        if tokens.shape != (M, rows) or tokens.dtype != torch.int32 or (rows > 1 and tokens.stride(1) != 1):
+            raise AbsError("tokens must be int32 [%d, %d] with contiguous rows" % (M, rows))
+        e_rs, e_ws = self._rows(E, M, vocab, d, what)
+        y_rs, y_ws = self._rows(Y, M, rows, d, "the rows")
+        return E, Y, M, vocab, d, rows, e_rs, e_ws, y_rs, y_ws, tokens.stride(0) if M > 1 else rows
+
+    def abs_embedding(self, E, tokens, Y, scale=1.0, stream=None):
+        """Y[m, t] = scale E[m, tokens[m, t]]: E fp32 [M, vocab, d] (or [vocab, d]; expanded over M: all replicas share it),
+        tokens int32 [M, rows], Y fp32 or bf16 [M, rows, d].  Tokens outside the table give zeros.  Returns Y."""
+        given = Y
+        E, Y, M, vocab, d, rows, e_rs, e_ws, y_rs, y_ws, t_ws = self._embedding_shapes(E, tokens, Y, "E")
+        rc = self._lib.abs_embedding(self._h, E.data_ptr(), M, vocab, d, e_rs, e_ws, tokens.data_ptr(), t_ws, rows, scale,
+                                     Y.data_ptr(), _dtype_code(Y), y_rs, y_ws, _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_embedding")
+        return given
+
+    def embedding_scratch(self, M, rows, vocab, d):
+        """Device scratch tensor (uint8) for abs_embedding_backward."""
+        out = ctypes.c_size_t()
+        rc = self._lib.abs_embedding_scratch_bytes(int(M), int(rows), int(vocab), int(d), ctypes.byref(out))
+        if rc != 0:
+            raise AbsError("abs_embedding_scratch_bytes failed (%d): %s" % (rc, self._lib.abs_last_error(None).decode()))
+        return torch.empty(out.value, dtype=torch.uint8, device="cuda:%d" % self.device)
+
+    def abs_embedding_backward(self, dY, tokens, dE, scratch, scale=1.0, accumulate=False, stream=None):
+        """Gradient of abs_embedding's table: dY [M, rows, d], dE fp32 [M, vocab, d], written whole (accumulate: added to);
+        scratch from embedding_scratch.  Returns dE."""
+        given = dE
+        dE, dY, M, vocab, d, rows, e_rs, e_ws, y_rs, y_ws, t_ws = self._embedding_shapes(dE, tokens, dY, "dE")
+        rc = self._lib.abs_embedding_backward(self._h, dY.data_ptr(), _dtype_code(dY), M, rows, d, y_rs, y_ws, tokens.data_ptr(), t_ws,
+                                              vocab, scale, dE.data_ptr(), e_rs, e_ws, int(bool(accumulate)), scratch.data_ptr(),
+                                              scratch.numel() * scratch.element_size(), _stream(stream))
+        if rc != 0:
+            self._check(rc, "abs_embedding_backward")
+        return given
 
     # ---- producers and rounds ----------------------------------------------------------------
     def abs_logreg_grads(self, A, y, idx, X, b, G, stream=None):
@@ -632,6 +874,13 @@ class Context:
     def replica_average(self, X, stream=None):
         X2, M, d, stride = self._replicas(X)
         self._check(self._lib.replica_average(self._h, _ptr(X2), M, d, stride, _stream(stream)), "replica_average")
+
+
+class AttentionPlan:
+    """A batch's plan on the device (Context.attention_plan)."""
+
+    def __init__(self, words, sequences, total):
+        self.words, self.sequences, self.total = words, sequences, total
 
 
 def abs_test_stats_noalloc(G, stats_out, gbar_out=None, stream=None):

@@ -1,0 +1,87 @@
+// Causal attention over packed sequences: what the host side and plan (abs_attention.cu), the CUDA-core kernels
+// (abs_attention_any.cu) and the tensor-core kernels (abs_attention_fwd.cu, abs_attention_bwd.cu) share.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "abs_internal.cuh"
+
+namespace absk {
+
+constexpr int kAttnMaxHead = 128;
+constexpr int kAttnFwdRows = 256;          // query rows of a forward tile
+constexpr int kAttnBwdRows = 128;          // keys of a backward tile
+constexpr int kAttnFlagWord = 9;           // word of abs_ctx::flags that a kernel whose wait ran out sets (cleared by every call)
+
+// The plan of a batch, int32 words on the device: the header, then the records of the forward and of the backward tiles in
+// the order in which they are worked off, then what the plan's own kernel needs.
+//   record: first row and end of the tile's sequence, number of the tile in the sequence, 0
+struct AttnPlanLayout {
+  long long fwd, bwd, starts, counts, words;   // places of the parts, and their end
+  int fwd_cap, bwd_cap, bins;
+};
+enum { kPlanFwdTiles = 0, kPlanBwdTiles = 1, kPlanBad = 2, kPlanTotal = 3, kPlanHeader = 16 };
+inline AttnPlanLayout attn_plan_layout(int n, int total) {
+  AttnPlanLayout l;
+  l.fwd_cap = total / kAttnFwdRows + n;
+  l.bwd_cap = total / kAttnBwdRows + n;
+  l.bins = total / kAttnBwdRows + 2;           // tiles of one sequence: 0 to bins - 1
+  l.fwd = kPlanHeader;
+  l.bwd = l.fwd + 4ll * l.fwd_cap;
+  l.starts = l.bwd + 4ll * l.bwd_cap;
+  l.counts = l.starts + n + 1;
+  l.words = l.counts + 6ll * (l.bins + 1);
+  l.words = (l.words + 3) & ~3ll;
+  return l;
+}
+
+// One tensor's rows: row r, head h at p + r * row + h * head.
+struct AttnRows {
+  const void* p;
+  long long row, head;
+};
+struct AttnOut {
+  void* p;
+  long long row, head;
+};
+struct AttnForward {
+  AttnRows q, k, v;
+  AttnOut o;
+  float* lse;                                  // [hq][total] or NULL
+  const int* plan;
+  int n, total, hq, hk, hd;
+  float scale;
+};
+struct AttnBackward {
+  AttnRows dout, q, k, v, o;
+  const float* lse;
+  const int* plan;
+  AttnOut dq, dk, dv;
+  int n, total, hq, hk, hd;
+  float scale;
+  void* scratch;
+  size_t scratch_bytes;
+};
+
+// Scratch of a backward pass: delta [hq][total] fp32, then, for the tensor-core kernel, the sums of dq [total][hq][dpad] fp32 and
+// a counter for each 128 rows of a sequence and head.
+struct AttnScratch {
+  size_t delta, sums, counters, bytes;
+  int dpad;
+};
+inline AttnScratch attn_scratch(int total, int hq, int hd, int n) {
+  AttnScratch s;
+  s.dpad = hd <= 64 ? 64 : 128;
+  s.delta = 0;
+  s.sums = (static_cast<size_t>(hq) * total * sizeof(float) + 255) & ~static_cast<size_t>(255);
+  s.counters = s.sums + static_cast<size_t>(total) * hq * s.dpad * sizeof(float);
+  s.counters = (s.counters + 255) & ~static_cast<size_t>(255);
+  s.bytes = s.counters + static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) * sizeof(unsigned);
+  s.bytes = (s.bytes + 255) & ~static_cast<size_t>(255);
+  return s;
+}
+
+int launch_attention_any(abs_ctx* ctx, const AttnForward& a, abs_dtype dtype, cudaStream_t st);
+int launch_attention_any_backward(abs_ctx* ctx, const AttnBackward& a, abs_dtype dtype, cudaStream_t st);
+
+}  // namespace absk

@@ -1,0 +1,374 @@
+"""Causal attention over packed sequences against its definition in 64 bits.
+
+Tolerances are sums of absolute values, element by element, with u = 2^-24 (fp32) and w = 2^-8 (bf16), the largest relative error
+of a rounding:
+  scores        a dot product of hd terms in fp32 is off by at most (hd + 2) u sum |q k|; the exponent carries that, and the
+                rounding of its argument (magnitude up to 2 max |s|), so a weight p is off by e_p = that + 8 u relative to itself
+  o             sum_j p |v| (2 e_p + n u), and w sum_j p |v| where the weights are rounded to bf16 for the tensor cores
+  ds            p (|dp - delta| e_p + (hd + 2) u (sum |do v| + sum |do o|)), and w |ds| where it is rounded to bf16
+  sums over n rows or keys: n u times the sum of magnitudes
+and half a step of the output's type.  Sums of n terms are taken to be off by n u, which no order of additions exceeds.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2406_13936_b200 as pkg
+
+pytestmark = pytest.mark.gpu
+U, W = 2.0 ** -24, 2.0 ** -8
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = pkg.Context(0)
+    yield c
+    c.close()
+
+
+class Batch:
+    """Packed inputs: `front` rows before the first sequence, `tail` behind the last, views of one fused tensor."""
+
+    def __init__(self, lens, hq, hk, hd, dtype, seed=0, front=0, tail=0, amp=1.0, pad=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        self.lens, self.hq, self.hk, self.hd, self.dtype = lens, hq, hk, hd, TYPES[dtype]
+        self.total = front + sum(lens) + tail
+        start = [front]
+        for n in lens:
+            start.append(start[-1] + n)
+        self.start = start
+        self.offsets = torch.tensor(start, dtype=torch.int32, device="cuda")
+        self.fused = (amp * torch.randn((self.total, (hq + 2 * hk) * hd + pad), device="cuda", generator=gen)).to(self.dtype)
+        width = (hq + 2 * hk) * hd
+        heads = self.fused[:, :width].view(self.total, hq + 2 * hk, hd) if pad == 0 else self.fused[:, :width].unflatten(1, (hq + 2 * hk, hd))
+        self.q, self.k, self.v = heads[:, :hq], heads[:, hq:hq + hk], heads[:, hq + hk:]
+        self.do = (0.1 * torch.randn((self.total, hq, hd), device="cuda", generator=gen)).to(self.dtype)
+        self.scale = hd ** -0.5
+
+    def outputs(self, fill=7.0):
+        o = torch.full((self.total, self.hq, self.hd), fill, device="cuda", dtype=self.dtype)
+        lse = torch.full((self.hq, self.total), fill, device="cuda")
+        return o, lse
+
+    def gradients(self, fill=7.0):
+        width = (self.hq + 2 * self.hk) * self.hd
+        g = torch.full((self.total, self.fused.shape[1]), fill, device="cuda", dtype=self.dtype)[:, :width].unflatten(
+            1, (self.hq + 2 * self.hk, self.hd))
+        return g[:, :self.hq], g[:, self.hq:self.hq + self.hk], g[:, self.hq + self.hk:]
+
+    def outside(self):
+        keep = torch.ones(self.total, dtype=torch.bool, device="cuda")
+        keep[self.start[0]:self.start[-1]] = False
+        return keep
+
+    def each(self):
+        """(rows, query head, key head) of every sequence that has rows."""
+        for i, n in enumerate(self.lens):
+            if n:
+                for h in range(self.hq):
+                    yield slice(self.start[i], self.start[i + 1]), h, h * self.hk // self.hq
+
+
+def half_step(x, dtype):
+    return x.abs() * (W if dtype == torch.bfloat16 else U)
+
+
+def weights(b, at, h, g):
+    """Scores, weights, their relative error bound, log of the sums."""
+    q, k = b.q[at, h].double(), b.k[at, g].double()
+    n = q.shape[0]
+    looks = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+    s = torch.where(looks, b.scale * (q @ k.T), torch.full((n, n), -math.inf, dtype=torch.float64, device="cuda"))
+    lse = torch.logsumexp(s, 1, keepdim=True)
+    size = abs(b.scale) * (q.abs() @ k.abs().T)
+    e = (b.hd + 2) * U * size.amax(1, keepdim=True) * 2 + (8 + 2 * s.masked_fill(~looks, 0).abs().amax(1, keepdim=True)) * U
+    return torch.exp(s - lse), e, lse
+
+
+def check_forward(b, o, lse):
+    rounded = W if b.dtype == torch.bfloat16 else 0.0
+    for at, h, g in b.each():
+        p, e, want_lse = weights(b, at, h, g)
+        v = b.v[at, g].double()
+        n = p.shape[0]
+        want, size = p @ v, p @ v.abs()
+        tol = size * (2 * e + rounded + n * U) + half_step(want, b.dtype) + 1e-30
+        worst = ((o[at, h].double() - want).abs() / tol).max().item()
+        assert worst <= 1.0, (n, h, worst)
+        if lse is not None:
+            tol = 2 * e + n * U + 2 * U * want_lse.abs()
+            worst = ((lse[h, at].double()[:, None] - want_lse).abs() / tol).max().item()
+            assert worst <= 1.0, (n, h, worst)
+
+
+def check_backward(b, o, lse, dq, dk, dv):
+    rounded = W if b.dtype == torch.bfloat16 else 0.0
+    want = {}
+    for at, h, g in b.each():
+        q, k, v, do, oo = (t.double() for t in (b.q[at, h], b.k[at, g], b.v[at, g], b.do[at, h], o[at, h]))
+        n = q.shape[0]
+        _, e, _ = weights(b, at, h, g)
+        l = lse[h, at].double()[:, None]
+        looks = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+        p = torch.where(looks, torch.exp(b.scale * (q @ k.T) - l), torch.zeros((n, n), dtype=torch.float64, device="cuda"))
+        e = e + 2 * U * l.abs()
+        dp, delta = do @ v.T, (do * oo).sum(1, keepdim=True)
+        ds = p * (dp - delta)
+        d_ds = p * ((dp - delta).abs() * e + (b.hd + 2) * U * (do.abs() @ v.abs().T + (do * oo).abs().sum(1, keepdim=True)))
+        d_ds = d_ds + rounded * (ds.abs() + d_ds)
+        group = (b.hq // b.hk) * n
+        x = want.setdefault((at.start, at.stop, g), [torch.zeros_like(k), torch.zeros_like(k), torch.zeros_like(k), torch.zeros_like(k)])
+        x[0] += b.scale * (ds.T @ q)
+        x[1] += b.scale * ((d_ds + group * U * ds.abs()).T @ q.abs())
+        x[2] += p.T @ do
+        x[3] += (p * (e + rounded + group * U)).T @ do.abs()
+        ref = b.scale * (ds @ k)
+        tol = abs(b.scale) * ((d_ds + n * U * ds.abs()) @ k.abs()) + half_step(ref, b.dtype) + 1e-30
+        worst = ((dq[at, h].double() - ref).abs() / tol).max().item()
+        assert worst <= 1.0, ("dq", n, h, worst)
+    for (first, end, g), (rk, tk, rv, tv) in want.items():
+        for name, got, ref, tol in (("dk", dk, rk, tk), ("dv", dv, rv, tv)):
+            worst = ((got[first:end, g].double() - ref).abs() / (tol + half_step(ref, b.dtype) + 1e-30)).max().item()
+            assert worst <= 1.0, (name, end - first, g, worst)
+
+
+def run_forward(ctx, b, fill=7.0, plan=None):
+    o, lse = b.outputs(fill)
+    plan = plan or ctx.attention_plan(b.offsets, b.total)
+    assert ctx.abs_attention(b.q, b.k, b.v, plan, o, lse, scale=b.scale) is o
+    return plan, o, lse
+
+
+def run_backward(ctx, b, plan, o, lse, fill=7.0):
+    dq, dk, dv = b.gradients(fill)
+    scratch = ctx.attention_scratch(b.total, b.hq, b.hk, b.hd, len(b.lens))
+    scratch.fill_(0xff)
+    ctx.abs_attention_backward(b.do, b.q, b.k, b.v, o, lse, plan, dq, dk, dv, scratch, scale=b.scale)
+    return dq, dk, dv
+
+
+EDGES = [63, 64, 65, 0, 127, 128, 129, 1, 255, 256, 257, 2]
+CASES = [
+    ([1], 1, 1, 64, "bf16", {}),
+    ([1], 2, 1, 128, "f32", {}),
+    ([5], 3, 3, 8, "bf16", {}),
+    (EDGES, 4, 2, 64, "bf16", dict(tail=3)),
+    (EDGES, 4, 4, 128, "bf16", dict(front=5, tail=200)),
+    (EDGES, 2, 1, 64, "f32", dict(front=1)),
+    ([300, 77, 0, 0, 513], 6, 1, 128, "bf16", {}),
+    ([300, 77, 0, 0, 513], 6, 2, 128, "f32", {}),
+    ([200, 385], 4, 2, 80, "bf16", dict(tail=1)),
+    ([200, 385], 4, 2, 96, "f32", dict(tail=1)),
+    ([130, 40], 2, 2, 40, "bf16", {}),
+    ([130, 40], 2, 2, 33, "bf16", {}),                       # rows that are not 16-byte aligned
+    ([130, 40], 3, 1, 64, "bf16", dict(pad=1)),
+    ([130, 40], 3, 1, 7, "f32", dict(pad=3)),
+    ([700], 2, 2, 64, "bf16", dict(amp=3.0)),                # weights that one key takes most of
+    ([700], 2, 2, 128, "bf16", dict(amp=2.5)),
+    ([1500, 3], 2, 1, 64, "bf16", {}),
+    ([1500, 3], 8, 1, 128, "bf16", {}),
+    ([2] * 50 + [129] * 3, 2, 2, 64, "bf16", {}),
+]
+
+
+@pytest.mark.parametrize("lens,hq,hk,hd,dtype,kw", CASES)
+def test_forward_and_backward(ctx, lens, hq, hk, hd, dtype, kw):
+    b = Batch(lens, hq, hk, hd, dtype, seed=hd + sum(lens), **kw)
+    plan, o, lse = run_forward(ctx, b)
+    check_forward(b, o, lse)
+    out = b.outside()
+    assert (o[out] == 7.0).all() and (lse[:, out] == 7.0).all()
+    dq, dk, dv = run_backward(ctx, b, plan, o, lse)
+    check_backward(b, o, lse, dq, dk, dv)
+    assert all((x[out] == 7.0).all() for x in (dq, dk, dv))
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32")])
+def test_nothing_outside_a_sequence_reaches_it(ctx, hd, dtype):
+    """NaN in the rows around the sequences, and in all of another sequence."""
+    b = Batch([70, 130, 200], 4, 2, hd, dtype, seed=3, front=9, tail=61)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    bad = b.outside()
+    bad[b.start[1]:b.start[2]] = True
+    for t in (b.fused, b.do):
+        t[bad] = math.nan
+    o2, lse2 = b.outputs()
+    o2[bad], lse2[:, bad] = math.nan, math.nan
+    ctx.abs_attention(b.q, b.k, b.v, plan, o2, lse2, scale=b.scale)
+    for t in (o2,):
+        assert torch.equal(t[~bad], o[~bad])
+    assert torch.equal(lse2[:, ~bad], lse[:, ~bad])
+    o2[b.outside()] = math.nan
+    again = run_backward(ctx, b, plan, o2, lse2)
+    for x, y in zip(grads, again):
+        assert torch.equal(x[~bad], y[~bad])
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "bf16"), (48, "f32")])
+def test_results_repeat_bit_for_bit(ctx, hd, dtype):
+    b = Batch([1100, 1, 640], 6, 2, hd, dtype, seed=4)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    for _ in range(3):
+        plan, o2, lse2 = run_forward(ctx, b)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        assert all(torch.equal(x, y) for x, y in zip(grads, run_backward(ctx, b, plan, o2, lse2)))
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32")])
+def test_large_scores_of_equal_keys(ctx, hd, dtype):
+    """All keys equal: every weight is 1 / (t + 1) whatever the scores' size, and the outputs are running means of V."""
+    b = Batch([333], 2, 1, hd, dtype, seed=5)
+    b.k[:] = 8.0 * torch.sign(b.k[:1])
+    b.q[:] = 8.0 * torch.sign(b.q)
+    _, o, lse = run_forward(ctx, b)
+    v = b.v[:, 0].double()
+    n = torch.arange(1, 334, device="cuda", dtype=torch.float64)[:, None]
+    mean, size = v.cumsum(0) / n, v.abs().cumsum(0) / n
+    tol = size * ((W if dtype == "bf16" else 0.0) + 400 * U) + half_step(mean, b.dtype)
+    for h in range(2):
+        assert ((o[:, h].double() - mean).abs() <= tol).all()
+        s = b.scale * (b.q[:, h].double() @ b.k[:, 0].double().T)[:, :1]        # exact: sums of +-64
+        assert ((lse[h].double()[:, None] - s - n.log()).abs() <= 400 * U + 6 * U * (s.abs() + n.log())).all()
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (64, "f32")])
+def test_scores_of_minus_infinity(ctx, hd, dtype):
+    """Keys whose scores are all -infinity weigh nothing; a row with no other key has no answer (NaN)."""
+    b = Batch([200], 1, 1, hd, dtype, seed=6)
+    b.q[:, :, 0] = 1.0
+    b.k[:150, :, 0] = -math.inf
+    _, o, lse = run_forward(ctx, b)
+    s = b.scale * (b.q[150:, 0].double() @ b.k[150:, 0].double().T)
+    n = s.shape[0]
+    s = s.masked_fill(torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1), -math.inf)
+    want = torch.softmax(s, 1) @ b.v[150:, 0].double()
+    assert torch.isnan(o[:150].float()).all()
+    size = torch.softmax(s, 1) @ b.v[150:, 0].double().abs()
+    assert ((o[150:, 0].double() - want).abs() <= size * (2 * W + 300 * U) + half_step(want, b.dtype)).all()
+    assert (lse[0, :150] == -math.inf).all() and torch.isfinite(lse[0, 150:]).all()
+
+
+def test_gradients_against_differences(ctx):
+    """<dO, O> along random directions of the inputs, fp32: central differences of step h are off by truncation, of the order
+    of h^2 of the values, and by rounding, u / h of the sum's size."""
+    b = Batch([90, 41], 4, 2, 32, "f32", seed=7)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    h = 2.0 ** -7
+    for t, g in zip((b.q, b.k, b.v), grads):
+        d = torch.randn(t.shape, device="cuda", generator=gen)
+        keep = t.clone()
+        values = []
+        for sign in (1, -1):
+            t.copy_(keep + sign * h * d)
+            values.append((run_forward(ctx, b, plan=plan)[1].double() * b.do.double()).sum().item())
+        t.copy_(keep)
+        got, want = (g.double() * d.double()).sum().item(), (values[0] - values[1]) / (2 * h)
+        scale = (b.do.double().norm() * o.double().norm()).item()
+        # each of the 131 x 4 rows moves by about |d| ~ sqrt(hd) / sqrt(hd) in its scores: third derivatives of order one
+        assert abs(got - want) <= scale * (4 * h * h + 64 * U / h), (got, want, scale)
+
+
+def test_replicas_are_packed_sequences(ctx):
+    """M replicas' [M, S, T, heads, hd] tensors flattened over their tokens: a sequence's result does not depend on what it is packed with."""
+    b = Batch([96] * 6, 4, 4, 64, "bf16", seed=9)
+    _, o, lse = run_forward(ctx, b)
+    for i in range(6):
+        at = slice(96 * i, 96 * (i + 1))
+        one = ctx.attention_plan(torch.tensor([0, 96], dtype=torch.int32, device="cuda"), 96)
+        oo, ll = torch.empty_like(o[at]), torch.empty((4, 96), device="cuda")
+        ctx.abs_attention(b.q[at], b.k[at], b.v[at], one, oo, ll)
+        assert torch.equal(oo, o[at]) and torch.equal(ll, lse[:, at])
+
+
+def test_capture_replay_and_new_offsets(ctx):
+    """A captured forward and backward pass follows the inputs and the plan that are there when it is replayed."""
+    b = Batch([300, 212], 4, 2, 64, "bf16", seed=10)
+    stream = torch.cuda.Stream()
+    plan = ctx.attention_plan(b.offsets, b.total)
+    scratch = ctx.attention_scratch(b.total, 4, 2, 64, 2)
+    o, lse = b.outputs()
+    grads = b.gradients()
+
+    def both():
+        ctx.abs_attention(b.q, b.k, b.v, plan, o, lse, scale=b.scale)
+        ctx.abs_attention_backward(b.do, b.q, b.k, b.v, o, lse, plan, *grads, scratch, scale=b.scale)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        both()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            both()
+    for lens in ([300, 212], [10, 502], [0, 512], [511, 1]):
+        b.lens, b.start = lens, [0, lens[0], 512]
+        ctx.attention_plan(torch.tensor(b.start, dtype=torch.int32, device="cuda"), b.total, plan=plan)
+        b.fused.copy_(torch.randn_like(b.fused))
+        for _ in range(2):
+            graph.replay()
+        torch.cuda.synchronize()
+        check_forward(b, o, lse)
+        check_backward(b, o, lse, *grads)
+
+
+def test_on_another_stream(ctx):
+    b = Batch([600, 9], 2, 2, 64, "bf16", seed=11)
+    plan, o, lse = run_forward(ctx, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o2, lse2 = b.outputs()
+    ctx.abs_attention(b.q, b.k, b.v, plan, o2, lse2, scale=b.scale, stream=side)
+    side.synchronize()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("table,lens,bad", [([5, 3, 40], [0, 35], 1), ([-4, 20, 90], [20, 20], 1), ([0, 7, 40], [7, 33], 0)])
+def test_bad_offsets_are_put_right(ctx, table, lens, bad):
+    b = Batch([40], 2, 1, 64, "bf16", seed=12)
+    b.lens = lens
+    b.start = [max(table[0], 0)]
+    for n in lens:
+        b.start.append(b.start[-1] + n)
+    b.offsets = torch.tensor(table, dtype=torch.int32, device="cuda")
+    plan, o, lse = run_forward(ctx, b)
+    assert plan.words[2].item() == bad
+    check_forward(b, o, lse)
+    check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
+    assert (o[b.outside()] == 7.0).all()
+
+
+def test_plan_covers_every_tile_once(ctx):
+    """Every tile of every sequence once; forward the most work first, backward a sequence's last tile first."""
+    gen = torch.Generator().manual_seed(13)
+    lens = torch.randint(0, 1500, (700,), generator=gen)
+    lens[::7] = 0
+    start = torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)])
+    total = int(start[-1]) + 50
+    plan = ctx.attention_plan(start.to(torch.int32).cuda(), total)
+    words = plan.words.cpu()
+    n = len(lens)
+    fwd_cap, bwd_cap = total // 256 + n, total // 128 + n
+    for kind, rows, at in ((0, 256, 16), (1, 128, 16 + 4 * fwd_cap)):
+        count = int(words[kind])
+        assert count <= (fwd_cap, bwd_cap)[kind]
+        recs = [tuple(r[:3].tolist()) for r in words[at:at + 4 * count].view(-1, 4)]
+        want = {(int(start[i]), int(start[i + 1]), t) for i in range(n) for t in range(-(-int(lens[i]) // rows))}
+        assert len(recs) == len(want) and set(recs) == want
+        work = [t + 1 if kind == 0 else -(-(e - s) // rows) - t for s, e, t in recs]
+        assert work == sorted(work, reverse=kind == 0)
+
+
+def test_nothing_to_do(ctx):
+    b = Batch([0, 0], 2, 2, 64, "bf16", tail=4)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    assert (o == 7.0).all() and (lse == 7.0).all() and all((g == 7.0).all() for g in grads)
+    empty = Batch([], 2, 2, 64, "bf16")
+    plan, o, lse = run_forward(ctx, empty)
+    run_backward(ctx, empty, plan, o, lse)
