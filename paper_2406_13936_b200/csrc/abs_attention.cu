@@ -140,13 +140,14 @@ int validate_sequences(abs_ctx* ctx, int sequences, long long total) {
     return set_error(ctx, ABS_ERR_UNSUPPORTED, "sequences <= 2^24 and total <= 2^30 (%d, %lld)", sequences, total);
   return ABS_OK;
 }
-int validate_heads(abs_ctx* ctx, long long total, int q_heads, int kv_heads, int head_dim) {
+int validate_heads(abs_ctx* ctx, int sequences, long long total, int q_heads, int kv_heads, int head_dim) {
   if (q_heads < 1 || kv_heads < 1 || q_heads % kv_heads != 0)
     return set_error(ctx, ABS_ERR_INVALID_ARG, "q_heads %d must be a multiple of kv_heads %d", q_heads, kv_heads);
   if (head_dim < 1) return set_error(ctx, ABS_ERR_INVALID_ARG, "head_dim must be >= 1 (%d)", head_dim);
-  if (head_dim > kAttnMaxHead || q_heads > 4096 || total * q_heads > (1ll << 32))
-    return set_error(ctx, ABS_ERR_UNSUPPORTED, "head_dim <= %d, q_heads <= 4096 and total * q_heads <= 2^32 (%d, %d, %lld)", kAttnMaxHead,
-                     head_dim, q_heads, total);
+  if (head_dim > kAttnMaxHead || q_heads > 4096 || total * q_heads > (1ll << 32) || static_cast<long long>(sequences) * q_heads > (1ll << 28))
+    return set_error(ctx, ABS_ERR_UNSUPPORTED,
+                     "head_dim <= %d, q_heads <= 4096, total * q_heads <= 2^32 and sequences * q_heads <= 2^28 (%d, %d, %lld, %d)", kAttnMaxHead,
+                     head_dim, q_heads, total, sequences);
   return ABS_OK;
 }
 // Rows are disjoint from one another: a token's heads lie within its row (stride of tokens the larger) or a head's tokens within
@@ -162,6 +163,12 @@ int validate_tensor(abs_ctx* ctx, const char* what, const abs_heads* t, long lon
 }
 AttnRows rows_of(const abs_heads* t) { return {t->data, t->row_stride, t->head_stride}; }
 AttnOut out_of(const abs_heads* t) { return {t->data, t->row_stride, t->head_stride}; }
+
+// Whether the tensor-core kernels take a tensor: bf16 rows that copies of 16 bytes can address, within a tensor map's limits.
+bool tc_tensor(const abs_heads* t) {
+  const unsigned long long row = static_cast<unsigned long long>(t->row_stride) * 2, head = static_cast<unsigned long long>(t->head_stride) * 2;
+  return ((reinterpret_cast<uintptr_t>(t->data) | row | head) & 15u) == 0 && row > 0 && head > 0 && row < (1ull << 40) && head < (1ull << 40);
+}
 
 }  // namespace
 }  // namespace absk
@@ -201,7 +208,7 @@ extern "C" int abs_attention_plan(abs_ctx* ctx, const int* offsets, int sequence
 extern "C" int abs_attention_scratch_bytes(long long total, int q_heads, int kv_heads, int head_dim, int sequences, size_t* out) {
   if (out == nullptr) return set_error(nullptr, ABS_ERR_INVALID_ARG, "out is null");
   int rc = validate_sequences(nullptr, sequences, total);
-  if (rc == ABS_OK) rc = validate_heads(nullptr, total, q_heads, kv_heads, head_dim);
+  if (rc == ABS_OK) rc = validate_heads(nullptr, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
   *out = attn_scratch(static_cast<int>(total), q_heads, head_dim, sequences).bytes;
   return ABS_OK;
@@ -213,7 +220,7 @@ extern "C" int abs_attention(abs_ctx* ctx, const abs_heads* Q, const abs_heads* 
   if (ctx == nullptr) return ABS_ERR_INVALID_ARG;
   if (dtype != ABS_F32 && dtype != ABS_BF16) return set_error(ctx, ABS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
   int rc = validate_sequences(ctx, sequences, total);
-  if (rc == ABS_OK) rc = validate_heads(ctx, total, q_heads, kv_heads, head_dim);
+  if (rc == ABS_OK) rc = validate_heads(ctx, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
   if (!(scale > -3.0e38f && scale < 3.0e38f)) return set_error(ctx, ABS_ERR_INVALID_ARG, "scale must be finite");
   if (total == 0 || sequences == 0) return ABS_OK;
@@ -226,7 +233,11 @@ extern "C" int abs_attention(abs_ctx* ctx, const abs_heads* Q, const abs_heads* 
   if (!guard.ok) return set_error(ctx, ABS_ERR_CUDA, "cannot select device %d", ctx->device);
   const AttnForward a{rows_of(Q), rows_of(K), rows_of(V), out_of(O), lse, static_cast<const int*>(plan), sequences,
                       static_cast<int>(total), q_heads, kv_heads, head_dim, scale};
-  return launch_attention_any(ctx, a, dtype, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // (the running maximum is taken before the scale is applied: a scale of zero or below goes the other way)
+  if (dtype == ABS_BF16 && head_dim % 8 == 0 && scale > 0.f && tc_tensor(Q) && tc_tensor(K) && tc_tensor(V) && tc_tensor(O))
+    return launch_attention_tc(ctx, a, st);
+  return launch_attention_any(ctx, a, dtype, st);
 }
 
 extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const abs_heads* Q, const abs_heads* K, const abs_heads* V,
@@ -236,7 +247,7 @@ extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const a
   if (ctx == nullptr) return ABS_ERR_INVALID_ARG;
   if (dtype != ABS_F32 && dtype != ABS_BF16) return set_error(ctx, ABS_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
   int rc = validate_sequences(ctx, sequences, total);
-  if (rc == ABS_OK) rc = validate_heads(ctx, total, q_heads, kv_heads, head_dim);
+  if (rc == ABS_OK) rc = validate_heads(ctx, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
   if (!(scale > -3.0e38f && scale < 3.0e38f)) return set_error(ctx, ABS_ERR_INVALID_ARG, "scale must be finite");
   if (total == 0 || sequences == 0) return ABS_OK;

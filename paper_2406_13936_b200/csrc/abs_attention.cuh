@@ -11,7 +11,6 @@ namespace absk {
 constexpr int kAttnMaxHead = 128;
 constexpr int kAttnFwdRows = 256;          // query rows of a forward tile
 constexpr int kAttnBwdRows = 128;          // keys of a backward tile
-constexpr int kAttnFlagWord = 9;           // word of abs_ctx::flags that a kernel whose wait ran out sets (cleared by every call)
 
 // The plan of a batch, int32 words on the device: the header, then the records of the forward and of the backward tiles in
 // the order in which they are worked off, then what the plan's own kernel needs.
@@ -81,6 +80,7 @@ inline AttnScratch attn_scratch(int total, int hq, int hd, int n) {
   return s;
 }
 
+int launch_attention_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st);          // bf16 rows of 16-byte pieces, scale > 0
 int launch_attention_any(abs_ctx* ctx, const AttnForward& a, abs_dtype dtype, cudaStream_t st);
 int launch_attention_any_backward(abs_ctx* ctx, const AttnBackward& a, abs_dtype dtype, cudaStream_t st);
 

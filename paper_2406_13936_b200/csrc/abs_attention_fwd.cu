@@ -1,0 +1,401 @@
+// Causal attention, forward, bf16 on the tcgen05 tensor cores.
+//
+//   s = c q k' (c = scale log2 e),  p = 2^(s - m),  o = (sum_j p_j v_j) / sum_j p_j,  lse = ln 2 (m + log2 sum_j p_j)
+//
+// One pass over the keys with a running reference m of each row.  A resident CTA an SM walks the plan's tiles of 256 queries of one
+// head, two halves of 128, longest first.  Per 128 keys and half: S = Q K' into tensor memory (128 columns of fp32); the half's four
+// warps, a thread a row, read it, take the exponentials and write P as bf16 over the first half of S, from where the tensor core takes
+// it as the operand of O += P V (P never touches shared memory).  While one half's warps work on their exponentials the other's
+// products run.
+//
+// m is raised only where a row's largest score is more than 8 above it: p is then at most 2^8, which costs nothing in fp32 sums or
+// bf16's relative steps, and O, which stays in tensor memory, is rescaled a few times a tile instead of once per 128 keys.
+// Rounded to fewer bits than 32: P to bf16, as an operand of the tensor core (its sums of p are taken before that), and O.
+//
+// Bound by the exponentials at 64 columns a head (16 a clock and SM: 1024 clocks per 128 x 128 scores, whose products take 512) and by
+// both at 128.
+//
+// Roles of the 12 warps: 0 loads (TMA; Q once a tile, K and V through a ring of 128-row places), 1 issues the products, 4-7 and 8-11
+// are the two halves.  All waits are bounded: one that runs out raises the CTA's abort flag, every role falls through, copies in
+// flight are waited for, tensor memory is freed, and the rows of tiles that were not finished are NaN.
+#include "abs_attention.cuh"
+#include "abs_tc.cuh"
+
+namespace absk {
+namespace {
+
+constexpr int kThreadsF = 384;
+constexpr int kFewRegs = 56, kManyRegs = 224;  // of a thread of warps 0-3 and of the halves; together what 168 a thread are at the launch
+static_assert(128 * kFewRegs + 256 * kManyRegs == kThreadsF * 168, "");
+constexpr int kHalf = 128;                    // rows of a half, keys of a step
+constexpr float kRaise = 8.f;
+constexpr float kLn2F = 0.6931471805599453f, kLog2eF = 1.4426950408889634f;
+
+template <int HD> struct FwdShape {
+  static constexpr uint32_t kRowsBytes = kHalf * HD * 2;          // 128 rows of one head
+  static constexpr int kPlaces = HD == 64 ? 8 : 5;
+  static constexpr size_t kSmem = (2 + kPlaces) * static_cast<size_t>(kRowsBytes) + 1024 + 512;
+};
+
+struct FwdMaps {
+  CUtensorMap q, k, v;
+};
+struct FwdParams {
+  AttnOut o;
+  float* lse;
+  const int* plan;
+  const int* tiles;
+  int total, hq, group, hd;
+  float by;                                   // scale log2 e
+  long long limit;
+  int drop_loads;                             // test hook: nothing is loaded, so every wait must run out
+};
+struct FwdItem {
+  int begin, len, row, head, kv, n0, n1;      // row: the tile's first in the sequence; n0, n1: steps of its halves
+};
+__device__ __forceinline__ FwdItem item_of(const FwdParams& p, int i) {
+  FwdItem it;
+  const int tile = i / p.hq;
+  it.head = i - tile * p.hq;
+  const int4 r = __ldg(reinterpret_cast<const int4*>(p.tiles) + tile);
+  it.begin = r.x;
+  it.len = r.y - r.x;
+  it.row = r.z * kAttnFwdRows;
+  it.kv = it.head / p.group;
+  it.n0 = 2 * r.z + 1;
+  it.n1 = it.row + kHalf < it.len ? it.n0 + 1 : 0;
+  return it;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreadsF, 1)
+attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
+  constexpr uint32_t kRows = FwdShape<HD>::kRowsBytes;
+  constexpr int kPlaces = FwdShape<HD>::kPlaces;
+  extern __shared__ unsigned char smem_dyn[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw = smem_u32(smem_dyn), q_at = (raw + 1023u) & ~1023u, ring = q_at + 2u * kRows;
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + (q_at - raw) + (2 + kPlaces) * kRows);
+  volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + 14 + 2 * kPlaces);
+  unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
+  const uint32_t q_full = smem_u32(bars), q_free = q_full + 16u, s_full = q_free + 16u, p_full = s_full + 16u, o_full = p_full + 16u,
+                 o_free = o_full + 16u, landed = o_free + 16u, done_bar = landed + 8u, full = done_bar + 8u, freed = full + 8u * kPlaces;
+  if (threadIdx.x == 0) {
+    for (uint32_t t = 0; t < 2; ++t) {
+      mbar_init(q_full + 8u * t, 1);
+      mbar_init(q_free + 8u * t, 1);
+      mbar_init(s_full + 8u * t, 1);
+      mbar_init(p_full + 8u * t, 4);
+      mbar_init(o_full + 8u * t, 1);
+      mbar_init(o_free + 8u * t, 4);
+    }
+    mbar_init(landed, 1);
+    mbar_init(done_bar, 1);
+    for (uint32_t s = 0; s < kPlaces; ++s) {
+      mbar_init(full + 8u * s, 1);
+      mbar_init(freed + 8u * s, 1);
+    }
+    *abort_flag = 0u;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc_all(smem_u32(tmem_slot));
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();
+  const int items = __ldg(p.plan + kPlanFwdTiles) * p.hq;
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+    if (warp == 0) {
+      // ---- loads ---------------------------------------------------------------------------------
+      uint32_t n = 0, lands = 0, uses[2] = {0, 0};
+      bool ok = !p.drop_loads;
+      // 128 rows of one head from the sequence's row r on
+      auto copy = [&](const CUtensorMap* map, uint32_t to, int head, int row, uint32_t bar) {
+        if (elect_lane()) {
+          mbar_expect_tx(bar, kRows);
+#pragma unroll
+          for (uint32_t c = 0; c < HD / 64; ++c) tma_load_3d(to + c * (kHalf * 128u), map, 64 * static_cast<int>(c), head, row, bar);
+        }
+        __syncwarp();
+      };
+      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
+        const FwdItem it = item_of(p, i);
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t) {
+          if (t == 1 && it.n1 == 0) continue;
+          if (uses[t] > 0) ok = ok && warp_wait(q_free + 8u * t, (uses[t] - 1) & 1u, abort_flag, p.limit);
+          if (!ok) break;
+          copy(&maps.q, q_at + t * kRows, it.head, it.begin + it.row + static_cast<int>(t) * kHalf, q_full + 8u * t);
+          ++uses[t];
+        }
+        const int steps = max(it.n0, it.n1);
+        for (int j = 0; j < 2 * steps && ok; ++j, ++n) {
+          const uint32_t s = n % kPlaces, pass = n / kPlaces, to = ring + s * kRows;
+          if (pass > 0) ok = warp_wait(freed + 8u * s, (pass - 1) & 1u, abort_flag, p.limit);
+          if (!ok) break;
+          const int key = (j >> 1) * kHalf, in = it.len - key;                   // rows of the sequence from the step's first key on
+          if ((j & 1) == 0) {
+            copy(&maps.k, to, it.kv, it.begin + key, full + 8u * s);
+          } else if (in >= kHalf) {
+            copy(&maps.v, to, it.kv, it.begin + key, full + 8u * s);
+          } else {
+            // rows of V behind the sequence have weights of zero, but may hold anything: zeros in their place
+            copy(&maps.v, to, it.kv, it.begin + key, landed);
+            ok = warp_wait(landed, lands & 1u, abort_flag, p.limit);
+            ++lands;
+            for (uint32_t c = 0; c < HD / 64; ++c)
+              for (uint32_t e = static_cast<uint32_t>(in) * 128u + lane * 16u; e < kHalf * 128u; e += 512u)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + c * (kHalf * 128u) + e), "r"(0u) : "memory");
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8u * s);
+          }
+        }
+      }
+      // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.
+      volatile unsigned ignore = 0u;
+      for (uint32_t s = 0; s < kPlaces; ++s) {
+        const uint32_t fills = n / kPlaces + (s < n % kPlaces ? 1u : 0u);
+        if (fills > 0) mbar_wait(full + 8u * s, (fills - 1) & 1u, &ignore, p.limit);
+      }
+      for (uint32_t t = 0; t < 2; ++t)
+        if (uses[t] > 0) mbar_wait(q_full + 8u * t, (uses[t] - 1) & 1u, &ignore, p.limit);
+    } else if (warp == 1) {
+      // ---- products --------------------------------------------------------------------------------
+      constexpr uint32_t idesc_s = mma_idesc(kHalf, kHalf, false, false), idesc_o = mma_idesc(kHalf, HD, false, true);
+      constexpr uint64_t desc_v = desc_mn(kHalf * 128);
+      uint32_t n = 0, uses[2] = {0, 0}, done[2] = {0, 0};        // places; tiles and steps of each half so far
+      bool ok = true;
+      auto scores = [&](uint32_t t, uint32_t place) {            // S of half t from Q and the K at the place
+        if (elect_lane()) {
+          const uint32_t a = desc_at(q_at + t * kRows), b = desc_at(ring + place * kRows);
+#pragma unroll
+          for (uint32_t k = 0; k < HD / 16; ++k) {
+            const uint32_t off = (k / 4) * (kHalf * 128u / 16u) + (k % 4) * 2u;
+            mma_ss(tmem + t * kHalf, kDescK | (a + off), kDescK | (b + off), idesc_s, k > 0);
+          }
+          mma_commit(s_full + 8u * t);
+        }
+        __syncwarp();
+      };
+      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
+        const FwdItem it = item_of(p, i);
+        const int steps = max(it.n0, it.n1);
+        ok = warp_wait(full + 8u * (n % kPlaces), (n / kPlaces) & 1u, abort_flag, p.limit);
+#pragma unroll
+        for (uint32_t t = 0; t < 2; ++t) {
+          if (t == 1 && it.n1 == 0) continue;
+          ok = ok && warp_wait(q_full + 8u * t, uses[t] & 1u, abort_flag, p.limit);
+          tc_fence_after();
+          scores(t, n % kPlaces);
+          if ((t == 0 ? it.n0 : it.n1) == 1 && elect_lane()) mma_commit(q_free + 8u * t);
+          __syncwarp();
+        }
+        if (elect_lane()) mma_commit(freed + 8u * (n % kPlaces));
+        __syncwarp();
+        for (int j = 0; j < steps && ok; ++j) {
+          const uint32_t v = n + 2 * j + 1, k = v + 1;           // places of this step's V and the next one's K
+          ok = warp_wait(full + 8u * (v % kPlaces), (v / kPlaces) & 1u, abort_flag, p.limit);
+          const uint32_t b = desc_at(ring + (v % kPlaces) * kRows);
+#pragma unroll
+          for (uint32_t t = 0; t < 2; ++t) {
+            const int last = t == 0 ? it.n0 : it.n1;
+            if (j >= last || !ok) continue;
+            if (j == 0 && uses[t] > 0) ok = warp_wait(o_free + 8u * t, (uses[t] - 1) & 1u, abort_flag, p.limit);
+            ok = ok && warp_wait(p_full + 8u * t, done[t] & 1u, abort_flag, p.limit);
+            if (!ok) continue;
+            ++done[t];
+            tc_fence_after();
+            if (elect_lane()) {
+#pragma unroll
+              for (uint32_t kk = 0; kk < kHalf / 16; ++kk)
+                mma_ts(tmem + 256u + t * HD, tmem + t * kHalf + 8u * kk, desc_v | (b + 128u * kk), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+              if (j == last - 1) mma_commit(o_full + 8u * t);
+            }
+            __syncwarp();
+            if (j + 1 < last) {
+              ok = warp_wait(full + 8u * (k % kPlaces), (k / kPlaces) & 1u, abort_flag, p.limit);
+              tc_fence_after();
+              scores(t, k % kPlaces);
+              if (j + 2 == last && elect_lane()) mma_commit(q_free + 8u * t);
+              __syncwarp();
+            }
+          }
+          if (elect_lane()) {
+            mma_commit(freed + 8u * (v % kPlaces));
+            if (j + 1 < steps) mma_commit(freed + 8u * (k % kPlaces));
+          }
+          __syncwarp();
+        }
+        n += 2 * steps;
+        ++uses[0];
+        if (it.n1 > 0) ++uses[1];
+      }
+      if (elect_lane()) mma_commit(done_bar);
+      __syncwarp();
+      volatile unsigned ignore = 0u;
+      mbar_wait(done_bar, 0u, &ignore, p.limit);                 // no product in flight when tensor memory is freed
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+    // ---- softmax: a thread has a row ------------------------------------------------------------------
+    const uint32_t t = static_cast<uint32_t>(warp - 4) >> 2;
+    const int r = (warp & 3) * 32 + lane;                        // row of the half
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + t * kHalf + lanes, o_at = tmem + 256u + t * HD + lanes;
+    const uint64_t by2 = pack2f(p.by, p.by);
+    uint32_t steps_done = 0, uses = 0;
+    bool ok = true;
+    for (int i = blockIdx.x; i < items; i += gridDim.x) {
+      const FwdItem it = item_of(p, i);
+      const int steps = t == 0 ? it.n0 : it.n1;
+      if (steps == 0) continue;
+      float m = -INFINITY;                                       // the reference
+      float sum = 0.f;
+      for (int j = 0; j < steps && ok; ++j, ++steps_done) {
+        ok = warp_wait(s_full + 8u * t, steps_done & 1u, abort_flag, p.limit);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t s[kHalf];
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) tmem_load32(s_at + c, s + c);
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) tmem_loaded(s + c);
+        if (j == steps - 1) {                                    // the diagonal
+#pragma unroll
+          for (int c = 0; c < kHalf; ++c) s[c] = c > r ? 0xff800000u : s[c];
+        }
+        float top[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(s[c]);
+#pragma unroll
+        for (int c = 4; c < kHalf; c += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            top[e] = c + 4 + e < kHalf ? fmaxf(fmaxf(top[e], __uint_as_float(s[c + e])), __uint_as_float(s[c + 4 + e]))
+                                       : fmaxf(top[e], __uint_as_float(s[c + e]));
+        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.by;
+        if (__any_sync(0xffffffffu, most > m + kRaise)) {
+          const float next = fmaxf(m, most);
+          const float less = m == -INFINITY ? 0.f : exp2_approx(m - next);       // (nothing has been added yet)
+          m = next;
+          sum *= less;
+          if (j > 0) {                                           // the products up to here are complete: S of this step came after them
+#pragma unroll
+            for (int c = 0; c < HD; c += 32) {
+              uint32_t o[32];
+              tmem_load32(o_at + c, o);
+              tmem_loaded(o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * less);
+              tmem_store32(o_at + c, o);
+            }
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : -m;
+        const uint64_t ref2 = pack2f(ref, ref);
+        uint64_t part[2] = {pack2f(0.f, 0.f), pack2f(0.f, 0.f)};
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 64) {
+          uint32_t w[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float2 x = unpack2f(fma2f(pack2f(__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])), by2, ref2));
+            const float a = exp2_approx(x.x), b = exp2_approx(x.y);
+            part[e & 1] = add2f(part[e & 1], pack2f(a, b));
+            w[e] = bf16_pair(a, b);
+          }
+          tmem_store32(s_at + c / 2, w);
+        }
+        const float2 all = unpack2f(add2f(part[0], part[1]));
+        sum += all.x + all.y;
+        tmem_stored();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8u * t);
+      }
+      ok = ok && warp_wait(o_full + 8u * t, uses & 1u, abort_flag, p.limit);
+      ++uses;
+      tc_fence_after();
+      const int row = it.row + static_cast<int>(t) * kHalf + r;
+      const bool live = row < it.len;
+      const float inv = ok ? 1.f / sum : __int_as_float(0x7fc00000);
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.o.p) + (it.begin + row) * p.o.row + it.head * p.o.head;
+#pragma unroll
+      for (int c = 0; c < HD; c += 32) {
+        uint32_t o[32];
+        if (ok) {
+          tmem_load32(o_at + c, o);
+          tmem_loaded(o);
+        }
+        if (c + 32 >= HD && ok) {                                // the last of O has been read
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(o_free + 8u * t);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            w[k] = ok ? bf16_pair(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv) : 0x7fc07fc0u;
+          if (live && c + e < p.hd) *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      if (live && p.lse)
+        p.lse[static_cast<long long>(it.head) * p.total + it.begin + row] = ok ? fmaf(m, kLn2F, logf(sum)) : __int_as_float(0x7fc00000);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_free_all(tmem);
+  }
+}
+
+bool encode_heads_map(const AttnRows& t, int total, int heads, int hd, CUtensorMap* map) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(total)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(t.head) * 2, static_cast<cuuint64_t>(t.row) * 2};
+  const cuuint32_t box[3] = {64u, 1u, static_cast<cuuint32_t>(kHalf)}, ones[3] = {1u, 1u, 1u};
+  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(t.p), dims, strides, box, ones,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD>
+int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
+  FwdMaps maps;
+  if (!encode_heads_map(a.q, a.total, a.hq, a.hd, &maps.q) || !encode_heads_map(a.k, a.total, a.hk, a.hd, &maps.k) ||
+      !encode_heads_map(a.v, a.total, a.hk, a.hd, &maps.v))
+    return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (%d rows, head_dim %d) failed", a.total, a.hd);
+  const AttnPlanLayout l = attn_plan_layout(a.n, a.total);
+  const FwdParams p{a.o, a.lse, a.plan, a.plan + l.fwd, a.total, a.hq, a.hq / a.hk, a.hd, a.scale * kLog2eF,
+                    ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
+                    ctx->tuning.stats_fault_drop_loads ? 1 : 0};
+  auto kern = attn_forward_kernel<HD>;
+  const size_t smem = FwdShape<HD>::kSmem;
+  ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
+  // the halves' registers come out of what the launch has: with fewer than 168 a thread they would never get them
+  static const int regs = [&] {
+    cudaFuncAttributes fa;
+    return cudaFuncGetAttributes(&fa, kern) == cudaSuccess ? fa.numRegs : 0;
+  }();
+  if (regs != 168) return set_error(ctx, ABS_ERR_CUDA, "the forward kernel was built with %d registers a thread, not 168", regs);
+  const long long most = static_cast<long long>(l.fwd_cap) * a.hq;
+  const unsigned grid = static_cast<unsigned>(most < ctx->sm_count ? most : ctx->sm_count);
+  ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(grid), dim3(kThreadsF), smem, st, maps, p));
+  return ABS_OK;
+}
+
+}  // namespace
+
+int launch_attention_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
+  if (encode_tiled_fn() == nullptr) return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  return a.hd <= 64 ? run_forward_tc<64>(ctx, a, st) : run_forward_tc<128>(ctx, a, st);
+}
+
+}  // namespace absk
