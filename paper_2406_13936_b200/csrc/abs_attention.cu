@@ -30,24 +30,69 @@ __device__ __forceinline__ int block_scan(int v, int* red, bool maximum) {      
   return v;
 }
 
-// One CTA.  The tiles in an order of their work: forward, tile i of a sequence reads the keys of i + 1 tiles, longest first, so
-// that the last ones to start are short; backward, tile j is read by the queries of the tiles from j on, shortest first, because the
-// sums of dq pass from the last tile of a sequence to the first (abs_attention_bwd.cu).  With sequences in the order of their
-// lengths, those with at least w tiles come first, so a tile's place is (tiles of more work) + (its sequence's place).  Which of two
-// sequences of one length comes first is left to chance; no result depends on it.
-// 128 sequences of 1024: 8 us.
+// The tiles of the sequences [s0, s1) to `out`, ordered by their work: most first (forward: tile i reads the keys of i + 1 tiles) or
+// least first (backward: tile j is read by the queries of the tiles from j on).  With sequences in the order of their lengths, those
+// with at least w tiles come first, so a tile's place is (tiles in front by their work) + (its sequence's place).  Which of two
+// sequences of one length comes first is left to chance; no result depends on it.  Returns the number of tiles.
+// counts: [3][bins], sequences of exactly b tiles, of at least b, and the tiles in front of those of work b.
+__device__ int order_tiles(const int* starts, int s0, int s1, int rows, bool most_first, int* counts, int bins, int4* out, int cap, int* red) {
+  const int tid = threadIdx.x;
+  int longest = 0;
+  for (int i = s0 + tid; i < s1; i += kPlanThreads) longest = max(longest, (starts[i + 1] - starts[i] + rows - 1) / rows);
+  block_scan(longest, red, true);
+  __syncthreads();
+  longest = red[31];
+  const int used = longest + 2;                    // bins 0 to longest + 1, the last one empty
+  int *exact = counts, *least = counts + bins, *before = least + bins;
+  for (int b = tid; b < used; b += kPlanThreads) exact[b] = 0;
+  __syncthreads();
+  for (int i = s0 + tid; i < s1; i += kPlanThreads) atomicAdd(exact + (starts[i + 1] - starts[i] + rows - 1) / rows, 1);
+  __syncthreads();
+  int carry = 0;
+  for (int at = 0; at < used; at += kPlanThreads) {
+    const int b = used - 1 - (at + tid);
+    const int v = carry + block_scan(b >= 0 ? exact[b] : 0, red, false);
+    if (b >= 0) least[b] = v;
+    __syncthreads();
+    carry += red[31];
+  }
+  __syncthreads();
+  carry = 0;
+  for (int at = 0; at < used; at += kPlanThreads) {
+    const int i = at + tid, b = most_first ? used - 1 - i : i;
+    const int own = b >= 1 && b < used ? least[b] : 0;
+    const int v = carry + block_scan(own, red, false);
+    if (b >= 0 && b < used) before[b] = v - own;
+    __syncthreads();
+    carry += red[31];
+  }
+  __syncthreads();
+  const int lane = tid & 31;
+  for (int i = s0 + (tid >> 5); i < s1; i += kPlanThreads / 32) {          // a warp a sequence
+    const int begin = starts[i], end = starts[i + 1], tiles = (end - begin + rows - 1) / rows;
+    int place = 0;
+    if (lane == 0) place = least[tiles + 1] + atomicSub(exact + tiles, 1) - 1;
+    place = __shfl_sync(0xffffffffu, place, 0);
+    for (int t = lane; t < tiles; t += 32) {
+      const int at = before[most_first ? t + 1 : tiles - t] + place;
+      if (at < cap) out[at] = make_int4(begin, end, t, begin / kAttnBwdRows + i);
+    }
+  }
+  __syncthreads();
+  return carry;
+}
+
+// One CTA.  Forward, the longest tiles first, so that the last ones to start are short.  Backward, the shortest first, because the
+// sums of dq pass from the last tile of a sequence to the first, and in groups, so that the sums under way stay in L2
+// (abs_attention_bwd.cu).
 __global__ void __launch_bounds__(kPlanThreads)
 attn_plan_kernel(const int* __restrict__ offsets, int n, int total, AttnPlanLayout l, int* plan) {
   __shared__ int red[32];
   __shared__ int bad;
   const int tid = threadIdx.x;
-  int* starts = plan + l.starts;
-  const int bins = l.bins + 1;
-  // per size of tile: sequences of exactly b tiles, then how many have been placed; sequences of at least b; tiles of more work
-  int* counts = plan + l.counts;
+  int *starts = plan + l.starts, *counts = plan + l.counts, *groups = plan + l.groups;
   if (tid == 0) bad = 0;
   pdl_wait();
-  for (int i = tid; i < 2 * bins; i += kPlanThreads) counts[(i / bins) * 3 * bins + i % bins] = 0;
   __syncthreads();
   // offsets inside [0, total] that never fall
   int carry = 0;
@@ -59,66 +104,30 @@ attn_plan_kernel(const int* __restrict__ offsets, int n, int total, AttnPlanLayo
       if (v != given) bad = 1;
     }
     __syncthreads();
-    if (tid == kPlanThreads - 1) red[0] = v;
-    __syncthreads();
-    carry = red[0];
+    carry = max(carry, red[31]);
   }
   __syncthreads();
-  for (int i = tid; i < n; i += kPlanThreads) {
-    const int len = starts[i + 1] - starts[i];
-    atomicAdd(counts + (len + kAttnFwdRows - 1) / kAttnFwdRows, 1);
-    atomicAdd(counts + 3 * bins + (len + kAttnBwdRows - 1) / kAttnBwdRows, 1);
-  }
-  __syncthreads();
-  for (int kind = 0; kind < 2; ++kind) {
-    int *exact = counts + kind * 3 * bins, *least = exact + bins, *before = least + bins;
-    // sequences of at least b tiles (sums from the last bin down), then the tiles of more (less) work than tile w = b - 1 has
-    carry = 0;
-    for (int at = 0; at < bins; at += kPlanThreads) {
-      const int b = bins - 1 - (at + tid);
-      const int v = carry + block_scan(b >= 0 ? exact[b] : 0, red, false);
-      if (b >= 0) least[b] = v;
-      __syncthreads();
-      if (tid == kPlanThreads - 1) red[0] = v;
-      __syncthreads();
-      carry = red[0];
+  const int fwd = order_tiles(starts, 0, n, kAttnFwdRows, true, counts, l.bins, reinterpret_cast<int4*>(plan + l.fwd), l.fwd_cap, red);
+  int tiles = 0, s0 = 0;
+  for (int g = 0; g < l.n_groups; ++g) {
+    if (tid == 0) groups[g] = tiles;
+    int lo = s0, hi = n;                           // the first sequence that begins behind the group
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if ((starts[mid] >> kAttnGroupBits) <= g) lo = mid + 1;
+      else hi = mid;
     }
-    __syncthreads();
-    carry = 0;
-    for (int at = 0; at < bins; at += kPlanThreads) {
-      const int i = at + tid, b = kind == 0 ? bins - 1 - i : i;       // bins 1.. hold tiles
-      const int own = b >= 1 && b < bins ? least[b] : 0;
-      const int v = carry + block_scan(own, red, false);
-      if (b >= 0 && b < bins) before[b] = v - own;
-      __syncthreads();
-      if (tid == kPlanThreads - 1) red[0] = v;
-      __syncthreads();
-      carry = red[0];
-    }
-    if (tid == 0) plan[kind == 0 ? kPlanFwdTiles : kPlanBwdTiles] = carry;
-    __syncthreads();
+    if (lo > s0)
+      tiles += order_tiles(starts, s0, lo, kAttnBwdRows, false, counts, l.bins, reinterpret_cast<int4*>(plan + l.bwd) + tiles,
+                           l.bwd_cap - tiles, red);
+    s0 = lo;
   }
   if (tid == 0) {
+    groups[l.n_groups] = tiles;
+    plan[kPlanFwdTiles] = fwd;
+    plan[kPlanBwdTiles] = tiles;
     plan[kPlanBad] = bad;
     plan[kPlanTotal] = total;
-  }
-  // a warp a sequence
-  const int lane = tid & 31;
-  for (int i = tid >> 5; i < n; i += kPlanThreads / 32) {
-    const int begin = starts[i], end = starts[i + 1];
-    for (int kind = 0; kind < 2; ++kind) {
-      const int rows = kind == 0 ? kAttnFwdRows : kAttnBwdRows, cap = kind == 0 ? l.fwd_cap : l.bwd_cap;
-      int *exact = counts + kind * 3 * bins, *least = exact + bins, *before = least + bins;
-      const int tiles = (end - begin + rows - 1) / rows;
-      int place = 0;
-      if (lane == 0) place = (tiles + 1 < bins ? least[tiles + 1] : 0) + atomicSub(exact + tiles, 1) - 1;
-      place = __shfl_sync(0xffffffffu, place, 0);
-      int4* out = reinterpret_cast<int4*>(plan + (kind == 0 ? l.fwd : l.bwd));
-      for (int t = lane; t < tiles; t += 32) {
-        const int work = kind == 0 ? t + 1 : tiles - t, at = before[work] + place;
-        if (at < cap) out[at] = make_int4(begin, end, t, 0);
-      }
-    }
   }
 }
 
@@ -267,5 +276,8 @@ extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const a
   const AttnBackward a{rows_of(dO), rows_of(Q), rows_of(K), rows_of(V), rows_of(O), lse, static_cast<const int*>(plan), out_of(dQ),
                        out_of(dK), out_of(dV), sequences, static_cast<int>(total), q_heads, kv_heads, head_dim, scale, scratch,
                        scratch_bytes};
-  return launch_attention_any_backward(ctx, a, dtype, static_cast<cudaStream_t>(stream));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  bool tc = dtype == ABS_BF16 && head_dim % 8 == 0;
+  for (const auto& x : all) tc = tc && tc_tensor(x.t);
+  return tc ? launch_attention_tc_backward(ctx, a, st) : launch_attention_any_backward(ctx, a, dtype, st);
 }

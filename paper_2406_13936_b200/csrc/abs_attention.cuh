@@ -2,6 +2,7 @@
 // (abs_attention_any.cu) and the tensor-core kernels (abs_attention_fwd.cu, abs_attention_bwd.cu) share.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "abs_internal.cuh"
@@ -14,22 +15,28 @@ constexpr int kAttnBwdRows = 128;          // keys of a backward tile
 
 // The plan of a batch, int32 words on the device: the header, then the records of the forward and of the backward tiles in
 // the order in which they are worked off, then what the plan's own kernel needs.
-//   record: first row and end of the tile's sequence, number of the tile in the sequence, 0
+//   record: first row and end of the tile's sequence, number of the tile in the sequence, and the sequence's first slot: a number
+//   such that slot + (tile of 128 rows) is each tile's own, below bwd_cap
+// Backward tiles are ordered within groups of sequences that begin in the same kAttnGroupRows rows, group g's from groups[g] to
+// groups[g + 1].
+constexpr int kAttnGroupBits = 16;
 struct AttnPlanLayout {
-  long long fwd, bwd, starts, counts, words;   // places of the parts, and their end
-  int fwd_cap, bwd_cap, bins;
+  long long fwd, bwd, groups, starts, counts, words;   // places of the parts, and their end
+  int fwd_cap, bwd_cap, bins, n_groups;
 };
 enum { kPlanFwdTiles = 0, kPlanBwdTiles = 1, kPlanBad = 2, kPlanTotal = 3, kPlanHeader = 16 };
 inline AttnPlanLayout attn_plan_layout(int n, int total) {
   AttnPlanLayout l;
   l.fwd_cap = total / kAttnFwdRows + n;
   l.bwd_cap = total / kAttnBwdRows + n;
-  l.bins = total / kAttnBwdRows + 2;           // tiles of one sequence: 0 to bins - 1
+  l.bins = total / kAttnBwdRows + 3;           // tiles of one sequence, and one more: 0 to bins - 1
+  l.n_groups = (total >> kAttnGroupBits) + 1;
   l.fwd = kPlanHeader;
   l.bwd = l.fwd + 4ll * l.fwd_cap;
-  l.starts = l.bwd + 4ll * l.bwd_cap;
+  l.groups = l.bwd + 4ll * l.bwd_cap;
+  l.starts = l.groups + l.n_groups + 1;
   l.counts = l.starts + n + 1;
-  l.words = l.counts + 6ll * (l.bins + 1);
+  l.words = l.counts + 3ll * l.bins;
   l.words = (l.words + 3) & ~3ll;
   return l;
 }
@@ -43,6 +50,7 @@ struct AttnOut {
   void* p;
   long long row, head;
 };
+bool encode_heads_map(const AttnRows& t, int total, int heads, int hd, CUtensorMap* map);      // boxes of 128 rows x 64 columns of a head
 struct AttnForward {
   AttnRows q, k, v;
   AttnOut o;
@@ -62,25 +70,25 @@ struct AttnBackward {
   size_t scratch_bytes;
 };
 
-// Scratch of a backward pass: delta [hq][total] fp32, then, for the tensor-core kernel, the sums of dq [total][hq][dpad] fp32 and
-// a counter for each 128 rows of a sequence and head.
+// Scratch of a backward pass: two rows of [hq][total] fp32 (delta; the tensor-core kernel: -lse log2 e and -delta), then, for the
+// tensor-core kernel, the sums of dq [hq][total][dpad] fp32 and a counter for each 128 rows of a sequence and head.
 struct AttnScratch {
   size_t delta, sums, counters, bytes;
   int dpad;
 };
 inline AttnScratch attn_scratch(int total, int hq, int hd, int n) {
   AttnScratch s;
+  auto up = [](size_t v) { return (v + 255) & ~static_cast<size_t>(255); };
   s.dpad = hd <= 64 ? 64 : 128;
   s.delta = 0;
-  s.sums = (static_cast<size_t>(hq) * total * sizeof(float) + 255) & ~static_cast<size_t>(255);
-  s.counters = s.sums + static_cast<size_t>(total) * hq * s.dpad * sizeof(float);
-  s.counters = (s.counters + 255) & ~static_cast<size_t>(255);
-  s.bytes = s.counters + static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) * sizeof(unsigned);
-  s.bytes = (s.bytes + 255) & ~static_cast<size_t>(255);
+  s.sums = up(static_cast<size_t>(hq) * total * 2 * sizeof(float));
+  s.counters = up(s.sums + static_cast<size_t>(total) * hq * s.dpad * sizeof(float));
+  s.bytes = up(s.counters + static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) * sizeof(unsigned));
   return s;
 }
 
 int launch_attention_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st);          // bf16 rows of 16-byte pieces, scale > 0
+int launch_attention_tc_backward(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st);
 int launch_attention_any(abs_ctx* ctx, const AttnForward& a, abs_dtype dtype, cudaStream_t st);
 int launch_attention_any_backward(abs_ctx* ctx, const AttnBackward& a, abs_dtype dtype, cudaStream_t st);
 

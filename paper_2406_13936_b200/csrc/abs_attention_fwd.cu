@@ -357,15 +357,6 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
   }
 }
 
-bool encode_heads_map(const AttnRows& t, int total, int heads, int hd, CUtensorMap* map) {
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(total)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(t.head) * 2, static_cast<cuuint64_t>(t.row) * 2};
-  const cuuint32_t box[3] = {64u, 1u, static_cast<cuuint32_t>(kHalf)}, ones[3] = {1u, 1u, 1u};
-  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(t.p), dims, strides, box, ones,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int HD>
 int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
   FwdMaps maps;
@@ -392,6 +383,15 @@ int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
 }
 
 }  // namespace
+
+bool encode_heads_map(const AttnRows& t, int total, int heads, int hd, CUtensorMap* map) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(total)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(t.head) * 2, static_cast<cuuint64_t>(t.row) * 2};
+  const cuuint32_t box[3] = {64u, 1u, static_cast<cuuint32_t>(kHalf)}, ones[3] = {1u, 1u, 1u};
+  return encode_tiled_fn()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(t.p), dims, strides, box, ones,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 int launch_attention_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
   if (encode_tiled_fn() == nullptr) return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");

@@ -286,6 +286,23 @@ def test_replicas_are_packed_sequences(ctx):
         assert torch.equal(oo, o[at]) and torch.equal(ll, lse[:, at])
 
 
+@pytest.mark.parametrize("lens,hq,hk,hd", [([512] * 40, 8, 8, 64), ([130, 700, 40] * 12, 8, 4, 128), ([100] * 300, 6, 6, 64)])
+def test_many_tiles_and_calls_behind_one_another(ctx, lens, hq, hk, hd):
+    """More tiles than a GPU holds at a time, and calls that nothing waits between: all the same, and right."""
+    b = Batch(lens, hq, hk, hd, "bf16", seed=14)
+    plan, o, lse = run_forward(ctx, b)
+    first = run_backward(ctx, b, plan, o, lse)
+    scratch = ctx.attention_scratch(b.total, hq, hk, hd, len(lens))
+    runs = [(b.outputs(), b.gradients(3.0)) for _ in range(12)]
+    for (o2, lse2), g in runs:
+        ctx.abs_attention(b.q, b.k, b.v, plan, o2, lse2, scale=b.scale)
+        ctx.abs_attention_backward(b.do, b.q, b.k, b.v, o2, lse2, plan, *g, scratch, scale=b.scale)
+    for (o2, lse2), g in runs:
+        assert torch.equal(o2, o) and torch.equal(lse2, lse) and all(torch.equal(x, y) for x, y in zip(g, first))
+    check_forward(b, o, lse)
+    check_backward(b, o, lse, *first)
+
+
 def test_capture_replay_and_new_offsets(ctx):
     """A captured forward and backward pass follows the inputs and the plan that are there when it is replayed."""
     b = Batch([300, 212], 4, 2, 64, "bf16", seed=10)
@@ -344,7 +361,7 @@ def test_bad_offsets_are_put_right(ctx, table, lens, bad):
 
 
 def test_plan_covers_every_tile_once(ctx):
-    """Every tile of every sequence once; forward the most work first, backward a sequence's last tile first."""
+    """Every tile of every sequence once; forward the most work first, backward the least within groups of 65536 rows."""
     gen = torch.Generator().manual_seed(13)
     lens = torch.randint(0, 1500, (700,), generator=gen)
     lens[::7] = 0
@@ -357,11 +374,14 @@ def test_plan_covers_every_tile_once(ctx):
     for kind, rows, at in ((0, 256, 16), (1, 128, 16 + 4 * fwd_cap)):
         count = int(words[kind])
         assert count <= (fwd_cap, bwd_cap)[kind]
-        recs = [tuple(r[:3].tolist()) for r in words[at:at + 4 * count].view(-1, 4)]
+        recs = [tuple(r.tolist()) for r in words[at:at + 4 * count].view(-1, 4)]
+        slots = {(r[3] + r[2]) for r in recs}
+        assert kind == 0 or (len(slots) == count and max(slots) < bwd_cap)
+        recs = [r[:3] for r in recs]
         want = {(int(start[i]), int(start[i + 1]), t) for i in range(n) for t in range(-(-int(lens[i]) // rows))}
         assert len(recs) == len(want) and set(recs) == want
-        work = [t + 1 if kind == 0 else -(-(e - s) // rows) - t for s, e, t in recs]
-        assert work == sorted(work, reverse=kind == 0)
+        work = [-t - 1 if kind == 0 else (s >> 16, -(-(e - s) // rows) - t) for s, e, t in recs]
+        assert work == sorted(work)
 
 
 def test_nothing_to_do(ctx):
