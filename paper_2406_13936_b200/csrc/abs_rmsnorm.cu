@@ -123,8 +123,9 @@ rms_forward_any_kernel(const RmsForward a) {
       unsigned top = 0u;
       for (int j = threadIdx.x; j < a.d; j += kRmsThreads) top = max(top, magnitude(again(j) * rstd * (w ? w[j] : 1.f)));
       scale = scale_of(block_max(top, red));
+      const float inv = 1.f / scale;
       unsigned char* q = static_cast<unsigned char*>(a.q.p) + m * a.q.ws + r * a.q.rs;
-      for (int j = threadIdx.x; j < a.d; j += kRmsThreads) q[j] = e4m3(again(j) * rstd * (w ? w[j] : 1.f) / scale);
+      for (int j = threadIdx.x; j < a.d; j += kRmsThreads) q[j] = e4m3(again(j) * rstd * (w ? w[j] : 1.f) * inv);
     }
     if (y)
       for (int j = threadIdx.x; j < a.d; j += kRmsThreads) y[j] = round1<T>(again(j) * rstd * (w ? w[j] : 1.f));
@@ -184,33 +185,65 @@ rms_weight_any_kernel(const RmsBackward a) {
   }
 }
 
-// Sums of rows: out[m][i] = sum_k in[m][i][k], `n` rows each, in a fixed order; eight lanes share them.
-struct RmsSums {
-  const float* in;
-  long long in_ws, in_group, in_rs;      // replica, group of rows, row
-  long long n;
-  float* out;
-  long long out_ws, out_group;
+// Pieces -> segments -> replica, in a fixed order: 32 columns of one replica and `per` of its segments a CTA.  Eight lanes share the
+// segments or, where there are few, the pieces of each.
+struct RmsJoin {
+  const float* part;                   // [M][samples][chunks][d], or NULL: the segments are in G
+  int chunks;
+  float* G;                            // segment i of replica m at m * g_ws + i * g_rs, or NULL (one segment)
+  long long g_rs, g_ws;
+  long long samples, per;
+  float* total;                        // sums over segments at m * t_ws + blockIdx.z * d, or NULL
+  long long t_ws;
   int d;
 };
 __global__ void __launch_bounds__(kRmsThreads)
-rms_sum_kernel(const RmsSums a) {
+rms_join_kernel(const RmsJoin a) {
   __shared__ float red[8][32];
   const int lane = threadIdx.x & 31, row = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
-  const float* p = a.in + blockIdx.y * a.in_ws + blockIdx.z * a.in_group + col;
+  const long long m = blockIdx.y, i0 = blockIdx.z * a.per, i1 = i0 + a.per < a.samples ? i0 + a.per : a.samples;
+  const bool in = col < a.d, by_segment = i1 - i0 >= 8 || a.part == nullptr;
   pdl_wait();
-  float s = 0.f;
-  if (col < a.d) {
+  float total = 0.f;
+  if (a.part == nullptr) {
+    if (in) {
+      const float* p = a.G + m * a.g_ws + col;
 #pragma unroll 8
-    for (long long k = row; k < a.n; k += 8) s += p[k * a.in_rs];
+      for (long long i = i0 + row; i < i1; i += 8) total += p[i * a.g_rs];
+    }
+  } else {
+    for (long long i = by_segment ? i0 + row : i0; i < i1; i += by_segment ? 8 : 1) {
+      const float* p = a.part + (m * a.samples + i) * a.chunks * a.d + col;
+      float s = 0.f;
+      if (in) {
+#pragma unroll 8
+        for (int c = by_segment ? 0 : row; c < a.chunks; c += by_segment ? 1 : 8) s += p[static_cast<long long>(c) * a.d];
+      }
+      if (!by_segment) {
+        __syncthreads();
+        red[row][lane] = s;
+        __syncthreads();
+        s = 0.f;
+        if (row == 0) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += red[k][lane];
+        }
+      }
+      if (in && (by_segment || row == 0)) {
+        if (a.G) a.G[m * a.g_ws + i * a.g_rs + col] = s;
+        total += s;
+      }
+    }
   }
-  red[row][lane] = s;
+  if (a.total == nullptr) return;
   __syncthreads();
-  if (row == 0 && col < a.d) {
-    s = 0.f;
+  red[row][lane] = total;
+  __syncthreads();
+  if (row == 0 && in) {
+    float s = 0.f;
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += red[k][lane];
-    a.out[blockIdx.y * a.out_ws + blockIdx.z * a.out_group + col] = s;
+    a.total[m * a.t_ws + static_cast<long long>(blockIdx.z) * a.d + col] = s;
   }
 }
 __global__ void __launch_bounds__(kRmsThreads)
@@ -218,6 +251,373 @@ rms_zero_kernel(float* p, long long ws, long long rs, long long n, int d) {
   pdl_wait();
   for (long long i = blockIdx.x; i < n; i += gridDim.x)
     for (int j = threadIdx.x; j < d; j += kRmsThreads) p[blockIdx.y * ws + i * rs + j] = 0.f;
+}
+
+// ---- rows in registers ------------------------------------------------------------------------------------
+// A group of `tpr` threads has a row: thread t its pieces t, t + tpr, ... of V elements, at most NV of them.  Pieces are of 16 bytes
+// where all rows are aligned to that, else of 8 or 4, or of one element.
+constexpr int kMostRow = 512;                        // threads of a row
+template <typename T, int V> struct RmsPiece;
+template <> struct RmsPiece<float, 4> { typedef uint4 Raw; };
+template <> struct RmsPiece<float, 2> { typedef uint2 Raw; };
+template <> struct RmsPiece<float, 1> { typedef uint32_t Raw; };
+template <> struct RmsPiece<__nv_bfloat16, 8> { typedef uint4 Raw; };
+template <> struct RmsPiece<__nv_bfloat16, 4> { typedef uint2 Raw; };
+template <> struct RmsPiece<__nv_bfloat16, 2> { typedef uint32_t Raw; };
+template <> struct RmsPiece<__nv_bfloat16, 1> { typedef unsigned short Raw; };
+__device__ __forceinline__ void open_two(uint32_t r, float& a, float& b) {
+  a = __uint_as_float(r << 16);
+  b = __uint_as_float(r & 0xffff0000u);
+}
+template <typename T, int V>
+__device__ __forceinline__ void open_piece(const typename RmsPiece<T, V>::Raw& r, float (&x)[V]) {
+  if constexpr (V * sizeof(T) == 16) {
+    Vec<T>::unpack(r, x);
+  } else if constexpr (sizeof(T) == 4) {
+    if constexpr (V == 2) {
+      x[0] = __uint_as_float(r.x);
+      x[1] = __uint_as_float(r.y);
+    } else {
+      x[0] = __uint_as_float(r);
+    }
+  } else if constexpr (V == 4) {
+    open_two(r.x, x[0], x[1]);
+    open_two(r.y, x[2], x[3]);
+  } else if constexpr (V == 2) {
+    open_two(r, x[0], x[1]);
+  } else {
+    x[0] = __uint_as_float(static_cast<uint32_t>(r) << 16);
+  }
+}
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T, int V>
+__device__ __forceinline__ typename RmsPiece<T, V>::Raw close_piece(const float (&x)[V]) {
+  if constexpr (V == 1) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(x[0]);
+    else return __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
+  } else if constexpr (V == 2) {
+    if constexpr (sizeof(T) == 4) return make_uint2(__float_as_uint(x[0]), __float_as_uint(x[1]));
+    else return two_bf16(x[0], x[1]);
+  } else if constexpr (V * sizeof(T) == 8) {
+    return make_uint2(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]));
+  } else if constexpr (sizeof(T) == 4) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  } else {
+    return make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
+  }
+}
+template <int V>
+__device__ __forceinline__ void weights_of(const float* w, int at, float (&x)[V]) {
+  if (w == nullptr) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = 1.f;
+  } else if constexpr (V < 4) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = __ldg(w + at + e);
+  } else if ((reinterpret_cast<uintptr_t>(w) & 15u) == 0) {
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(w + at + e));
+      x[e] = f.x; x[e + 1] = f.y; x[e + 2] = f.z; x[e + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = __ldg(w + at + e);
+  }
+}
+template <int V>
+__device__ __forceinline__ void store_e4m3(unsigned char* q, const float (&x)[V]) {
+  if constexpr (V == 1) {
+    *q = e4m3(x[0]);
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<unsigned short*>(q) = __nv_cvt_float2_to_fp8x2(make_float2(x[0], x[1]), __NV_SATFINITE, __NV_E4M3);
+  } else {
+    uint32_t w[V / 4];
+#pragma unroll
+    for (int e = 0; e < V; e += 4) {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[e], x[e + 1]), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[e + 2], x[e + 3]), __NV_SATFINITE, __NV_E4M3);
+      w[e / 4] = lo | (hi << 16);
+    }
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(q) = w[0];
+  }
+}
+// Sum (or largest) over a group's threads, the same in each.  red: 32 words of the group, used by one of these at a time.
+template <bool ONE_WARP>
+__device__ __forceinline__ float group_sum(float v, float* red, int group, int t, int tpr) {
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+  if constexpr (ONE_WARP) return v;
+  if ((t & 31) == 0) red[t >> 5] = v;
+  named_bar_sync(1 + group, tpr);
+  v = 0.f;
+  for (int w = 0; w < tpr / 32; ++w) v += red[w];
+  return v;
+}
+template <bool ONE_WARP>
+__device__ __forceinline__ unsigned group_max(unsigned v, float* red, int group, int t, int tpr) {
+  v = __reduce_max_sync(0xffffffffu, v);
+  if constexpr (ONE_WARP) return v;
+  if ((t & 31) == 0) red[t >> 5] = __uint_as_float(v);
+  named_bar_sync(1 + group, tpr);
+  for (int w = 0; w < tpr / 32; ++w) v = max(v, __float_as_uint(red[w]));
+  return v;
+}
+
+// A row a group, one each; the bytes under way come from the number of groups on an SM, so at most 64 registers a thread.  (A group that
+// loads its next row ahead needs 100 and more: 4099 x 4096 bf16 27 us for 23.)
+template <typename T, int V, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(ONE_WARP ? 256 : kMostRow, ONE_WARP ? 4 : 2)
+rms_forward_kernel(const RmsForward a, int tpr, int pieces) {
+  typedef typename RmsPiece<T, V>::Raw Raw;
+  __shared__ float red_mem[2][4][32];
+  const int group = threadIdx.x / tpr, t = threadIdx.x - group * tpr, groups = blockDim.x / tpr;
+  const unsigned rows = static_cast<unsigned>(a.rows), rr = blockIdx.x * groups + group;      // (at most 2^31 of all replicas)
+  pdl_wait();
+  if (rr >= rows * a.M) return;                      // (a whole group: its barriers are its own)
+  const long long m = rr / rows, r = rr - m * rows;
+  const Raw* x = reinterpret_cast<const Raw*>(static_cast<const T*>(a.x.p) + m * a.x.ws + r * a.x.rs);
+  const Raw* res = reinterpret_cast<const Raw*>(static_cast<const T*>(a.r.p) + m * a.r.ws + r * a.r.rs);
+  Raw rx[NV], rr_[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+    if (v < pieces) {
+      rx[k] = __ldcs(x + v);
+      if (a.r.p) rr_[k] = __ldcs(res + v);
+    }
+  }
+  float h[NV][V];
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+    if (v < pieces) {
+      open_piece<T, V>(rx[k], h[k]);
+      if (a.r.p) {
+        float o[V];
+        open_piece<T, V>(rr_[k], o);
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[k][e] += o[e];
+        const Raw sum = close_piece<T, V>(h[k]);
+        open_piece<T, V>(sum, h[k]);
+        if (a.h.p) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.h.p) + m * a.h.ws + r * a.h.rs) + v, sum);
+      } else if (a.h.p) {
+        __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.h.p) + m * a.h.ws + r * a.h.rs) + v, rx[k]);
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) s = fmaf(h[k][e], h[k][e], s);
+    }
+  }
+  s = group_sum<ONE_WARP>(s, red_mem[0][ONE_WARP ? 0 : group], group, t, tpr);
+  const float rstd = 1.0f / sqrtf(s / static_cast<float>(a.d) + a.eps);
+  const float* weight = a.weight ? a.weight + m * a.p_stride : nullptr;
+  unsigned top = 0u;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+    if (v < pieces) {
+      float w[V];
+      weights_of<V>(weight, v * V, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        h[k][e] = h[k][e] * rstd * w[e];
+        top = max(top, magnitude(h[k][e]));
+      }
+      if (a.y.p) __stcs(reinterpret_cast<Raw*>(static_cast<T*>(a.y.p) + m * a.y.ws + r * a.y.rs) + v, close_piece<T, V>(h[k]));
+    }
+  }
+  if (a.q.p) {
+    const float scale = scale_of(group_max<ONE_WARP>(top, red_mem[1][ONE_WARP ? 0 : group], group, t, tpr));
+    const float inv = 1.f / scale;
+    unsigned char* q = static_cast<unsigned char*>(a.q.p) + m * a.q.ws + r * a.q.rs;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) h[k][e] *= inv;
+        store_e4m3<V>(q + v * V, h[k]);
+      }
+    }
+    if (t == 0) a.scales[rr] = scale;
+  }
+  if (t == 0 && a.rstd) a.rstd[rr] = rstd;
+}
+
+// ---- rows through a ring in shared memory ------------------------------------------------------------------------
+// Backward, rows of aligned pieces: a thread copies its own pieces of the rows ahead into its own places of a ring (cp.async), so what is
+// under way does not depend on registers and nobody waits for anybody else's copies.  A CTA has a piece of a segment and its groups take
+// the rows in turn, the sums of dw staying in registers; or (by_group) every group has a segment of its own.
+constexpr int kDeep = 4;                             // rows of a group's ring
+__device__ __forceinline__ void ring_copy(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+template <typename T, int NV, bool ONE_WARP>
+__global__ void __launch_bounds__(ONE_WARP ? 128 : kMostRow)
+rms_backward_ring_kernel(const RmsBackward a, int tpr, int pieces, int by_group) {
+  constexpr int V = 16 / sizeof(T);
+  extern __shared__ __align__(16) unsigned char ring_mem[];          // [kDeep][3][NV][threads] pieces; the groups' sums afterwards
+  __shared__ float red_mem[2][4][32];
+  const int group = threadIdx.x / tpr, t = threadIdx.x - group * tpr, groups = blockDim.x / tpr;
+  const uint32_t step = blockDim.x * 16u, mine = smem_u32(ring_mem) + threadIdx.x * 16u;
+  const long long job = by_group ? static_cast<long long>(blockIdx.x) * groups + group : blockIdx.x;
+  const long long segments = static_cast<long long>(a.M) * a.samples;
+  const long long seg = by_group ? job : job / a.chunks;
+  const bool live = seg < segments;
+  const long long m = live ? seg / a.samples : 0;
+  const long long first = by_group || !live ? 0 : (job - seg * a.chunks) * a.chunk;
+  const long long n = !live ? 0 : by_group ? a.tokens : (a.tokens - first < a.chunk ? a.tokens - first : a.chunk);
+  const int stride = by_group ? 1 : groups, off = by_group ? 0 : group;
+  const int count = n > off ? static_cast<int>((n - off + stride - 1) / stride) : 0;                 // this group's rows
+  long long row = live ? (seg - m * a.samples) * a.tokens + first + off : 0;                         // of the replica
+  const bool with_dh = a.dh.p != nullptr;
+  const char* c_dy = reinterpret_cast<const char*>(static_cast<const T*>(a.dy.p) + m * a.dy.ws + row * a.dy.rs) + t * 16;
+  const char* c_h = reinterpret_cast<const char*>(static_cast<const T*>(a.h.p) + m * a.h.ws + row * a.h.rs) + t * 16;
+  const char* c_dh = reinterpret_cast<const char*>(static_cast<const T*>(a.dh.p) + m * a.dh.ws + row * a.dh.rs) + t * 16;
+  const float* rstd_in = a.rstd + m * a.samples * a.tokens + row;
+  pdl_wait();
+  int copied = 0;
+  uint32_t c_at = 0;
+  auto copy_row = [&]() {
+    if (copied < count) {
+      const uint32_t to = mine + c_at * (3u * NV) * step;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        if (t + k * tpr < pieces) {
+          ring_copy(to + k * step, c_dy + k * tpr * 16);
+          ring_copy(to + (NV + k) * step, c_h + k * tpr * 16);
+          if (with_dh) ring_copy(to + (2 * NV + k) * step, c_dh + k * tpr * 16);
+        }
+      }
+      ++copied;
+      c_dy += stride * a.dy.rs * sizeof(T);
+      c_h += stride * a.h.rs * sizeof(T);
+      c_dh += stride * a.dh.rs * sizeof(T);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    c_at = c_at + 1 == kDeep ? 0 : c_at + 1;
+  };
+#pragma unroll
+  for (int k = 0; k < kDeep - 1; ++k) copy_row();
+  float next = count > 0 ? __ldg(rstd_in) : 0.f;
+  const float* weight = a.weight ? a.weight + m * a.p_stride : nullptr;
+  float dw[NV][V], kept[ONE_WARP ? NV : 1][V];       // (a row of one warp leaves registers for the weight)
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) dw[k][e] = 0.f;
+    if (ONE_WARP && t + k * tpr < pieces) weights_of<V>(weight, (t + k * tpr) * V, kept[k]);
+  }
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  uint32_t at = 0;
+  int flip = 0;
+  for (int i = 0; i < count; ++i) {
+    copy_row();
+    const float rstd = next;
+    rstd_in += stride;
+    if (i + 1 < count) next = __ldg(rstd_in);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
+    const uint32_t from = mine + at * (3u * NV) * step;
+    at = at + 1 == kDeep ? 0 : at + 1;
+    float g[NV][V], xh[NV][V];
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) {
+        float w[V];
+        Vec<T>::unpack(lds128(from + k * step), g[k]);
+        Vec<T>::unpack(lds128(from + (NV + k) * step), xh[k]);
+        if constexpr (!ONE_WARP) weights_of<V>(weight, v * V, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if constexpr (ONE_WARP) w[e] = kept[k][e];
+          xh[k][e] *= rstd;
+          dw[k][e] = fmaf(g[k][e], xh[k][e], dw[k][e]);
+          g[k][e] *= w[e];
+          s = fmaf(g[k][e], xh[k][e], s);
+        }
+      }
+    }
+    if (a.dx.p != nullptr) {
+      const float c = group_sum<ONE_WARP>(s, red_mem[flip][ONE_WARP ? 0 : group], group, t, tpr) * inv_d;
+      flip ^= 1;
+      char* dx = reinterpret_cast<char*>(static_cast<T*>(a.dx.p) + m * a.dx.ws + row * a.dx.rs);
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int v = t + k * tpr;
+        if (v < pieces) {
+          float o[V];
+          if (with_dh) {
+            Vec<T>::unpack(lds128(from + (2 * NV + k) * step), o);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] = fmaf(rstd, fmaf(-xh[k][e], c, g[k][e]), o[e]);
+          __stcs(reinterpret_cast<uint4*>(dx) + v, close_piece<T, V>(o));
+        }
+      }
+    }
+    row += stride;
+  }
+  if (a.out == nullptr) return;
+  float* out = a.part ? a.part + job * a.d : a.out + m * a.o_ws + (seg - m * a.samples) * a.o_rs;
+  if (!by_group && groups > 1) {                     // the groups' sums, in order, through the ring's place
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float* sums = reinterpret_cast<float*>(ring_mem);
+    __syncthreads();
+    if (group > 0) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int v = t + k * tpr;
+        if (v < pieces) {
+#pragma unroll
+          for (int e = 0; e < V; e += 4)
+            *reinterpret_cast<float4*>(sums + static_cast<size_t>(group - 1) * a.d + v * V + e) = make_float4(dw[k][e], dw[k][e + 1], dw[k][e + 2], dw[k][e + 3]);
+        }
+      }
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = t + k * tpr;
+      if (v < pieces) {
+        for (int o = 0; o < groups - 1; ++o) {
+#pragma unroll
+          for (int e = 0; e < V; e += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(sums + static_cast<size_t>(o) * a.d + v * V + e);
+            dw[k][e] += f.x; dw[k][e + 1] += f.y; dw[k][e + 2] += f.z; dw[k][e + 3] += f.w;
+          }
+        }
+      }
+    }
+  }
+  if (!live) return;
+  const bool wide = (reinterpret_cast<uintptr_t>(out) & 15u) == 0;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = t + k * tpr;
+    if (v < pieces) {
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        if (wide) {
+          *reinterpret_cast<float4*>(out + v * V + e) = make_float4(dw[k][e], dw[k][e + 1], dw[k][e + 2], dw[k][e + 3]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) out[v * V + e + q] = dw[k][e + q];
+        }
+      }
+    }
+  }
 }
 
 struct DeviceGuardRms {
@@ -255,11 +655,11 @@ unsigned rms_grid(const abs_ctx* ctx, long long work) {
 struct RmsPlan {
   long long samples, tokens, chunk;
   int chunks;
-  long long groups, per_group;       // of the totals' sum: groups of segments that are summed first, segments of a group
-  size_t sums_at;                    // floats in front of the groups' sums
+  long long groups, per_group;       // CTAs that share a column's segments, segments of one
+  size_t sums_at;                    // floats in front of those CTAs' totals
 };
 RmsPlan plan_rms(int M, long long samples, long long tokens, long long d, bool per_sample, bool totals, long long jobs_wanted,
-                 size_t workspace_bytes) {
+                 bool by_group, int sm_count, size_t workspace_bytes) {
   RmsPlan p = {};
   if (!per_sample) {
     tokens *= samples;
@@ -271,32 +671,119 @@ RmsPlan plan_rms(int M, long long samples, long long tokens, long long d, bool p
   long long chunks = (jobs_wanted + samples * M - 1) / (samples * M);
   if (chunks > (tokens + 7) / 8) chunks = (tokens + 7) / 8;            // eight rows a piece at least
   if (chunks * samples * M > room) chunks = room / (samples * M);
-  if (chunks < 1) chunks = 1;
+  if (chunks < 1 || by_group) chunks = 1;
   p.chunk = (tokens + chunks - 1) / chunks;
   if (p.chunk < 1) p.chunk = 1;
   p.chunks = static_cast<int>(tokens > 0 ? (tokens + p.chunk - 1) / p.chunk : 1);
   const long long used = p.chunks > 1 ? p.chunks * samples * M : 0;
   p.sums_at = static_cast<size_t>(used) * d;
-  p.groups = 1;
-  if (totals && per_sample && samples > 256) {
-    p.groups = (samples + 127) / 128;
-    if (p.groups > 1024) p.groups = 1024;
-    if (p.groups * M > room - used) p.groups = (room - used) / M;
-    if (p.groups < 1) p.groups = 1;
-  }
+  // segments of a CTA of rms_join_kernel: as many CTAs as fill the GPU twice, eight segments at least
+  const long long wide = (d + 31) / 32 * M;
+  p.groups = (2 * sm_count + wide - 1) / wide;
+  if (p.groups > (samples + 7) / 8) p.groups = (samples + 7) / 8;
+  if (totals && p.groups > 1 && p.groups * M > room - used) p.groups = (room - used) / M;
+  if (p.groups < 1) p.groups = 1;
   p.per_group = (samples + p.groups - 1) / p.groups;
-  if (p.per_group < 1) p.per_group = 1;
-  p.groups = samples > 0 ? (samples + p.per_group - 1) / p.per_group : 1;
+  p.groups = (samples + p.per_group - 1) / p.per_group;
   return p;
 }
 
+unsigned long long rms_bits(const void* p, int es, int M, long long rs, long long ws) {
+  return p == nullptr ? 0 : reinterpret_cast<uintptr_t>(p) | static_cast<unsigned long long>(rs) * es | (M > 1 ? static_cast<unsigned long long>(ws) * es : 0);
+}
+// Threads of a row of `pieces`, at most `most` pieces each; 0: too wide.
+int threads_of(long long pieces, int most) {
+  for (int tpr = 32; tpr <= kMostRow; tpr *= 2)
+    if (pieces <= static_cast<long long>(tpr) * most) return tpr;
+  return 0;
+}
+template <typename T, int V, int NV>
+int launch_forward(abs_ctx* ctx, const RmsForward& a, int tpr, cudaStream_t st) {
+  const int groups = tpr < 256 ? 256 / tpr : 1;
+  const long long grid = (a.rows * a.M + groups - 1) / groups;
+  auto kern = tpr == 32 ? rms_forward_kernel<T, V, NV, true> : rms_forward_kernel<T, V, NV, false>;
+  ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(tpr * groups), 0, st, a, tpr, a.d / V));
+  return ABS_OK;
+}
+// 32 elements a thread at most: what 64 registers leave room for.
+template <typename T, int V>
+int run_pieces(abs_ctx* ctx, const RmsForward& a, cudaStream_t st) {
+  const int tpr = threads_of(a.d / V, 32 / V > 16 ? 16 : 32 / V), nv = (a.d / V + tpr - 1) / tpr;
+  if constexpr (V == 8) {
+    switch (nv) {
+      case 1: return launch_forward<T, V, 1>(ctx, a, tpr, st);
+      case 2: return launch_forward<T, V, 2>(ctx, a, tpr, st);
+      case 3: return launch_forward<T, V, 3>(ctx, a, tpr, st);
+      default: return launch_forward<T, V, 4>(ctx, a, tpr, st);
+    }
+  } else if constexpr (V == 4) {
+    return nv <= 2 ? launch_forward<T, V, 2>(ctx, a, tpr, st) : nv <= 4 ? launch_forward<T, V, 4>(ctx, a, tpr, st)
+         : nv <= 6 ? launch_forward<T, V, 6>(ctx, a, tpr, st) : launch_forward<T, V, 8>(ctx, a, tpr, st);
+  } else {
+    return nv <= 4 ? launch_forward<T, V, 4>(ctx, a, tpr, st) : nv <= 8 ? launch_forward<T, V, 8>(ctx, a, tpr, st) : launch_forward<T, V, 16>(ctx, a, tpr, st);
+  }
+}
 template <typename T>
 int run_forward(abs_ctx* ctx, const RmsForward& a, cudaStream_t st) {
+  constexpr int es = sizeof(T);
+  const unsigned long long bits = rms_bits(a.x.p, es, a.M, a.x.rs, a.x.ws) | rms_bits(a.r.p, es, a.M, a.r.rs, a.r.ws) |
+                                  rms_bits(a.h.p, es, a.M, a.h.rs, a.h.ws) | rms_bits(a.y.p, es, a.M, a.y.rs, a.y.ws) |
+                                  static_cast<unsigned long long>(a.d) * es;
+  const unsigned long long q_bits = rms_bits(a.q.p, 1, a.M, a.q.rs, a.q.ws);
+  auto takes = [&](int V) { return (bits & (V * es - 1)) == 0 && (q_bits & (V - 1)) == 0 && threads_of(a.d / V, 32 / V > 16 ? 16 : 32 / V) > 0; };
+  if (a.rows <= (1ll << 31) / a.M) {
+    if constexpr (es == 2) {
+      if (takes(8)) return run_pieces<T, 8>(ctx, a, st);
+    }
+    if (takes(4)) return run_pieces<T, 4>(ctx, a, st);
+    if (takes(2)) return run_pieces<T, 2>(ctx, a, st);
+    if (takes(1)) return run_pieces<T, 1>(ctx, a, st);
+  }
   ABS_CUDA_TRY(ctx, launch_dependent(rms_forward_any_kernel<T>, dim3(rms_grid(ctx, a.rows * a.M)), dim3(kRmsThreads), 0, st, a));
   return ABS_OK;
 }
+
+// How a backward pass runs: rows in rings (threads of a row, pieces of a thread, threads of a CTA), or tpr = 0.
+struct RmsRows {
+  int tpr, NV, threads, by_group;
+};
 template <typename T>
-int run_backward(abs_ctx* ctx, const RmsBackward& a, bool sums, cudaStream_t st) {
+RmsRows plan_rows(const RmsBackward& a, long long tokens) {
+  constexpr int V = 16 / sizeof(T), es = sizeof(T);
+  const unsigned long long bits = rms_bits(a.dy.p, es, a.M, a.dy.rs, a.dy.ws) | rms_bits(a.h.p, es, a.M, a.h.rs, a.h.ws) |
+                                  rms_bits(a.dh.p, es, a.M, a.dh.rs, a.dh.ws) | rms_bits(a.dx.p, es, a.M, a.dx.rs, a.dx.ws) |
+                                  static_cast<unsigned long long>(a.d) * es;
+  RmsRows r = {0, 0, 0, 0};
+  if ((bits & 15u) != 0) return r;
+  r.tpr = threads_of(a.d / V, 4);
+  if (r.tpr == 0) return r;
+  r.NV = (a.d / V + r.tpr - 1) / r.tpr;
+  r.threads = r.tpr < 128 ? 128 : r.tpr;
+  if (static_cast<size_t>(kDeep) * 3 * r.NV * r.threads * 16 > 200 * 1024) r.tpr = 0;
+  r.by_group = tokens < r.threads / (r.tpr ? r.tpr : 1);
+  return r;
+}
+template <typename T, int NV>
+int launch_backward(abs_ctx* ctx, const RmsBackward& a, const RmsRows& r, cudaStream_t st) {
+  const int groups = r.threads / r.tpr;
+  const size_t smem = static_cast<size_t>(kDeep) * 3 * NV * r.threads * 16;       // (three times what the groups' sums take, or more)
+  const long long jobs = r.by_group ? (static_cast<long long>(a.M) * a.samples + groups - 1) / groups : static_cast<long long>(a.M) * a.samples * a.chunks;
+  auto kern = r.tpr == 32 ? rms_backward_ring_kernel<T, NV, true> : rms_backward_ring_kernel<T, NV, false>;
+  ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));
+  ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(static_cast<unsigned>(jobs)), dim3(r.threads), smem, st, a, r.tpr,
+                                     static_cast<int>(a.d * sizeof(T) / 16), r.by_group));
+  return ABS_OK;
+}
+template <typename T>
+int run_backward(abs_ctx* ctx, const RmsBackward& a, bool sums, const RmsRows& r, cudaStream_t st) {
+  if (r.tpr > 0) {
+    switch (r.NV) {
+      case 1: return launch_backward<T, 1>(ctx, a, r, st);
+      case 2: return launch_backward<T, 2>(ctx, a, r, st);
+      case 3: return launch_backward<T, 3>(ctx, a, r, st);
+      default: return launch_backward<T, 4>(ctx, a, r, st);
+    }
+  }
   if (sums) {                      // before dx, which may take the place of dy or h
     const long long work = static_cast<long long>(a.M) * a.samples * a.chunks * ((a.d + kRmsThreads - 1) / kRmsThreads);
     const long long most = 1 << 30;
@@ -377,37 +864,31 @@ extern "C" int abs_rms_norm_backward(abs_ctx* ctx, const void* dY, long long dy_
       ABS_CUDA_TRY(ctx, launch_dependent(rms_zero_kernel, dim3(1, M), dim3(kRmsThreads), 0, st, dW, grad_stride, 0ll, 1ll, static_cast<int>(d)));
     return ABS_OK;
   }
-  const RmsPlan p = plan_rms(M, samples, tokens, d, Gw != nullptr, dW != nullptr, ctx->sm_count * 8ll, ctx->workspace_bytes);
   RmsBackward a{{dY, dy_row_stride, dy_worker_stride}, {H, h_row_stride, h_worker_stride}, {dH, dh_row_stride, dh_worker_stride}, rstd,
-                weight, param_stride, {dX, dx_row_stride, dx_worker_stride}, M, p.samples, p.tokens, static_cast<int>(d), p.chunk,
-                p.chunks, nullptr, Gw ? Gw : dW, Gw ? g_row_stride : 0, Gw ? g_worker_stride : grad_stride};
+                weight, param_stride, {dX, dx_row_stride, dx_worker_stride}, M, samples, tokens, static_cast<int>(d), 0, 1, nullptr, nullptr,
+                0, 0};
+  // (without Gw a replica's rows are one segment)
+  const RmsRows r = dtype == ABS_F32 ? plan_rows<float>(a, Gw ? tokens : rows) : plan_rows<__nv_bfloat16>(a, Gw ? tokens : rows);
+  const RmsPlan p = plan_rms(M, samples, tokens, d, Gw != nullptr, dW != nullptr, ctx->sm_count * 8ll, r.by_group != 0, ctx->sm_count, ctx->workspace_bytes);
+  a.samples = p.samples;
+  a.tokens = p.tokens;
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  a.out = Gw ? Gw : dW;
+  a.o_rs = Gw ? g_row_stride : 0;
+  a.o_ws = Gw ? g_worker_stride : grad_stride;
   float* ws = static_cast<float*>(ctx->workspace);
   if (p.chunks > 1) a.part = ws;
-  rc = dtype == ABS_F32 ? run_backward<float>(ctx, a, sums, st) : run_backward<__nv_bfloat16>(ctx, a, sums, st);
+  rc = dtype == ABS_F32 ? run_backward<float>(ctx, a, sums, r, st) : run_backward<__nv_bfloat16>(ctx, a, sums, r, st);
   if (rc != ABS_OK || !sums) return rc;
-  if (p.chunks > 1) {              // pieces -> segments
-    for (long long s0 = 0; s0 < p.samples; s0 += 32768) {
-      const unsigned n = static_cast<unsigned>(p.samples - s0 < 32768 ? p.samples - s0 : 32768);
-      const RmsSums q{ws + s0 * p.chunks * d, p.samples * p.chunks * d, static_cast<long long>(p.chunks) * d, d, p.chunks, a.out + s0 * a.o_rs,
-                      a.o_ws, a.o_rs, static_cast<int>(d)};
-      ABS_CUDA_TRY(ctx, launch_dependent(rms_sum_kernel, dim3(col_tiles, M, n), dim3(kRmsThreads), 0, st, q));
-    }
-  }
-  if (Gw && dW) {                  // segments -> replica
-    const long long tail = p.samples - (p.groups - 1) * p.per_group;
-    if (p.groups == 1) {
-      const RmsSums q{Gw, g_worker_stride, 0, g_row_stride, p.samples, dW, grad_stride, 0, static_cast<int>(d)};
-      ABS_CUDA_TRY(ctx, launch_dependent(rms_sum_kernel, dim3(col_tiles, M), dim3(kRmsThreads), 0, st, q));
-    } else {
-      float* to = ws + p.sums_at;
-      const RmsSums q{Gw, g_worker_stride, p.per_group * g_row_stride, g_row_stride, p.per_group, to, p.groups * d, d, static_cast<int>(d)};
-      ABS_CUDA_TRY(ctx, launch_dependent(rms_sum_kernel, dim3(col_tiles, M, static_cast<unsigned>(p.groups - 1)), dim3(kRmsThreads), 0, st, q));
-      const RmsSums t{Gw + (p.groups - 1) * p.per_group * g_row_stride, g_worker_stride, 0, g_row_stride, tail, to + (p.groups - 1) * d,
-                      p.groups * d, 0, static_cast<int>(d)};
-      ABS_CUDA_TRY(ctx, launch_dependent(rms_sum_kernel, dim3(col_tiles, M), dim3(kRmsThreads), 0, st, t));
-      const RmsSums u{to, p.groups * d, 0, d, p.groups, dW, grad_stride, 0, static_cast<int>(d)};
-      ABS_CUDA_TRY(ctx, launch_dependent(rms_sum_kernel, dim3(col_tiles, M), dim3(kRmsThreads), 0, st, u));
-    }
+  if (p.chunks == 1 && !(Gw && dW)) return ABS_OK;          // in place already
+  const bool two = dW != nullptr && p.groups > 1;
+  const RmsJoin j{a.part, p.chunks, Gw, g_row_stride, g_worker_stride, p.samples, p.per_group, two ? ws + p.sums_at : dW,
+                  two ? p.groups * d : grad_stride, static_cast<int>(d)};
+  ABS_CUDA_TRY(ctx, launch_dependent(rms_join_kernel, dim3(col_tiles, M, static_cast<unsigned>(p.groups)), dim3(kRmsThreads), 0, st, j));
+  if (two) {
+    const RmsJoin k{nullptr, 1, ws + p.sums_at, d, p.groups * d, p.groups, p.groups, dW, grad_stride, static_cast<int>(d)};
+    ABS_CUDA_TRY(ctx, launch_dependent(rms_join_kernel, dim3(col_tiles, M), dim3(kRmsThreads), 0, st, k));
   }
   return ABS_OK;
 }
