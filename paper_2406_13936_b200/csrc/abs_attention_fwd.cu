@@ -25,7 +25,7 @@ namespace absk {
 namespace {
 
 constexpr int kThreadsF = 384;
-constexpr int kFewRegs = 56, kManyRegs = 224;  // of a thread of warps 0-3 and of the halves; together what 168 a thread are at the launch
+constexpr int kFewRegs = 88, kManyRegs = 208;  // of a thread of warps 0-3 and of the halves; together what 168 a thread are at the launch
 static_assert(128 * kFewRegs + 256 * kManyRegs == kThreadsF * 168, "");
 constexpr int kHalf = 128;                    // rows of a half, keys of a step
 constexpr float kRaise = 8.f;
@@ -259,24 +259,27 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         ok = warp_wait(s_full + 8u * t, steps_done & 1u, abort_flag, p.limit);
         if (!ok) break;
         tc_fence_after();
-        uint32_t s[kHalf];
+        // S is read twice, 32 columns at a time and the next ones under way, instead of being held: 128 more registers a thread spill
+        const bool diagonal = j == steps - 1;
+        uint32_t s[2][32];
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        tmem_load32(s_at, s[0]);
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) tmem_load32(s_at + c, s + c);
+        for (int c = 0; c < kHalf; c += 32) {
+          uint32_t* x = s[(c / 32) & 1];
+          tmem_loaded(x);
+          tmem_load32(s_at + ((c + 32) & (kHalf - 1)), s[(c / 32 + 1) & 1]);       // (after the last: the first again)
+          if (diagonal) {
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) tmem_loaded(s + c);
-        if (j == steps - 1) {                                    // the diagonal
+            for (int e = 0; e < 32; ++e)
+              if (c + e <= r) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[e]));
+          } else {
 #pragma unroll
-          for (int c = 0; c < kHalf; ++c) s[c] = c > r ? 0xff800000u : s[c];
+            for (int e = 0; e < 32; e += 8)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], __uint_as_float(x[e + k])), __uint_as_float(x[e + k + 4]));
+          }
         }
-        float top[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(s[c]);
-#pragma unroll
-        for (int c = 4; c < kHalf; c += 8)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            top[e] = c + 4 + e < kHalf ? fmaxf(fmaxf(top[e], __uint_as_float(s[c + e])), __uint_as_float(s[c + 4 + e]))
-                                       : fmaxf(top[e], __uint_as_float(s[c + e]));
         const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.by;
         if (__any_sync(0xffffffffu, most > m + kRaise)) {
           const float next = fmaxf(m, most);
@@ -299,16 +302,23 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         const uint64_t ref2 = pack2f(ref, ref);
         uint64_t part[2] = {pack2f(0.f, 0.f), pack2f(0.f, 0.f)};
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 64) {
-          uint32_t w[32];
+        for (int c = 0; c < kHalf; c += 32) {
+          uint32_t* x = s[(c / 32) & 1];
+          tmem_loaded(x);
+          if (c + 32 < kHalf) tmem_load32(s_at + c + 32, s[(c / 32 + 1) & 1]);
+          if (diagonal) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float2 x = unpack2f(fma2f(pack2f(__uint_as_float(s[c + 2 * e]), __uint_as_float(s[c + 2 * e + 1])), by2, ref2));
-            const float a = exp2_approx(x.x), b = exp2_approx(x.y);
-            part[e & 1] = add2f(part[e & 1], pack2f(a, b));
-            w[e] = bf16_pair(a, b);
+            for (int e = 0; e < 32; ++e) x[e] = c + e > r ? 0xff800000u : x[e];
           }
-          tmem_store32(s_at + c / 2, w);
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 y = unpack2f(fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2));
+            const float u = exp2_approx(y.x), v = exp2_approx(y.y);
+            part[e & 1] = add2f(part[e & 1], pack2f(u, v));
+            w[e] = bf16_pair(u, v);
+          }
+          tmem_store16(s_at + c / 2, w);                         // over columns that have been read
         }
         const float2 all = unpack2f(add2f(part[0], part[1]));
         sum += all.x + all.y;
