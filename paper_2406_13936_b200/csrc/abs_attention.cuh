@@ -71,7 +71,8 @@ struct AttnBackward {
 };
 
 // Scratch of a backward pass: two rows of [hq][total] fp32 (delta; the tensor-core kernel: -lse log2 e and -delta), then, for the
-// tensor-core kernel, the sums of dq [hq][total][dpad] fp32 and a counter for each 128 rows of a sequence and head.
+// tensor-core kernel, the sums of dq [hq][total][dpad] fp32 and a counter for each 128 rows of a sequence and head,
+// and one of the tiles taken.
 struct AttnScratch {
   size_t delta, sums, counters, bytes;
   int dpad;
@@ -83,7 +84,7 @@ inline AttnScratch attn_scratch(int total, int hq, int hd, int n) {
   s.delta = 0;
   s.sums = up(static_cast<size_t>(hq) * total * 2 * sizeof(float));
   s.counters = up(s.sums + static_cast<size_t>(total) * hq * s.dpad * sizeof(float));
-  s.bytes = up(s.counters + static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) * sizeof(unsigned));
+  s.bytes = up(s.counters + (static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) + 1) * sizeof(unsigned));
   return s;
 }
 

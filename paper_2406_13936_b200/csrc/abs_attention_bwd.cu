@@ -10,21 +10,21 @@
 // memory, dK += dS' Q and dQ = dS K with dS' in shared memory once, read along its rows for the one and along its columns (MN-major)
 // for the other.
 //
-// dQ is a sum over key tiles, which different CTAs have.  They add to fp32 sums in scratch (bulk reductions, L2), for each block of
+// dQ is a sum over key tiles, which different CTAs have.  They add to fp32 sums in scratch (reductions in L2), for each block of
 // queries in a fixed order, so results repeat bit for bit: tile j of a sequence starts at query block j and goes up, so block i is
-// reached first by tile i, then by i - 1, and so on, each a step later than the one before; a counter a block says whose turn it is,
-// and the wait is rarely one.  The first of them stores instead of adding (nothing is cleared), and the last, tile 0, adds its own part
+// reached first by tile i, then by i - 1, and so on, each a step later than the one before; a counter says whose turn
+// it is, and the wait is rarely one.  The first of them stores instead of adding (nothing is cleared), and the last, tile 0, adds its own part
 // to the sums and writes dq: sequences of up to 128 rows never touch the sums.  Tiles are worked off shortest first within a group of
 // sequences and some of the heads (attn_plan_kernel), so that the sums under way stay in L2.
-// The grid is resident (a cooperative launch) and every CTA takes its tiles in that order, in which each comes after those that it waits
-// for, so the first unfinished tile of all never waits.
+// The grid is resident (a cooperative launch) and CTAs take the tiles in that order as they are free, in which each comes after those that it
+// waits for, so the first unfinished tile of all never waits.
 //
 // Rounded to fewer bits than 32: P and dS to bf16, as operands of the tensor core, and the results.
 //
 // Bound by the products at 128 columns a head (five of 512 clocks per 128 x 128 scores), at 64 (five of 256) by the products and by
 // what the softmax warps issue alike.
 //
-// Roles of the 16 warps: 0 loads (TMA), 1 issues the products, 2 loads lse and delta, 3 sends dq's sums, 4-7 take dq out of tensor memory,
+// Roles of the 16 warps: 0 loads (TMA), 1 issues the products, 2 takes tiles and loads lse and delta, 3 looks after the turns, 4-7 take dq out of tensor memory,
 // 8-15 are the softmax: 64 of a block's 128 queries each half.  While they compute P' of a block, dQ and dK of the block before and
 // dP' of this one run; while they compute dS', dV and the next S'.  All waits are bounded: one that runs out raises the CTA's
 // abort flag, every role falls through, copies in flight are waited for, tensor memory is freed, and what was not finished is NaN.
@@ -35,23 +35,20 @@ namespace absk {
 namespace {
 
 constexpr int kThreadsB = 512;
+constexpr uint32_t kItems = 4;                // tiles of a CTA that are known ahead of time
 constexpr int kBlock = 128;                   // keys of a tile, queries of a block
-constexpr int kRegsLoad = 72, kRegsOut = 104, kRegsSoft = 168;      // of a thread; together what 128 a thread are at the launch
+constexpr int kRegsLoad = 104, kRegsOut = 104, kRegsSoft = 152;      // of a thread; together what 128 a thread are at the launch
 static_assert(128 * (kRegsLoad + kRegsOut + 2 * kRegsSoft) == kThreadsB * 128, "");
 constexpr float kLog2eB = 1.4426950408889634f;
 
 template <int HD> struct BwdShape {
   static constexpr uint32_t kRows = kBlock * HD * 2;              // 128 rows of one head, bf16
   static constexpr uint32_t kKv = HD == 64 ? 2 : 1;               // places for a tile's K and V
-  static constexpr uint32_t kQ = 2, kDo = HD == 64 ? 2 : 1;       // places for Q and dO
-  static constexpr uint32_t kDs = kBlock * kBlock * 2;
-  static constexpr int kPart = 32;                                // columns of dq that a place for sums has
-  static constexpr int kParts = HD / kPart;
-  static constexpr uint32_t kStage = kBlock * kPart * 4;          // 16 KB
-  static constexpr uint32_t kStages = HD == 64 ? 3 : 1;
+  static constexpr uint32_t kQ = 2, kDo = 2;                      // places for Q and dO
+  static constexpr uint32_t kDs = kBlock * kBlock * 2, kDss = HD == 64 ? 2 : 1;     // dS' of a block, places for it
   static constexpr uint32_t kStats = 2 * kBlock * 4;              // -lse and -delta of a block
-  static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDs + kStages * kStage + 2 * kStats;
-  static constexpr size_t kSmem = kData + 1024 + 512;
+  static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDss * kDs + 2 * kStats;
+  static constexpr size_t kSmem = kData + 512;
   // tensor memory: S' (P' over it), dP', dV, dK, dQ (128 columns a head: over dP')
   static constexpr uint32_t kS = 0, kDp = 128, kDv = 256, kDk = 256 + HD, kDq = HD == 64 ? 384 : kDp;
 };
@@ -63,8 +60,8 @@ struct BwdMaps {
 struct BwdParams {
   AttnOut dq, dk, dv;
   const float* stats;                         // [2][hq][total]
-  float* sums;                                // [hq][total][HD], 16-byte pieces of row r permuted by r
-  unsigned* counters;                         // [hq][cap]
+  float* sums;                                // [hq][total][HD]; of 32 rows at a time: [HD / 4][rows] pieces of 16 bytes
+  unsigned* counters;                         // [hq][cap], then the next tile that nobody has
   const int* plan;
   const int* tiles;
   const int* groups;
@@ -102,43 +99,27 @@ __device__ __forceinline__ void bwd_step(const BwdParams& p, const BwdItem& it, 
   block = it.tile + t - h * it.blocks;
 }
 
-// Waits (bounded) until the counter has reached `target`.
-__device__ __forceinline__ bool wait_turn(const unsigned* c, unsigned target, volatile unsigned* abort_flag, long long limit) {
-  const long long t0 = clock64();
-  for (;;) {
-    unsigned v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(c) : "memory");
-    if (v >= target) return true;
-    if (*abort_flag || clock64() - t0 > limit) {
-      *abort_flag = 1u;
-      return false;
-    }
-    __nanosleep(64);
-  }
-}
-
 template <int HD>
 __global__ void __launch_bounds__(kThreadsB, 1)
 attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant__ BwdParams p) {
   typedef BwdShape<HD> Sh;
   constexpr uint32_t kRows = Sh::kRows;
-  extern __shared__ unsigned char smem_dyn[];
+  extern __shared__ __align__(1024) unsigned char smem_dyn[];       // (there is no room to align it here; checked below)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t raw = smem_u32(smem_dyn), kv_at = (raw + 1023u) & ~1023u, q_at = kv_at + 2u * Sh::kKv * kRows,
-                 do_at = q_at + Sh::kQ * kRows, ds_at = do_at + Sh::kDo * kRows, stage_at = ds_at + Sh::kDs,
-                 stats_at = stage_at + Sh::kStages * Sh::kStage;
-  unsigned char* base = smem_dyn + (kv_at - raw);
-  float* stats = reinterpret_cast<float*>(base + (stats_at - kv_at));
-  unsigned long long* bars = reinterpret_cast<unsigned long long*>(base + Sh::kData);
-  constexpr int kBars = 36;
+  const uint32_t kv_at = smem_u32(smem_dyn), q_at = kv_at + 2u * Sh::kKv * kRows,
+                 do_at = q_at + Sh::kQ * kRows, ds_at = do_at + Sh::kDo * kRows, stats_at = ds_at + Sh::kDss * Sh::kDs;
+  float* stats = reinterpret_cast<float*>(smem_dyn + (stats_at - kv_at));
+  unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + Sh::kData);
+  constexpr int kBars = 38;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
+  int4* ring = reinterpret_cast<int4*>(bars + kBars + 2);          // four items of two pieces of 16 bytes
   const uint32_t b0 = smem_u32(bars);
-  // two (sums: three) of each of the first ones
+  // two of each of the first ones
   const uint32_t kv_full = b0, kv_free = b0 + 16u, q_full = b0 + 32u, q_free = b0 + 48u, do_full = b0 + 64u, do_free = b0 + 80u,
-                 st_full = b0 + 96u, st_free = b0 + 112u, staged = b0 + 128u, stage_free = b0 + 152u, sums_in = b0 + 176u, s_full = b0 + 200u,
-                 p_full = b0 + 208u, dp_full = b0 + 216u, ds_full = b0 + 224u, dq_full = b0 + 232u, dq_read = b0 + 240u, acc_full = b0 + 248u,
-                 acc_free = b0 + 256u, landed = b0 + 264u, done_bar = b0 + 272u;
+                 st_full = b0 + 96u, st_free = b0 + 112u, s_full = b0 + 128u, p_full = b0 + 136u, dp_full = b0 + 144u, ds_full = b0 + 152u,
+                 dq_full = b0 + 160u, dq_read = b0 + 168u, acc_full = b0 + 176u, acc_free = b0 + 184u, landed = b0 + 192u, done_bar = b0 + 200u,
+                 turn_ok = b0 + 208u, added = b0 + 224u, item_full = b0 + 240u, item_free = b0 + 272u;
   if (threadIdx.x == 0) {
     for (uint32_t k = 0; k < 2; ++k) {
       mbar_init(kv_full + 8u * k, 1);
@@ -149,11 +130,12 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       mbar_init(do_free + 8u * k, 1);
       mbar_init(st_full + 8u * k, 1);
       mbar_init(st_free + 8u * k, 8);
+      mbar_init(turn_ok + 8u * k, 1);
+      mbar_init(added + 8u * k, 4);
     }
-    for (uint32_t k = 0; k < 3; ++k) {
-      mbar_init(staged + 8u * k, 4);
-      mbar_init(stage_free + 8u * k, 1);
-      mbar_init(sums_in + 8u * k, 1);
+    for (uint32_t k = 0; k < kItems; ++k) {
+      mbar_init(item_full + 8u * k, 1);
+      mbar_init(item_free + 8u * k, 15);                           // loads, products, turns, four of dq, eight of the softmax
     }
     mbar_init(s_full, 1);
     mbar_init(p_full, 8);
@@ -165,7 +147,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     mbar_init(acc_free, 8);
     mbar_init(landed, 1);
     mbar_init(done_bar, 1);
-    *abort_flag = 0u;
+    *abort_flag = (kv_at & 1023u) ? 1u : 0u;
+    for (uint32_t k = 0; k < 2 * kItems; ++k) ring[k] = make_int4(0, 0, 0, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc_all(smem_u32(tmem_slot));
@@ -174,13 +157,26 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const int items = __ldg(p.plan + kPlanBwdTiles) * p.hk;
+  unsigned* next_item = p.counters + static_cast<long long>(p.hq) * p.cap;
+  // The CTA's k-th tile; false: there is none (or a wait ran out).  last: whether this role is done with the place in the ring.
+  auto read_item = [&](uint32_t k) {
+    const int4 a = ring[2 * (k % kItems)], b = ring[2 * (k % kItems) + 1];
+    return BwdItem{a.x, a.y, a.z, a.w, b.x, b.y, b.z};
+  };
+  auto take_item = [&](uint32_t k, BwdItem& it) {
+    if (!warp_wait(item_full + 8u * (k % kItems), (k / kItems) & 1u, abort_flag, p.limit)) return false;
+    it = read_item(k);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(item_free + 8u * (k % kItems));
+    return it.steps > 0;
+  };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLoad));
     if (warp == 0) {
       // ---- loads -----------------------------------------------------------------------------------
       uint32_t lands = 0, tiles = 0, n = 0;                      // tiles and steps so far
-      bool ok = !p.drop_loads;
+      bool ok = !p.drop_loads && *abort_flag == 0u;
       auto copy = [&](const CUtensorMap* map, uint32_t to, int head, int row, uint32_t bar) {
         if (elect_lane()) {
 #pragma unroll
@@ -212,8 +208,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
       };
-      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
-        const BwdItem it = bwd_item(p, i);
+      BwdItem it;
+      while (ok && take_item(tiles, it)) {
         const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         if (tiles >= Sh::kKv) ok = warp_wait(kv_free + 8u * kv, (tiles / Sh::kKv - 1) & 1u, abort_flag, p.limit);
         if (!ok) break;
@@ -275,17 +271,10 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         __syncwarp();
       };
-      // dQ and dK of step m (counted over all tiles) from its dS'
-      auto gradients = [&](uint32_t m, bool first, uint32_t kvs) {
-        ok = ok && warp_wait(ds_full, m & 1u, abort_flag, p.limit);
-        if (ok && m > 0 && HD == 64) ok = warp_wait(dq_read, (m - 1) & 1u, abort_flag, p.limit);
-        if (!ok) return;
-        tc_fence_after();
+      // dK and dQ of step m (counted over all tiles) from its dS'
+      auto key_gradient = [&](uint32_t m, bool first) {
         if (elect_lane()) {
-          const uint32_t d = desc_at(ds_at), k_ = desc_at(kvs), q = desc_at(q_at + (m % Sh::kQ) * kRows);
-#pragma unroll
-          for (uint32_t k = 0; k < kBlock / 16; ++k) mma_ss(tmem + Sh::kDq, mn | (d + 128u * k), mn | (k_ + 128u * k), idesc_q, k > 0);
-          mma_commit(dq_full);
+          const uint32_t d = desc_at(ds_at + (m % Sh::kDss) * Sh::kDs), q = desc_at(q_at + (m % Sh::kQ) * kRows);
 #pragma unroll
           for (uint32_t k = 0; k < kBlock / 16; ++k) {
             const uint32_t off = (k / 4) * (kBlock * 128u / 16u) + (k % 4) * 2u;
@@ -295,8 +284,17 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         __syncwarp();
       };
-      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
-        const BwdItem it = bwd_item(p, i);
+      auto query_gradient = [&](uint32_t m, uint32_t kvs) {
+        if (elect_lane()) {
+          const uint32_t d = desc_at(ds_at + (m % Sh::kDss) * Sh::kDs), k_ = desc_at(kvs);
+#pragma unroll
+          for (uint32_t k = 0; k < kBlock / 16; ++k) mma_ss(tmem + Sh::kDq, mn | (d + 128u * k), mn | (k_ + 128u * k), idesc_q, k > 0);
+          mma_commit(dq_full);
+        }
+        __syncwarp();
+      };
+      BwdItem it;
+      while (ok && take_item(tiles, it)) {
         const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         ok = warp_wait(kv_full + 8u * kv, (tiles / Sh::kKv) & 1u, abort_flag, p.limit);
         ok = ok && warp_wait(q_full + 8u * (n % Sh::kQ), (n / Sh::kQ) & 1u, abort_flag, p.limit);
@@ -304,13 +302,27 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         tc_fence_after();
         scores(Sh::kS, kvs, q_at + (n % Sh::kQ) * kRows, s_full);
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
-          if (t > 0) gradients(n - 1, t == 1, kvs);
+          // dK and dQ of the step before and this one's dP'.  At 128 columns dQ lies over dP': it is taken out before dP' is written, while
+          // dK runs.  At 64 it has a place of its own, which may still be read: it comes last.
+          if (t > 0) {
+            ok = warp_wait(ds_full, (n - 1) & 1u, abort_flag, p.limit);
+            if (!ok) break;
+            tc_fence_after();
+            if (HD == 128) query_gradient(n - 1, kvs);
+            key_gradient(n - 1, t == 1);
+          }
           const uint32_t ds = n % Sh::kDo;
-          ok = ok && warp_wait(do_full + 8u * ds, (n / Sh::kDo) & 1u, abort_flag, p.limit);
-          if (HD == 128 && n > 0) ok = ok && warp_wait(dq_read, (n - 1) & 1u, abort_flag, p.limit);       // dQ of the step before lies over dP'
+          ok = warp_wait(do_full + 8u * ds, (n / Sh::kDo) & 1u, abort_flag, p.limit);
+          if (HD == 128 && n > 0) ok = ok && warp_wait(dq_read, (n - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           tc_fence_after();
           scores(Sh::kDp, kvs + kRows, do_at + ds * kRows, dp_full);
+          if (HD == 64 && t > 0) {
+            if (n > 1) ok = warp_wait(dq_read, (n - 2) & 1u, abort_flag, p.limit);
+            if (!ok) break;
+            tc_fence_after();
+            query_gradient(n - 1, kvs);
+          }
           ok = warp_wait(p_full, n & 1u, abort_flag, p.limit);
           if (ok && t == 0 && tiles > 0) ok = warp_wait(acc_free, (tiles - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
@@ -332,7 +344,12 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           }
         }
         if (!ok) break;
-        gradients(n - 1, it.steps == 1, kvs);
+        ok = warp_wait(ds_full, (n - 1) & 1u, abort_flag, p.limit);
+        if (HD == 64 && n > 1) ok = ok && warp_wait(dq_read, (n - 2) & 1u, abort_flag, p.limit);
+        if (!ok) break;
+        tc_fence_after();
+        query_gradient(n - 1, kvs);
+        key_gradient(n - 1, it.steps == 1);
         if (elect_lane()) {
           mma_commit(acc_full);
           mma_commit(kv_free + 8u * kv);
@@ -345,11 +362,28 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       volatile unsigned ignore = 0u;
       mbar_wait(done_bar, 0u, &ignore, p.limit);                 // no product in flight when tensor memory is freed
     } else if (warp == 2) {
-      // ---- lse and delta of a block's queries ------------------------------------------------------
-      uint32_t n = 0;
+      // ---- the tiles, and lse and delta of a block's queries --------------------------------------------
+      // Tiles are taken in order by whoever is free, one ahead of the one whose rows are being fetched.
+      uint32_t n = 0, told = 0;
       bool ok = true;
-      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
-        const BwdItem it = bwd_item(p, i);
+      auto tell = [&]() {                                          // the next tile (after the last: one without steps)
+        if (told >= kItems) ok = ok && warp_wait(item_free + 8u * (told % kItems), (told / kItems - 1) & 1u, abort_flag, p.limit);
+        if (ok && lane == 0) {
+          const unsigned i = atomicAdd(next_item, 1u);
+          BwdItem it = {};
+          if (i < static_cast<unsigned>(items)) it = bwd_item(p, static_cast<int>(i));
+          ring[2 * (told % kItems)] = make_int4(it.begin, it.len, it.slot, it.tile);
+          ring[2 * (told % kItems) + 1] = make_int4(it.kv, it.blocks, it.steps, 0);
+          mbar_arrive(item_full + 8u * (told % kItems));
+        }
+        __syncwarp();
+        if (ok) ++told;
+      };
+      tell();
+      for (uint32_t k = 0; ok; ++k) {
+        const BwdItem it = read_item(k);
+        if (it.steps == 0) break;
+        tell();
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
           int head, block;
           bwd_step(p, it, t, head, block);
@@ -377,140 +411,143 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
       }
     } else if (lane == 0) {
-      // ---- dq's sums: taken to scratch in turn, and for tile 0 fetched from there ------------------
-      // A place is filled by the dq warps (staged) and sent, or filled from scratch (sums_in) and read by them (staged); either way
-      // stage_free ends the use, here, before the next one begins: nobody is ever two uses ahead of anybody.
-      uint32_t m = 0, read = 0;                                  // places used so far; bit s: place s was last read by the dq warps
-      bool ok = true;
-      for (int i = blockIdx.x; i < items && ok; i += gridDim.x) {
-        const BwdItem it = bwd_item(p, i);
-        for (int t = 0; t < it.steps && ok; ++t) {
-          int head, block;
-          bwd_step(p, it, t, head, block);
-          if (block == 0) continue;                              // tile 0's own block: no sums
-          unsigned* turn = p.counters + static_cast<long long>(head) * p.cap + it.slot + block;
-          const int rows = min(kBlock, it.len - block * kBlock);
-          float* to = p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock) * HD;
-          const uint32_t bytes = static_cast<uint32_t>(rows) * Sh::kPart * 4u;
-          const unsigned before = static_cast<unsigned>(block - it.tile);      // tiles whose parts are in
-          for (int part = 0; part < Sh::kParts && ok; ++part, ++m) {
-            const uint32_t s = m % Sh::kStages, use = m / Sh::kStages, at = stage_at + s * Sh::kStage;
-            // parts lie one after the other: [part][rows of the block][kPart]
-            float* dst = to + static_cast<long long>(part) * rows * Sh::kPart;
-            if ((read >> s) & 1u) {
-              ok = mbar_wait(staged + 8u * s, (use - 1) & 1u, abort_flag, p.limit);
-              if (ok) mbar_arrive(stage_free + 8u * s);
-            }
-            if (ok && it.tile != 0) ok = mbar_wait(staged + 8u * s, use & 1u, abort_flag, p.limit);
-            if (ok && part == 0 && before > 0) ok = wait_turn(turn, before, abort_flag, p.limit);
-            if (!ok) break;
-            asm volatile("fence.proxy.async.global;" ::: "memory");
-            if (it.tile == 0) {
-              read |= 1u << s;
-              mbar_expect_tx(sums_in + 8u * s, bytes);
-              asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(at), "l"(dst),
-                           "r"(bytes), "r"(sums_in + 8u * s)
-                           : "memory");
-            } else {
-              read &= ~(1u << s);
-              if (before == 0)
-                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(at), "r"(bytes) : "memory");
-              else
-                asm volatile("cp.reduce.async.bulk.global.shared::cta.bulk_group.add.f32 [%0], [%1], %2;" ::"l"(dst), "r"(at), "r"(bytes) : "memory");
-              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-              asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-              mbar_arrive(stage_free + 8u * s);
-            }
-          }
-          if (ok && it.tile != 0) {
-            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+      // ---- turns: looks for the next step's and passes on those whose additions are done ---------------
+      // (both take their time in L2; the dq warps wait for neither)
+      struct Cursor {
+        uint32_t k, n;                                             // tiles and steps so far
+        int t;
+        bool have;
+        BwdItem it;
+      } look = {}, pass = {};
+      // (the place in the ring is given back behind the second of the two)
+      auto fetch = [&](Cursor& c) {
+        if (!c.have && mbar_test(item_full + 8u * (c.k % kItems), (c.k / kItems) & 1u)) {
+          c.it = read_item(c.k);
+          c.have = true;
+        }
+      };
+      auto step_on = [&](Cursor& c, bool second) {
+        ++c.n;
+        if (++c.t == c.it.steps) {
+          if (second) mbar_arrive(item_free + 8u * (c.k % kItems));
+          c.t = 0;
+          c.have = false;
+          ++c.k;
+        }
+      };
+      auto counter = [&](const Cursor& c, unsigned& before) {
+        int head, block;
+        bwd_step(p, c.it, c.t, head, block);
+        before = static_cast<unsigned>(block - c.it.tile);       // tiles whose parts are in
+        return p.counters + static_cast<long long>(head) * p.cap + c.it.slot + block;
+      };
+      long long since = clock64();
+      for (;;) {
+        fetch(pass);
+        if (pass.have && pass.it.steps == 0) break;
+        if (pass.have && mbar_test(added + 8u * (pass.n & 1u), (pass.n >> 1) & 1u)) {
+          if (pass.it.tile != 0) {
+            unsigned before;
+            unsigned* c = counter(pass, before);
             asm volatile("fence.acq_rel.gpu;" ::: "memory");
-            asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(turn) : "memory");
+            asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c) : "memory");
+          }
+          step_on(pass, true);
+          since = clock64();
+        }
+        fetch(look);
+        if (look.have && look.it.steps > 0 && look.n < pass.n + 2) {
+          unsigned before, v;
+          const unsigned* c = counter(look, before);
+          v = before;
+          if (before > 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(c) : "memory");
+          if (v >= before) {
+            mbar_arrive(turn_ok + 8u * (look.n & 1u));
+            step_on(look, false);
+            since = clock64();
           }
         }
+        if (*abort_flag || clock64() - since > p.limit) {
+          *abort_flag = 1u;
+          break;
+        }
       }
-      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-      // (what was fetched and not waited for by its readers, after an abort)
-      volatile unsigned ignore = 0u;
-      if (*abort_flag)
-        for (uint32_t s = 0; s < Sh::kStages; ++s)
-          for (uint32_t ph = 0; ph < 2; ++ph) mbar_wait(sums_in + 8u * s, ph, &ignore, 1000000);
     }
   } else if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOut));
-    // ---- dq out of tensor memory: a thread has a query's row -----------------------------------------
-    const int r = (warp & 3) * 32 + lane;
-    const uint32_t at_t = tmem + Sh::kDq + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-    uint32_t n = 0, m = 0;
-    uint32_t fetched = 0;                                        // bit s: parity of the fetches into place s
+    // ---- dq out of tensor memory and into the sums: a thread has a query's row -------
+    const int sub = warp & 3, r = sub * 32 + lane;
+    const uint32_t at_t = tmem + Sh::kDq + (static_cast<uint32_t>(sub * 32) << 16);
+    uint32_t n = 0;
     bool ok = true;
-    for (int i = blockIdx.x; i < items; i += gridDim.x) {
-      const BwdItem it = bwd_item(p, i);
+    BwdItem it;
+    for (uint32_t k = 0; take_item(k, it); ++k) {
       for (int t = 0; t < it.steps; ++t, ++n) {
         int head, block;
         bwd_step(p, it, t, head, block);
-        const int row = block * kBlock + r;
-        const bool live = row < it.len, last = it.tile == 0, alone = block == 0;
-        const uint32_t sw = static_cast<uint32_t>(r) & (Sh::kPart / 4 - 1);
+        const int row = block * kBlock + r, rows = min(32, it.len - block * kBlock - 32 * sub);      // of the warp's in the sequence
+        const bool live = row < it.len;
+        const unsigned before = static_cast<unsigned>(block - it.tile);                             // tiles whose parts are in
+        float4* sums = reinterpret_cast<float4*>(p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock + 32 * sub) * HD) + lane;
         ok = ok && warp_wait(dq_full, n & 1u, abort_flag, p.limit);
         tc_fence_after();
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head;
 #pragma unroll
-        for (int part = 0; part < Sh::kParts; ++part) {
-          uint32_t v[Sh::kPart];
+        for (int c0 = 0; c0 < HD; c0 += 64) {
+          uint32_t v[64];
           if (ok) {
-#pragma unroll
-            for (int c = 0; c < Sh::kPart; c += 32) tmem_load32(at_t + part * Sh::kPart + c, v + c);
-#pragma unroll
-            for (int c = 0; c < Sh::kPart; c += 32) tmem_loaded(v + c);
+            tmem_load32(at_t + c0, v);
+            tmem_load32(at_t + c0 + 32, v + 32);
+            tmem_loaded(v);
+            tmem_loaded(v + 32);
           }
-          if (part == Sh::kParts - 1 && ok) {
+          if (c0 + 64 >= HD && ok) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(dq_read);
           }
-          const uint32_t s = m % Sh::kStages, mine = stage_at + s * Sh::kStage + static_cast<uint32_t>(r) * (Sh::kPart * 4u);
-          if (!last) {
-            const uint32_t use = m / Sh::kStages;
-            if (ok && use > 0) ok = warp_wait(stage_free + 8u * s, (use - 1) & 1u, abort_flag, p.limit);
-            if (ok) {
+          if (c0 == 0) ok = ok && warp_wait(turn_ok + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, p.limit);
+          if (it.tile != 0) {
+            if (ok && live) {
 #pragma unroll
-              for (uint32_t c = 0; c < Sh::kPart / 4; ++c)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine + ((c ^ sw) << 4)), "r"(v[4 * c]), "r"(v[4 * c + 1]),
-                             "r"(v[4 * c + 2]), "r"(v[4 * c + 3])
-                             : "memory");
-              fence_async_smem();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(staged + 8u * s);
+              for (int c = 0; c < 16; ++c) {
+                float4* to = sums + static_cast<long long>(c0 / 4 + c) * rows;
+                if (before == 0)
+                  asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(v[4 * c]), "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
+                else
+                  asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(__uint_as_float(v[4 * c])),
+                               "f"(__uint_as_float(v[4 * c + 1])), "f"(__uint_as_float(v[4 * c + 2])), "f"(__uint_as_float(v[4 * c + 3]))
+                               : "memory");
+              }
             }
           } else {
-            if (!alone && ok) {
-              ok = warp_wait(sums_in + 8u * s, (fetched >> s) & 1u, abort_flag, p.limit);
-              fetched ^= 1u << s;
-              if (ok) {
+            if (ok && live && before > 0) {
 #pragma unroll
-                for (uint32_t c = 0; c < Sh::kPart / 4; ++c) {
-                  const uint4 x = lds128(mine + ((c ^ sw) << 4));
-                  v[4 * c] = __float_as_uint(__uint_as_float(v[4 * c]) + __uint_as_float(x.x));
-                  v[4 * c + 1] = __float_as_uint(__uint_as_float(v[4 * c + 1]) + __uint_as_float(x.y));
-                  v[4 * c + 2] = __float_as_uint(__uint_as_float(v[4 * c + 2]) + __uint_as_float(x.z));
-                  v[4 * c + 3] = __float_as_uint(__uint_as_float(v[4 * c + 3]) + __uint_as_float(x.w));
+              for (int h = 0; h < 16; h += 8) {
+                float4 x[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) x[c] = __ldcg(sums + static_cast<long long>(c0 / 4 + h + c) * rows);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                  v[4 * (h + c)] = __float_as_uint(__uint_as_float(v[4 * (h + c)]) + x[c].x);
+                  v[4 * (h + c) + 1] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 1]) + x[c].y);
+                  v[4 * (h + c) + 2] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 2]) + x[c].z);
+                  v[4 * (h + c) + 3] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 3]) + x[c].w);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(staged + 8u * s);
               }
             }
 #pragma unroll
-            for (int c = 0; c < Sh::kPart; c += 8) {
+            for (int c = 0; c < 64; c += 8) {
               uint32_t w[4];
 #pragma unroll
               for (int k = 0; k < 4; ++k)
                 w[k] = ok ? bf16_pair(__uint_as_float(v[c + 2 * k]) * p.scale, __uint_as_float(v[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
-              if (live && part * Sh::kPart + c < p.hd) *reinterpret_cast<uint4*>(out + part * Sh::kPart + c) = make_uint4(w[0], w[1], w[2], w[3]);
+              if (live && c0 + c < p.hd) *reinterpret_cast<uint4*>(out + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
             }
           }
-          if (!alone) ++m;
         }
+        __syncwarp();
+        if (ok && lane == 0) mbar_arrive(added + 8u * (n & 1u));
       }
     }
   } else {
@@ -523,8 +560,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     const uint64_t by2 = pack2f(p.by, p.by);
     uint32_t n = 0, tiles = 0;
     bool ok = true;
-    for (int i = blockIdx.x; i < items; i += gridDim.x, ++tiles) {
-      const BwdItem it = bwd_item(p, i);
+    BwdItem it;
+    for (; take_item(tiles, it); ++tiles) {
       for (int t = 0; t < it.steps && ok; ++t, ++n) {
         const bool diagonal = t % it.blocks == 0;
         const uint32_t st = n & 1u;
@@ -595,7 +632,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
               b[2 * k] = bf16_pair(x.x, x.y);
               b[2 * k + 1] = bf16_pair(y.x, y.y);
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ds_row + ((static_cast<uint32_t>((h + c) / 8) ^ sw) << 4)), "r"(b[0]),
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ds_row + (n % Sh::kDss) * Sh::kDs + ((static_cast<uint32_t>((h + c) / 8) ^ sw) << 4)), "r"(b[0]),
                          "r"(b[1]), "r"(b[2]), "r"(b[3])
                          : "memory");
           }
@@ -611,32 +648,46 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       // the tile's results: one half of the warps has dv, the other dk
       ok = ok && warp_wait(acc_full, tiles & 1u, abort_flag, p.limit);
       tc_fence_after();
-      const int row = it.tile * kBlock + r;
-      const bool live = row < it.len;
       const AttnOut& to = half == 0 ? p.dv : p.dk;
       const float by = half == 0 ? 1.f : p.scale;
       const uint32_t acc = tmem + (half == 0 ? Sh::kDv : Sh::kDk) + lanes;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + (it.begin + row) * to.row + it.kv * to.head;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + it.begin * to.row + it.kv * to.head;
 #pragma unroll
-      for (int c = 0; c < HD; c += 32) {
-        uint32_t v[32];
-        if (ok) {
-          tmem_load32(acc + c, v);
-          tmem_loaded(v);
-        }
-        if (c + 32 >= HD && ok) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(acc_free);
-        }
+      for (int c0 = 0; c0 < HD; c0 += 64) {
+        // a warp's 32 rows of 128 bytes pass through its share of the dS' buffer, whose products are complete, so that it stores whole rows
+        const uint32_t mine = ds_at + static_cast<uint32_t>(warp - 8) * 4096u;
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          uint32_t x[4];
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t v[32];
+          if (ok) {
+            tmem_load32(acc + c0 + c, v);
+            tmem_loaded(v);
+          }
+          if (c0 + c + 32 >= HD && ok) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_free);
+          }
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            x[k] = ok ? bf16_pair(__uint_as_float(v[e + 2 * k]) * by, __uint_as_float(v[e + 2 * k + 1]) * by) : 0x7fc07fc0u;
-          if (live && c + e < p.hd) *reinterpret_cast<uint4*>(out + c + e) = make_uint4(x[0], x[1], x[2], x[3]);
+          for (int e = 0; e < 32; e += 8) {
+            uint32_t x[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              x[k] = ok ? bf16_pair(__uint_as_float(v[e + 2 * k]) * by, __uint_as_float(v[e + 2 * k + 1]) * by) : 0x7fc07fc0u;
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine + lane * 128u + ((static_cast<uint32_t>((c + e) / 8) ^ (lane & 7u)) << 4)),
+                         "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
+                         : "memory");
+          }
         }
+        __syncwarp();
+        const int piece = lane & 7;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int w = 4 * q + (lane >> 3), row = it.tile * kBlock + (warp & 3) * 32 + w;
+          const uint4 x = lds128(mine + static_cast<uint32_t>(w) * 128u + (static_cast<uint32_t>(piece ^ (w & 7)) << 4));
+          if (row < it.len && c0 + 8 * piece < p.hd) *reinterpret_cast<uint4*>(out + row * to.row + c0 + 8 * piece) = x;
+        }
+        __syncwarp();
       }
     }
   }
@@ -645,6 +696,35 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   if (warp == 1) {
     tc_fence_after();
     tmem_free_all(tmem);
+  }
+  if (*abort_flag) {                          // a wait ran out: NaN for what this CTA had taken and for what nobody has
+    for (uint32_t k = 0;; ++k) {
+      __syncthreads();
+      if (threadIdx.x == 0 && k >= kItems) {
+        const unsigned i = atomicAdd(next_item, 1u);
+        BwdItem next = {};
+        if (i < static_cast<unsigned>(items)) next = bwd_item(p, static_cast<int>(i));
+        ring[0] = make_int4(next.begin, next.len, next.slot, next.tile);
+        ring[1] = make_int4(next.kv, next.blocks, next.steps, 0);
+      }
+      __syncthreads();
+      const BwdItem it = read_item(k < kItems ? k : 0);
+      if (it.steps == 0) {
+        if (k < kItems) continue;
+        break;
+      }
+      const __nv_bfloat16 nan = __ushort_as_bfloat16(0x7fc0);
+      auto fill = [&](const AttnOut& o, int head, int from, int to) {
+        for (long long e = threadIdx.x; e < static_cast<long long>(to - from) * p.hd; e += kThreadsB) {
+          const long long row = it.begin + from + e / p.hd;
+          static_cast<__nv_bfloat16*>(o.p)[row * o.row + head * o.head + e % p.hd] = nan;
+        }
+      };
+      const int first = it.tile * kBlock, end = min(it.len, first + kBlock);
+      fill(p.dk, it.kv, first, end);
+      fill(p.dv, it.kv, first, end);
+      for (int h = 0; h < p.group && it.tile == 0; ++h) fill(p.dq, it.kv * p.group + h, 0, it.len);
+    }
   }
 }
 
@@ -691,7 +771,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
     return cudaFuncGetAttributes(&fa, kern) == cudaSuccess ? fa.numRegs : 0;
   }();
   if (regs != 128) return set_error(ctx, ABS_ERR_CUDA, "the backward kernel was built with %d registers a thread, not 128", regs);
-  const long long counters = static_cast<long long>(a.hq) * l.bwd_cap;
+  const long long counters = static_cast<long long>(a.hq) * l.bwd_cap + 1;
   const int lanes = HD / 8;
   const long long threads = static_cast<long long>(a.total) * a.hq * lanes;
   ABS_CUDA_TRY(ctx, launch_dependent(attn_backward_start_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a,

@@ -310,13 +310,20 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = c + e > r ? 0xff800000u : x[e];
           }
+          uint64_t y[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) y[e] = fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 v = unpack2f(y[e]);
+            y[e] = pack2f(exp2_approx(v.x), exp2_approx(v.y));
+          }
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const float2 y = unpack2f(fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2));
-            const float u = exp2_approx(y.x), v = exp2_approx(y.y);
-            part[e & 1] = add2f(part[e & 1], pack2f(u, v));
-            w[e] = bf16_pair(u, v);
+            part[e & 1] = add2f(part[e & 1], y[e]);
+            const float2 v = unpack2f(y[e]);
+            w[e] = bf16_pair(v.x, v.y);
           }
           tmem_store16(s_at + c / 2, w);                         // over columns that have been read
         }
