@@ -37,8 +37,6 @@ namespace {
 constexpr int kThreadsB = 512;
 constexpr uint32_t kItems = 4;                // tiles of a CTA that are known ahead of time
 constexpr int kBlock = 128;                   // keys of a tile, queries of a block
-constexpr int kRegsLoad = 104, kRegsOut = 104, kRegsSoft = 152;      // of a thread; together what 128 a thread are at the launch
-static_assert(128 * (kRegsLoad + kRegsOut + 2 * kRegsSoft) == kThreadsB * 128, "");
 constexpr float kLog2eB = 1.4426950408889634f;
 
 template <int HD> struct BwdShape {
@@ -49,6 +47,9 @@ template <int HD> struct BwdShape {
   static constexpr uint32_t kStats = 2 * kBlock * 4;              // -lse and -delta of a block
   static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDss * kDs + 2 * kStats;
   static constexpr size_t kSmem = kData + 512;
+  // registers of a thread of warps 0-3, of dq's and of the softmax; together what 128 a thread are at the launch
+  static constexpr int kRegsLoad = HD == 64 ? 104 : 88, kRegsOut = HD == 64 ? 104 : 152, kRegsSoft = HD == 64 ? 152 : 136;
+  static_assert(128 * (kRegsLoad + kRegsOut + 2 * kRegsSoft) == kThreadsB * 128, "");
   // tensor memory: S' (P' over it), dP', dV, dK, dQ (128 columns a head: over dP')
   static constexpr uint32_t kS = 0, kDp = 128, kDv = 256, kDk = 256 + HD, kDq = HD == 64 ? 384 : kDp;
 };
@@ -172,7 +173,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   };
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLoad));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kRegsLoad));
     if (warp == 0) {
       // ---- loads -----------------------------------------------------------------------------------
       uint32_t lands = 0, tiles = 0, n = 0;                      // tiles and steps so far
@@ -190,39 +191,38 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       };
       // 128 rows of one head from the sequence's row `first` on; those behind the sequence, which may hold anything, become zeros
       // (all of them are operands of products that run along these rows)
-      auto copy_rows = [&](const CUtensorMap* map, uint32_t to, const BwdItem& it, int head, int first, uint32_t bar) {
-        const int in = it.len - first;
-        if (in >= kBlock) {
-          expect(bar, kRows);
-          copy(map, to, head, it.begin + first, bar);
-          return;
-        }
+      auto zero_behind = [&](const CUtensorMap* map, uint32_t to, const BwdItem& it, int head, int first) {
         expect(landed, kRows);
         copy(map, to, head, it.begin + first, landed);
         ok = warp_wait(landed, lands & 1u, abort_flag, p.limit);
         ++lands;
         for (uint32_t c = 0; c < HD / 64; ++c)
-          for (uint32_t e = static_cast<uint32_t>(in) * 128u + lane * 16u; e < kBlock * 128u; e += 512u)
+          for (uint32_t e = static_cast<uint32_t>(it.len - first) * 128u + lane * 16u; e < kBlock * 128u; e += 512u)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + c * (kBlock * 128u) + e), "r"(0u) : "memory");
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
+      };
+      auto copy_rows = [&](const CUtensorMap* map, uint32_t to, const BwdItem& it, int head, int first, uint32_t bar) {
+        if (it.len - first >= kBlock) {
+          expect(bar, kRows);
+          copy(map, to, head, it.begin + first, bar);
+        } else {
+          zero_behind(map, to, it, head, first);
+          if (lane == 0) mbar_arrive(bar);
+        }
       };
       BwdItem it;
       while (ok && take_item(tiles, it)) {
         const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         if (tiles >= Sh::kKv) ok = warp_wait(kv_free + 8u * kv, (tiles / Sh::kKv - 1) & 1u, abort_flag, p.limit);
         if (!ok) break;
-        // V is an operand along its rows only once, of products whose rows behind the sequence are masked: as it comes
+        // (two copies of a full tile arrive as one; V's zeros make dP' of rows behind the sequence zero, so that p = 0 times it is)
         if (it.len - it.tile * kBlock >= kBlock) {
           expect(kv_full + 8u * kv, 2u * kRows);
           copy(&maps.k, kvs, it.kv, it.begin + it.tile * kBlock, kv_full + 8u * kv);
           copy(&maps.v, kvs + kRows, it.kv, it.begin + it.tile * kBlock, kv_full + 8u * kv);
         } else {
-          expect(landed, kRows);
-          copy(&maps.v, kvs + kRows, it.kv, it.begin + it.tile * kBlock, landed);
-          ok = warp_wait(landed, lands & 1u, abort_flag, p.limit);
-          ++lands;
+          zero_behind(&maps.v, kvs + kRows, it, it.kv, it.tile * kBlock);
           if (ok) copy_rows(&maps.k, kvs, it, it.kv, it.tile * kBlock, kv_full + 8u * kv);
         }
         ++tiles;
@@ -474,7 +474,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       }
     }
   } else if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOut));
+    if constexpr (Sh::kRegsOut <= 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kRegsOut));
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kRegsOut));
     // ---- dq out of tensor memory and into the sums: a thread has a query's row -------
     const int sub = warp & 3, r = sub * 32 + lane;
     const uint32_t at_t = tmem + Sh::kDq + (static_cast<uint32_t>(sub * 32) << 16);
@@ -489,61 +490,57 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         const bool live = row < it.len;
         const unsigned before = static_cast<unsigned>(block - it.tile);                             // tiles whose parts are in
         float4* sums = reinterpret_cast<float4*>(p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock + 32 * sub) * HD) + lane;
+        ok = ok && warp_wait(turn_ok + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, p.limit);
         ok = ok && warp_wait(dq_full, n & 1u, abort_flag, p.limit);
         tc_fence_after();
         __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head;
+        // all of it first: at 128 columns a head the next dP' waits for the place
+        uint32_t v[HD];
+        if (ok) {
 #pragma unroll
-        for (int c0 = 0; c0 < HD; c0 += 64) {
-          uint32_t v[64];
-          if (ok) {
-            tmem_load32(at_t + c0, v);
-            tmem_load32(at_t + c0 + 32, v + 32);
-            tmem_loaded(v);
-            tmem_loaded(v + 32);
-          }
-          if (c0 + 64 >= HD && ok) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(dq_read);
-          }
-          if (c0 == 0) ok = ok && warp_wait(turn_ok + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, p.limit);
-          if (it.tile != 0) {
-            if (ok && live) {
+          for (int c = 0; c < HD; c += 32) tmem_load32(at_t + c, v + c);
 #pragma unroll
-              for (int c = 0; c < 16; ++c) {
-                float4* to = sums + static_cast<long long>(c0 / 4 + c) * rows;
-                if (before == 0)
-                  asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(v[4 * c]), "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
-                else
-                  asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(__uint_as_float(v[4 * c])),
-                               "f"(__uint_as_float(v[4 * c + 1])), "f"(__uint_as_float(v[4 * c + 2])), "f"(__uint_as_float(v[4 * c + 3]))
-                               : "memory");
-              }
+          for (int c = 0; c < HD; c += 32) tmem_loaded(v + c);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(dq_read);
+        }
+        if (it.tile != 0) {
+          if (ok && live) {
+#pragma unroll
+            for (int c = 0; c < HD / 4; ++c) {
+              float4* to = sums + static_cast<long long>(c) * rows;
+              if (before == 0)
+                asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(v[4 * c]), "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
+              else
+                asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(__uint_as_float(v[4 * c])),
+                             "f"(__uint_as_float(v[4 * c + 1])), "f"(__uint_as_float(v[4 * c + 2])), "f"(__uint_as_float(v[4 * c + 3]))
+                             : "memory");
             }
-          } else {
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < HD / 4; h += 4) {
             if (ok && live && before > 0) {
+              float4 x[4];
 #pragma unroll
-              for (int h = 0; h < 16; h += 8) {
-                float4 x[8];
+              for (int c = 0; c < 4; ++c) x[c] = __ldcg(sums + static_cast<long long>(h + c) * rows);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) x[c] = __ldcg(sums + static_cast<long long>(c0 / 4 + h + c) * rows);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                  v[4 * (h + c)] = __float_as_uint(__uint_as_float(v[4 * (h + c)]) + x[c].x);
-                  v[4 * (h + c) + 1] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 1]) + x[c].y);
-                  v[4 * (h + c) + 2] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 2]) + x[c].z);
-                  v[4 * (h + c) + 3] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 3]) + x[c].w);
-                }
+              for (int c = 0; c < 4; ++c) {
+                v[4 * (h + c)] = __float_as_uint(__uint_as_float(v[4 * (h + c)]) + x[c].x);
+                v[4 * (h + c) + 1] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 1]) + x[c].y);
+                v[4 * (h + c) + 2] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 2]) + x[c].z);
+                v[4 * (h + c) + 3] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 3]) + x[c].w);
               }
             }
+          }
 #pragma unroll
-            for (int c = 0; c < 64; c += 8) {
-              uint32_t w[4];
+          for (int c = 0; c < HD; c += 8) {
+            uint32_t w[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                w[k] = ok ? bf16_pair(__uint_as_float(v[c + 2 * k]) * p.scale, __uint_as_float(v[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
-              if (live && c0 + c < p.hd) *reinterpret_cast<uint4*>(out + c0 + c) = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            for (int k = 0; k < 4; ++k)
+              w[k] = ok ? bf16_pair(__uint_as_float(v[c + 2 * k]) * p.scale, __uint_as_float(v[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
+            if (live && c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
         __syncwarp();
@@ -551,7 +548,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoft));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kRegsSoft));
     // ---- softmax: a thread has a key's row and 64 of a block's queries ---------------------------------
     const int half = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -622,13 +619,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
             for (int k = 0; k < 2; ++k) {
               const float4 e = delta[(h + c) / 4 + k];
               const int q = (h + c) / 2 + 2 * k;
-              float2 x = unpack2f(mul2f(w[q], add2f(pack2f(__uint_as_float(d[c + 4 * k]), __uint_as_float(d[c + 4 * k + 1])), pack2f(e.x, e.y))));
-              float2 y = unpack2f(mul2f(w[q + 1], add2f(pack2f(__uint_as_float(d[c + 4 * k + 2]), __uint_as_float(d[c + 4 * k + 3])), pack2f(e.z, e.w))));
-              if (diagonal) {                                    // (zero whatever dP' is there)
-                const int from = r - 64 * half - (h + c + 4 * k);
-                x = make_float2(0 < from ? 0.f : x.x, 1 < from ? 0.f : x.y);
-                y = make_float2(2 < from ? 0.f : y.x, 3 < from ? 0.f : y.y);
-              }
+              const float2 x = unpack2f(mul2f(w[q], add2f(pack2f(__uint_as_float(d[c + 4 * k]), __uint_as_float(d[c + 4 * k + 1])), pack2f(e.x, e.y))));
+              const float2 y = unpack2f(mul2f(w[q + 1], add2f(pack2f(__uint_as_float(d[c + 4 * k + 2]), __uint_as_float(d[c + 4 * k + 3])), pack2f(e.z, e.w))));
               b[2 * k] = bf16_pair(x.x, x.y);
               b[2 * k + 1] = bf16_pair(y.x, y.y);
             }
@@ -776,9 +768,14 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   const long long threads = static_cast<long long>(a.total) * a.hq * lanes;
   ABS_CUDA_TRY(ctx, launch_dependent(attn_backward_start_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a,
                                      reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<unsigned*>(mem + s.counters), counters, lanes));
-  // heads whose sums of dq are under way at a time: 48 MB of them
+  // Key heads whose sums of dq are under way at a time: 48 MB of them, or, up to 96 MB, as many as make a tile's predecessor in the order of
+  // the sums more than a grid away in the order of the tiles, where it is done and nobody waits for it.  16 x 1024 tokens, 12 heads of 128:
+  // HEADS_FIG.
   const long long group = a.hq / a.hk, rows = a.total < (1 << kAttnGroupBits) ? a.total : 1 << kAttnGroupBits;
-  long long heads = (48ll << 20) / (rows * group * HD * 4);
+  const long long size = rows * group * HD * 4, sequences = a.n * rows / a.total > 1 ? a.n * rows / a.total : 1;
+  long long heads = (48ll << 20) / size;
+  const long long apart = (ctx->sm_count + ctx->sm_count / 4 + sequences - 1) / sequences, most_heads = (96ll << 20) / size;
+  if (heads < apart) heads = apart < most_heads ? apart : most_heads;
   heads = heads < 1 ? 1 : heads > a.hk ? a.hk : heads;
   const BwdParams p{a.dq, a.dk, a.dv, reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<float*>(mem + s.sums),
                     reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.plan + l.groups, a.total, a.hq, a.hk,
