@@ -219,7 +219,7 @@ extern "C" int abs_attention_scratch_bytes(long long total, int q_heads, int kv_
   int rc = validate_sequences(nullptr, sequences, total);
   if (rc == ABS_OK) rc = validate_heads(nullptr, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
-  *out = attn_scratch(static_cast<int>(total), q_heads, head_dim, sequences).bytes;
+  *out = attn_scratch(static_cast<int>(total), q_heads, kv_heads, head_dim, sequences).bytes;
   return ABS_OK;
 }
 
@@ -267,7 +267,7 @@ extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const a
       {"dQ", dQ, q_heads}, {"dK", dK, kv_heads}, {"dV", dV, kv_heads}};
   for (const auto& x : all)
     if ((rc = validate_tensor(ctx, x.what, x.t, total, x.heads, head_dim)) != ABS_OK) return rc;
-  const AttnScratch s = attn_scratch(static_cast<int>(total), q_heads, head_dim, sequences);
+  const AttnScratch s = attn_scratch(static_cast<int>(total), q_heads, kv_heads, head_dim, sequences);
   if (scratch == nullptr || scratch_bytes < s.bytes)
     return set_error(ctx, ABS_ERR_WORKSPACE, "scratch of %zu bytes needed, %zu given", s.bytes, scratch ? scratch_bytes : 0);
   if (reinterpret_cast<uintptr_t>(scratch) & 255u) return set_error(ctx, ABS_ERR_INVALID_ARG, "scratch must be 256-byte aligned");

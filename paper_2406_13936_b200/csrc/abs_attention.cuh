@@ -70,20 +70,36 @@ struct AttnBackward {
   size_t scratch_bytes;
 };
 
+// Into how many parts the tensor-core kernel's backward pass splits a group's query heads: a key tile and head is one CTA's work for all
+// queries of the group, and with fewer than eight tiles an SM the last ones to finish (128 keys of a long sequence, 8 query heads:
+// hundreds of blocks) are most of the time.  (A rule of sizes alone: the scratch depends on it.)
+inline int attn_parts(int total, int hq, int hk, int n) {
+  const long long tiles = (static_cast<long long>(total) / kAttnBwdRows + n) * hk;
+  const int group = hq / hk;
+  int parts = 1;
+  while (parts < group && tiles * parts < 8 * kSmCountFallback) {
+    ++parts;
+    while (group % parts != 0) ++parts;
+  }
+  return parts;
+}
 // Scratch of a backward pass: two rows of [hq][total] fp32 (delta; the tensor-core kernel: -lse log2 e and -delta), then, for the
-// tensor-core kernel, the sums of dq [hq][total][dpad] fp32 and a counter for each 128 rows of a sequence and head,
-// and one of the tiles taken.
+// tensor-core kernel, the sums of dq [hq][total][dpad] fp32, dv and dk of the parts of a group, a counter for each 128 rows of a
+// sequence and head, and one of the tiles taken.
 struct AttnScratch {
-  size_t delta, sums, counters, bytes;
+  size_t delta, sums, partial, counters, bytes;
   int dpad;
 };
-inline AttnScratch attn_scratch(int total, int hq, int hd, int n) {
+inline AttnScratch attn_scratch(int total, int hq, int hk, int hd, int n) {
   AttnScratch s;
   auto up = [](size_t v) { return (v + 255) & ~static_cast<size_t>(255); };
+  const int parts = attn_parts(total, hq, hk, n);
   s.dpad = hd <= 64 ? 64 : 128;
+  const size_t head = static_cast<size_t>(total) * s.dpad * sizeof(float);
   s.delta = 0;
   s.sums = up(static_cast<size_t>(hq) * total * 2 * sizeof(float));
-  s.counters = up(s.sums + static_cast<size_t>(total) * hq * s.dpad * sizeof(float));
+  s.partial = up(s.sums + hq * head);
+  s.counters = up(s.partial + (parts > 1 ? 2 * static_cast<size_t>(parts) * hk * head : 0));
   s.bytes = up(s.counters + (static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) + 1) * sizeof(unsigned));
   return s;
 }

@@ -48,7 +48,7 @@ template <int HD> struct BwdShape {
   static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDss * kDs + 2 * kStats;
   static constexpr size_t kSmem = kData + 512;
   // registers of a thread of warps 0-3, of dq's and of the softmax; together what 128 a thread are at the launch
-  static constexpr int kRegsLoad = HD == 64 ? 104 : 88, kRegsOut = HD == 64 ? 104 : 152, kRegsSoft = HD == 64 ? 152 : 136;
+  static constexpr int kRegsLoad = HD == 64 ? 88 : 72, kRegsOut = HD == 64 ? 120 : 168, kRegsSoft = HD == 64 ? 152 : 136;
   static_assert(128 * (kRegsLoad + kRegsOut + 2 * kRegsSoft) == kThreadsB * 128, "");
   // tensor memory: S' (P' over it), dP', dV, dK, dQ (128 columns a head: over dP')
   static constexpr uint32_t kS = 0, kDp = 128, kDv = 256, kDk = 256 + HD, kDq = HD == 64 ? 384 : kDp;
@@ -66,25 +66,27 @@ struct BwdParams {
   const int* plan;
   const int* tiles;
   const int* groups;
-  int total, hq, hk, group, hd, cap;
-  int heads_at_once;
+  int total, hq, hk, parts, hd, cap;
+  // A key head's group of query heads in `parts` of `group` heads, each a head of its own in the list of tiles, `heads` in all.
+  int heads, group, heads_at_once;
+  float* partial;                             // [parts][dv, dk][hk][total][HD], laid out as sums; NULL: parts = 1
   float by, scale;                            // scale log2 e, scale
   long long limit;
   int drop_loads;
 };
 struct BwdItem {
-  int begin, len, slot, tile, kv;
+  int begin, len, slot, tile, head;           // head: of the list of tiles
   int blocks, steps;                          // query blocks from the tile on, and of all the group's heads
 };
 __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, int i) {
   const int4* recs = reinterpret_cast<const int4*>(p.tiles);
-  const int g = __ldg(recs + i / p.hk).x >> kAttnGroupBits;
-  const int t0 = __ldg(p.groups + g), n = __ldg(p.groups + g + 1) - t0, local = i - p.hk * t0;
+  const int g = __ldg(recs + i / p.heads).x >> kAttnGroupBits;
+  const int t0 = __ldg(p.groups + g), n = __ldg(p.groups + g + 1) - t0, local = i - p.heads * t0;
   const int chunk = local / (n * p.heads_at_once), first = chunk * p.heads_at_once, rem = local - first * n;
-  const int heads = min(p.heads_at_once, p.hk - first);
+  const int heads = min(p.heads_at_once, p.heads - first);
   const int4 r = __ldg(recs + t0 + rem / heads);
   BwdItem it;
-  it.kv = first + rem % heads;
+  it.head = first + rem % heads;
   it.begin = r.x;
   it.len = r.y - r.x;
   it.tile = r.z;
@@ -96,7 +98,7 @@ __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, int i) {
 // Step t of a tile: the query head and the block.
 __device__ __forceinline__ void bwd_step(const BwdParams& p, const BwdItem& it, int t, int& head, int& block) {
   const int h = t / it.blocks;
-  head = it.kv * p.group + h;
+  head = it.head * p.group + h;
   block = it.tile + t - h * it.blocks;
 }
 
@@ -145,7 +147,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     mbar_init(dq_full, 1);
     mbar_init(dq_read, 4);
     mbar_init(acc_full, 1);
-    mbar_init(acc_free, 8);
+    mbar_init(acc_free, 4);
     mbar_init(landed, 1);
     mbar_init(done_bar, 1);
     *abort_flag = (kv_at & 1023u) ? 1u : 0u;
@@ -157,7 +159,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int items = __ldg(p.plan + kPlanBwdTiles) * p.hk;
+  const int items = __ldg(p.plan + kPlanBwdTiles) * p.heads;
   unsigned* next_item = p.counters + static_cast<long long>(p.hq) * p.cap;
   // The CTA's k-th tile; false: there is none (or a wait ran out).  last: whether this role is done with the place in the ring.
   auto read_item = [&](uint32_t k) {
@@ -216,14 +218,15 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         if (tiles >= Sh::kKv) ok = warp_wait(kv_free + 8u * kv, (tiles / Sh::kKv - 1) & 1u, abort_flag, p.limit);
         if (!ok) break;
+        const int kv_head = it.head / p.parts;
         // (two copies of a full tile arrive as one; V's zeros make dP' of rows behind the sequence zero, so that p = 0 times it is)
         if (it.len - it.tile * kBlock >= kBlock) {
           expect(kv_full + 8u * kv, 2u * kRows);
-          copy(&maps.k, kvs, it.kv, it.begin + it.tile * kBlock, kv_full + 8u * kv);
-          copy(&maps.v, kvs + kRows, it.kv, it.begin + it.tile * kBlock, kv_full + 8u * kv);
+          copy(&maps.k, kvs, kv_head, it.begin + it.tile * kBlock, kv_full + 8u * kv);
+          copy(&maps.v, kvs + kRows, kv_head, it.begin + it.tile * kBlock, kv_full + 8u * kv);
         } else {
-          zero_behind(&maps.v, kvs + kRows, it, it.kv, it.tile * kBlock);
-          if (ok) copy_rows(&maps.k, kvs, it, it.kv, it.tile * kBlock, kv_full + 8u * kv);
+          zero_behind(&maps.v, kvs + kRows, it, kv_head, it.tile * kBlock);
+          if (ok) copy_rows(&maps.k, kvs, it, kv_head, it.tile * kBlock, kv_full + 8u * kv);
         }
         ++tiles;
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
@@ -373,7 +376,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           BwdItem it = {};
           if (i < static_cast<unsigned>(items)) it = bwd_item(p, static_cast<int>(i));
           ring[2 * (told % kItems)] = make_int4(it.begin, it.len, it.slot, it.tile);
-          ring[2 * (told % kItems) + 1] = make_int4(it.kv, it.blocks, it.steps, 0);
+          ring[2 * (told % kItems) + 1] = make_int4(it.head, it.blocks, it.steps, 0);
           mbar_arrive(item_full + 8u * (told % kItems));
         }
         __syncwarp();
@@ -482,7 +485,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     uint32_t n = 0;
     bool ok = true;
     BwdItem it;
+#pragma unroll 1
     for (uint32_t k = 0; take_item(k, it); ++k) {
+#pragma unroll 1
       for (int t = 0; t < it.steps; ++t, ++n) {
         int head, block;
         bwd_step(p, it, t, head, block);
@@ -546,6 +551,46 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         __syncwarp();
         if (ok && lane == 0) mbar_arrive(added + 8u * (n & 1u));
       }
+      // the tile's dv and dk: rows of keys.  (The softmax warps are on the next tile meanwhile.)
+      ok = ok && warp_wait(acc_full, k & 1u, abort_flag, p.limit);
+      tc_fence_after();
+      const int row = it.tile * kBlock + r, rows = min(32, it.len - it.tile * kBlock - 32 * sub), kv = it.head / p.parts;
+#pragma unroll 1
+      for (int q = 0; q < 2 * (HD / 32); ++q) {                    // 32 columns of dv, then of dk
+        const bool is_dk = q >= HD / 32;
+        const int c0 = 32 * (is_dk ? q - HD / 32 : q);
+        uint32_t v[32];
+        if (ok) {
+          tmem_load32(tmem + (is_dk ? Sh::kDk : Sh::kDv) + c0 + (static_cast<uint32_t>(sub * 32) << 16), v);
+          tmem_loaded(v);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) v[c] = 0x7fc00000u;
+        }
+        if (q == 2 * (HD / 32) - 1 && ok) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_free);
+        }
+        if (row < it.len && p.parts > 1) {
+          float4* part = reinterpret_cast<float4*>(p.partial + ((static_cast<long long>((it.head - kv * p.parts) * 2 + is_dk) * p.hk + kv) * p.total +
+                                                                it.begin + it.tile * kBlock + 32 * sub) * HD) + static_cast<long long>(c0 / 4) * rows + lane;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+            part[c * rows] = make_float4(__uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]), __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
+        } else if (row < it.len) {
+          const float by = is_dk ? p.scale : 1.f;
+          const AttnOut to = is_dk ? p.dk : p.dv;
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + (it.begin + row) * to.row + kv * to.head + c0;
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = bf16_pair(__uint_as_float(v[c + 2 * e]) * by, __uint_as_float(v[c + 2 * e + 1]) * by);
+            if (c0 + c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kRegsSoft));
@@ -558,7 +603,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     uint32_t n = 0, tiles = 0;
     bool ok = true;
     BwdItem it;
+#pragma unroll 1
     for (; take_item(tiles, it); ++tiles) {
+#pragma unroll 1
       for (int t = 0; t < it.steps && ok; ++t, ++n) {
         const bool diagonal = t % it.blocks == 0;
         const uint32_t st = n & 1u;
@@ -637,50 +684,6 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           mbar_arrive(st_free + 8u * st);
         }
       }
-      // the tile's results: one half of the warps has dv, the other dk
-      ok = ok && warp_wait(acc_full, tiles & 1u, abort_flag, p.limit);
-      tc_fence_after();
-      const AttnOut& to = half == 0 ? p.dv : p.dk;
-      const float by = half == 0 ? 1.f : p.scale;
-      const uint32_t acc = tmem + (half == 0 ? Sh::kDv : Sh::kDk) + lanes;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + it.begin * to.row + it.kv * to.head;
-#pragma unroll
-      for (int c0 = 0; c0 < HD; c0 += 64) {
-        // a warp's 32 rows of 128 bytes pass through its share of the dS' buffer, whose products are complete, so that it stores whole rows
-        const uint32_t mine = ds_at + static_cast<uint32_t>(warp - 8) * 4096u;
-#pragma unroll
-        for (int c = 0; c < 64; c += 32) {
-          uint32_t v[32];
-          if (ok) {
-            tmem_load32(acc + c0 + c, v);
-            tmem_loaded(v);
-          }
-          if (c0 + c + 32 >= HD && ok) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(acc_free);
-          }
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t x[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              x[k] = ok ? bf16_pair(__uint_as_float(v[e + 2 * k]) * by, __uint_as_float(v[e + 2 * k + 1]) * by) : 0x7fc07fc0u;
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(mine + lane * 128u + ((static_cast<uint32_t>((c + e) / 8) ^ (lane & 7u)) << 4)),
-                         "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3])
-                         : "memory");
-          }
-        }
-        __syncwarp();
-        const int piece = lane & 7;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int w = 4 * q + (lane >> 3), row = it.tile * kBlock + (warp & 3) * 32 + w;
-          const uint4 x = lds128(mine + static_cast<uint32_t>(w) * 128u + (static_cast<uint32_t>(piece ^ (w & 7)) << 4));
-          if (row < it.len && c0 + 8 * piece < p.hd) *reinterpret_cast<uint4*>(out + row * to.row + c0 + 8 * piece) = x;
-        }
-        __syncwarp();
-      }
     }
   }
   tc_fence_before();
@@ -697,7 +700,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         BwdItem next = {};
         if (i < static_cast<unsigned>(items)) next = bwd_item(p, static_cast<int>(i));
         ring[0] = make_int4(next.begin, next.len, next.slot, next.tile);
-        ring[1] = make_int4(next.kv, next.blocks, next.steps, 0);
+        ring[1] = make_int4(next.head, next.blocks, next.steps, 0);
       }
       __syncthreads();
       const BwdItem it = read_item(k < kItems ? k : 0);
@@ -712,10 +715,47 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           static_cast<__nv_bfloat16*>(o.p)[row * o.row + head * o.head + e % p.hd] = nan;
         }
       };
-      const int first = it.tile * kBlock, end = min(it.len, first + kBlock);
-      fill(p.dk, it.kv, first, end);
-      fill(p.dv, it.kv, first, end);
-      for (int h = 0; h < p.group && it.tile == 0; ++h) fill(p.dq, it.kv * p.group + h, 0, it.len);
+      const int first = it.tile * kBlock, end = min(it.len, first + kBlock), kv = it.head / p.parts;
+      if (p.parts == 1) {
+        fill(p.dk, kv, first, end);
+        fill(p.dv, kv, first, end);
+      } else {
+        for (int which = 0; which < 2; ++which) {
+          float* part = p.partial + ((static_cast<long long>((it.head - kv * p.parts) * 2 + which) * p.hk + kv) * p.total + it.begin + first) * HD;
+          for (int e = threadIdx.x; e < (end - first) * HD; e += kThreadsB) part[e] = __int_as_float(0x7fc00000);
+        }
+      }
+      for (int h = 0; h < p.group && it.tile == 0; ++h) fill(p.dq, it.head * p.group + h, 0, it.len);
+    }
+  }
+}
+
+// dv and dk of a tile and key head from the parts of its group, in order: a thread a row.
+template <int HD>
+__global__ void __launch_bounds__(kBlock)
+attn_join_kernel(const BwdParams p) {
+  pdl_wait();
+  const int tile = blockIdx.x, kv = blockIdx.y, r = threadIdx.x;
+  if (tile >= __ldg(p.plan + kPlanBwdTiles)) return;
+  const int4 rec = __ldg(reinterpret_cast<const int4*>(p.tiles) + tile);
+  const int row = rec.z * kBlock + r, rows = min(32, rec.y - rec.x - rec.z * kBlock - (r & ~31));
+  if (row >= rec.y - rec.x) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const AttnOut& to = which == 0 ? p.dv : p.dk;
+    const float by = which == 0 ? 1.f : p.scale;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + (rec.x + row) * to.row + kv * to.head;
+    for (int c = 0; c < p.hd; c += 8) {
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+      for (int part = 0; part < p.parts; ++part) {
+        const float4* from = reinterpret_cast<const float4*>(p.partial + ((static_cast<long long>(part * 2 + which) * p.hk + kv) * p.total + rec.x +
+                                                                          rec.z * kBlock + (r & ~31)) * HD) + (r & 31);
+        const float4 x = __ldcs(from + static_cast<long long>(c / 4) * rows), y = __ldcs(from + static_cast<long long>(c / 4 + 1) * rows);
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+      }
+      *reinterpret_cast<uint4*>(out + c) = make_uint4(bf16_pair(a.x * by, a.y * by), bf16_pair(a.z * by, a.w * by), bf16_pair(b.x * by, b.y * by),
+                                                      bf16_pair(b.z * by, b.w * by));
     }
   }
 }
@@ -753,7 +793,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
       !encode_heads_map(a.v, a.total, a.hk, a.hd, &maps.v) || !encode_heads_map(a.dout, a.total, a.hq, a.hd, &maps.dout))
     return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (%d rows, head_dim %d) failed", a.total, a.hd);
   const AttnPlanLayout l = attn_plan_layout(a.n, a.total);
-  const AttnScratch s = attn_scratch(a.total, a.hq, a.hd, a.n);
+  const AttnScratch s = attn_scratch(a.total, a.hq, a.hk, a.hd, a.n);
   char* mem = static_cast<char*>(a.scratch);
   auto kern = attn_backward_kernel<HD>;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, Sh::kSmem));
@@ -771,18 +811,19 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   // Key heads whose sums of dq are under way at a time: 48 MB of them, or, up to 96 MB, as many as make a tile's predecessor in the order of
   // the sums more than a grid away in the order of the tiles, where it is done and nobody waits for it.  16 x 1024 tokens, 12 heads of 128:
   // HEADS_FIG.
-  const long long group = a.hq / a.hk, rows = a.total < (1 << kAttnGroupBits) ? a.total : 1 << kAttnGroupBits;
+  const int parts = attn_parts(a.total, a.hq, a.hk, a.n), group = a.hq / a.hk / parts, all = a.hk * parts;
+  const long long rows = a.total < (1 << kAttnGroupBits) ? a.total : 1 << kAttnGroupBits;
   const long long size = rows * group * HD * 4, sequences = a.n * rows / a.total > 1 ? a.n * rows / a.total : 1;
   long long heads = (48ll << 20) / size;
   const long long apart = (ctx->sm_count + ctx->sm_count / 4 + sequences - 1) / sequences, most_heads = (96ll << 20) / size;
   if (heads < apart) heads = apart < most_heads ? apart : most_heads;
-  heads = heads < 1 ? 1 : heads > a.hk ? a.hk : heads;
+  heads = heads < 1 ? 1 : heads > all ? all : heads;
   const BwdParams p{a.dq, a.dk, a.dv, reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<float*>(mem + s.sums),
                     reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.plan + l.groups, a.total, a.hq, a.hk,
-                    static_cast<int>(group), a.hd, l.bwd_cap, static_cast<int>(heads), a.scale * kLog2eB, a.scale,
+                    parts, a.hd, l.bwd_cap, all, group, static_cast<int>(heads), reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
                     ctx->tuning.stats_fault_drop_loads ? 1 : 0};
-  const long long most = static_cast<long long>(l.bwd_cap) * a.hk;
+  const long long most = static_cast<long long>(l.bwd_cap) * all;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
@@ -794,6 +835,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   ABS_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, kern, maps, p));
+  if (parts > 1) ABS_CUDA_TRY(ctx, launch_dependent(attn_join_kernel<HD>, dim3(l.bwd_cap, a.hk), dim3(kBlock), 0, st, p));
   return ABS_OK;
 }
 
