@@ -85,7 +85,7 @@ inline int attn_parts(int total, int hq, int hk, int n) {
 }
 // Scratch of a backward pass: two rows of [hq][total] fp32 (delta; the tensor-core kernel: -lse log2 e and -delta), then, for the
 // tensor-core kernel, the sums of dq [hq][total][dpad] fp32, dv and dk of the parts of a group, a counter for each 128 rows of a
-// sequence and head, and one of the tiles taken.
+// sequence, head and 64 columns, and one of the tiles taken.
 struct AttnScratch {
   size_t delta, sums, partial, counters, bytes;
   int dpad;
@@ -100,7 +100,7 @@ inline AttnScratch attn_scratch(int total, int hq, int hk, int hd, int n) {
   s.sums = up(static_cast<size_t>(hq) * total * 2 * sizeof(float));
   s.partial = up(s.sums + hq * head);
   s.counters = up(s.partial + (parts > 1 ? 2 * static_cast<size_t>(parts) * hk * head : 0));
-  s.bytes = up(s.counters + (static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) + 1) * sizeof(unsigned));
+  s.bytes = up(s.counters + (static_cast<size_t>(hq) * (static_cast<size_t>(total) / kAttnBwdRows + n) * (s.dpad / 64) + 1) * sizeof(unsigned));
   return s;
 }
 

@@ -10,7 +10,7 @@
 // memory, dK += dS' Q and dQ = dS K with dS' in shared memory once, read along its rows for the one and along its columns (MN-major)
 // for the other.
 //
-// dQ is a sum over key tiles, which different CTAs have.  They add to fp32 sums in scratch (reductions in L2), for each block of
+// dQ is a sum over key tiles, which different CTAs have.  They add to fp32 sums in scratch (bulk reductions in L2), for each block of
 // queries in a fixed order, so results repeat bit for bit: tile j of a sequence starts at query block j and goes up, so block i is
 // reached first by tile i, then by i - 1, and so on, each a step later than the one before; a counter says whose turn
 // it is, and the wait is rarely one.  The first of them stores instead of adding (nothing is cleared), and the last, tile 0, adds its own part
@@ -24,7 +24,7 @@
 // Bound by the products at 128 columns a head (five of 512 clocks per 128 x 128 scores), at 64 (five of 256) by the products and by
 // what the softmax warps issue alike.
 //
-// Roles of the 16 warps: 0 loads (TMA), 1 issues the products, 2 takes tiles and loads lse and delta, 3 looks after the turns, 4-7 take dq out of tensor memory,
+// Roles of the 16 warps: 0 takes tiles and loads (TMA), 1 issues the products, 2 and 3 look after the sums, 4-7 take results out of tensor memory,
 // 8-15 are the softmax: 64 of a block's 128 queries each half.  While they compute P' of a block, dQ and dK of the block before and
 // dP' of this one run; while they compute dS', dV and the next S'.  All waits are bounded: one that runs out raises the CTA's
 // abort flag, every role falls through, copies in flight are waited for, tensor memory is freed, and what was not finished is NaN.
@@ -42,16 +42,18 @@ constexpr float kLog2eB = 1.4426950408889634f;
 template <int HD> struct BwdShape {
   static constexpr uint32_t kRows = kBlock * HD * 2;              // 128 rows of one head, bf16
   static constexpr uint32_t kKv = HD == 64 ? 2 : 1;               // places for a tile's K and V
-  static constexpr uint32_t kQ = 2, kDo = 2;                      // places for Q and dO
-  static constexpr uint32_t kDs = kBlock * kBlock * 2, kDss = HD == 64 ? 2 : 1;     // dS' of a block, places for it
+  static constexpr uint32_t kQ = 2, kDo = HD == 64 ? 2 : 1;       // places for Q and dO
+  static constexpr uint32_t kDs = kBlock * kBlock * 2;
+  static constexpr uint32_t kHalves = HD / 64;                    // dq leaves in pieces of 64 columns
+  static constexpr uint32_t kStage = kBlock * 64 * 4, kStages = HD == 64 ? 2 : 1;      // places for these
   static constexpr uint32_t kStats = 2 * kBlock * 4;              // -lse and -delta of a block
-  static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDss * kDs + 2 * kStats;
+  static constexpr uint32_t kData = 2 * kKv * kRows + (kQ + kDo) * kRows + kDs + kStages * kStage + 2 * kStats;
   static constexpr size_t kSmem = kData + 512;
   // registers of a thread of warps 0-3, of dq's and of the softmax; together what 128 a thread are at the launch
   static constexpr int kRegsLoad = HD == 64 ? 88 : 72, kRegsOut = HD == 64 ? 120 : 168, kRegsSoft = HD == 64 ? 152 : 136;
   static_assert(128 * (kRegsLoad + kRegsOut + 2 * kRegsSoft) == kThreadsB * 128, "");
   // tensor memory: S' (P' over it), dP', dV, dK, dQ (128 columns a head: over dP')
-  static constexpr uint32_t kS = 0, kDp = 128, kDv = 256, kDk = 256 + HD, kDq = HD == 64 ? 384 : kDp;
+  static constexpr uint32_t kS = 0, kDp = 128, kDv = 256, kDk = 256 + HD, kDq = HD == 64 ? 384 : kDp, kDqs = HD == 64 ? 2 : 1;      // (two of dQ)
 };
 static_assert(BwdShape<64>::kSmem <= 232448 && BwdShape<128>::kSmem <= 232448, "");
 
@@ -61,8 +63,8 @@ struct BwdMaps {
 struct BwdParams {
   AttnOut dq, dk, dv;
   const float* stats;                         // [2][hq][total]
-  float* sums;                                // [hq][total][HD]; of 32 rows at a time: [HD / 4][rows] pieces of 16 bytes
-  unsigned* counters;                         // [hq][cap], then the next tile that nobody has
+  float* sums;                                // [hq][total][HD]; of a block: [HD / 64][16][rows] pieces of 16 bytes
+  unsigned* counters;                         // [hq][cap][HD / 64], then the next tile that nobody has
   const int* plan;
   const int* tiles;
   const int* groups;
@@ -102,6 +104,20 @@ __device__ __forceinline__ void bwd_step(const BwdParams& p, const BwdItem& it, 
   block = it.tile + t - h * it.blocks;
 }
 
+// Waits (bounded) until the counter has reached `target`.
+__device__ __forceinline__ bool wait_turn(const unsigned* c, unsigned target, volatile unsigned* abort_flag, long long limit) {
+  const long long t0 = clock64();
+  for (;;) {
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(c) : "memory");
+    if (v >= target) return true;
+    if (*abort_flag || clock64() - t0 > limit) {
+      *abort_flag = 1u;
+      return false;
+    }
+  }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(kThreadsB, 1)
 attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant__ BwdParams p) {
@@ -110,19 +126,21 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   extern __shared__ __align__(1024) unsigned char smem_dyn[];       // (there is no room to align it here; checked below)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t kv_at = smem_u32(smem_dyn), q_at = kv_at + 2u * Sh::kKv * kRows,
-                 do_at = q_at + Sh::kQ * kRows, ds_at = do_at + Sh::kDo * kRows, stats_at = ds_at + Sh::kDss * Sh::kDs;
+                 do_at = q_at + Sh::kQ * kRows, ds_at = do_at + Sh::kDo * kRows, stage_at = ds_at + Sh::kDs,
+                 stats_at = stage_at + Sh::kStages * Sh::kStage;
   float* stats = reinterpret_cast<float*>(smem_dyn + (stats_at - kv_at));
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + Sh::kData);
-  constexpr int kBars = 38;
+  constexpr int kBars = 42;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   int4* ring = reinterpret_cast<int4*>(bars + kBars + 2);          // four items of two pieces of 16 bytes
   const uint32_t b0 = smem_u32(bars);
-  // two of each of the first ones
+  // two of each of the first ones (where one is waited for by several who may be a step apart, steps alternate between the two: with a
+  // single one it could be two phases on when the slower looks, which looks like none)
   const uint32_t kv_full = b0, kv_free = b0 + 16u, q_full = b0 + 32u, q_free = b0 + 48u, do_full = b0 + 64u, do_free = b0 + 80u,
-                 st_full = b0 + 96u, st_free = b0 + 112u, s_full = b0 + 128u, p_full = b0 + 136u, dp_full = b0 + 144u, ds_full = b0 + 152u,
-                 dq_full = b0 + 160u, dq_read = b0 + 168u, acc_full = b0 + 176u, acc_free = b0 + 184u, landed = b0 + 192u, done_bar = b0 + 200u,
-                 turn_ok = b0 + 208u, added = b0 + 224u, item_full = b0 + 240u, item_free = b0 + 272u;
+                 st_full = b0 + 96u, st_free = b0 + 112u, turn_ok = b0 + 128u, staged = b0 + 144u, stage_free = b0 + 160u, dq_full = b0 + 176u,
+                 dq_read = b0 + 192u, item_full = b0 + 208u, item_free = b0 + 240u, s_full = b0 + 272u, p_full = b0 + 280u, dp_full = b0 + 288u,
+                 ds_full = b0 + 296u, acc_full = b0 + 304u, acc_free = b0 + 312u, landed = b0 + 320u, done_bar = b0 + 328u;
   if (threadIdx.x == 0) {
     for (uint32_t k = 0; k < 2; ++k) {
       mbar_init(kv_full + 8u * k, 1);
@@ -131,21 +149,22 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       mbar_init(q_free + 8u * k, 1);
       mbar_init(do_full + 8u * k, 1);
       mbar_init(do_free + 8u * k, 1);
-      mbar_init(st_full + 8u * k, 1);
+      mbar_init(st_full + 8u * k, 32);
       mbar_init(st_free + 8u * k, 8);
       mbar_init(turn_ok + 8u * k, 1);
-      mbar_init(added + 8u * k, 4);
+      mbar_init(staged + 8u * k, 4);
+      mbar_init(stage_free + 8u * k, 1);
+      mbar_init(dq_full + 8u * k, 1);
+      mbar_init(dq_read + 8u * k, 4);
     }
     for (uint32_t k = 0; k < kItems; ++k) {
       mbar_init(item_full + 8u * k, 1);
-      mbar_init(item_free + 8u * k, 15);                           // loads, products, turns, four of dq, eight of the softmax
+      mbar_init(item_free + 8u * k, 15);                           // products, two of sums, four of dq, eight of the softmax
     }
     mbar_init(s_full, 1);
     mbar_init(p_full, 8);
     mbar_init(dp_full, 1);
     mbar_init(ds_full, 8);
-    mbar_init(dq_full, 1);
-    mbar_init(dq_read, 4);
     mbar_init(acc_full, 1);
     mbar_init(acc_free, 4);
     mbar_init(landed, 1);
@@ -160,7 +179,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const int items = __ldg(p.plan + kPlanBwdTiles) * p.heads;
-  unsigned* next_item = p.counters + static_cast<long long>(p.hq) * p.cap;
+  unsigned* next_item = p.counters + static_cast<long long>(p.hq) * p.cap * Sh::kHalves;
   // The CTA's k-th tile; false: there is none (or a wait ran out).  last: whether this role is done with the place in the ring.
   auto read_item = [&](uint32_t k) {
     const int4 a = ring[2 * (k % kItems)], b = ring[2 * (k % kItems) + 1];
@@ -213,8 +232,40 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           if (lane == 0) mbar_arrive(bar);
         }
       };
-      BwdItem it;
-      while (ok && take_item(tiles, it)) {
+      // Tiles are taken in order by whoever is free, one ahead of the one whose rows are being fetched; after the last comes one without
+      // steps.
+      uint32_t told = 0;
+      auto tell = [&]() {
+        if (told >= kItems) ok = ok && warp_wait(item_free + 8u * (told % kItems), (told / kItems - 1) & 1u, abort_flag, p.limit);
+        if (ok && lane == 0) {
+          const unsigned i = atomicAdd(next_item, 1u);
+          BwdItem it = {};
+          if (i < static_cast<unsigned>(items)) it = bwd_item(p, static_cast<int>(i));
+          ring[2 * (told % kItems)] = make_int4(it.begin, it.len, it.slot, it.tile);
+          ring[2 * (told % kItems) + 1] = make_int4(it.head, it.blocks, it.steps, 0);
+          mbar_arrive(item_full + 8u * (told % kItems));
+        }
+        __syncwarp();
+        if (ok) ++told;
+      };
+      // -lse and -delta of a block's queries; zeros behind the sequence, where Q and dO are zeros and what the weights are changes nothing
+      auto copy_stats = [&](const BwdItem& it, int head, int block) {
+        const uint32_t s = n & 1u, to = stats_at + s * Sh::kStats + lane * 4u;
+        if (n >= 2) ok = warp_wait(st_free + 8u * s, (n / 2 - 1) & 1u, abort_flag, p.limit);
+        if (!ok) return;
+        const float* from = p.stats + static_cast<long long>(head) * p.total + it.begin;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int row = block * kBlock + 32 * (e & 3) + lane;
+          const float* at = from + (row < it.len ? row : 0) + (e < 4 ? 0ll : static_cast<long long>(p.hq) * p.total);
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 128u * e), "l"(at), "r"(row < it.len ? 4 : 0) : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(st_full + 8u * s) : "memory");
+      };
+      if (ok) tell();
+      while (ok) {
+        const BwdItem it = read_item(tiles);
+        if (it.steps == 0) break;
         const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         if (tiles >= Sh::kKv) ok = warp_wait(kv_free + 8u * kv, (tiles / Sh::kKv - 1) & 1u, abort_flag, p.limit);
         if (!ok) break;
@@ -236,11 +287,14 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           if (n >= Sh::kQ) ok = warp_wait(q_free + 8u * qs, (n / Sh::kQ - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           copy_rows(&maps.q, q_at + qs * kRows, it, head, block * kBlock, q_full + 8u * qs);
+          if (ok) copy_stats(it, head, block);
           if (ok && n >= Sh::kDo) ok = warp_wait(do_free + 8u * ds, (n / Sh::kDo - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           copy_rows(&maps.dout, do_at + ds * kRows, it, head, block * kBlock, do_full + 8u * ds);
+          if (ok && t == 0) tell();
         }
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.  (After an abort a place's last
       // copy may be one further on than the count says: its wait may run out for nothing, which is bounded too.)
       volatile unsigned ignore = 0u;
@@ -277,7 +331,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       // dK and dQ of step m (counted over all tiles) from its dS'
       auto key_gradient = [&](uint32_t m, bool first) {
         if (elect_lane()) {
-          const uint32_t d = desc_at(ds_at + (m % Sh::kDss) * Sh::kDs), q = desc_at(q_at + (m % Sh::kQ) * kRows);
+          const uint32_t d = desc_at(ds_at), q = desc_at(q_at + (m % Sh::kQ) * kRows);
 #pragma unroll
           for (uint32_t k = 0; k < kBlock / 16; ++k) {
             const uint32_t off = (k / 4) * (kBlock * 128u / 16u) + (k % 4) * 2u;
@@ -289,10 +343,10 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       };
       auto query_gradient = [&](uint32_t m, uint32_t kvs) {
         if (elect_lane()) {
-          const uint32_t d = desc_at(ds_at + (m % Sh::kDss) * Sh::kDs), k_ = desc_at(kvs);
+          const uint32_t d = desc_at(ds_at), k_ = desc_at(kvs), to = tmem + Sh::kDq + (m % Sh::kDqs) * 64u;
 #pragma unroll
-          for (uint32_t k = 0; k < kBlock / 16; ++k) mma_ss(tmem + Sh::kDq, mn | (d + 128u * k), mn | (k_ + 128u * k), idesc_q, k > 0);
-          mma_commit(dq_full);
+          for (uint32_t k = 0; k < kBlock / 16; ++k) mma_ss(to, mn | (d + 128u * k), mn | (k_ + 128u * k), idesc_q, k > 0);
+          mma_commit(dq_full + 8u * (m & 1u));
         }
         __syncwarp();
       };
@@ -305,27 +359,22 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         tc_fence_after();
         scores(Sh::kS, kvs, q_at + (n % Sh::kQ) * kRows, s_full);
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
-          // dK and dQ of the step before and this one's dP'.  At 128 columns dQ lies over dP': it is taken out before dP' is written, while
-          // dK runs.  At 64 it has a place of its own, which may still be read: it comes last.
+          // dQ and dK of the step before and this one's dP'.  At 128 columns dQ lies over dP' and is taken out, while dK runs, before dP' is
+          // written; at 64 it has two places of its own.
           if (t > 0) {
             ok = warp_wait(ds_full, (n - 1) & 1u, abort_flag, p.limit);
+            if (HD == 64 && n > 2) ok = ok && warp_wait(dq_read + 8u * ((n - 3) & 1u), ((n - 3) >> 1) & 1u, abort_flag, p.limit);
             if (!ok) break;
             tc_fence_after();
-            if (HD == 128) query_gradient(n - 1, kvs);
+            query_gradient(n - 1, kvs);
             key_gradient(n - 1, t == 1);
           }
           const uint32_t ds = n % Sh::kDo;
           ok = warp_wait(do_full + 8u * ds, (n / Sh::kDo) & 1u, abort_flag, p.limit);
-          if (HD == 128 && n > 0) ok = ok && warp_wait(dq_read, (n - 1) & 1u, abort_flag, p.limit);
+          if (HD == 128 && n > 0) ok = ok && warp_wait(dq_read + 8u * ((n - 1) & 1u), ((n - 1) >> 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           tc_fence_after();
           scores(Sh::kDp, kvs + kRows, do_at + ds * kRows, dp_full);
-          if (HD == 64 && t > 0) {
-            if (n > 1) ok = warp_wait(dq_read, (n - 2) & 1u, abort_flag, p.limit);
-            if (!ok) break;
-            tc_fence_after();
-            query_gradient(n - 1, kvs);
-          }
           ok = warp_wait(p_full, n & 1u, abort_flag, p.limit);
           if (ok && t == 0 && tiles > 0) ok = warp_wait(acc_free, (tiles - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
@@ -348,7 +397,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         if (!ok) break;
         ok = warp_wait(ds_full, (n - 1) & 1u, abort_flag, p.limit);
-        if (HD == 64 && n > 1) ok = ok && warp_wait(dq_read, (n - 2) & 1u, abort_flag, p.limit);
+        if (HD == 64 && n > 2) ok = ok && warp_wait(dq_read + 8u * ((n - 3) & 1u), ((n - 3) >> 1) & 1u, abort_flag, p.limit);
         if (!ok) break;
         tc_fence_after();
         query_gradient(n - 1, kvs);
@@ -364,117 +413,51 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       __syncwarp();
       volatile unsigned ignore = 0u;
       mbar_wait(done_bar, 0u, &ignore, p.limit);                 // no product in flight when tensor memory is freed
-    } else if (warp == 2) {
-      // ---- the tiles, and lse and delta of a block's queries --------------------------------------------
-      // Tiles are taken in order by whoever is free, one ahead of the one whose rows are being fetched.
-      uint32_t n = 0, told = 0;
+    } else if (lane == 0) {
+      // ---- dq's sums: two threads, every other piece of 64 columns each, so that one's way to L2 and back is hidden behind the other's ---
+      // A piece's place is filled by the dq warps (staged) and sent from here, or, for tile 0, it is their turn to read (turn_ok, then
+      // staged); either way stage_free ends the use.
+      const uint32_t h = static_cast<uint32_t>(warp) - 2u;
+      uint32_t n = 0;
       bool ok = true;
-      auto tell = [&]() {                                          // the next tile (after the last: one without steps)
-        if (told >= kItems) ok = ok && warp_wait(item_free + 8u * (told % kItems), (told / kItems - 1) & 1u, abort_flag, p.limit);
-        if (ok && lane == 0) {
-          const unsigned i = atomicAdd(next_item, 1u);
-          BwdItem it = {};
-          if (i < static_cast<unsigned>(items)) it = bwd_item(p, static_cast<int>(i));
-          ring[2 * (told % kItems)] = make_int4(it.begin, it.len, it.slot, it.tile);
-          ring[2 * (told % kItems) + 1] = make_int4(it.head, it.blocks, it.steps, 0);
-          mbar_arrive(item_full + 8u * (told % kItems));
-        }
-        __syncwarp();
-        if (ok) ++told;
-      };
-      tell();
       for (uint32_t k = 0; ok; ++k) {
+        ok = mbar_wait(item_full + 8u * (k % kItems), (k / kItems) & 1u, abort_flag, p.limit);
+        if (!ok) break;
         const BwdItem it = read_item(k);
+        mbar_arrive(item_free + 8u * (k % kItems));
         if (it.steps == 0) break;
-        tell();
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
+          if (HD == 64 && (n & 1u) != h) continue;
+          const uint32_t half = HD == 64 ? 0u : h, u = HD == 64 ? n : 2u * n + h, s = u % Sh::kStages;
           int head, block;
           bwd_step(p, it, t, head, block);
-          const float* from = p.stats + static_cast<long long>(head) * p.total + it.begin;
-          const long long other = static_cast<long long>(p.hq) * p.total;
-          float l[4], d[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = block * kBlock + 32 * e + lane;
-            const bool in = row < it.len;
-            l[e] = in ? __ldg(from + row) : -INFINITY;           // (rows behind the sequence weigh nothing)
-            d[e] = in ? __ldg(from + other + row) : 0.f;
-          }
-          const uint32_t s = n & 1u;
-          if (n >= 2) ok = warp_wait(st_free + 8u * s, (n / 2 - 1) & 1u, abort_flag, p.limit);
+          const unsigned before = static_cast<unsigned>(block - it.tile);      // tiles whose parts are in
+          unsigned* turn = p.counters + (static_cast<long long>(head) * p.cap + it.slot + block) * Sh::kHalves + half;
+          if (before > 0) ok = wait_turn(turn, before, abort_flag, p.limit);
+          if (ok && it.tile == 0) mbar_arrive(turn_ok + 8u * h);
+          ok = ok && mbar_wait(staged + 8u * h, (u >> 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
-          float* to = stats + s * 2 * kBlock;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            to[32 * e + lane] = l[e];
-            to[kBlock + 32 * e + lane] = d[e];
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(st_full + 8u * s);
-        }
-      }
-    } else if (lane == 0) {
-      // ---- turns: looks for the next step's and passes on those whose additions are done ---------------
-      // (both take their time in L2; the dq warps wait for neither)
-      struct Cursor {
-        uint32_t k, n;                                             // tiles and steps so far
-        int t;
-        bool have;
-        BwdItem it;
-      } look = {}, pass = {};
-      // (the place in the ring is given back behind the second of the two)
-      auto fetch = [&](Cursor& c) {
-        if (!c.have && mbar_test(item_full + 8u * (c.k % kItems), (c.k / kItems) & 1u)) {
-          c.it = read_item(c.k);
-          c.have = true;
-        }
-      };
-      auto step_on = [&](Cursor& c, bool second) {
-        ++c.n;
-        if (++c.t == c.it.steps) {
-          if (second) mbar_arrive(item_free + 8u * (c.k % kItems));
-          c.t = 0;
-          c.have = false;
-          ++c.k;
-        }
-      };
-      auto counter = [&](const Cursor& c, unsigned& before) {
-        int head, block;
-        bwd_step(p, c.it, c.t, head, block);
-        before = static_cast<unsigned>(block - c.it.tile);       // tiles whose parts are in
-        return p.counters + static_cast<long long>(head) * p.cap + c.it.slot + block;
-      };
-      long long since = clock64();
-      for (;;) {
-        fetch(pass);
-        if (pass.have && pass.it.steps == 0) break;
-        if (pass.have && mbar_test(added + 8u * (pass.n & 1u), (pass.n >> 1) & 1u)) {
-          if (pass.it.tile != 0) {
-            unsigned before;
-            unsigned* c = counter(pass, before);
+          if (it.tile != 0) {
+            const int rows = min(kBlock, it.len - block * kBlock);
+            float* to = p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock) * HD + half * rows * 64;
+            const uint32_t bytes = static_cast<uint32_t>(rows) * 256u, from = stage_at + s * Sh::kStage;
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+            if (before == 0)
+              asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+            else
+              asm volatile("cp.reduce.async.bulk.global.shared::cta.bulk_group.add.f32 [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            mbar_arrive(stage_free + 8u * s);
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             asm volatile("fence.acq_rel.gpu;" ::: "memory");
-            asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(c) : "memory");
+            asm volatile("red.relaxed.gpu.global.add.u32 [%0], 1;" ::"l"(turn) : "memory");
+          } else {
+            mbar_arrive(stage_free + 8u * s);
           }
-          step_on(pass, true);
-          since = clock64();
-        }
-        fetch(look);
-        if (look.have && look.it.steps > 0 && look.n < pass.n + 2) {
-          unsigned before, v;
-          const unsigned* c = counter(look, before);
-          v = before;
-          if (before > 0) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(c) : "memory");
-          if (v >= before) {
-            mbar_arrive(turn_ok + 8u * (look.n & 1u));
-            step_on(look, false);
-            since = clock64();
-          }
-        }
-        if (*abort_flag || clock64() - since > p.limit) {
-          *abort_flag = 1u;
-          break;
         }
       }
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
   } else if (warp < 8) {
     if constexpr (Sh::kRegsOut <= 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kRegsOut));
@@ -482,7 +465,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     // ---- dq out of tensor memory and into the sums: a thread has a query's row -------
     const int sub = warp & 3, r = sub * 32 + lane;
     const uint32_t at_t = tmem + Sh::kDq + (static_cast<uint32_t>(sub * 32) << 16);
-    uint32_t n = 0;
+    uint32_t n = 0, reads = 0;                                   // bit h: parity of what helper h let this warp read
     bool ok = true;
     BwdItem it;
 #pragma unroll 1
@@ -491,65 +474,69 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       for (int t = 0; t < it.steps; ++t, ++n) {
         int head, block;
         bwd_step(p, it, t, head, block);
-        const int row = block * kBlock + r, rows = min(32, it.len - block * kBlock - 32 * sub);      // of the warp's in the sequence
+        const int row = block * kBlock + r, rows = min(kBlock, it.len - block * kBlock);
         const bool live = row < it.len;
-        const unsigned before = static_cast<unsigned>(block - it.tile);                             // tiles whose parts are in
-        float4* sums = reinterpret_cast<float4*>(p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock + 32 * sub) * HD) + lane;
-        ok = ok && warp_wait(turn_ok + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, p.limit);
-        ok = ok && warp_wait(dq_full, n & 1u, abort_flag, p.limit);
+        ok = ok && warp_wait(dq_full + 8u * (n & 1u), (n >> 1) & 1u, abort_flag, p.limit);
         tc_fence_after();
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head;
         // all of it first: at 128 columns a head the next dP' waits for the place
         uint32_t v[HD];
         if (ok) {
 #pragma unroll
-          for (int c = 0; c < HD; c += 32) tmem_load32(at_t + c, v + c);
+          for (int c = 0; c < HD; c += 32) tmem_load32(at_t + (n % Sh::kDqs) * 64u + c, v + c);
 #pragma unroll
           for (int c = 0; c < HD; c += 32) tmem_loaded(v + c);
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(dq_read);
+          if (lane == 0) mbar_arrive(dq_read + 8u * (n & 1u));
         }
-        if (it.tile != 0) {
-          if (ok && live) {
 #pragma unroll
-            for (int c = 0; c < HD / 4; ++c) {
-              float4* to = sums + static_cast<long long>(c) * rows;
-              if (before == 0)
-                asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(to), "r"(v[4 * c]), "r"(v[4 * c + 1]), "r"(v[4 * c + 2]), "r"(v[4 * c + 3]) : "memory");
-              else
-                asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(__uint_as_float(v[4 * c])),
-                             "f"(__uint_as_float(v[4 * c + 1])), "f"(__uint_as_float(v[4 * c + 2])), "f"(__uint_as_float(v[4 * c + 3]))
+        for (uint32_t half = 0; half < Sh::kHalves; ++half) {
+          const uint32_t u = Sh::kHalves * n + half, s = u % Sh::kStages;
+          uint32_t* x = v + 64 * half;
+          if (u >= Sh::kStages) ok = ok && warp_wait(stage_free + 8u * s, (u / Sh::kStages - 1) & 1u, abort_flag, p.limit);
+          if (it.tile != 0) {
+            if (ok && live) {
+#pragma unroll
+              for (int c = 0; c < 16; ++c)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage_at + s * Sh::kStage + static_cast<uint32_t>(c * rows + r) * 16u), "r"(x[4 * c]),
+                             "r"(x[4 * c + 1]), "r"(x[4 * c + 2]), "r"(x[4 * c + 3])
                              : "memory");
             }
-          }
-        } else {
+            fence_async_smem();
+          } else {
+            const uint32_t who = u & 1u;                           // of the two threads that look after the sums
+            ok = ok && warp_wait(turn_ok + 8u * who, (reads >> who) & 1u, abort_flag, p.limit);
+            reads ^= 1u << who;
+            if (ok && live && block > 0) {
+              const float4* sums = reinterpret_cast<const float4*>(p.sums + (static_cast<long long>(head) * p.total + it.begin + block * kBlock) * HD +
+                                                                   half * rows * 64) + r;
 #pragma unroll
-          for (int h = 0; h < HD / 4; h += 4) {
-            if (ok && live && before > 0) {
-              float4 x[4];
+              for (int h = 0; h < 16; h += 4) {
+                float4 y[4];
 #pragma unroll
-              for (int c = 0; c < 4; ++c) x[c] = __ldcg(sums + static_cast<long long>(h + c) * rows);
+                for (int c = 0; c < 4; ++c) y[c] = __ldcg(sums + (h + c) * rows);
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                v[4 * (h + c)] = __float_as_uint(__uint_as_float(v[4 * (h + c)]) + x[c].x);
-                v[4 * (h + c) + 1] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 1]) + x[c].y);
-                v[4 * (h + c) + 2] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 2]) + x[c].z);
-                v[4 * (h + c) + 3] = __float_as_uint(__uint_as_float(v[4 * (h + c) + 3]) + x[c].w);
+                for (int c = 0; c < 4; ++c) {
+                  x[4 * (h + c)] = __float_as_uint(__uint_as_float(x[4 * (h + c)]) + y[c].x);
+                  x[4 * (h + c) + 1] = __float_as_uint(__uint_as_float(x[4 * (h + c) + 1]) + y[c].y);
+                  x[4 * (h + c) + 2] = __float_as_uint(__uint_as_float(x[4 * (h + c) + 2]) + y[c].z);
+                  x[4 * (h + c) + 3] = __float_as_uint(__uint_as_float(x[4 * (h + c) + 3]) + y[c].w);
+                }
               }
             }
-          }
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head + 64 * half;
 #pragma unroll
-          for (int c = 0; c < HD; c += 8) {
-            uint32_t w[4];
+            for (int c = 0; c < 64; c += 8) {
+              uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = ok ? bf16_pair(__uint_as_float(v[c + 2 * k]) * p.scale, __uint_as_float(v[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
-            if (live && c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int k = 0; k < 4; ++k)
+                w[k] = ok ? bf16_pair(__uint_as_float(x[c + 2 * k]) * p.scale, __uint_as_float(x[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
+              if (live && 64 * static_cast<int>(half) + c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
           }
+          __syncwarp();
+          if (ok && lane == 0) mbar_arrive(staged + 8u * (u & 1u));
         }
-        __syncwarp();
-        if (ok && lane == 0) mbar_arrive(added + 8u * (n & 1u));
       }
       // the tile's dv and dk: rows of keys.  (The softmax warps are on the next tile meanwhile.)
       ok = ok && warp_wait(acc_full, k & 1u, abort_flag, p.limit);
@@ -671,7 +658,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
               b[2 * k] = bf16_pair(x.x, x.y);
               b[2 * k + 1] = bf16_pair(y.x, y.y);
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ds_row + (n % Sh::kDss) * Sh::kDs + ((static_cast<uint32_t>((h + c) / 8) ^ sw) << 4)), "r"(b[0]),
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ds_row + ((static_cast<uint32_t>((h + c) / 8) ^ sw) << 4)), "r"(b[0]),
                          "r"(b[1]), "r"(b[2]), "r"(b[3])
                          : "memory");
           }
@@ -803,7 +790,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
     return cudaFuncGetAttributes(&fa, kern) == cudaSuccess ? fa.numRegs : 0;
   }();
   if (regs != 128) return set_error(ctx, ABS_ERR_CUDA, "the backward kernel was built with %d registers a thread, not 128", regs);
-  const long long counters = static_cast<long long>(a.hq) * l.bwd_cap + 1;
+  const long long counters = static_cast<long long>(a.hq) * l.bwd_cap * Sh::kHalves + 1;
   const int lanes = HD / 8;
   const long long threads = static_cast<long long>(a.total) * a.hq * lanes;
   ABS_CUDA_TRY(ctx, launch_dependent(attn_backward_start_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a,
