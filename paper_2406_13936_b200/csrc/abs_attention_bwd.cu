@@ -68,7 +68,7 @@ struct BwdParams {
   const int* plan;
   const int* tiles;
   const int* groups;
-  int total, hq, hk, parts, hd, cap;
+  int total, hq, hk, parts, hd, cap, n_groups;
   // A key head's group of query heads in `parts` of `group` heads, each a head of its own in the list of tiles, `heads` in all.
   int heads, group, heads_at_once;
   float* partial;                             // [parts][dv, dk][hk][total][HD], laid out as sums; NULL: parts = 1
@@ -80,13 +80,20 @@ struct BwdItem {
   int begin, len, slot, tile, head;           // head: of the list of tiles
   int blocks, steps;                          // query blocks from the tile on, and of all the group's heads
 };
+// Tile i of the list, for a whole warp (the same i in all lanes).
 __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, int i) {
-  const int4* recs = reinterpret_cast<const int4*>(p.tiles);
-  const int g = __ldg(recs + i / p.heads).x >> kAttnGroupBits;
+  const int lane = threadIdx.x & 31;
+  int g = 0;                                  // the group: those whose tiles end at or before i
+  for (int at = 0; at < p.n_groups; at += 32) {
+    const bool behind = at + lane < p.n_groups && __ldg(p.groups + at + lane + 1) * p.heads <= i;
+    const int n = __popc(__ballot_sync(0xffffffffu, behind));
+    g += n;
+    if (n < 32) break;
+  }
   const int t0 = __ldg(p.groups + g), n = __ldg(p.groups + g + 1) - t0, local = i - p.heads * t0;
   const int chunk = local / (n * p.heads_at_once), first = chunk * p.heads_at_once, rem = local - first * n;
   const int heads = min(p.heads_at_once, p.heads - first);
-  const int4 r = __ldg(recs + t0 + rem / heads);
+  const int4 r = __ldg(reinterpret_cast<const int4*>(p.tiles) + t0 + rem / heads);
   BwdItem it;
   it.head = first + rem % heads;
   it.begin = r.x;
@@ -130,7 +137,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
                  stats_at = stage_at + Sh::kStages * Sh::kStage;
   float* stats = reinterpret_cast<float*>(smem_dyn + (stats_at - kv_at));
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + Sh::kData);
-  constexpr int kBars = 42;
+  constexpr int kBars = 44;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   int4* ring = reinterpret_cast<int4*>(bars + kBars + 2);          // four items of two pieces of 16 bytes
@@ -140,7 +147,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   const uint32_t kv_full = b0, kv_free = b0 + 16u, q_full = b0 + 32u, q_free = b0 + 48u, do_full = b0 + 64u, do_free = b0 + 80u,
                  st_full = b0 + 96u, st_free = b0 + 112u, turn_ok = b0 + 128u, staged = b0 + 144u, stage_free = b0 + 160u, dq_full = b0 + 176u,
                  dq_read = b0 + 192u, item_full = b0 + 208u, item_free = b0 + 240u, s_full = b0 + 272u, p_full = b0 + 280u, dp_full = b0 + 288u,
-                 ds_full = b0 + 296u, acc_full = b0 + 304u, acc_free = b0 + 312u, landed = b0 + 320u, done_bar = b0 + 328u;
+                 ds_full = b0 + 296u, acc_full = b0 + 304u, dv_free = b0 + 312u, dk_free = b0 + 320u, landed = b0 + 328u,
+                 done_bar = b0 + 336u;
   if (threadIdx.x == 0) {
     for (uint32_t k = 0; k < 2; ++k) {
       mbar_init(kv_full + 8u * k, 1);
@@ -166,7 +174,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     mbar_init(dp_full, 1);
     mbar_init(ds_full, 8);
     mbar_init(acc_full, 1);
-    mbar_init(acc_free, 4);
+    mbar_init(dv_free, 4);
+    mbar_init(dk_free, 4);
     mbar_init(landed, 1);
     mbar_init(done_bar, 1);
     *abort_flag = (kv_at & 1023u) ? 1u : 0u;
@@ -234,19 +243,25 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       };
       // Tiles are taken in order by whoever is free, one ahead of the one whose rows are being fetched; after the last comes one without
       // steps.
+      // (taking one is a way to L2 and back, which is under way while the next copies are issued)
       uint32_t told = 0;
+      unsigned taken = 0;
+      auto take = [&]() {
+        if (lane == 0) taken = atomicAdd(next_item, 1u);
+      };
       auto tell = [&]() {
         if (told >= kItems) ok = ok && warp_wait(item_free + 8u * (told % kItems), (told / kItems - 1) & 1u, abort_flag, p.limit);
-        if (ok && lane == 0) {
-          const unsigned i = atomicAdd(next_item, 1u);
-          BwdItem it = {};
-          if (i < static_cast<unsigned>(items)) it = bwd_item(p, static_cast<int>(i));
-          ring[2 * (told % kItems)] = make_int4(it.begin, it.len, it.slot, it.tile);
-          ring[2 * (told % kItems) + 1] = make_int4(it.head, it.blocks, it.steps, 0);
+        if (!ok) return;
+        const unsigned i = __shfl_sync(0xffffffffu, taken, 0);
+        BwdItem next = {};
+        if (i < static_cast<unsigned>(items)) next = bwd_item(p, static_cast<int>(i));
+        if (lane == 0) {
+          ring[2 * (told % kItems)] = make_int4(next.begin, next.len, next.slot, next.tile);
+          ring[2 * (told % kItems) + 1] = make_int4(next.head, next.blocks, next.steps, 0);
           mbar_arrive(item_full + 8u * (told % kItems));
         }
         __syncwarp();
-        if (ok) ++told;
+        ++told;
       };
       // -lse and -delta of a block's queries; zeros behind the sequence, where Q and dO are zeros and what the weights are changes nothing
       auto copy_stats = [&](const BwdItem& it, int head, int block) {
@@ -262,6 +277,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(st_full + 8u * s) : "memory");
       };
+      take();
       if (ok) tell();
       while (ok) {
         const BwdItem it = read_item(tiles);
@@ -291,7 +307,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           if (ok && n >= Sh::kDo) ok = warp_wait(do_free + 8u * ds, (n / Sh::kDo - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           copy_rows(&maps.dout, do_at + ds * kRows, it, head, block * kBlock, do_full + 8u * ds);
-          if (ok && t == 0) tell();
+          if (t == 0) take();
+          if (ok && (t == 1 || it.steps == 1)) tell();
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
@@ -350,14 +367,20 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         __syncwarp();
       };
-      BwdItem it;
-      while (ok && take_item(tiles, it)) {
-        const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
-        ok = warp_wait(kv_full + 8u * kv, (tiles / Sh::kKv) & 1u, abort_flag, p.limit);
-        ok = ok && warp_wait(q_full + 8u * (n % Sh::kQ), (n / Sh::kQ) & 1u, abort_flag, p.limit);
-        if (!ok) break;
+      // the first S' of the CTA's k-th tile, whose first step is the m-th
+      auto first_scores = [&](uint32_t k, uint32_t m) {
+        const uint32_t kv = k % Sh::kKv;
+        ok = warp_wait(kv_full + 8u * kv, (k / Sh::kKv) & 1u, abort_flag, p.limit);
+        ok = ok && warp_wait(q_full + 8u * (m % Sh::kQ), (m / Sh::kQ) & 1u, abort_flag, p.limit);
+        if (!ok) return;
         tc_fence_after();
-        scores(Sh::kS, kvs, q_at + (n % Sh::kQ) * kRows, s_full);
+        scores(Sh::kS, kv_at + kv * 2u * kRows, q_at + (m % Sh::kQ) * kRows, s_full);
+      };
+      BwdItem it, following;
+      bool more = take_item(0, it);
+      if (more) first_scores(0, 0);
+      while (ok && more) {
+        const uint32_t kv = tiles % Sh::kKv, kvs = kv_at + kv * 2u * kRows;
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
           // dQ and dK of the step before and this one's dP'.  At 128 columns dQ lies over dP' and is taken out, while dK runs, before dP' is
           // written; at 64 it has two places of its own.
@@ -367,6 +390,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
             if (!ok) break;
             tc_fence_after();
             query_gradient(n - 1, kvs);
+            if (t == 1 && tiles > 0) ok = warp_wait(dk_free, (tiles - 1) & 1u, abort_flag, p.limit);
+            if (!ok) break;
+            tc_fence_after();
             key_gradient(n - 1, t == 1);
           }
           const uint32_t ds = n % Sh::kDo;
@@ -376,7 +402,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           tc_fence_after();
           scores(Sh::kDp, kvs + kRows, do_at + ds * kRows, dp_full);
           ok = warp_wait(p_full, n & 1u, abort_flag, p.limit);
-          if (ok && t == 0 && tiles > 0) ok = warp_wait(acc_free, (tiles - 1) & 1u, abort_flag, p.limit);
+          if (ok && t == 0 && tiles > 0) ok = warp_wait(dv_free, (tiles - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           tc_fence_after();
           if (elect_lane()) {
@@ -393,6 +419,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
             if (!ok) break;
             tc_fence_after();
             scores(Sh::kS, kvs, q_at + (next % Sh::kQ) * kRows, s_full);
+          } else {                                               // (with places for two tiles' K and V the next tile's S' comes before this one's last dQ and dK)
+            more = take_item(tiles + 1, following);
+            if (Sh::kKv == 2 && more) first_scores(tiles + 1, n + 1);
           }
         }
         if (!ok) break;
@@ -401,6 +430,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         if (!ok) break;
         tc_fence_after();
         query_gradient(n - 1, kvs);
+        if (it.steps == 1 && tiles > 0) ok = warp_wait(dk_free, (tiles - 1) & 1u, abort_flag, p.limit);
+        if (!ok) break;
+        tc_fence_after();
         key_gradient(n - 1, it.steps == 1);
         if (elect_lane()) {
           mma_commit(acc_full);
@@ -408,6 +440,8 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         __syncwarp();
         ++tiles;
+        if (Sh::kKv == 1 && more) first_scores(tiles, n);
+        it = following;
       }
       if (elect_lane()) mma_commit(done_bar);
       __syncwarp();
@@ -554,10 +588,10 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
 #pragma unroll
           for (int c = 0; c < 32; ++c) v[c] = 0x7fc00000u;
         }
-        if (q == 2 * (HD / 32) - 1 && ok) {
+        if ((q + 1) % (HD / 32) == 0 && ok) {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(acc_free);
+          if (lane == 0) mbar_arrive(is_dk ? dk_free : dv_free);
         }
         if (row < it.len && p.parts > 1) {
           float4* part = reinterpret_cast<float4*>(p.partial + ((static_cast<long long>((it.head - kv * p.parts) * 2 + is_dk) * p.hk + kv) * p.total +
@@ -682,12 +716,16 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   if (*abort_flag) {                          // a wait ran out: NaN for what this CTA had taken and for what nobody has
     for (uint32_t k = 0;; ++k) {
       __syncthreads();
-      if (threadIdx.x == 0 && k >= kItems) {
-        const unsigned i = atomicAdd(next_item, 1u);
+      if (warp == 0 && k >= kItems) {
+        unsigned i = 0;
+        if (lane == 0) i = atomicAdd(next_item, 1u);
+        i = __shfl_sync(0xffffffffu, i, 0);
         BwdItem next = {};
         if (i < static_cast<unsigned>(items)) next = bwd_item(p, static_cast<int>(i));
-        ring[0] = make_int4(next.begin, next.len, next.slot, next.tile);
-        ring[1] = make_int4(next.head, next.blocks, next.steps, 0);
+        if (lane == 0) {
+          ring[0] = make_int4(next.begin, next.len, next.slot, next.tile);
+          ring[1] = make_int4(next.head, next.blocks, next.steps, 0);
+        }
       }
       __syncthreads();
       const BwdItem it = read_item(k < kItems ? k : 0);
@@ -795,7 +833,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   const long long threads = static_cast<long long>(a.total) * a.hq * lanes;
   ABS_CUDA_TRY(ctx, launch_dependent(attn_backward_start_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a,
                                      reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<unsigned*>(mem + s.counters), counters, lanes));
-  // Key heads whose sums of dq are under way at a time: 48 MB of them, or, up to 96 MB, as many as make a tile's predecessor in the order of
+  // Heads whose sums of dq are under way at a time: 48 MB of them, or, up to 96 MB, as many as make a tile's predecessor in the order of
   // the sums more than a grid away in the order of the tiles, where it is done and nobody waits for it.  16 x 1024 tokens, 12 heads of 128:
   // HEADS_FIG.
   const int parts = attn_parts(a.total, a.hq, a.hk, a.n), group = a.hq / a.hk / parts, all = a.hk * parts;
@@ -807,7 +845,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   heads = heads < 1 ? 1 : heads > all ? all : heads;
   const BwdParams p{a.dq, a.dk, a.dv, reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<float*>(mem + s.sums),
                     reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.plan + l.groups, a.total, a.hq, a.hk,
-                    parts, a.hd, l.bwd_cap, all, group, static_cast<int>(heads), reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
+                    parts, a.hd, l.bwd_cap, l.n_groups, all, group, static_cast<int>(heads), reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
                     ctx->tuning.stats_fault_drop_loads ? 1 : 0};
   const long long most = static_cast<long long>(l.bwd_cap) * all;
