@@ -34,6 +34,8 @@ constexpr float kLn2F = 0.6931471805599453f, kLog2eF = 1.4426950408889634f;
 template <int HD> struct FwdShape {
   static constexpr uint32_t kRowsBytes = kHalf * HD * 2;          // 128 rows of one head
   static constexpr int kPlaces = HD == 64 ? 8 : 5;
+  // tensor memory: S of the halves, O of the halves from 256 on; P over S, or beside it where there is room
+  static __device__ __forceinline__ uint32_t p_at(uint32_t t) { return HD == 64 ? 384u + 64u * t : 128u * t; }
   static constexpr size_t kSmem = (2 + kPlaces) * static_cast<size_t>(kRowsBytes) + 1024 + 512;
 };
 
@@ -76,10 +78,10 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_u32(smem_dyn), q_at = (raw + 1023u) & ~1023u, ring = q_at + 2u * kRows;
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + (q_at - raw) + (2 + kPlaces) * kRows);
-  volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + 14 + 2 * kPlaces);
+  volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + 18 + 2 * kPlaces);
   unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
   const uint32_t q_full = smem_u32(bars), q_free = q_full + 16u, s_full = q_free + 16u, p_full = s_full + 16u, o_full = p_full + 16u,
-                 o_free = o_full + 16u, landed = o_free + 16u, done_bar = landed + 8u, full = done_bar + 8u, freed = full + 8u * kPlaces;
+                 o_free = o_full + 16u, s_read = o_free + 16u, pv_done = s_read + 16u, landed = pv_done + 16u, done_bar = landed + 8u, full = done_bar + 8u, freed = full + 8u * kPlaces;
   if (threadIdx.x == 0) {
     for (uint32_t t = 0; t < 2; ++t) {
       mbar_init(q_full + 8u * t, 1);
@@ -88,6 +90,8 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
       mbar_init(p_full + 8u * t, 4);
       mbar_init(o_full + 8u * t, 1);
       mbar_init(o_free + 8u * t, 4);
+      mbar_init(s_read + 8u * t, 4);
+      mbar_init(pv_done + 8u * t, 1);
     }
     mbar_init(landed, 1);
     mbar_init(done_bar, 1);
@@ -200,6 +204,19 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
           const uint32_t v = n + 2 * j + 1, k = v + 1;           // places of this step's V and the next one's K
           ok = warp_wait(full + 8u * (v % kPlaces), (v / kPlaces) & 1u, abort_flag, p.limit);
           const uint32_t b = desc_at(ring + (v % kPlaces) * kRows);
+          // P beside S: the next S as soon as this one has been read, while its exponentials are still being taken
+#pragma unroll
+          for (uint32_t t = 0; t < 2; ++t) {
+            const int last = t == 0 ? it.n0 : it.n1;
+            if (HD != 64 || j + 1 >= last || !ok) continue;
+            ok = warp_wait(full + 8u * (k % kPlaces), (k / kPlaces) & 1u, abort_flag, p.limit);
+            ok = ok && warp_wait(s_read + 8u * t, done[t] & 1u, abort_flag, p.limit);
+            if (!ok) continue;
+            tc_fence_after();
+            scores(t, k % kPlaces);
+            if (j + 2 == last && elect_lane()) mma_commit(q_free + 8u * t);
+            __syncwarp();
+          }
 #pragma unroll
           for (uint32_t t = 0; t < 2; ++t) {
             const int last = t == 0 ? it.n0 : it.n1;
@@ -212,11 +229,12 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
             if (elect_lane()) {
 #pragma unroll
               for (uint32_t kk = 0; kk < kHalf / 16; ++kk)
-                mma_ts(tmem + 256u + t * HD, tmem + t * kHalf + 8u * kk, desc_v | (b + 128u * kk), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+                mma_ts(tmem + 256u + t * HD, tmem + FwdShape<HD>::p_at(t) + 8u * kk, desc_v | (b + 128u * kk), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+              if (HD == 64) mma_commit(pv_done + 8u * t);
               if (j == last - 1) mma_commit(o_full + 8u * t);
             }
             __syncwarp();
-            if (j + 1 < last) {
+            if (HD == 128 && j + 1 < last) {
               ok = warp_wait(full + 8u * (k % kPlaces), (k / kPlaces) & 1u, abort_flag, p.limit);
               tc_fence_after();
               scores(t, k % kPlaces);
@@ -245,7 +263,8 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
     const uint32_t t = static_cast<uint32_t>(warp - 4) >> 2;
     const int r = (warp & 3) * 32 + lane;                        // row of the half
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_at = tmem + t * kHalf + lanes, o_at = tmem + 256u + t * HD + lanes;
+    const uint32_t s_at = tmem + t * kHalf + lanes, o_at = tmem + 256u + t * HD + lanes,
+                   p_at = tmem + FwdShape<HD>::p_at(t) + lanes;
     const uint64_t by2 = pack2f(p.by, p.by);
     uint32_t steps_done = 0, uses = 0;
     bool ok = true;
@@ -253,40 +272,50 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
       const FwdItem it = item_of(p, i);
       const int steps = t == 0 ? it.n0 : it.n1;
       if (steps == 0) continue;
+      const int row = it.row + static_cast<int>(t) * kHalf + r;
+      const bool live = row < it.len;
       float m = -INFINITY;                                       // the reference
       float sum = 0.f;
       for (int j = 0; j < steps && ok; ++j, ++steps_done) {
         ok = warp_wait(s_full + 8u * t, steps_done & 1u, abort_flag, p.limit);
         if (!ok) break;
         tc_fence_after();
-        // S is read twice, 32 columns at a time and the next ones under way, instead of being held: 128 more registers a thread spill
+        // S is read twice, 32 columns at a time and the next ones under way, instead of being held: 128 more registers a thread spill.
+        // Loops of two pieces, not unrolled further: a warp that runs through long straight code waits for its instructions.
         const bool diagonal = j == steps - 1;
         uint32_t s[2][32];
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         tmem_load32(s_at, s[0]);
+#pragma unroll 1
+        for (int c = 0; c < kHalf; c += 64) {
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-          uint32_t* x = s[(c / 32) & 1];
-          tmem_loaded(x);
-          tmem_load32(s_at + ((c + 32) & (kHalf - 1)), s[(c / 32 + 1) & 1]);       // (after the last: the first again)
-          if (diagonal) {
+          for (int q = 0; q < 2; ++q) {
+            uint32_t* x = s[q];
+            tmem_loaded(x);
+            tmem_load32(s_at + ((c + 32 * q + 32) & (kHalf - 1)), s[q ^ 1]);       // (after the last: the first again)
+            if (diagonal) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (c + e <= r) top[e & 3] = fmaxf(top[e & 3], __uint_as_float(x[e]));
-          } else {
+              for (int e = 0; e < 32; ++e) x[e] = e > r - c - 32 * q ? 0xff800000u : x[e];
+            }
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) top[k] = fmaxf(fmaxf(top[k], __uint_as_float(x[e + k])), __uint_as_float(x[e + k + 4]));
+              for (int k = 0; k < 4; ++k) top[k] = max3f(top[k], __uint_as_float(x[e + k]), __uint_as_float(x[e + k + 4]));
           }
         }
-        const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.by;
-        if (__any_sync(0xffffffffu, most > m + kRaise)) {
-          const float next = fmaxf(m, most);
-          const float less = m == -INFINITY ? 0.f : exp2_approx(m - next);       // (nothing has been added yet)
+        const float most = max3f(max3f(top[0], top[1], top[2]), top[3], top[3]) * p.by;
+        // the products of the step before, which read P and add to O (with P over S they came before this S)
+        if (HD == 64 && steps_done > 0) ok = warp_wait(pv_done + 8u * t, (steps_done - 1) & 1u, abort_flag, p.limit);
+        if (!ok) break;
+        tc_fence_after();
+        // (rows behind the sequence, which may hold anything, have no say, and a row's reference depends on that row alone)
+        const bool raise = live && most > m + kRaise;
+        if (__any_sync(0xffffffffu, raise)) {
+          const float next = raise ? most : m;
+          const float less = m == next ? 1.f : m == -INFINITY ? 0.f : exp2_approx(m - next);       // (0: nothing has been added yet)
           m = next;
           sum *= less;
-          if (j > 0) {                                           // the products up to here are complete: S of this step came after them
+          if (j > 0) {
 #pragma unroll
             for (int c = 0; c < HD; c += 32) {
               uint32_t o[32];
@@ -301,31 +330,33 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         const float ref = m == -INFINITY ? 0.f : -m;
         const uint64_t ref2 = pack2f(ref, ref);
         uint64_t part[2] = {pack2f(0.f, 0.f), pack2f(0.f, 0.f)};
+#pragma unroll 1
+        for (int c = 0; c < kHalf; c += 64) {
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-          uint32_t* x = s[(c / 32) & 1];
-          tmem_loaded(x);
-          if (c + 32 < kHalf) tmem_load32(s_at + c + 32, s[(c / 32 + 1) & 1]);
-          if (diagonal) {
+          for (int q = 0; q < 2; ++q) {
+            uint32_t* x = s[q];
+            tmem_loaded(x);
+            if (c + 32 * q + 32 < kHalf) {
+              tmem_load32(s_at + c + 32 * q + 32, s[q ^ 1]);
+            } else if (HD == 64) {                                 // the last of S has been read
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(s_read + 8u * t);
+            }
+            if (diagonal) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = c + e > r ? 0xff800000u : x[e];
+              for (int e = 0; e < 32; ++e) x[e] = e > r - c - 32 * q ? 0xff800000u : x[e];
+            }
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float2 y = unpack2f(fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2));
+              const float u = exp2_approx(y.x), v = exp2_approx(y.y);
+              part[e & 1] = add2f(part[e & 1], pack2f(u, v));
+              w[e] = bf16_pair(u, v);
+            }
+            tmem_store16(p_at + (c + 32 * q) / 2, w);              // (over S: columns that have been read)
           }
-          uint64_t y[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) y[e] = fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float2 v = unpack2f(y[e]);
-            y[e] = pack2f(exp2_approx(v.x), exp2_approx(v.y));
-          }
-          uint32_t w[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            part[e & 1] = add2f(part[e & 1], y[e]);
-            const float2 v = unpack2f(y[e]);
-            w[e] = bf16_pair(v.x, v.y);
-          }
-          tmem_store16(s_at + c / 2, w);                         // over columns that have been read
         }
         const float2 all = unpack2f(add2f(part[0], part[1]));
         sum += all.x + all.y;
@@ -337,8 +368,6 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
       ok = ok && warp_wait(o_full + 8u * t, uses & 1u, abort_flag, p.limit);
       ++uses;
       tc_fence_after();
-      const int row = it.row + static_cast<int>(t) * kHalf + r;
-      const bool live = row < it.len;
       const float inv = ok ? 1.f / sum : __int_as_float(0x7fc00000);
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.o.p) + (it.begin + row) * p.o.row + it.head * p.o.head;
 #pragma unroll
