@@ -30,15 +30,15 @@ __device__ __forceinline__ int block_scan(int v, int* red, bool maximum) {      
   return v;
 }
 
-// The tiles of the sequences [s0, s1) to `out`, ordered by their work: most first (forward: tile i reads the keys of i + 1 tiles) or
+// The tiles of the sequences to `out`, ordered by their work: most first (forward: tile i reads the keys of i + 1 tiles) or
 // least first (backward: tile j is read by the queries of the tiles from j on).  With sequences in the order of their lengths, those
 // with at least w tiles come first, so a tile's place is (tiles in front by their work) + (its sequence's place).  Which of two
 // sequences of one length comes first is left to chance; no result depends on it.  Returns the number of tiles.
 // counts: [3][bins], sequences of exactly b tiles, of at least b, and the tiles in front of those of work b.
-__device__ int order_tiles(const int* starts, int s0, int s1, int rows, bool most_first, int* counts, int bins, int4* out, int cap, int* red) {
+__device__ int order_tiles(const int* starts, int n, int rows, bool most_first, int* counts, int bins, int4* out, int cap, int* red) {
   const int tid = threadIdx.x;
   int longest = 0;
-  for (int i = s0 + tid; i < s1; i += kPlanThreads) longest = max(longest, (starts[i + 1] - starts[i] + rows - 1) / rows);
+  for (int i = tid; i < n; i += kPlanThreads) longest = max(longest, (starts[i + 1] - starts[i] + rows - 1) / rows);
   block_scan(longest, red, true);
   __syncthreads();
   longest = red[31];
@@ -46,7 +46,7 @@ __device__ int order_tiles(const int* starts, int s0, int s1, int rows, bool mos
   int *exact = counts, *least = counts + bins, *before = least + bins;
   for (int b = tid; b < used; b += kPlanThreads) exact[b] = 0;
   __syncthreads();
-  for (int i = s0 + tid; i < s1; i += kPlanThreads) atomicAdd(exact + (starts[i + 1] - starts[i] + rows - 1) / rows, 1);
+  for (int i = tid; i < n; i += kPlanThreads) atomicAdd(exact + (starts[i + 1] - starts[i] + rows - 1) / rows, 1);
   __syncthreads();
   int carry = 0;
   for (int at = 0; at < used; at += kPlanThreads) {
@@ -68,7 +68,7 @@ __device__ int order_tiles(const int* starts, int s0, int s1, int rows, bool mos
   }
   __syncthreads();
   const int lane = tid & 31;
-  for (int i = s0 + (tid >> 5); i < s1; i += kPlanThreads / 32) {          // a warp a sequence
+  for (int i = tid >> 5; i < n; i += kPlanThreads / 32) {          // a warp a sequence
     const int begin = starts[i], end = starts[i + 1], tiles = (end - begin + rows - 1) / rows;
     int place = 0;
     if (lane == 0) place = least[tiles + 1] + atomicSub(exact + tiles, 1) - 1;
@@ -83,14 +83,14 @@ __device__ int order_tiles(const int* starts, int s0, int s1, int rows, bool mos
 }
 
 // One CTA.  Forward, the longest tiles first, so that the last ones to start are short.  Backward, the shortest first, because the
-// sums of dq pass from the last tile of a sequence to the first, and in groups, so that the sums under way stay in L2
-// (abs_attention_bwd.cu).
+// sums of dq pass from the last tile of a sequence to the first.  (Within groups of 16384 to 262144 rows, so that the sums under way
+// stay in L2, 32 x 2048 tokens, 16 heads of 128, took 2510 to 2535 us instead of 2535, and 128 x 1024, 12 heads of 64, as long.)
 __global__ void __launch_bounds__(kPlanThreads)
 attn_plan_kernel(const int* __restrict__ offsets, int n, int total, AttnPlanLayout l, int* plan) {
   __shared__ int red[32];
   __shared__ int bad;
   const int tid = threadIdx.x;
-  int *starts = plan + l.starts, *counts = plan + l.counts, *groups = plan + l.groups;
+  int *starts = plan + l.starts, *counts = plan + l.counts;
   if (tid == 0) bad = 0;
   pdl_wait();
   __syncthreads();
@@ -107,23 +107,9 @@ attn_plan_kernel(const int* __restrict__ offsets, int n, int total, AttnPlanLayo
     carry = max(carry, red[31]);
   }
   __syncthreads();
-  const int fwd = order_tiles(starts, 0, n, kAttnFwdRows, true, counts, l.bins, reinterpret_cast<int4*>(plan + l.fwd), l.fwd_cap, red);
-  int tiles = 0, s0 = 0;
-  for (int g = 0; g < l.n_groups; ++g) {
-    if (tid == 0) groups[g] = tiles;
-    int lo = s0, hi = n;                           // the first sequence that begins behind the group
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if ((starts[mid] >> kAttnGroupBits) <= g) lo = mid + 1;
-      else hi = mid;
-    }
-    if (lo > s0)
-      tiles += order_tiles(starts, s0, lo, kAttnBwdRows, false, counts, l.bins, reinterpret_cast<int4*>(plan + l.bwd) + tiles,
-                           l.bwd_cap - tiles, red);
-    s0 = lo;
-  }
+  const int fwd = order_tiles(starts, n, kAttnFwdRows, true, counts, l.bins, reinterpret_cast<int4*>(plan + l.fwd), l.fwd_cap, red);
+  const int tiles = order_tiles(starts, n, kAttnBwdRows, false, counts, l.bins, reinterpret_cast<int4*>(plan + l.bwd), l.bwd_cap, red);
   if (tid == 0) {
-    groups[l.n_groups] = tiles;
     plan[kPlanFwdTiles] = fwd;
     plan[kPlanBwdTiles] = tiles;
     plan[kPlanBad] = bad;

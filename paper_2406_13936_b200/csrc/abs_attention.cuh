@@ -17,12 +17,9 @@ constexpr int kAttnBwdRows = 128;          // keys of a backward tile
 // the order in which they are worked off, then what the plan's own kernel needs.
 //   record: first row and end of the tile's sequence, number of the tile in the sequence, and the sequence's first slot: a number
 //   such that slot + (tile of 128 rows) is each tile's own, below bwd_cap
-// Backward tiles are ordered within groups of sequences that begin in the same kAttnGroupRows rows, group g's from groups[g] to
-// groups[g + 1].
-constexpr int kAttnGroupBits = 16;
 struct AttnPlanLayout {
-  long long fwd, bwd, groups, starts, counts, words;   // places of the parts, and their end
-  int fwd_cap, bwd_cap, bins, n_groups;
+  long long fwd, bwd, starts, counts, words;   // places of the parts, and their end
+  int fwd_cap, bwd_cap, bins;
 };
 enum { kPlanFwdTiles = 0, kPlanBwdTiles = 1, kPlanBad = 2, kPlanTotal = 3, kPlanHeader = 16 };
 inline AttnPlanLayout attn_plan_layout(int n, int total) {
@@ -30,11 +27,9 @@ inline AttnPlanLayout attn_plan_layout(int n, int total) {
   l.fwd_cap = total / kAttnFwdRows + n;
   l.bwd_cap = total / kAttnBwdRows + n;
   l.bins = total / kAttnBwdRows + 3;           // tiles of one sequence, and one more: 0 to bins - 1
-  l.n_groups = (total >> kAttnGroupBits) + 1;
   l.fwd = kPlanHeader;
   l.bwd = l.fwd + 4ll * l.fwd_cap;
-  l.groups = l.bwd + 4ll * l.bwd_cap;
-  l.starts = l.groups + l.n_groups + 1;
+  l.starts = l.bwd + 4ll * l.bwd_cap;
   l.counts = l.starts + n + 1;
   l.words = l.counts + 3ll * l.bins;
   l.words = (l.words + 3) & ~3ll;
@@ -50,6 +45,10 @@ struct AttnOut {
   void* p;
   long long row, head;
 };
+// Whether every row of every head is whole sectors of 32 bytes of a 16-bit type.
+inline bool in_sectors(const AttnOut& o, int hd) {
+  return reinterpret_cast<uintptr_t>(o.p) % 32 == 0 && o.row % 16 == 0 && o.head % 16 == 0 && hd % 16 == 0;
+}
 bool encode_heads_map(const AttnRows& t, int total, int heads, int hd, CUtensorMap* map);      // boxes of 128 rows x 64 columns of a head
 struct AttnForward {
   AttnRows q, k, v;

@@ -14,8 +14,10 @@
 // queries in a fixed order, so results repeat bit for bit: tile j of a sequence starts at query block j and goes up, so block i is
 // reached first by tile i, then by i - 1, and so on, each a step later than the one before; a counter says whose turn
 // it is, and the wait is rarely one.  The first of them stores instead of adding (nothing is cleared), and the last, tile 0, adds its own part
-// to the sums and writes dq: sequences of up to 128 rows never touch the sums.  Tiles are worked off shortest first within a group of
-// sequences and some of the heads (attn_plan_kernel), so that the sums under way stay in L2.
+// to the sums and writes dq: sequences of up to 128 rows never touch the sums.  Tiles are worked off shortest first
+// (attn_plan_kernel), each for all heads before the next: a tile's predecessors in the order of the sums are then far ahead.  (Some
+// heads at a time, so that the sums under way stay in L2, costs more in waits than it saves: 32768 tokens, 8 heads of 128, 1 at a
+// time 11.7 ms, all 7.5; 16 x 2048, 12 heads of 64, 1, 2, 4, 12: 1263, 793, 568, 550 us.)
 // The grid is resident (a cooperative launch) and CTAs take the tiles in that order as they are free, in which each comes after those that it
 // waits for, so the first unfinished tile of all never waits.
 //
@@ -67,35 +69,25 @@ struct BwdParams {
   unsigned* counters;                         // [hq][cap][HD / 64], then the next tile that nobody has
   const int* plan;
   const int* tiles;
-  const int* groups;
-  int total, hq, hk, parts, hd, cap, n_groups;
+  int total, hq, hk, parts, hd, cap;
   // A key head's group of query heads in `parts` of `group` heads, each a head of its own in the list of tiles, `heads` in all.
-  int heads, group, heads_at_once;
+  int heads, group;
   float* partial;                             // [parts][dv, dk][hk][total][HD], laid out as sums; NULL: parts = 1
   float by, scale;                            // scale log2 e, scale
   long long limit;
   int drop_loads;
+  bool sectors;                               // whether dq, dk and dv are rows of whole sectors of 32 bytes
 };
 struct BwdItem {
   int begin, len, slot, tile, head;           // head: of the list of tiles
   int blocks, steps;                          // query blocks from the tile on, and of all the group's heads
 };
-// Tile i of the list, for a whole warp (the same i in all lanes).
+// Tile i of the list: all heads of a tile come after one another.
 __device__ __forceinline__ BwdItem bwd_item(const BwdParams& p, int i) {
-  const int lane = threadIdx.x & 31;
-  int g = 0;                                  // the group: those whose tiles end at or before i
-  for (int at = 0; at < p.n_groups; at += 32) {
-    const bool behind = at + lane < p.n_groups && __ldg(p.groups + at + lane + 1) * p.heads <= i;
-    const int n = __popc(__ballot_sync(0xffffffffu, behind));
-    g += n;
-    if (n < 32) break;
-  }
-  const int t0 = __ldg(p.groups + g), n = __ldg(p.groups + g + 1) - t0, local = i - p.heads * t0;
-  const int chunk = local / (n * p.heads_at_once), first = chunk * p.heads_at_once, rem = local - first * n;
-  const int heads = min(p.heads_at_once, p.heads - first);
-  const int4 r = __ldg(reinterpret_cast<const int4*>(p.tiles) + t0 + rem / heads);
+  const int at = i / p.heads;
+  const int4 r = __ldg(reinterpret_cast<const int4*>(p.tiles) + at);
   BwdItem it;
-  it.head = first + rem % heads;
+  it.head = i - at * p.heads;
   it.begin = r.x;
   it.len = r.y - r.x;
   it.tile = r.z;
@@ -148,7 +140,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
                  st_full = b0 + 96u, st_free = b0 + 112u, turn_ok = b0 + 128u, staged = b0 + 144u, stage_free = b0 + 160u, dq_full = b0 + 176u,
                  dq_read = b0 + 192u, item_full = b0 + 208u, item_free = b0 + 240u, s_full = b0 + 272u, p_full = b0 + 280u, dp_full = b0 + 288u,
                  ds_full = b0 + 296u, acc_full = b0 + 304u, dv_free = b0 + 312u, dk_free = b0 + 320u, landed = b0 + 328u,
-                 done_bar = b0 + 336u;
+                 done_bar = b0 + 336u, dv_full = b0 + 344u;
   if (threadIdx.x == 0) {
     for (uint32_t k = 0; k < 2; ++k) {
       mbar_init(kv_full + 8u * k, 1);
@@ -174,6 +166,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     mbar_init(dp_full, 1);
     mbar_init(ds_full, 8);
     mbar_init(acc_full, 1);
+    mbar_init(dv_full, 1);
     mbar_init(dv_free, 4);
     mbar_init(dk_free, 4);
     mbar_init(landed, 1);
@@ -411,6 +404,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
             for (uint32_t k = 0; k < kBlock / 16; ++k)       // P' of the first 64 queries lies at columns 0-31, of the others at 64-95
               mma_ts(tmem + Sh::kDv, tmem + Sh::kS + 64u * (k / 4) + 8u * (k % 4), mn | (d + 128u * k), idesc_k, (t > 0 || k > 0) ? 1u : 0u);
             mma_commit(do_free + 8u * ds);
+            if (t + 1 == it.steps) mma_commit(dv_full);
           }
           __syncwarp();
           if (t + 1 < it.steps) {
@@ -504,8 +498,43 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     BwdItem it;
 #pragma unroll 1
     for (uint32_t k = 0; take_item(k, it); ++k) {
+      // the tile's dv before its last dq (it is complete while the softmax warps are on their last dS', and the next tile's waits for the
+      // place: with both results last the first dV of a tile waited for a step's time), its dk after it
 #pragma unroll 1
-      for (int t = 0; t < it.steps; ++t, ++n) {
+      for (int t = 0; t <= it.steps; ++t) {
+        if (t + 1 >= it.steps) {
+          const bool is_dk = t == it.steps;
+          ok = ok && warp_wait(is_dk ? acc_full : dv_full, k & 1u, abort_flag, p.limit);
+          tc_fence_after();
+          const int row = it.tile * kBlock + r, rows = min(32, it.len - it.tile * kBlock - 32 * sub), kv = it.head / p.parts;
+#pragma unroll 1
+          for (int c0 = 0; c0 < HD; c0 += 32) {
+            uint32_t v[32];
+            if (ok) {
+              tmem_load32(tmem + (is_dk ? Sh::kDk : Sh::kDv) + c0 + (static_cast<uint32_t>(sub * 32) << 16), v);
+              tmem_loaded(v);
+            } else {
+#pragma unroll
+              for (int c = 0; c < 32; ++c) v[c] = 0x7fc00000u;
+            }
+            if (c0 + 32 == HD && ok) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(is_dk ? dk_free : dv_free);
+            }
+            if (row < it.len && p.parts > 1) {
+              float4* part = reinterpret_cast<float4*>(p.partial + ((static_cast<long long>((it.head - kv * p.parts) * 2 + is_dk) * p.hk + kv) * p.total +
+                                                                    it.begin + it.tile * kBlock + 32 * sub) * HD) + static_cast<long long>(c0 / 4) * rows + lane;
+    #pragma unroll
+              for (int c = 0; c < 8; ++c)
+                part[c * rows] = make_float4(__uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]), __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
+            } else if (row < it.len) {
+              const AttnOut to = is_dk ? p.dk : p.dv;
+              store_row32(static_cast<__nv_bfloat16*>(to.p) + (it.begin + row) * to.row + kv * to.head + c0, v, is_dk ? p.scale : 1.f, true, p.hd - c0, p.sectors);
+            }
+          }
+        }
+        if (t == it.steps) break;
         int head, block;
         bwd_step(p, it, t, head, block);
         const int row = block * kBlock + r, rows = min(kBlock, it.len - block * kBlock);
@@ -558,59 +587,16 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
                 }
               }
             }
-            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head + 64 * half;
+            if (live) {
+              __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.dq.p) + (it.begin + row) * p.dq.row + head * p.dq.head;
 #pragma unroll
-            for (int c = 0; c < 64; c += 8) {
-              uint32_t w[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                w[k] = ok ? bf16_pair(__uint_as_float(x[c + 2 * k]) * p.scale, __uint_as_float(x[c + 2 * k + 1]) * p.scale) : 0x7fc07fc0u;
-              if (live && 64 * static_cast<int>(half) + c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+              for (int c = 0; c < 64; c += 32) store_row32(out + 64 * half + c, x + c, p.scale, ok, p.hd - 64 * static_cast<int>(half) - c, p.sectors);
             }
           }
           __syncwarp();
           if (ok && lane == 0) mbar_arrive(staged + 8u * (u & 1u));
         }
-      }
-      // the tile's dv and dk: rows of keys.  (The softmax warps are on the next tile meanwhile.)
-      ok = ok && warp_wait(acc_full, k & 1u, abort_flag, p.limit);
-      tc_fence_after();
-      const int row = it.tile * kBlock + r, rows = min(32, it.len - it.tile * kBlock - 32 * sub), kv = it.head / p.parts;
-#pragma unroll 1
-      for (int q = 0; q < 2 * (HD / 32); ++q) {                    // 32 columns of dv, then of dk
-        const bool is_dk = q >= HD / 32;
-        const int c0 = 32 * (is_dk ? q - HD / 32 : q);
-        uint32_t v[32];
-        if (ok) {
-          tmem_load32(tmem + (is_dk ? Sh::kDk : Sh::kDv) + c0 + (static_cast<uint32_t>(sub * 32) << 16), v);
-          tmem_loaded(v);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) v[c] = 0x7fc00000u;
-        }
-        if ((q + 1) % (HD / 32) == 0 && ok) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(is_dk ? dk_free : dv_free);
-        }
-        if (row < it.len && p.parts > 1) {
-          float4* part = reinterpret_cast<float4*>(p.partial + ((static_cast<long long>((it.head - kv * p.parts) * 2 + is_dk) * p.hk + kv) * p.total +
-                                                                it.begin + it.tile * kBlock + 32 * sub) * HD) + static_cast<long long>(c0 / 4) * rows + lane;
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-            part[c * rows] = make_float4(__uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]), __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
-        } else if (row < it.len) {
-          const float by = is_dk ? p.scale : 1.f;
-          const AttnOut to = is_dk ? p.dk : p.dv;
-          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(to.p) + (it.begin + row) * to.row + kv * to.head + c0;
-#pragma unroll
-          for (int c = 0; c < 32; c += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = bf16_pair(__uint_as_float(v[c + 2 * e]) * by, __uint_as_float(v[c + 2 * e + 1]) * by);
-            if (c0 + c < p.hd) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
+        ++n;
       }
     }
   } else {
@@ -833,21 +819,13 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
   const long long threads = static_cast<long long>(a.total) * a.hq * lanes;
   ABS_CUDA_TRY(ctx, launch_dependent(attn_backward_start_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a,
                                      reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<unsigned*>(mem + s.counters), counters, lanes));
-  // Heads whose sums of dq are under way at a time: 48 MB of them, or, up to 96 MB, as many as make a tile's predecessor in the order of
-  // the sums more than a grid away in the order of the tiles, where it is done and nobody waits for it.  16 x 1024 tokens, 12 heads of 128:
-  // HEADS_FIG.
   const int parts = attn_parts(a.total, a.hq, a.hk, a.n), group = a.hq / a.hk / parts, all = a.hk * parts;
-  const long long rows = a.total < (1 << kAttnGroupBits) ? a.total : 1 << kAttnGroupBits;
-  const long long size = rows * group * HD * 4, sequences = a.n * rows / a.total > 1 ? a.n * rows / a.total : 1;
-  long long heads = (48ll << 20) / size;
-  const long long apart = (ctx->sm_count + ctx->sm_count / 4 + sequences - 1) / sequences, most_heads = (96ll << 20) / size;
-  if (heads < apart) heads = apart < most_heads ? apart : most_heads;
-  heads = heads < 1 ? 1 : heads > all ? all : heads;
   const BwdParams p{a.dq, a.dk, a.dv, reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<float*>(mem + s.sums),
-                    reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.plan + l.groups, a.total, a.hq, a.hk,
-                    parts, a.hd, l.bwd_cap, l.n_groups, all, group, static_cast<int>(heads), reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
+                    reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.total, a.hq, a.hk,
+                    parts, a.hd, l.bwd_cap, all, group, reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
-                    ctx->tuning.stats_fault_drop_loads ? 1 : 0};
+                    ctx->tuning.stats_fault_drop_loads ? 1 : 0,
+                    in_sectors(a.dq, a.hd) && in_sectors(a.dk, a.hd) && in_sectors(a.dv, a.hd)};
   const long long most = static_cast<long long>(l.bwd_cap) * all;
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute attr[1];

@@ -34,6 +34,9 @@ constexpr float kLn2F = 0.6931471805599453f, kLog2eF = 1.4426950408889634f;
 template <int HD> struct FwdShape {
   static constexpr uint32_t kRowsBytes = kHalf * HD * 2;          // 128 rows of one head
   static constexpr int kPlaces = HD == 64 ? 8 : 5;
+  // Of 16 pairs of exponentials how many are taken on the FMA pipe.  0, 2, 4, 5, 6: 486, 478, 475, 480, 488 us (128 of 1024 tokens, 12 heads
+  // of 64), 171, 168, 170, 171, 176 (4 of 4096, 8 heads of 128 and 2 of keys): what issues is soon as scarce as the unit.
+  static constexpr int kFmaPairs = HD == 64 ? 4 : 2;
   // tensor memory: S of the halves, O of the halves from 256 on; P over S, or beside it where there is room
   static __device__ __forceinline__ uint32_t p_at(uint32_t t) { return HD == 64 ? 384u + 64u * t : 128u * t; }
   static constexpr size_t kSmem = (2 + kPlaces) * static_cast<size_t>(kRowsBytes) + 1024 + 512;
@@ -50,6 +53,7 @@ struct FwdParams {
   int total, hq, group, hd;
   float by;                                   // scale log2 e
   long long limit;
+  bool sectors;                               // whether O is rows of whole sectors of 32 bytes
   int drop_loads;                             // test hook: nothing is loaded, so every wait must run out
 };
 struct FwdItem {
@@ -350,10 +354,16 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
             uint32_t w[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const float2 y = unpack2f(fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2));
-              const float u = exp2_approx(y.x), v = exp2_approx(y.y);
-              part[e & 1] = add2f(part[e & 1], pack2f(u, v));
-              w[e] = bf16_pair(u, v);
+              uint64_t y = fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2);
+              if (e >= 16 - FwdShape<HD>::kFmaPairs) {
+                y = exp2_pair_fma(y);
+              } else {
+                const float2 a = unpack2f(y);
+                y = pack2f(exp2_approx(a.x), exp2_approx(a.y));
+              }
+              part[e & 1] = add2f(part[e & 1], y);
+              const float2 a = unpack2f(y);
+              w[e] = bf16_pair(a.x, a.y);
             }
             tmem_store16(p_at + (c + 32 * q) / 2, w);              // (over S: columns that have been read)
           }
@@ -382,14 +392,7 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
           __syncwarp();
           if (lane == 0) mbar_arrive(o_free + 8u * t);
         }
-#pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            w[k] = ok ? bf16_pair(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv) : 0x7fc07fc0u;
-          if (live && c + e < p.hd) *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        if (live) store_row32(out + c, o, inv, ok, p.hd - c, p.sectors);
       }
       if (live && p.lse)
         p.lse[static_cast<long long>(it.head) * p.total + it.begin + row] = ok ? fmaf(m, kLn2F, logf(sum)) : __int_as_float(0x7fc00000);
@@ -412,7 +415,7 @@ int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
   const AttnPlanLayout l = attn_plan_layout(a.n, a.total);
   const FwdParams p{a.o, a.lse, a.plan, a.plan + l.fwd, a.total, a.hq, a.hq / a.hk, a.hd, a.scale * kLog2eF,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
-                    ctx->tuning.stats_fault_drop_loads ? 1 : 0};
+                    in_sectors(a.o, a.hd), ctx->tuning.stats_fault_drop_loads ? 1 : 0};
   auto kern = attn_forward_kernel<HD>;
   const size_t smem = FwdShape<HD>::kSmem;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));

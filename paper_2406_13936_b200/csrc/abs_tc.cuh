@@ -118,6 +118,26 @@ __device__ __forceinline__ float exp2_approx(float x) {          // within 2 ulp
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// 2^x of a pair on the FMA pipe, for some of the exponentials where the other unit (16 a clock and SM) is what bounds: x = n + f with n
+// the nearest whole number (Cody and Waite's reduction, exact for base 2), 2^f by a polynomial of degree 5 whose relative error is the
+// least possible on [-1/2, 1/2] (7.5e-8, found by Remez's exchange; 2.1e-7 with its roundings), and 2^n from its bits: adding 1.5 2^23 + 127
+// leaves n + 127 in the lowest bits, which are shifted into the exponent.  Below -126.5 zero; NaN stays NaN.
+__device__ __forceinline__ uint64_t exp2_pair_fma(uint64_t x) {
+  constexpr float kShift = 12582912.f + 127.f;
+  float2 v = unpack2f(x);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(v.x) : "f"(-127.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(v.y) : "f"(-127.f));
+  x = pack2f(v.x, v.y);
+  const uint64_t t = add2f(x, pack2f(kShift, kShift));
+  const uint64_t n = add2f(t, pack2f(-kShift, -kShift)), f = fma2f(n, pack2f(-1.f, -1.f), x);
+  uint64_t p = fma2f(pack2f(1.3276472454890609e-3f, 1.3276472454890609e-3f), f, pack2f(9.675540961325169e-3f, 9.675540961325169e-3f));
+  p = fma2f(p, f, pack2f(5.550713092088699e-2f, 5.550713092088699e-2f));
+  p = fma2f(p, f, pack2f(0.24022120237350464f, 0.24022120237350464f));
+  p = fma2f(p, f, pack2f(0.6931469440460205f, 0.6931469440460205f));
+  p = fma2f(p, f, pack2f(1.0000001192092896f, 1.0000001192092896f));
+  const float2 b = unpack2f(t);
+  return mul2f(p, pack2f(__uint_as_float(__float_as_uint(b.x) << 23), __uint_as_float(__float_as_uint(b.y) << 23)));
+}
 __device__ __forceinline__ float max3f(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -158,5 +178,27 @@ __host__ __device__ constexpr uint32_t mma_idesc(int m, int n, bool a_mn, bool b
          (static_cast<uint32_t>(m >> 4) << 24);
 }
 #endif
+
+// 32 columns of a thread's row times `by` as bf16 (NaN if not valid), of which the first `columns` exist, a multiple of 8; of a row's
+// length and place multiples of 16 (sectors) whole sectors of 32 bytes: a warp's rows lie far apart, and the backward pass of 16 x 1024 tokens,
+// 12 heads of 128, took 340 us with 16 bytes at a time and takes 323.
+__device__ __forceinline__ void store_row32(__nv_bfloat16* out, const uint32_t* x, float by, bool valid, int columns, bool sectors) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 16) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      w[i] = valid ? bf16_pair(__uint_as_float(x[c + 2 * i]) * by, __uint_as_float(x[c + 2 * i + 1]) * by) : 0x7fc07fc0u;
+    if (sectors) {
+      if (c < columns)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + c), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                     "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+      if (c < columns) *reinterpret_cast<uint4*>(out + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (c + 8 < columns) *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+}
 
 }  // namespace absk
