@@ -131,7 +131,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   unsigned long long* bars = reinterpret_cast<unsigned long long*>(smem_dyn + Sh::kData);
   constexpr int kBars = 44;
   volatile unsigned* abort_flag = reinterpret_cast<volatile unsigned*>(bars + kBars);
-  unsigned* tmem_slot = const_cast<unsigned*>(abort_flag) + 1;
+  unsigned *tmem_slot = const_cast<unsigned*>(abort_flag) + 1, *untold = tmem_slot + 1;    // untold: a tile that was taken when a wait ran out
   int4* ring = reinterpret_cast<int4*>(bars + kBars + 2);          // four items of two pieces of 16 bytes
   const uint32_t b0 = smem_u32(bars);
   // two of each of the first ones (where one is waited for by several who may be a step apart, steps alternate between the two: with a
@@ -172,6 +172,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     mbar_init(landed, 1);
     mbar_init(done_bar, 1);
     *abort_flag = (kv_at & 1023u) ? 1u : 0u;
+    *untold = ~0u;
     for (uint32_t k = 0; k < 2 * kItems; ++k) ring[k] = make_int4(0, 0, 0, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -239,8 +240,10 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       // (taking one is a way to L2 and back, which is under way while the next copies are issued)
       uint32_t told = 0;
       unsigned taken = 0;
+      bool has_taken = false;
       auto take = [&]() {
         if (lane == 0) taken = atomicAdd(next_item, 1u);
+        has_taken = true;
       };
       auto tell = [&]() {
         if (told >= kItems) ok = ok && warp_wait(item_free + 8u * (told % kItems), (told / kItems - 1) & 1u, abort_flag, p.limit);
@@ -255,6 +258,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
         }
         __syncwarp();
         ++told;
+        has_taken = false;
       };
       // -lse and -delta of a block's queries; zeros behind the sequence, where Q and dO are zeros and what the weights are changes nothing
       auto copy_stats = [&](const BwdItem& it, int head, int block) {
@@ -304,6 +308,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           if (ok && (t == 1 || it.steps == 1)) tell();
         }
       }
+      if (has_taken && lane == 0) *untold = taken;
       asm volatile("cp.async.wait_all;" ::: "memory");
       // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.  (After an abort a place's last
       // copy may be one further on than the count says: its wait may run out for nothing, which is bounded too.)
@@ -704,7 +709,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       __syncthreads();
       if (warp == 0 && k >= kItems) {
         unsigned i = 0;
-        if (lane == 0) i = atomicAdd(next_item, 1u);
+        if (lane == 0) i = k == kItems && *untold != ~0u ? *untold : atomicAdd(next_item, 1u);
         i = __shfl_sync(0xffffffffu, i, 0);
         BwdItem next = {};
         if (i < static_cast<unsigned>(items)) next = bwd_item(p, static_cast<int>(i));

@@ -392,3 +392,68 @@ def test_nothing_to_do(ctx):
     empty = Batch([], 2, 2, 64, "bf16")
     plan, o, lse = run_forward(ctx, empty)
     run_backward(ctx, empty, plan, o, lse)
+
+
+@pytest.mark.parametrize("hq,hk,parts", [(6, 2, 1), (6, 2, 3), (4, 1, 4)])
+def test_groups_of_heads_whole_and_in_parts(ctx, hq, hk, parts):
+    """Many tiles: a group's query heads are one tile's work; few: each part's dk and dv are summed at the end."""
+    b = Batch([5, 131] * 300 if parts == 1 else [700, 129], hq, hk, 64, "bf16", seed=31)
+    tiles = (b.total // 128 + len(b.lens)) * hk
+    assert (tiles >= 8 * 148) == (parts == 1)
+    plan, o, lse = run_forward(ctx, b)
+    check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
+
+
+@pytest.mark.parametrize("hd,pad", [(64, 8), (128, 8), (72, 0), (72, 8), (64, 16)])
+def test_rows_that_are_no_whole_sectors(ctx, hd, pad):
+    """Strides of 16 bytes that are not 32, and heads whose last sector is half: rows are stored 16 bytes at a time, nothing beside them."""
+    b = Batch([3, 150, 300], 4, 2, hd, "bf16", seed=32, front=2, tail=3, pad=pad)
+    plan = ctx.attention_plan(b.offsets, b.total)
+    wide = torch.full((b.total, b.hq * hd + pad), 7.0, device="cuda", dtype=torch.bfloat16)
+    o, lse = wide[:, :b.hq * hd].unflatten(1, (b.hq, hd)), torch.full((b.hq, b.total), 7.0, device="cuda")
+    ctx.abs_attention(b.q, b.k, b.v, plan, o, lse, scale=b.scale)
+    check_forward(b, o, lse)
+    assert (wide[:, b.hq * hd:] == 7.0).all() and (o[b.outside()] == 7.0).all()
+    width = (b.hq + 2 * b.hk) * hd
+    grads = torch.full(b.fused.shape, 7.0, device="cuda", dtype=torch.bfloat16)
+    heads = grads[:, :width].unflatten(1, (b.hq + 2 * b.hk, hd))
+    dq, dk, dv = heads[:, :b.hq], heads[:, b.hq:b.hq + b.hk], heads[:, b.hq + b.hk:]
+    scratch = ctx.attention_scratch(b.total, b.hq, b.hk, hd, len(b.lens))
+    ctx.abs_attention_backward(b.do, b.q, b.k, b.v, o, lse, plan, dq, dk, dv, scratch, scale=b.scale)
+    check_backward(b, o, lse, dq, dk, dv)
+    assert (grads[:, width:] == 7.0).all() and (grads[b.outside()] == 7.0).all()
+
+
+@pytest.mark.parametrize("hd,hq,hk", [(64, 4, 4), (128, 4, 4), (64, 6, 2)])
+def test_a_wait_that_runs_out_leaves_nan_and_the_next_call_is_right(ctx, hd, hq, hk):
+    b = Batch([300, 0, 1, 700], hq, hk, hd, "bf16", seed=33, front=1, tail=2)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    ctx.set_tuning("stats_timeout_cycles", 200000)
+    ctx.set_tuning("stats_fault_drop_loads", 1)
+    try:
+        _, lost, lost_lse = run_forward(ctx, b)
+        lost_grads = run_backward(ctx, b, plan, o, lse)
+        torch.cuda.synchronize()
+    finally:
+        ctx.set_tuning("stats_fault_drop_loads", 0)
+        ctx.set_tuning("stats_timeout_cycles", 0)
+    inside = ~b.outside()
+    assert torch.isnan(lost[inside]).all() and torch.isnan(lost_lse[:, inside]).all()
+    for g in lost_grads:
+        assert torch.isnan(g[inside]).all() and (g[~inside] == 7.0).all()
+    assert (lost[~inside] == 7.0).all()
+    _, again, again_lse = run_forward(ctx, b)
+    assert torch.equal(again, o) and torch.equal(again_lse, lse)
+    for g, want in zip(run_backward(ctx, b, plan, o, lse), grads):
+        assert torch.equal(g, want)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_of_zero_and_below(ctx, dtype, scale):
+    b = Batch([1, 65, 200], 2, 1, 64, dtype, seed=34)
+    b.scale = scale
+    plan, o, lse = run_forward(ctx, b)
+    check_forward(b, o, lse)
+    check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
