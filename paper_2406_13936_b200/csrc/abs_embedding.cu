@@ -5,8 +5,8 @@
 // Both are bound by memory: forward reads a row of the table and writes one of Y a token, backward reads dY and writes dE once.
 // The gradient's sums must not depend on the order of atomics, so the tokens are sorted (stable, so that a token's places are in
 // order) and every row of dE is summed by one group of threads, or, where a token's places cross from one run of the sorted
-// list to the next, from the runs' partial sums in order.  8 x 16384 tokens, 50000 rows of 768, bf16: 70 us forward, 283 backward (5.0 and
-// 5.1 TB/s of what has to move).
+// list to the next, from the runs' partial sums in order.  8 x 16384 tokens, 50000 rows of 768, bf16: 68 us forward, 267 backward (5.1 and
+// 5.4 TB/s of what has to move).
 #include "abs_pipeline.cuh"
 
 namespace absk {
@@ -90,7 +90,8 @@ __device__ __forceinline__ void load_row(const float* p, float (&x)[V]) {
   }
 }
 
-// A thread has one piece of V elements of kUnroll rows: the tokens' numbers first, then every row's loads, then the stores.
+// A thread has one piece of V elements of kUnroll rows, whose loads all go before the first store.  (8 x 16384 tokens, 50000 rows of 768, bf16:
+// 68 us; two rows 79, eight 78, all tokens' numbers before the first row 74.)
 template <typename T, int V>
 __global__ void __launch_bounds__(kEmbThreads)
 embedding_kernel(const Embedding a, int pieces, long long work) {
@@ -204,13 +205,14 @@ emb_scan_kernel(const EmbeddingGrad a) {
 // The lanes with the same value of the digit as this one; lanes without a key have values of their own.
 __device__ __forceinline__ unsigned same_digit(unsigned digit) { return __match_any_sync(0xffffffffu, digit); }
 
-// A tile's keys to their places.  counts: [warps][kBinsR], zero.
+// A tile's keys, `each` a thread, to their places.  counts: [warps][kBinsR], zero.
 __device__ __forceinline__ void place_keys(unsigned short* counts, const unsigned (&digit)[kKeysPerThread], const bool (&live)[kKeysPerThread],
-                                           unsigned (&rank)[kKeysPerThread]) {
+                                           unsigned (&rank)[kKeysPerThread], int each = kKeysPerThread) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned short* mine = counts + warp * kBinsR;
 #pragma unroll
   for (int k = 0; k < kKeysPerThread; ++k) {
+    if (k >= each) break;
     const unsigned peers = same_digit(live[k] ? digit[k] : kBinsR + lane);
     const unsigned before = __popc(peers & ((1u << lane) - 1u));
     if (live[k]) rank[k] = mine[digit[k]] + before;
@@ -276,11 +278,12 @@ emb_sort_small_kernel(const EmbeddingGrad a, int passes) {
   pdl_wait();
   unsigned key[kKeysPerThread], pos[kKeysPerThread], digit[kKeysPerThread], rank[kKeysPerThread];
   bool live[kKeysPerThread];
+  const int each = (a.rows + kSmallThreads - 1) / kSmallThreads;
   for (int pass = 0; pass < passes; ++pass) {
 #pragma unroll
     for (int k = 0; k < kKeysPerThread; ++k) {
-      const int i = 32 * (warp * kKeysPerThread + k) + lane;
-      live[k] = i < a.rows;
+      const int i = 32 * (warp * each + k) + lane;
+      live[k] = k < each && i < a.rows;
       key[k] = pos[k] = 0;
       if (live[k]) {
         key[k] = pass == 0 ? token_key(a, m, i) : keys[i];
@@ -290,7 +293,7 @@ emb_sort_small_kernel(const EmbeddingGrad a, int passes) {
     }
     for (int b = threadIdx.x; b < kBinsR * (kSmallThreads / 32); b += kSmallThreads) (&counts[0][0])[b] = 0;
     __syncthreads();
-    place_keys(&counts[0][0], digit, live, rank);
+    place_keys(&counts[0][0], digit, live, rank, each);
     __syncthreads();
     unsigned s = 0;                                // thread b: value b's keys in all, then in the values before
 #pragma unroll
@@ -375,18 +378,28 @@ emb_sum_kernel(const EmbeddingGrad a, int width, int pieces, int sum_ctas) {
     float sum[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[e] = 0.f;
+    // kDeep rows at a time; the next ones' numbers are on their way while these are (8 x 16384 tokens: 2, 3, 4, 8 rows 275, 270, 267,
+    // 316 us, without looking ahead 283)
     constexpr int kDeep = 4;
+    unsigned next[kDeep], place[kDeep];
+    auto look = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < kDeep; ++u) {
+        const bool in = i + u < end;
+        next[u] = in ? keys[i + u] : none;
+        place[u] = in ? places[i + u] : 0u;
+      }
+    };
+    look(first);
     for (int i = first; i < end && now != none; i += kDeep) {
       Raw raw[kDeep];
       unsigned k[kDeep];
 #pragma unroll
       for (int u = 0; u < kDeep; ++u) {
-        k[u] = none;
-        if (i + u < end) {
-          k[u] = keys[i + u];
-          if (k[u] != none) raw[u] = __ldcs(reinterpret_cast<const Raw*>(dy + static_cast<long long>(places[i + u]) * a.dy_rs));
-        }
+        k[u] = next[u];
+        if (k[u] != none) raw[u] = __ldcs(reinterpret_cast<const Raw*>(dy + static_cast<long long>(place[u]) * a.dy_rs));
       }
+      look(i + kDeep);
 #pragma unroll
       for (int u = 0; u < kDeep; ++u) {
         if (i + u >= end) continue;
@@ -475,11 +488,22 @@ emb_join_kernel(const EmbeddingGrad a, int width, int pieces) {
   float sum[V];
   load_row<V>(part + a.d, sum);
   part += 2 * a.d;
-  for (int r = run + 1; r < a.runs && keys[r * a.run] == now; ++r, part += 2 * a.d) {
-    float x[V];
-    load_row<V>(part, x);
+  // (four runs at a time: a frequent token's are a long chain; what is loaded of runs that do not have it is not looked at)
+  bool on = true;
+  for (int r = run + 1; on && r < a.runs; r += 4, part += 8 * a.d) {
+    float x[4][V];
+    bool has[4];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] += x[e];
+    for (int u = 0; u < 4; ++u) {
+      has[u] = r + u < a.runs && keys[(r + u) * a.run] == now;
+      if (r + u < a.runs) load_row<V>(part + u * 2 * a.d, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      on = on && has[u];
+#pragma unroll
+      for (int e = 0; e < V; ++e) sum[e] = on ? sum[e] + x[u][e] : sum[e];
+    }
   }
 #pragma unroll
   for (int e = 0; e < V; ++e) sum[e] *= a.scale;
@@ -521,9 +545,11 @@ int key_passes(long long vocab) {
   while ((vocab >> bits) > 0) ++bits;              // keys go up to vocab
   return (bits + kRadixBits - 1) / kRadixBits;
 }
-// Runs of 32 tokens, longer ones where a frequent token would cross hundreds of them.
-int run_length(long long rows) {
-  long long r = 32;
+// Runs of 32 tokens, longer ones where a frequent token would cross hundreds of them, shorter ones (down to 8) where they would be
+// fewer than a few an SM.
+int run_length(int M, long long rows) {
+  long long r = 8;
+  while (r < 32 && M * rows / r > 4 * kSmCountFallback) r *= 2;
   while (r < 1024 && rows / r > 2048) r *= 2;
   return static_cast<int>(r);
 }
@@ -540,7 +566,7 @@ EmbScratch emb_scratch(int M, long long rows, long long d) {
     return r;
   };
   const size_t n = static_cast<size_t>(M) * rows * sizeof(unsigned);
-  s.run = run_length(rows);
+  s.run = run_length(M, rows);
   s.runs = static_cast<int>((rows + s.run - 1) / s.run);
   s.tiles = static_cast<int>((rows + kTileKeys - 1) / kTileKeys);
   const bool small = rows <= kSmallKeys;
