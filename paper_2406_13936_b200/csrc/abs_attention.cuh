@@ -71,7 +71,7 @@ struct AttnBackward {
 
 // Into how many parts the tensor-core kernel's backward pass splits a group's query heads: a key tile and head is one CTA's work for all
 // queries of the group, and with fewer than eight tiles an SM the last ones to finish (128 keys of a long sequence, 8 query heads:
-// hundreds of blocks) are most of the time: 9 sequences of 1 to 1500 rows, 16 heads of 128 and 2 of keys, whole 502 us, in parts 263.
+// hundreds of blocks) are most of the time: 9 sequences of 1 to 1500 rows, 16 heads of 128 and 2 of keys, whole 502 us, in parts 263 (since then 130).
 // (A rule of sizes alone: the scratch depends on it.)
 inline int attn_parts(int total, int hq, int hk, int n) {
   const long long tiles = (static_cast<long long>(total) / kAttnBwdRows + n) * hk;

@@ -24,7 +24,7 @@
 // Rounded to fewer bits than 32: P and dS to bf16, as operands of the tensor core, and the results.
 //
 // At 64 columns a head the softmax warps are busiest (1024 clocks of exponentials per 128 x 128 scores and as many of everything else, while
-// five products take 1280), and a block's steps depend on one another: 128 of 1024 tokens, 12 heads of 64, 1.35 to 1.44 ms, 360 to
+// five products take 1280), and a block's steps depend on one another: 128 of 1024 tokens, 12 heads of 64, 1.35 to 1.43 ms, 360 to
 // 380 TFLOP/s; 65536 tokens in one 560.  At 128 columns five products take 2560 clocks and the sums of dq, 64 KB a block to L2, about
 // as long: 32768 tokens, 8 heads, 735 TFLOP/s, 32 of 2048, 16 heads, 540.
 //

@@ -12,10 +12,11 @@
 // bf16's relative steps, and O, which stays in tensor memory, is rescaled a few times a tile instead of once per 128 keys.
 // Rounded to fewer bits than 32: P to bf16, as an operand of the tensor core (its sums of p are taken before that), and O.
 //
-// Bound by the exponentials at 64 columns a head (16 a clock and SM: 1024 clocks per 128 x 128 scores, whose products take 512) and by
-// both at 128, together with the instructions around them: two passes over S from tensor memory, the first for its largest, because 128
-// scores a thread held in registers spill (672 us for 500).  128 of 1024 tokens, 12 heads of 64: 455 to 500 us by the data (all exponentials
-// on their unit alone 200, products 146 at the sustained rate); 8191 and 4097 tokens, 8 heads of 128 and 2 of keys: 229 us, 750 TFLOP/s.
+// The floor is the exponentials at 64 columns a head (16 a clock and SM: 1024 clocks per 128 x 128 scores, whose products take 512) and
+// both at 128; what bounds it are the softmax warps, two a scheduler, whose steps depend on one another (issue slots 45 % busy): two
+// passes over S from tensor memory, the first for its largest, because 128 scores a thread held in registers spill (672 us for 500).
+// 128 of 1024 tokens, 12 heads of 64: 460 to 500 us (all exponentials on their unit alone 200, products 146 at the sustained rate);
+// 8191 and 4097 tokens, 8 heads of 128 and 2 of keys: 225 us, 760 TFLOP/s.
 //
 // Roles of the 12 warps: 0 loads (TMA; Q once a tile, K and V through a ring of 128-row places), 1 issues the products, 4-7 and 8-11
 // are the two halves.  All waits are bounded: one that runs out raises the CTA's abort flag, every role falls through, copies in

@@ -5,7 +5,7 @@
 // Both are bound by memory: forward reads a row of the table and writes one of Y a token, backward reads dY and writes dE once.
 // The gradient's sums must not depend on the order of atomics, so the tokens are sorted (stable, so that a token's places are in
 // order) and every row of dE is summed by one group of threads, or, where a token's places cross from one run of the sorted
-// list to the next, from the runs' partial sums in order.  8 x 16384 tokens, 50000 rows of 768, bf16: 68 us forward, 267 backward (5.1 and
+// list to the next, from the runs' partial sums in order.  8 x 16384 tokens, 50000 rows of 768, bf16: 68 us forward, 266 backward (5.1 and
 // 5.4 TB/s of what has to move).
 #include "abs_pipeline.cuh"
 
