@@ -457,3 +457,46 @@ def test_scales_of_zero_and_below(ctx, dtype, scale):
     plan, o, lse = run_forward(ctx, b)
     check_forward(b, o, lse)
     check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "bf16"), (64, "f32")])
+def test_rows_far_apart(ctx, hd, dtype):
+    """Elements behind the 2^31-st of a tensor: the same bits as from rows that lie together."""
+    b = Batch([520, 30], 2, 1, hd, dtype, seed=35)
+    plan, o, lse = run_forward(ctx, b)
+    want = (o, *run_backward(ctx, b, plan, o, lse))
+    heads, apart = b.hq + 2 * b.hk, 1 << 22
+    far = torch.empty((b.total, apart), device="cuda", dtype=b.dtype)[:, -heads * hd:].unflatten(1, (heads, hd))
+    assert b.total * apart > 2 ** 31
+    far.copy_(b.fused.view(b.total, heads, hd))
+    views = far.split((b.hq, b.hk, b.hk), dim=1)
+    far_o = torch.empty((b.total, apart), device="cuda", dtype=b.dtype)[:, -b.hq * hd:].unflatten(1, (b.hq, hd))
+    ctx.abs_attention(*views, plan, far_o, lse, scale=b.scale)
+    grads = torch.empty((b.total, apart), device="cuda", dtype=b.dtype)[:, -heads * hd:].unflatten(1, (heads, hd)).split((b.hq, b.hk, b.hk), dim=1)
+    scratch = ctx.attention_scratch(b.total, b.hq, b.hk, hd, 2)
+    ctx.abs_attention_backward(b.do, *views, far_o, lse, plan, *grads, scratch, scale=b.scale)
+    for got, ref in zip((far_o, *grads), want):
+        assert torch.equal(got, ref)
+
+
+def test_calls_on_two_streams_at_once(ctx):
+    """Two batches' passes side by side, each with its own plan and scratch: the same bits as one after the other."""
+    batches = [Batch([1000, 300, 77] * 8, 6, 2, 64, "bf16", seed=36), Batch([700, 2048], 4, 4, 128, "bf16", seed=37)]
+    want, sides = [], [torch.cuda.Stream() for _ in batches]
+    for b in batches:
+        plan, o, lse = run_forward(ctx, b)
+        want.append((o, *run_backward(ctx, b, plan, o, lse)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        outs = [(b.outputs(), b.gradients(), ctx.attention_scratch(b.total, b.hq, b.hk, b.hd, len(b.lens))) for b in batches]
+        torch.cuda.synchronize()
+        for b, side, ((o, lse), grads, scratch) in zip(batches, sides, outs):
+            with torch.cuda.stream(side):
+                plan = ctx.attention_plan(b.offsets, b.total)
+                ctx.abs_attention(b.q, b.k, b.v, plan, o, lse, scale=b.scale)
+                ctx.abs_attention_backward(b.do, b.q, b.k, b.v, o, lse, plan, *grads, scratch, scale=b.scale)
+                got.append((plan, (o, *grads)))
+        torch.cuda.synchronize()
+        for (_, g), w in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(g, w))

@@ -145,3 +145,23 @@ def test_capture(ctx, rows):
         torch.cuda.synchronize()
         for m in range(2):                     # sums of ones are counts, exact
             assert torch.equal(dE[m, :, 0], torch.bincount(tokens[m].long(), minlength=600).float())
+
+
+@pytest.mark.parametrize("d,rows", [(64, 300), (13, 5000)])
+def test_rows_far_apart(ctx, d, rows):
+    """Elements behind the 2^31-st of a table: the same bits as from rows that lie together."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    vocab, apart = 520, 1 << 22
+    E = torch.randn((vocab, d), device="cuda", generator=gen)
+    far = torch.empty((vocab, apart), device="cuda")[:, -((d + 3) // 4 * 4):][:, :d]
+    far.copy_(E)
+    tokens = torch.randint(0, vocab, (rows,), device="cuda", generator=gen, dtype=torch.int32)
+    tokens[0] = vocab - 1
+    dy = torch.randn((rows, d), device="cuda", generator=gen)
+    got = []
+    for table in (E, far):
+        y = ctx.abs_embedding(table, tokens, torch.empty((rows, d), device="cuda"))
+        scratch = ctx.embedding_scratch(1, rows, vocab, d)
+        ctx.abs_embedding_backward(dy, tokens, table, scratch, scale=0.5, accumulate=True)
+        got.append((y, table))
+    assert all(torch.equal(p, q) for p, q in zip(*got))

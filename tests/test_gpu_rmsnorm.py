@@ -226,3 +226,21 @@ def test_capture(ctx):
         graph.replay()
         torch.cuda.synchronize()
         check_backward(dy, h, None, rstd, w, 10, dx, dw, gw)
+
+
+@pytest.mark.parametrize("d", [768, 77])
+def test_rows_far_apart(ctx, d):
+    """Elements behind the 2^31-st of a tensor: the same bits as from rows that lie together."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rows, apart = 520, 1 << 22
+    x = torch.randn((rows, d), device="cuda", generator=gen).bfloat16()
+    w = torch.rand(d, device="cuda", generator=gen)
+    far_x, far_y, far_dx = (torch.empty((rows, apart), device="cuda", dtype=torch.bfloat16)[:, -((d + 7) // 8 * 8):][:, :d] for _ in range(3))
+    far_x.copy_(x)
+    got = []
+    for a, y, dx in ((x, torch.empty_like(x), torch.empty_like(x)), (far_x, far_y, far_dx)):
+        rstd, dw = torch.empty((1, rows), device="cuda"), torch.empty((1, d), device="cuda")
+        ctx.abs_rms_norm(a, w, 1e-6, y, rstd=rstd)
+        ctx.abs_rms_norm_backward(y, a, rstd, w, dX=dx, dW=dw)
+        got.append((y, rstd, dx))
+    assert all(torch.equal(p, q) for p, q in zip(*got))
