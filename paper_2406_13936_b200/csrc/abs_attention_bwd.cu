@@ -637,10 +637,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
 #pragma unroll
           for (int c = 0; c < 64; c += 4) {
             const float4 l = lse[c / 4];
-            const float2 a = unpack2f(fma2f(pack2f(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), by2, pack2f(l.x, l.y)));
-            const float2 b = unpack2f(fma2f(pack2f(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), by2, pack2f(l.z, l.w)));
-            w[c / 2] = pack2f(exp2_approx(a.x), exp2_approx(a.y));
-            w[c / 2 + 1] = pack2f(exp2_approx(b.x), exp2_approx(b.y));
+            // (all on their unit: a quarter of them on the FMA pipe, as the forward pass does, is 1 % slower here)
+            w[c / 2] = exp2_pair(fma2f(pack2f(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), by2, pack2f(l.x, l.y)));
+            w[c / 2 + 1] = exp2_pair(fma2f(pack2f(__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])), by2, pack2f(l.z, l.w)));
           }
         }
         if (diagonal) {

@@ -358,12 +358,7 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               uint64_t y = fma2f(pack2f(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), by2, ref2);
-              if (e >= 16 - FwdShape<HD>::kFmaPairs) {
-                y = exp2_pair_fma(y);
-              } else {
-                const float2 a = unpack2f(y);
-                y = pack2f(exp2_approx(a.x), exp2_approx(a.y));
-              }
+              y = e >= 16 - FwdShape<HD>::kFmaPairs ? exp2_pair_fma(y) : exp2_pair(y);
               part[e & 1] = add2f(part[e & 1], y);
               const float2 a = unpack2f(y);
               w[e] = bf16_pair(a.x, a.y);

@@ -118,6 +118,10 @@ __device__ __forceinline__ float exp2_approx(float x) {          // within 2 ulp
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+  const float2 v = unpack2f(x);
+  return pack2f(exp2_approx(v.x), exp2_approx(v.y));
+}
 // 2^x of a pair on the FMA pipe, for some of the exponentials where the other unit (16 a clock and SM) is what bounds: x = n + f with n
 // the nearest whole number (Cody and Waite's reduction, exact for base 2), 2^f by a polynomial of degree 5 whose relative error is the
 // least possible on [-1/2, 1/2] (7.5e-8, found by Remez's exchange; 2.1e-7 with its roundings), and 2^n from its bits: adding 1.5 2^23 + 127
