@@ -500,3 +500,28 @@ def test_calls_on_two_streams_at_once(ctx):
         torch.cuda.synchronize()
         for (_, g), w in zip(got, want):
             assert all(torch.equal(x, y) for x, y in zip(g, w))
+
+
+@pytest.mark.parametrize("hd,dtype", [(64, "bf16"), (128, "bf16"), (40, "f32")])
+def test_heads_in_front_of_tokens_and_no_lse(ctx, hd, dtype):
+    """Tensors [heads][total][hd], forward with and without lse: the same bits as from [total][heads][hd]."""
+    b = Batch([140, 1, 300], 6, 3, hd, dtype, seed=38, front=1, tail=2)
+    plan, o, lse = run_forward(ctx, b)
+    want = (o, *run_backward(ctx, b, plan, o, lse))
+    by_head = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)  # noqa: E731
+    q, k, v, do = (by_head(t) for t in (b.q, b.k, b.v, b.do))
+    got_o = by_head(torch.full_like(o, 7.0))
+    ctx.abs_attention(q, k, v, plan, got_o, None, scale=b.scale)
+    grads = tuple(by_head(torch.full_like(t, 7.0)) for t in (q, k, v))
+    scratch = ctx.attention_scratch(b.total, b.hq, b.hk, hd, len(b.lens))
+    ctx.abs_attention_backward(do, q, k, v, got_o, lse, plan, *grads, scratch, scale=b.scale)
+    for got, ref in zip((got_o, *grads), want):
+        assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("hq,hk,hd", [(64, 1, 64), (96, 96, 8), (30, 10, 128)])
+def test_many_heads(ctx, hq, hk, hd):
+    b = Batch([129, 70], hq, hk, hd, "bf16", seed=39)
+    plan, o, lse = run_forward(ctx, b)
+    check_forward(b, o, lse)
+    check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
