@@ -604,9 +604,11 @@ int abs_plan_layer_norm_backward(abs_dtype dtype, int M, long long samples, long
  *               worker strides are ignored for M == 1).  R (the residual stream) and H (its new
  *               value) are NULL or of X's type.  H may be R or X, Y may be X (same strides each).
  *   Q, scales   NULL, or the rows in 8 bits (e4m3, one byte an element, strides in bytes) and
- *               [M][rows] fp32: scales = max_j |y_j| / 448 (1 for a row of zeros), Q = y / scales
- *               rounded to nearest.  Y may be NULL then.  A row with a NaN or an infinity gives
- *               NaN scales and NaN in Q.
+ *               [M][rows] fp32: scales = max_j |y_j| / 448 (1 for a row of zeros, for any other no
+ *               less than 2^-149), Q = y / scales rounded to nearest, at most 448 in magnitude (a
+ *               subnormal scale is a whole number of steps of 2^-149 and may be too small for its
+ *               row).  y is the value before its rounding to Y's type.  Y may be NULL then.  A row
+ *               with a NaN or an infinity among its y gives NaN scales and NaN in Q.
  *   weight      replica m at + m*param_stride (0: all replicas share it), or NULL (ones)
  *   rstd        [M][rows] fp32 for the backward pass, or NULL
  *   rows may be 0.  Sums and y are fp32; y is rounded once.                                     */

@@ -244,3 +244,53 @@ def test_rows_far_apart(ctx, d):
         ctx.abs_rms_norm_backward(y, a, rstd, w, dX=dx, dW=dw)
         got.append((y, rstd, dx))
     assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+LEAST = 2.0 ** -149                                  # the least positive fp32
+
+
+@pytest.mark.parametrize("d", [64, 258, 1021, 20000])
+@pytest.mark.parametrize("residual", [False, True])
+def test_8_bits_of_rows_of_very_small_values(ctx, d, residual):
+    """Largest values from 1 down to the least positive fp32, zeros beside them: with y as it was written, scales and Q are the
+    quotients in fp32, bit for bit, and a scale that would round to zero is the least positive number instead."""
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    tops = [1.0, 1e-30, 5e-36, 1.2e-36, 1e-36, 1e-37, 1e-39, 1e-41, 1e-42] + [k * LEAST for k in (1, 100, 223, 224, 225, 448, 700)]
+    M = len(tops)
+    x = 2.0 * torch.rand((M, 3, d), device="cuda", generator=gen) - 1.0
+    x[:, :, ::3] = 0.0
+    x[:, 2] = 0.0
+    r = torch.zeros_like(x) if residual else None
+    w = torch.tensor(tops, device="cuda", dtype=torch.float64).float()[:, None].expand(M, d).contiguous()
+    y, q = torch.empty_like(x), torch.empty((M, 3, d), device="cuda", dtype=torch.float8_e4m3fn)
+    s, h = torch.empty((M, 3), device="cuda"), torch.empty_like(x) if residual else None
+    ctx.abs_rms_norm(x, w, 1e-6, y, residual=r, summed=h, Q=q, scales=s)
+    top = y.abs().amax(2)
+    assert (top[:, :2] > 0).all()
+    want = (top.cpu() / 448.0).clamp_(min=LEAST).cuda()
+    want[top == 0] = 1.0
+    assert torch.equal(s, want)
+    scaled = (y.cpu() / want.cpu()[:, :, None]).clamp_(-448.0, 448.0)
+    assert torch.equal(q.cpu().float(), scaled.to(torch.float8_e4m3fn).float())
+
+
+@pytest.mark.parametrize("d", [64, 1021, 20000])
+def test_8_bits_of_small_bf16_rows(ctx, d):
+    """Subnormal bf16 rows with eps = 0 are of order one; with small weights they are finite, zeros stay zeros."""
+    gen = torch.Generator(device="cuda").manual_seed(d + 1)
+    x = torch.randn((1, 4, d), device="cuda", generator=gen).bfloat16()
+    x[:, :, 1::2] = 0.0
+    w = torch.full((1, d), 1e-37, device="cuda")
+    q, s = torch.empty((1, 4, d), device="cuda", dtype=torch.float8_e4m3fn), torch.empty((1, 4), device="cuda")
+    ctx.abs_rms_norm(x, w, 1e-6, None, Q=q, scales=s)
+    v = x.double()
+    want = v * (v.square().mean(2, keepdim=True) + 1e-6).rsqrt() * w.double()
+    got = q.double() * s.double()[:, :, None]
+    assert torch.isfinite(got).all() and (got[:, :, 1::2] == 0).all()
+    # the scale is a subnormal number of steps of 2^-149; half a step of e4m3 is 2^-4 of the value, below 2^-6 scales half of 2^-9; y is off by
+    # its own roundings and by a step of 2^-149
+    top = want.abs().amax(2, keepdim=True)
+    assert ((s.double() - top[:, :, 0] / 448).abs() <= LEAST + (d / 2 + 14) * U * top[:, :, 0] / 448).all()
+    lost = (want.abs() - 448 * s.double()[:, :, None]).clamp(min=0)                # (what a scale that was rounded down leaves out)
+    step = torch.maximum(want.abs() * 2.0 ** -4, s.double()[:, :, None] * 2.0 ** -10)
+    assert ((got - want).abs() <= step + lost + (d / 2 + 16) * U * want.abs() + 2 * LEAST).all()
