@@ -611,7 +611,7 @@ int abs_plan_layer_norm_backward(abs_dtype dtype, int M, long long samples, long
  *               with a NaN or an infinity among its y gives NaN scales and NaN in Q.
  *   weight      replica m at + m*param_stride (0: all replicas share it), or NULL (ones)
  *   rstd        [M][rows] fp32 for the backward pass, or NULL
- *   rows may be 0.  Sums and y are fp32; y is rounded once.                                     */
+ *   rows may be 0.  Sums and y are fp32; y is rounded once.  A row of zeros with eps = 0 is 0 / 0: NaN. */
 int abs_rms_norm(abs_ctx* ctx, const void* X, abs_dtype dtype, int M, long long rows, long long d,
                  long long x_row_stride, long long x_worker_stride, const void* R, long long r_row_stride,
                  long long r_worker_stride, void* H, long long h_row_stride, long long h_worker_stride,

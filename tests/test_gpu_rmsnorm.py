@@ -294,3 +294,14 @@ def test_8_bits_of_small_bf16_rows(ctx, d):
     lost = (want.abs() - 448 * s.double()[:, :, None]).clamp(min=0)                # (what a scale that was rounded down leaves out)
     step = torch.maximum(want.abs() * 2.0 ** -4, s.double()[:, :, None] * 2.0 ** -10)
     assert ((got - want).abs() <= step + lost + (d / 2 + 16) * U * want.abs() + 2 * LEAST).all()
+
+
+@pytest.mark.parametrize("d", [64, 77, 20000])
+def test_a_row_of_zeros_without_eps_is_nan(ctx, d):
+    """0 / 0: y, the scale and the row in 8 bits are NaN; its neighbours are as ever."""
+    x = torch.ones((1, 3, d), device="cuda")
+    x[0, 1] = 0.0
+    q, s, y = torch.empty(x.shape, device="cuda", dtype=torch.float8_e4m3fn), torch.empty((1, 3), device="cuda"), torch.empty_like(x)
+    ctx.abs_rms_norm(x, None, 0.0, y, Q=q, scales=s)
+    for t in (y, q.float(), s.unsqueeze(2)):
+        assert t[0, 1].isnan().all() and torch.isfinite(t[0, ::2]).all()
