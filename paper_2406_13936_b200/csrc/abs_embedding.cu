@@ -362,81 +362,85 @@ emb_sum_kernel(const EmbeddingGrad a, int width, int pieces, int sum_ctas) {
   pdl_wait();
   const int groups = blockDim.x / width;
   if (static_cast<int>(blockIdx.x) < sum_ctas) {
-    const int group = threadIdx.x / width, piece = blockIdx.y * width + threadIdx.x - group * width;
+    const int group = threadIdx.x / width;
     const long long job = static_cast<long long>(blockIdx.x) * groups + group;
-    if (group >= groups || job >= static_cast<long long>(a.M) * a.runs || piece >= pieces) return;
+    if (group >= groups || job >= static_cast<long long>(a.M) * a.runs) return;
     const int m = static_cast<int>(job / a.runs), run = static_cast<int>(job - static_cast<long long>(m) * a.runs);
     const long long base = static_cast<long long>(m) * a.rows;
     const unsigned *keys = a.key[a.sorted] + base, *places = a.pos[a.sorted] + base;
-    const int first = run * a.run, end = min(first + a.run, a.rows), c = piece * V;
-    const T* dy = static_cast<const T*>(a.dY) + m * a.dy_ws + c;
-    float* de = a.dE + m * a.e_ws + c;
-    float* part = a.part + job * 2 * a.d + c;
+    const int first = run * a.run, end = min(first + a.run, a.rows);
     const unsigned none = static_cast<unsigned>(a.vocab);
-    unsigned now = keys[first];
-    bool open = first > 0 && keys[first - 1] == now;      // the token began in a run before
-    float sum[V];
+    // (one turn, but for rows of more than 65535 blocks of columns)
+    for (int piece = blockIdx.y * width + threadIdx.x - group * width; piece < pieces; piece += gridDim.y * width) {
+      const int c = piece * V;
+      const T* dy = static_cast<const T*>(a.dY) + m * a.dy_ws + c;
+      float* de = a.dE + m * a.e_ws + c;
+      float* part = a.part + job * 2 * a.d + c;
+      unsigned now = keys[first];
+      bool open = first > 0 && keys[first - 1] == now;      // the token began in a run before
+      float sum[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = 0.f;
-    // kDeep rows at a time; the next ones' numbers are on their way while these are (8 x 16384 tokens: 2, 3, 4, 8 rows 275, 270, 267,
-    // 316 us, without looking ahead 283)
-    constexpr int kDeep = 4;
-    unsigned next[kDeep], place[kDeep];
-    auto look = [&](int i) {
+      for (int e = 0; e < V; ++e) sum[e] = 0.f;
+      // kDeep rows at a time; the next ones' numbers are on their way while these are (8 x 16384 tokens: 2, 3, 4, 8 rows 275, 270, 267,
+      // 316 us, without looking ahead 283)
+      constexpr int kDeep = 4;
+      unsigned next[kDeep], place[kDeep];
+      auto look = [&](int i) {
 #pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const bool in = i + u < end;
-        next[u] = in ? keys[i + u] : none;
-        place[u] = in ? places[i + u] : 0u;
-      }
-    };
-    look(first);
-    for (int i = first; i < end && now != none; i += kDeep) {
-      Raw raw[kDeep];
-      unsigned k[kDeep];
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        k[u] = next[u];
-        if (k[u] != none) raw[u] = __ldcs(reinterpret_cast<const Raw*>(dy + static_cast<long long>(place[u]) * a.dy_rs));
-      }
-      look(i + kDeep);
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        if (i + u >= end) continue;
-        if (k[u] != now) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            if (!open) sum[e] *= a.scale;
-          }
-          if (open) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) part[e] = sum[e];
-          } else if (now != none) {
-            store_sum<V>(a, de + now * a.e_rs, sum);
-          }
-          open = false;
-          now = k[u];
-#pragma unroll
-          for (int e = 0; e < V; ++e) sum[e] = 0.f;
+        for (int u = 0; u < kDeep; ++u) {
+          const bool in = i + u < end;
+          next[u] = in ? keys[i + u] : none;
+          place[u] = in ? places[i + u] : 0u;
         }
-        if (k[u] != none) {
-          float x[V];
-          widen<T, V>(raw[u], x);
+      };
+      look(first);
+      for (int i = first; i < end && now != none; i += kDeep) {
+        Raw raw[kDeep];
+        unsigned k[kDeep];
 #pragma unroll
-          for (int e = 0; e < V; ++e) sum[e] += x[e];
+        for (int u = 0; u < kDeep; ++u) {
+          k[u] = next[u];
+          if (k[u] != none) raw[u] = __ldcs(reinterpret_cast<const Raw*>(dy + static_cast<long long>(place[u]) * a.dy_rs));
+        }
+        look(i + kDeep);
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) {
+          if (i + u >= end) continue;
+          if (k[u] != now) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              if (!open) sum[e] *= a.scale;
+            }
+            if (open) {
+#pragma unroll
+              for (int e = 0; e < V; ++e) part[e] = sum[e];
+            } else if (now != none) {
+              store_sum<V>(a, de + now * a.e_rs, sum);
+            }
+            open = false;
+            now = k[u];
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] = 0.f;
+          }
+          if (k[u] != none) {
+            float x[V];
+            widen<T, V>(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += x[e];
+          }
         }
       }
-    }
-    if (now == none) return;
-    const bool on = end < a.rows && keys[end] == now;     // the token goes on in the next run
-    if (open || on) {
-      float* p = open ? part : part + a.d;
+      if (now == none) continue;
+      const bool on = end < a.rows && keys[end] == now;     // the token goes on in the next run
+      if (open || on) {
+        float* p = open ? part : part + a.d;
 #pragma unroll
-      for (int e = 0; e < V; ++e) p[e] = sum[e];
-    } else {
+        for (int e = 0; e < V; ++e) p[e] = sum[e];
+      } else {
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] *= a.scale;
-      store_sum<V>(a, de + now * a.e_rs, sum);
+        for (int e = 0; e < V; ++e) sum[e] *= a.scale;
+        store_sum<V>(a, de + now * a.e_rs, sum);
+      }
     }
     return;
   }
@@ -458,9 +462,9 @@ emb_sum_kernel(const EmbeddingGrad a, int width, int pieces, int sum_ctas) {
     present[v - v0] = lo < a.rows && keys[lo] == static_cast<unsigned>(v);
   }
   __syncthreads();
-  const int wide = V == 1 ? 1 : 4, count = a.d / wide;
-  for (int i = threadIdx.x; i < (v1 - v0) * count; i += blockDim.x) {
-    const int r = i / count, c = (i - r * count) * wide;
+  const unsigned wide = V == 1 ? 1 : 4, count = a.d / wide;        // (up to 2^31 elements)
+  for (unsigned i = threadIdx.x; i < (v1 - v0) * count; i += blockDim.x) {
+    const unsigned r = i / count, c = (i - r * count) * wide;
     if (present[r]) continue;
     float* p = a.dE + m * a.e_ws + static_cast<long long>(v0 + r) * a.e_rs + c;
     if (wide == 4) __stcs(reinterpret_cast<float4*>(p), make_float4(0.f, 0.f, 0.f, 0.f));
@@ -473,41 +477,44 @@ template <int V>
 __global__ void __launch_bounds__(kEmbThreads)
 emb_join_kernel(const EmbeddingGrad a, int width, int pieces) {
   pdl_wait();
-  const int groups = blockDim.x / width, group = threadIdx.x / width, piece = blockIdx.y * width + threadIdx.x - group * width;
+  const int groups = blockDim.x / width, group = threadIdx.x / width;
   const long long job = static_cast<long long>(blockIdx.x) * groups + group;
-  if (group >= groups || job >= static_cast<long long>(a.M) * a.runs || piece >= pieces) return;
+  if (group >= groups || job >= static_cast<long long>(a.M) * a.runs) return;
   const int m = static_cast<int>(job / a.runs), run = static_cast<int>(job - static_cast<long long>(m) * a.runs);
   const unsigned* keys = a.key[a.sorted] + static_cast<long long>(m) * a.rows;
-  const int first = run * a.run, end = min(first + a.run, a.rows), c = piece * V;
+  const int first = run * a.run, end = min(first + a.run, a.rows);
   if (end >= a.rows) return;
   const unsigned now = keys[end - 1];
   if (now == static_cast<unsigned>(a.vocab) || keys[end] != now) return;               // does not go on
   if (first > 0 && keys[first] == now && keys[first - 1] == now) return;                // did not start here
-  // the last run with the token: every run in between holds nothing else
-  const float* part = a.part + job * 2 * a.d + c;
-  float sum[V];
-  load_row<V>(part + a.d, sum);
-  part += 2 * a.d;
-  // (four runs at a time: a frequent token's are a long chain; what is loaded of runs that do not have it is not looked at)
-  bool on = true;
-  for (int r = run + 1; on && r < a.runs; r += 4, part += 8 * a.d) {
-    float x[4][V];
-    bool has[4];
+  for (int piece = blockIdx.y * width + threadIdx.x - group * width; piece < pieces; piece += gridDim.y * width) {
+    const int c = piece * V;
+    // the last run with the token: every run in between holds nothing else
+    const float* part = a.part + job * 2 * a.d + c;
+    float sum[V];
+    load_row<V>(part + a.d, sum);
+    part += 2 * a.d;
+    // (four runs at a time: a frequent token's are a long chain; what is loaded of runs that do not have it is not looked at)
+    bool on = true;
+    for (int r = run + 1; on && r < a.runs; r += 4, part += 8 * a.d) {
+      float x[4][V];
+      bool has[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      has[u] = r + u < a.runs && keys[(r + u) * a.run] == now;
-      if (r + u < a.runs) load_row<V>(part + u * 2 * a.d, x[u]);
+      for (int u = 0; u < 4; ++u) {
+        has[u] = r + u < a.runs && keys[(r + u) * a.run] == now;
+        if (r + u < a.runs) load_row<V>(part + u * 2 * a.d, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        on = on && has[u];
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[e] = on ? sum[e] + x[u][e] : sum[e];
+      }
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      on = on && has[u];
-#pragma unroll
-      for (int e = 0; e < V; ++e) sum[e] = on ? sum[e] + x[u][e] : sum[e];
-    }
+    for (int e = 0; e < V; ++e) sum[e] *= a.scale;
+    store_sum<V>(a, a.dE + m * a.e_ws + c + now * a.e_rs, sum);
   }
-#pragma unroll
-  for (int e = 0; e < V; ++e) sum[e] *= a.scale;
-  store_sum<V>(a, a.dE + m * a.e_ws + c + now * a.e_rs, sum);
 }
 
 struct DeviceGuardEmb {
@@ -593,7 +600,7 @@ int run_embedding(abs_ctx* ctx, const Embedding& a, cudaStream_t st) {
 template <typename T, int V>
 int run_sums(abs_ctx* ctx, const EmbeddingGrad& a, cudaStream_t st) {
   const int pieces = a.d / V, width = pieces < kEmbThreads ? pieces : kEmbThreads, groups = kEmbThreads / width;
-  const int cols = (pieces + width - 1) / width;
+  const int blocks = (pieces + width - 1) / width, cols = blocks < 65535 ? blocks : 65535;       // (the grid's second dimension)
   const int sum_ctas = static_cast<int>((static_cast<long long>(a.M) * a.runs + groups - 1) / groups);
   const int zero_ctas = a.accumulate ? 0 : a.M * ((a.vocab + kZeroRows - 1) / kZeroRows);
   if (sum_ctas + zero_ctas == 0) return ABS_OK;

@@ -165,3 +165,18 @@ def test_rows_far_apart(ctx, d, rows):
         ctx.abs_embedding_backward(dy, tokens, table, scratch, scale=0.5, accumulate=True)
         got.append((y, table))
     assert all(torch.equal(p, q) for p, q in zip(*got))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_widest_rows_of_odd_strides(ctx, accumulate):
+    """d = 2^24 in single elements: more blocks of columns than a grid has in its second dimension.  Whole numbers, so sums are exact."""
+    d, vocab = 1 << 24, 3
+    tokens = torch.tensor([[1, 0, 1, 5, 1]], dtype=torch.int32, device="cuda")
+    dy = torch.randint(-8, 9, (1, 5, d), device="cuda", generator=torch.Generator(device="cuda").manual_seed(5), dtype=torch.int32).float()
+    full = torch.full((1, vocab, d + 1), 7.0, device="cuda")
+    got = full[:, :, :d]
+    ctx.abs_embedding_backward(dy, tokens, got, ctx.embedding_scratch(1, 5, vocab, d), scale=2.0, accumulate=accumulate)
+    base = 7.0 if accumulate else 0.0
+    assert torch.equal(got[0, 0], base + 2.0 * dy[0, 1])
+    assert torch.equal(got[0, 1], base + 2.0 * (dy[0, 0] + dy[0, 2] + dy[0, 4]))
+    assert (got[0, 2] == base).all() and (full[:, :, d] == 7.0).all()
