@@ -95,8 +95,11 @@ const char* abs_last_error(const abs_ctx* ctx);
  * cluster and tcgen05 kernels issue no copies, abs_logreg_rounds_fused sends no
  * partial gradients and the tensor-core products of the MLP producer fill no
  * operand tile, so every wait runs out and the records come back flagged
- * ABS_STATUS_TIMEOUT; the Newton-Schulz products load nothing and their results are
- * NaN; nothing traps or hangs),
+ * ABS_STATUS_TIMEOUT; the Newton-Schulz products and the tensor-core attention kernels
+ * load nothing and their results are NaN; nothing traps or hangs),
+ * "attention_fault_stop_after" (fault injection for tests: in every other CTA of the
+ * tensor-core attention kernels the loads stop after so many steps, so that waits run out
+ * in the middle of a tile and in CTAs that depend on it; 0 = never),
  * "stats_cluster_rows" (target rows per CTA of the cluster kernel, 16..512),
  * "stats_no_cluster" (1 = do not split the rows of a batch over a thread-block
  * cluster when b > 256),

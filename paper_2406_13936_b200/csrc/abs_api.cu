@@ -189,6 +189,8 @@ extern "C" int abs_set_tuning(abs_ctx* ctx, const char* key, long long value) {
     ctx->tuning.stats_no_recheck = value ? 1 : 0;
   } else if (strcmp(key, "stats_fault_drop_loads") == 0) {
     ctx->tuning.stats_fault_drop_loads = value ? 1 : 0;
+  } else if (strcmp(key, "attention_fault_stop_after") == 0) {
+    ctx->tuning.attention_fault_stop_after = value;
   } else if (strcmp(key, "stats_cluster_rows") == 0) {
     if (value != 0 && (value < 16 || value > 512)) return set_error(ctx, ABS_ERR_INVALID_ARG, "stats_cluster_rows must be 0 or 16..512");
     ctx->tuning.stats_cluster_rows = value;

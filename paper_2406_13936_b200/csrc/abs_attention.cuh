@@ -104,6 +104,11 @@ inline AttnScratch attn_scratch(int total, int hq, int hk, int hd, int n) {
   return s;
 }
 
+inline uint32_t fault_steps(const abs_ctx* ctx) {
+  const long long n = ctx->tuning.attention_fault_stop_after;
+  return n > 0 && n < 0xffffffffll ? static_cast<uint32_t>(n) : 0xffffffffu;
+}
+
 int launch_attention_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st);          // bf16 rows of 16-byte pieces, scale > 0
 int launch_attention_tc_backward(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st);
 int launch_attention_any(abs_ctx* ctx, const AttnForward& a, abs_dtype dtype, cudaStream_t st);

@@ -77,7 +77,8 @@ struct BwdParams {
   float* partial;                             // [parts][dv, dk][hk][total][HD], laid out as sums; NULL: parts = 1
   float by, scale;                            // scale log2 e, scale
   long long limit;
-  int drop_loads;
+  int drop_loads;                             // test hooks, as the forward pass's; steps of blocks here
+  uint32_t stop_after;
   bool sectors;                               // whether dq, dk and dv are rows of whole sectors of 32 bytes
 };
 struct BwdItem {
@@ -202,7 +203,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kRegsLoad));
     if (warp == 0) {
       // ---- loads -----------------------------------------------------------------------------------
-      uint32_t lands = 0, tiles = 0, n = 0;                      // tiles and steps so far
+      uint32_t lands = 0, tiles = 0, n = 0, fills_q = 0, fills_do = 0, fills_st = 0;       // tiles and steps so far, and places filled
       bool ok = !p.drop_loads && *abort_flag == 0u;
       auto copy = [&](const CUtensorMap* map, uint32_t to, int head, int row, uint32_t bar) {
         if (elect_lane()) {
@@ -220,8 +221,9 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
       auto zero_behind = [&](const CUtensorMap* map, uint32_t to, const BwdItem& it, int head, int first) {
         expect(landed, kRows);
         copy(map, to, head, it.begin + first, landed);
-        ok = warp_wait(landed, lands & 1u, abort_flag, p.limit);
+        ok = warp_arrival(landed, lands & 1u, abort_flag, p.limit);
         ++lands;
+        if (!ok) return;
         for (uint32_t c = 0; c < HD / 64; ++c)
           for (uint32_t e = static_cast<uint32_t>(it.len - first) * 128u + lane * 16u; e < kBlock * 128u; e += 512u)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + c * (kBlock * 128u) + e), "r"(0u) : "memory");
@@ -234,7 +236,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           copy(map, to, head, it.begin + first, bar);
         } else {
           zero_behind(map, to, it, head, first);
-          if (lane == 0) mbar_arrive(bar);
+          if (ok && lane == 0) mbar_arrive(bar);
         }
       };
       // Tiles are taken in order by whoever is free, one ahead of the one whose rows are being fetched; after the last comes one without
@@ -275,6 +277,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 128u * e), "l"(at), "r"(row < it.len ? 4 : 0) : "memory");
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(st_full + 8u * s) : "memory");
+        ++fills_st;
       };
       take();
       if (ok) tell();
@@ -294,37 +297,42 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
           zero_behind(&maps.v, kvs + kRows, it, kv_head, it.tile * kBlock);
           if (ok) copy_rows(&maps.k, kvs, it, kv_head, it.tile * kBlock, kv_full + 8u * kv);
         }
+        if (!ok) break;
         ++tiles;
         for (int t = 0; t < it.steps && ok; ++t, ++n) {
           int head, block;
           bwd_step(p, it, t, head, block);
           const uint32_t qs = n % Sh::kQ, ds = n % Sh::kDo;
-          if (n >= Sh::kQ) ok = warp_wait(q_free + 8u * qs, (n / Sh::kQ - 1) & 1u, abort_flag, p.limit);
+          if (n >= p.stop_after && (blockIdx.x & 1u) == 0u) ok = false;
+          if (ok && n >= Sh::kQ) ok = warp_wait(q_free + 8u * qs, (n / Sh::kQ - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           copy_rows(&maps.q, q_at + qs * kRows, it, head, block * kBlock, q_full + 8u * qs);
-          if (ok) copy_stats(it, head, block);
+          if (!ok) break;
+          ++fills_q;
+          copy_stats(it, head, block);
           if (ok && n >= Sh::kDo) ok = warp_wait(do_free + 8u * ds, (n / Sh::kDo - 1) & 1u, abort_flag, p.limit);
           if (!ok) break;
           copy_rows(&maps.dout, do_at + ds * kRows, it, head, block * kBlock, do_full + 8u * ds);
+          if (!ok) break;
+          ++fills_do;
           if (t == 0) take();
           if (ok && (t == 1 || it.steps == 1)) tell();
         }
       }
       if (has_taken && lane == 0) *untold = taken;
       asm volatile("cp.async.wait_all;" ::: "memory");
-      // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.  (After an abort a place's last
-      // copy may be one further on than the count says: its wait may run out for nothing, which is bounded too.)
-      volatile unsigned ignore = 0u;
-      const bool stopped = *abort_flag != 0u;
+      // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.
       for (uint32_t k = 0; k < 2; ++k) {
         const uint32_t f_kv = k < Sh::kKv ? tiles / Sh::kKv + (k < tiles % Sh::kKv ? 1u : 0u) : 0u;
-        const uint32_t f_q = n / Sh::kQ + (k < n % Sh::kQ ? 1u : 0u);
-        const uint32_t f_do = k < Sh::kDo ? n / Sh::kDo + (k < n % Sh::kDo ? 1u : 0u) : 0u;
-        if (f_kv > 0) mbar_wait(kv_full + 8u * k, (f_kv - 1) & 1u, &ignore, p.limit);
-        if (f_q > 0) mbar_wait(q_full + 8u * k, (f_q - 1) & 1u, &ignore, p.limit);
-        if (f_do > 0) mbar_wait(do_full + 8u * k, (f_do - 1) & 1u, &ignore, p.limit);
+        const uint32_t f_q = fills_q / Sh::kQ + (k < fills_q % Sh::kQ ? 1u : 0u);
+        const uint32_t f_do = k < Sh::kDo ? fills_do / Sh::kDo + (k < fills_do % Sh::kDo ? 1u : 0u) : 0u;
+        if (f_kv > 0) warp_arrival(kv_full + 8u * k, (f_kv - 1) & 1u, abort_flag, p.limit);
+        if (f_q > 0) warp_arrival(q_full + 8u * k, (f_q - 1) & 1u, abort_flag, p.limit);
+        const uint32_t f_st = fills_st / 2 + (k < fills_st % 2 ? 1u : 0u);
+        if (f_do > 0) warp_arrival(do_full + 8u * k, (f_do - 1) & 1u, abort_flag, p.limit);
+        if (f_st > 0) warp_arrival(st_full + 8u * k, (f_st - 1) & 1u, abort_flag, p.limit);
       }
-      if (stopped) mbar_wait(q_full + 8u * (n % Sh::kQ), (n / Sh::kQ) & 1u, &ignore, 1000000);
+      if (lands > 0) warp_arrival(landed, (lands - 1) & 1u, abort_flag, p.limit);
     } else if (warp == 1) {
       // ---- products --------------------------------------------------------------------------------
       constexpr uint32_t idesc_s = mma_idesc(kBlock, kBlock, false, false), idesc_k = mma_idesc(kBlock, HD, false, true),
@@ -842,7 +850,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
                     reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.total, a.hq, a.hk,
                     parts, a.hd, l.bwd_cap, all, group, reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
-                    ctx->tuning.stats_fault_drop_loads ? 1 : 0,
+                    ctx->tuning.stats_fault_drop_loads ? 1 : 0, fault_steps(ctx),
                     in_sectors(a.dq, a.hd) && in_sectors(a.dk, a.hd) && in_sectors(a.dv, a.hd)};
   const long long most = static_cast<long long>(l.bwd_cap) * all;
   cudaLaunchConfig_t cfg = {};

@@ -58,6 +58,7 @@ struct FwdParams {
   long long limit;
   bool sectors;                               // whether O is rows of whole sectors of 32 bytes
   int drop_loads;                             // test hook: nothing is loaded, so every wait must run out
+  uint32_t stop_after;                        // test hook: no more than so many keys' and values' places are filled by CTAs of even numbers
 };
 struct FwdItem {
   int begin, len, row, head, kv, n0, n1;      // row: the tile's first in the sequence; n0, n1: steps of its halves
@@ -146,6 +147,7 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         for (int j = 0; j < 2 * steps && ok; ++j, ++n) {
           const uint32_t s = n % kPlaces, pass = n / kPlaces, to = ring + s * kRows;
           if (pass > 0) ok = warp_wait(freed + 8u * s, (pass - 1) & 1u, abort_flag, p.limit);
+          if (n >= p.stop_after && (blockIdx.x & 1u) == 0u) ok = false;
           if (!ok) break;
           const int key = (j >> 1) * kHalf, in = it.len - key;                   // rows of the sequence from the step's first key on
           if ((j & 1) == 0) {
@@ -155,8 +157,9 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
           } else {
             // rows of V behind the sequence have weights of zero, but may hold anything: zeros in their place
             copy(&maps.v, to, it.kv, it.begin + key, landed);
-            ok = warp_wait(landed, lands & 1u, abort_flag, p.limit);
+            ok = warp_arrival(landed, lands & 1u, abort_flag, p.limit);
             ++lands;
+            if (!ok) break;
             for (uint32_t c = 0; c < HD / 64; ++c)
               for (uint32_t e = static_cast<uint32_t>(in) * 128u + lane * 16u; e < kHalf * 128u; e += 512u)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + c * (kHalf * 128u) + e), "r"(0u) : "memory");
@@ -167,13 +170,13 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         }
       }
       // Waits (bounded) until every copy that was issued has arrived, whatever made the other roles stop.
-      volatile unsigned ignore = 0u;
       for (uint32_t s = 0; s < kPlaces; ++s) {
         const uint32_t fills = n / kPlaces + (s < n % kPlaces ? 1u : 0u);
-        if (fills > 0) mbar_wait(full + 8u * s, (fills - 1) & 1u, &ignore, p.limit);
+        if (fills > 0) warp_arrival(full + 8u * s, (fills - 1) & 1u, abort_flag, p.limit);
       }
       for (uint32_t t = 0; t < 2; ++t)
-        if (uses[t] > 0) mbar_wait(q_full + 8u * t, (uses[t] - 1) & 1u, &ignore, p.limit);
+        if (uses[t] > 0) warp_arrival(q_full + 8u * t, (uses[t] - 1) & 1u, abort_flag, p.limit);
+      if (lands > 0) warp_arrival(landed, (lands - 1) & 1u, abort_flag, p.limit);
     } else if (warp == 1) {
       // ---- products --------------------------------------------------------------------------------
       constexpr uint32_t idesc_s = mma_idesc(kHalf, kHalf, false, false), idesc_o = mma_idesc(kHalf, HD, false, true);
@@ -413,7 +416,7 @@ int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
   const AttnPlanLayout l = attn_plan_layout(a.n, a.total);
   const FwdParams p{a.o, a.lse, a.plan, a.plan + l.fwd, a.total, a.hq, a.hq / a.hk, a.hd, a.scale * kLog2eF,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
-                    in_sectors(a.o, a.hd), ctx->tuning.stats_fault_drop_loads ? 1 : 0};
+                    in_sectors(a.o, a.hd), ctx->tuning.stats_fault_drop_loads ? 1 : 0, fault_steps(ctx)};
   auto kern = attn_forward_kernel<HD>;
   const size_t smem = FwdShape<HD>::kSmem;
   ABS_CUDA_TRY(ctx, ensure_dynamic_smem(ctx, kern, smem));

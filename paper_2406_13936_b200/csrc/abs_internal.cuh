@@ -37,6 +37,7 @@ struct Tuning {
   long long ns_pair_tiles = 0;             // Newton-Schulz products: 1 single-CTA tiles, 2 CTA-pair tiles
   long long ns_max_cluster = 0;            // Newton-Schulz of small matrices: 8..16, no larger clusters than that
   long long stats_fault_drop_loads = 0;    // test hook: the tiled kernel's loader issues no copies
+  long long attention_fault_stop_after = 0;  // test hook: every other CTA's loader of the attention kernels stops after so many steps (0: none)
 };
 
 // What the launchers remember per kernel function, so that a call does not repeat host-side runtime

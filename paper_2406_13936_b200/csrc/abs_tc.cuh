@@ -169,6 +169,16 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
 }
 
+// The same for copies that were issued: no other role's abort ends it, since they write to shared memory that must still be this CTA's.  One
+// that does run out raises the abort flag.
+__device__ __forceinline__ bool warp_arrival(uint32_t bar, uint32_t parity, volatile unsigned* abort_flag, long long limit) {
+  bool here = mbar_try_wait(bar, parity);
+  for (const long long t0 = clock64(); !here && clock64() - t0 <= limit;) here = mbar_try_wait(bar, parity);
+  here = __all_sync(0xffffffffu, here);
+  if (!here) *abort_flag = 1u;
+  return here;
+}
+
 // Operand descriptors without the address (in units of 16 bytes): 128-byte swizzled rows, version 1 (bit 46), swizzle mode 2 (bits
 // 61-63).  K-major: a row is 64 values of k, groups of 8 rows 1024 bytes apart; 16 values of k are 32 bytes.  MN-major: a row is
 // 64 columns at one value of k, groups of 8 values of k 1024 bytes apart (stride offset), further blocks of 64 columns `block`

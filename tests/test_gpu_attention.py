@@ -525,3 +525,36 @@ def test_many_heads(ctx, hq, hk, hd):
     plan, o, lse = run_forward(ctx, b)
     check_forward(b, o, lse)
     check_backward(b, o, lse, *run_backward(ctx, b, plan, o, lse))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 5, 10])
+@pytest.mark.parametrize("lens,hd,hq,hk", [([300, 0, 1, 700, 129, 64, 1500, 17], 64, 6, 2), ([300, 0, 1, 700, 129, 64, 1500, 17], 128, 6, 2),
+                                           ([5, 131, 400] * 200, 64, 2, 2), ([5, 131, 400] * 200, 128, 2, 2), ([2000, 1100], 64, 4, 1),
+                                           ([2000, 1100], 128, 4, 1)])
+def test_loads_that_stop_in_the_middle(ctx, lens, hd, hq, hk, steps):
+    """Every other CTA's loads stop after some steps: waits run out in the middle of tiles, and in CTAs that wait for such a tile's part of dq
+    while their own copies, whole and partial blocks', are under way.  What is not NaN has the undisturbed calls' bits, and the next
+    calls are right.  (Groups of heads in parts and whole; one to sixteen tiles of keys a sequence.)"""
+    b = Batch(lens, hq, hk, hd, "bf16", seed=40, front=1, tail=2)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    ctx.set_tuning("stats_timeout_cycles", 200000)
+    ctx.set_tuning("attention_fault_stop_after", steps)
+    try:
+        _, some_o, some_lse = run_forward(ctx, b)
+        some_grads = run_backward(ctx, b, plan, o, lse)
+        torch.cuda.synchronize()
+    finally:
+        ctx.set_tuning("attention_fault_stop_after", 0)
+        ctx.set_tuning("stats_timeout_cycles", 0)
+    inside = ~b.outside()
+    lost = 0
+    for got, want in ((some_o, o), (some_lse.t(), lse.t()), *zip(some_grads, grads)):
+        nan = torch.isnan(got)
+        assert torch.equal(got[~nan], want[~nan]) and (got[~inside] == 7.0).all()
+        lost += nan.sum().item()
+    assert lost > 0
+    again_o, again_lse = run_forward(ctx, b)[1:]
+    assert torch.equal(again_o, o) and torch.equal(again_lse, lse)
+    for g, want in zip(run_backward(ctx, b, plan, o, lse), grads):
+        assert torch.equal(g, want)
