@@ -316,7 +316,10 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
         const float most = max3f(max3f(top[0], top[1], top[2]), top[3], top[3]) * p.by;
         // the products of the step before, which read P and add to O (with P over S they came before this S)
         if (HD == 64 && steps_done > 0) ok = warp_wait(pv_done + 8u * t, (steps_done - 1) & 1u, abort_flag, p.limit);
-        if (!ok) break;
+        if (!ok) {
+          tmem_loaded(s[0]);                                       // (the load ahead: its registers are somebody else's from here on)
+          break;
+        }
         tc_fence_after();
         // (rows behind the sequence, which may hold anything, have no say, and a row's reference depends on that row alone)
         const bool raise = live && most > m + kRaise;
