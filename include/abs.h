@@ -665,6 +665,7 @@ typedef struct {
  * below its predecessor is raised to it, which sets the plan's third int32 to 1 (else 0).  plan: device memory of
  * abs_attention_plan_bytes, 16-byte aligned.  A plan for other offsets of as many sequences and the same total may be written over it, also
  * between replays of a graph that captured the calls that read it.
+ * A call with a plan of another number of sequences or another total gives NaN in all rows of its outputs.
  * sequences <= 2^24, total <= 2^30.                                                                  */
 int abs_attention_plan_bytes(int sequences, long long total, size_t* out);
 int abs_attention_plan(abs_ctx* ctx, const int* offsets, int sequences, long long total, void* plan, size_t plan_bytes,

@@ -114,6 +114,7 @@ attn_plan_kernel(const int* __restrict__ offsets, int n, int total, AttnPlanLayo
     plan[kPlanBwdTiles] = tiles;
     plan[kPlanBad] = bad;
     plan[kPlanTotal] = total;
+    plan[kPlanSequences] = n;
   }
 }
 

@@ -21,7 +21,7 @@ struct AttnPlanLayout {
   long long fwd, bwd, starts, counts, words;   // places of the parts, and their end
   int fwd_cap, bwd_cap, bins;
 };
-enum { kPlanFwdTiles = 0, kPlanBwdTiles = 1, kPlanBad = 2, kPlanTotal = 3, kPlanHeader = 16 };
+enum { kPlanFwdTiles = 0, kPlanBwdTiles = 1, kPlanBad = 2, kPlanTotal = 3, kPlanSequences = 4, kPlanHeader = 16 };
 inline AttnPlanLayout attn_plan_layout(int n, int total) {
   AttnPlanLayout l;
   l.fwd_cap = total / kAttnFwdRows + n;
@@ -45,6 +45,19 @@ struct AttnOut {
   void* p;
   long long row, head;
 };
+#ifdef __CUDACC__
+// Whether the plan was made for the call's numbers: where its records lie depends on them, and what they say are rows.
+__device__ __forceinline__ bool plan_fits(const int* plan, int n, int total) {
+  return __ldg(plan + kPlanTotal) == total && __ldg(plan + kPlanSequences) == n;
+}
+// Every row of every head, NaN: what a plan that does not fit gives.  The caller is warp `at` of `step`.
+template <typename T>
+__device__ __forceinline__ void fill_nan(const AttnOut& o, int total, int heads, int hd, int at, int step) {
+  for (long long row = at; row < total; row += step)
+    for (int head = 0; head < heads; ++head)
+      for (int c = threadIdx.x & 31; c < hd; c += 32) static_cast<T*>(o.p)[row * o.row + head * o.head + c] = static_cast<T>(__int_as_float(0x7fc00000));
+}
+#endif
 // Whether every row of every head is whole sectors of 32 bytes of a 16-bit type.
 inline bool in_sectors(const AttnOut& o, int hd) {
   return reinterpret_cast<uintptr_t>(o.p) % 32 == 0 && o.row % 16 == 0 && o.head % 16 == 0 && hd % 16 == 0;

@@ -32,6 +32,10 @@ __device__ __forceinline__ TileRec tile_rec(const int* p, int i) {
   return {r.x, r.y, r.z};
 }
 
+// Warps of the CTAs of the grid's first row.
+__device__ __forceinline__ int warp_of_row() { return blockIdx.x * (kThreadsA / 32) + threadIdx.x / 32; }
+__device__ __forceinline__ int warps_of_row() { return gridDim.x * (kThreadsA / 32); }
+
 // Rows [row0, row0 + 64) of one head into shared memory, zeros from `end` on and behind the head's width.
 template <typename T, int HDP>
 __device__ __forceinline__ void load_rows(float* to, const AttnRows& t, int head, int row0, int end, int hd) {
@@ -110,6 +114,12 @@ attn_any_forward_kernel(const AttnForward a, const int* tiles) {
   constexpr int kParts = kAttnFwdRows / kT;
   pdl_wait();
   const int tile = blockIdx.x / kParts, part = blockIdx.x % kParts, head = blockIdx.y;
+  if (!plan_fits(a.plan, a.n, a.total)) {
+    if (head > 0) return;
+    fill_nan<T>(a.o, a.total, a.hq, a.hd, warp_of_row(), warps_of_row());
+    if (a.lse) fill_nan<float>({a.lse, 1, a.total}, a.total, a.hq, 1, warp_of_row(), warps_of_row());
+    return;
+  }
   if (tile >= a.plan[kPlanFwdTiles]) return;
   const TileRec rec = tile_rec(tiles, tile);
   const int row0 = rec.begin + rec.block * kAttnFwdRows + part * kT;
@@ -220,6 +230,12 @@ attn_any_keys_kernel(const AttnBackward a, const int* tiles) {
   constexpr int kParts = kAttnBwdRows / kT;
   pdl_wait();
   const int tile = blockIdx.x / kParts, part = blockIdx.x % kParts, kv = blockIdx.y;
+  if (!plan_fits(a.plan, a.n, a.total)) {
+    if (kv > 0) return;
+    fill_nan<T>(a.dk, a.total, a.hk, a.hd, warp_of_row(), warps_of_row());
+    fill_nan<T>(a.dv, a.total, a.hk, a.hd, warp_of_row(), warps_of_row());
+    return;
+  }
   if (tile >= a.plan[kPlanBwdTiles]) return;
   const TileRec rec = tile_rec(tiles, tile);
   const int k0 = rec.begin + rec.block * kAttnBwdRows + part * kT;
@@ -259,6 +275,11 @@ attn_any_queries_kernel(const AttnBackward a, const int* tiles) {
   constexpr int kParts = kAttnFwdRows / kT;
   pdl_wait();
   const int tile = blockIdx.x / kParts, part = blockIdx.x % kParts, head = blockIdx.y;
+  if (!plan_fits(a.plan, a.n, a.total)) {
+    if (head > 0) return;
+    fill_nan<T>(a.dq, a.total, a.hq, a.hd, warp_of_row(), warps_of_row());
+    return;
+  }
   if (tile >= a.plan[kPlanFwdTiles]) return;
   const TileRec rec = tile_rec(tiles, tile);
   const int q0 = rec.begin + rec.block * kAttnFwdRows + part * kT;

@@ -71,7 +71,7 @@ struct BwdParams {
   unsigned* counters;                         // [hq][cap][HD / 64], then the next tile that nobody has
   const int* plan;
   const int* tiles;
-  int total, hq, hk, parts, hd, cap;
+  int n, total, hq, hk, parts, hd, cap;
   // A key head's group of query heads in `parts` of `group` heads, each a head of its own in the list of tiles, `heads` in all.
   int heads, group;
   float* partial;                             // [parts][dv, dk][hk][total][HD], laid out as sums; NULL: parts = 1
@@ -184,7 +184,7 @@ attn_backward_kernel(const __grid_constant__ BwdMaps maps, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int items = __ldg(p.plan + kPlanBwdTiles) * p.heads;
+  const int items = plan_fits(p.plan, p.n, p.total) ? __ldg(p.plan + kPlanBwdTiles) * p.heads : 0;
   unsigned* next_item = p.counters + static_cast<long long>(p.hq) * p.cap * Sh::kHalves;
   // The CTA's k-th tile; false: there is none (or a wait ran out).  last: whether this role is done with the place in the ring.
   auto read_item = [&](uint32_t k) {
@@ -762,7 +762,7 @@ __global__ void __launch_bounds__(kBlock)
 attn_join_kernel(const BwdParams p) {
   pdl_wait();
   const int tile = blockIdx.x, kv = blockIdx.y, r = threadIdx.x;
-  if (tile >= __ldg(p.plan + kPlanBwdTiles)) return;
+  if (!plan_fits(p.plan, p.n, p.total) || tile >= __ldg(p.plan + kPlanBwdTiles)) return;
   const int4 rec = __ldg(reinterpret_cast<const int4*>(p.tiles) + tile);
   const int row = rec.z * kBlock + r, rows = min(32, rec.y - rec.x - rec.z * kBlock - (r & ~31));
   if (row >= rec.y - rec.x) return;
@@ -785,13 +785,21 @@ attn_join_kernel(const BwdParams p) {
 }
 
 // -lse log2 e and -delta of every row and head, and the counters' start: LANES threads a row and head, 16 bytes each, four of these at
-// a time; 32 rows of one head before the next head's, so that what is written are whole sectors.
+// a time; 32 rows of one head before the next head's, so that what is written are whole sectors.  With a plan of another batch, NaN in all
+// results instead: the kernels behind this one find nothing to do.
 template <int LANES>
 __global__ void __launch_bounds__(256)
 attn_backward_start_kernel(const AttnBackward a, float* stats, unsigned* counters, long long n_counters) {
   constexpr int kRowsOf = 256 / LANES, kUnroll = 4;
   pdl_wait();
   for (long long c = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; c < n_counters; c += static_cast<long long>(gridDim.x) * 256) counters[c] = 0u;
+  if (!plan_fits(a.plan, a.n, a.total)) {
+    const int at = blockIdx.x * 8 + threadIdx.x / 32, step = gridDim.x * 8;
+    fill_nan<__nv_bfloat16>(a.dq, a.total, a.hq, a.hd, at, step);
+    fill_nan<__nv_bfloat16>(a.dk, a.total, a.hk, a.hd, at, step);
+    fill_nan<__nv_bfloat16>(a.dv, a.total, a.hk, a.hd, at, step);
+    return;
+  }
   const int lane = threadIdx.x % LANES, c = lane * 8;
   uint4 x[kUnroll], y[kUnroll];
   long long at[kUnroll];
@@ -847,7 +855,7 @@ int run_backward_tc(abs_ctx* ctx, const AttnBackward& a, cudaStream_t st) {
                                      reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<unsigned*>(mem + s.counters), counters));
   const int parts = attn_parts(a.total, a.hq, a.hk, a.n), group = a.hq / a.hk / parts, all = a.hk * parts;
   const BwdParams p{a.dq, a.dk, a.dv, reinterpret_cast<float*>(mem + s.delta), reinterpret_cast<float*>(mem + s.sums),
-                    reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.total, a.hq, a.hk,
+                    reinterpret_cast<unsigned*>(mem + s.counters), a.plan, a.plan + l.bwd, a.n, a.total, a.hq, a.hk,
                     parts, a.hd, l.bwd_cap, all, group, reinterpret_cast<float*>(mem + s.partial), a.scale * kLog2eB, a.scale,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
                     ctx->tuning.stats_fault_drop_loads ? 1 : 0, fault_steps(ctx),

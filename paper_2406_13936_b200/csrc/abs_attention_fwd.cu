@@ -53,7 +53,7 @@ struct FwdParams {
   float* lse;
   const int* plan;
   const int* tiles;
-  int total, hq, group, hd;
+  int n, total, hq, group, hd;
   float by;                                   // scale log2 e
   long long limit;
   bool sectors;                               // whether O is rows of whole sectors of 32 bytes
@@ -116,7 +116,7 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_wait();
-  const int items = __ldg(p.plan + kPlanFwdTiles) * p.hq;
+  const int items = plan_fits(p.plan, p.n, p.total) ? __ldg(p.plan + kPlanFwdTiles) * p.hq : 0;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
@@ -408,6 +408,11 @@ attn_forward_kernel(const __grid_constant__ FwdMaps maps, const FwdParams p) {
     tc_fence_after();
     tmem_free_all(tmem);
   }
+  if (items == 0 && !plan_fits(p.plan, p.n, p.total)) {
+    const int at = blockIdx.x * (kThreadsF / 32) + warp, step = gridDim.x * (kThreadsF / 32);
+    fill_nan<__nv_bfloat16>(p.o, p.total, p.hq, p.hd, at, step);
+    if (p.lse) fill_nan<float>({p.lse, 1, p.total}, p.total, p.hq, 1, at, step);
+  }
 }
 
 template <int HD>
@@ -417,7 +422,7 @@ int run_forward_tc(abs_ctx* ctx, const AttnForward& a, cudaStream_t st) {
       !encode_heads_map(a.v, a.total, a.hk, a.hd, &maps.v))
     return set_error(ctx, ABS_ERR_CUDA, "cuTensorMapEncodeTiled (%d rows, head_dim %d) failed", a.total, a.hd);
   const AttnPlanLayout l = attn_plan_layout(a.n, a.total);
-  const FwdParams p{a.o, a.lse, a.plan, a.plan + l.fwd, a.total, a.hq, a.hq / a.hk, a.hd, a.scale * kLog2eF,
+  const FwdParams p{a.o, a.lse, a.plan, a.plan + l.fwd, a.n, a.total, a.hq, a.hq / a.hk, a.hd, a.scale * kLog2eF,
                     ctx->tuning.stats_timeout_cycles ? ctx->tuning.stats_timeout_cycles : kDefaultTimeoutCycles,
                     in_sectors(a.o, a.hd), ctx->tuning.stats_fault_drop_loads ? 1 : 0, fault_steps(ctx)};
   auto kern = attn_forward_kernel<HD>;

@@ -558,3 +558,30 @@ def test_loads_that_stop_in_the_middle(ctx, lens, hd, hq, hk, steps):
     assert torch.equal(again_o, o) and torch.equal(again_lse, lse)
     for g, want in zip(run_backward(ctx, b, plan, o, lse), grads):
         assert torch.equal(g, want)
+
+
+@pytest.mark.parametrize("hd,dtype,hq,hk", [(64, "bf16", 6, 2), (128, "bf16", 2, 2), (64, "f32", 4, 2), (24, "bf16", 3, 3)])
+@pytest.mark.parametrize("change", ["sequences", "total", "zeros", "words"])
+def test_a_plan_of_another_batch_gives_nan(ctx, hd, dtype, hq, hk, change):
+    """Nothing of such a plan but its header is looked at."""
+    b = Batch([300, 5, 200], hq, hk, hd, dtype, seed=41, front=1, tail=2, pad=1 if hd == 24 else 0)
+    plan, o, lse = run_forward(ctx, b)
+    grads = run_backward(ctx, b, plan, o, lse)
+    n = len(b.lens)
+    words = plan.words.clone()
+    if change == "sequences":
+        words = ctx.attention_plan(torch.tensor([1, 301, 306], dtype=torch.int32, device="cuda"), b.total).words
+    elif change == "total":
+        words = ctx.attention_plan(b.offsets, b.total + 1).words
+    elif change == "zeros":
+        words.zero_()
+    elif change == "words":
+        words = torch.randint(-2 ** 31, 2 ** 31 - 1, words.shape, device="cuda", dtype=torch.int32)
+    other = pkg.AttentionPlan(words, n, b.total)
+    wrong_o, wrong_lse = run_forward(ctx, b, plan=other)[1:]
+    for t in (wrong_o, wrong_lse, *run_backward(ctx, b, other, o, lse)):
+        assert torch.isnan(t).all()
+    again_o, again_lse = run_forward(ctx, b, plan=plan)[1:]
+    assert torch.equal(again_o, o) and torch.equal(again_lse, lse)
+    for g, want in zip(run_backward(ctx, b, plan, o, lse), grads):
+        assert torch.equal(g, want)
