@@ -261,8 +261,7 @@ extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const a
   DeviceGuardAttn guard(ctx->device);
   if (!guard.ok) return set_error(ctx, ABS_ERR_CUDA, "cannot select device %d", ctx->device);
   const AttnBackward a{rows_of(dO), rows_of(Q), rows_of(K), rows_of(V), rows_of(O), lse, static_cast<const int*>(plan), out_of(dQ),
-                       out_of(dK), out_of(dV), sequences, static_cast<int>(total), q_heads, kv_heads, head_dim, scale, scratch,
-                       scratch_bytes};
+                       out_of(dK), out_of(dV), sequences, static_cast<int>(total), q_heads, kv_heads, head_dim, scale, scratch};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   bool tc = dtype == ABS_BF16 && head_dim % 8 == 0;
   for (const auto& x : all) tc = tc && tc_tensor(x.t);

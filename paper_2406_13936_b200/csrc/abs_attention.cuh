@@ -79,7 +79,6 @@ struct AttnBackward {
   int n, total, hq, hk, hd;
   float scale;
   void* scratch;
-  size_t scratch_bytes;
 };
 
 // Into how many parts the tensor-core kernel's backward pass splits a group's query heads: a key tile and head is one CTA's work for all
