@@ -671,7 +671,7 @@ int abs_attention_plan_bytes(int sequences, long long total, size_t* out);
 int abs_attention_plan(abs_ctx* ctx, const int* offsets, int sequences, long long total, void* plan, size_t plan_bytes,
                        void* stream);
 
-/* lse: fp32 [q_heads][total], or NULL.  O overlaps no input.  q_heads <= 4096, total * q_heads <= 2^32 and
+/* lse: fp32 [q_heads][total], or NULL.  O overlaps no input.  |scale| < 2e38.  q_heads <= 4096, total * q_heads <= 2^32 and
  * sequences * q_heads <= 2^28.  The tensor-core kernels' waits are bounded ("stats_timeout_cycles"): rows whose tile a wait
  * that ran out left unfinished are NaN.                                                              */
 int abs_attention(abs_ctx* ctx, const abs_heads* Q, const abs_heads* K, const abs_heads* V, abs_dtype dtype, const void* plan,

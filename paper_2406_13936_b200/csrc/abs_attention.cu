@@ -146,6 +146,9 @@ int validate_heads(abs_ctx* ctx, int sequences, long long total, int q_heads, in
                      head_dim, q_heads, total, sequences);
   return ABS_OK;
 }
+int validate_scale(abs_ctx* ctx, float scale) {       // (the kernels take it log2 e times)
+  return scale > -2.0e38f && scale < 2.0e38f ? ABS_OK : set_error(ctx, ABS_ERR_INVALID_ARG, "scale must be within 2e38 of zero");
+}
 // Rows are disjoint from one another: a token's heads lie within its row (stride of tokens the larger) or a head's tokens within
 // the head's block.
 int validate_tensor(abs_ctx* ctx, const char* what, const abs_heads* t, long long total, int heads, int head_dim) {
@@ -218,7 +221,7 @@ extern "C" int abs_attention(abs_ctx* ctx, const abs_heads* Q, const abs_heads* 
   int rc = validate_sequences(ctx, sequences, total);
   if (rc == ABS_OK) rc = validate_heads(ctx, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
-  if (!(scale > -3.0e38f && scale < 3.0e38f)) return set_error(ctx, ABS_ERR_INVALID_ARG, "scale must be finite");
+  if ((rc = validate_scale(ctx, scale)) != ABS_OK) return rc;
   if (total == 0 || sequences == 0) return ABS_OK;
   if (plan == nullptr || (reinterpret_cast<uintptr_t>(plan) & 15u)) return set_error(ctx, ABS_ERR_INVALID_ARG, "plan is null or not 16-byte aligned");
   if ((rc = validate_tensor(ctx, "Q", Q, total, q_heads, head_dim)) != ABS_OK) return rc;
@@ -245,7 +248,7 @@ extern "C" int abs_attention_backward(abs_ctx* ctx, const abs_heads* dO, const a
   int rc = validate_sequences(ctx, sequences, total);
   if (rc == ABS_OK) rc = validate_heads(ctx, sequences, total, q_heads, kv_heads, head_dim);
   if (rc != ABS_OK) return rc;
-  if (!(scale > -3.0e38f && scale < 3.0e38f)) return set_error(ctx, ABS_ERR_INVALID_ARG, "scale must be finite");
+  if ((rc = validate_scale(ctx, scale)) != ABS_OK) return rc;
   if (total == 0 || sequences == 0) return ABS_OK;
   if (plan == nullptr || (reinterpret_cast<uintptr_t>(plan) & 15u)) return set_error(ctx, ABS_ERR_INVALID_ARG, "plan is null or not 16-byte aligned");
   if (lse == nullptr) return set_error(ctx, ABS_ERR_INVALID_ARG, "lse is null");

@@ -585,3 +585,16 @@ def test_a_plan_of_another_batch_gives_nan(ctx, hd, dtype, hq, hk, change):
     assert torch.equal(again_o, o) and torch.equal(again_lse, lse)
     for g, want in zip(run_backward(ctx, b, plan, o, lse), grads):
         assert torch.equal(g, want)
+
+
+@pytest.mark.parametrize("scale", [2.5e38, -2.5e38, math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_that_overflow_are_refused(ctx, dtype, scale):
+    """Scores are taken log2 e times in the exponent: a scale that is finite but overflows there would make every row NaN."""
+    b = Batch([3], 2, 1, 64, dtype, seed=42)
+    plan, o, lse = run_forward(ctx, b)
+    b.scale = scale
+    with pytest.raises(pkg.AbsError, match="scale"):
+        run_forward(ctx, b, plan=plan)
+    with pytest.raises(pkg.AbsError, match="scale"):
+        run_backward(ctx, b, plan, o, lse)
