@@ -82,7 +82,8 @@ __device__ int order_tiles(const int* starts, int n, int rows, bool most_first, 
   return carry;
 }
 
-// One CTA.  Forward, the longest tiles first, so that the last ones to start are short.  Backward, the shortest first, because the
+// One CTA, once a batch: 8 us for a few sequences, 10 for 128 of 1024 tokens; sequences of one length take their places one after another
+// (2000 of 64 tokens 89 us, 100000 of one 4.9 ms).  Forward, the longest tiles first, so that the last ones to start are short.  Backward, the shortest first, because the
 // sums of dq pass from the last tile of a sequence to the first.  (Within groups of 16384 to 262144 rows, so that the sums under way
 // stay in L2, 32 x 2048 tokens, 16 heads of 128, took 2510 to 2535 us instead of 2535, and 128 x 1024, 12 heads of 64, as long.)
 __global__ void __launch_bounds__(kPlanThreads)

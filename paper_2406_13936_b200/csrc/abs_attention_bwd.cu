@@ -24,9 +24,11 @@
 // Rounded to fewer bits than 32: P and dS to bf16, as operands of the tensor core, and the results.
 //
 // At 64 columns a head the softmax warps are busiest (1024 clocks of exponentials per 128 x 128 scores and as many of everything else, while
-// five products take 1280), and a block's steps depend on one another: 128 of 1024 tokens, 12 heads of 64, 1.35 to 1.43 ms, 360 to
-// 380 TFLOP/s; 65536 tokens in one 560.  At 128 columns five products take 2560 clocks and the sums of dq, 64 KB a block to L2, about
-// as long: 32768 tokens, 8 heads, 735 TFLOP/s, 32 of 2048, 16 heads, 540.
+// five products take 1280), and a block's steps depend on one another: 128 of 1024 tokens, 12 heads of 64, 1.38 to 1.45 ms, 355 to
+// 375 TFLOP/s; 65536 tokens in one 560.  At 128 columns five products take 2560 clocks and the sums of dq, 64 KB a block to L2, about
+// as long: 32768 tokens, 8 heads, 735 TFLOP/s, 32 of 2048, 16 heads, 540; that kernel spills (264 bytes of stores and 376 of loads a thread,
+// most likely the 64 weights that a softmax thread holds beside as many scores; at 64 columns 8 and 16).  Heads of other widths cost what 64
+// and 128 do: 4 of 4096 tokens, 8 heads and 2 of keys, 32, 64, 80, 96 and 128 columns 330, 341, 561, 573, 598 us.
 //
 // Roles of the 16 warps: 0 takes tiles and loads (TMA), 1 issues the products, 2 and 3 look after the sums, 4-7 take results out of tensor memory,
 // 8-15 are the softmax: 64 of a block's 128 queries each half.  While they compute P' of a block, dQ and dK of the block before and

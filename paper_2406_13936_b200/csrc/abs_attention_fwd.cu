@@ -15,8 +15,11 @@
 // The floor is the exponentials at 64 columns a head (16 a clock and SM: 1024 clocks per 128 x 128 scores, whose products take 512) and
 // both at 128; what bounds it are the softmax warps, two a scheduler, whose steps depend on one another (issue slots 45 % busy): two
 // passes over S from tensor memory, the first for its largest, because 128 scores a thread held in registers spill (672 us for 500).
-// 128 of 1024 tokens, 12 heads of 64: 460 to 500 us (all exponentials on their unit alone 200, products 146 at the sustained rate);
-// 8191 and 4097 tokens, 8 heads of 128 and 2 of keys: 225 us, 760 TFLOP/s.
+// 128 of 1024 tokens, 12 heads of 64: 455 us over the same tensors again and again, 505 over others each time (all exponentials on their
+// unit alone 200, products 146 at the sustained rate); 8191 and 4097 tokens, 8 heads of 128 and 2 of keys: 225 us, 760 TFLOP/s.  A sequence of
+// up to 128 tokens has one half's warps idle (2000 of 64 tokens, 12 heads of 64: 480 us), half 0 of a tile has a step less than half 1, and
+// heads of other widths than 64 and 128 cost what these do (4 of 4096 tokens, 8 heads and 2 of keys, 32, 64, 80, 96 and 128 columns: 146,
+// 147, 160, 160, 161 us).
 //
 // Roles of the 12 warps: 0 loads (TMA; Q once a tile, K and V through a ring of 128-row places), 1 issues the products, 4-7 and 8-11
 // are the two halves.  All waits are bounded: one that runs out raises the CTA's abort flag, every role falls through, copies in

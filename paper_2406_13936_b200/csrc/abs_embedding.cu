@@ -6,7 +6,8 @@
 // The gradient's sums must not depend on the order of atomics, so the tokens are sorted (stable, so that a token's places are in
 // order) and every row of dE is summed by one group of threads, or, where a token's places cross from one run of the sorted
 // list to the next, from the runs' partial sums in order.  8 x 16384 tokens, 50000 rows of 768, bf16: 68 us forward, 266 backward (5.1 and
-// 5.4 TB/s of what has to move).
+// 5.4 TB/s of what has to move).  Rows that are not whole 16-byte pieces are taken in single elements: 4 x 16384 tokens, 50000 rows of
+// 766 for 768, bf16 149 us for 35 forward and 325 for 153 backward, fp32 148 for 53 and 328 for 172.
 #include "abs_pipeline.cuh"
 
 namespace absk {

@@ -4,8 +4,8 @@
 //   xh = h rstd,  a = w dy,  dx = dh + rstd (a - xh mean(a xh)),  dw = sum_rows dy xh
 //
 // Each pass must read its inputs and write its outputs once; the arithmetic (5 and 9 operations an element) is far below
-// what the memory rate leaves time for.  8 x 16384 x 768 bf16 with the residual: 128 us forward, 130 backward, 6.3 and 6.2 TB/s; 4099 x 4096
-// bf16 to 8 bits 17 us.  Through the kernels for any width 471, 596 and 70.
+// what the memory rate leaves time for.  8 x 16384 x 768 bf16 with the residual: 128 us forward, 131 backward, 6.3 and 6.2 TB/s; fp32 239 and
+// 327; 4099 x 4096 bf16 to 8 bits 18 us.  Through the kernels for any width 471, 596 and 70 (bf16).
 #include <cuda_fp8.h>
 
 #include "abs_tc.cuh"
@@ -480,7 +480,9 @@ rms_forward_kernel(const RmsForward a, int tpr, int pieces) {
 }
 
 // ---- rows through a ring in shared memory ------------------------------------------------------------------------
-// Backward, rows of aligned pieces: a thread copies its own pieces of the rows ahead into its own places of a ring (cp.async), so what is
+// Backward, rows of whole 16-byte pieces up to 4096 fp32 or 8192 bf16 columns (200 KB of ring); all others go through the kernels for any
+// width, which read them twice or thrice in single elements (16384 x 1020 bf16 91 us, 1024 columns 42; 2000 x 8192 fp32 130 us, the memory
+// rate allows 30).  A thread copies its own pieces of the rows ahead into its own places of a ring (cp.async), so what is
 // under way does not depend on registers and nobody waits for anybody else's copies.  A CTA has a piece of a segment and its groups take
 // the rows in turn, the sums of dw staying in registers; or (by_group) every group has a segment of its own.
 constexpr int kDeep = 4;                             // rows of a group's ring
@@ -735,7 +737,10 @@ int launch_forward(abs_ctx* ctx, const RmsForward& a, int tpr, cudaStream_t st) 
   ABS_CUDA_TRY(ctx, launch_dependent(kern, dim3(static_cast<unsigned>(grid)), dim3(tpr * groups), 0, st, a, tpr, a.d / V));
   return ABS_OK;
 }
-// 32 elements a thread at most: what 64 registers leave room for.
+// 32 elements a thread at most, 16 single ones.  Row, residual and sum are all held: bf16 pieces of 16 and 8 bytes fit 64 registers; rows of
+// 32 fp32 elements a thread, in pieces of 16 and 8 bytes, spill 100 to 148 bytes, the other full rows up to 56 (16384 x 4096 fp32 122 us, 210 with
+// the residual, of 82 and 164 that the memory rate allows).  Rows of 16384 x 1020, 1022 and 1021 bf16, pieces of 8, 4 and 2 bytes: 18, 31, 53 us
+// for 15 at 1024.
 template <typename T, int V>
 int run_pieces(abs_ctx* ctx, const RmsForward& a, cudaStream_t st) {
   const int tpr = threads_of(a.d / V, 32 / V > 16 ? 16 : 32 / V), nv = (a.d / V + tpr - 1) / tpr;
